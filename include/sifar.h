@@ -379,6 +379,145 @@ size_t sifar_noalloc_max_elems(void);
  */
 int sifar_noalloc_counters(unsigned long long out[3]);
 
+/*
+ * What a transformer layer does at its all-reduce.  The paper has no counterpart for these four calls; the layer it
+ * describes (two all-reduces, Section 2) has them directly behind each.  Like sifar_allreduce_noalloc they read P
+ * caller-owned plain partials (1 <= P <= 8) that are complete in the order of `stream`, sum them in rank order in
+ * binary32, take no context and allocate nothing; unlike it they round nothing but what they store, once.
+ *
+ * Common rules.
+ *   - One argument block per call, read before the call returns (a program may keep one per layer and pass it again).
+ *     Unused pointers are NULL.  Everything is launched on the CURRENT device and on `stream`; nothing synchronizes.
+ *   - `rows` x `cols` arrays have a row stride ld_* in elements, at least cols; 0 stands for cols.  Addresses need the
+ *     alignment of their element type.  Where the bases and strides of all row arrays are multiples of 16 bytes (and
+ *     those of the weights too) the kernels move 16 bytes per access, otherwise single elements.
+ *   - An output may overlap nothing else, except as stated.  Arrays that share a buffer column by column (same stride,
+ *     disjoint columns) do not overlap.
+ *   - SIFAR_ERR_INVALID: nothing was launched.  rows = 0 (tokens = 0) is valid: no row is read or written; gradients
+ *     summed over the rows become 0.
+ *   - The first call of each kind on a device loads its kernel; make it before a stream capture begins and while no
+ *     kernel waits for another.  Captured calls keep the argument block's addresses.
+ *   - Results do not depend on what else runs: sums over a row or over rows have a fixed order.
+ */
+
+/* Largest hidden size of sifar_block_norm and its backward pass. */
+enum { SIFAR_NORM_MAX_COLS = 32768 };
+
+/*
+ * The sum of P partials with the norms, gate and residual scale around a block, per row of `cols` elements:
+ *     z = x_0 + x_1 + ... + x_{P-1}                                (binary32, rank order, as in sifar_allreduce)
+ *     u = z * r1 * (post_weight + weight_offset)                   r1 = 1 / sqrt(mean(z^2) + eps)       (post_norm)
+ *     u = z                                                                                         (no post_norm)
+ *     h = alpha * residual + beta * gate * u
+ *     y = h * r2 * (pre_weight + weight_offset)                    r2 = 1 / sqrt(mean(h^2) + eps)        (pre_norm)
+ * all in binary32; y is computed from h before h is rounded.
+ */
+typedef struct {
+    const void *x[SIFAR_MAX_RANKS];   /* P partials, rows x cols                                                     */
+    const void *residual;             /* rows x cols, or NULL: 0                                                     */
+    const void *post_weight;          /* cols, or NULL: a factor of 1 (without weight_offset)                        */
+    const void *gate;                 /* ceil(rows / rows_per_gate) x cols, or NULL: 1                               */
+    const void *pre_weight;           /* cols, or NULL: a factor of 1                                                */
+    void *z;                          /* rows x cols, or NULL: the plain sum, bit for bit that of sifar_allreduce    */
+    void *h;                          /* rows x cols, or NULL; may be `residual` itself (same address and stride)    */
+    void *y;                          /* rows x cols with pre_norm (or NULL), NULL without                           */
+    float *stats;                     /* 2 x rows, or NULL: r1 of every row, then r2 of every row; 1 where no norm   */
+    size_t rows, cols;                /* cols: 1 .. SIFAR_NORM_MAX_COLS                                              */
+    size_t ld_x, ld_residual, ld_gate, ld_z, ld_h, ld_y;
+    size_t rows_per_gate;             /* that many consecutive rows share a gate row; 0: all of them                 */
+    float alpha, beta, eps, weight_offset;
+    int P, dtype, post_norm, pre_norm;/* dtype (of all row and weight arrays): SIFAR_BF16 or SIFAR_F32               */
+} sifar_block_norm_args;
+
+/* At least one of z, h, y must be given. */
+int sifar_block_norm(const sifar_block_norm_args *args, void *stream);
+
+/*
+ * Its backward pass.  With h, z and stats as the forward pass stored them, dh the gradient of h by its other uses and
+ * dy_r the P partials of the gradient of y (a column-parallel layer leaves one per rank):
+ *     G = dy_0 + ... + dy_{P-1};   n2 = h * r2;   a = G * (pre_weight + weight_offset)
+ *     D = dh + r2 * (a - n2 * mean(a * n2))                                        dpre_weight  = sum over rows of G * n2
+ *     dresidual = alpha * D
+ *     n1 = z * r1;   u = n1 * (post_weight + weight_offset);   d = beta * gate * D
+ *                                         dgate = sum over the rows of a gate row of beta * D * u
+ *     b = d * (post_weight + weight_offset);   dx = r1 * (b - n1 * mean(b * n1))   dpost_weight = sum over rows of d * n1
+ * Without post_norm u = z and dx = d; without pre_norm D = dh.  dx is the gradient of every partial x_r.
+ */
+typedef struct {
+    const void *dy[SIFAR_MAX_RANKS];  /* with pre_norm: P partials, rows x cols                                      */
+    const void *dh;                   /* rows x cols, or NULL: 0 (not without pre_norm)                              */
+    const void *h;                    /* rows x cols, with pre_norm                                                  */
+    const void *z;                    /* rows x cols, with post_norm or where dgate is asked for                     */
+    const float *stats;               /* 2 x rows, with post_norm or pre_norm                                        */
+    const void *post_weight, *gate, *pre_weight;                     /* as in the forward pass                       */
+    void *dx, *dresidual;             /* rows x cols, each may be NULL; dresidual may be dh itself                   */
+    float *dpost_weight, *dpre_weight;/* cols, binary32, each may be NULL; overwritten                               */
+    float *dgate;                     /* ceil(rows / rows_per_gate) x cols, binary32, contiguous, or NULL            */
+    void *workspace;                  /* 16-byte aligned, for this call alone until it has run                       */
+    size_t workspace_bytes;           /* at least sifar_block_norm_backward_workspace(args)                          */
+    size_t rows, cols;
+    size_t ld_dy, ld_dh, ld_h, ld_z, ld_gate, ld_dx, ld_dresidual;
+    size_t rows_per_gate;
+    float alpha, beta, weight_offset;
+    int P, dtype, post_norm, pre_norm;/* P is not looked at without pre_norm                                         */
+} sifar_block_norm_grad_args;
+
+/* Bytes of workspace for these sizes (pure function; 0 if no gradient over rows is asked for or the sizes are refused). */
+size_t sifar_block_norm_backward_workspace(const sifar_block_norm_grad_args *args);
+int sifar_block_norm_backward(const sifar_block_norm_grad_args *args, void *stream);
+
+/*
+ * The choice of experts.  Per token, over `experts` logits:
+ *     l = logits_0 + ... + logits_{P-1}            (binary32, rank order: a router whose input is split over ranks)
+ *     s = softmax(l) or sigmoid(l)
+ *     v = s + bias                                 (the bias decides the choice and does not enter the weights)
+ *     groups > 1: the experts lie in `groups` equal runs; the top_groups runs with the largest group value stay in:
+ *         SIFAR_GROUP_MAX  the largest v of the run,  SIFAR_GROUP_TOP2  the sum of its two largest
+ *     indices = the top_k experts by v, largest first
+ *     weights = scale * s of the chosen, divided by the sum of the chosen s if `renormalize`
+ * Choices are made as in exact arithmetic up to binary64: v is compared in binary64 where a bias or a sum of two
+ * enters, else by the logits themselves.  Equal values go to the lower index (of the expert, of the group).  NaN
+ * counts as the lowest value, as -infinity does; it stays NaN in the weights.  A logit of -infinity closes an expert:
+ * its weight is 0, and it is chosen only where too few others are left (with a bias the choice goes by v, and a bias
+ * of -infinity closes the expert).  A token whose chosen experts (softmax without renormalize: all of whose experts)
+ * have logits of -infinity has weights 0.
+ */
+enum { SIFAR_SCORE_SOFTMAX = 0, SIFAR_SCORE_SIGMOID = 1 };
+enum { SIFAR_GROUP_MAX = 0, SIFAR_GROUP_TOP2 = 1 };
+enum { SIFAR_ROUTE_MAX_EXPERTS = 1024, SIFAR_ROUTE_MAX_TOP_K = 32, SIFAR_ROUTE_MAX_GROUPS = 32 };
+
+typedef struct {
+    const void *logits[SIFAR_MAX_RANKS];  /* P partials, tokens x experts                                            */
+    const float *bias;                    /* experts, or NULL: 0                                                     */
+    int *indices;                         /* tokens x top_k, contiguous                                              */
+    float *weights;                       /* tokens x top_k, contiguous                                              */
+    size_t tokens, ld_logits;
+    float scale;
+    int P, dtype;                         /* dtype of the logits                                                     */
+    int experts, top_k;                   /* top_k <= top_groups * (experts / groups)                                */
+    int groups, top_groups, group_score;  /* groups divides experts; groups = 1: top_groups = 1                      */
+    int score, renormalize;
+} sifar_route_args;
+
+int sifar_route(const sifar_route_args *args, void *stream);
+
+/*
+ * Its backward pass: the gradient of every partial logits_r from that of the weights, at the indices that sifar_route
+ * chose.  The choice itself and the bias have no gradient.  An index outside 0 .. experts - 1 marks a choice that was
+ * dropped: it has no score and no gradient.
+ */
+typedef struct {
+    const void *logits[SIFAR_MAX_RANKS];
+    const int *indices;                   /* tokens x top_k                                                          */
+    const float *dweights;                /* tokens x top_k                                                          */
+    void *dlogits;                        /* tokens x experts, of the logits' type; every element is written         */
+    size_t tokens, ld_logits, ld_dlogits;
+    float scale;
+    int P, dtype, experts, top_k, score, renormalize;
+} sifar_route_grad_args;
+
+int sifar_route_backward(const sifar_route_grad_args *args, void *stream);
+
 /* Geometry helpers (no device work). */
 size_t sifar_slot_count(int dtype, size_t n);          /* slots needed for n elements  */
 size_t sifar_algorithmic_bytes(int P, int dtype, size_t n, int mode);  /* bytes the method must move per call:

@@ -63,6 +63,11 @@ def lib() -> ctypes.CDLL:
             "sifar_allreduce_noalloc": (ci, [vp, ci, vp, sz, ci, vp]),
             "sifar_noalloc_max_elems": (sz, []),
             "sifar_noalloc_counters": (ci, [ctypes.POINTER(ctypes.c_ulonglong)]),
+            "sifar_block_norm": (ci, [vp, vp]),
+            "sifar_block_norm_backward": (ci, [vp, vp]),
+            "sifar_block_norm_backward_workspace": (sz, [vp]),
+            "sifar_route": (ci, [vp, vp]),
+            "sifar_route_backward": (ci, [vp, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -194,6 +199,95 @@ def sifar_noalloc_counters() -> dict:
     buf = (ctypes.c_ulonglong * 3)()
     _check(lib().sifar_noalloc_counters(buf))
     return {"cta_arrive": int(buf[0]), "calls": int(buf[1]), "elements": int(buf[2])}
+
+
+# ---------------------------------------------------------------------------
+# what a transformer layer does at its all-reduce: norms, gate and residual, the choice of experts (see include/sifar.h)
+# ---------------------------------------------------------------------------
+MAX_RANKS = 8
+NORM_MAX_COLS = 32768
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_TOP2 = 0, 1
+ROUTE_MAX_EXPERTS, ROUTE_MAX_TOP_K, ROUTE_MAX_GROUPS = 1024, 32, 32
+
+
+def _struct(name: str, **groups: str) -> type:
+    """A ctypes structure from the names of its fields, by type, in the header's order."""
+    kinds = {"ranks": ctypes.c_void_p * MAX_RANKS, "ptr": ctypes.c_void_p, "size": ctypes.c_size_t,
+             "float": ctypes.c_float, "int": ctypes.c_int}
+    fields = [(f, kinds[kind.rstrip("_")]) for kind, names in groups.items() for f in names.split()]
+    return type(name, (ctypes.Structure,), {"_fields_": fields})
+
+
+sifar_block_norm_args = _struct(
+    "sifar_block_norm_args", ranks="x", ptr="residual post_weight gate pre_weight z h y stats",
+    size="rows cols ld_x ld_residual ld_gate ld_z ld_h ld_y rows_per_gate", float="alpha beta eps weight_offset",
+    int="P dtype post_norm pre_norm")
+sifar_block_norm_grad_args = _struct(
+    "sifar_block_norm_grad_args", ranks="dy",
+    ptr="dh h z stats post_weight gate pre_weight dx dresidual dpost_weight dpre_weight dgate workspace",
+    size="workspace_bytes rows cols ld_dy ld_dh ld_h ld_z ld_gate ld_dx ld_dresidual rows_per_gate",
+    float="alpha beta weight_offset", int="P dtype post_norm pre_norm")
+sifar_route_args = _struct(
+    "sifar_route_args", ranks="logits", ptr="bias indices weights", size="tokens ld_logits", float="scale",
+    int="P dtype experts top_k groups top_groups group_score score renormalize")
+sifar_route_grad_args = _struct(
+    "sifar_route_grad_args", ranks="logits", ptr="indices dweights dlogits", size="tokens ld_logits ld_dlogits",
+    float="scale", int="P dtype experts top_k score renormalize")
+
+
+def _ranks(ptrs) -> ctypes.Array:
+    if len(ptrs) > MAX_RANKS:
+        raise SifarError(ERR_INVALID, f"{len(ptrs)} partials: at most {MAX_RANKS} ranks")
+    return (ctypes.c_void_p * MAX_RANKS)(*ptrs)
+
+
+def make_block_norm(x, *, rows: int, cols: int, dtype: int, alpha: float = 1.0, beta: float = 1.0, eps: float = 1e-6,
+                    **fields) -> sifar_block_norm_args:
+    """Argument block of sifar_block_norm: `x` the P partials' addresses, `fields` as in the header, absent ones 0."""
+    return sifar_block_norm_args(x=_ranks(x), P=len(x), rows=rows, cols=cols, dtype=dtype, alpha=alpha, beta=beta,
+                                 eps=eps, **fields)
+
+
+def make_block_norm_grad(dy, *, rows: int, cols: int, dtype: int, alpha: float = 1.0, beta: float = 1.0,
+                         **fields) -> sifar_block_norm_grad_args:
+    """Argument block of sifar_block_norm_backward: `dy` the P partials' addresses (none without pre_norm)."""
+    return sifar_block_norm_grad_args(dy=_ranks(dy), P=len(dy), rows=rows, cols=cols, dtype=dtype, alpha=alpha,
+                                      beta=beta, **fields)
+
+
+def make_route(logits, *, tokens: int, experts: int, top_k: int, dtype: int, scale: float = 1.0, groups: int = 1,
+               top_groups: int = 1, **fields) -> sifar_route_args:
+    """Argument block of sifar_route: `logits` the P partials' addresses."""
+    return sifar_route_args(logits=_ranks(logits), P=len(logits), tokens=tokens, experts=experts, top_k=top_k,
+                            dtype=dtype, scale=scale, groups=groups, top_groups=top_groups, **fields)
+
+
+def make_route_grad(logits, *, tokens: int, experts: int, top_k: int, dtype: int, scale: float = 1.0,
+                    **fields) -> sifar_route_grad_args:
+    """Argument block of sifar_route_backward."""
+    return sifar_route_grad_args(logits=_ranks(logits), P=len(logits), tokens=tokens, experts=experts, top_k=top_k,
+                                 dtype=dtype, scale=scale, **fields)
+
+
+def sifar_block_norm(args: sifar_block_norm_args, stream: int = 0) -> int:
+    return _check(lib().sifar_block_norm(ctypes.byref(args), stream))
+
+
+def sifar_block_norm_backward(args: sifar_block_norm_grad_args, stream: int = 0) -> int:
+    return _check(lib().sifar_block_norm_backward(ctypes.byref(args), stream))
+
+
+def sifar_block_norm_backward_workspace(args: sifar_block_norm_grad_args) -> int:
+    return lib().sifar_block_norm_backward_workspace(ctypes.byref(args))
+
+
+def sifar_route(args: sifar_route_args, stream: int = 0) -> int:
+    return _check(lib().sifar_route(ctypes.byref(args), stream))
+
+
+def sifar_route_backward(args: sifar_route_grad_args, stream: int = 0) -> int:
+    return _check(lib().sifar_route_backward(ctypes.byref(args), stream))
 
 
 # ---------------------------------------------------------------------------

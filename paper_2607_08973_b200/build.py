@@ -1,7 +1,8 @@
 """Builds the two CUDA libraries (sm_100a) in-tree with nvcc.
 
 ``libsifar.so``        the all-reduce itself: context, producer-side store path,
-                       reducer kernels, the allocation-free entry point
+                       reducer kernels, the allocation-free entry point, the norms
+                       and the routing behind an all-reduce
                        (``include/sifar.h``).
 ``libsifar_bench.so``  the synthetic decode-step chains, generator probes and
                        measurement helpers (``include/sifar_workload.h``); it
@@ -33,7 +34,8 @@ LIB_BENCH = os.path.join(PKG, "libsifar_bench.so")
 LIB_S8X2 = os.path.join(PKG, "libsifar_s8x2.so")
 
 # which translation units go into which library
-CORE_UNITS = ("sifar_core", "sifar_noalloc")
+CORE_UNITS = ("sifar_core", "sifar_noalloc", "sifar_norm", "sifar_norm_grad", "sifar_route")
+SLOT_UNITS = ("sifar_core", "sifar_noalloc")          # ... and know the slot format: built a second time for it
 BENCH_UNITS = ("sifar_workload", "sifar_symmetric", "sifar_chain_cluster", "sifar_chain_pipe")
 
 NVCC_FLAGS = [
@@ -90,10 +92,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if unknown:
         raise RuntimeError(f"csrc/{unknown[0]}.cu is assigned to neither library (see build.py)")
     os.makedirs(OBJ, exist_ok=True)
-    jobs = [(u, "") for u in units] + [(u, "s8x2") for u in CORE_UNITS]
+    jobs = [(u, "") for u in units] + [(u, "s8x2") for u in SLOT_UNITS]
     with ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 1)) as pool:
         objs = dict(zip(jobs, pool.map(lambda j: _compile(j[0], force, verbose, j[1]), jobs)))
-    fallback = [objs[(u, "s8x2")] for u in CORE_UNITS]
+    fallback = [objs[(u, "s8x2" if u in SLOT_UNITS else "")] for u in CORE_UNITS]
     objs = {u: objs[(u, "")] for u in units}
     _link(LIB_S8X2, fallback, ["-Xlinker", "-soname=libsifar_s8x2.so"])
     _link(LIB, [objs[u] for u in CORE_UNITS], ["-Xlinker", "-soname=libsifar.so"])
