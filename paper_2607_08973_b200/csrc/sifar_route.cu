@@ -18,6 +18,7 @@ struct RouteArgs {
     unsigned long long tokens, ld_logits;    /* bytes between two tokens */
     float scale;
     int P, experts, top_k, groups, top_groups, group_score, score, renormalize;
+    uint32_t per_magic;                      /* ceil(2^20 / experts of a group): e / per = e * per_magic >> 20 for e, per < 2^10 */
 };
 
 struct RouteGradArgs {
@@ -44,23 +45,69 @@ __device__ __forceinline__ double warp_sum(double v)
     return v;
 }
 
-/* l[j] = the rank-order sum of the logits of expert 32 j + lane; -infinity behind the last expert. */
+/* l[j] = the rank-order sum of the logits of expert 32 j + lane; -infinity behind the last expert.  The loads of
+   several ranks are under way together. */
 template <int DT, int NI>
 __device__ __forceinline__ void load_logits(float (&l)[NI], const void *const *logits, int P, unsigned long long at, int experts)
 {
     using T = typename Elem<DT>::type;
+    constexpr int B = NI <= 4 ? 8 : NI <= 8 ? 4 : NI <= 16 ? 2 : 1;
     const int lane = threadIdx.x & 31;
-    T w[NI];
-    for (int r = 0; r < P; ++r) {
-        const T *p = reinterpret_cast<const T *>(static_cast<const char *>(logits[r]) + at);
+    for (int r0 = 0; r0 < P; r0 += B) {
+        T w[B][NI];
 #pragma unroll
-        for (int j = 0; j < NI; ++j) w[j] = j * 32 + lane < experts ? p[j * 32 + lane] : (T)0;
+        for (int b = 0; b < B; ++b) {
+            if (r0 + b >= P) break;
+            const T *p = reinterpret_cast<const T *>(static_cast<const char *>(logits[r0 + b]) + at);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) l[j] = r == 0 ? widen<DT>(w[j]) : __fadd_rn(l[j], widen<DT>(w[j]));
+            for (int j = 0; j < NI; ++j) w[b][j] = j * 32 + lane < experts ? p[j * 32 + lane] : (T)0;
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            if (r0 + b >= P) break;
+#pragma unroll
+            for (int j = 0; j < NI; ++j) l[j] = r0 + b == 0 ? widen<DT>(w[b][j]) : __fadd_rn(l[j], widen<DT>(w[b][j]));
+        }
     }
 #pragma unroll
     for (int j = 0; j < NI; ++j)
         if (j * 32 + lane >= experts) l[j] = -INFINITY;
+}
+
+/*
+ * Keys: unsigned words that compare as the values do, 0 below all of them.  NaN is as low as -infinity, -0 is 0.
+ */
+__device__ __forceinline__ uint32_t key_of(float v)
+{
+    const uint32_t u = __float_as_uint(v != v ? -INFINITY : v + 0.0f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_key(uint32_t k)
+{
+    return __uint_as_float(k ^ ((uint32_t)((int32_t)~k >> 31) | 0x80000000u));
+}
+__device__ __forceinline__ unsigned long long key_of(double v)
+{
+    const long long u = __double_as_longlong(v != v ? -INFINITY : v + 0.0);
+    return (unsigned long long)(u ^ ((u >> 63) | (long long)0x8000000000000000ull));
+}
+
+/* Keys of a lane, largest first: Batcher's odd-even merge exchange. */
+template <int N> __device__ __forceinline__ void sort_keys(uint32_t (&k)[N])
+{
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+            for (int j = q % p; j + q < N; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < (q < N - j - q ? q : N - j - q); ++i)
+                    if ((i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+                        const uint32_t hi = max(k[i + j], k[i + j + q]), lo = min(k[i + j], k[i + j + q]);
+                        k[i + j] = hi;
+                        k[i + j + q] = lo;
+                    }
 }
 
 __device__ __forceinline__ double lowest(double v) { return v != v ? -INFINITY : v; }
@@ -85,112 +132,255 @@ __device__ __forceinline__ float scaled_sigmoid(float l, float max)
     return max < 0.0f ? expf(l - max) / (1.0f + expf(l)) : sigmoid(l);
 }
 
+/* The lanes of a group when a warp looks at all groups: group lane / step, step lanes each. */
+__device__ __forceinline__ int lanes_per_group(int groups) { return 32 >> (groups > 1 ? 32 - __clz(groups - 1) : 0); }
+
+/* The value of the lane's group: the largest of `v`'s run, or the sum of its two largest. */
+template <typename F> __device__ __forceinline__ F group_value(const F *v, int per, int groups, int step, bool top2)
+{
+    const int lane = threadIdx.x & 31, g = lane / step;
+    F m1 = -INFINITY, m2 = -INFINITY;
+    if (g < groups)
+        for (int i = lane % step; i < per; i += step) {
+            const F x = v[g * per + i];
+            m2 = max(m2, min(m1, x));
+            m1 = max(m1, x);
+        }
+    for (int d = step / 2; d > 0; d >>= 1) {
+        const F o1 = __shfl_xor_sync(0xFFFFFFFFu, m1, d), o2 = __shfl_xor_sync(0xFFFFFFFFu, m2, d);
+        m2 = max(max(m2, o2), min(m1, o1));
+        m1 = max(m1, o1);
+    }
+    if (!top2 || per == 1) return m1;
+    const F sum = m1 + m2;
+    return sum != sum ? (F)-INFINITY : sum;
+}
+
+/* Whether the lane's group is among the best. */
+template <typename F> __device__ __forceinline__ bool group_open(F mine, int groups, int step, int top_groups)
+{
+    const int g = (threadIdx.x & 31) / step;
+    int better = 0;
+    for (int i = 0; i < groups; ++i) {
+        const F o = __shfl_sync(0xFFFFFFFFu, mine, i * step);
+        better += (o > mine || (o == mine && i < g)) ? 1 : 0;
+    }
+    return g < groups && better < top_groups;
+}
+
+/*
+ * The choice in binary64, from the logits in shared memory: for the tokens of which binary32 cannot tell.
+ * Lane i returns choice i.
+ */
+template <int NI>
+__device__ __noinline__ int choose_exactly(const RouteArgs &a, const float *l, double *v, float top)
+{
+    const int lane = threadIdx.x & 31;
+    const bool by_value = a.bias != nullptr, top2 = a.groups > 1 && a.group_score == SIFAR_GROUP_TOP2;
+    double total = 1.0;
+    if ((by_value || top2) && a.score == SIFAR_SCORE_SOFTMAX) {
+        total = 0.0;
+        for (int e = lane; e < a.experts; e += 32) total += exp((double)l[e] - (double)top);
+        total = warp_sum(total);
+    }
+    for (int e = lane; e < a.experts; e += 32) {
+        double x = (double)l[e];
+        if (by_value || top2) {
+            x = a.score == SIFAR_SCORE_SIGMOID ? sigmoid(x) : top == -INFINITY ? 0.0 : exp(x - (double)top) / total;
+            if (by_value) x += (double)a.bias[e];
+        }
+        v[e] = lowest(x);
+    }
+    __syncwarp();
+    uint32_t open = 0xFFFFFFFFu;
+    int step = 1;
+    if (a.groups > 1) {
+        step = lanes_per_group(a.groups);
+        const double mine = group_value(v, a.experts / a.groups, a.groups, step, top2);
+        open = __ballot_sync(0xFFFFFFFFu, group_open(mine, a.groups, step, a.top_groups));
+    }
+    uint32_t closed = 0u;
+#pragma unroll 1
+    for (int j = 0; j < NI; ++j) {
+        const int e = j * 32 + lane;
+        if (e >= a.experts || (a.groups > 1 && !(open >> (e / (a.experts / a.groups)) * step & 1u))) closed |= 1u << j;
+    }
+    int chosen = 0;
+    for (int i = 0; i < a.top_k; ++i) {
+        unsigned long long best = 0ull;
+        uint32_t be = 0xFFFFFFFFu;
+#pragma unroll 1
+        for (int j = 0; j < NI; ++j) {
+            if (closed >> j & 1u) continue;
+            const int e = j * 32 + lane;
+            const unsigned long long k = key_of(by_value ? v[e] : (double)l[e]);
+            if (k > best) { best = k; be = (uint32_t)e; }
+        }
+        const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(best >> 32));
+        if ((uint32_t)(best >> 32) != hi) be = 0xFFFFFFFFu;
+        const uint32_t lo = __reduce_max_sync(0xFFFFFFFFu, be != 0xFFFFFFFFu ? (uint32_t)best : 0u);
+        if ((uint32_t)best != lo) be = 0xFFFFFFFFu;
+        be = __reduce_min_sync(0xFFFFFFFFu, be);
+        if ((int)(be & 31u) == lane) closed |= 1u << (be >> 5);
+        if (lane == i) chosen = (int)be;
+    }
+    return chosen;
+}
+
+/*
+ * The choice goes by keys of binary32 values whose lowest bits are the item's number, so that a key says where it came
+ * from and equal values come in the order of the experts.  A lane sorts its keys once; a round then takes the largest
+ * head of the 32 lists (one reduction over the warp, one ballot).
+ *
+ * What binary32 and the cut bits may hide is looked at afterwards: where two neighbours of the chosen, or the last of
+ * them and the best that is left, lie closer than the error of both and are not equal by their inputs, the token is
+ * chosen again in binary64 (choose_exactly).  Logits that are compared themselves have no error but the cut bits.
+ */
 template <int DT, int NI>
 __global__ void __launch_bounds__(32 * kRouteWarps) k_route(const RouteArgs a)
 {
+    __shared__ float s_l[kRouteWarps][NI * 32];
+    __shared__ double s_v[kRouteWarps][NI * 32];
     grid_let_next_in();
     const int lane = threadIdx.x & 31;
     const unsigned long long token = (unsigned long long)blockIdx.x * kRouteWarps + threadIdx.x / 32;
     grid_wait();
     if (token >= a.tokens) return;
-    float l[NI];
+    float l[NI], *const sl = s_l[threadIdx.x / 32];
+    double *const sv = s_v[threadIdx.x / 32];
     load_logits<DT, NI>(l, a.logits, a.P, token * a.ld_logits, a.experts);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) sl[j * 32 + lane] = l[j];
 
-    float top = -INFINITY, sum = 0.0f;                    /* of the softmax over all experts */
-    const bool whole_softmax = a.score == SIFAR_SCORE_SOFTMAX && (!a.renormalize || a.bias || a.groups > 1);
-    if (whole_softmax) {
+    const bool by_value = a.bias != nullptr, top2 = a.groups > 1 && a.group_score == SIFAR_GROUP_TOP2;
+    const bool softmax = a.score == SIFAR_SCORE_SOFTMAX;
+    float top = -INFINITY, sum = 1.0f;                    /* of the softmax over all experts */
+    if (softmax && (!a.renormalize || by_value || top2)) {
         bool nan = false;
 #pragma unroll
         for (int j = 0; j < NI; ++j) { top = fmaxf(top, l[j]); nan = nan || l[j] != l[j]; }
         top = warp_max(top);
         if (__any_sync(0xFFFFFFFFu, nan)) top = NAN;
+        if (top != -INFINITY) {
+            sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < NI; ++j) sum += expf(l[j] - top);
-        if (top == -INFINITY) sum = 1.0f;
-        else sum = sifar::warp_sum(sum);
+            for (int j = 0; j < NI; ++j) sum += expf(l[j] - top);
+            sum = sifar::warp_sum(sum);
+        }
     }
 
-    /* what is compared: v in binary64, or the logits */
-    double v[NI];
-    const bool by_value = a.bias != nullptr, top2 = a.groups > 1 && a.group_score == SIFAR_GROUP_TOP2;
+    /* what is compared, and its error: `fixed`, and `relative` times its size, both for a pair */
+    float v[NI], fixed = 0.0f, relative = 0.0f;
+    bool unsure = false;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) v[j] = l[j];
     if (by_value || top2) {
-        double total = 0.0;
-        if (a.score == SIFAR_SCORE_SOFTMAX) {
+        if (softmax) {
+            /* l - top, expf, the sum's NI + 5 adds, the division: of a score of at most 1 / sum */
+            const float inv = top == -INFINITY ? 0.0f : 1.0f / sum;
+            fixed = 2.5f * (NI + 16) * 0x1p-24f * inv;
 #pragma unroll
-            for (int j = 0; j < NI; ++j) { v[j] = exp((double)l[j] - (double)top); total += v[j]; }
-            total = warp_sum(total);
-        }
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            v[j] = a.score == SIFAR_SCORE_SOFTMAX ? (top == -INFINITY ? 0.0 : v[j] / total) : sigmoid((double)l[j]);
-            if (by_value && j * 32 + lane < a.experts) v[j] += (double)a.bias[j * 32 + lane];
-            v[j] = lowest(v[j]);
-        }
-    }
-    uint32_t closed = 0u;                                 /* bit j: item j cannot be chosen (any more) */
-#pragma unroll
-    for (int j = 0; j < NI; ++j)
-        if (j * 32 + lane >= a.experts) closed |= 1u << j;
-
-    if (a.groups > 1) {
-        const int per = a.experts / a.groups;
-        double mine = -INFINITY;                          /* lane g: the value of group g */
-        for (int g = 0; g < a.groups; ++g) {
-            double m1 = -INFINITY, m2 = -INFINITY;
+            for (int j = 0; j < NI; ++j) v[j] = top == -INFINITY ? 0.0f : __expf(l[j] - top) * inv;
+            fixed += 2.5f * 0x1p-21f * inv;               /* ... __expf for expf: two steps and the argument's product */
+        } else {
+            /* __expf: two steps and the argument's product, |l| exp(-|l|) <= 0.37 steps; the reciprocal: one step */
+            fixed = 2.5f * 0x1p-21f;
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const int e = j * 32 + lane;
-                if (e >= g * per && e < (g + 1) * per) {
-                    const double x = by_value || top2 ? v[j] : lowest((double)l[j]);
-                    m2 = fmax(m2, fmin(m1, x));
-                    m1 = fmax(m1, x);
-                }
+                const float t = __expf(-fabsf(l[j]));
+                v[j] = __fdividef(l[j] < 0.0f ? t : 1.0f, 1.0f + t);
             }
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) {
-                const double o1 = __shfl_xor_sync(0xFFFFFFFFu, m1, d), o2 = __shfl_xor_sync(0xFFFFFFFFu, m2, d);
-                m2 = fmax(fmax(m2, o2), fmin(m1, o1));
-                m1 = fmax(m1, o1);
-            }
-            const double value = top2 && per > 1 ? lowest(m1 + m2) : m1;
-            if (lane == g) mine = value;
         }
-        int better = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const double o = __shfl_sync(0xFFFFFFFFu, mine, g);
-            better += (o > mine || (o == mine && g < lane)) ? 1 : 0;
-        }
-        const uint32_t open = __ballot_sync(0xFFFFFFFFu, lane < a.groups && better < a.top_groups);
+        relative = 2.5f * 0x1p-24f + 1.25f * NI * 0x1p-23f;
+        if (by_value) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const int e = j * 32 + lane;
-            if (e < a.experts && !(open >> (e / per) & 1u)) closed |= 1u << j;
+            for (int j = 0; j < NI; ++j)
+                if (j * 32 + lane < a.experts) v[j] += a.bias[j * 32 + lane];
+        }
+        bool nan = false;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) nan = nan || (j * 32 + lane < a.experts && v[j] != v[j]);
+        unsure = __any_sync(0xFFFFFFFFu, nan);
+    }
+    uint32_t open = 0xFFFFFFFFu;
+    int step = 1, per = a.experts;
+    if (a.groups > 1) {
+        float *const sf = reinterpret_cast<float *>(sv);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) sf[j * 32 + lane] = v[j] != v[j] ? -INFINITY : v[j];
+        __syncwarp();
+        step = lanes_per_group(a.groups);
+        per = a.experts / a.groups;
+        const float mine = group_value(sf, per, a.groups, step, top2);
+        const bool in = group_open(mine, a.groups, step, a.top_groups);
+        open = __ballot_sync(0xFFFFFFFFu, in);
+        if (by_value || top2) {
+            const float least = of_key(__reduce_min_sync(0xFFFFFFFFu, in ? key_of(mine) : 0xFFFFFFFFu));
+            const float most = of_key(__reduce_max_sync(0xFFFFFFFFu, in || lane / step >= a.groups ? 0u : key_of(mine)));
+            /* a sum of two: twice the error, and its own rounding */
+            unsure = unsure || !(least - most > 2.0f * fixed + 2.0f * relative * fmaxf(fabsf(least), fabsf(most)));
         }
     }
 
-    int chosen = 0;                                       /* lane i: the i-th choice and its logit */
-    float logit = 0.0f;
+    const bool logits_decide = !by_value;
+    uint32_t key[NI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const uint32_t e = (uint32_t)(j * 32 + lane);
+        key[j] = (key_of(logits_decide ? l[j] : v[j]) & ~(uint32_t)(NI - 1)) | (uint32_t)(NI - 1 - j);
+        bool in = e < (uint32_t)a.experts;
+        if (a.groups > 1) in = in && (open >> ((e * a.per_magic >> 20) * step) & 1u);
+        if (!in) key[j] = 0u;
+    }
+    if (logits_decide) fixed = relative = 0.0f;
+    sort_keys(key);
+
+    int chosen = 0;                                       /* lane i: the i-th choice and its key */
+    uint32_t mykey = 0u;
     for (int i = 0; i < a.top_k; ++i) {
-        double best = -INFINITY;
-        float bl = 0.0f;
-        int be = 0x7FFFFFFF;
+        const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+        const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, key[0] == k)) - 1;
+        if (lane == i) { mykey = k; chosen = (NI - 1 - (int)(k & (NI - 1))) * 32 + owner; }
+        if (lane == owner) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const double x = by_value ? v[j] : lowest((double)l[j]);
-            if (!(closed >> j & 1u) && (be == 0x7FFFFFFF || x > best)) { best = x; be = j * 32 + lane; bl = l[j]; }
+            for (int j = 0; j + 1 < NI; ++j) key[j] = key[j + 1];
+            key[NI - 1] = 0u;
         }
+    }
+    __syncwarp();
+    bool mine = lane < a.top_k;
+    float logit = mine ? sl[chosen] : 0.0f;
+    {
+        const float b = by_value && mine ? a.bias[chosen] : 0.0f, x = of_key(mykey & ~(uint32_t)(NI - 1));
+        const float nx = __shfl_down_sync(0xFFFFFFFFu, x, 1), nl = __shfl_down_sync(0xFFFFFFFFu, logit, 1);
+        const float nb = __shfl_down_sync(0xFFFFFFFFu, b, 1);
+        bool far = x - nx > fixed + relative * fmaxf(fabsf(x), fabsf(nx)) || (logit == nl && b == nb);
+        /* the last one against what is left, as far as that is equal to it */
+        const int last = a.top_k - 1;
+        const float ll = __shfl_sync(0xFFFFFFFFu, logit, last), lb = __shfl_sync(0xFFFFFFFFu, b, last);
+        const float lx = __shfl_sync(0xFFFFFFFFu, x, last);
+        if (lane >= last) far = true;
+        unsure = unsure || !__all_sync(0xFFFFFFFFu, far);
+        for (int i = 0; !unsure; ++i) {
+            const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+            const float rx = of_key(k & ~(uint32_t)(NI - 1));
+            if (k == 0u || lx - rx > fixed + relative * fmaxf(fabsf(lx), fabsf(rx))) break;
+            const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, key[0] == k)) - 1;
+            const int e = (NI - 1 - (int)(k & (NI - 1))) * 32 + owner;
+            if (i == 16 || sl[e] != ll || (by_value && a.bias[e] != lb)) unsure = true;
+            if (lane == owner) {
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            const double ob = __shfl_xor_sync(0xFFFFFFFFu, best, d);
-            const int oe = __shfl_xor_sync(0xFFFFFFFFu, be, d);
-            const float ol = __shfl_xor_sync(0xFFFFFFFFu, bl, d);
-            if (ob > best || (ob == best && oe < be)) { best = ob; be = oe; bl = ol; }
+                for (int j = 0; j + 1 < NI; ++j) key[j] = key[j + 1];
+                key[NI - 1] = 0u;
+            }
         }
-        if ((be & 31) == lane) closed |= 1u << (be >> 5);
-        if (lane == i) { chosen = be; logit = bl; }
+    }
+    if (unsure) {
+        __syncwarp();
+        chosen = choose_exactly<NI>(a, sl, sv, top);
+        logit = mine ? sl[chosen] : 0.0f;
     }
 
-    const bool mine = lane < a.top_k;
     float w;
     if (a.renormalize) {
         bool nan = mine && logit != logit;
@@ -374,6 +564,8 @@ extern "C" int sifar_route(const sifar_route_args *g, void *stream)
     a.groups = g->top_groups == g->groups ? 1 : g->groups;       /* all groups stay in: none to choose */
     a.top_groups = g->top_groups; a.group_score = g->group_score;
     a.score = g->score; a.renormalize = g->renormalize != 0;
+    const uint32_t per = (uint32_t)(a.experts / a.groups);
+    a.per_magic = ((1u << 20) + per - 1u) / per;
     const dim3 grid((unsigned)((g->tokens + kRouteWarps - 1) / kRouteWarps));
     const cudaError_t err = g->dtype == SIFAR_BF16 ? launch_route<SIFAR_BF16>(grid, (cudaStream_t)stream, a)
                                                    : launch_route<SIFAR_F32>(grid, (cudaStream_t)stream, a);
