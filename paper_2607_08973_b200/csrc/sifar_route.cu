@@ -18,7 +18,8 @@ struct RouteArgs {
     unsigned long long tokens, ld_logits;    /* bytes between two tokens */
     float scale;
     int P, experts, top_k, groups, top_groups, group_score, score, renormalize;
-    uint32_t per_magic;                      /* ceil(2^20 / experts of a group): e / per = e * per_magic >> 20 for e, per < 2^10 */
+    int per;                                 /* experts of a group */
+    uint32_t per_magic;                      /* ceil(2^20 / per): e / per = e * per_magic >> 20 for e, per < 2^10 */
 };
 
 struct RouteGradArgs {
@@ -45,6 +46,13 @@ __device__ __forceinline__ double warp_sum(double v)
     return v;
 }
 
+/* Whether the lane's item j is an expert.  NI is the smallest of 2, 4, 8, 16, 32 that holds the experts: from 4 on the
+   lower half of the items always is. */
+template <int NI> __device__ __forceinline__ bool is_expert(int j, int experts)
+{
+    return (NI > 2 && j < NI / 2) || j * 32 + (int)(threadIdx.x & 31) < experts;
+}
+
 /* l[j] = the rank-order sum of the logits of expert 32 j + lane; -infinity behind the last expert.  The loads of
    several ranks are under way together. */
 template <int DT, int NI>
@@ -53,6 +61,12 @@ __device__ __forceinline__ void load_logits(float (&l)[NI], const void *const *l
     using T = typename Elem<DT>::type;
     constexpr int B = NI <= 4 ? 8 : NI <= 8 ? 4 : NI <= 16 ? 2 : 1;
     const int lane = threadIdx.x & 31;
+    if (P == 1) {
+        const T *p = reinterpret_cast<const T *>(static_cast<const char *>(logits[0]) + at) + lane;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) l[j] = is_expert<NI>(j, experts) ? widen<DT>(p[j * 32]) : -INFINITY;
+        return;
+    }
     for (int r0 = 0; r0 < P; r0 += B) {
         T w[B][NI];
 #pragma unroll
@@ -60,7 +74,7 @@ __device__ __forceinline__ void load_logits(float (&l)[NI], const void *const *l
             if (r0 + b >= P) break;
             const T *p = reinterpret_cast<const T *>(static_cast<const char *>(logits[r0 + b]) + at);
 #pragma unroll
-            for (int j = 0; j < NI; ++j) w[b][j] = j * 32 + lane < experts ? p[j * 32 + lane] : (T)0;
+            for (int j = 0; j < NI; ++j) w[b][j] = is_expert<NI>(j, experts) ? p[j * 32 + lane] : (T)0;
         }
 #pragma unroll
         for (int b = 0; b < B; ++b) {
@@ -71,7 +85,7 @@ __device__ __forceinline__ void load_logits(float (&l)[NI], const void *const *l
     }
 #pragma unroll
     for (int j = 0; j < NI; ++j)
-        if (j * 32 + lane >= experts) l[j] = -INFINITY;
+        if (!is_expert<NI>(j, experts)) l[j] = -INFINITY;
 }
 
 /*
@@ -132,20 +146,22 @@ __device__ __forceinline__ float scaled_sigmoid(float l, float max)
     return max < 0.0f ? expf(l - max) / (1.0f + expf(l)) : sigmoid(l);
 }
 
-/* The lanes of a group when a warp looks at all groups: group lane / step, step lanes each. */
-__device__ __forceinline__ int lanes_per_group(int groups) { return 32 >> (groups > 1 ? 32 - __clz(groups - 1) : 0); }
+/* The lanes of a group when a warp looks at all groups: group lane >> shift, 1 << shift lanes each. */
+__device__ __forceinline__ int group_shift(int groups) { return __clz(groups - 1) - 27; }
 
 /* The value of the lane's group: the largest of `v`'s run, or the sum of its two largest. */
-template <typename F> __device__ __forceinline__ F group_value(const F *v, int per, int groups, int step, bool top2)
+template <typename F> __device__ __forceinline__ F group_value(const F *v, int per, int groups, int shift, bool top2)
 {
-    const int lane = threadIdx.x & 31, g = lane / step;
+    const int lane = threadIdx.x & 31, g = lane >> shift, step = 1 << shift;
     F m1 = -INFINITY, m2 = -INFINITY;
-    if (g < groups)
-        for (int i = lane % step; i < per; i += step) {
+    if (g < groups) {
+#pragma unroll 4
+        for (int i = lane & (step - 1); i < per; i += step) {
             const F x = v[g * per + i];
             m2 = max(m2, min(m1, x));
             m1 = max(m1, x);
         }
+    }
     for (int d = step / 2; d > 0; d >>= 1) {
         const F o1 = __shfl_xor_sync(0xFFFFFFFFu, m1, d), o2 = __shfl_xor_sync(0xFFFFFFFFu, m2, d);
         m2 = max(max(m2, o2), min(m1, o1));
@@ -156,54 +172,56 @@ template <typename F> __device__ __forceinline__ F group_value(const F *v, int p
     return sum != sum ? (F)-INFINITY : sum;
 }
 
-/* Whether the lane's group is among the best. */
-template <typename F> __device__ __forceinline__ bool group_open(F mine, int groups, int step, int top_groups)
+/* What the choice compares, in binary64. */
+__device__ __forceinline__ double value64(const RouteArgs &a, int e, float l, bool scored, double total, float top)
 {
-    const int g = (threadIdx.x & 31) / step;
-    int better = 0;
-    for (int i = 0; i < groups; ++i) {
-        const F o = __shfl_sync(0xFFFFFFFFu, mine, i * step);
-        better += (o > mine || (o == mine && i < g)) ? 1 : 0;
+    double x = (double)l;
+    if (scored) {
+        x = a.score == SIFAR_SCORE_SIGMOID ? sigmoid(x) : top == -INFINITY ? 0.0 : exp(x - (double)top) / total;
+        if (a.bias) x += (double)a.bias[e];
     }
-    return g < groups && better < top_groups;
+    return lowest(x);
 }
 
-/*
- * The choice in binary64, from the logits in shared memory: for the tokens of which binary32 cannot tell.
- * Lane i returns choice i.
- */
+__device__ __noinline__ double softmax_total(const RouteArgs &a, const float *l, float top)
+{
+    double total = 0.0;
+#pragma unroll 4
+    for (int e = threadIdx.x & 31; e < a.experts; e += 32) total += exp((double)l[e] - (double)top);
+    return warp_sum(total);
+}
+
+/* The open groups (bit g) by values in binary64; leaves the values of all experts in v. */
+__device__ __noinline__ uint32_t groups_exactly(const RouteArgs &a, const float *l, double *v, float top, double total)
+{
+    const int lane = threadIdx.x & 31, shift = group_shift(a.groups), g = lane >> shift;
+    const bool top2 = a.group_score == SIFAR_GROUP_TOP2;
+    __syncwarp();
+#pragma unroll 4
+    for (int e = lane; e < a.experts; e += 32) v[e] = value64(a, e, l[e], a.bias || top2, total, top);
+    __syncwarp();
+    const double mine = group_value(v, a.per, a.groups, shift, top2);
+    int better = 0;
+#pragma unroll 4
+    for (int i = 0; i < a.groups; ++i) {
+        const double o = __shfl_sync(0xFFFFFFFFu, mine, i << shift);
+        better += (o > mine || (o == mine && i < g)) ? 1 : 0;
+    }
+    return __reduce_or_sync(0xFFFFFFFFu, g < a.groups && better < a.top_groups ? 1u << g : 0u);
+}
+
+/* The choice by values in binary64, one expert after the other: lane i returns choice i. */
 template <int NI>
-__device__ __noinline__ int choose_exactly(const RouteArgs &a, const float *l, double *v, float top)
+__device__ __noinline__ int choose_exactly(const RouteArgs &a, const float *l, double *v, float top, double total, uint32_t open)
 {
     const int lane = threadIdx.x & 31;
-    const bool by_value = a.bias != nullptr, top2 = a.groups > 1 && a.group_score == SIFAR_GROUP_TOP2;
-    double total = 1.0;
-    if ((by_value || top2) && a.score == SIFAR_SCORE_SOFTMAX) {
-        total = 0.0;
-        for (int e = lane; e < a.experts; e += 32) total += exp((double)l[e] - (double)top);
-        total = warp_sum(total);
-    }
-    for (int e = lane; e < a.experts; e += 32) {
-        double x = (double)l[e];
-        if (by_value || top2) {
-            x = a.score == SIFAR_SCORE_SIGMOID ? sigmoid(x) : top == -INFINITY ? 0.0 : exp(x - (double)top) / total;
-            if (by_value) x += (double)a.bias[e];
-        }
-        v[e] = lowest(x);
-    }
     __syncwarp();
-    uint32_t open = 0xFFFFFFFFu;
-    int step = 1;
-    if (a.groups > 1) {
-        step = lanes_per_group(a.groups);
-        const double mine = group_value(v, a.experts / a.groups, a.groups, step, top2);
-        open = __ballot_sync(0xFFFFFFFFu, group_open(mine, a.groups, step, a.top_groups));
-    }
     uint32_t closed = 0u;
 #pragma unroll 1
     for (int j = 0; j < NI; ++j) {
         const int e = j * 32 + lane;
-        if (e >= a.experts || (a.groups > 1 && !(open >> (e / (a.experts / a.groups)) * step & 1u))) closed |= 1u << j;
+        if (e >= a.experts || !(open >> (e / a.per) & 1u)) closed |= 1u << j;
+        else v[e] = value64(a, e, l[e], a.bias != nullptr, total, top);
     }
     int chosen = 0;
     for (int i = 0; i < a.top_k; ++i) {
@@ -212,8 +230,8 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, const float *l, d
 #pragma unroll 1
         for (int j = 0; j < NI; ++j) {
             if (closed >> j & 1u) continue;
-            const int e = j * 32 + lane;
-            const unsigned long long k = key_of(by_value ? v[e] : (double)l[e]);
+            const int e = j * 32 + lane;                  /* the lane's own value: it stored it */
+            const unsigned long long k = key_of(v[e]);
             if (k > best) { best = k; be = (uint32_t)e; }
         }
         const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, (uint32_t)(best >> 32));
@@ -227,170 +245,201 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, const float *l, d
     return chosen;
 }
 
+/* The candidates e of lanes 0 .. n - 1 in order of their values in binary64: lane i returns the i-th. */
+__device__ __noinline__ int order_exactly(const RouteArgs &a, const float *l, int *order, float top, double total, int e, int n)
+{
+    const int lane = threadIdx.x & 31;
+    const double mine = lane < n ? value64(a, e, l[e], a.bias != nullptr, total, top) : 0.0;
+    int place = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const double o = __shfl_sync(0xFFFFFFFFu, mine, i);
+        const int oe = __shfl_sync(0xFFFFFFFFu, e, i);
+        place += (o > mine || (o == mine && oe < e)) ? 1 : 0;
+    }
+    __syncwarp();
+    if (lane < n) order[place] = e;
+    __syncwarp();
+    return lane < n ? order[lane] : 0;
+}
+
 /*
  * The choice goes by keys of binary32 values whose lowest bits are the item's number, so that a key says where it came
  * from and equal values come in the order of the experts.  A lane sorts its keys once; a round then takes the largest
  * head of the 32 lists (one reduction over the warp, one ballot).
  *
  * What binary32 and the cut bits may hide is looked at afterwards: where two neighbours of the chosen, or the last of
- * them and the best that is left, lie closer than the error of both and are not equal by their inputs, the token is
- * chosen again in binary64 (choose_exactly).  Logits that are compared themselves have no error but the cut bits.
+ * them and the best that is left, lie closer than the error of both and are not equal by their inputs, rounds go on
+ * until the rest is far enough, and the candidates, one per lane, are put in order by their values in binary64.
+ * Logits that are compared themselves have no error but the cut bits.  The groups are looked at in the same way.
  */
-template <int DT, int NI>
-__global__ void __launch_bounds__(32 * kRouteWarps) k_route(const RouteArgs a)
+template <int DT, int NI, bool BIAS, bool GROUPS>
+__global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 : 3) k_route(const __grid_constant__ RouteArgs a)
 {
     __shared__ float s_l[kRouteWarps][NI * 32];
     __shared__ double s_v[kRouteWarps][NI * 32];
+    constexpr uint32_t kCut = NI - 1;
     grid_let_next_in();
     const int lane = threadIdx.x & 31;
     const unsigned long long token = (unsigned long long)blockIdx.x * kRouteWarps + threadIdx.x / 32;
     grid_wait();
     if (token >= a.tokens) return;
-    float l[NI], *const sl = s_l[threadIdx.x / 32];
+    float v[NI], *const sl = s_l[threadIdx.x / 32];
     double *const sv = s_v[threadIdx.x / 32];
-    load_logits<DT, NI>(l, a.logits, a.P, token * a.ld_logits, a.experts);
+    load_logits<DT, NI>(v, a.logits, a.P, token * a.ld_logits, a.experts);
+    bool nan = false;
 #pragma unroll
-    for (int j = 0; j < NI; ++j) sl[j * 32 + lane] = l[j];
+    for (int j = 0; j < NI; ++j) { sl[j * 32 + lane] = v[j]; nan = nan || v[j] != v[j]; }
+    nan = __any_sync(0xFFFFFFFFu, nan);
+    if (nan) {                                            /* in the choice: the lowest */
+#pragma unroll
+        for (int j = 0; j < NI; ++j) if (v[j] != v[j]) v[j] = -INFINITY;
+    }
 
-    const bool by_value = a.bias != nullptr, top2 = a.groups > 1 && a.group_score == SIFAR_GROUP_TOP2;
-    const bool softmax = a.score == SIFAR_SCORE_SOFTMAX;
+    const bool scored = BIAS || (GROUPS && a.group_score == SIFAR_GROUP_TOP2), softmax = a.score == SIFAR_SCORE_SOFTMAX;
     float top = -INFINITY, sum = 1.0f;                    /* of the softmax over all experts */
-    if (softmax && (!a.renormalize || by_value || top2)) {
-        bool nan = false;
+    if (softmax && (!a.renormalize || scored)) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) { top = fmaxf(top, l[j]); nan = nan || l[j] != l[j]; }
-        top = warp_max(top);
-        if (__any_sync(0xFFFFFFFFu, nan)) top = NAN;
+        for (int j = 0; j < NI; ++j) top = fmaxf(top, v[j]);
+        top = nan ? NAN : of_key(__reduce_max_sync(0xFFFFFFFFu, key_of(top)));
         if (top != -INFINITY) {
             sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < NI; ++j) sum += expf(l[j] - top);
+            for (int j = 0; j < NI; ++j) sum += expf(v[j] - top);
             sum = sifar::warp_sum(sum);
         }
     }
 
     /* what is compared, and its error: `fixed`, and `relative` times its size, both for a pair */
-    float v[NI], fixed = 0.0f, relative = 0.0f;
-    bool unsure = false;
-#pragma unroll
-    for (int j = 0; j < NI; ++j) v[j] = l[j];
-    if (by_value || top2) {
+    float fixed = 0.0f, relative = 0.0f;
+    bool lost = false;                                    /* binary32 does not have the values */
+    if (scored) {
         if (softmax) {
-            /* l - top, expf, the sum's NI + 5 adds, the division: of a score of at most 1 / sum */
+            /* l - top, two exponentials, the sum's NI + 5 adds, the division: of a score of at most 1 / sum */
             const float inv = top == -INFINITY ? 0.0f : 1.0f / sum;
-            fixed = 2.5f * (NI + 16) * 0x1p-24f * inv;
+            fixed = 2.5f * ((NI + 16) * 0x1p-24f + 0x1p-21f) * inv;
 #pragma unroll
-            for (int j = 0; j < NI; ++j) v[j] = top == -INFINITY ? 0.0f : __expf(l[j] - top) * inv;
-            fixed += 2.5f * 0x1p-21f * inv;               /* ... __expf for expf: two steps and the argument's product */
+            for (int j = 0; j < NI; ++j) v[j] = top == -INFINITY ? 0.0f : __expf(v[j] - top) * inv;
         } else {
-            /* __expf: two steps and the argument's product, |l| exp(-|l|) <= 0.37 steps; the reciprocal: one step */
+            /* __expf: two steps and the argument's product, |l| exp(-|l|) <= 0.37 steps; the quotient: two steps */
             fixed = 2.5f * 0x1p-21f;
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const float t = __expf(-fabsf(l[j]));
-                v[j] = __fdividef(l[j] < 0.0f ? t : 1.0f, 1.0f + t);
+                const float t = __expf(-fabsf(v[j]));
+                v[j] = __fdividef(v[j] < 0.0f ? t : 1.0f, 1.0f + t);
             }
         }
         relative = 2.5f * 0x1p-24f + 1.25f * NI * 0x1p-23f;
-        if (by_value) {
+        if (BIAS) {
 #pragma unroll
             for (int j = 0; j < NI; ++j)
-                if (j * 32 + lane < a.experts) v[j] += a.bias[j * 32 + lane];
+                if (is_expert<NI>(j, a.experts)) v[j] += a.bias[j * 32 + lane];
         }
-        bool nan = false;
+        bool odd = nan;
 #pragma unroll
-        for (int j = 0; j < NI; ++j) nan = nan || (j * 32 + lane < a.experts && v[j] != v[j]);
-        unsure = __any_sync(0xFFFFFFFFu, nan);
+        for (int j = 0; j < NI; ++j) odd = odd || v[j] != v[j];
+        lost = __any_sync(0xFFFFFFFFu, odd);
     }
+    double total = 1.0;
+    bool have_total = !softmax || !scored;
     uint32_t open = 0xFFFFFFFFu;
-    int step = 1, per = a.experts;
-    if (a.groups > 1) {
+    if (GROUPS) {
         float *const sf = reinterpret_cast<float *>(sv);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) sf[j * 32 + lane] = v[j] != v[j] ? -INFINITY : v[j];
+        for (int j = 0; j < NI; ++j) sf[j * 32 + lane] = v[j];
         __syncwarp();
-        step = lanes_per_group(a.groups);
-        per = a.experts / a.groups;
-        const float mine = group_value(sf, per, a.groups, step, top2);
-        const bool in = group_open(mine, a.groups, step, a.top_groups);
-        open = __ballot_sync(0xFFFFFFFFu, in);
-        if (by_value || top2) {
-            const float least = of_key(__reduce_min_sync(0xFFFFFFFFu, in ? key_of(mine) : 0xFFFFFFFFu));
-            const float most = of_key(__reduce_max_sync(0xFFFFFFFFu, in || lane / step >= a.groups ? 0u : key_of(mine)));
+        const int shift = group_shift(a.groups);
+        const float mine = group_value(sf, a.per, a.groups, shift, a.group_score == SIFAR_GROUP_TOP2);
+        uint32_t k = lane >> shift < a.groups ? key_of(mine) : 0u, least = 0u;
+        open = 0u;
+        for (int i = 0; i < a.top_groups; ++i) {
+            least = __reduce_max_sync(0xFFFFFFFFu, k);
+            const int g = (__ffs(__ballot_sync(0xFFFFFFFFu, k == least)) - 1) >> shift;
+            open |= 1u << g;
+            if (lane >> shift == g) k = 0u;
+        }
+        if (scored) {
+            const float x = of_key(least), y = of_key(__reduce_max_sync(0xFFFFFFFFu, k));
             /* a sum of two: twice the error, and its own rounding */
-            unsure = unsure || !(least - most > 2.0f * fixed + 2.0f * relative * fmaxf(fabsf(least), fabsf(most)));
-        }
-    }
-
-    const bool logits_decide = !by_value;
-    uint32_t key[NI];
+            if (lost || !(x - y > 2.0f * fixed + 2.0f * relative * fmaxf(fabsf(x), fabsf(y)))) {
+                if (!have_total) total = softmax_total(a, sl, top);
+                have_total = true;
+                open = groups_exactly(a, sl, sv, top, total);
+            }
+            if (!BIAS) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-        const uint32_t e = (uint32_t)(j * 32 + lane);
-        key[j] = (key_of(logits_decide ? l[j] : v[j]) & ~(uint32_t)(NI - 1)) | (uint32_t)(NI - 1 - j);
-        bool in = e < (uint32_t)a.experts;
-        if (a.groups > 1) in = in && (open >> ((e * a.per_magic >> 20) * step) & 1u);
-        if (!in) key[j] = 0u;
-    }
-    if (logits_decide) fixed = relative = 0.0f;
-    sort_keys(key);
-
-    int chosen = 0;                                       /* lane i: the i-th choice and its key */
-    uint32_t mykey = 0u;
-    for (int i = 0; i < a.top_k; ++i) {
-        const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
-        const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, key[0] == k)) - 1;
-        if (lane == i) { mykey = k; chosen = (NI - 1 - (int)(k & (NI - 1))) * 32 + owner; }
-        if (lane == owner) {
+                for (int j = 0; j < NI; ++j) v[j] = sl[j * 32 + lane];
+                if (nan) {
 #pragma unroll
-            for (int j = 0; j + 1 < NI; ++j) key[j] = key[j + 1];
-            key[NI - 1] = 0u;
-        }
-    }
-    __syncwarp();
-    bool mine = lane < a.top_k;
-    float logit = mine ? sl[chosen] : 0.0f;
-    {
-        const float b = by_value && mine ? a.bias[chosen] : 0.0f, x = of_key(mykey & ~(uint32_t)(NI - 1));
-        const float nx = __shfl_down_sync(0xFFFFFFFFu, x, 1), nl = __shfl_down_sync(0xFFFFFFFFu, logit, 1);
-        const float nb = __shfl_down_sync(0xFFFFFFFFu, b, 1);
-        bool far = x - nx > fixed + relative * fmaxf(fabsf(x), fabsf(nx)) || (logit == nl && b == nb);
-        /* the last one against what is left, as far as that is equal to it */
-        const int last = a.top_k - 1;
-        const float ll = __shfl_sync(0xFFFFFFFFu, logit, last), lb = __shfl_sync(0xFFFFFFFFu, b, last);
-        const float lx = __shfl_sync(0xFFFFFFFFu, x, last);
-        if (lane >= last) far = true;
-        unsure = unsure || !__all_sync(0xFFFFFFFFu, far);
-        for (int i = 0; !unsure; ++i) {
-            const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
-            const float rx = of_key(k & ~(uint32_t)(NI - 1));
-            if (k == 0u || lx - rx > fixed + relative * fmaxf(fabsf(lx), fabsf(rx))) break;
-            const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, key[0] == k)) - 1;
-            const int e = (NI - 1 - (int)(k & (NI - 1))) * 32 + owner;
-            if (i == 16 || sl[e] != ll || (by_value && a.bias[e] != lb)) unsure = true;
-            if (lane == owner) {
-#pragma unroll
-                for (int j = 0; j + 1 < NI; ++j) key[j] = key[j + 1];
-                key[NI - 1] = 0u;
+                    for (int j = 0; j < NI; ++j) if (v[j] != v[j]) v[j] = -INFINITY;
+                }
             }
         }
     }
-    if (unsure) {
-        __syncwarp();
-        chosen = choose_exactly<NI>(a, sl, sv, top);
+    if (!BIAS) { fixed = relative = 0.0f; lost = false; }
+
+    uint32_t key[NI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const uint32_t u = __float_as_uint(v[j] + 0.0f);
+        key[j] = ((u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) & ~kCut) | (kCut - (uint32_t)j);
+        if (!is_expert<NI>(j, a.experts) || (GROUPS && !(open >> ((uint32_t)(j * 32 + lane) * a.per_magic >> 20) & 1u))) key[j] = 0u;
+    }
+    sort_keys(key);
+
+    uint32_t mykey = 0u;                                  /* lane i: the i-th candidate */
+    int owner = 0;
+    auto take = [&](int i) {
+        const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+        const int who = __ffs(__ballot_sync(0xFFFFFFFFu, key[0] == k)) - 1;
+        if (lane == i) { mykey = k; owner = who; }
+        const bool pop = lane == who;
+#pragma unroll
+        for (int j = 0; j + 1 < NI; ++j) key[j] = pop ? key[j + 1] : key[j];
+        if (pop) key[NI - 1] = 0u;
+        return k;
+    };
+    auto apart = [&](float x, float y) { return x - y > fixed + relative * fmaxf(fabsf(x), fabsf(y)); };
+    for (int i = 0; i < a.top_k; ++i) take(i);
+    __syncwarp();
+    const bool mine = lane < a.top_k;
+    int chosen = (int)(kCut - (mykey & kCut)) * 32 + owner;
+    float logit = mine ? sl[chosen] : 0.0f;
+
+    const int last = a.top_k - 1;
+    const float x = of_key(mykey & ~kCut), lx = __shfl_sync(0xFFFFFFFFu, x, last);
+    const float b = BIAS && mine ? a.bias[chosen] : 0.0f;
+    const float nx = __shfl_down_sync(0xFFFFFFFFu, x, 1), nl = __shfl_down_sync(0xFFFFFFFFu, logit, 1);
+    const float nb = __shfl_down_sync(0xFFFFFFFFu, b, 1);
+    const uint32_t rest = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+    const bool sure = lane > last || (lane == last ? rest == 0u || apart(lx, of_key(rest & ~kCut))
+                                                   : apart(x, nx) || (logit == nl && b == nb));
+    if (lost || !__all_sync(0xFFFFFFFFu, sure)) {
+        if (!have_total) total = softmax_total(a, sl, top);
+        /* candidates: as many more as are not far from the last one */
+        int n = a.top_k;
+        for (uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+             k != 0u && n < 32 && !lost && !apart(lx, of_key(k & ~kCut)); k = __reduce_max_sync(0xFFFFFFFFu, key[0]))
+            take(n++);
+        const uint32_t k = __reduce_max_sync(0xFFFFFFFFu, key[0]);
+        if (lost || !(k == 0u || apart(lx, of_key(k & ~kCut)))) {
+            chosen = choose_exactly<NI>(a, sl, sv, top, total, open);
+        } else {
+            const int e = (int)(kCut - (mykey & kCut)) * 32 + owner;
+            chosen = order_exactly(a, sl, reinterpret_cast<int *>(sv), top, total, e, n);
+        }
         logit = mine ? sl[chosen] : 0.0f;
     }
 
     float w;
     if (a.renormalize) {
-        bool nan = mine && logit != logit;
-        float max = warp_max(mine ? logit : -INFINITY);
-        if (__any_sync(0xFFFFFFFFu, nan)) max = NAN;
-        w = a.score == SIFAR_SCORE_SOFTMAX ? expf(logit - max) : scaled_sigmoid(logit, max);
+        float max = of_key(__reduce_max_sync(0xFFFFFFFFu, mine ? key_of(logit) : 0u));
+        if (nan && __any_sync(0xFFFFFFFFu, mine && logit != logit)) max = NAN;
+        w = softmax ? expf(logit - max) : scaled_sigmoid(logit, max);
         if (!mine || max == -INFINITY) w = 0.0f;
         const float total = sifar::warp_sum(w);
         w = max == -INFINITY ? 0.0f : w / total;
-    } else if (a.score == SIFAR_SCORE_SOFTMAX) {
+    } else if (softmax) {
         w = top == -INFINITY ? 0.0f : expf(logit - top) / sum;
     } else {
         w = sigmoid(logit);
@@ -402,7 +451,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) k_route(const RouteArgs a)
 }
 
 template <int DT, int NI>
-__global__ void __launch_bounds__(32 * kRouteWarps) k_route_grad(const RouteGradArgs a)
+__global__ void __launch_bounds__(32 * kRouteWarps) k_route_grad(const __grid_constant__ RouteGradArgs a)
 {
     using T = typename Elem<DT>::type;
     grid_let_next_in();
@@ -483,15 +532,25 @@ __global__ void __launch_bounds__(32 * kRouteWarps) k_route_grad(const RouteGrad
     if (first) out[e] = narrow<DT>(total);
 }
 
+template <int DT, int NI>
+static cudaError_t launch_route_n(dim3 grid, cudaStream_t stream, const RouteArgs &a)
+{
+    const dim3 block(32 * kRouteWarps);
+    if (a.bias)
+        return a.groups > 1 ? launch_op(k_route<DT, NI, true, true>, grid, block, 1, 0, stream, a)
+                            : launch_op(k_route<DT, NI, true, false>, grid, block, 1, 0, stream, a);
+    return a.groups > 1 ? launch_op(k_route<DT, NI, false, true>, grid, block, 1, 0, stream, a)
+                        : launch_op(k_route<DT, NI, false, false>, grid, block, 1, 0, stream, a);
+}
+
 template <int DT>
 static cudaError_t launch_route(dim3 grid, cudaStream_t stream, const RouteArgs &a)
 {
-    const dim3 block(32 * kRouteWarps);
-    if (a.experts <= 64) return launch_op(k_route<DT, 2>, grid, block, 1, 0, stream, a);
-    if (a.experts <= 128) return launch_op(k_route<DT, 4>, grid, block, 1, 0, stream, a);
-    if (a.experts <= 256) return launch_op(k_route<DT, 8>, grid, block, 1, 0, stream, a);
-    if (a.experts <= 512) return launch_op(k_route<DT, 16>, grid, block, 1, 0, stream, a);
-    return launch_op(k_route<DT, 32>, grid, block, 1, 0, stream, a);
+    if (a.experts <= 64) return launch_route_n<DT, 2>(grid, stream, a);
+    if (a.experts <= 128) return launch_route_n<DT, 4>(grid, stream, a);
+    if (a.experts <= 256) return launch_route_n<DT, 8>(grid, stream, a);
+    if (a.experts <= 512) return launch_route_n<DT, 16>(grid, stream, a);
+    return launch_route_n<DT, 32>(grid, stream, a);
 }
 
 template <int DT>
@@ -564,8 +623,8 @@ extern "C" int sifar_route(const sifar_route_args *g, void *stream)
     a.groups = g->top_groups == g->groups ? 1 : g->groups;       /* all groups stay in: none to choose */
     a.top_groups = g->top_groups; a.group_score = g->group_score;
     a.score = g->score; a.renormalize = g->renormalize != 0;
-    const uint32_t per = (uint32_t)(a.experts / a.groups);
-    a.per_magic = ((1u << 20) + per - 1u) / per;
+    a.per = a.experts / a.groups;
+    a.per_magic = ((1u << 20) + (uint32_t)a.per - 1u) / (uint32_t)a.per;
     const dim3 grid((unsigned)((g->tokens + kRouteWarps - 1) / kRouteWarps));
     const cudaError_t err = g->dtype == SIFAR_BF16 ? launch_route<SIFAR_BF16>(grid, (cudaStream_t)stream, a)
                                                    : launch_route<SIFAR_F32>(grid, (cudaStream_t)stream, a);
