@@ -389,8 +389,8 @@ int sifar_noalloc_counters(unsigned long long out[3]);
  *   - One argument block per call, read before the call returns (a program may keep one per layer and pass it again).
  *     Unused pointers are NULL.  Everything is launched on the CURRENT device and on `stream`; nothing synchronizes.
  *   - `rows` x `cols` arrays have a row stride ld_* in elements, at least cols; 0 stands for cols.  Addresses need the
- *     alignment of their element type.  Where the bases and strides of all row arrays are multiples of 16 bytes (and
- *     those of the weights too) the kernels move 16 bytes per access, otherwise single elements.
+ *     alignment of their element type.  Where the bases and strides of all row arrays are multiples of 16 bytes the
+ *     kernels move 16 bytes per access, otherwise single elements.
  *   - An output may overlap nothing else, except as stated.  Arrays that share a buffer column by column (same stride,
  *     disjoint columns) do not overlap.
  *   - SIFAR_ERR_INVALID: nothing was launched.  rows = 0 (tokens = 0) is valid: no row is read or written; gradients

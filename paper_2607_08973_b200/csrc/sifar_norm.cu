@@ -33,6 +33,8 @@ __global__ void __launch_bounds__(kMaxRowThreads) k_block_norm(const NormArgs a)
     const bool live = row < a.rows;
     const Columns<DT, VEC> c(part, tx, t, live ? a.cols : 0u);
     const unsigned long long at = live ? row : 0ull;
+    clear_row_sum(s);
+    __syncthreads();
     grid_wait();
 
     Raw<DT> x[PT], res, w1, w2, g;
@@ -40,9 +42,9 @@ __global__ void __launch_bounds__(kMaxRowThreads) k_block_norm(const NormArgs a)
     for (int r = 0; r < PT; ++r)
         if (r < a.P) load_row(x[r], static_cast<const char *>(a.x[r]) + at * a.ld_x, c);
     if (a.residual) load_row(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c);
-    if (a.post && a.post_weight) load_row(w1, a.post_weight, c);
-    if (a.gate) load_row(g, static_cast<const char *>(a.gate) + (unsigned long long)((uint32_t)at / a.rows_per_gate) * a.ld_gate, c);
-    if (a.pre && a.pre_weight) load_row(w2, a.pre_weight, c);
+    if (a.post && a.post_weight) load_any(w1, a.post_weight, c);
+    if (a.gate) load_any(g, static_cast<const char *>(a.gate) + (unsigned long long)((uint32_t)at / a.rows_per_gate) * a.ld_gate, c);
+    if (a.pre && a.pre_weight) load_any(w2, a.pre_weight, c);
     if (a.parts > 1) cluster_wait();
 
     float f[kItems];
@@ -137,14 +139,14 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     const bool in_place = g->h && g->h == g->residual && (h.ld == residual.ld || rows == 1);
     if (in_place) { if (int rc = check_array(fn, residual)) return rc; }
     else all[n++] = residual;
-    all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
-    all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
-    all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
     all[n++] = RowArray{"z", g->z, rows, cols, or_cols(g->ld_z, cols), es, true};
     all[n++] = h;
     all[n++] = RowArray{"y", g->y, rows, cols, or_cols(g->ld_y, cols), es, true};
     bool vec = rows_aligned16(residual);
     for (int i = 0; i < n; ++i) vec = vec && rows_aligned16(all[i]);
+    all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
+    all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
+    all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
     all[n++] = RowArray{"stats", g->stats, 1, 2 * rows, 2 * rows, sizeof(float), true};
     if (int rc = check_arrays(fn, all, n)) return rc;
 

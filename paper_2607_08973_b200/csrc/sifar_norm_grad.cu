@@ -6,6 +6,8 @@
  * registers from row to row and stored once per block.  The second adds the blocks' sums in order, so that the
  * result does not depend on which CTA was first.
  */
+#include <atomic>
+
 #include "sifar_norm.cuh"
 
 namespace sifar {
@@ -23,7 +25,7 @@ struct NormGradArgs {
     float *sum_post, *sum_pre, *sum_gate;    /* workspace: [block][pitch], [block][pitch], [block][2][pitch]; or NULL */
     unsigned long long ld_dy, ld_dh, ld_h, ld_z, ld_gate, ld_dx, ld_dresidual;    /* bytes between two rows */
     float alpha, beta, offset;
-    uint32_t rows, cols, pitch, blocks, rows_per_gate, parts;
+    uint32_t rows, cols, pitch, blocks, rows_per_gate, parts, stages;
     int P, post, pre;
 };
 
@@ -54,61 +56,113 @@ __device__ __forceinline__ void flush_gate(const NormGradArgs &a, const Columns<
     for (int j = 0; j < kItems; ++j) acc[j] = 0.0f;
 }
 
-template <int DT, int PT, bool VEC>
-__global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const NormGradArgs a)
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
+    extern __shared__ __align__(16) unsigned char ring_bytes[];
     __shared__ RowSum s;
     grid_let_next_in();
     const uint32_t tx = blockDim.x, t = threadIdx.x;
     const uint32_t part = a.parts > 1 ? cluster_rank() : 0u;
+    clear_row_sum(s);
+    __syncthreads();
     if (a.parts > 1) { cluster_arrive(); cluster_wait(); }
     const uint32_t b = (blockIdx.x / a.parts) * blockDim.y + threadIdx.y;
     const bool live = b < a.blocks;
     const uint32_t first = live ? block_start(a.rows, a.blocks, b) : 0u, end = live ? block_start(a.rows, a.blocks, b + 1) : 0u;
     const uint32_t turns = (a.rows + a.blocks - 1) / a.blocks;        /* the same for all threads: they meet in the sums */
     const Columns<DT, VEC> all(part, tx, t, a.cols);
+    const Ring<DT, VEC> ring(ring_bytes);
+    const uint32_t partials = a.pre ? (uint32_t)a.P : 0u, arrays = partials + (a.pre ? 1u : 0u) + (a.dh ? 1u : 0u) + (a.z ? 1u : 0u);
     grid_wait();
 
+    /* row `row` into stage `stage`: the partials, then h, dh, z */
+    auto fetch = [&](uint32_t stage, uint32_t row) {
+        if (row < end) {
+            uint32_t k = stage * arrays;
+            for (uint32_t r = 0; r < partials; ++r) ring.fetch(k++, static_cast<const char *>(a.dy[r]) + row * a.ld_dy, all);
+            if (a.pre) ring.fetch(k++, static_cast<const char *>(a.h) + row * a.ld_h, all);
+            if (a.dh) ring.fetch(k++, static_cast<const char *>(a.dh) + row * a.ld_dh, all);
+            if (a.z) ring.fetch(k++, static_cast<const char *>(a.z) + row * a.ld_z, all);
+        }
+        ring.commit();
+    };
+    if (Ring<DT, VEC>::possible)
+        for (uint32_t i = 0; i < a.stages; ++i) fetch(i, first + i);
+
     Raw<DT> w1, w2;
-    if (a.post_weight) load_row(w1, a.post_weight, all);
-    if (a.pre_weight) load_row(w2, a.pre_weight, all);
+    if (a.post_weight) load_any(w1, a.post_weight, all);
+    if (a.pre_weight) load_any(w2, a.pre_weight, all);
     float acc1[kItems], acc2[kItems], accg[kItems];
 #pragma unroll
     for (int j = 0; j < kItems; ++j) acc1[j] = acc2[j] = accg[j] = 0.0f;
     const float inv = 1.0f / (float)a.cols;
-    uint32_t segment = first;
+    uint32_t segment = first, stage = 0;
     int turn = 0;
+    float next1 = a.post && live ? a.stats[first] : 1.0f, next2 = a.pre && live ? a.stats[a.rows + first] : 1.0f;
 
     for (uint32_t i = 0; i < turns; ++i) {
         const bool on = first + i < end;
         const uint32_t row = on ? first + i : 0u;
         const Columns<DT, VEC> c(part, tx, t, on ? a.cols : 0u);
-        Raw<DT> x[PT], xh, xn, xz, xg;
-        if (a.pre) {
-#pragma unroll
-            for (int r = 0; r < PT; ++r)
-                if (r < a.P) load_row(x[r], static_cast<const char *>(a.dy[r]) + row * a.ld_dy, c);
-            load_row(xn, static_cast<const char *>(a.h) + row * a.ld_h, c);
+        const float r1 = next1, r2 = next2;
+        if (first + i + 1 < end) {
+            if (a.post) next1 = a.stats[row + 1];
+            if (a.pre) next2 = a.stats[a.rows + row + 1];
         }
-        if (a.dh) load_row(xh, static_cast<const char *>(a.dh) + row * a.ld_dh, c);
-        if (a.z) load_row(xz, static_cast<const char *>(a.z) + row * a.ld_z, c);
-        if (a.gate) load_row(xg, static_cast<const char *>(a.gate) + (row / a.rows_per_gate) * a.ld_gate, c);
-        const float r1 = a.post ? a.stats[row] : 1.0f, r2 = a.pre ? a.stats[a.rows + row] : 1.0f;
         if (a.dgate && on && row != segment && row % a.rows_per_gate == 0) {
             flush_gate(a, all, accg, b, first, segment, row);
             segment = row;
         }
+        Raw<DT> xg;
+        if (a.gate) load_any(xg, static_cast<const char *>(a.gate) + (row / a.rows_per_gate) * a.ld_gate, c);
 
-        float D[kItems];
+        float D[kItems], G[kItems];
+        Raw<DT> xn, xz;
+        if (Ring<DT, VEC>::possible) {
+            ring.wait(a.stages - 1);
+            uint32_t k = stage * arrays;
+            if (a.pre) {
+                Raw<DT> x;
+                ring.read(x, k++);
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) D[j] = a.dh ? item(xh, j) : 0.0f;
+                for (int j = 0; j < kItems; ++j) G[j] = item(x, j);
+                for (uint32_t r = 1; r < partials; ++r) { ring.read(x, k++); add_items(G, x); }
+                ring.read(xn, k++);
+            }
+            Raw<DT> x;
+            if (a.dh) ring.read(x, k++);
+#pragma unroll
+            for (int j = 0; j < kItems; ++j) D[j] = a.dh ? item(x, j) : 0.0f;
+            if (a.z) ring.read(xz, k);
+            fetch(stage, first + i + a.stages);            /* the thread has read its places */
+            stage = stage + 1 == a.stages ? 0u : stage + 1;
+        } else {
+            if (a.pre) {
+                Raw<DT> x;
+                load_row(x, static_cast<const char *>(a.dy[0]) + row * a.ld_dy, c);
+#pragma unroll
+                for (int j = 0; j < kItems; ++j) G[j] = item(x, j);
+                for (uint32_t r = 1; r < partials; ++r) {
+                    load_row(x, static_cast<const char *>(a.dy[r]) + row * a.ld_dy, c);
+                    add_items(G, x);
+                }
+                load_row(xn, static_cast<const char *>(a.h) + row * a.ld_h, c);
+            }
+            Raw<DT> x;
+            if (a.dh) load_row(x, static_cast<const char *>(a.dh) + row * a.ld_dh, c);
+#pragma unroll
+            for (int j = 0; j < kItems; ++j) D[j] = a.dh ? item(x, j) : 0.0f;
+            if (a.z) load_row(xz, static_cast<const char *>(a.z) + row * a.ld_z, c);
+        }
+        if (!on) {                                         /* nothing was fetched for this thread */
+#pragma unroll
+            for (int j = 0; j < kItems; ++j) D[j] = G[j] = 0.0f;
+            xn = xz = Raw<DT>{};
+        }
+
         if (a.pre) {
-            float G[kItems], q = 0.0f;
-#pragma unroll
-            for (int j = 0; j < kItems; ++j) G[j] = item(x[0], j);
-#pragma unroll
-            for (int r = 1; r < PT; ++r)
-                if (r < a.P) add_items(G, x[r]);
+            float q = 0.0f;
 #pragma unroll
             for (int j = 0; j < kItems; ++j) {
                 const float n2 = item(xn, j) * r2;
@@ -148,6 +202,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const Nor
         }
         if (a.dx) store_row(static_cast<char *>(a.dx) + row * a.ld_dx, D, c);
     }
+    if (Ring<DT, VEC>::possible) ring.wait(0);
     if (!live) return;
     if (a.sum_post) store_f32(a.sum_post + (size_t)b * a.pitch, acc1, all);
     if (a.sum_pre) store_f32(a.sum_pre + (size_t)b * a.pitch, acc2, all);
@@ -231,20 +286,27 @@ static GradShape grad_shape(size_t rows, size_t cols)
     return s;
 }
 
-template <int DT, int PT>
-static cudaError_t launch_grad_p(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormGradArgs &a)
+/* The ring takes the shared memory that a CTA can have: the attribute is set once per kernel and device. */
+template <int DT, bool VEC>
+static cudaError_t launch_grad(dim3 grid, dim3 block, cudaStream_t stream, NormGradArgs &a, unsigned arrays)
 {
-    return vec ? launch_op(k_block_norm_grad<DT, PT, true>, grid, block, cluster, 0, stream, a)
-               : launch_op(k_block_norm_grad<DT, PT, false>, grid, block, cluster, 0, stream, a);
-}
-
-template <int DT>
-static cudaError_t launch_grad(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormGradArgs &a)
-{
-    if (a.P <= 1) return launch_grad_p<DT, 1>(vec, grid, block, cluster, stream, a);
-    if (a.P <= 2) return launch_grad_p<DT, 2>(vec, grid, block, cluster, stream, a);
-    if (a.P <= 4) return launch_grad_p<DT, 4>(vec, grid, block, cluster, stream, a);
-    return launch_grad_p<DT, 8>(vec, grid, block, cluster, stream, a);
+    const size_t row = (size_t)block.x * block.y * arrays * Ring<DT, VEC>::bytes;
+    size_t smem = 0;
+    a.stages = 1;
+    if (Ring<DT, VEC>::possible) {
+        a.stages = (uint32_t)(kRingBytes / row < kMaxStages ? kRingBytes / row : kMaxStages);
+        smem = row * a.stages;
+    }
+    static std::atomic<unsigned long long> ready{0};       /* a bit per device */
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (Ring<DT, VEC>::possible && (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1ull))) {
+        e = cudaFuncSetAttribute(k_block_norm_grad<DT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+        if (e != cudaSuccess) return e;
+        if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_release);
+    }
+    return launch_op(k_block_norm_grad<DT, VEC>, grid, block, a.parts, smem, stream, a);
 }
 
 }  /* namespace sifar */
@@ -317,12 +379,12 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     all[n++] = dres;
     if (pre) all[n++] = RowArray{"h", g->h, rows, cols, or_cols(g->ld_h, cols), es, false};
     if (need_z) all[n++] = RowArray{"z", g->z, rows, cols, or_cols(g->ld_z, cols), es, false};
-    if (post) all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
-    if (pre) all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
-    all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
     all[n++] = RowArray{"dx", g->dx, rows, cols, or_cols(g->ld_dx, cols), es, true};
     bool vec = rows_aligned16(dh);
     for (int i = 0; i < n; ++i) vec = vec && rows_aligned16(all[i]);
+    if (post) all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
+    if (pre) all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
+    all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
     if (post || pre) all[n++] = RowArray{"stats", g->stats, 1, 2 * rows, 2 * rows, sizeof(float), false};
     all[n++] = RowArray{"dpost_weight", g->dpost_weight, 1, cols, cols, sizeof(float), true};
     all[n++] = RowArray{"dpre_weight", g->dpre_weight, 1, cols, cols, sizeof(float), true};
@@ -350,9 +412,12 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     a.P = pre ? g->P : 1; a.post = post; a.pre = pre;
     if (rows) {
         const dim3 grid((sh.blocks + sh.ry - 1) / sh.ry * sh.row.parts), block(sh.row.tx, sh.ry);
-        const cudaError_t err =
-            g->dtype == SIFAR_BF16 ? launch_grad<SIFAR_BF16>(vec, grid, block, sh.row.parts, (cudaStream_t)stream, a)
-                                   : launch_grad<SIFAR_F32>(vec, grid, block, sh.row.parts, (cudaStream_t)stream, a);
+        const unsigned arrays = (pre ? (unsigned)g->P + 1u : 0u) + (g->dh ? 1u : 0u) + (need_z ? 1u : 0u);
+        const cudaStream_t q = (cudaStream_t)stream;
+        const cudaError_t err = g->dtype == SIFAR_BF16 ? (vec ? launch_grad<SIFAR_BF16, true>(grid, block, q, a, arrays)
+                                                              : launch_grad<SIFAR_BF16, false>(grid, block, q, a, arrays))
+                                                       : (vec ? launch_grad<SIFAR_F32, true>(grid, block, q, a, arrays)
+                                                              : launch_grad<SIFAR_F32, false>(grid, block, q, a, arrays));
         SIFAR_CUDA(err);
     }
     if (g->dpost_weight || g->dpre_weight || g->dgate) {
