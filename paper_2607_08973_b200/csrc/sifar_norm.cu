@@ -10,75 +10,103 @@ struct NormArgs {
     const void *residual, *post_weight, *gate, *pre_weight;
     void *z, *h, *y;
     float *stats;
-    unsigned long long rows;
-    unsigned long long ld_x, ld_residual, ld_gate, ld_z, ld_h, ld_y;    /* bytes between two rows */
+    uint32_t ld_x, ld_residual, ld_gate, ld_z, ld_h, ld_y;    /* bytes between two rows */
     float alpha, beta, eps, offset;
-    uint32_t cols, parts, rows_per_gate;
-    int P, post, pre;
+    uint32_t rows, cols, parts, rows_per_gate;
+    int P, post, pre, aligned;               /* aligned: the weights and the gate are, as the rows, on 16 bytes */
 };
 
 /*
  * One row per threadIdx.y (and cluster).  All loads of a row go out before the first sum; z, h and y never leave the
  * registers between.  PT is P or the next power of two above it.
  */
+template <int DT, int PT> constexpr int kNormCtasPerSm = DT == SIFAR_BF16 ? (PT <= 2 ? 3 : 2) : (PT <= 2 ? 2 : 1);
+
 template <int DT, int PT, bool VEC>
-__global__ void __launch_bounds__(kMaxRowThreads) k_block_norm(const NormArgs a)
+__global__ void __launch_bounds__(kMaxRowThreads, kNormCtasPerSm<DT, PT>) k_block_norm(const __grid_constant__ NormArgs a)
 {
-    __shared__ RowSum s;
+    __shared__ __align__(16) RowSum<1> s;
     grid_let_next_in();
-    const uint32_t tx = blockDim.x, t = threadIdx.x;
-    const uint32_t part = a.parts > 1 ? cluster_rank() : 0u;
-    if (a.parts > 1) cluster_arrive();                   /* a CTA's shared memory may be written once it has started */
-    const unsigned long long row = (unsigned long long)(blockIdx.x / a.parts) * blockDim.y + threadIdx.y;
-    const bool live = row < a.rows;
-    const Columns<DT, VEC> c(part, tx, t, live ? a.cols : 0u);
-    const unsigned long long at = live ? row : 0ull;
+    const RowPlace p{blockDim.x, threadIdx.x, threadIdx.y, a.parts, a.parts > 1 ? cluster_rank() : 0u};
     clear_row_sum(s);
     __syncthreads();
+    if (a.parts > 1) cluster_arrive();                   /* a CTA's shared memory may be written once it has started */
+    const uint32_t row = (blockIdx.x / a.parts) * blockDim.y + threadIdx.y;
+    const bool live = row < a.rows;
+    const Columns<DT, VEC> c(p.part, p.tx, p.t, live ? a.cols : 0u);
+    const Lane<DT, VEC> l(c);
+    const unsigned long long at = live ? row : 0u;
     grid_wait();
 
-    Raw<DT> x[PT], res, w1, w2, g;
+    Raw<DT> x[PT], res, rg, rw1, rw2;
+    const char *gate = nullptr;
+    if (a.gate) gate = static_cast<const char *>(a.gate) + (unsigned long long)((uint32_t)at / a.rows_per_gate) * a.ld_gate;
+    /* the weights and the gate may lack the rows' alignment: those warps look at every element too */
+    if (!l.ragged && a.aligned) {
+        const unsigned long long o = at * a.ld_x;
 #pragma unroll
-    for (int r = 0; r < PT; ++r)
-        if (r < a.P) load_row(x[r], static_cast<const char *>(a.x[r]) + at * a.ld_x, c);
-    if (a.residual) load_row(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c);
-    if (a.post && a.post_weight) load_any(w1, a.post_weight, c);
-    if (a.gate) load_any(g, static_cast<const char *>(a.gate) + (unsigned long long)((uint32_t)at / a.rows_per_gate) * a.ld_gate, c);
-    if (a.pre && a.pre_weight) load_any(w2, a.pre_weight, c);
+        for (int r = 0; r < PT; ++r)
+            if (r < a.P) load_whole(x[r], static_cast<const char *>(a.x[r]) + o, l);
+        if (a.residual) load_whole(res, static_cast<const char *>(a.residual) + at * a.ld_residual, l);
+        if (a.gate) load_whole(rg, gate, l);
+        if (a.post_weight) load_whole(rw1, a.post_weight, l);
+        if (a.pre_weight) load_whole(rw2, a.pre_weight, l);
+    } else {
+#pragma unroll
+        for (int r = 0; r < PT; ++r)
+            if (r < a.P) load_row(x[r], static_cast<const char *>(a.x[r]) + at * a.ld_x, c);
+        if (a.residual) load_row(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c);
+        if (a.gate) load_any(rg, gate, c);
+        if (a.post_weight) load_any(rw1, a.post_weight, c);
+        if (a.pre_weight) load_any(rw2, a.pre_weight, c);
+    }
     if (a.parts > 1) cluster_wait();
 
-    float f[kItems];
-#pragma unroll
-    for (int j = 0; j < kItems; ++j) f[j] = item(x[0], j);
+    Items f = items(x[0]);
 #pragma unroll
     for (int r = 1; r < PT; ++r)
         if (r < a.P) add_items(f, x[r]);
-    if (a.z) store_row(static_cast<char *>(a.z) + at * a.ld_z, f, c);
+    if (a.z) store_items(static_cast<char *>(a.z) + at * a.ld_z, f, c, l);
 
     float r1 = 1.0f, r2 = 1.0f;
+    uint32_t call = 0;
     if (a.post) {
-        float q = 0.0f;
+        float sum[1] = {squares(f, l)};
+        row_sums(sum, s, call++, p);
+        r1 = rrms(sum[0], a.cols, a.eps);
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) q = fmaf(f[j], f[j], q);
-        r1 = rrms(row_sum(q, s, 0, tx, t, threadIdx.y, a.parts, part), a.cols, a.eps);
+        for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r1));
+        if (a.post_weight) {
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) f[j] *= a.post_weight ? r1 * (item(w1, j) + a.offset) : r1;
+            for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair(rw1, j), both(a.offset)));
+        }
     }
-    float q = 0.0f;
+    if (a.gate) {
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-        f[j] *= a.gate ? a.beta * item(g, j) : a.beta;
-        if (a.residual) f[j] = fmaf(a.alpha, item(res, j), f[j]);
-        q = fmaf(f[j], f[j], q);
+        for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], pair(rg, j));
     }
-    if (a.h) store_row(static_cast<char *>(a.h) + at * a.ld_h, f, c);
+#pragma unroll
+    for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], both(a.beta));
+    if (a.residual) {
+#pragma unroll
+        for (int j = 0; j < kItems / 2; ++j) f.p[j] = __ffma2_rn(both(a.alpha), pair(res, j), f.p[j]);
+    }
+    if (a.h) store_items(static_cast<char *>(a.h) + at * a.ld_h, f, c, l);
     if (a.pre) {
-        r2 = rrms(row_sum(q, s, 1, tx, t, threadIdx.y, a.parts, part), a.cols, a.eps);
+        float sum[1] = {squares(f, l)};
+        row_sums(sum, s, call++, p);
+        r2 = rrms(sum[0], a.cols, a.eps);
+        if (a.y) {
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) f[j] *= a.pre_weight ? r2 * (item(w2, j) + a.offset) : r2;
-        if (a.y) store_row(static_cast<char *>(a.y) + at * a.ld_y, f, c);
+            for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r2));
+            if (a.pre_weight) {
+#pragma unroll
+                for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair(rw2, j), both(a.offset)));
+            }
+            store_items(static_cast<char *>(a.y) + at * a.ld_y, f, c, l);
+        }
     }
-    if (a.stats && live && t == 0 && part == 0) {
+    if (a.stats && live && p.t == 0 && p.part == 0) {
         a.stats[row] = r1;
         a.stats[a.rows + row] = r2;
     }
@@ -144,26 +172,31 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     all[n++] = RowArray{"y", g->y, rows, cols, or_cols(g->ld_y, cols), es, true};
     bool vec = rows_aligned16(residual);
     for (int i = 0; i < n; ++i) vec = vec && rows_aligned16(all[i]);
+    const int weights = n;
     all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
     all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
     all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
+    bool aligned = true;
+    for (int i = weights; i < n; ++i) aligned = aligned && rows_aligned16(all[i]);
     all[n++] = RowArray{"stats", g->stats, 1, 2 * rows, 2 * rows, sizeof(float), true};
     if (int rc = check_arrays(fn, all, n)) return rc;
 
     NormArgs a;
     for (int r = 0; r < kMaxRanks; ++r) a.x[r] = r < g->P ? g->x[r] : nullptr;
-    a.residual = g->residual; a.post_weight = g->post_weight; a.gate = g->gate; a.pre_weight = g->pre_weight;
+    a.residual = g->residual; a.gate = g->gate;
+    a.post_weight = g->post_norm ? g->post_weight : nullptr; a.pre_weight = g->y ? g->pre_weight : nullptr;
     a.z = g->z; a.h = g->h; a.y = g->y; a.stats = g->stats;
-    a.rows = rows; a.cols = (uint32_t)cols;
-    a.ld_x = or_cols(g->ld_x, cols) * es; a.ld_residual = residual.ld * es; a.ld_gate = or_cols(g->ld_gate, cols) * es;
-    a.ld_z = or_cols(g->ld_z, cols) * es; a.ld_h = h.ld * es; a.ld_y = or_cols(g->ld_y, cols) * es;
+    a.rows = (uint32_t)rows; a.cols = (uint32_t)cols;
+    const auto bytes = [&](size_t ld) { return (uint32_t)(or_cols(ld, cols) * es); };
+    a.ld_x = bytes(g->ld_x); a.ld_residual = bytes(g->ld_residual); a.ld_gate = bytes(g->ld_gate);
+    a.ld_z = bytes(g->ld_z); a.ld_h = bytes(g->ld_h); a.ld_y = bytes(g->ld_y);
     a.rows_per_gate = (uint32_t)span;
     a.alpha = g->alpha; a.beta = g->beta; a.eps = g->eps; a.offset = g->weight_offset;
-    a.P = g->P; a.post = g->post_norm != 0; a.pre = g->pre_norm != 0;
-    const RowShape sh = row_shape(cols);
+    a.P = g->P; a.post = g->post_norm != 0; a.pre = g->pre_norm != 0; a.aligned = aligned;
+    const RowShape sh = row_shape(rows, cols);
     a.parts = sh.parts;
     unsigned ry = 1;
-    while (sh.parts == 1 && 2 * ry * sh.tx <= 256 && rows >= (size_t)2 * ry * 296) ry *= 2;
+    while (sh.parts == 1 && 2 * ry * sh.tx <= 256 && rows >= (size_t)2 * ry * 2 * kNormCtas) ry *= 2;
     const unsigned long long grid = (rows + ry - 1) / ry * sh.parts;
     if (grid > 0x7FFFFFFFull) { set_error("%s: too many rows of this width", fn); return SIFAR_ERR_INVALID; }
     const dim3 gd((unsigned)grid), bd(sh.tx, ry);

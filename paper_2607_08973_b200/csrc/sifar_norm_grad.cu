@@ -6,13 +6,10 @@
  * registers from row to row and stored once per block.  The second adds the blocks' sums in order, so that the
  * result does not depend on which CTA was first.
  */
-#include <atomic>
-
 #include "sifar_norm.cuh"
 
 namespace sifar {
 
-constexpr unsigned kGradCtas = 148;          /* one per SM: the row in flight and the sums over rows fill its registers */
 constexpr unsigned kSumWarps = 16;
 
 struct NormGradArgs {
@@ -23,190 +20,208 @@ struct NormGradArgs {
     void *dx, *dresidual;
     float *dgate;
     float *sum_post, *sum_pre, *sum_gate;    /* workspace: [block][pitch], [block][pitch], [block][2][pitch]; or NULL */
-    unsigned long long ld_dy, ld_dh, ld_h, ld_z, ld_gate, ld_dx, ld_dresidual;    /* bytes between two rows */
+    uint32_t ld_dy, ld_dh, ld_h, ld_z, ld_gate, ld_dx, ld_dresidual;         /* bytes between two rows */
     float alpha, beta, offset;
     uint32_t rows, cols, pitch, blocks, rows_per_gate, parts, stages;
     int P, post, pre;
 };
 
-/* Rows of block b: [block_start(b), block_start(b + 1)). */
-__host__ __device__ inline uint32_t block_start(uint32_t rows, uint32_t blocks, uint32_t b)
+/*
+ * End of the rows [begin, end) of a block that share a gate row, with acc = their sum of D * n1: it gives the gate's
+ * gradient, beta * (post_weight + offset) * acc, and adds beta * gate * acc to the post weight's.
+ * The gate's is final where all rows of the gate row are here.  Otherwise it is a part: place 0 of the block's two
+ * where it holds the block's first row, else place 1.
+ */
+template <int DT, bool VEC>
+__device__ __forceinline__ void end_of_gate(const NormGradArgs &a, const Columns<DT, VEC> &c, Items &acc, Items &post, const Items &gate,
+                                            uint32_t b, uint32_t first, uint32_t begin, uint32_t end)
 {
-    return (uint32_t)((unsigned long long)rows * b / blocks);
-}
-__host__ __device__ inline uint32_t block_of(uint32_t rows, uint32_t blocks, uint32_t row)
-{
-    return (uint32_t)((((unsigned long long)row + 1ull) * blocks - 1ull) / rows);
+#pragma unroll
+    for (int j = 0; j < kItems / 2; ++j) post.p[j] = __ffma2_rn(gate.p[j], acc.p[j], post.p[j]);
+    if (a.dgate) {
+        const Items w = load_factor<DT, VEC>(a.post_weight, a.offset, c);
+#pragma unroll
+        for (int j = 0; j < kItems / 2; ++j) acc.p[j] = __fmul2_rn(__fmul2_rn(acc.p[j], both(a.beta)), w.p[j]);
+        const uint32_t g = begin / a.rows_per_gate;
+        const unsigned long long g0 = (unsigned long long)g * a.rows_per_gate, g1 = g0 + a.rows_per_gate;
+        const bool whole = begin == g0 && (end == g1 || end == a.rows);
+        if (whole) store_f32(a.dgate + (size_t)g * a.cols, acc, c);
+        else store_f32(a.sum_gate + ((size_t)b * 2 + (begin == first ? 0 : 1)) * a.pitch, acc, c);
+    }
+    acc = all_items(0.0f);
 }
 
 /*
- * The gate gradient of one gate row, as far as this block's rows [begin, end) go.  All rows of the gate row: the
- * final value.  Otherwise a part of it: place 0 of the block's two where it holds the block's first row, else place 1.
+ * Both sums of a row in one pass.  With t = dh + r2 * a and f = beta * gate * (post_weight + offset) the second,
+ * sum(f * n1 * D) with D = t - r2 * m2 * n2, is sum(f * n1 * t) - r2 * m2 * sum(f * n1 * n2), so that neither has to
+ * wait for the other.
  */
-template <int DT, bool VEC>
-__device__ __forceinline__ void flush_gate(const NormGradArgs &a, const Columns<DT, VEC> &c, float (&acc)[kItems], uint32_t b,
-                                           uint32_t first, uint32_t begin, uint32_t end)
-{
-    const uint32_t g = begin / a.rows_per_gate;
-    const unsigned long long g0 = (unsigned long long)g * a.rows_per_gate, g1 = g0 + a.rows_per_gate;
-    const bool whole = begin == g0 && (end == g1 || end == a.rows);
-    if (whole) store_f32(a.dgate + (size_t)g * a.cols, acc, c);
-    else store_f32(a.sum_gate + ((size_t)b * 2 + (begin == first ? 0 : 1)) * a.pitch, acc, c);
-#pragma unroll
-    for (int j = 0; j < kItems; ++j) acc[j] = 0.0f;
-}
-
-template <int DT, bool VEC>
+template <int DT, bool VEC, bool POST, bool PRE>
 __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
+    constexpr int kSums = POST && PRE ? 3 : 1;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
-    __shared__ RowSum s;
+    __shared__ __align__(16) RowSum<kSums> s;
     grid_let_next_in();
-    const uint32_t tx = blockDim.x, t = threadIdx.x;
-    const uint32_t part = a.parts > 1 ? cluster_rank() : 0u;
+    const RowPlace p{blockDim.x, threadIdx.x, threadIdx.y, a.parts, a.parts > 1 ? cluster_rank() : 0u};
     clear_row_sum(s);
     __syncthreads();
-    if (a.parts > 1) { cluster_arrive(); cluster_wait(); }
+    if (a.parts > 1) { cluster_arrive(); cluster_wait(); }           /* all CTAs of the cluster have started */
     const uint32_t b = (blockIdx.x / a.parts) * blockDim.y + threadIdx.y;
     const bool live = b < a.blocks;
     const uint32_t first = live ? block_start(a.rows, a.blocks, b) : 0u, end = live ? block_start(a.rows, a.blocks, b + 1) : 0u;
-    const uint32_t turns = (a.rows + a.blocks - 1) / a.blocks;        /* the same for all threads: they meet in the sums */
-    const Columns<DT, VEC> all(part, tx, t, a.cols);
-    const Ring<DT, VEC> ring(ring_bytes);
-    const uint32_t partials = a.pre ? (uint32_t)a.P : 0u, arrays = partials + (a.pre ? 1u : 0u) + (a.dh ? 1u : 0u) + (a.z ? 1u : 0u);
+    /* blocks of a CTA that meet in its barrier take the same number of turns, the others end with their rows */
+    const uint32_t turns = blockDim.y > 1 && p.tx > 32 ? (a.rows + a.blocks - 1) / a.blocks : end - first;
+    const Columns<DT, VEC> c(p.part, p.tx, p.t, a.cols);
+    const Lane<DT, VEC> l(c);
+    const Ring<DT, VEC> ring(ring_bytes, c);
+    const int partials = PRE ? a.P : 0;
+    const bool with_z = POST || a.z;
+    const uint32_t pitch = ring.threads * ring.bytes, stage_bytes = pitch * ((uint32_t)partials + (PRE ? 1u : 0u) + (a.dh ? 1u : 0u) + (with_z ? 1u : 0u));
     grid_wait();
 
-    /* row `row` into stage `stage`: the partials, then h, dh, z */
-    auto fetch = [&](uint32_t stage, uint32_t row) {
+    /* row `row` to place `to` of the ring: the partials, then h, dh, z */
+    auto fetch = [&](uint32_t to, uint32_t row) {
         if (row < end) {
-            uint32_t k = stage * arrays;
-            for (uint32_t r = 0; r < partials; ++r) ring.fetch(k++, static_cast<const char *>(a.dy[r]) + row * a.ld_dy, all);
-            if (a.pre) ring.fetch(k++, static_cast<const char *>(a.h) + row * a.ld_h, all);
-            if (a.dh) ring.fetch(k++, static_cast<const char *>(a.dh) + row * a.ld_dh, all);
-            if (a.z) ring.fetch(k++, static_cast<const char *>(a.z) + row * a.ld_z, all);
+            const unsigned long long at = row;
+            if (PRE) {
+                const unsigned long long o = at * a.ld_dy;
+                for (int r = 0; r < partials; ++r, to += pitch) ring.fetch(to, static_cast<const char *>(a.dy[r]) + o);
+                ring.fetch(to, static_cast<const char *>(a.h) + at * a.ld_h);
+                to += pitch;
+            }
+            if (a.dh) { ring.fetch(to, static_cast<const char *>(a.dh) + at * a.ld_dh); to += pitch; }
+            if (with_z) ring.fetch(to, static_cast<const char *>(a.z) + at * a.ld_z);
         }
         ring.commit();
     };
     if (Ring<DT, VEC>::possible)
-        for (uint32_t i = 0; i < a.stages; ++i) fetch(i, first + i);
+        for (uint32_t i = 0; i < a.stages; ++i) fetch(i * stage_bytes, first + i);
 
-    Raw<DT> w1, w2;
-    if (a.post_weight) load_any(w1, a.post_weight, all);
-    if (a.pre_weight) load_any(w2, a.pre_weight, all);
-    float acc1[kItems], acc2[kItems], accg[kItems];
+    const Items w2 = load_factor<DT, VEC>(a.pre_weight, a.offset, c);
+    Items f = load_factor<DT, VEC>(a.post_weight, a.offset, c);      /* of dx over D, from here on with beta * gate */
+    Items g = all_items(a.beta);                          /* beta * gate */
 #pragma unroll
-    for (int j = 0; j < kItems; ++j) acc1[j] = acc2[j] = accg[j] = 0.0f;
+    for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
+    Items post = all_items(0.0f), pre = post, acc = post;
     const float inv = 1.0f / (float)a.cols;
-    uint32_t segment = first, stage = 0;
-    int turn = 0;
-    float next1 = a.post && live ? a.stats[first] : 1.0f, next2 = a.pre && live ? a.stats[a.rows + first] : 1.0f;
+    uint32_t segment = first, gate_end = a.gate ? first : 0xFFFFFFFFu, place = 0;
+    const uint32_t places = stage_bytes * a.stages;
+    float next1 = POST && live ? a.stats[first] : 1.0f, next2 = PRE && live ? a.stats[a.rows + first] : 1.0f;
 
     for (uint32_t i = 0; i < turns; ++i) {
-        const bool on = first + i < end;
-        const uint32_t row = on ? first + i : 0u;
-        const Columns<DT, VEC> c(part, tx, t, on ? a.cols : 0u);
+        const uint32_t row = first + i;
+        const bool on = row < end;
+        const unsigned long long at = row;
         const float r1 = next1, r2 = next2;
-        if (first + i + 1 < end) {
-            if (a.post) next1 = a.stats[row + 1];
-            if (a.pre) next2 = a.stats[a.rows + row + 1];
+        if (row + 1 < end) {
+            if (POST) next1 = a.stats[row + 1];
+            if (PRE) next2 = a.stats[a.rows + row + 1];
         }
-        if (a.dgate && on && row != segment && row % a.rows_per_gate == 0) {
-            flush_gate(a, all, accg, b, first, segment, row);
+        if (on && row >= gate_end) {                      /* the rows of another gate row begin */
+            if (row != first) end_of_gate(a, c, acc, post, g, b, first, segment, row);
             segment = row;
-        }
-        Raw<DT> xg;
-        if (a.gate) load_any(xg, static_cast<const char *>(a.gate) + (row / a.rows_per_gate) * a.ld_gate, c);
-
-        float D[kItems], G[kItems];
-        Raw<DT> xn, xz;
-        if (Ring<DT, VEC>::possible) {
-            ring.wait(a.stages - 1);
-            uint32_t k = stage * arrays;
-            if (a.pre) {
-                Raw<DT> x;
-                ring.read(x, k++);
+            const uint32_t k = row / a.rows_per_gate;
+            gate_end = (k + 1) * a.rows_per_gate;
+            g = load_factor<DT, VEC>(static_cast<const char *>(a.gate) + (unsigned long long)k * a.ld_gate, 0.0f, c);
+            f = load_factor<DT, VEC>(a.post_weight, a.offset, c);
 #pragma unroll
-                for (int j = 0; j < kItems; ++j) G[j] = item(x, j);
-                for (uint32_t r = 1; r < partials; ++r) { ring.read(x, k++); add_items(G, x); }
-                ring.read(xn, k++);
+            for (int j = 0; j < kItems / 2; ++j) {
+                g.p[j] = __fmul2_rn(g.p[j], both(a.beta));
+                f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
             }
+        }
+
+        /* D: the gradient of h; G: of the normed h; n2, n1: h and z in units of their root mean square */
+        Items D, G, n2, n1;
+        float sum[kSums] = {};
+        if (on) {
             Raw<DT> x;
-            if (a.dh) ring.read(x, k++);
-#pragma unroll
-            for (int j = 0; j < kItems; ++j) D[j] = a.dh ? item(x, j) : 0.0f;
-            if (a.z) ring.read(xz, k);
-            fetch(stage, first + i + a.stages);            /* the thread has read its places */
-            stage = stage + 1 == a.stages ? 0u : stage + 1;
-        } else {
-            if (a.pre) {
-                Raw<DT> x;
-                load_row(x, static_cast<const char *>(a.dy[0]) + row * a.ld_dy, c);
-#pragma unroll
-                for (int j = 0; j < kItems; ++j) G[j] = item(x, j);
-                for (uint32_t r = 1; r < partials; ++r) {
-                    load_row(x, static_cast<const char *>(a.dy[r]) + row * a.ld_dy, c);
-                    add_items(G, x);
+            if (Ring<DT, VEC>::possible) {
+                ring.wait(a.stages - 1);
+                uint32_t from = place;
+                if (PRE) {
+                    ring.read(x, from);
+                    from += pitch;
+                    G = items(x);
+                    for (int r = 1; r < partials; ++r, from += pitch) { ring.read(x, from); add_items(G, x); }
+                    ring.read(x, from);
+                    from += pitch;
+                    n2 = items(x);
                 }
-                load_row(xn, static_cast<const char *>(a.h) + row * a.ld_h, c);
+                D = all_items(0.0f);
+                if (a.dh) { ring.read(x, from); from += pitch; D = items(x); }
+                if (with_z) { ring.read(x, from); n1 = items(x); }
+                fetch(place, row + a.stages);             /* the thread has read its places */
+                place = place + stage_bytes == places ? 0u : place + stage_bytes;
+            } else {
+                if (PRE) {
+                    load_row(x, static_cast<const char *>(a.dy[0]) + at * a.ld_dy, c);
+                    G = items(x);
+#pragma unroll 4
+                    for (int r = 1; r < partials; ++r) {
+                        load_row(x, static_cast<const char *>(a.dy[r]) + at * a.ld_dy, c);
+                        add_items(G, x);
+                    }
+                    load_row(x, static_cast<const char *>(a.h) + at * a.ld_h, c);
+                    n2 = items(x);
+                }
+                D = all_items(0.0f);
+                if (a.dh) { load_row(x, static_cast<const char *>(a.dh) + at * a.ld_dh, c); D = items(x); }
+                if (with_z) { load_row(x, static_cast<const char *>(a.z) + at * a.ld_z, c); n1 = items(x); }
             }
-            Raw<DT> x;
-            if (a.dh) load_row(x, static_cast<const char *>(a.dh) + row * a.ld_dh, c);
+            float2 q2 = both(0.0f), qt = q2, qn = q2;     /* sums of a * n2, f * n1 * t, f * n1 * n2 */
 #pragma unroll
-            for (int j = 0; j < kItems; ++j) D[j] = a.dh ? item(x, j) : 0.0f;
-            if (a.z) load_row(xz, static_cast<const char *>(a.z) + row * a.ld_z, c);
-        }
-        if (!on) {                                         /* nothing was fetched for this thread */
-#pragma unroll
-            for (int j = 0; j < kItems; ++j) D[j] = G[j] = 0.0f;
-            xn = xz = Raw<DT>{};
-        }
-
-        if (a.pre) {
-            float q = 0.0f;
-#pragma unroll
-            for (int j = 0; j < kItems; ++j) {
-                const float n2 = item(xn, j) * r2;
-                acc2[j] = fmaf(G[j], n2, acc2[j]);
-                if (a.pre_weight) G[j] *= item(w2, j) + a.offset;
-                q = fmaf(G[j], n2, q);
+            for (int j = 0; j < kItems / 2; ++j) {
+                if (PRE) {
+                    n2.p[j] = __fmul2_rn(n2.p[j], both(r2));
+                    pre.p[j] = __ffma2_rn(G.p[j], n2.p[j], pre.p[j]);
+                    G.p[j] = __fmul2_rn(G.p[j], w2.p[j]);
+                    q2 = __ffma2_rn(G.p[j], n2.p[j], q2);
+                    D.p[j] = __ffma2_rn(both(r2), G.p[j], D.p[j]);
+                }
+                if (POST) {
+                    n1.p[j] = __fmul2_rn(n1.p[j], both(r1));
+                    const float2 fn = __fmul2_rn(f.p[j], n1.p[j]);
+                    qt = __ffma2_rn(fn, D.p[j], qt);
+                    if (PRE) qn = __ffma2_rn(fn, n2.p[j], qn);
+                }
             }
-            const float m = row_sum(q, s, turn, tx, t, threadIdx.y, a.parts, part) * inv;
-            turn ^= 1;
+            sum[0] = PRE ? q2.x + q2.y : qt.x + qt.y;
+            if (kSums == 3) { sum[1 % kSums] = qt.x + qt.y; sum[2 % kSums] = qn.x + qn.y; }
+        }
+        if (POST || PRE) row_sums(sum, s, i, p);
+        if (!on) continue;
+        const float m2 = PRE ? r2 * (sum[0] * inv) : 0.0f;
+        const float m1 = !POST ? 0.0f : PRE ? (sum[1 % kSums] - m2 * sum[2 % kSums]) * inv : sum[0] * inv;
+        if (PRE) {
 #pragma unroll
-            for (int j = 0; j < kItems; ++j) D[j] = fmaf(r2, fmaf(-m, item(xn, j) * r2, G[j]), D[j]);
+            for (int j = 0; j < kItems / 2; ++j) D.p[j] = __ffma2_rn(both(-m2), n2.p[j], D.p[j]);
         }
         if (a.dresidual) {
-            float o[kItems];
+            Items o;
 #pragma unroll
-            for (int j = 0; j < kItems; ++j) o[j] = a.alpha * D[j];
-            store_row(static_cast<char *>(a.dresidual) + row * a.ld_dresidual, o, c);
+            for (int j = 0; j < kItems / 2; ++j) o.p[j] = __fmul2_rn(both(a.alpha), D.p[j]);
+            store_items(static_cast<char *>(a.dresidual) + at * a.ld_dresidual, o, c, l);
         }
-        float q = 0.0f;
+        if (with_z) {
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) {
-            const float w = a.post && a.post_weight ? item(w1, j) + a.offset : 1.0f;
-            const float n1 = a.z ? item(xz, j) * r1 : 0.0f;
-            if (a.dgate) accg[j] = fmaf(a.beta * D[j], n1 * w, accg[j]);
-            D[j] *= a.gate ? a.beta * item(xg, j) : a.beta;
-            if (a.post) {
-                acc1[j] = fmaf(D[j], n1, acc1[j]);
-                D[j] *= w;
-                q = fmaf(D[j], n1, q);
+            for (int j = 0; j < kItems / 2; ++j) acc.p[j] = __ffma2_rn(D.p[j], n1.p[j], acc.p[j]);
+        }
+        if (a.dx) {
+#pragma unroll
+            for (int j = 0; j < kItems / 2; ++j) {
+                D.p[j] = __fmul2_rn(f.p[j], D.p[j]);
+                if (POST) D.p[j] = __fmul2_rn(both(r1), __ffma2_rn(both(-m1), n1.p[j], D.p[j]));
             }
+            store_items(static_cast<char *>(a.dx) + at * a.ld_dx, D, c, l);
         }
-        if (a.post) {
-            const float m = row_sum(q, s, turn, tx, t, threadIdx.y, a.parts, part) * inv;
-            turn ^= 1;
-#pragma unroll
-            for (int j = 0; j < kItems; ++j) D[j] = r1 * fmaf(-m, item(xz, j) * r1, D[j]);
-        }
-        if (a.dx) store_row(static_cast<char *>(a.dx) + row * a.ld_dx, D, c);
     }
     if (Ring<DT, VEC>::possible) ring.wait(0);
     if (!live) return;
-    if (a.sum_post) store_f32(a.sum_post + (size_t)b * a.pitch, acc1, all);
-    if (a.sum_pre) store_f32(a.sum_pre + (size_t)b * a.pitch, acc2, all);
-    if (a.dgate) flush_gate(a, all, accg, b, first, segment, end);
+    end_of_gate(a, c, acc, post, g, b, first, segment, end);
+    if (a.sum_post) store_f32(a.sum_post + (size_t)b * a.pitch, post, c);
+    if (a.sum_pre) store_f32(a.sum_pre + (size_t)b * a.pitch, pre, c);
 }
 
 struct NormSumArgs {
@@ -267,47 +282,22 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const NormSu
     }
 }
 
-/* Blocks of rows, and how many of them a CTA holds. */
-struct GradShape {
-    RowShape row;
-    unsigned ry;
-    uint32_t blocks;
-    size_t pitch;
-};
-static GradShape grad_shape(size_t rows, size_t cols)
+template <int DT, bool VEC, bool POST, bool PRE>
+static cudaError_t launch_grad_n(const RowShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
-    GradShape s;
-    s.row = row_shape(cols);
-    s.ry = kMaxRowThreads / s.row.tx;
-    while (s.ry > 1 && rows <= (size_t)(s.ry - 1) * kGradCtas) --s.ry;
-    const size_t most = (size_t)(kGradCtas / s.row.parts) * s.ry;
-    s.blocks = (uint32_t)(rows < most ? rows : most);
-    s.pitch = (cols + kItems - 1) / kItems * kItems;
-    return s;
+    static std::atomic<unsigned long long> ready{0};
+    return launch_rows<DT, VEC>(k_block_norm_grad<DT, VEC, POST, PRE>, ready, sh, arrays, stream, a);
 }
 
-/* The ring takes the shared memory that a CTA can have: the attribute is set once per kernel and device. */
 template <int DT, bool VEC>
-static cudaError_t launch_grad(dim3 grid, dim3 block, cudaStream_t stream, NormGradArgs &a, unsigned arrays)
+static cudaError_t launch_grad(const RowShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
-    const size_t row = (size_t)block.x * block.y * arrays * Ring<DT, VEC>::bytes;
-    size_t smem = 0;
-    a.stages = 1;
-    if (Ring<DT, VEC>::possible) {
-        a.stages = (uint32_t)(kRingBytes / row < kMaxStages ? kRingBytes / row : kMaxStages);
-        smem = row * a.stages;
-    }
-    static std::atomic<unsigned long long> ready{0};       /* a bit per device */
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (Ring<DT, VEC>::possible && (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1ull))) {
-        e = cudaFuncSetAttribute(k_block_norm_grad<DT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
-        if (e != cudaSuccess) return e;
-        if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_release);
-    }
-    return launch_op(k_block_norm_grad<DT, VEC>, grid, block, a.parts, smem, stream, a);
+    if (a.post) return a.pre ? launch_grad_n<DT, VEC, true, true>(sh, arrays, stream, a) : launch_grad_n<DT, VEC, true, false>(sh, arrays, stream, a);
+    return a.pre ? launch_grad_n<DT, VEC, false, true>(sh, arrays, stream, a) : launch_grad_n<DT, VEC, false, false>(sh, arrays, stream, a);
 }
+
+/* Words between two blocks' sums. */
+static size_t sum_pitch(size_t cols) { return (cols + kItems - 1) / kItems * kItems; }
 
 }  /* namespace sifar */
 
@@ -331,9 +321,9 @@ static int check_grad_sizes(const sifar_block_norm_grad_args *g, const char *fn)
 extern "C" size_t sifar_block_norm_backward_workspace(const sifar_block_norm_grad_args *g)
 {
     if (check_grad_sizes(g, "sifar_block_norm_backward_workspace")) return 0;
-    const GradShape s = grad_shape(g->rows, g->cols);
+    const RowShape s = row_shape(g->rows, g->cols);
     const size_t arrays = (g->dpost_weight ? 1 : 0) + (g->dpre_weight ? 1 : 0) + (g->dgate ? 2 : 0);
-    return arrays * s.blocks * s.pitch * sizeof(float);
+    return arrays * s.blocks * sum_pitch(g->cols) * sizeof(float);
 }
 
 extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, void *stream)
@@ -392,9 +382,9 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     if (need) all[n++] = RowArray{"workspace", g->workspace, 1, need / sizeof(float), need / sizeof(float), sizeof(float), true};
     if (int rc = check_arrays(fn, all, n)) return rc;
 
-    const GradShape sh = grad_shape(rows, cols);
+    const RowShape sh = row_shape(rows, cols);
     float *ws = static_cast<float *>(g->workspace);
-    const size_t plane = (size_t)sh.blocks * sh.pitch;
+    const size_t plane = (size_t)sh.blocks * sum_pitch(cols);
     NormGradArgs a;
     for (int r = 0; r < kMaxRanks; ++r) a.dy[r] = pre && r < g->P ? g->dy[r] : nullptr;
     a.dh = g->dh; a.h = g->h; a.z = need_z ? g->z : nullptr; a.stats = g->stats;
@@ -403,21 +393,19 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     a.sum_post = g->dpost_weight ? ws : nullptr; ws += g->dpost_weight ? plane : 0;
     a.sum_pre = g->dpre_weight ? ws : nullptr; ws += g->dpre_weight ? plane : 0;
     a.sum_gate = g->dgate ? ws : nullptr;
-    a.ld_dy = or_cols(g->ld_dy, cols) * es; a.ld_dh = dh.ld * es; a.ld_h = or_cols(g->ld_h, cols) * es;
-    a.ld_z = or_cols(g->ld_z, cols) * es; a.ld_gate = or_cols(g->ld_gate, cols) * es;
-    a.ld_dx = or_cols(g->ld_dx, cols) * es; a.ld_dresidual = dres.ld * es;
+    const auto bytes = [&](size_t ld) { return (uint32_t)(or_cols(ld, cols) * es); };
+    a.ld_dy = bytes(g->ld_dy); a.ld_dh = bytes(g->ld_dh); a.ld_h = bytes(g->ld_h); a.ld_z = bytes(g->ld_z);
+    a.ld_gate = bytes(g->ld_gate); a.ld_dx = bytes(g->ld_dx); a.ld_dresidual = bytes(g->ld_dresidual);
     a.alpha = g->alpha; a.beta = g->beta; a.offset = g->weight_offset;
-    a.rows = (uint32_t)rows; a.cols = (uint32_t)cols; a.pitch = (uint32_t)sh.pitch; a.blocks = sh.blocks;
-    a.rows_per_gate = (uint32_t)span; a.parts = sh.row.parts;
+    a.rows = (uint32_t)rows; a.cols = (uint32_t)cols; a.pitch = (uint32_t)sum_pitch(cols); a.blocks = sh.blocks;
+    a.rows_per_gate = (uint32_t)span; a.parts = sh.parts;
     a.P = pre ? g->P : 1; a.post = post; a.pre = pre;
     if (rows) {
-        const dim3 grid((sh.blocks + sh.ry - 1) / sh.ry * sh.row.parts), block(sh.row.tx, sh.ry);
         const unsigned arrays = (pre ? (unsigned)g->P + 1u : 0u) + (g->dh ? 1u : 0u) + (need_z ? 1u : 0u);
         const cudaStream_t q = (cudaStream_t)stream;
-        const cudaError_t err = g->dtype == SIFAR_BF16 ? (vec ? launch_grad<SIFAR_BF16, true>(grid, block, q, a, arrays)
-                                                              : launch_grad<SIFAR_BF16, false>(grid, block, q, a, arrays))
-                                                       : (vec ? launch_grad<SIFAR_F32, true>(grid, block, q, a, arrays)
-                                                              : launch_grad<SIFAR_F32, false>(grid, block, q, a, arrays));
+        const cudaError_t err = g->dtype == SIFAR_BF16
+            ? (vec ? launch_grad<SIFAR_BF16, true>(sh, arrays, q, a) : launch_grad<SIFAR_BF16, false>(sh, arrays, q, a))
+            : (vec ? launch_grad<SIFAR_F32, true>(sh, arrays, q, a) : launch_grad<SIFAR_F32, false>(sh, arrays, q, a));
         SIFAR_CUDA(err);
     }
     if (g->dpost_weight || g->dpre_weight || g->dgate) {

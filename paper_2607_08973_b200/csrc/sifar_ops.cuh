@@ -43,12 +43,19 @@ __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-/* One word into the same place of CTA `rank`'s shared memory. */
-__device__ __forceinline__ void store_cluster_f32(float *local, uint32_t rank, float v)
+/* A value and its tag in one 8-byte word: written into the same place of CTA `rank`'s shared memory, read from the own. */
+__device__ __forceinline__ void store_cluster_tagged(unsigned long long *local, uint32_t rank, float v, uint32_t tag)
 {
     const uint32_t a = (uint32_t)__cvta_generic_to_shared(local);
-    asm volatile("{\n\t.reg .u32 q;\n\tmapa.shared::cluster.u32 q, %0, %1;\n\tst.shared::cluster.f32 [q], %2;\n\t}"
-                 :: "r"(a), "r"(rank), "f"(v) : "memory");
+    const unsigned long long w = (unsigned long long)tag << 32 | __float_as_uint(v);
+    asm volatile("{\n\t.reg .u32 q;\n\tmapa.shared::cluster.u32 q, %0, %1;\n\tst.relaxed.cluster.shared::cluster.b64 [q], %2;\n\t}"
+                 :: "r"(a), "r"(rank), "l"(w) : "memory");
+}
+__device__ __forceinline__ unsigned long long load_tagged(const unsigned long long *local)
+{
+    unsigned long long w;
+    asm volatile("ld.relaxed.cluster.shared::cta.b64 %0, [%1];" : "=l"(w) : "r"((uint32_t)__cvta_generic_to_shared(local)) : "memory");
+    return w;
 }
 
 /* ------------------------------------------------------------------------ */
@@ -88,7 +95,7 @@ struct RowArray {
 };
 
 constexpr size_t kMaxRows = (size_t)1 << 31;
-constexpr size_t kMaxStride = (size_t)1 << 40;
+constexpr size_t kMaxStride = ((size_t)1 << 30) - 1;      /* elements; in bytes it fits 32 bits */
 
 /* Whether two arrays share an element.  Rows of one stride side by side in one buffer do not. */
 inline bool share_elements(const RowArray &a, const RowArray &b)

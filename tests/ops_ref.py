@@ -77,7 +77,11 @@ def norm_grad(dys, dh, h, z, r1, r2, w1, gate, w2, *, post, pre, alpha, beta, of
         out["dw2"] = (G * n2).sum(0)
         err["dw2"] = (eG * n2.abs() + (rows + 40) * U * (G * n2).abs()).sum(0)
         eD = r2[:, None] * (ea + n2.abs() * em + 4 * U * (a.abs() + (n2 * m).abs())) + 2 * U * D.abs()
+        t, et = D + r2[:, None] * a, r2[:, None] * (ea + 3 * U * a.abs()) + U * (D + r2[:, None] * a).abs()
+        m2, em2, n2sum = r2[:, None] * m, r2[:, None] * em + 2 * U * (r2[:, None] * m).abs(), n2
         D = D + r2[:, None] * (a - n2 * m)
+    else:
+        t, et, m2, em2, n2sum = D, 0.0 * D, torch.zeros(rows, 1, dtype=torch.float64), torch.zeros(rows, 1, dtype=torch.float64), 0.0 * D
     eD = eD + U * D.abs()
     out["dres"], err["dres"] = alpha * D, abs(alpha) * eD + U * (alpha * D).abs()
     g = gate_of_rows(gate, rows, span)
@@ -96,7 +100,13 @@ def norm_grad(dys, dh, h, z, r1, r2, w1, gate, w2, *, post, pre, alpha, beta, of
         b = d * f1
         eb = ed * f1.abs() + 3 * U * b.abs()
         m = (b * n1).mean(1, keepdim=True)
-        em = (eb * n1.abs() + (DEPTH + 8) * U * (b * n1).abs()).mean(1, keepdim=True) + 2 * U * m.abs()
+        # the kernel takes this sum as that of (b n1 with t = dh + r2 a for D) - r2 m2 * that of (b n1 with n2 for D), so
+        # that both sums of a row need one pass: each term has three products and the sum's DEPTH, t and m2 their own error
+        fn = (beta if g is None else beta * g) * f1 * n1
+        em = (fn.abs() * et + (DEPTH + 8) * U * (fn * t).abs()).mean(1, keepdim=True)
+        em = em + m2.abs() * ((DEPTH + 8) * U * (fn * n2sum).abs()).mean(1, keepdim=True)
+        em = em + em2 * (fn * n2sum).abs().mean(1, keepdim=True)
+        em = em + 3 * U * ((fn * t).abs().mean(1, keepdim=True) + (m2 * fn * n2sum).abs().mean(1, keepdim=True))
         ed = r1[:, None] * (eb + n1.abs() * em + 5 * U * (b.abs() + (n1 * m).abs()))
         d = r1[:, None] * (b - n1 * m)
     out["dx"], err["dx"] = d, ed
