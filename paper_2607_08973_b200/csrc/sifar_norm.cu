@@ -13,17 +13,17 @@ struct NormArgs {
     uint32_t ld_x, ld_residual, ld_gate, ld_z, ld_h, ld_y;    /* bytes between two rows */
     float alpha, beta, eps, offset;
     uint32_t rows, cols, parts, rows_per_gate;
-    int P, post, pre, aligned;               /* aligned: the weights and the gate are, as the rows, on 16 bytes */
+    int P, post, pre;
 };
 
 /*
  * One row per threadIdx.y (and cluster).  All loads of a row go out before the first sum; z, h and y never leave the
  * registers between.  PT is P or the next power of two above it.
  */
-template <int DT, int PT> constexpr int kNormCtasPerSm = DT == SIFAR_BF16 ? (PT <= 2 ? 3 : 2) : (PT <= 2 ? 2 : 1);
+template <int PT> constexpr int kNormRegisters = PT <= 4 ? 72 : 128;
 
-template <int DT, int PT, bool VEC>
-__global__ void __launch_bounds__(kMaxRowThreads, kNormCtasPerSm<DT, PT>) k_block_norm(const __grid_constant__ NormArgs a)
+template <typename F, int PT>
+__global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(kNormRegisters<PT>) k_block_norm(const __grid_constant__ NormArgs a)
 {
     __shared__ __align__(16) RowSum<1> s;
     grid_let_next_in();
@@ -33,36 +33,32 @@ __global__ void __launch_bounds__(kMaxRowThreads, kNormCtasPerSm<DT, PT>) k_bloc
     if (a.parts > 1) cluster_arrive();                   /* a CTA's shared memory may be written once it has started */
     const uint32_t row = (blockIdx.x / a.parts) * blockDim.y + threadIdx.y;
     const bool live = row < a.rows;
-    const Columns<DT, VEC> c(p.part, p.tx, p.t, live ? a.cols : 0u);
-    const Lane<DT, VEC> l(c);
+    const Columns<F> c(p.part, p.tx, p.t, live ? a.cols : 0u);
+    const Lane<F> l(c);
     const unsigned long long at = live ? row : 0u;
     grid_wait();
 
-    Raw<DT> x[PT], res, rg, rw1, rw2;
+    Raw<F> x[PT], res, rg, rw1, rw2;
     const char *gate = nullptr;
     if (a.gate) gate = static_cast<const char *>(a.gate) + (unsigned long long)((uint32_t)at / a.rows_per_gate) * a.ld_gate;
-    /* the weights and the gate may lack the rows' alignment: those warps look at every element too */
-    if (!l.ragged && a.aligned) {
+    if (!l.ragged) {
         const unsigned long long o = at * a.ld_x;
 #pragma unroll
         for (int r = 0; r < PT; ++r)
             if (r < a.P) load_whole(x[r], static_cast<const char *>(a.x[r]) + o, l);
         if (a.residual) load_whole(res, static_cast<const char *>(a.residual) + at * a.ld_residual, l);
-        if (a.gate) load_whole(rg, gate, l);
-        if (a.post_weight) load_whole(rw1, a.post_weight, l);
-        if (a.pre_weight) load_whole(rw2, a.pre_weight, l);
     } else {
 #pragma unroll
         for (int r = 0; r < PT; ++r)
-            if (r < a.P) load_row(x[r], static_cast<const char *>(a.x[r]) + at * a.ld_x, c);
-        if (a.residual) load_row(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c);
-        if (a.gate) load_any(rg, gate, c);
-        if (a.post_weight) load_any(rw1, a.post_weight, c);
-        if (a.pre_weight) load_any(rw2, a.pre_weight, c);
+            if (r < a.P) load_each(x[r], static_cast<const char *>(a.x[r]) + at * a.ld_x, c);
+        if (a.residual) load_each(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c);
     }
+    if (a.gate) load_weight(rg, gate, c, l);
+    if (a.post_weight) load_weight(rw1, a.post_weight, c, l);
+    if (a.pre_weight) load_weight(rw2, a.pre_weight, c, l);
     if (a.parts > 1) cluster_wait();
 
-    Items f = items(x[0]);
+    Items<F> f = items<F>(x[0]);
 #pragma unroll
     for (int r = 1; r < PT; ++r)
         if (r < a.P) add_items(f, x[r]);
@@ -75,21 +71,21 @@ __global__ void __launch_bounds__(kMaxRowThreads, kNormCtasPerSm<DT, PT>) k_bloc
         row_sums(sum, s, call++, p);
         r1 = rrms(sum[0], a.cols, a.eps);
 #pragma unroll
-        for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r1));
+        for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r1));
         if (a.post_weight) {
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair(rw1, j), both(a.offset)));
+            for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair<F>(rw1, j), both(a.offset)));
         }
     }
     if (a.gate) {
 #pragma unroll
-        for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], pair(rg, j));
+        for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], pair<F>(rg, j));
     }
 #pragma unroll
-    for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], both(a.beta));
+    for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], both(a.beta));
     if (a.residual) {
 #pragma unroll
-        for (int j = 0; j < kItems / 2; ++j) f.p[j] = __ffma2_rn(both(a.alpha), pair(res, j), f.p[j]);
+        for (int j = 0; j < f.N; ++j) f.p[j] = __ffma2_rn(both(a.alpha), pair<F>(res, j), f.p[j]);
     }
     if (a.h) store_items(static_cast<char *>(a.h) + at * a.ld_h, f, c, l);
     if (a.pre) {
@@ -98,10 +94,10 @@ __global__ void __launch_bounds__(kMaxRowThreads, kNormCtasPerSm<DT, PT>) k_bloc
         r2 = rrms(sum[0], a.cols, a.eps);
         if (a.y) {
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r2));
+            for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r2));
             if (a.pre_weight) {
 #pragma unroll
-                for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair(rw2, j), both(a.offset)));
+                for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair<F>(rw2, j), both(a.offset)));
             }
             store_items(static_cast<char *>(a.y) + at * a.ld_y, f, c, l);
         }
@@ -112,11 +108,14 @@ __global__ void __launch_bounds__(kMaxRowThreads, kNormCtasPerSm<DT, PT>) k_bloc
     }
 }
 
+/* 32 bytes of every array per thread */
+template <int DT> constexpr int kNormWords = 8;
+
 template <int DT, int PT>
 static cudaError_t launch_norm_p(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormArgs &a)
 {
-    return vec ? launch_op(k_block_norm<DT, PT, true>, grid, block, cluster, 0, stream, a)
-               : launch_op(k_block_norm<DT, PT, false>, grid, block, cluster, 0, stream, a);
+    return vec ? launch_op(k_block_norm<Form<DT, kNormWords<DT>, true>, PT>, grid, block, cluster, 0, stream, a)
+               : launch_op(k_block_norm<Form<DT, kNormWords<DT>, false>, PT>, grid, block, cluster, 0, stream, a);
 }
 
 template <int DT>
@@ -172,12 +171,9 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     all[n++] = RowArray{"y", g->y, rows, cols, or_cols(g->ld_y, cols), es, true};
     bool vec = rows_aligned16(residual);
     for (int i = 0; i < n; ++i) vec = vec && rows_aligned16(all[i]);
-    const int weights = n;
     all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
     all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
     all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
-    bool aligned = true;
-    for (int i = weights; i < n; ++i) aligned = aligned && rows_aligned16(all[i]);
     all[n++] = RowArray{"stats", g->stats, 1, 2 * rows, 2 * rows, sizeof(float), true};
     if (int rc = check_arrays(fn, all, n)) return rc;
 
@@ -192,11 +188,12 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     a.ld_z = bytes(g->ld_z); a.ld_h = bytes(g->ld_h); a.ld_y = bytes(g->ld_y);
     a.rows_per_gate = (uint32_t)span;
     a.alpha = g->alpha; a.beta = g->beta; a.eps = g->eps; a.offset = g->weight_offset;
-    a.P = g->P; a.post = g->post_norm != 0; a.pre = g->pre_norm != 0; a.aligned = aligned;
-    const RowShape sh = row_shape(rows, cols);
+    a.P = g->P; a.post = g->post_norm != 0; a.pre = g->pre_norm != 0;
+    const RowShape sh = row_shape((g->dtype == SIFAR_BF16 ? kNormWords<SIFAR_BF16> : kNormWords<SIFAR_F32>) * 4 / (int)es, cols);
     a.parts = sh.parts;
+    /* short rows: several to a CTA once there is one for every SM */
     unsigned ry = 1;
-    while (sh.parts == 1 && 2 * ry * sh.tx <= 256 && rows >= (size_t)2 * ry * 2 * kNormCtas) ry *= 2;
+    while (sh.parts == 1 && 2 * ry * sh.tx <= 256 && rows >= (size_t)2 * ry * 2 * kSms) ry *= 2;
     const unsigned long long grid = (rows + ry - 1) / ry * sh.parts;
     if (grid > 0x7FFFFFFFull) { set_error("%s: too many rows of this width", fn); return SIFAR_ERR_INVALID; }
     const dim3 gd((unsigned)grid), bd(sh.tx, ry);

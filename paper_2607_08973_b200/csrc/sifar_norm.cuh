@@ -1,9 +1,11 @@
 /*
- * How the norm kernels lay a row over threads, and the sum over a row.
+ * How the norm kernels lay a row over threads, and the sums over a row.
  *
- * A thread holds kItems elements of a row in registers from its first load to its last store, so a row is read once
- * however many sums go over it.  A row takes `tx` threads of a CTA; where it is longer than kMaxRowThreads * kItems
- * elements, a cluster of up to eight CTAs holds it and its sums meet in their shared memory.
+ * A thread holds 16 or 32 bytes of every array of a row in registers from its first load to its
+ * last store, so a row is read once however many sums go over it.  A row takes `tx` threads of a CTA; where it is longer
+ * than a CTA of kMaxRowThreads holds, a cluster of up to eight CTAs has it and its sums meet in their shared memory.
+ * (16 bytes of bf16 per thread: 109 us for the backward pass of 8192 x 4096 and two ranks instead of what stands there;
+ * what a thread does per row whatever its items, addresses, exchanges, barriers, was more than half of its work.)
  */
 #ifndef SIFAR_NORM_CUH
 #define SIFAR_NORM_CUH
@@ -14,18 +16,27 @@
 
 namespace sifar {
 
-constexpr int kItems = 8;                    /* elements of a row per thread: 16 bytes of bf16, 2 x 16 bytes of fp32 */
 constexpr int kMaxRowThreads = 512;
 constexpr unsigned kMaxNormCluster = 8;
-static_assert(SIFAR_NORM_MAX_COLS == kItems * kMaxRowThreads * (int)kMaxNormCluster, "columns a cluster holds");
 
-/* The columns of a thread: item j is column at(j). */
-template <int DT, bool VEC> struct Columns {
-    static constexpr int EPV = VEC ? Elem<DT>::per_vec : 1;      /* neighbours that are fetched together */
-    static constexpr int NV = kItems / EPV;
+/* The form of a kernel: element type, 32-bit words of a row and array per thread, 16-byte accesses (VEC) or elements. */
+template <int DT_, int W_, bool VEC_> struct Form {
+    static constexpr int DT = DT_, W = W_;
+    static constexpr bool VEC = VEC_;
+    using T = typename Elem<DT_>::type;
+    static constexpr uint32_t es = sizeof(T);
+    static constexpr int items = W_ * 4 / (int)sizeof(T), pairs = items / 2;
+    static constexpr int vectors = W_ / 4, vector_pairs = pairs / vectors;       /* of 16 bytes */
+    static_assert(SIFAR_NORM_MAX_COLS <= items * kMaxRowThreads * (int)kMaxNormCluster, "columns that a cluster holds");
+};
+
+/* The columns of a thread: item j is column at(j).  VEC: two runs of 16 bytes, else single elements. */
+template <typename F> struct Columns {
+    static constexpr int N = F::items;
+    static constexpr int EPV = F::VEC ? Elem<F::DT>::per_vec : 1;      /* neighbours that are fetched together */
     uint32_t first, step, cols;
     __device__ __forceinline__ Columns(uint32_t part, uint32_t tx, uint32_t t, uint32_t cols_)
-        : first((part * NV * tx + t) * EPV), step(tx * EPV), cols(cols_) {}
+        : first(part * N * tx + t * EPV), step(tx * EPV), cols(cols_) {}
     __device__ __forceinline__ uint32_t at(int j) const { return first + (uint32_t)(j / EPV) * step + (uint32_t)(j % EPV); }
     __device__ __forceinline__ bool has(int j) const { return at(j) < cols; }
 };
@@ -35,216 +46,175 @@ template <int DT, bool VEC> struct Columns {
  * same and its value is left out later), which of them exist, and whether the warp holds the row's last, short vector
  * and has to look at every element.  Computed once: all rows are alike.
  */
-template <int DT, bool VEC> struct Lane {
-    static constexpr int NV = VEC ? Columns<DT, VEC>::NV : 1;
-    uint32_t at[NV];
-    bool in[NV];
+template <typename F> struct Lane {
+    uint32_t at[F::vectors];
+    bool in[F::vectors];
     bool ragged;
-    __device__ __forceinline__ explicit Lane(const Columns<DT, VEC> &c)
+    __device__ __forceinline__ explicit Lane(const Columns<F> &c)
     {
-        constexpr uint32_t es = sizeof(typename Elem<DT>::type);
-        bool cut = !VEC;
+                bool cut = !F::VEC;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
+        for (int v = 0; v < F::vectors; ++v) {
             const uint32_t i = c.at(v * c.EPV);
             in[v] = i < c.cols;
-            at[v] = in[v] ? i * es : 0u;
+            at[v] = in[v] ? i * F::es : 0u;
             cut = cut || (in[v] && i + c.EPV > c.cols);
         }
         ragged = __any_sync(0xFFFFFFFFu, cut);
     }
 };
 
-/* The thread's items of one row as they lie in memory: packed words. */
-template <int DT> struct Raw { uint32_t w[kItems / (DT == SIFAR_BF16 ? 2 : 1)]; };
+/* The thread's items of one row as they lie in memory. */
+template <typename F> struct Raw { uint32_t w[F::W]; };
 
-template <int DT, bool VEC>
-__device__ __forceinline__ void load_row(Raw<DT> &x, const void *row, const Columns<DT, VEC> &c)
+/* Every element looked at: absent ones are 0.  The first four words and the last four, or one of the two. */
+template <typename F>
+__device__ __forceinline__ void load_half(Raw<F> &x, int v, const void *row, const Columns<F> &c)
 {
-    using T = typename Elem<DT>::type;
+    using T = typename F::T;
     const T *p = static_cast<const T *>(row);
-    constexpr int W = VEC ? 4 : 1;
-    if (VEC) {
 #pragma unroll
-        for (int v = 0; v < Columns<DT, VEC>::NV; ++v) {
-            const uint32_t i = c.at(v * c.EPV);
-            uint4 q = make_uint4(0u, 0u, 0u, 0u);
-            if (i + c.EPV <= c.cols) {
-                q = *reinterpret_cast<const uint4 *>(p + i);
-            } else if (i < c.cols) {                      /* the row's last, short vector */
-                uint32_t t[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int k = 0; k < c.EPV; ++k)
-                    if (i + k < c.cols) {
-                        if (DT == SIFAR_BF16) t[k / 2] |= (uint32_t)p[i + k] << (16 * (k & 1));
-                        else t[k & 3] = p[i + k];
-                    }
-                q = make_uint4(t[0], t[1], t[2], t[3]);
-            }
-            x.w[(v * W + 0) % (sizeof x.w / 4)] = q.x;
-            x.w[(v * W + 1) % (sizeof x.w / 4)] = q.y;
-            x.w[(v * W + 2) % (sizeof x.w / 4)] = q.z;
-            x.w[(v * W + 3) % (sizeof x.w / 4)] = q.w;
+    for (int i = 4 * v; i < 4 * v + 4; ++i) {
+        if (F::DT == SIFAR_F32) {
+            x.w[i] = c.has(i) ? (uint32_t)p[c.at(i)] : 0u;
+        } else {
+            const uint32_t lo = c.has(2 * i) ? (uint32_t)p[c.at(2 * i)] : 0u, hi = c.has(2 * i + 1) ? (uint32_t)p[c.at(2 * i + 1)] : 0u;
+            x.w[i] = lo | hi << 16;
         }
-    } else if (DT == SIFAR_BF16) {
+    }
+}
+template <typename F>
+__device__ __forceinline__ void load_each(Raw<F> &x, const void *row, const Columns<F> &c)
+{
 #pragma unroll
-        for (int j = 0; j < kItems; j += 2) {
-            const uint32_t lo = c.has(j) ? (uint32_t)p[c.at(j)] : 0u, hi = c.has(j + 1) ? (uint32_t)p[c.at(j + 1)] : 0u;
-            x.w[(j / 2) % (sizeof x.w / 4)] = lo | hi << 16;
-        }
-    } else {
+    for (int v = 0; v < F::vectors; ++v) load_half(x, v, row, c);
+}
+
+/* Whole vectors of a row (its warp is not ragged); what lies behind the row's end is some other element of it. */
+template <typename F>
+__device__ __forceinline__ void load_whole(Raw<F> &x, const void *row, const Lane<F> &l)
+{
 #pragma unroll
-        for (int j = 0; j < kItems; ++j) x.w[j % (sizeof x.w / 4)] = c.has(j) ? (uint32_t)p[c.at(j)] : 0u;
+    for (int v = 0; v < F::vectors; ++v) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + l.at[v]);
+        x.w[4 * v] = q.x;
+        x.w[4 * v + 1] = q.y;
+        x.w[4 * v + 2] = q.z;
+        x.w[4 * v + 3] = q.w;
     }
 }
 
-/* The same where the array may lack the rows' alignment (weights, gates). */
-template <int DT, bool VEC>
-__device__ __forceinline__ void load_any(Raw<DT> &x, const void *row, const Columns<DT, VEC> &c)
+/* Weights and gates: they may lack the rows' alignment. */
+template <typename F>
+__device__ __forceinline__ void load_weight(Raw<F> &x, const void *row, const Columns<F> &c, const Lane<F> &l)
 {
-    if (!VEC || ((uintptr_t)row & 15u) == 0) { load_row(x, row, c); return; }
-    using T = typename Elem<DT>::type;
-    const T *p = static_cast<const T *>(row);
-#pragma unroll
-    for (int j = 0; j < kItems; ++j) {
-        const uint32_t q = c.has(j) ? (uint32_t)p[c.at(j)] : 0u;
-        if (DT == SIFAR_F32) x.w[j % (sizeof x.w / 4)] = q;
-        else x.w[j / 2 % (sizeof x.w / 4)] = (j & 1) ? x.w[j / 2 % (sizeof x.w / 4)] | q << 16 : q;
-    }
+    if (!l.ragged && ((uintptr_t)row & 15u) == 0) load_whole(x, row, l);
+    else load_each(x, row, c);
 }
 
 /*
- * A thread's items in binary32, two by two: the arithmetic below takes two per instruction (the packed forms round
- * each half as the plain ones do).
+ * A thread's items in binary32, two by two: the arithmetic takes two per instruction (the packed forms round each half
+ * as the plain ones do).
  */
-struct Items {
-    float2 p[kItems / 2];
+template <typename F> struct Items {
+    static constexpr int N = F::pairs;
+    float2 p[N];
 };
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-/* Whole vectors of a row (its warp is not ragged); what lies behind the row's end is some other element of it. */
-template <int DT, bool VEC>
-__device__ __forceinline__ void load_whole(Raw<DT> &x, const void *row, const Lane<DT, VEC> &l)
+template <typename F> __device__ __forceinline__ float2 pair(const Raw<F> &x, int i)
 {
-#pragma unroll
-    for (int v = 0; v < Lane<DT, VEC>::NV; ++v) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + l.at[v]);
-        x.w[(4 * v) % (sizeof x.w / 4)] = q.x;
-        x.w[(4 * v + 1) % (sizeof x.w / 4)] = q.y;
-        x.w[(4 * v + 2) % (sizeof x.w / 4)] = q.z;
-        x.w[(4 * v + 3) % (sizeof x.w / 4)] = q.w;
-    }
+    if (F::DT == SIFAR_BF16) return make_float2(bf16lo_to_f32(x.w[i % F::W]), bf16hi_to_f32(x.w[i % F::W]));
+    return make_float2(__uint_as_float(x.w[(2 * i) % F::W]), __uint_as_float(x.w[(2 * i + 1) % F::W]));
 }
-
-template <int DT> __device__ __forceinline__ float2 pair(const Raw<DT> &x, int i)
+template <typename F> __device__ __forceinline__ Items<F> items(const Raw<F> &x)
 {
-    if (DT == SIFAR_BF16) return make_float2(bf16lo_to_f32(x.w[i]), bf16hi_to_f32(x.w[i]));
-    return make_float2(__uint_as_float(x.w[(2 * i) % (sizeof x.w / 4)]), __uint_as_float(x.w[(2 * i + 1) % (sizeof x.w / 4)]));
-}
-template <int DT> __device__ __forceinline__ Items items(const Raw<DT> &x)
-{
-    Items f;
+    Items<F> f;
 #pragma unroll
-    for (int i = 0; i < kItems / 2; ++i) f.p[i] = pair(x, i);
+    for (int i = 0; i < f.N; ++i) f.p[i] = pair<F>(x, i);
     return f;
 }
-__device__ __forceinline__ Items all_items(float v)
+template <typename F> __device__ __forceinline__ Items<F> all_items(float v)
 {
-    Items f;
+    Items<F> f;
 #pragma unroll
-    for (int i = 0; i < kItems / 2; ++i) f.p[i] = both(v);
+    for (int i = 0; i < f.N; ++i) f.p[i] = both(v);
     return f;
 }
 
-/* acc += the items of x, one binary32 add each */
-template <int DT> __device__ __forceinline__ void add_items(Items &acc, const Raw<DT> &x)
+/* acc += items of x, one binary32 add each */
+template <typename F> __device__ __forceinline__ void add_pair(float2 &acc, const Raw<F> &x, int i)
+{
+    if (F::DT == SIFAR_BF16) acc = make_float2(add_bf16lo(acc.x, x.w[i % F::W]), add_bf16hi(acc.y, x.w[i % F::W]));
+    else acc = __fadd2_rn(acc, pair<F>(x, i));
+}
+template <typename F> __device__ __forceinline__ void add_items(Items<F> &acc, const Raw<F> &x)
 {
 #pragma unroll
-    for (int i = 0; i < kItems / 2; ++i) {
-        if (DT == SIFAR_BF16) acc.p[i] = make_float2(add_bf16lo(acc.p[i].x, x.w[i]), add_bf16hi(acc.p[i].y, x.w[i]));
-        else acc.p[i] = __fadd2_rn(acc.p[i], pair(x, i));
-    }
+    for (int i = 0; i < acc.N; ++i) add_pair<F>(acc.p[i], x, i);
 }
 
 /* weight + offset, or 1 where there is no weight */
-template <int DT, bool VEC>
-__device__ __forceinline__ Items load_factor(const void *weight, float offset, const Columns<DT, VEC> &c)
+template <typename F>
+__device__ __forceinline__ Items<F> load_factor(const void *weight, float offset, const Columns<F> &c, const Lane<F> &l)
 {
-    if (!weight) return all_items(1.0f);
-    Raw<DT> w;
-    load_any(w, weight, c);
-    Items f = items(w);
+    if (!weight) return all_items<F>(1.0f);
+    Raw<F> w;
+    load_weight(w, weight, c, l);
+    Items<F> f = items<F>(w);
 #pragma unroll
-    for (int i = 0; i < kItems / 2; ++i) f.p[i] = __fadd2_rn(f.p[i], both(offset));
+    for (int i = 0; i < f.N; ++i) f.p[i] = __fadd2_rn(f.p[i], both(offset));
     return f;
 }
 
-template <int DT, bool VEC>
-__device__ __forceinline__ void store_row(void *row, const Items &f, const Columns<DT, VEC> &c)
+template <typename F>
+__device__ __forceinline__ void store_items(void *row, const Items<F> &f, const Columns<F> &c, const Lane<F> &l)
 {
-    using T = typename Elem<DT>::type;
-    T *p = static_cast<T *>(row);
+    using T = typename F::T;
+    if (l.ragged) {
 #pragma unroll
-    for (int v = 0; v < Columns<DT, VEC>::NV; ++v) {
-        const uint32_t i = c.at(v * c.EPV);
-        if (VEC && i + c.EPV <= c.cols) {
-            uint4 q;
-            if (DT == SIFAR_BF16)
-                q = make_uint4(f32x2_to_bf16x2(f.p[0].x, f.p[0].y), f32x2_to_bf16x2(f.p[1].x, f.p[1].y),
-                               f32x2_to_bf16x2(f.p[2].x, f.p[2].y), f32x2_to_bf16x2(f.p[3].x, f.p[3].y));
-            else
-                q = make_uint4(__float_as_uint(f.p[(2 * v) % 4].x), __float_as_uint(f.p[(2 * v) % 4].y),
-                               __float_as_uint(f.p[(2 * v + 1) % 4].x), __float_as_uint(f.p[(2 * v + 1) % 4].y));
-            *reinterpret_cast<uint4 *>(p + i) = q;
-        } else {
-#pragma unroll
-            for (int k = 0; k < c.EPV; ++k) {
-                const int j = v * c.EPV + k;
-                if (i + k < c.cols) p[i + k] = narrow<DT>((j & 1) ? f.p[j / 2].y : f.p[j / 2].x);
-            }
-        }
+        for (int j = 0; j < F::items; ++j)
+            if (c.has(j)) static_cast<T *>(row)[c.at(j)] = narrow<F::DT>((j & 1) ? f.p[j / 2].y : f.p[j / 2].x);
+        return;
     }
-}
-
-template <int DT, bool VEC>
-__device__ __forceinline__ void store_items(void *row, const Items &f, const Columns<DT, VEC> &c, const Lane<DT, VEC> &l)
-{
-    if (l.ragged) { store_row(row, f, c); return; }
 #pragma unroll
-    for (int v = 0; v < Lane<DT, VEC>::NV; ++v) {
+    for (int v = 0; v < F::vectors; ++v) {
         if (!l.in[v]) continue;
+        constexpr int N = F::vector_pairs;                /* 4 of bf16, 2 of fp32 */
+        const float2 *p = &f.p[v * N];
         uint4 q;
-        if (DT == SIFAR_BF16)
-            q = make_uint4(f32x2_to_bf16x2(f.p[0].x, f.p[0].y), f32x2_to_bf16x2(f.p[1].x, f.p[1].y),
-                           f32x2_to_bf16x2(f.p[2].x, f.p[2].y), f32x2_to_bf16x2(f.p[3].x, f.p[3].y));
+        if (F::DT == SIFAR_BF16)
+            q = make_uint4(f32x2_to_bf16x2(p[0].x, p[0].y), f32x2_to_bf16x2(p[1].x, p[1].y), f32x2_to_bf16x2(p[2 % N].x, p[2 % N].y),
+                           f32x2_to_bf16x2(p[3 % N].x, p[3 % N].y));
         else
-            q = make_uint4(__float_as_uint(f.p[(2 * v) % 4].x), __float_as_uint(f.p[(2 * v) % 4].y),
-                           __float_as_uint(f.p[(2 * v + 1) % 4].x), __float_as_uint(f.p[(2 * v + 1) % 4].y));
+            q = make_uint4(__float_as_uint(p[0].x), __float_as_uint(p[0].y), __float_as_uint(p[1].x), __float_as_uint(p[1].y));
         *reinterpret_cast<uint4 *>(static_cast<char *>(row) + l.at[v]) = q;
     }
 }
 
 /* Sum of the squares of the items that exist. */
-template <int DT, bool VEC>
-__device__ __forceinline__ float squares(const Items &f, const Lane<DT, VEC> &l)
+template <typename F>
+__device__ __forceinline__ float squares(const Items<F> &f, const Lane<F> &l)
 {
-    if (VEC && Lane<DT, VEC>::NV == 2) {
-        const float2 a = __ffma2_rn(f.p[1], f.p[1], __fmul2_rn(f.p[0], f.p[0])), b = __ffma2_rn(f.p[3], f.p[3], __fmul2_rn(f.p[2], f.p[2]));
-        return (l.in[0] ? a.x + a.y : 0.0f) + (l.in[Lane<DT, VEC>::NV - 1] ? b.x + b.y : 0.0f);
-    }
-    float2 q = __fmul2_rn(f.p[0], f.p[0]);
+    constexpr int N = F::vector_pairs;
+    float sum = 0.0f;
 #pragma unroll
-    for (int j = 1; j < kItems / 2; ++j) q = __ffma2_rn(f.p[j], f.p[j], q);
-    return VEC && !l.in[0] ? 0.0f : q.x + q.y;
+    for (int v = 0; v < F::vectors; ++v) {
+        float2 q = __fmul2_rn(f.p[v * N], f.p[v * N]);
+#pragma unroll
+        for (int i = 1; i < N; ++i) q = __ffma2_rn(f.p[v * N + i], f.p[v * N + i], q);
+        sum += F::VEC && !l.in[v] ? 0.0f : q.x + q.y;
+    }
+    return sum;
 }
 
-/* The same for binary32 arrays beside rows of either type (sums over rows). */
-template <int DT, bool VEC>
-__device__ __forceinline__ void store_f32(float *row, const Items &f, const Columns<DT, VEC> &c)
+/* Items to a binary32 array (sums over rows). */
+template <typename F>
+__device__ __forceinline__ void store_f32(float *row, const Items<F> &f, const Columns<F> &c)
 {
-    const bool wide = VEC && ((uintptr_t)row & 15u) == 0;
+    const bool wide = F::VEC && ((uintptr_t)row & 15u) == 0;
 #pragma unroll
-    for (int j = 0; j < kItems; j += 4) {
+    for (int j = 0; j < F::items; j += 4) {
         const float4 q = make_float4(f.p[j / 2].x, f.p[j / 2].y, f.p[j / 2 + 1].x, f.p[j / 2 + 1].y);
         if (wide && c.at(j) + 4 <= c.cols) {
             *reinterpret_cast<float4 *>(row + c.at(j)) = q;
@@ -263,8 +233,8 @@ __device__ __forceinline__ void store_f32(float *row, const Items &f, const Colu
  * together; calls use two places in turn, so that a fast warp or CTA does not overwrite what a slow one still reads
  * (whoever has come to the call after next has seen that all have passed the next one's barrier).
  * Between CTAs each value travels with the call's number in one word, which the readers poll for: a cluster barrier
- * would wait for the rows' stores as well.  CTAs of a cluster run at the same time, so the wait ends; its limit is
- * there for the case that it does not: the sum is NaN then.
+ * would wait for the rows' stores as well (1003 x 4099 fp32, three ranks: 52 us with barriers, 42 with words).  CTAs of a
+ * cluster run at the same time, so the wait ends; its limit is there for the case that it does not: the sum is NaN then.
  */
 template <int N> struct RowSum {
     float4 warps[2][N][kMaxRowThreads / 32]; /* [turn][value][row of the CTA * vectors per row]: a word per warp, 0 behind the last */
@@ -281,6 +251,20 @@ template <int N> __device__ __forceinline__ void clear_row_sum(RowSum<N> &s)
         reinterpret_cast<float4 *>(&s)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
 
+/* Sums of three values over a warp with six exchanges: halves of the warp take over different values, then quarters.
+   Every lane of quarter k has the total of value k (k = 3: 0). */
+__device__ __forceinline__ float warp_sum3(float a, float b, float c)
+{
+    const uint32_t lane = threadIdx.x & 31u;
+    const bool up = lane & 16u, odd = lane & 8u;
+    float x = (up ? c : a) + __shfl_xor_sync(0xFFFFFFFFu, up ? a : c, 16);          /* a below, c above */
+    float y = (up ? 0.0f : b) + __shfl_xor_sync(0xFFFFFFFFu, up ? b : 0.0f, 16);    /* b below, 0 above */
+    x = (odd ? y : x) + __shfl_xor_sync(0xFFFFFFFFu, odd ? x : y, 8);               /* a, b, c, 0 */
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    return x;
+}
+
 struct RowPlace {
     uint32_t tx, t, row, parts, part;        /* threads of a row, which of them, row of the CTA, CTAs of a row, which of them */
 };
@@ -288,15 +272,23 @@ struct RowPlace {
 /* `call` counts the calls from 0. */
 template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], RowSum<N> &s, uint32_t call, const RowPlace &p)
 {
+    static_assert(N == 1 || N == 3, "one value or three");
     const uint32_t turn = call & 1u;
+    if (N == 1) {
+        v[0] = warp_sum(v[0]);
+    } else {
+        const float x = warp_sum3(v[0], v[1 % N], v[2 % N]);
+        if (p.tx > 32) {
+            v[0] = x;                                     /* lane 8 k: value k */
+        } else {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
-    if (p.tx > 32) {
-        const uint32_t n = sum_vectors(p.tx);
-        if ((p.t & 31u) == 0) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) reinterpret_cast<float *>(&s.warps[turn][k][p.row * n])[p.t / 32] = v[k];
+            for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xFFFFFFFFu, x, 8 * k);
         }
+    }
+    if (p.tx > 32) {
+        const uint32_t n = sum_vectors(p.tx), lane = p.t & 31u;
+        if (N == 1 ? lane == 0 : (lane & 7u) == 0 && lane < 24u)
+            reinterpret_cast<float *>(&s.warps[turn][lane / 8][p.row * n])[p.t / 32] = v[0];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -332,36 +324,35 @@ __device__ __forceinline__ float rrms(float sum, uint32_t cols, float eps) { ret
 
 /*
  * Rows that are under way while others are worked on: a ring of shared memory that each thread fills with its own items
- * by asynchronous copies and reads itself, so that no barrier goes with it.  Place of (array k of a stage, word w of the
- * thread's Raw): words of the threads side by side, 16 bytes each (VEC) or 4.
+ * by asynchronous copies and reads itself, so that no barrier goes with it.  A place (an array of a row) holds the
+ * threads' words side by side, 16 bytes each (VEC) or 4.
  */
-template <int DT, bool VEC> struct Ring {
-    static constexpr bool possible = VEC || DT == SIFAR_F32;         /* a copy moves 4 bytes at least */
-    static constexpr uint32_t bytes = sizeof(Raw<DT>);               /* per thread and array */
-    static constexpr uint32_t unit = VEC ? 16 : 4;
+template <typename F> struct Ring {
+    static constexpr bool possible = F::VEC || F::DT == SIFAR_F32;         /* a copy moves 4 bytes at least */
+    static constexpr uint32_t bytes = sizeof(Raw<F>);                   /* per thread and array */
+    static constexpr uint32_t unit = F::VEC ? 16 : 4;
     static constexpr int N = bytes / unit;
     uint32_t first, threads;                                         /* the thread's place in slot 0; of the CTA */
     uint32_t from[N], n[N];                                          /* of each copy: bytes into the row, bytes to move (the rest becomes 0) */
-    __device__ __forceinline__ Ring(const void *smem, const Columns<DT, VEC> &c)
+    __device__ __forceinline__ Ring(const void *smem, const Columns<F> &c)
     {
-        constexpr uint32_t es = sizeof(typename Elem<DT>::type);
-        threads = blockDim.x * blockDim.y;
+                threads = blockDim.x * blockDim.y;
         first = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.y * blockDim.x + threadIdx.x) * unit;
 #pragma unroll
         for (int v = 0; v < N; ++v) {
             const uint32_t i = c.at(v * c.EPV);
-            n[v] = i < c.cols ? min((uint32_t)c.EPV, c.cols - i) * es : 0u;
-            from[v] = n[v] ? i * es : 0u;
+            n[v] = i < c.cols ? min((uint32_t)c.EPV, c.cols - i) * F::es : 0u;
+            from[v] = n[v] ? i * F::es : 0u;
         }
     }
-    /* a row of an array to place `at` (bytes; a place takes `threads * bytes`) */
+    /* a row of an array to place `at` (bytes; a place takes threads * bytes) */
     __device__ __forceinline__ void fetch(uint32_t at, const void *row) const
     {
         const uint32_t to = first + at;
 #pragma unroll
         for (int v = 0; v < N; ++v) {
             const char *p = static_cast<const char *>(row) + from[v];
-            if (VEC)
+            if (F::VEC)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to + v * threads * unit), "l"(p), "r"(n[v]) : "memory");
             else
                 asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(to + v * threads * unit), "l"(p), "r"(n[v]) : "memory");
@@ -376,79 +367,33 @@ template <int DT, bool VEC> struct Ring {
         else if (k == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else asm volatile("cp.async.wait_group 3;" ::: "memory");
     }
-    __device__ __forceinline__ void read(Raw<DT> &x, uint32_t from) const
+    /* the first four words of the thread, or the last four */
+    __device__ __forceinline__ void read_half(Raw<F> &x, int v, uint32_t at) const
     {
-        const uint32_t at = first + from;
+        const uint32_t p = first + at;
+        if (F::VEC) {
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x.w[4 * v]), "=r"(x.w[4 * v + 1]), "=r"(x.w[4 * v + 2]), "=r"(x.w[4 * v + 3]) : "r"(p + v * threads * unit) : "memory");
+        } else {
 #pragma unroll
-        for (int v = 0; v < N; ++v) {
-            if (VEC)
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                             : "=r"(x.w[4 * v % (bytes / 4)]), "=r"(x.w[(4 * v + 1) % (bytes / 4)]), "=r"(x.w[(4 * v + 2) % (bytes / 4)]),
-                               "=r"(x.w[(4 * v + 3) % (bytes / 4)]) : "r"(at + v * threads * unit) : "memory");
-            else
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x.w[v % (bytes / 4)]) : "r"(at + v * threads * unit) : "memory");
+            for (int i = 4 * v; i < 4 * v + 4; ++i)
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x.w[i]) : "r"(p + i * threads * unit) : "memory");
         }
     }
 };
-constexpr uint32_t kMaxStages = 4;
-constexpr size_t kRingBytes = 220 * 1024;    /* of the 227 KB a CTA may have */
 
-/* Rows of block b: [block_start(b), block_start(b + 1)). */
-__host__ __device__ inline uint32_t block_start(uint32_t rows, uint32_t blocks, uint32_t b)
-{
-    return (uint32_t)((unsigned long long)rows * b / blocks);
-}
-__host__ __device__ inline uint32_t block_of(uint32_t rows, uint32_t blocks, uint32_t row)
-{
-    return (uint32_t)((((unsigned long long)row + 1ull) * blocks - 1ull) / rows);
-}
-
-/* How many CTAs hold a row and how many threads of each; into how many blocks of consecutive rows the rows are cut and
-   how many of them a CTA walks side by side. */
-constexpr unsigned kNormCtas = 148;          /* one per SM: rows under way and sums over rows fill its memory and registers */
+/* How many CTAs hold a row and how many threads of each. */
 struct RowShape {
-    unsigned tx, parts, ry;
-    uint32_t blocks;
+    unsigned tx, parts;
 };
-inline RowShape row_shape(size_t rows, size_t cols)
+inline RowShape row_shape(int items, size_t cols)          /* items: of a thread */
 {
-    const size_t need = (cols + kItems - 1) / kItems;
+    const size_t need = (cols + items - 1) / items;
     RowShape s;
-    s.parts = 1;
-    while ((need + s.parts - 1) / s.parts > (size_t)kMaxRowThreads) s.parts *= 2;
-    s.tx = (unsigned)(((need + s.parts - 1) / s.parts + 31) / 32 * 32);
-    s.ry = kMaxRowThreads / s.tx;
-    while (s.ry > 1 && rows <= (size_t)(s.ry - 1) * kNormCtas) --s.ry;
-    const size_t most = (size_t)(kNormCtas / s.parts) * s.ry;
-    s.blocks = (uint32_t)(rows < most ? rows : most);
-    return s;
-}
-
-/* Launches a kernel of blocks of rows with its ring; the attribute for that much shared memory is set once per kernel
-   and device. */
-template <int DT, bool VEC, typename Args>
-cudaError_t launch_rows(void (*kernel)(Args), std::atomic<unsigned long long> &ready, const RowShape &sh, unsigned arrays,
-                        cudaStream_t stream, Args &a)
-{
-    const size_t row = (size_t)sh.tx * sh.ry * arrays * Ring<DT, VEC>::bytes;
-    const size_t turns = (a.rows + sh.blocks - 1) / sh.blocks;
-    size_t stages = 1, smem = 0;
-    if (Ring<DT, VEC>::possible) {
-        stages = kRingBytes / row < kMaxStages ? kRingBytes / row : kMaxStages;
-        if (stages > turns) stages = turns;
-        smem = row * stages;
-        int dev = 0;
-        cudaError_t e = cudaGetDevice(&dev);
-        if (e != cudaSuccess) return e;
-        if (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1ull)) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
-            if (e != cudaSuccess) return e;
-            if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_release);
-        }
+    for (s.parts = 1;; s.parts *= 2) {
+        s.tx = (unsigned)(((need + s.parts - 1) / s.parts + 31) / 32 * 32);
+        if (s.tx <= (unsigned)kMaxRowThreads) return s;
     }
-    a.stages = (uint32_t)stages;
-    const dim3 grid((sh.blocks + sh.ry - 1) / sh.ry * sh.parts), block(sh.tx, sh.ry);
-    return launch_op(kernel, grid, block, sh.parts, smem, stream, a);
 }
 
 }  /* namespace sifar */

@@ -26,38 +26,74 @@ struct NormGradArgs {
     int P, post, pre;
 };
 
+/* Rows of block b: [block_start(b), block_start(b + 1)). */
+__host__ __device__ inline uint32_t block_start(uint32_t rows, uint32_t blocks, uint32_t b)
+{
+    return (uint32_t)((unsigned long long)rows * b / blocks);
+}
+__host__ __device__ inline uint32_t block_of(uint32_t rows, uint32_t blocks, uint32_t row)
+{
+    return (uint32_t)((((unsigned long long)row + 1ull) * blocks - 1ull) / rows);
+}
+
+/* beta * gate of a row */
+template <typename F>
+__device__ __forceinline__ Items<F> gate_factor(const NormGradArgs &a, const Columns<F> &c, const Lane<F> &l, uint32_t row)
+{
+    if (!a.gate) return all_items<F>(a.beta);
+    Items<F> g = load_factor(static_cast<const char *>(a.gate) + (unsigned long long)(row / a.rows_per_gate) * a.ld_gate, 0.0f, c, l);
+#pragma unroll
+    for (int j = 0; j < g.N; ++j) g.p[j] = __fmul2_rn(g.p[j], both(a.beta));
+    return g;
+}
+
 /*
  * End of the rows [begin, end) of a block that share a gate row, with acc = their sum of D * n1: it gives the gate's
  * gradient, beta * (post_weight + offset) * acc, and adds beta * gate * acc to the post weight's.
  * The gate's is final where all rows of the gate row are here.  Otherwise it is a part: place 0 of the block's two
- * where it holds the block's first row, else place 1.
+ * where it holds the block's first row, else place 1.  The post weight's sum is kept in the block's place of the
+ * workspace, not in registers: gate rows end seldom.
  */
-template <int DT, bool VEC>
-__device__ __forceinline__ void end_of_gate(const NormGradArgs &a, const Columns<DT, VEC> &c, Items &acc, Items &post, const Items &gate,
+template <typename F>
+__device__ __forceinline__ void end_of_gate(const NormGradArgs &a, const Columns<F> &c, const Lane<F> &l, Items<F> &acc,
                                             uint32_t b, uint32_t first, uint32_t begin, uint32_t end)
 {
+    if (a.sum_post) {
+        float *const place = a.sum_post + (size_t)b * a.pitch;
+        Items<F> post = gate_factor(a, c, l, begin);
 #pragma unroll
-    for (int j = 0; j < kItems / 2; ++j) post.p[j] = __ffma2_rn(gate.p[j], acc.p[j], post.p[j]);
+        for (int j = 0; j < acc.N; ++j) post.p[j] = __fmul2_rn(post.p[j], acc.p[j]);
+        if (begin != first) {
+#pragma unroll
+            for (int j = 0; j < F::items; ++j)
+                if (c.has(j)) { if (j & 1) post.p[j / 2].y += place[c.at(j)]; else post.p[j / 2].x += place[c.at(j)]; }
+        }
+        store_f32(place, post, c);
+    }
     if (a.dgate) {
-        const Items w = load_factor<DT, VEC>(a.post_weight, a.offset, c);
+        const Items<F> w = load_factor(a.post_weight, a.offset, c, l);
 #pragma unroll
-        for (int j = 0; j < kItems / 2; ++j) acc.p[j] = __fmul2_rn(__fmul2_rn(acc.p[j], both(a.beta)), w.p[j]);
+        for (int j = 0; j < acc.N; ++j) acc.p[j] = __fmul2_rn(__fmul2_rn(acc.p[j], both(a.beta)), w.p[j]);
         const uint32_t g = begin / a.rows_per_gate;
         const unsigned long long g0 = (unsigned long long)g * a.rows_per_gate, g1 = g0 + a.rows_per_gate;
         const bool whole = begin == g0 && (end == g1 || end == a.rows);
         if (whole) store_f32(a.dgate + (size_t)g * a.cols, acc, c);
         else store_f32(a.sum_gate + ((size_t)b * 2 + (begin == first ? 0 : 1)) * a.pitch, acc, c);
     }
-    acc = all_items(0.0f);
+    acc = all_items<F>(0.0f);
 }
 
 /*
  * Both sums of a row in one pass.  With t = dh + r2 * a and f = beta * gate * (post_weight + offset) the second,
  * sum(f * n1 * D) with D = t - r2 * m2 * n2, is sum(f * n1 * t) - r2 * m2 * sum(f * n1 * n2), so that neither has to
- * wait for the other.
+ * wait for the other.  h and z stay as they came and are widened again behind the sums: their binary32 forms would take
+ * the registers of a second CTA.
  */
-template <int DT, bool VEC, bool POST, bool PRE>
-__global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
+template <int DT> constexpr int kGradWords = DT == SIFAR_BF16 ? 4 : 8;
+template <int DT> constexpr int kGradCtas = 1;   /* of kMaxRowThreads threads on an SM */
+
+template <typename F, bool POST, bool PRE>
+__global__ void __launch_bounds__(kMaxRowThreads, kGradCtas<F::DT>) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
     constexpr int kSums = POST && PRE ? 3 : 1;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
@@ -67,17 +103,17 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
     clear_row_sum(s);
     __syncthreads();
     if (a.parts > 1) { cluster_arrive(); cluster_wait(); }           /* all CTAs of the cluster have started */
+    /* rows of more than a warp have their CTA to themselves: blocks never meet in a barrier */
     const uint32_t b = (blockIdx.x / a.parts) * blockDim.y + threadIdx.y;
     const bool live = b < a.blocks;
     const uint32_t first = live ? block_start(a.rows, a.blocks, b) : 0u, end = live ? block_start(a.rows, a.blocks, b + 1) : 0u;
-    /* blocks of a CTA that meet in its barrier take the same number of turns, the others end with their rows */
-    const uint32_t turns = blockDim.y > 1 && p.tx > 32 ? (a.rows + a.blocks - 1) / a.blocks : end - first;
-    const Columns<DT, VEC> c(p.part, p.tx, p.t, a.cols);
-    const Lane<DT, VEC> l(c);
-    const Ring<DT, VEC> ring(ring_bytes, c);
+    const Columns<F> c(p.part, p.tx, p.t, a.cols);
+    const Lane<F> l(c);
+    const Ring<F> ring(ring_bytes, c);
     const int partials = PRE ? a.P : 0;
     const bool with_z = POST || a.z;
-    const uint32_t pitch = ring.threads * ring.bytes, stage_bytes = pitch * ((uint32_t)partials + (PRE ? 1u : 0u) + (a.dh ? 1u : 0u) + (with_z ? 1u : 0u));
+    const uint32_t pitch = ring.threads * ring.bytes;
+    const uint32_t stage_bytes = pitch * ((uint32_t)partials + (PRE ? 1u : 0u) + (a.dh ? 1u : 0u) + (with_z ? 1u : 0u));
     grid_wait();
 
     /* row `row` to place `to` of the ring: the partials, then h, dh, z */
@@ -95,132 +131,120 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
         }
         ring.commit();
     };
-    if (Ring<DT, VEC>::possible)
+    if (Ring<F>::possible)
         for (uint32_t i = 0; i < a.stages; ++i) fetch(i * stage_bytes, first + i);
 
-    const Items w2 = load_factor<DT, VEC>(a.pre_weight, a.offset, c);
-    Items f = load_factor<DT, VEC>(a.post_weight, a.offset, c);      /* of dx over D, from here on with beta * gate */
-    Items g = all_items(a.beta);                          /* beta * gate */
+    const Items<F> w2 = load_factor(a.pre_weight, a.offset, c, l);
+    Items<F> f = load_factor(a.post_weight, a.offset, c, l);        /* of dx over D: post_weight + offset, beta, gate */
 #pragma unroll
-    for (int j = 0; j < kItems / 2; ++j) f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
-    Items post = all_items(0.0f), pre = post, acc = post;
+    for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], both(a.beta));
+    Items<F> pre = all_items<F>(0.0f), acc = pre;
     const float inv = 1.0f / (float)a.cols;
     uint32_t segment = first, gate_end = a.gate ? first : 0xFFFFFFFFu, place = 0;
     const uint32_t places = stage_bytes * a.stages;
     float next1 = POST && live ? a.stats[first] : 1.0f, next2 = PRE && live ? a.stats[a.rows + first] : 1.0f;
 
-    for (uint32_t i = 0; i < turns; ++i) {
-        const uint32_t row = first + i;
-        const bool on = row < end;
+    for (uint32_t row = first; row < end; ++row) {
         const unsigned long long at = row;
         const float r1 = next1, r2 = next2;
         if (row + 1 < end) {
             if (POST) next1 = a.stats[row + 1];
             if (PRE) next2 = a.stats[a.rows + row + 1];
         }
-        if (on && row >= gate_end) {                      /* the rows of another gate row begin */
-            if (row != first) end_of_gate(a, c, acc, post, g, b, first, segment, row);
+        if (row >= gate_end) {                            /* the rows of another gate row begin */
+            if (row != first) end_of_gate(a, c, l, acc, b, first, segment, row);
             segment = row;
-            const uint32_t k = row / a.rows_per_gate;
-            gate_end = (k + 1) * a.rows_per_gate;
-            g = load_factor<DT, VEC>(static_cast<const char *>(a.gate) + (unsigned long long)k * a.ld_gate, 0.0f, c);
-            f = load_factor<DT, VEC>(a.post_weight, a.offset, c);
+            gate_end = (row / a.rows_per_gate + 1) * a.rows_per_gate;
+            f = load_factor(a.post_weight, a.offset, c, l);
+            const Items<F> g = gate_factor(a, c, l, row);
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) {
-                g.p[j] = __fmul2_rn(g.p[j], both(a.beta));
-                f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
-            }
+            for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
         }
 
-        /* D: the gradient of h; G: of the normed h; n2, n1: h and z in units of their root mean square */
-        Items D, G, n2, n1;
-        float sum[kSums] = {};
-        if (on) {
-            Raw<DT> x;
-            if (Ring<DT, VEC>::possible) {
-                ring.wait(a.stages - 1);
-                uint32_t from = place;
-                if (PRE) {
-                    ring.read(x, from);
-                    from += pitch;
-                    G = items(x);
-                    for (int r = 1; r < partials; ++r, from += pitch) { ring.read(x, from); add_items(G, x); }
-                    ring.read(x, from);
-                    from += pitch;
-                    n2 = items(x);
-                }
-                D = all_items(0.0f);
-                if (a.dh) { ring.read(x, from); from += pitch; D = items(x); }
-                if (with_z) { ring.read(x, from); n1 = items(x); }
-                fetch(place, row + a.stages);             /* the thread has read its places */
-                place = place + stage_bytes == places ? 0u : place + stage_bytes;
-            } else {
-                if (PRE) {
-                    load_row(x, static_cast<const char *>(a.dy[0]) + at * a.ld_dy, c);
-                    G = items(x);
-#pragma unroll 4
-                    for (int r = 1; r < partials; ++r) {
-                        load_row(x, static_cast<const char *>(a.dy[r]) + at * a.ld_dy, c);
-                        add_items(G, x);
-                    }
-                    load_row(x, static_cast<const char *>(a.h) + at * a.ld_h, c);
-                    n2 = items(x);
-                }
-                D = all_items(0.0f);
-                if (a.dh) { load_row(x, static_cast<const char *>(a.dh) + at * a.ld_dh, c); D = items(x); }
-                if (with_z) { load_row(x, static_cast<const char *>(a.z) + at * a.ld_z, c); n1 = items(x); }
-            }
-            float2 q2 = both(0.0f), qt = q2, qn = q2;     /* sums of a * n2, f * n1 * t, f * n1 * n2 */
+        if (Ring<F>::possible) ring.wait(a.stages - 1);
+        Items<F> D;                                      /* the gradient of h */
+        Raw<F> xh, xz;
+        float2 q2 = both(0.0f), qt = q2, qn = q2;         /* sums of a * n2, f * z * t, f * z * n2 */
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) {
+        for (int v = 0; v < F::vectors; ++v) {              /* a half of the items after the other: fewer registers */
+            constexpr int N = F::vector_pairs;
+            Raw<F> x;
+            float2 G[N];                                  /* the gradient of the normed h */
+            uint32_t from = place;
+            auto get = [&](Raw<F> &y, const void *base, uint32_t ld) {
+                if (Ring<F>::possible) { ring.read_half(y, v, from); from += pitch; }
+                else load_half(y, v, static_cast<const char *>(base) + at * ld, c);
+            };
+            if (PRE) {
+                get(x, a.dy[0], a.ld_dy);
+#pragma unroll
+                for (int j = 0; j < N; ++j) G[j] = pair<F>(x, v * N + j);
+                for (int r = 1; r < partials; ++r) {
+                    get(x, a.dy[r], a.ld_dy);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) add_pair<F>(G[j], x, v * N + j);
+                }
+                get(xh, a.h, a.ld_h);
+            }
+            if (a.dh) get(x, a.dh, a.ld_dh);
+#pragma unroll
+            for (int j = 0; j < N; ++j) D.p[v * N + j] = a.dh ? pair<F>(x, v * N + j) : both(0.0f);
+            if (with_z) get(xz, a.z, a.ld_z);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int i = v * N + j;
+                float2 n2;
                 if (PRE) {
-                    n2.p[j] = __fmul2_rn(n2.p[j], both(r2));
-                    pre.p[j] = __ffma2_rn(G.p[j], n2.p[j], pre.p[j]);
-                    G.p[j] = __fmul2_rn(G.p[j], w2.p[j]);
-                    q2 = __ffma2_rn(G.p[j], n2.p[j], q2);
-                    D.p[j] = __ffma2_rn(both(r2), G.p[j], D.p[j]);
+                    n2 = __fmul2_rn(pair<F>(xh, i), both(r2));
+                    pre.p[i] = __ffma2_rn(G[j], n2, pre.p[i]);
+                    G[j] = __fmul2_rn(G[j], w2.p[i]);
+                    q2 = __ffma2_rn(G[j], n2, q2);
+                    D.p[i] = __ffma2_rn(both(r2), G[j], D.p[i]);
                 }
                 if (POST) {
-                    n1.p[j] = __fmul2_rn(n1.p[j], both(r1));
-                    const float2 fn = __fmul2_rn(f.p[j], n1.p[j]);
-                    qt = __ffma2_rn(fn, D.p[j], qt);
-                    if (PRE) qn = __ffma2_rn(fn, n2.p[j], qn);
+                    const float2 fz = __fmul2_rn(f.p[i], pair<F>(xz, i));
+                    qt = __ffma2_rn(fz, D.p[i], qt);
+                    if (PRE) qn = __ffma2_rn(fz, n2, qn);
                 }
             }
-            sum[0] = PRE ? q2.x + q2.y : qt.x + qt.y;
-            if (kSums == 3) { sum[1 % kSums] = qt.x + qt.y; sum[2 % kSums] = qn.x + qn.y; }
         }
-        if (POST || PRE) row_sums(sum, s, i, p);
-        if (!on) continue;
+        if (Ring<F>::possible) {
+            fetch(place, row + a.stages);                 /* the thread has read its places */
+            place = place + stage_bytes == places ? 0u : place + stage_bytes;
+        }
+        float sum[kSums];
+        sum[0] = PRE ? q2.x + q2.y : qt.x + qt.y;
+        if (kSums == 3) { sum[1 % kSums] = qt.x + qt.y; sum[2 % kSums] = qn.x + qn.y; }
+        if (POST || PRE) row_sums(sum, s, row - first, p);
         const float m2 = PRE ? r2 * (sum[0] * inv) : 0.0f;
-        const float m1 = !POST ? 0.0f : PRE ? (sum[1 % kSums] - m2 * sum[2 % kSums]) * inv : sum[0] * inv;
+        const float m1 = !POST ? 0.0f : r1 * ((PRE ? sum[1 % kSums] - m2 * sum[2 % kSums] : sum[0]) * inv);
         if (PRE) {
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) D.p[j] = __ffma2_rn(both(-m2), n2.p[j], D.p[j]);
+            for (int j = 0; j < D.N; ++j) D.p[j] = __ffma2_rn(both(-m2 * r2), pair<F>(xh, j), D.p[j]);
         }
         if (a.dresidual) {
-            Items o;
+            Items<F> o;
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) o.p[j] = __fmul2_rn(both(a.alpha), D.p[j]);
+            for (int j = 0; j < D.N; ++j) o.p[j] = __fmul2_rn(both(a.alpha), D.p[j]);
             store_items(static_cast<char *>(a.dresidual) + at * a.ld_dresidual, o, c, l);
         }
         if (with_z) {
 #pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) acc.p[j] = __ffma2_rn(D.p[j], n1.p[j], acc.p[j]);
-        }
-        if (a.dx) {
-#pragma unroll
-            for (int j = 0; j < kItems / 2; ++j) {
+            for (int j = 0; j < D.N; ++j) {
+                const float2 n1 = POST ? __fmul2_rn(pair<F>(xz, j), both(r1)) : pair<F>(xz, j);
+                acc.p[j] = __ffma2_rn(D.p[j], n1, acc.p[j]);
                 D.p[j] = __fmul2_rn(f.p[j], D.p[j]);
-                if (POST) D.p[j] = __fmul2_rn(both(r1), __ffma2_rn(both(-m1), n1.p[j], D.p[j]));
+                if (POST) D.p[j] = __fmul2_rn(both(r1), __ffma2_rn(both(-m1), n1, D.p[j]));
             }
-            store_items(static_cast<char *>(a.dx) + at * a.ld_dx, D, c, l);
+        } else {
+#pragma unroll
+            for (int j = 0; j < D.N; ++j) D.p[j] = __fmul2_rn(f.p[j], D.p[j]);
         }
+        if (a.dx) store_items(static_cast<char *>(a.dx) + at * a.ld_dx, D, c, l);
     }
-    if (Ring<DT, VEC>::possible) ring.wait(0);
+    if (Ring<F>::possible) ring.wait(0);
     if (!live) return;
-    end_of_gate(a, c, acc, post, g, b, first, segment, end);
-    if (a.sum_post) store_f32(a.sum_post + (size_t)b * a.pitch, post, c);
+    end_of_gate(a, c, l, acc, b, first, segment, end);
     if (a.sum_pre) store_f32(a.sum_pre + (size_t)b * a.pitch, pre, c);
 }
 
@@ -282,22 +306,71 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const NormSu
     }
 }
 
-template <int DT, bool VEC, bool POST, bool PRE>
-static cudaError_t launch_grad_n(const RowShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
+/*
+ * Into how many blocks of consecutive rows the rows are cut, and how the blocks lie in CTAs: as many as have room at
+ * once, 512 threads per SM (the rows under way and the sums over rows fill its memory and registers).
+ */
+constexpr uint32_t kMaxStages = 4;
+constexpr size_t kRingBytes = 216 * 1024;    /* of the 227 KB that an SM has for its CTAs */
+struct GradShape {
+    RowShape row;
+    unsigned ry, per_sm;                     /* blocks of a CTA, CTAs of an SM */
+    uint32_t blocks;
+};
+template <int DT> GradShape grad_shape_of(size_t rows, size_t cols)
 {
+    GradShape s;
+    s.row = row_shape(kGradWords<DT> * 4 / (int)elem_size(DT), cols);
+    s.ry = s.row.tx == 32 ? 4 : 1;
+    s.per_sm = kMaxRowThreads * kGradCtas<DT> / (s.row.tx * s.ry);
+    /* few rows: a CTA of its own for each */
+    while (s.ry > 1 && rows <= (size_t)kSms * s.per_sm * (s.ry / 2)) s.ry /= 2;
+    const size_t most = (size_t)(kSms * s.per_sm / s.row.parts) * s.ry;
+    s.blocks = (uint32_t)(rows < most ? rows : most);
+    return s;
+}
+static GradShape grad_shape(int dtype, size_t rows, size_t cols)
+{
+    return dtype == SIFAR_BF16 ? grad_shape_of<SIFAR_BF16>(rows, cols) : grad_shape_of<SIFAR_F32>(rows, cols);
+}
+
+/* The attribute for the ring's shared memory is set once per kernel and device. */
+template <int DT, bool VEC, bool POST, bool PRE>
+static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
+{
+    using F = Form<DT, kGradWords<DT>, VEC>;
     static std::atomic<unsigned long long> ready{0};
-    return launch_rows<DT, VEC>(k_block_norm_grad<DT, VEC, POST, PRE>, ready, sh, arrays, stream, a);
+    const auto kernel = k_block_norm_grad<F, POST, PRE>;
+    size_t stages = 1, smem = 0;
+    if (Ring<F>::possible) {
+        const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes, turns = (a.rows + sh.blocks - 1) / sh.blocks;
+        stages = kRingBytes / sh.per_sm / row;
+        if (stages > kMaxStages) stages = kMaxStages;
+        if (stages > turns) stages = turns;
+        smem = row * stages;
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1ull)) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+            if (e != cudaSuccess) return e;
+            if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_release);
+        }
+    }
+    a.stages = (uint32_t)stages;
+    const dim3 grid((sh.blocks + sh.ry - 1) / sh.ry * sh.row.parts), block(sh.row.tx, sh.ry);
+    return launch_op(kernel, grid, block, sh.row.parts, smem, stream, a);
 }
 
 template <int DT, bool VEC>
-static cudaError_t launch_grad(const RowShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
+static cudaError_t launch_grad(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
     if (a.post) return a.pre ? launch_grad_n<DT, VEC, true, true>(sh, arrays, stream, a) : launch_grad_n<DT, VEC, true, false>(sh, arrays, stream, a);
     return a.pre ? launch_grad_n<DT, VEC, false, true>(sh, arrays, stream, a) : launch_grad_n<DT, VEC, false, false>(sh, arrays, stream, a);
 }
 
 /* Words between two blocks' sums. */
-static size_t sum_pitch(size_t cols) { return (cols + kItems - 1) / kItems * kItems; }
+static size_t sum_pitch(size_t cols) { return (cols + 7) / 8 * 8; }
 
 }  /* namespace sifar */
 
@@ -321,7 +394,7 @@ static int check_grad_sizes(const sifar_block_norm_grad_args *g, const char *fn)
 extern "C" size_t sifar_block_norm_backward_workspace(const sifar_block_norm_grad_args *g)
 {
     if (check_grad_sizes(g, "sifar_block_norm_backward_workspace")) return 0;
-    const RowShape s = row_shape(g->rows, g->cols);
+    const GradShape s = grad_shape(g->dtype, g->rows, g->cols);
     const size_t arrays = (g->dpost_weight ? 1 : 0) + (g->dpre_weight ? 1 : 0) + (g->dgate ? 2 : 0);
     return arrays * s.blocks * sum_pitch(g->cols) * sizeof(float);
 }
@@ -382,7 +455,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     if (need) all[n++] = RowArray{"workspace", g->workspace, 1, need / sizeof(float), need / sizeof(float), sizeof(float), true};
     if (int rc = check_arrays(fn, all, n)) return rc;
 
-    const RowShape sh = row_shape(rows, cols);
+    const GradShape sh = grad_shape(g->dtype, rows, cols);
     float *ws = static_cast<float *>(g->workspace);
     const size_t plane = (size_t)sh.blocks * sum_pitch(cols);
     NormGradArgs a;
@@ -398,7 +471,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     a.ld_gate = bytes(g->ld_gate); a.ld_dx = bytes(g->ld_dx); a.ld_dresidual = bytes(g->ld_dresidual);
     a.alpha = g->alpha; a.beta = g->beta; a.offset = g->weight_offset;
     a.rows = (uint32_t)rows; a.cols = (uint32_t)cols; a.pitch = (uint32_t)sum_pitch(cols); a.blocks = sh.blocks;
-    a.rows_per_gate = (uint32_t)span; a.parts = sh.parts;
+    a.rows_per_gate = (uint32_t)span; a.parts = sh.row.parts;
     a.P = pre ? g->P : 1; a.post = post; a.pre = pre;
     if (rows) {
         const unsigned arrays = (pre ? (unsigned)g->P + 1u : 0u) + (g->dh ? 1u : 0u) + (need_z ? 1u : 0u);
