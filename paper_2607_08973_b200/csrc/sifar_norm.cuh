@@ -243,7 +243,7 @@ template <int N> struct RowSum {
 constexpr int kPartPolls = 1 << 22;
 __host__ __device__ inline uint32_t sum_vectors(uint32_t tx) { return (tx / 32 + 3) / 4; }
 
-/* Before the first row_sums; a barrier (of the cluster) must follow. */
+/* Before the first sum; a barrier (of the cluster) must follow. */
 template <int N> __device__ __forceinline__ void clear_row_sum(RowSum<N> &s)
 {
     static_assert(sizeof(RowSum<N>) % 16 == 0, "cleared by vectors");
@@ -269,54 +269,80 @@ struct RowPlace {
     uint32_t tx, t, row, parts, part;        /* threads of a row, which of them, row of the CTA, CTAs of a row, which of them */
 };
 
-/* `call` counts the calls from 0. */
-template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], RowSum<N> &s, uint32_t call, const RowPlace &p)
+/*
+ * A sum in three steps, so that other work can lie between: publish_sums (a barrier of the CTA must follow, where a row
+ * has more than a warp), send_sums (clusters), collect_sums.  `call` counts the sums from 0.
+ */
+template <int N> __device__ __forceinline__ void publish_sums(float (&v)[N], RowSum<N> &s, uint32_t call, const RowPlace &p)
 {
     static_assert(N == 1 || N == 3, "one value or three");
-    const uint32_t turn = call & 1u;
-    if (N == 1) {
-        v[0] = warp_sum(v[0]);
-    } else {
-        const float x = warp_sum3(v[0], v[1 % N], v[2 % N]);
-        if (p.tx > 32) {
-            v[0] = x;                                     /* lane 8 k: value k */
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xFFFFFFFFu, x, 8 * k);
-        }
-    }
+    float x;
+    if (N == 1) x = warp_sum(v[0]);
+    else x = warp_sum3(v[0], v[1 % N], v[2 % N]);         /* lane 8 k: value k */
     if (p.tx > 32) {
-        const uint32_t n = sum_vectors(p.tx), lane = p.t & 31u;
+        const uint32_t lane = p.t & 31u;
         if (N == 1 ? lane == 0 : (lane & 7u) == 0 && lane < 24u)
-            reinterpret_cast<float *>(&s.warps[turn][lane / 8][p.row * n])[p.t / 32] = v[0];
-        __syncthreads();
+            reinterpret_cast<float *>(&s.warps[call & 1u][lane / 8][p.row * sum_vectors(p.tx)])[p.t / 32] = x;
+    } else if (N == 1) {
+        v[0] = x;
+    } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const float4 *w = &s.warps[turn][k][p.row * n];
-            float2 x = make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (uint32_t i = 0; i < kMaxRowThreads / 128; ++i)
-                if (i < n) { const float4 q = w[i]; x = __fadd2_rn(x, __fadd2_rn(make_float2(q.x, q.y), make_float2(q.z, q.w))); }
-            v[k] = x.x + x.y;
-        }
+        for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xFFFFFFFFu, x, 8 * k);
     }
-    if (p.parts > 1) {
-        if (p.t < p.parts) {
+}
+
+/* The CTA's own totals. */
+template <int N> __device__ __forceinline__ void local_sums(float (&v)[N], const RowSum<N> &s, uint32_t call, const RowPlace &p)
+{
+    const uint32_t n = sum_vectors(p.tx);
 #pragma unroll
-            for (int k = 0; k < N; ++k) store_cluster_tagged(&s.parts[turn][k][p.part], p.t, v[k], call + 1u);
-        }
-        int polls = 0;
+    for (int k = 0; k < N; ++k) {
+        const float4 *w = &s.warps[call & 1u][k][p.row * n];
+        float2 x = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            float x = 0.0f;
-            for (uint32_t i = 0; i < p.parts; ++i) {
-                unsigned long long w = load_tagged(&s.parts[turn][k][i]);
-                while ((uint32_t)(w >> 32) != call + 1u && ++polls < kPartPolls) w = load_tagged(&s.parts[turn][k][i]);
-                x += (uint32_t)(w >> 32) == call + 1u ? __uint_as_float((uint32_t)w) : NAN;
-            }
-            v[k] = x;
-        }
+        for (uint32_t i = 0; i < kMaxRowThreads / 128; ++i)
+            if (i < n) { const float4 q = w[i]; x = __fadd2_rn(x, __fadd2_rn(make_float2(q.x, q.y), make_float2(q.z, q.w))); }
+        v[k] = x.x + x.y;
     }
+}
+
+template <int N> __device__ __forceinline__ void send_sums(RowSum<N> &s, uint32_t call, const RowPlace &p)
+{
+    if (p.t < p.parts) {
+        float v[N];
+        local_sums(v, s, call, p);
+#pragma unroll
+        for (int k = 0; k < N; ++k) store_cluster_tagged(&s.parts[call & 1u][k][p.part], p.t, v[k], call + 1u);
+    }
+}
+
+/* In: what publish_sums left.  Out: the row's totals. */
+template <int N> __device__ __forceinline__ void collect_sums(float (&v)[N], const RowSum<N> &s, uint32_t call, const RowPlace &p)
+{
+    if (p.parts == 1) {
+        if (p.tx > 32) local_sums(v, s, call, p);
+        return;
+    }
+    int polls = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float x = 0.0f;
+        for (uint32_t i = 0; i < p.parts; ++i) {
+            unsigned long long w = load_tagged(&s.parts[call & 1u][k][i]);
+            while ((uint32_t)(w >> 32) != call + 1u && ++polls < kPartPolls) w = load_tagged(&s.parts[call & 1u][k][i]);
+            x += (uint32_t)(w >> 32) == call + 1u ? __uint_as_float((uint32_t)w) : NAN;
+        }
+        v[k] = x;
+    }
+}
+
+/* The three in a row. */
+template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], RowSum<N> &s, uint32_t call, const RowPlace &p)
+{
+    publish_sums(v, s, call, p);
+    if (p.tx > 32) __syncthreads();
+    if (p.parts > 1) send_sums(s, call, p);
+    collect_sums(v, s, call, p);
 }
 
 /* 1 / sqrt(mean + eps) */
@@ -367,17 +393,20 @@ template <typename F> struct Ring {
         else if (k == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else asm volatile("cp.async.wait_group 3;" ::: "memory");
     }
-    /* the first four words of the thread, or the last four */
-    __device__ __forceinline__ void read_half(Raw<F> &x, int v, uint32_t at) const
+    /* words 4 v to 4 v + 3 of the thread.  Plain loads: the compiler puts those of a row side by side, but not before the
+       wait or behind the fetch that comes after them */
+    __device__ __forceinline__ void read_half(Raw<F> &x, int v, const unsigned char *smem, uint32_t at) const
     {
-        const uint32_t p = first + at;
+        const unsigned char *p = smem + at + (threadIdx.y * blockDim.x + threadIdx.x) * unit;
         if (F::VEC) {
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(x.w[4 * v]), "=r"(x.w[4 * v + 1]), "=r"(x.w[4 * v + 2]), "=r"(x.w[4 * v + 3]) : "r"(p + v * threads * unit) : "memory");
+            const uint4 q = *reinterpret_cast<const uint4 *>(p + v * threads * unit);
+            x.w[4 * v] = q.x;
+            x.w[4 * v + 1] = q.y;
+            x.w[4 * v + 2] = q.z;
+            x.w[4 * v + 3] = q.w;
         } else {
 #pragma unroll
-            for (int i = 4 * v; i < 4 * v + 4; ++i)
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x.w[i]) : "r"(p + i * threads * unit) : "memory");
+            for (int i = 4 * v; i < 4 * v + 4; ++i) x.w[i] = *reinterpret_cast<const uint32_t *>(p + i * threads * unit);
         }
     }
 };

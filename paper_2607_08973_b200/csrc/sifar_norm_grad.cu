@@ -83,16 +83,24 @@ __device__ __forceinline__ void end_of_gate(const NormGradArgs &a, const Columns
     acc = all_items<F>(0.0f);
 }
 
+/* What a row leaves between the pass that takes its sums and the one that uses them. */
+template <typename F, int N> struct Pending {
+    Items<F> D;                              /* dh + r2 * a */
+    Raw<F> h, z;
+    float r1, r2, sum[N];
+};
+
 /*
  * Both sums of a row in one pass.  With t = dh + r2 * a and f = beta * gate * (post_weight + offset) the second,
  * sum(f * n1 * D) with D = t - r2 * m2 * n2, is sum(f * n1 * t) - r2 * m2 * sum(f * n1 * n2), so that neither has to
- * wait for the other.  h and z stay as they came and are widened again behind the sums: their binary32 forms would take
- * the registers of a second CTA.
+ * wait for the other.
+ * The pass over a row that takes its sums runs before the one that uses those of the row before it: what the sums need
+ * to meet, a barrier, in a cluster a word from every CTA, passes while there is other work.
  */
 template <int DT> constexpr int kGradWords = DT == SIFAR_BF16 ? 4 : 8;
 template <int DT> constexpr int kGradCtas = 1;   /* of kMaxRowThreads threads on an SM */
 
-template <typename F, bool POST, bool PRE>
+template <typename F, bool POST, bool PRE, bool AHEAD>
 __global__ void __launch_bounds__(kMaxRowThreads, kGradCtas<F::DT>) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
     constexpr int kSums = POST && PRE ? 3 : 1;
@@ -144,66 +152,56 @@ __global__ void __launch_bounds__(kMaxRowThreads, kGradCtas<F::DT>) k_block_norm
     const uint32_t places = stage_bytes * a.stages;
     float next1 = POST && live ? a.stats[first] : 1.0f, next2 = PRE && live ? a.stats[a.rows + first] : 1.0f;
 
-    for (uint32_t row = first; row < end; ++row) {
+    auto take_sums = [&](Pending<F, kSums> &o, uint32_t row) {
         const unsigned long long at = row;
-        const float r1 = next1, r2 = next2;
+        o.r1 = next1;
+        o.r2 = next2;
         if (row + 1 < end) {
             if (POST) next1 = a.stats[row + 1];
             if (PRE) next2 = a.stats[a.rows + row + 1];
         }
-        if (row >= gate_end) {                            /* the rows of another gate row begin */
-            if (row != first) end_of_gate(a, c, l, acc, b, first, segment, row);
-            segment = row;
-            gate_end = (row / a.rows_per_gate + 1) * a.rows_per_gate;
-            f = load_factor(a.post_weight, a.offset, c, l);
-            const Items<F> g = gate_factor(a, c, l, row);
-#pragma unroll
-            for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
-        }
-
         if (Ring<F>::possible) ring.wait(a.stages - 1);
-        Items<F> D;                                      /* the gradient of h */
-        Raw<F> xh, xz;
         float2 q2 = both(0.0f), qt = q2, qn = q2;         /* sums of a * n2, f * z * t, f * z * n2 */
 #pragma unroll
-        for (int v = 0; v < F::vectors; ++v) {              /* a half of the items after the other: fewer registers */
+        for (int v = 0; v < F::vectors; ++v) {            /* 16 bytes after 16 bytes: fewer registers */
             constexpr int N = F::vector_pairs;
             Raw<F> x;
             float2 G[N];                                  /* the gradient of the normed h */
             uint32_t from = place;
             auto get = [&](Raw<F> &y, const void *base, uint32_t ld) {
-                if (Ring<F>::possible) { ring.read_half(y, v, from); from += pitch; }
+                if (Ring<F>::possible) { ring.read_half(y, v, ring_bytes, from); from += pitch; }
                 else load_half(y, v, static_cast<const char *>(base) + at * ld, c);
             };
             if (PRE) {
                 get(x, a.dy[0], a.ld_dy);
 #pragma unroll
                 for (int j = 0; j < N; ++j) G[j] = pair<F>(x, v * N + j);
+#pragma unroll 4
                 for (int r = 1; r < partials; ++r) {
                     get(x, a.dy[r], a.ld_dy);
 #pragma unroll
                     for (int j = 0; j < N; ++j) add_pair<F>(G[j], x, v * N + j);
                 }
-                get(xh, a.h, a.ld_h);
+                get(o.h, a.h, a.ld_h);
             }
             if (a.dh) get(x, a.dh, a.ld_dh);
 #pragma unroll
-            for (int j = 0; j < N; ++j) D.p[v * N + j] = a.dh ? pair<F>(x, v * N + j) : both(0.0f);
-            if (with_z) get(xz, a.z, a.ld_z);
+            for (int j = 0; j < N; ++j) o.D.p[v * N + j] = a.dh ? pair<F>(x, v * N + j) : both(0.0f);
+            if (with_z) get(o.z, a.z, a.ld_z);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const int i = v * N + j;
                 float2 n2;
                 if (PRE) {
-                    n2 = __fmul2_rn(pair<F>(xh, i), both(r2));
+                    n2 = __fmul2_rn(pair<F>(o.h, i), both(o.r2));
                     pre.p[i] = __ffma2_rn(G[j], n2, pre.p[i]);
                     G[j] = __fmul2_rn(G[j], w2.p[i]);
                     q2 = __ffma2_rn(G[j], n2, q2);
-                    D.p[i] = __ffma2_rn(both(r2), G[j], D.p[i]);
+                    o.D.p[i] = __ffma2_rn(both(o.r2), G[j], o.D.p[i]);
                 }
                 if (POST) {
-                    const float2 fz = __fmul2_rn(f.p[i], pair<F>(xz, i));
-                    qt = __ffma2_rn(fz, D.p[i], qt);
+                    const float2 fz = __fmul2_rn(f.p[i], pair<F>(o.z, i));
+                    qt = __ffma2_rn(fz, o.D.p[i], qt);
                     if (PRE) qn = __ffma2_rn(fz, n2, qn);
                 }
             }
@@ -212,35 +210,84 @@ __global__ void __launch_bounds__(kMaxRowThreads, kGradCtas<F::DT>) k_block_norm
             fetch(place, row + a.stages);                 /* the thread has read its places */
             place = place + stage_bytes == places ? 0u : place + stage_bytes;
         }
-        float sum[kSums];
-        sum[0] = PRE ? q2.x + q2.y : qt.x + qt.y;
-        if (kSums == 3) { sum[1 % kSums] = qt.x + qt.y; sum[2 % kSums] = qn.x + qn.y; }
-        if (POST || PRE) row_sums(sum, s, row - first, p);
-        const float m2 = PRE ? r2 * (sum[0] * inv) : 0.0f;
-        const float m1 = !POST ? 0.0f : r1 * ((PRE ? sum[1 % kSums] - m2 * sum[2 % kSums] : sum[0]) * inv);
+        o.sum[0] = PRE ? q2.x + q2.y : qt.x + qt.y;
+        if (kSums == 3) { o.sum[1 % kSums] = qt.x + qt.y; o.sum[2 % kSums] = qn.x + qn.y; }
+        if (POST || PRE) publish_sums(o.sum, s, row - first, p);
+    };
+
+    auto use_sums = [&](Pending<F, kSums> &o, uint32_t row) {
+        const unsigned long long at = row;
+        Items<F> &D = o.D;                                /* from here on the gradient of h */
+        if (POST || PRE) collect_sums(o.sum, s, row - first, p);
+        const float m2 = PRE ? o.r2 * (o.sum[0] * inv) : 0.0f;
+        const float m1 = !POST ? 0.0f : o.r1 * ((PRE ? o.sum[1 % kSums] - m2 * o.sum[2 % kSums] : o.sum[0]) * inv);
         if (PRE) {
 #pragma unroll
-            for (int j = 0; j < D.N; ++j) D.p[j] = __ffma2_rn(both(-m2 * r2), pair<F>(xh, j), D.p[j]);
+            for (int j = 0; j < D.N; ++j) D.p[j] = __ffma2_rn(both(-m2 * o.r2), pair<F>(o.h, j), D.p[j]);
         }
         if (a.dresidual) {
-            Items<F> o;
+            Items<F> r;
 #pragma unroll
-            for (int j = 0; j < D.N; ++j) o.p[j] = __fmul2_rn(both(a.alpha), D.p[j]);
-            store_items(static_cast<char *>(a.dresidual) + at * a.ld_dresidual, o, c, l);
+            for (int j = 0; j < D.N; ++j) r.p[j] = __fmul2_rn(both(a.alpha), D.p[j]);
+            store_items(static_cast<char *>(a.dresidual) + at * a.ld_dresidual, r, c, l);
         }
         if (with_z) {
 #pragma unroll
             for (int j = 0; j < D.N; ++j) {
-                const float2 n1 = POST ? __fmul2_rn(pair<F>(xz, j), both(r1)) : pair<F>(xz, j);
+                const float2 n1 = POST ? __fmul2_rn(pair<F>(o.z, j), both(o.r1)) : pair<F>(o.z, j);
                 acc.p[j] = __ffma2_rn(D.p[j], n1, acc.p[j]);
                 D.p[j] = __fmul2_rn(f.p[j], D.p[j]);
-                if (POST) D.p[j] = __fmul2_rn(both(r1), __ffma2_rn(both(-m1), n1, D.p[j]));
+                if (POST) D.p[j] = __fmul2_rn(both(o.r1), __ffma2_rn(both(-m1), n1, D.p[j]));
             }
         } else {
 #pragma unroll
             for (int j = 0; j < D.N; ++j) D.p[j] = __fmul2_rn(f.p[j], D.p[j]);
         }
         if (a.dx) store_items(static_cast<char *>(a.dx) + at * a.ld_dx, D, c, l);
+    };
+
+    auto gate_of = [&](uint32_t row) {                    /* the rows of another gate row begin */
+        segment = row;
+        gate_end = (row / a.rows_per_gate + 1) * a.rows_per_gate;
+        f = load_factor(a.post_weight, a.offset, c, l);
+        const Items<F> g = gate_factor(a, c, l, row);
+#pragma unroll
+        for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], g.p[j]);
+    };
+
+    if (!AHEAD) {
+        for (uint32_t row = first; row < end; ++row) {
+            if (row >= gate_end) {
+                if (row != first) end_of_gate(a, c, l, acc, b, first, segment, row);
+                gate_of(row);
+            }
+            Pending<F, kSums> now;
+            take_sums(now, row);
+            if ((POST || PRE) && p.tx > 32) __syncthreads();
+            if ((POST || PRE) && p.parts > 1) send_sums(s, row - first, p);
+            use_sums(now, row);
+        }
+    } else {
+        Pending<F, kSums> last;                           /* of row - 1, if `pending` */
+        bool pending = false;
+        for (uint32_t row = first; live; ++row) {
+            if (pending && p.parts > 1 && (POST || PRE)) send_sums(s, row - 1 - first, p);
+            if (row < end && row >= gate_end) {
+                if (pending) {
+                    use_sums(last, row - 1);
+                    pending = false;
+                    end_of_gate(a, c, l, acc, b, first, segment, row);
+                }
+                gate_of(row);
+            }
+            Pending<F, kSums> now;
+            if (row < end) take_sums(now, row);
+            if (pending) use_sums(last, row - 1);
+            if (row >= end) break;
+            last = now;
+            pending = true;
+            if (p.tx > 32) __syncthreads();
+        }
     }
     if (Ring<F>::possible) ring.wait(0);
     if (!live) return;
@@ -317,15 +364,27 @@ struct GradShape {
     unsigned ry, per_sm;                     /* blocks of a CTA, CTAs of an SM */
     uint32_t blocks;
 };
+
+/* Clusters of `parts` CTAs that a B200 holds at once with k CTAs per SM (cudaOccupancyMaxActiveClusters): its GPCs do not
+   all have a multiple of 4 SMs. */
+static unsigned clusters_at_once(unsigned parts, unsigned k)
+{
+    static const unsigned four[4] = {33, 71, 104, 142}, eight[4] = {15, 33, 48, 71};
+    if (parts <= 2) return kSms * k / parts;
+    const unsigned *t = parts == 4 ? four : eight;
+    return k <= 4 ? t[k - 1] : t[3] * (k / 4);
+}
+
 template <int DT> GradShape grad_shape_of(size_t rows, size_t cols)
 {
+    const int items = kGradWords<DT> * 4 / (int)elem_size(DT);
     GradShape s;
-    s.row = row_shape(kGradWords<DT> * 4 / (int)elem_size(DT), cols);
+    s.row = row_shape(items, cols);
     s.ry = s.row.tx == 32 ? 4 : 1;
-    s.per_sm = kMaxRowThreads * kGradCtas<DT> / (s.row.tx * s.ry);
+    s.per_sm = kMaxRowThreads / (s.row.tx * s.ry);
+    uint32_t most = clusters_at_once(s.row.parts, s.per_sm) * s.ry;
     /* few rows: a CTA of its own for each */
-    while (s.ry > 1 && rows <= (size_t)kSms * s.per_sm * (s.ry / 2)) s.ry /= 2;
-    const size_t most = (size_t)(kSms * s.per_sm / s.row.parts) * s.ry;
+    while (s.ry > 1 && rows <= most / 2) { s.ry /= 2; most /= 2; }
     s.blocks = (uint32_t)(rows < most ? rows : most);
     return s;
 }
@@ -335,12 +394,11 @@ static GradShape grad_shape(int dtype, size_t rows, size_t cols)
 }
 
 /* The attribute for the ring's shared memory is set once per kernel and device. */
-template <int DT, bool VEC, bool POST, bool PRE>
-static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
+template <typename F, bool POST, bool PRE, bool AHEAD>
+static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
-    using F = Form<DT, kGradWords<DT>, VEC>;
     static std::atomic<unsigned long long> ready{0};
-    const auto kernel = k_block_norm_grad<F, POST, PRE>;
+    const auto kernel = k_block_norm_grad<F, POST, PRE, AHEAD>;
     size_t stages = 1, smem = 0;
     if (Ring<F>::possible) {
         const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes, turns = (a.rows + sh.blocks - 1) / sh.blocks;
@@ -360,6 +418,15 @@ static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStrea
     a.stages = (uint32_t)stages;
     const dim3 grid((sh.blocks + sh.ry - 1) / sh.ry * sh.row.parts), block(sh.row.tx, sh.ry);
     return launch_op(kernel, grid, block, sh.row.parts, smem, stream, a);
+}
+
+template <int DT, bool VEC, bool POST, bool PRE>
+static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
+{
+    using F = Form<DT, kGradWords<DT>, VEC>;
+    if constexpr (DT == SIFAR_BF16)
+        if (sh.row.parts > 1) return launch_grad_k<F, POST, PRE, true>(sh, arrays, stream, a);
+    return launch_grad_k<F, POST, PRE, false>(sh, arrays, stream, a);
 }
 
 template <int DT, bool VEC>
