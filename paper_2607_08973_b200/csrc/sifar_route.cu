@@ -139,6 +139,14 @@ __device__ __forceinline__ double sigmoid(double l)
     return (l < 0.0 ? t : 1.0) / (1.0 + t);
 }
 
+/* One step; 0 of infinity. */
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 /* s / (sum of the chosen s) needs the s only up to a common factor: where all chosen logits are negative they are
    scaled up by exp(-max), so that the ratio does not underflow with them. */
 __device__ __forceinline__ float scaled_sigmoid(float l, float max)
@@ -154,13 +162,20 @@ template <typename F> __device__ __forceinline__ F group_value(const F *v, int p
 {
     const int lane = threadIdx.x & 31, g = lane >> shift, step = 1 << shift;
     F m1 = -INFINITY, m2 = -INFINITY;
-    if (g < groups) {
+    const auto look = [&](F x) {
+        m2 = max(m2, min(m1, x));
+        m1 = max(m1, x);
+    };
+    const int share = per >> shift;
+    if (sizeof(F) == 4 && share << shift == per && (share & 3) == 0) {
+        if (g < groups)                                   /* vectors: a lane's share of the group lies side by side */
+            for (int i = 0; i < share; i += 4) {
+                const float4 q = *reinterpret_cast<const float4 *>(v + lane * share + i);
+                look((F)q.x); look((F)q.y); look((F)q.z); look((F)q.w);
+            }
+    } else if (g < groups) {
 #pragma unroll 4
-        for (int i = lane & (step - 1); i < per; i += step) {
-            const F x = v[g * per + i];
-            m2 = max(m2, min(m1, x));
-            m1 = max(m1, x);
-        }
+        for (int i = lane & (step - 1); i < per; i += step) look(v[g * per + i]);
     }
     for (int d = step / 2; d > 0; d >>= 1) {
         const F o1 = __shfl_xor_sync(0xFFFFFFFFu, m1, d), o2 = __shfl_xor_sync(0xFFFFFFFFu, m2, d);
@@ -321,13 +336,11 @@ __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 :
 #pragma unroll
             for (int j = 0; j < NI; ++j) v[j] = top == -INFINITY ? 0.0f : __expf(v[j] - top) * inv;
         } else {
-            /* __expf: two steps and the argument's product, |l| exp(-|l|) <= 0.37 steps; the quotient: two steps */
-            fixed = 2.5f * 0x1p-21f;
+            /* 1 / (1 + exp(-l)): the exponential's two steps and its argument's product count s (1 - s) times, the sum and
+               the reciprocal s times: below 2^-22 together */
+            fixed = 2.5f * 0x1p-22f;
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const float t = __expf(-fabsf(v[j]));
-                v[j] = __fdividef(v[j] < 0.0f ? t : 1.0f, 1.0f + t);
-            }
+            for (int j = 0; j < NI; ++j) v[j] = reciprocal(1.0f + __expf(-v[j]));
         }
         relative = 2.5f * 0x1p-24f + 1.25f * NI * 0x1p-23f;
         if (BIAS) {
@@ -348,15 +361,15 @@ __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 :
 #pragma unroll
         for (int j = 0; j < NI; ++j) sf[j * 32 + lane] = v[j];
         __syncwarp();
-        const int shift = group_shift(a.groups);
+        const int shift = group_shift(a.groups), mygroup = lane >> shift;
         const float mine = group_value(sf, a.per, a.groups, shift, a.group_score == SIFAR_GROUP_TOP2);
-        uint32_t k = lane >> shift < a.groups ? key_of(mine) : 0u, least = 0u;
+        uint32_t k = mygroup < a.groups ? key_of(mine) : 0u, least = 0u;
         open = 0u;
         for (int i = 0; i < a.top_groups; ++i) {
             least = __reduce_max_sync(0xFFFFFFFFu, k);
             const int g = (__ffs(__ballot_sync(0xFFFFFFFFu, k == least)) - 1) >> shift;
             open |= 1u << g;
-            if (lane >> shift == g) k = 0u;
+            if (mygroup == g) k = 0u;
         }
         if (scored) {
             const float x = of_key(least), y = of_key(__reduce_max_sync(0xFFFFFFFFu, k));
@@ -378,12 +391,23 @@ __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 :
     }
     if (!BIAS) { fixed = relative = 0.0f; lost = false; }
 
+    uint32_t in = 0xFFFFFFFFu;                            /* bit j: item j is in an open group */
+    if (GROUPS) {
+        in = 0u;
+        if ((a.per & 31) == 0) {                          /* a group is a.per / 32 items of every lane */
+            const int items = a.per >> 5;
+            for (uint32_t rest = open; rest; rest &= rest - 1u) in |= ((1u << items) - 1u) << ((__ffs(rest) - 1) * items);
+        } else {
+#pragma unroll
+            for (int j = 0; j < NI; ++j) in |= (open >> ((uint32_t)(j * 32 + lane) * a.per_magic >> 20) & 1u) << j;
+        }
+    }
     uint32_t key[NI];
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
         const uint32_t u = __float_as_uint(v[j] + 0.0f);
         key[j] = ((u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u)) & ~kCut) | (kCut - (uint32_t)j);
-        if (!is_expert<NI>(j, a.experts) || (GROUPS && !(open >> ((uint32_t)(j * 32 + lane) * a.per_magic >> 20) & 1u))) key[j] = 0u;
+        if (!is_expert<NI>(j, a.experts) || (GROUPS && !(in >> j & 1u))) key[j] = 0u;
     }
     sort_keys(key);
 
@@ -438,9 +462,9 @@ __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 :
         w = softmax ? expf(logit - max) : scaled_sigmoid(logit, max);
         if (!mine || max == -INFINITY) w = 0.0f;
         const float total = sifar::warp_sum(w);
-        w = max == -INFINITY ? 0.0f : w / total;
+        w = max == -INFINITY ? 0.0f : __fdividef(w, total);
     } else if (softmax) {
-        w = top == -INFINITY ? 0.0f : expf(logit - top) / sum;
+        w = top == -INFINITY ? 0.0f : __fdividef(expf(logit - top), sum);
     } else {
         w = sigmoid(logit);
     }
