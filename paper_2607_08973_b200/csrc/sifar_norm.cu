@@ -20,10 +20,10 @@ struct NormArgs {
  * One row per threadIdx.y (and cluster).  All loads of a row go out before the first sum; z, h and y never leave the
  * registers between.  PT is P or the next power of two above it.
  */
-template <int PT> constexpr int kNormRegisters = PT <= 4 ? 72 : 128;
+template <typename F, int PT> constexpr int kNormRegisters = F::W > 8 ? 112 : PT > 4 ? 128 : F::DT == SIFAR_BF16 && PT > 2 ? 80 : 72;
 
 template <typename F, int PT>
-__global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(kNormRegisters<PT>) k_block_norm(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F, PT>)) k_block_norm(const __grid_constant__ NormArgs a)
 {
     __shared__ __align__(16) RowSum<1> s;
     grid_let_next_in();
@@ -38,30 +38,40 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(kNormRegisters<PT>
     const unsigned long long at = live ? row : 0u;
     grid_wait();
 
-    Raw<F> x[PT], res, rg, rw1, rw2;
+    constexpr int B = F::W == 8 ? PT : F::DT == SIFAR_BF16 ? 2 : 4;     /* partials under way at once */
+    Raw<F> res, rg, rw1, rw2;
+    Items<F> f;
     const char *gate = nullptr;
     if (a.gate) gate = static_cast<const char *>(a.gate) + (unsigned long long)((uint32_t)at / a.rows_per_gate) * a.ld_gate;
-    if (!l.ragged) {
-        const unsigned long long o = at * a.ld_x;
 #pragma unroll
-        for (int r = 0; r < PT; ++r)
-            if (r < a.P) load_whole(x[r], static_cast<const char *>(a.x[r]) + o, l);
-        if (a.residual) load_whole(res, static_cast<const char *>(a.residual) + at * a.ld_residual, l);
-    } else {
+    for (int r0 = 0; r0 < PT; r0 += B) {
+        if (r0 >= a.P) break;
+        Raw<F> x[B];
 #pragma unroll
-        for (int r = 0; r < PT; ++r)
-            if (r < a.P) load_each(x[r], static_cast<const char *>(a.x[r]) + at * a.ld_x, c);
-        if (a.residual) load_each(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c);
+        for (int r = 0; r < B; ++r) {
+            if (r0 + r >= a.P) continue;
+            const char *row_r = static_cast<const char *>(a.x[r0 + r]) + at * a.ld_x;
+            if (!l.ragged) load_whole(x[r], row_r, l);
+            else load_each(x[r], row_r, c);
+        }
+        if (r0 == 0) {                                    /* what the sums do not wait for goes out behind the first partials */
+            if (a.residual) {
+                const char *row_r = static_cast<const char *>(a.residual) + at * a.ld_residual;
+                if (!l.ragged) load_whole(res, row_r, l);
+                else load_each(res, row_r, c);
+            }
+            if (F::W == 8) {
+                if (a.gate) load_weight(rg, gate, c, l);
+                if (a.post_weight) load_weight(rw1, a.post_weight, c, l);
+                if (a.pre_weight) load_weight(rw2, a.pre_weight, c, l);
+            }
+            f = items<F>(x[0]);
+        }
+#pragma unroll
+        for (int r = r0 == 0 ? 1 : 0; r < B; ++r)
+            if (r0 + r < a.P) add_items(f, x[r]);
     }
-    if (a.gate) load_weight(rg, gate, c, l);
-    if (a.post_weight) load_weight(rw1, a.post_weight, c, l);
-    if (a.pre_weight) load_weight(rw2, a.pre_weight, c, l);
     if (a.parts > 1) cluster_wait();
-
-    Items<F> f = items<F>(x[0]);
-#pragma unroll
-    for (int r = 1; r < PT; ++r)
-        if (r < a.P) add_items(f, x[r]);
     if (a.z) store_items(static_cast<char *>(a.z) + at * a.ld_z, f, c, l);
 
     float r1 = 1.0f, r2 = 1.0f;
@@ -73,11 +83,13 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(kNormRegisters<PT>
 #pragma unroll
         for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r1));
         if (a.post_weight) {
+            if (F::W > 8) load_weight(rw1, a.post_weight, c, l);
 #pragma unroll
             for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair<F>(rw1, j), both(a.offset)));
         }
     }
     if (a.gate) {
+        if (F::W > 8) load_weight(rg, gate, c, l);
 #pragma unroll
         for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], pair<F>(rg, j));
     }
@@ -96,6 +108,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(kNormRegisters<PT>
 #pragma unroll
             for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], both(r2));
             if (a.pre_weight) {
+                if (F::W > 8) load_weight(rw2, a.pre_weight, c, l);
 #pragma unroll
                 for (int j = 0; j < f.N; ++j) f.p[j] = __fmul2_rn(f.p[j], __fadd2_rn(pair<F>(rw2, j), both(a.offset)));
             }
@@ -108,23 +121,21 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(kNormRegisters<PT>
     }
 }
 
-/* 32 bytes of every array per thread */
-template <int DT> constexpr int kNormWords = 8;
-
-template <int DT, int PT>
+template <int DT, int W, int PT>
 static cudaError_t launch_norm_p(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormArgs &a)
 {
-    return vec ? launch_op(k_block_norm<Form<DT, kNormWords<DT>, true>, PT>, grid, block, cluster, 0, stream, a)
-               : launch_op(k_block_norm<Form<DT, kNormWords<DT>, false>, PT>, grid, block, cluster, 0, stream, a);
+    return vec ? launch_op(k_block_norm<Form<DT, W, true>, PT>, grid, block, cluster, 0, stream, a)
+               : launch_op(k_block_norm<Form<DT, W, false>, PT>, grid, block, cluster, 0, stream, a);
 }
 
 template <int DT>
-static cudaError_t launch_norm(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormArgs &a)
+static cudaError_t launch_norm(int words, bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormArgs &a)
 {
-    if (a.P <= 1) return launch_norm_p<DT, 1>(vec, grid, block, cluster, stream, a);
-    if (a.P <= 2) return launch_norm_p<DT, 2>(vec, grid, block, cluster, stream, a);
-    if (a.P <= 4) return launch_norm_p<DT, 4>(vec, grid, block, cluster, stream, a);
-    return launch_norm_p<DT, 8>(vec, grid, block, cluster, stream, a);
+    if (words == 16) return launch_norm_p<DT, 16, 8>(vec, grid, block, cluster, stream, a);
+    if (a.P <= 1) return launch_norm_p<DT, 8, 1>(vec, grid, block, cluster, stream, a);
+    if (a.P <= 2) return launch_norm_p<DT, 8, 2>(vec, grid, block, cluster, stream, a);
+    if (a.P <= 4) return launch_norm_p<DT, 8, 4>(vec, grid, block, cluster, stream, a);
+    return launch_norm_p<DT, 8, 8>(vec, grid, block, cluster, stream, a);
 }
 
 }  /* namespace sifar */
@@ -189,7 +200,13 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     a.rows_per_gate = (uint32_t)span;
     a.alpha = g->alpha; a.beta = g->beta; a.eps = g->eps; a.offset = g->weight_offset;
     a.P = g->P; a.post = g->post_norm != 0; a.pre = g->pre_norm != 0;
-    const RowShape sh = row_shape((g->dtype == SIFAR_BF16 ? kNormWords<SIFAR_BF16> : kNormWords<SIFAR_F32>) * 4 / (int)es, cols);
+    /* 32 bytes of an array per thread; 64 where that keeps many rows out of clusters, whose sums cost more: 2000 x 8192
+       fp32 104 -> 62 us, 4000 x 16384 bf16 220 -> 132 (four ranks: 245 -> 197).  Not where the row is just longer than a
+       CTA (2000 x 4200 fp32: 39 against 47 us; from 9/8 on the 64 bytes win), not for more than four ranks (2000 x 8192
+       fp32, eight: 131 against 147 us), not for few rows (one of 8192 fp32: 4.4 against 5.7 us). */
+    const size_t cta = (size_t)kMaxRowThreads * 32 / es;
+    const int words = rows > kSms && g->P <= 4 && cols > cta + cta / 8 && cols <= 2 * cta ? 16 : 8;
+    const RowShape sh = row_shape(words * 4 / (int)es, cols);
     a.parts = sh.parts;
     /* short rows: several to a CTA once there is one for every SM */
     unsigned ry = 1;
@@ -197,8 +214,8 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     const unsigned long long grid = (rows + ry - 1) / ry * sh.parts;
     if (grid > 0x7FFFFFFFull) { set_error("%s: too many rows of this width", fn); return SIFAR_ERR_INVALID; }
     const dim3 gd((unsigned)grid), bd(sh.tx, ry);
-    const cudaError_t err = g->dtype == SIFAR_BF16 ? launch_norm<SIFAR_BF16>(vec, gd, bd, sh.parts, (cudaStream_t)stream, a)
-                                                   : launch_norm<SIFAR_F32>(vec, gd, bd, sh.parts, (cudaStream_t)stream, a);
+    const cudaError_t err = g->dtype == SIFAR_BF16 ? launch_norm<SIFAR_BF16>(words, vec, gd, bd, sh.parts, (cudaStream_t)stream, a)
+                                                   : launch_norm<SIFAR_F32>(words, vec, gd, bd, sh.parts, (cudaStream_t)stream, a);
     SIFAR_CUDA(err);
     return SIFAR_OK;
 }

@@ -1,11 +1,9 @@
 /*
  * How the norm kernels lay a row over threads, and the sums over a row.
  *
- * A thread holds 16 or 32 bytes of every array of a row in registers from its first load to its
- * last store, so a row is read once however many sums go over it.  A row takes `tx` threads of a CTA; where it is longer
- * than a CTA of kMaxRowThreads holds, a cluster of up to eight CTAs has it and its sums meet in their shared memory.
- * (16 bytes of bf16 per thread: 109 us for the backward pass of 8192 x 4096 and two ranks instead of what stands there;
- * what a thread does per row whatever its items, addresses, exchanges, barriers, was more than half of its work.)
+ * A thread holds 16, 32 or 64 bytes of every array of a row in registers from its first load to its last store, so a row
+ * is read once however many sums go over it.  A row takes `tx` threads of a CTA; where it is longer than a CTA of
+ * kMaxRowThreads holds, a cluster of up to eight CTAs has it and its sums meet in their shared memory.
  */
 #ifndef SIFAR_NORM_CUH
 #define SIFAR_NORM_CUH

@@ -97,11 +97,12 @@ template <typename F, int N> struct Pending {
  * The pass over a row that takes its sums runs before the one that uses those of the row before it: what the sums need
  * to meet, a barrier, in a cluster a word from every CTA, passes while there is other work.
  */
+/* 16 bytes of an array per thread in bf16: with 32 the sums over rows spill (8192 x 4096, two ranks: 107 us against 134;
+   two CTAs per SM with 64 registers each: 163). */
 template <int DT> constexpr int kGradWords = DT == SIFAR_BF16 ? 4 : 8;
-template <int DT> constexpr int kGradCtas = 1;   /* of kMaxRowThreads threads on an SM */
 
 template <typename F, bool POST, bool PRE, bool AHEAD>
-__global__ void __launch_bounds__(kMaxRowThreads, kGradCtas<F::DT>) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
+__global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
     constexpr int kSums = POST && PRE ? 3 : 1;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
@@ -298,58 +299,61 @@ __global__ void __launch_bounds__(kMaxRowThreads, kGradCtas<F::DT>) k_block_norm
 struct NormSumArgs {
     const float *sum_post, *sum_pre, *sum_gate;
     float *dpost_weight, *dpre_weight, *dgate;
-    uint32_t rows, cols, pitch, blocks, rows_per_gate, gates;
+    uint32_t rows, cols, pitch, blocks, rows_per_gate, gates, gate_jobs, gate_warps;
 };
 
-/* 32 columns of a CTA: out[column] = the sum of `n` rows that are `step` floats apart. */
-__device__ __forceinline__ void sum_blocks(const float *p, uint32_t n, size_t step, uint32_t col, uint32_t cols, float *out,
-                                           float (*s)[32])
-{
-    float v = 0.0f;
-    if (col < cols) {
-#pragma unroll 4
-        for (uint32_t i = threadIdx.y; i < n; i += kSumWarps) v += p[i * step + col];
-    }
-    s[threadIdx.y][threadIdx.x] = v;
-    __syncthreads();
-    if (threadIdx.y == 0 && col < cols) {
-        for (uint32_t i = 1; i < kSumWarps; ++i) v += s[i][threadIdx.x];
-        out[col] = v;
-    }
-    __syncthreads();
-}
-
-/* blockIdx.y = 0: post weight, 1: pre weight, from 2 on: the gate rows in turn. */
-__global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const NormSumArgs a)
+/*
+ * 32 columns per CTA, its warps over the blocks: blockIdx.y = 0 the post weight, 1 the pre weight, from 2 on the gate
+ * rows that lie in more than one block, `gate_warps` warps each.  A gate row has a few blocks, a weight all of them:
+ * with all warps on one gate row at a time 17 gate rows of 1003 x 4099 took 11 us.
+ */
+__global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid_constant__ NormSumArgs a)
 {
     __shared__ float s[kSumWarps][32];
     grid_let_next_in();
     grid_wait();
-    const uint32_t col = blockIdx.x * 32 + threadIdx.x;
-    if (blockIdx.y == 0) {
-        if (a.dpost_weight) sum_blocks(a.sum_post, a.blocks, a.pitch, col, a.cols, a.dpost_weight, s);
-    } else if (blockIdx.y == 1) {
-        if (a.dpre_weight) sum_blocks(a.sum_pre, a.blocks, a.pitch, col, a.cols, a.dpre_weight, s);
+    const uint32_t col = blockIdx.x * 32 + threadIdx.x, warp = threadIdx.y;
+    const uint32_t team = blockIdx.y < 2 ? kSumWarps : a.gate_warps, member = warp % team;
+    const float *p = nullptr;                             /* of the member's blocks; the first one may lie elsewhere */
+    float *out = nullptr;
+    size_t step = a.pitch;
+    uint32_t n = 0;
+    float v = 0.0f;
+    if (blockIdx.y < 2) {
+        p = blockIdx.y == 0 ? a.sum_post : a.sum_pre;
+        out = blockIdx.y == 0 ? a.dpost_weight : a.dpre_weight;
+        n = out ? a.blocks : 0u;
     } else {
-        for (uint32_t g = blockIdx.y - 2; g < a.gates; g += gridDim.y - 2) {
-            const unsigned long long last = min((unsigned long long)(g + 1ull) * a.rows_per_gate, (unsigned long long)a.rows) - 1;
-            const uint32_t r0 = g * a.rows_per_gate;
-            const uint32_t b0 = block_of(a.rows, a.blocks, r0), b1 = block_of(a.rows, a.blocks, (uint32_t)last);
-            if (b0 == b1) continue;                       /* within one block: already there */
-            /* place 0 or 1 of the first block, place 0 of all others */
-            const uint32_t place = block_start(a.rows, a.blocks, b0) == r0 ? 0u : 1u;
-            float v = 0.0f;
-            if (col < a.cols)
-                for (uint32_t i = threadIdx.y; i <= b1 - b0; i += kSumWarps)
-                    v += a.sum_gate[((size_t)(b0 + i) * 2 + (i ? 0u : place)) * a.pitch + col];
-            s[threadIdx.y][threadIdx.x] = v;
-            __syncthreads();
-            if (threadIdx.y == 0 && col < a.cols) {
-                for (uint32_t i = 1; i < kSumWarps; ++i) v += s[i][threadIdx.x];
-                a.dgate[(size_t)g * a.cols + col] = v;
+        const uint32_t job = (blockIdx.y - 2) * (kSumWarps / team) + warp / team;
+        /* more gate rows than blocks: one of them at most lies across the end of block `job` */
+        const uint32_t g = a.gates < a.blocks || job + 1 >= a.blocks ? job : block_start(a.rows, a.blocks, job + 1) / a.rows_per_gate;
+        if (job < a.gate_jobs) {
+            const uint32_t r0 = g * a.rows_per_gate, r1 = a.rows - r0 > a.rows_per_gate ? r0 + a.rows_per_gate - 1 : a.rows - 1;
+            const uint32_t b0 = block_of(a.rows, a.blocks, r0), b1 = block_of(a.rows, a.blocks, r1);
+            /* within one block: already there; across several ends: the first end's */
+            if (b0 != b1 && (a.gates < a.blocks || b0 == job)) {
+                /* place 0 or 1 of the first block, place 0 of all others */
+                n = b1 - b0 + 1;
+                p = a.sum_gate + (size_t)b0 * 2 * a.pitch;
+                step = 2 * (size_t)a.pitch;
+                out = a.dgate + (size_t)g * a.cols;
+                if (member == 0 && col < a.cols) {
+                    const uint32_t place = block_start(a.rows, a.blocks, b0) == r0 ? 0u : 1u;
+                    v = p[(size_t)place * a.pitch + col];
+                }
             }
-            __syncthreads();
         }
+    }
+    const bool gate = blockIdx.y >= 2;
+    if (out && col < a.cols) {
+#pragma unroll 8
+        for (uint32_t i = member + (gate && member == 0 ? team : 0u); i < n; i += team) v += p[i * step + col];
+    }
+    s[warp][threadIdx.x] = v;
+    __syncthreads();
+    if (member == 0 && out && col < a.cols) {
+        for (uint32_t i = 1; i < team; ++i) v += s[warp + i][threadIdx.x];
+        out[col] = v;
     }
 }
 
@@ -424,6 +428,8 @@ template <int DT, bool VEC, bool POST, bool PRE>
 static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
     using F = Form<DT, kGradWords<DT>, VEC>;
+    /* bf16 in clusters: a row ahead (2000 x 8200: 162 -> 124 us).  Without a cluster the barrier costs less than what the
+       second row takes (8192 x 4096: 107 -> 115 us), fp32 has no registers for it (1003 x 4099: 50 -> 56 us). */
     if constexpr (DT == SIFAR_BF16)
         if (sh.row.parts > 1) return launch_grad_k<F, POST, PRE, true>(sh, arrays, stream, a);
     return launch_grad_k<F, POST, PRE, false>(sh, arrays, stream, a);
@@ -554,8 +560,11 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         q.dpost_weight = g->dpost_weight; q.dpre_weight = g->dpre_weight; q.dgate = g->dgate;
         q.rows = a.rows; q.cols = a.cols; q.pitch = a.pitch; q.blocks = a.blocks; q.rows_per_gate = a.rows_per_gate;
         q.gates = g->dgate ? (uint32_t)gates : 0u;
-        const unsigned gate_turns = q.gates < 64u ? q.gates : 64u;
-        const dim3 grid((unsigned)((cols + 31) / 32), 2 + gate_turns), block(32, kSumWarps);
+        q.gate_warps = 1;
+        while (q.gates && q.gate_warps < kSumWarps && q.blocks / q.gates >= 8 * q.gate_warps) q.gate_warps *= 2;
+        const unsigned teams = kSumWarps / q.gate_warps;
+        q.gate_jobs = q.gates < q.blocks ? q.gates : q.blocks ? q.blocks - 1 : 0u;
+        const dim3 grid((unsigned)((cols + 31) / 32), 2 + (q.gate_jobs + teams - 1) / teams), block(32, kSumWarps);
         SIFAR_CUDA(launch_op(k_block_norm_sums, grid, block, 1, 0, (cudaStream_t)stream, q));
     }
     return SIFAR_OK;
