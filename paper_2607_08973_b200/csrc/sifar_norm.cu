@@ -13,7 +13,7 @@ struct NormArgs {
     uint32_t ld_x, ld_residual, ld_gate, ld_z, ld_h, ld_y;    /* bytes between two rows */
     float alpha, beta, eps, offset;
     uint32_t rows, cols, parts, rows_per_gate;
-    int P, post, pre;
+    int P, post, pre, narrow;                /* narrow: rows so short that a vector may reach over the one beside it */
 };
 
 /*
@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F,
     const Columns<F> c(p.part, p.tx, p.t, live ? a.cols : 0u);
     const Lane<F> l(c);
     const unsigned long long at = live ? row : 0u;
+    const bool edge = at == 0 || at + 1 >= a.rows || a.narrow;
     grid_wait();
 
     constexpr int B = F::W == 8 ? PT : F::DT == SIFAR_BF16 ? 2 : 4;     /* partials under way at once */
@@ -47,19 +48,15 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F,
     for (int r0 = 0; r0 < PT; r0 += B) {
         if (r0 >= a.P) break;
         Raw<F> x[B];
+        const auto load = [&](bool each) {
 #pragma unroll
-        for (int r = 0; r < B; ++r) {
-            if (r0 + r >= a.P) continue;
-            const char *row_r = static_cast<const char *>(a.x[r0 + r]) + at * a.ld_x;
-            if (!l.ragged) load_whole(x[r], row_r, l);
-            else load_each(x[r], row_r, c);
-        }
-        if (r0 == 0) {                                    /* what the sums do not wait for goes out behind the first partials */
-            if (a.residual) {
-                const char *row_r = static_cast<const char *>(a.residual) + at * a.ld_residual;
-                if (!l.ragged) load_whole(res, row_r, l);
-                else load_each(res, row_r, c);
-            }
+            for (int r = 0; r < B; ++r)
+                if (r0 + r < a.P) load_row(x[r], static_cast<const char *>(a.x[r0 + r]) + at * a.ld_x, c, l, each);
+            if (r0 == 0 && a.residual) load_row(res, static_cast<const char *>(a.residual) + at * a.ld_residual, c, l, each);
+        };
+        if (by_element(l, edge)) load(true);
+        else load(false);
+        if (r0 == 0) {
             if (F::W == 8) {
                 if (a.gate) load_weight(rg, gate, c, l);
                 if (a.post_weight) load_weight(rw1, a.post_weight, c, l);
@@ -124,8 +121,8 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F,
 template <int DT, int W, int PT>
 static cudaError_t launch_norm_p(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormArgs &a)
 {
-    return vec ? launch_op(k_block_norm<Form<DT, W, true>, PT>, grid, block, cluster, 0, stream, a)
-               : launch_op(k_block_norm<Form<DT, W, false>, PT>, grid, block, cluster, 0, stream, a);
+    return vec ? launch_op(k_block_norm<Form<DT, W, kWhole>, PT>, grid, block, cluster, 0, stream, a)
+               : launch_op(k_block_norm<Form<DT, W, DT == SIFAR_BF16 ? kShifted : kElement>, PT>, grid, block, cluster, 0, stream, a);
 }
 
 template <int DT>
@@ -198,6 +195,7 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
     a.ld_x = bytes(g->ld_x); a.ld_residual = bytes(g->ld_residual); a.ld_gate = bytes(g->ld_gate);
     a.ld_z = bytes(g->ld_z); a.ld_h = bytes(g->ld_h); a.ld_y = bytes(g->ld_y);
     a.rows_per_gate = (uint32_t)span;
+    a.narrow = a.ld_x < 32 || a.ld_residual < 32;
     a.alpha = g->alpha; a.beta = g->beta; a.eps = g->eps; a.offset = g->weight_offset;
     a.P = g->P; a.post = g->post_norm != 0; a.pre = g->pre_norm != 0;
     /* 32 bytes of an array per thread; 64 where that keeps many rows out of clusters, whose sums cost more: 2000 x 8192

@@ -17,10 +17,21 @@ namespace sifar {
 constexpr int kMaxRowThreads = 512;
 constexpr unsigned kMaxNormCluster = 8;
 
-/* The form of a kernel: element type, 32-bit words of a row and array per thread, 16-byte accesses (VEC) or elements. */
-template <int DT_, int W_, bool VEC_> struct Form {
+/*
+ * How a kernel reaches its rows.
+ *   kWhole    every row of every array starts on a 16-byte boundary: a vector is one access.
+ *   kShifted  rows start anywhere, as contiguous rows of an odd number of columns do: a vector is put together from the two
+ *             aligned ones that it lies in, and stored in the largest pieces that its address allows.
+ *             (4096 x 4097 bf16: by elements 77 us forward and 244 us back.)
+ *   kElement  single elements, neighbours by neighbouring threads.
+ */
+enum Access { kWhole, kShifted, kElement };
+
+/* The form of a kernel: element type, 32-bit words of a row and array per thread, access. */
+template <int DT_, int W_, Access A_> struct Form {
     static constexpr int DT = DT_, W = W_;
-    static constexpr bool VEC = VEC_;
+    static constexpr Access ACCESS = A_;
+    static constexpr bool VEC = A_ != kElement;
     using T = typename Elem<DT_>::type;
     static constexpr uint32_t es = sizeof(T);
     static constexpr int items = W_ * 4 / (int)sizeof(T), pairs = items / 2;
@@ -42,7 +53,7 @@ template <typename F> struct Columns {
 /*
  * The thread's 16-byte vectors of a row: byte offsets (0 where the row has ended, so that a load may go there all the
  * same and its value is left out later), which of them exist, and whether the warp holds the row's last, short vector
- * and has to look at every element.  Computed once: all rows are alike.
+ * (ragged) and looks at every element.  Computed once: all rows are alike.
  */
 template <typename F> struct Lane {
     uint32_t at[F::vectors];
@@ -65,9 +76,9 @@ template <typename F> struct Lane {
 /* The thread's items of one row as they lie in memory. */
 template <typename F> struct Raw { uint32_t w[F::W]; };
 
-/* Every element looked at: absent ones are 0.  The first four words and the last four, or one of the two. */
+/* Four words (vector v), every element looked at: absent ones are 0. */
 template <typename F>
-__device__ __forceinline__ void load_half(Raw<F> &x, int v, const void *row, const Columns<F> &c)
+__device__ __forceinline__ void load_each(Raw<F> &x, int v, const void *row, const Columns<F> &c)
 {
     using T = typename F::T;
     const T *p = static_cast<const T *>(row);
@@ -81,33 +92,65 @@ __device__ __forceinline__ void load_half(Raw<F> &x, int v, const void *row, con
         }
     }
 }
+
+/* An aligned vector; where the row has ended, some other element of it (or of the next row, behind a short vector). */
 template <typename F>
-__device__ __forceinline__ void load_each(Raw<F> &x, const void *row, const Columns<F> &c)
+__device__ __forceinline__ void load_whole(Raw<F> &x, int v, const void *row, const Lane<F> &l)
 {
-#pragma unroll
-    for (int v = 0; v < F::vectors; ++v) load_half(x, v, row, c);
+    const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + l.at[v]);
+    x.w[4 * v] = q.x;
+    x.w[4 * v + 1] = q.y;
+    x.w[4 * v + 2] = q.z;
+    x.w[4 * v + 3] = q.w;
 }
 
-/* Whole vectors of a row (its warp is not ragged); what lies behind the row's end is some other element of it. */
+/* A vector that starts anywhere, from the two aligned ones around it: their eight words moved down by the bytes between. */
 template <typename F>
-__device__ __forceinline__ void load_whole(Raw<F> &x, const void *row, const Lane<F> &l)
+__device__ __forceinline__ void load_shifted(Raw<F> &x, int v, const void *row, const Lane<F> &l)
 {
+    const uintptr_t p = (uintptr_t)row + l.at[v];
+    const uint32_t m = (uint32_t)p & 15u;
+    const uint4 *g = reinterpret_cast<const uint4 *>(p - m);
+    const uint4 a = g[0], b = g[m ? 1 : 0];
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int v = 0; v < F::vectors; ++v) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const char *>(row) + l.at[v]);
-        x.w[4 * v] = q.x;
-        x.w[4 * v + 1] = q.y;
-        x.w[4 * v + 2] = q.z;
-        x.w[4 * v + 3] = q.w;
-    }
+    for (int i = 0; i < 6; ++i) w[i] = m & 8u ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = m & 4u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.w[4 * v + i] = F::DT == SIFAR_F32 ? w[i] : __funnelshift_r(w[i], w[i + 1], (m & 2u) * 8u);
 }
 
-/* Weights and gates: they may lack the rows' alignment. */
+/* Whether the warp looks at every element of the row: at its ragged end, and in the array's first and last row
+   (`edge`) where a shifted vector might reach out of the array.  The caller branches on it once and passes the constant. */
+template <typename F> __device__ __forceinline__ bool by_element(const Lane<F> &l, bool edge)
+{
+    return F::ACCESS == kElement || l.ragged || (F::ACCESS == kShifted && edge);
+}
+template <typename F>
+__device__ __forceinline__ void load_vector(Raw<F> &x, int v, const void *row, const Columns<F> &c, const Lane<F> &l, bool each)
+{
+    if (F::ACCESS == kElement || each) load_each(x, v, row, c);
+    else if (F::ACCESS == kWhole) load_whole(x, v, row, l);
+    else load_shifted(x, v, row, l);
+}
+template <typename F>
+__device__ __forceinline__ void load_row(Raw<F> &x, const void *row, const Columns<F> &c, const Lane<F> &l, bool each)
+{
+#pragma unroll
+    for (int v = 0; v < F::vectors; ++v) load_vector(x, v, row, c, l, each);
+}
+
+/* Weights and gate rows, whatever the alignment of the rows: nothing around them is read. */
 template <typename F>
 __device__ __forceinline__ void load_weight(Raw<F> &x, const void *row, const Columns<F> &c, const Lane<F> &l)
 {
-    if (!l.ragged && ((uintptr_t)row & 15u) == 0) load_whole(x, row, l);
-    else load_each(x, row, c);
+    const bool whole = F::VEC && !l.ragged && ((uintptr_t)row & 15u) == 0;
+#pragma unroll
+    for (int v = 0; v < F::vectors; ++v) {
+        if (whole) load_whole(x, v, row, l);
+        else load_each(x, v, row, c);
+    }
 }
 
 /*
@@ -169,24 +212,41 @@ template <typename F>
 __device__ __forceinline__ void store_items(void *row, const Items<F> &f, const Columns<F> &c, const Lane<F> &l)
 {
     using T = typename F::T;
-    if (l.ragged) {
-#pragma unroll
-        for (int j = 0; j < F::items; ++j)
-            if (c.has(j)) static_cast<T *>(row)[c.at(j)] = narrow<F::DT>((j & 1) ? f.p[j / 2].y : f.p[j / 2].x);
-        return;
-    }
 #pragma unroll
     for (int v = 0; v < F::vectors; ++v) {
-        if (!l.in[v]) continue;
         constexpr int N = F::vector_pairs;                /* 4 of bf16, 2 of fp32 */
         const float2 *p = &f.p[v * N];
+        if (F::ACCESS == kElement || (l.ragged && c.at(v * c.EPV) + c.EPV > c.cols)) {
+#pragma unroll
+            for (int j = 2 * N * v; j < 2 * N * (v + 1); ++j)
+                if (c.has(j)) static_cast<T *>(row)[c.at(j)] = narrow<F::DT>((j & 1) ? f.p[j / 2].y : f.p[j / 2].x);
+            continue;
+        }
+        if (!l.in[v]) continue;
         uint4 q;
         if (F::DT == SIFAR_BF16)
             q = make_uint4(f32x2_to_bf16x2(p[0].x, p[0].y), f32x2_to_bf16x2(p[1].x, p[1].y), f32x2_to_bf16x2(p[2 % N].x, p[2 % N].y),
                            f32x2_to_bf16x2(p[3 % N].x, p[3 % N].y));
         else
             q = make_uint4(__float_as_uint(p[0].x), __float_as_uint(p[0].y), __float_as_uint(p[1].x), __float_as_uint(p[1].y));
-        *reinterpret_cast<uint4 *>(static_cast<char *>(row) + l.at[v]) = q;
+        char *const to = static_cast<char *>(row) + l.at[v];
+        const uint32_t m = F::ACCESS == kWhole ? 0u : (uint32_t)(uintptr_t)to & 15u;
+        if (m == 0u) {
+            *reinterpret_cast<uint4 *>(to) = q;
+        } else if ((m & 7u) == 0u) {
+            reinterpret_cast<uint2 *>(to)[0] = make_uint2(q.x, q.y);
+            reinterpret_cast<uint2 *>(to)[1] = make_uint2(q.z, q.w);
+        } else if ((m & 3u) == 0u) {
+            uint32_t *const w = reinterpret_cast<uint32_t *>(to);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else {                                          /* bf16 at an odd element: half a word, three words, half a word */
+            *reinterpret_cast<uint16_t *>(to) = (uint16_t)q.x;
+            uint32_t *const w = reinterpret_cast<uint32_t *>(to + 2);
+            w[0] = __funnelshift_r(q.x, q.y, 16);
+            w[1] = __funnelshift_r(q.y, q.z, 16);
+            w[2] = __funnelshift_r(q.z, q.w, 16);
+            *reinterpret_cast<uint16_t *>(to + 14) = (uint16_t)(q.w >> 16);
+        }
     }
 }
 
@@ -352,7 +412,7 @@ __device__ __forceinline__ float rrms(float sum, uint32_t cols, float eps) { ret
  * threads' words side by side, 16 bytes each (VEC) or 4.
  */
 template <typename F> struct Ring {
-    static constexpr bool possible = F::VEC || F::DT == SIFAR_F32;         /* a copy moves 4 bytes at least */
+    static constexpr bool possible = F::ACCESS == kWhole || (F::ACCESS == kElement && F::DT == SIFAR_F32);   /* of 16 or 4 bytes */
     static constexpr uint32_t bytes = sizeof(Raw<F>);                   /* per thread and array */
     static constexpr uint32_t unit = F::VEC ? 16 : 4;
     static constexpr int N = bytes / unit;
@@ -393,7 +453,7 @@ template <typename F> struct Ring {
     }
     /* words 4 v to 4 v + 3 of the thread.  Plain loads: the compiler puts those of a row side by side, but not before the
        wait or behind the fetch that comes after them */
-    __device__ __forceinline__ void read_half(Raw<F> &x, int v, const unsigned char *smem, uint32_t at) const
+    __device__ __forceinline__ void read_vector(Raw<F> &x, int v, const unsigned char *smem, uint32_t at) const
     {
         const unsigned char *p = smem + at + (threadIdx.y * blockDim.x + threadIdx.x) * unit;
         if (F::VEC) {

@@ -23,7 +23,7 @@ struct NormGradArgs {
     uint32_t ld_dy, ld_dh, ld_h, ld_z, ld_gate, ld_dx, ld_dresidual;         /* bytes between two rows */
     float alpha, beta, offset;
     uint32_t rows, cols, pitch, blocks, rows_per_gate, parts, stages;
-    int P, post, pre;
+    int P, post, pre, narrow;                /* narrow: rows so short that a vector may reach over the one beside it */
 };
 
 /* Rows of block b: [block_start(b), block_start(b + 1)). */
@@ -161,51 +161,73 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
             if (POST) next1 = a.stats[row + 1];
             if (PRE) next2 = a.stats[a.rows + row + 1];
         }
+        const bool edge = row == 0 || row + 1 == a.rows || a.narrow;
         if (Ring<F>::possible) ring.wait(a.stages - 1);
         float2 q2 = both(0.0f), qt = q2, qn = q2;         /* sums of a * n2, f * z * t, f * z * n2 */
+        const auto pass = [&](bool each) {
 #pragma unroll
-        for (int v = 0; v < F::vectors; ++v) {            /* 16 bytes after 16 bytes: fewer registers */
-            constexpr int N = F::vector_pairs;
-            Raw<F> x;
-            float2 G[N];                                  /* the gradient of the normed h */
-            uint32_t from = place;
-            auto get = [&](Raw<F> &y, const void *base, uint32_t ld) {
-                if (Ring<F>::possible) { ring.read_half(y, v, ring_bytes, from); from += pitch; }
-                else load_half(y, v, static_cast<const char *>(base) + at * ld, c);
+            for (int v = 0; v < F::vectors; ++v) {            /* 16 bytes after 16 bytes: fewer registers */
+                constexpr int N = F::vector_pairs;
+                Raw<F> x, xd;
+                float2 G[N];                                  /* the gradient of the normed h */
+                const float2 before[3] = {q2, qt, qn};
+                /* array k of the row in fetch's order */
+                const auto get = [&](Raw<F> &y, int k, const void *base, uint32_t ld) {
+                    if (Ring<F>::possible) ring.read_vector(y, v, ring_bytes, place + (uint32_t)k * pitch);
+                    else load_vector(y, v, static_cast<const char *>(base) + at * ld, c, l, each);
+                };
+                int k = partials;
+                if (PRE) get(o.h, k++, a.h, a.ld_h);
+                if (a.dh) get(xd, k++, a.dh, a.ld_dh);
+                if (with_z) get(o.z, k, a.z, a.ld_z);
+                if (PRE) {
+                    get(x, 0, a.dy[0], a.ld_dy);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) G[j] = pair<F>(x, v * N + j);
+#pragma unroll 4
+                    for (int r = 1; r < partials; ++r) {
+                        get(x, r, a.dy[r], a.ld_dy);
+#pragma unroll
+                        for (int j = 0; j < N; ++j) add_pair<F>(G[j], x, v * N + j);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) o.D.p[v * N + j] = a.dh ? pair<F>(xd, v * N + j) : both(0.0f);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const int i = v * N + j;
+                    float2 n2;
+                    if (PRE) {
+                        n2 = __fmul2_rn(pair<F>(o.h, i), both(o.r2));
+                        pre.p[i] = __ffma2_rn(G[j], n2, pre.p[i]);
+                        G[j] = __fmul2_rn(G[j], w2.p[i]);
+                        q2 = __ffma2_rn(G[j], n2, q2);
+                        o.D.p[i] = __ffma2_rn(both(o.r2), G[j], o.D.p[i]);
+                    }
+                    if (POST) {
+                        const float2 fz = __fmul2_rn(f.p[i], pair<F>(o.z, i));
+                        qt = __ffma2_rn(fz, o.D.p[i], qt);
+                        if (PRE) qn = __ffma2_rn(fz, n2, qn);
+                    }
+                }
+                if (!Ring<F>::possible && F::VEC && !l.in[v]) q2 = before[0], qt = before[1], qn = before[2];
+            }
+        };
+        if (!Ring<F>::possible && by_element(l, edge)) pass(true);
+        else pass(false);
+        if (!Ring<F>::possible && row + 2 < end && (p.t & 7u) == 0) {           /* a line of the row after next, into the L2 */
+            const unsigned long long next = at + 2;
+            const auto ahead = [&](const void *base, uint32_t ld) {
+#pragma unroll
+                for (int v = 0; v < F::vectors; ++v)
+                    if (l.in[v]) asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const char *>(base) + next * ld + l.at[v]));
             };
             if (PRE) {
-                get(x, a.dy[0], a.ld_dy);
-#pragma unroll
-                for (int j = 0; j < N; ++j) G[j] = pair<F>(x, v * N + j);
-#pragma unroll 4
-                for (int r = 1; r < partials; ++r) {
-                    get(x, a.dy[r], a.ld_dy);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) add_pair<F>(G[j], x, v * N + j);
-                }
-                get(o.h, a.h, a.ld_h);
+                for (int r = 0; r < partials; ++r) ahead(a.dy[r], a.ld_dy);
+                ahead(a.h, a.ld_h);
             }
-            if (a.dh) get(x, a.dh, a.ld_dh);
-#pragma unroll
-            for (int j = 0; j < N; ++j) o.D.p[v * N + j] = a.dh ? pair<F>(x, v * N + j) : both(0.0f);
-            if (with_z) get(o.z, a.z, a.ld_z);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int i = v * N + j;
-                float2 n2;
-                if (PRE) {
-                    n2 = __fmul2_rn(pair<F>(o.h, i), both(o.r2));
-                    pre.p[i] = __ffma2_rn(G[j], n2, pre.p[i]);
-                    G[j] = __fmul2_rn(G[j], w2.p[i]);
-                    q2 = __ffma2_rn(G[j], n2, q2);
-                    o.D.p[i] = __ffma2_rn(both(o.r2), G[j], o.D.p[i]);
-                }
-                if (POST) {
-                    const float2 fz = __fmul2_rn(f.p[i], pair<F>(o.z, i));
-                    qt = __ffma2_rn(fz, o.D.p[i], qt);
-                    if (PRE) qn = __ffma2_rn(fz, n2, qn);
-                }
-            }
+            if (a.dh) ahead(a.dh, a.ld_dh);
+            if (with_z) ahead(a.z, a.ld_z);
         }
         if (Ring<F>::possible) {
             fetch(place, row + a.stages);                 /* the thread has read its places */
@@ -424,10 +446,10 @@ static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStrea
     return launch_op(kernel, grid, block, sh.row.parts, smem, stream, a);
 }
 
-template <int DT, bool VEC, bool POST, bool PRE>
+template <int DT, Access A, bool POST, bool PRE>
 static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
-    using F = Form<DT, kGradWords<DT>, VEC>;
+    using F = Form<DT, kGradWords<DT>, A>;
     /* bf16 in clusters: a row ahead (2000 x 8200: 162 -> 124 us).  Without a cluster the barrier costs less than what the
        second row takes (8192 x 4096: 107 -> 115 us), fp32 has no registers for it (1003 x 4099: 50 -> 56 us). */
     if constexpr (DT == SIFAR_BF16)
@@ -435,11 +457,11 @@ static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStrea
     return launch_grad_k<F, POST, PRE, false>(sh, arrays, stream, a);
 }
 
-template <int DT, bool VEC>
+template <int DT, Access A>
 static cudaError_t launch_grad(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
-    if (a.post) return a.pre ? launch_grad_n<DT, VEC, true, true>(sh, arrays, stream, a) : launch_grad_n<DT, VEC, true, false>(sh, arrays, stream, a);
-    return a.pre ? launch_grad_n<DT, VEC, false, true>(sh, arrays, stream, a) : launch_grad_n<DT, VEC, false, false>(sh, arrays, stream, a);
+    if (a.post) return a.pre ? launch_grad_n<DT, A, true, true>(sh, arrays, stream, a) : launch_grad_n<DT, A, true, false>(sh, arrays, stream, a);
+    return a.pre ? launch_grad_n<DT, A, false, true>(sh, arrays, stream, a) : launch_grad_n<DT, A, false, false>(sh, arrays, stream, a);
 }
 
 /* Words between two blocks' sums. */
@@ -542,6 +564,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     const auto bytes = [&](size_t ld) { return (uint32_t)(or_cols(ld, cols) * es); };
     a.ld_dy = bytes(g->ld_dy); a.ld_dh = bytes(g->ld_dh); a.ld_h = bytes(g->ld_h); a.ld_z = bytes(g->ld_z);
     a.ld_gate = bytes(g->ld_gate); a.ld_dx = bytes(g->ld_dx); a.ld_dresidual = bytes(g->ld_dresidual);
+    a.narrow = a.ld_dy < 32 || a.ld_dh < 32 || a.ld_h < 32 || a.ld_z < 32;
     a.alpha = g->alpha; a.beta = g->beta; a.offset = g->weight_offset;
     a.rows = (uint32_t)rows; a.cols = (uint32_t)cols; a.pitch = (uint32_t)sum_pitch(cols); a.blocks = sh.blocks;
     a.rows_per_gate = (uint32_t)span; a.parts = sh.row.parts;
@@ -550,8 +573,8 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         const unsigned arrays = (pre ? (unsigned)g->P + 1u : 0u) + (g->dh ? 1u : 0u) + (need_z ? 1u : 0u);
         const cudaStream_t q = (cudaStream_t)stream;
         const cudaError_t err = g->dtype == SIFAR_BF16
-            ? (vec ? launch_grad<SIFAR_BF16, true>(sh, arrays, q, a) : launch_grad<SIFAR_BF16, false>(sh, arrays, q, a))
-            : (vec ? launch_grad<SIFAR_F32, true>(sh, arrays, q, a) : launch_grad<SIFAR_F32, false>(sh, arrays, q, a));
+            ? (vec ? launch_grad<SIFAR_BF16, kWhole>(sh, arrays, q, a) : launch_grad<SIFAR_BF16, kShifted>(sh, arrays, q, a))
+            : (vec ? launch_grad<SIFAR_F32, kWhole>(sh, arrays, q, a) : launch_grad<SIFAR_F32, kElement>(sh, arrays, q, a));
         SIFAR_CUDA(err);
     }
     if (g->dpost_weight || g->dpre_weight || g->dgate) {

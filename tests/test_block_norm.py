@@ -231,6 +231,10 @@ SHAPES = [
     (1, 4096, 8, 0, 0), (2, 4095, 8, 1, 0), (2, 4096, 3, 8, 0), (3, 4097, 2, 0, 0), (1, 4104, 8, 24, 0), (2, 8192, 4, 0, 0),
     (2, 8191, 1, 0, 0), (1, 20001, 2, 0, 0), (1, 32768, 6, 0, 0), (2, 32767, 1, 9, 0), (4, 512, 8, 0, 3), (4, 100, 7, 4, 8),
     (700, 64, 1, 0, 0), (1300, 130, 2, 2, 0), (601, 300, 1, 0, 0), (2500, 33, 1, 0, 1),
+    # more rows than SMs: 64 bytes of an array per thread
+    (149, 5000, 2, 0, 0), (150, 4609, 1, 7, 0), (152, 8192, 4, 0, 0), (149, 10000, 3, 0, 0), (150, 16384, 1, 8, 0), (151, 16383, 2, 0, 0),
+    # rows that start at every place of a 16-byte vector, on either side of the shortest that vectors may reach over
+    (9, 24, 2, 1, 1), (17, 15, 3, 0, 0), (17, 16, 1, 1, 0), (19, 8, 2, 9, 5), (40, 4097, 3, 0, 0), (33, 1023, 8, 0, 7), (21, 130, 2, 4, 2), (12, 7, 4, 1, 0),
 ]
 
 
@@ -375,6 +379,8 @@ BACK = [
     (2, 4096, 8, 0, 0, "none", 0), (3, 4095, 3, 1, 0, "channel", 0), (2, 4097, 2, 0, 0, "group", 1), (2, 8192, 4, 8, 0, "channel", 0),
     (40, 20001, 1, 0, 0, "group", 7), (19, 32768, 2, 0, 0, "group", 3), (4, 512, 8, 0, 3, "group", 4), (149, 100, 1, 4, 8, "channel", 0),
     (1500, 64, 1, 0, 0, "group", 37), (2600, 33, 2, 0, 1, "group", 1), (3000, 130, 1, 2, 0, "group", 999), (601, 300, 5, 0, 0, "channel", 0),
+    (9, 24, 2, 1, 1, "channel", 0), (17, 15, 3, 0, 0, "group", 5), (17, 16, 1, 1, 0, "none", 0), (19, 8, 2, 9, 5, "channel", 0),
+    (40, 4097, 3, 0, 0, "group", 7), (33, 1023, 8, 0, 7, "channel", 0), (21, 130, 2, 4, 2, "none", 0), (200, 1001, 1, 0, 0, "group", 50),
     (296, 1024, 2, 0, 0, "group", 2), (297, 1032, 1, 8, 0, "group", 5), (500, 4096, 1, 0, 0, "group", 250),
 ]
 
