@@ -52,7 +52,8 @@
  *                           resident while the kernel before it on its stream drains: a reducer with more CTAs than
  *                           the GPU has SMs, one whose producers were all enqueued on other streams or all on its
  *                           own (sifar_pack, sifar_arrive), the sweep kernel, a pack of at most one CTA per SM,
- *                           sifar_arrive, sifar_wait_writable and sifar_allreduce_noalloc.  In the two barrier-free
+ *                           sifar_arrive, sifar_wait_writable, sifar_allreduce_noalloc and the operators behind an
+ *                           all-reduce (sifar_block_norm, sifar_route and their backward passes).  In the two barrier-free
  *                           modes the loads of a reducer whose producers are on other streams then start at once
  *                           (they are ordered by flags or tags, not by the stream); everything else that such a
  *                           kernel reads or writes waits until the kernel before it is complete.
@@ -387,10 +388,10 @@ int sifar_noalloc_counters(unsigned long long out[3]);
  *
  * Common rules.
  *   - One argument block per call, read before the call returns (a program may keep one per layer and pass it again).
- *     Unused pointers are NULL.  Everything is launched on the CURRENT device and on `stream`; nothing synchronizes.
- *   - `rows` x `cols` arrays have a row stride ld_* in elements, at least cols; 0 stands for cols.  Addresses need the
- *     alignment of their element type.  Where the bases and strides of all row arrays are multiples of 16 bytes the
- *     kernels move 16 bytes per access, otherwise single elements.
+ *     Unused pointers and sizes are 0.  Everything is launched on the CURRENT device and on `stream`; nothing synchronizes.
+ *   - `rows` x `cols` arrays have a row stride ld_* in elements, at least cols and below 2^30; 0 stands for cols.
+ *     Addresses need the alignment of their element type.   Everything works at any address and stride; it is fastest where all rows start on
+ *     16-byte boundaries.
  *   - An output may overlap nothing else, except as stated.  Arrays that share a buffer column by column (same stride,
  *     disjoint columns) do not overlap.
  *   - SIFAR_ERR_INVALID: nothing was launched.  rows = 0 (tokens = 0) is valid: no row is read or written; gradients

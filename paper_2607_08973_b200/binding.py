@@ -63,11 +63,11 @@ def lib() -> ctypes.CDLL:
             "sifar_allreduce_noalloc": (ci, [vp, ci, vp, sz, ci, vp]),
             "sifar_noalloc_max_elems": (sz, []),
             "sifar_noalloc_counters": (ci, [ctypes.POINTER(ctypes.c_ulonglong)]),
-            "sifar_block_norm": (ci, [vp, vp]),
-            "sifar_block_norm_backward": (ci, [vp, vp]),
-            "sifar_block_norm_backward_workspace": (sz, [vp]),
-            "sifar_route": (ci, [vp, vp]),
-            "sifar_route_backward": (ci, [vp, vp]),
+            "sifar_block_norm": (ci, [ctypes.POINTER(sifar_block_norm_args), vp]),
+            "sifar_block_norm_backward": (ci, [ctypes.POINTER(sifar_block_norm_grad_args), vp]),
+            "sifar_block_norm_backward_workspace": (sz, [ctypes.POINTER(sifar_block_norm_grad_args)]),
+            "sifar_route": (ci, [ctypes.POINTER(sifar_route_args), vp]),
+            "sifar_route_backward": (ci, [ctypes.POINTER(sifar_route_grad_args), vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -242,6 +242,7 @@ def _ranks(ptrs) -> ctypes.Array:
     return (ctypes.c_void_p * MAX_RANKS)(*ptrs)
 
 
+# The argument blocks keep addresses, not tensors: whoever fills one keeps its tensors alive.
 def make_block_norm(x, *, rows: int, cols: int, dtype: int, alpha: float = 1.0, beta: float = 1.0, eps: float = 1e-6,
                     **fields) -> sifar_block_norm_args:
     """Argument block of sifar_block_norm: `x` the P partials' addresses, `fields` as in the header, absent ones 0."""
@@ -271,23 +272,23 @@ def make_route_grad(logits, *, tokens: int, experts: int, top_k: int, dtype: int
 
 
 def sifar_block_norm(args: sifar_block_norm_args, stream: int = 0) -> int:
-    return _check(lib().sifar_block_norm(ctypes.byref(args), stream))
+    return _check(lib().sifar_block_norm(args, stream))
 
 
 def sifar_block_norm_backward(args: sifar_block_norm_grad_args, stream: int = 0) -> int:
-    return _check(lib().sifar_block_norm_backward(ctypes.byref(args), stream))
+    return _check(lib().sifar_block_norm_backward(args, stream))
 
 
 def sifar_block_norm_backward_workspace(args: sifar_block_norm_grad_args) -> int:
-    return lib().sifar_block_norm_backward_workspace(ctypes.byref(args))
+    return lib().sifar_block_norm_backward_workspace(args)
 
 
 def sifar_route(args: sifar_route_args, stream: int = 0) -> int:
-    return _check(lib().sifar_route(ctypes.byref(args), stream))
+    return _check(lib().sifar_route(args, stream))
 
 
 def sifar_route_backward(args: sifar_route_grad_args, stream: int = 0) -> int:
-    return _check(lib().sifar_route_backward(ctypes.byref(args), stream))
+    return _check(lib().sifar_route_backward(args, stream))
 
 
 # ---------------------------------------------------------------------------

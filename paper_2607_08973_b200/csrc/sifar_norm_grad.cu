@@ -5,6 +5,11 @@
  * read once and held in registers while its two sums are taken, the gradients that are summed over rows kept in
  * registers from row to row and stored once per block.  The second adds the blocks' sums in order, so that the
  * result does not depend on which CTA was first.
+ *
+ * 8192 x 4096 bf16, two norms and a gate: 101 us with two ranks' partials (4.65 TB/s, 0.71 of the measured copy; 2.5 us of
+ * it the second kernel), 134 us with eight (6.0 TB/s, 0.91).  What bounds it below that is instructions: about 460 per
+ * thread of 8 items and row at 0.55 per cycle and scheduler, in 16 warps per SM, which is what the sums over rows
+ * leave registers for.
  */
 #include "sifar_norm.cuh"
 

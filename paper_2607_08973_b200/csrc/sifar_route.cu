@@ -287,12 +287,17 @@ __device__ __noinline__ int order_exactly(const RouteArgs &a, const float *l, in
  * them and the best that is left, lie closer than the error of both and are not equal by their inputs, rounds go on
  * until the rest is far enough, and the candidates, one per lane, are put in order by their values in binary64.
  * Logits that are compared themselves have no error but the cut bits.  The groups are looked at in the same way.
+ * (All values in binary64 and lists searched anew for every choice: 57 us for 8192 tokens, 8 of 256 experts in 8 groups
+ * with a bias; so 10.4 us.)
+ *
+ * Bound by instructions, 890 per token of that shape (250 of them the groups', 21 a choice), issued in 63 % of the
+ * cycles with 27 warps per SM; the logits are there in a tenth of the time.  One token takes a launch, 2.7 to 3 us.
  */
 template <int DT, int NI, bool BIAS, bool GROUPS>
 __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 : 3) k_route(const __grid_constant__ RouteArgs a)
 {
     __shared__ float s_l[kRouteWarps][NI * 32];
-    __shared__ double s_v[kRouteWarps][NI * 32];
+    __shared__ __align__(16) double s_v[kRouteWarps][NI * 32];
     constexpr uint32_t kCut = NI - 1;
     grid_let_next_in();
     const int lane = threadIdx.x & 31;
