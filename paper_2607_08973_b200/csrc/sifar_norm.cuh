@@ -104,14 +104,9 @@ __device__ __forceinline__ void load_whole(Raw<F> &x, int v, const void *row, co
     x.w[4 * v + 3] = q.w;
 }
 
-/* A vector that starts anywhere, from the two aligned ones around it: their eight words moved down by the bytes between. */
-template <typename F>
-__device__ __forceinline__ void load_shifted(Raw<F> &x, int v, const void *row, const Lane<F> &l)
+/* Vector v that starts m bytes into two aligned ones: their eight words moved down. */
+template <typename F> __device__ __forceinline__ void shift_vectors(Raw<F> &x, int v, const uint4 &a, const uint4 &b, uint32_t m)
 {
-    const uintptr_t p = (uintptr_t)row + l.at[v];
-    const uint32_t m = (uint32_t)p & 15u;
-    const uint4 *g = reinterpret_cast<const uint4 *>(p - m);
-    const uint4 a = g[0], b = g[m ? 1 : 0];
     uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int i = 0; i < 6; ++i) w[i] = m & 8u ? w[i + 2] : w[i];
@@ -120,9 +115,18 @@ __device__ __forceinline__ void load_shifted(Raw<F> &x, int v, const void *row, 
 #pragma unroll
     for (int i = 0; i < 4; ++i) x.w[4 * v + i] = F::DT == SIFAR_F32 ? w[i] : __funnelshift_r(w[i], w[i + 1], (m & 2u) * 8u);
 }
+template <typename F>
+__device__ __forceinline__ void load_shifted(Raw<F> &x, int v, const void *row, const Lane<F> &l)
+{
+    const uintptr_t p = (uintptr_t)row + l.at[v];
+    const uint32_t m = (uint32_t)p & 15u;
+    const uint4 *g = reinterpret_cast<const uint4 *>(p - m);
+    shift_vectors(x, v, g[0], g[m ? 1 : 0], m);
+}
 
-/* Whether the warp looks at every element of the row: at its ragged end, and in the array's first and last row
-   (`edge`) where a shifted vector might reach out of the array.  The caller branches on it once and passes the constant. */
+/* Whether the warp looks at every element of the row: at its ragged end (vectors of which the items behind it are cut
+   off again were slower: 33 us against 28 for 1003 x 4099 fp32), and in the array's first and last row (`edge`) where a
+   shifted vector might reach out of the array.  The caller branches on it once and passes the constant. */
 template <typename F> __device__ __forceinline__ bool by_element(const Lane<F> &l, bool edge)
 {
     return F::ACCESS == kElement || l.ragged || (F::ACCESS == kShifted && edge);
@@ -412,22 +416,31 @@ __device__ __forceinline__ float rrms(float sum, uint32_t cols, float eps) { ret
  * threads' words side by side, 16 bytes each (VEC) or 4.
  */
 template <typename F> struct Ring {
-    static constexpr bool possible = F::ACCESS == kWhole || (F::ACCESS == kElement && F::DT == SIFAR_F32);   /* of 16 or 4 bytes */
-    static constexpr uint32_t bytes = sizeof(Raw<F>);                   /* per thread and array */
+    static constexpr bool possible = F::ACCESS != kElement || F::DT == SIFAR_F32;    /* a copy moves 4 bytes at least */
+    static constexpr bool shifted = F::ACCESS == kShifted;
     static constexpr uint32_t unit = F::VEC ? 16 : 4;
-    static constexpr int N = bytes / unit;
+    static constexpr int copies = shifted ? 2 : 1;                   /* of a vector: the two aligned ones around it */
+    static constexpr uint32_t bytes = sizeof(Raw<F>) * copies;       /* per thread and array */
+    static constexpr int N = sizeof(Raw<F>) / unit;
     uint32_t first, threads;                                         /* the thread's place in slot 0; of the CTA */
-    uint32_t from[N], n[N];                                          /* of each copy: bytes into the row, bytes to move (the rest becomes 0) */
+    uint32_t from[N], n[N];                                          /* of each unit: bytes into the row, bytes to move (the rest becomes 0) */
+    uint32_t row_bytes;
     __device__ __forceinline__ Ring(const void *smem, const Columns<F> &c)
     {
-                threads = blockDim.x * blockDim.y;
+        threads = blockDim.x * blockDim.y;
         first = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.y * blockDim.x + threadIdx.x) * unit;
+        row_bytes = c.cols * F::es;
 #pragma unroll
         for (int v = 0; v < N; ++v) {
             const uint32_t i = c.at(v * c.EPV);
             n[v] = i < c.cols ? min((uint32_t)c.EPV, c.cols - i) * F::es : 0u;
             from[v] = n[v] ? i * F::es : 0u;
         }
+    }
+    __device__ __forceinline__ void copy(uint32_t to, const char *p, uint32_t bytes_) const
+    {
+        if (F::VEC) asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(p), "r"(bytes_) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(to), "l"(p), "r"(bytes_) : "memory");
     }
     /* a row of an array to place `at` (bytes; a place takes threads * bytes) */
     __device__ __forceinline__ void fetch(uint32_t at, const void *row) const
@@ -436,10 +449,17 @@ template <typename F> struct Ring {
 #pragma unroll
         for (int v = 0; v < N; ++v) {
             const char *p = static_cast<const char *>(row) + from[v];
-            if (F::VEC)
+            if (shifted) {
+                /* up to the row's end: what follows becomes 0.  The bytes before the row in its first vector are the row
+                   before's and are moved out */
+                const uint32_t m = (uint32_t)(uintptr_t)p & 15u, end = n[v] ? row_bytes - from[v] + m : 0u;
+                copy(to + 2 * v * threads * unit, p - m, min(16u, end));
+                copy(to + (2 * v + 1) * threads * unit, end > 16u ? p - m + 16 : p - m, m && end > 16u ? min(16u, end - 16u) : 0u);
+            } else if (F::VEC) {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to + v * threads * unit), "l"(p), "r"(n[v]) : "memory");
-            else
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(to + v * threads * unit), "l"(p), "r"(n[v]) : "memory");
+            } else {
+                copy(to + v * threads * unit, p, n[v]);
+            }
         }
     }
     __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -451,12 +471,15 @@ template <typename F> struct Ring {
         else if (k == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
         else asm volatile("cp.async.wait_group 3;" ::: "memory");
     }
-    /* words 4 v to 4 v + 3 of the thread.  Plain loads: the compiler puts those of a row side by side, but not before the
-       wait or behind the fetch that comes after them */
-    __device__ __forceinline__ void read_vector(Raw<F> &x, int v, const unsigned char *smem, uint32_t at) const
+    /* words 4 v to 4 v + 3 of the thread; `row`: where the array's row starts.  Plain loads: the compiler puts those of a
+       row side by side, but not before the wait or behind the fetch that comes after them */
+    __device__ __forceinline__ void read_vector(Raw<F> &x, int v, const unsigned char *smem, uint32_t at, const void *row) const
     {
         const unsigned char *p = smem + at + (threadIdx.y * blockDim.x + threadIdx.x) * unit;
-        if (F::VEC) {
+        if (shifted) {
+            shift_vectors(x, v, *reinterpret_cast<const uint4 *>(p + 2 * v * threads * unit),
+                          *reinterpret_cast<const uint4 *>(p + (2 * v + 1) * threads * unit), (uint32_t)(uintptr_t)row & 15u);
+        } else if (F::VEC) {
             const uint4 q = *reinterpret_cast<const uint4 *>(p + v * threads * unit);
             x.w[4 * v] = q.x;
             x.w[4 * v + 1] = q.y;

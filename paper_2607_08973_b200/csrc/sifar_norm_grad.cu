@@ -28,7 +28,9 @@ struct NormGradArgs {
     uint32_t ld_dy, ld_dh, ld_h, ld_z, ld_gate, ld_dx, ld_dresidual;         /* bytes between two rows */
     float alpha, beta, offset;
     uint32_t rows, cols, pitch, blocks, rows_per_gate, parts, stages;
-    int P, post, pre, narrow;                /* narrow: rows so short that a vector may reach over the one beside it */
+    int P, post, pre;
+    int narrow, odd_start;                   /* rows so short that a vector may reach over the one beside it; an array that does
+                                                not start on 16 bytes */
 };
 
 /* Rows of block b: [block_start(b), block_start(b + 1)). */
@@ -110,6 +112,9 @@ template <typename F, bool POST, bool PRE, bool AHEAD>
 __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
     constexpr int kSums = POST && PRE ? 3 : 1;
+    /* shifted rows: copied ahead in clusters (4096 x 4097, four ranks: 227 -> 185 us), read from memory, their lines asked
+       for two rows before, where a CTA holds them (16384 x 515: 73 us against 86 with copies) */
+    constexpr bool kRing = F::ACCESS == kShifted ? AHEAD : Ring<F>::possible;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
     __shared__ __align__(16) RowSum<kSums> s;
     grid_let_next_in();
@@ -130,9 +135,13 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
     const uint32_t stage_bytes = pitch * ((uint32_t)partials + (PRE ? 1u : 0u) + (a.dh ? 1u : 0u) + (with_z ? 1u : 0u));
     grid_wait();
 
+    /* rows that are read by elements when their turn comes: where a copy might reach over the array's start */
+    const auto direct = [&](uint32_t row) {
+        return Ring<F>::shifted && (a.narrow || (row == 0 && a.odd_start));
+    };
     /* row `row` to place `to` of the ring: the partials, then h, dh, z */
     auto fetch = [&](uint32_t to, uint32_t row) {
-        if (row < end) {
+        if (row < end && !direct(row)) {
             const unsigned long long at = row;
             if (PRE) {
                 const unsigned long long o = at * a.ld_dy;
@@ -145,7 +154,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
         }
         ring.commit();
     };
-    if (Ring<F>::possible)
+    if (kRing)
         for (uint32_t i = 0; i < a.stages; ++i) fetch(i * stage_bytes, first + i);
 
     const Items<F> w2 = load_factor(a.pre_weight, a.offset, c, l);
@@ -166,8 +175,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
             if (POST) next1 = a.stats[row + 1];
             if (PRE) next2 = a.stats[a.rows + row + 1];
         }
-        const bool edge = row == 0 || row + 1 == a.rows || a.narrow;
-        if (Ring<F>::possible) ring.wait(a.stages - 1);
+        if (kRing) ring.wait(a.stages - 1);
         float2 q2 = both(0.0f), qt = q2, qn = q2;         /* sums of a * n2, f * z * t, f * z * n2 */
         const auto pass = [&](bool each) {
 #pragma unroll
@@ -178,8 +186,9 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
                 const float2 before[3] = {q2, qt, qn};
                 /* array k of the row in fetch's order */
                 const auto get = [&](Raw<F> &y, int k, const void *base, uint32_t ld) {
-                    if (Ring<F>::possible) ring.read_vector(y, v, ring_bytes, place + (uint32_t)k * pitch);
-                    else load_vector(y, v, static_cast<const char *>(base) + at * ld, c, l, each);
+                    const char *row_k = static_cast<const char *>(base) + at * ld;
+                    if (kRing && !each) ring.read_vector(y, v, ring_bytes, place + (uint32_t)k * pitch, row_k);
+                    else load_vector(y, v, row_k, c, l, each);
                 };
                 int k = partials;
                 if (PRE) get(o.h, k++, a.h, a.ld_h);
@@ -215,17 +224,16 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
                         if (PRE) qn = __ffma2_rn(fz, n2, qn);
                     }
                 }
-                if (!Ring<F>::possible && F::VEC && !l.in[v]) q2 = before[0], qt = before[1], qn = before[2];
+                if (!kRing && F::VEC && !l.in[v]) { q2 = before[0]; qt = before[1]; qn = before[2]; }    /* nothing is 0 there */
             }
         };
-        if (!Ring<F>::possible && by_element(l, edge)) pass(true);
+        if (kRing ? direct(row) : by_element(l, row == 0 || row + 1 == a.rows || a.narrow)) pass(true);
         else pass(false);
-        if (!Ring<F>::possible && row + 2 < end && (p.t & 7u) == 0) {           /* a line of the row after next, into the L2 */
-            const unsigned long long next = at + 2;
+        if (!kRing && row + 2 < end && (p.t & 7u) == 0) { /* a line of the row after next, into the L2 */
             const auto ahead = [&](const void *base, uint32_t ld) {
 #pragma unroll
                 for (int v = 0; v < F::vectors; ++v)
-                    if (l.in[v]) asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const char *>(base) + next * ld + l.at[v]));
+                    if (l.in[v]) asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const char *>(base) + (at + 2) * ld + l.at[v]));
             };
             if (PRE) {
                 for (int r = 0; r < partials; ++r) ahead(a.dy[r], a.ld_dy);
@@ -234,7 +242,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
             if (a.dh) ahead(a.dh, a.ld_dh);
             if (with_z) ahead(a.z, a.ld_z);
         }
-        if (Ring<F>::possible) {
+        if (kRing) {
             fetch(place, row + a.stages);                 /* the thread has read its places */
             place = place + stage_bytes == places ? 0u : place + stage_bytes;
         }
@@ -317,7 +325,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
             if (p.tx > 32) __syncthreads();
         }
     }
-    if (Ring<F>::possible) ring.wait(0);
+    if (kRing) ring.wait(0);
     if (!live) return;
     end_of_gate(a, c, l, acc, b, first, segment, end);
     if (a.sum_pre) store_f32(a.sum_pre + (size_t)b * a.pitch, pre, c);
@@ -431,7 +439,7 @@ static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStrea
     static std::atomic<unsigned long long> ready{0};
     const auto kernel = k_block_norm_grad<F, POST, PRE, AHEAD>;
     size_t stages = 1, smem = 0;
-    if (Ring<F>::possible) {
+    if (F::ACCESS == kShifted ? AHEAD : Ring<F>::possible) {
         const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes, turns = (a.rows + sh.blocks - 1) / sh.blocks;
         stages = kRingBytes / sh.per_sm / row;
         if (stages > kMaxStages) stages = kMaxStages;
@@ -543,8 +551,12 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     if (pre) all[n++] = RowArray{"h", g->h, rows, cols, or_cols(g->ld_h, cols), es, false};
     if (need_z) all[n++] = RowArray{"z", g->z, rows, cols, or_cols(g->ld_z, cols), es, false};
     all[n++] = RowArray{"dx", g->dx, rows, cols, or_cols(g->ld_dx, cols), es, true};
-    bool vec = rows_aligned16(dh);
-    for (int i = 0; i < n; ++i) vec = vec && rows_aligned16(all[i]);
+    bool vec = rows_aligned16(dh), odd_start = false;
+    for (int i = 0; i < n; ++i) {
+        vec = vec && rows_aligned16(all[i]);
+        odd_start = odd_start || ((uintptr_t)all[i].p & 15u) != 0;
+    }
+    odd_start = odd_start || ((uintptr_t)dh.p & 15u) != 0;
     if (post) all[n++] = RowArray{"post_weight", g->post_weight, 1, cols, cols, es, false};
     if (pre) all[n++] = RowArray{"pre_weight", g->pre_weight, 1, cols, cols, es, false};
     all[n++] = RowArray{"gate", g->gate, gates, cols, or_cols(g->ld_gate, cols), es, false};
@@ -569,6 +581,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     const auto bytes = [&](size_t ld) { return (uint32_t)(or_cols(ld, cols) * es); };
     a.ld_dy = bytes(g->ld_dy); a.ld_dh = bytes(g->ld_dh); a.ld_h = bytes(g->ld_h); a.ld_z = bytes(g->ld_z);
     a.ld_gate = bytes(g->ld_gate); a.ld_dx = bytes(g->ld_dx); a.ld_dresidual = bytes(g->ld_dresidual);
+    a.odd_start = odd_start;
     a.narrow = a.ld_dy < 32 || a.ld_dh < 32 || a.ld_h < 32 || a.ld_z < 32;
     a.alpha = g->alpha; a.beta = g->beta; a.offset = g->weight_offset;
     a.rows = (uint32_t)rows; a.cols = (uint32_t)cols; a.pitch = (uint32_t)sum_pitch(cols); a.blocks = sh.blocks;

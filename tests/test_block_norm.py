@@ -235,6 +235,7 @@ SHAPES = [
     (149, 5000, 2, 0, 0), (150, 4609, 1, 7, 0), (152, 8192, 4, 0, 0), (149, 10000, 3, 0, 0), (150, 16384, 1, 8, 0), (151, 16383, 2, 0, 0),
     # rows that start at every place of a 16-byte vector, on either side of the shortest that vectors may reach over
     (9, 24, 2, 1, 1), (17, 15, 3, 0, 0), (17, 16, 1, 1, 0), (19, 8, 2, 9, 5), (40, 4097, 3, 0, 0), (33, 1023, 8, 0, 7), (21, 130, 2, 4, 2), (12, 7, 4, 1, 0),
+    (5, 9001, 2, 3, 5), (160, 9003, 2, 0, 1),
 ]
 
 
@@ -381,6 +382,7 @@ BACK = [
     (1500, 64, 1, 0, 0, "group", 37), (2600, 33, 2, 0, 1, "group", 1), (3000, 130, 1, 2, 0, "group", 999), (601, 300, 5, 0, 0, "channel", 0),
     (9, 24, 2, 1, 1, "channel", 0), (17, 15, 3, 0, 0, "group", 5), (17, 16, 1, 1, 0, "none", 0), (19, 8, 2, 9, 5, "channel", 0),
     (40, 4097, 3, 0, 0, "group", 7), (33, 1023, 8, 0, 7, "channel", 0), (21, 130, 2, 4, 2, "none", 0), (200, 1001, 1, 0, 0, "group", 50),
+    (5, 5001, 2, 3, 3, "group", 2), (90, 4097, 1, 0, 1, "channel", 0), (4, 12345, 8, 2, 0, "group", 3), (3, 8193, 2, 0, 6, "group", 100),
     (296, 1024, 2, 0, 0, "group", 2), (297, 1032, 1, 8, 0, "group", 5), (500, 4096, 1, 0, 0, "group", 250),
 ]
 
