@@ -39,7 +39,7 @@ template <int DT_, int W_, Access A_> struct Form {
     static_assert(SIFAR_NORM_MAX_COLS <= items * kMaxRowThreads * (int)kMaxNormCluster, "columns that a cluster holds");
 };
 
-/* The columns of a thread: item j is column at(j).  VEC: two runs of 16 bytes, else single elements. */
+/* The columns of a thread: item j is column at(j).  VEC: runs of 16 bytes, else single elements. */
 template <typename F> struct Columns {
     static constexpr int N = F::items;
     static constexpr int EPV = F::VEC ? Elem<F::DT>::per_vec : 1;      /* neighbours that are fetched together */
@@ -61,7 +61,7 @@ template <typename F> struct Lane {
     bool ragged;
     __device__ __forceinline__ explicit Lane(const Columns<F> &c)
     {
-                bool cut = !F::VEC;
+                bool cut = !F::VEC || c.cols == 0;                /* a row that is not there: nothing is read */
 #pragma unroll
         for (int v = 0; v < F::vectors; ++v) {
             const uint32_t i = c.at(v * c.EPV);

@@ -90,6 +90,10 @@ __device__ __forceinline__ void end_of_gate(const NormGradArgs &a, const Columns
     acc = all_items<F>(0.0f);
 }
 
+/* 16 bytes of an array per thread in bf16: with 32 the sums over rows spill (8192 x 4096, two ranks: 107 us against 134;
+   two CTAs per SM with 64 registers each: 163). */
+template <int DT> constexpr int kGradWords = DT == SIFAR_BF16 ? 4 : 8;
+
 /* What a row leaves between the pass that takes its sums and the one that uses them. */
 template <typename F, int N> struct Pending {
     Items<F> D;                              /* dh + r2 * a */
@@ -101,13 +105,9 @@ template <typename F, int N> struct Pending {
  * Both sums of a row in one pass.  With t = dh + r2 * a and f = beta * gate * (post_weight + offset) the second,
  * sum(f * n1 * D) with D = t - r2 * m2 * n2, is sum(f * n1 * t) - r2 * m2 * sum(f * n1 * n2), so that neither has to
  * wait for the other.
- * The pass over a row that takes its sums runs before the one that uses those of the row before it: what the sums need
- * to meet, a barrier, in a cluster a word from every CTA, passes while there is other work.
+ * AHEAD: the pass over a row that takes its sums runs before the one that uses those of the row before it: what the sums
+ * need to meet, a barrier and in a cluster a word from every CTA, passes while there is other work.
  */
-/* 16 bytes of an array per thread in bf16: with 32 the sums over rows spill (8192 x 4096, two ranks: 107 us against 134;
-   two CTAs per SM with 64 registers each: 163). */
-template <int DT> constexpr int kGradWords = DT == SIFAR_BF16 ? 4 : 8;
-
 template <typename F, bool POST, bool PRE, bool AHEAD>
 __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
@@ -334,11 +334,11 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
 struct NormSumArgs {
     const float *sum_post, *sum_pre, *sum_gate;
     float *dpost_weight, *dpre_weight, *dgate;
-    uint32_t rows, cols, pitch, blocks, rows_per_gate, gates, gate_jobs, gate_warps;
+    uint32_t rows, cols, pitch, blocks, rows_per_gate, gates, gate_jobs, gate_warps, first_job;
 };
 
 /*
- * 32 columns per CTA, its warps over the blocks: blockIdx.y = 0 the post weight, 1 the pre weight, from 2 on the gate
+ * 32 columns per CTA, its warps over the blocks: part 0 is the post weight, 1 the pre weight, from 2 on the gate
  * rows that lie in more than one block, `gate_warps` warps each.  A gate row has a few blocks, a weight all of them:
  * with all warps on one gate row at a time 17 gate rows of 1003 x 4099 took 11 us.
  */
@@ -348,18 +348,19 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid
     grid_let_next_in();
     grid_wait();
     const uint32_t col = blockIdx.x * 32 + threadIdx.x, warp = threadIdx.y;
-    const uint32_t team = blockIdx.y < 2 ? kSumWarps : a.gate_warps, member = warp % team;
+    const uint32_t part = blockIdx.y + a.first_job;
+    const uint32_t team = part < 2 ? kSumWarps : a.gate_warps, member = warp % team;
     const float *p = nullptr;                             /* of the member's blocks; the first one may lie elsewhere */
     float *out = nullptr;
     size_t step = a.pitch;
     uint32_t n = 0;
     float v = 0.0f;
-    if (blockIdx.y < 2) {
-        p = blockIdx.y == 0 ? a.sum_post : a.sum_pre;
-        out = blockIdx.y == 0 ? a.dpost_weight : a.dpre_weight;
+    if (part < 2) {
+        p = part == 0 ? a.sum_post : a.sum_pre;
+        out = part == 0 ? a.dpost_weight : a.dpre_weight;
         n = out ? a.blocks : 0u;
     } else {
-        const uint32_t job = (blockIdx.y - 2) * (kSumWarps / team) + warp / team;
+        const uint32_t job = (part - 2) * (kSumWarps / team) + warp / team;
         /* more gate rows than blocks: one of them at most lies across the end of block `job` */
         const uint32_t g = a.gates < a.blocks || job + 1 >= a.blocks ? job : block_start(a.rows, a.blocks, job + 1) / a.rows_per_gate;
         if (job < a.gate_jobs) {
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid
             }
         }
     }
-    const bool gate = blockIdx.y >= 2;
+    const bool gate = part >= 2;
     if (out && col < a.cols) {
 #pragma unroll 8
         for (uint32_t i = member + (gate && member == 0 ? team : 0u); i < n; i += team) v += p[i * step + col];
@@ -605,7 +606,10 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         while (q.gates && q.gate_warps < kSumWarps && q.blocks / q.gates >= 8 * q.gate_warps) q.gate_warps *= 2;
         const unsigned teams = kSumWarps / q.gate_warps;
         q.gate_jobs = q.gates < q.blocks ? q.gates : q.blocks ? q.blocks - 1 : 0u;
-        const dim3 grid((unsigned)((cols + 31) / 32), 2 + (q.gate_jobs + teams - 1) / teams), block(32, kSumWarps);
+        /* from the first part that is asked for to the last */
+        q.first_job = q.dpost_weight ? 0u : q.dpre_weight ? 1u : 2u;
+        const unsigned parts = q.gate_jobs ? 2 + (q.gate_jobs + teams - 1) / teams : q.dpre_weight ? 2u : 1u;
+        const dim3 grid((unsigned)((cols + 31) / 32), parts > q.first_job ? parts - q.first_job : 1u), block(32, kSumWarps);
         SIFAR_CUDA(launch_op(k_block_norm_sums, grid, block, 1, 0, (cudaStream_t)stream, q));
     }
     return SIFAR_OK;
