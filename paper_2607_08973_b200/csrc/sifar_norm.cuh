@@ -353,28 +353,42 @@ template <int N> __device__ __forceinline__ void publish_sums(float (&v)[N], Row
     }
 }
 
-/* The CTA's own totals. */
+/* The CTA's own totals.  Three values: every lane adds four warps' parts of one of them, the lanes of a value meet by
+   exchanges; twelve vectors read and added by every thread would be 50 instructions for 12.  All lanes of a warp call. */
 template <int N> __device__ __forceinline__ void local_sums(float (&v)[N], const RowSum<N> &s, uint32_t call, const RowPlace &p)
 {
-    const uint32_t n = sum_vectors(p.tx);
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const float4 *w = &s.warps[call & 1u][k][p.row * n];
+    constexpr uint32_t kVectors = kMaxRowThreads / 128;      /* of a value at most */
+    const uint32_t n = sum_vectors(p.tx), lane = p.t & 31u;
+    if (N == 1) {
+        const float4 *w = &s.warps[call & 1u][0][p.row * n];
         float2 x = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (uint32_t i = 0; i < kMaxRowThreads / 128; ++i)
+        for (uint32_t i = 0; i < kVectors; ++i)
             if (i < n) { const float4 q = w[i]; x = __fadd2_rn(x, __fadd2_rn(make_float2(q.x, q.y), make_float2(q.z, q.w))); }
-        v[k] = x.x + x.y;
+        v[0] = x.x + x.y;
+        return;
     }
+    static_assert(kVectors == 4, "lane 4 k + i: vector i of value k");
+    float x = 0.0f;
+    if ((lane & 3u) < n && lane < 4 * N) {
+        const float4 q = s.warps[call & 1u][lane / 4 % N][p.row * n + (lane & 3u)];
+        x = (q.x + q.y) + (q.z + q.w);
+    }
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 1);
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 2);
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __shfl_sync(0xFFFFFFFFu, x, 4 * k);
 }
 
 template <int N> __device__ __forceinline__ void send_sums(RowSum<N> &s, uint32_t call, const RowPlace &p)
 {
-    if (p.t < p.parts) {
+    if (p.t < 32u) {
         float v[N];
         local_sums(v, s, call, p);
+        if (p.t < p.parts) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) store_cluster_tagged(&s.parts[call & 1u][k][p.part], p.t, v[k], call + 1u);
+            for (int k = 0; k < N; ++k) store_cluster_tagged(&s.parts[call & 1u][k][p.part], p.t, v[k], call + 1u);
+        }
     }
 }
 
