@@ -6,10 +6,9 @@
  * registers from row to row and stored once per block.  The second adds the blocks' sums in order, so that the
  * result does not depend on which CTA was first.
  *
- * 8192 x 4096 bf16, two norms and a gate: 101 us with two ranks' partials (4.65 TB/s, 0.71 of the measured copy; 2.5 us of
- * it the second kernel), 134 us with eight (6.0 TB/s, 0.91).  What bounds it below that is instructions: about 460 per
- * thread of 8 items and row at 0.55 per cycle and scheduler, in 16 warps per SM, which is what the sums over rows
- * leave registers for.
+ * 8192 x 4096 bf16, two norms and a gate: 86 us with two ranks' partials (5.45 TB/s, 0.83 of the measured copy; 2.5 us of
+ * it the second kernel), 102 us with four (5.95 TB/s, 0.91).  What bounds it below that is instructions, in 16 warps per
+ * SM, which is what the sums over rows leave registers for; each tenth of them that went brought 5 to 6 % of the time.
  */
 #include "sifar_norm.cuh"
 
@@ -108,7 +107,8 @@ template <typename F, int N> struct Pending {
  * AHEAD: the pass over a row that takes its sums runs before the one that uses those of the row before it: what the sums
  * need to meet, a barrier and in a cluster a word from every CTA, passes while there is other work.
  */
-template <typename F, bool POST, bool PRE, bool AHEAD>
+/* RANKS: that many partials, or 0: any number. */
+template <typename F, bool POST, bool PRE, bool AHEAD, int RANKS>
 __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __grid_constant__ NormGradArgs a)
 {
     constexpr int kSums = POST && PRE ? 3 : 1;
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
     const Columns<F> c(p.part, p.tx, p.t, a.cols);
     const Lane<F> l(c);
     const Ring<F> ring(ring_bytes, c);
-    const int partials = PRE ? a.P : 0;
+    const int partials = !PRE ? 0 : RANKS ? RANKS : a.P;
     const bool with_z = POST || a.z;
     const uint32_t pitch = ring.threads * ring.bytes;
     const uint32_t stage_bytes = pitch * ((uint32_t)partials + (PRE ? 1u : 0u) + (a.dh ? 1u : 0u) + (with_z ? 1u : 0u));
@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
             const unsigned long long at = row;
             if (PRE) {
                 const unsigned long long o = at * a.ld_dy;
+#pragma unroll (RANKS ? RANKS : 1)
                 for (int r = 0; r < partials; ++r, to += pitch) ring.fetch(to, static_cast<const char *>(a.dy[r]) + o);
                 ring.fetch(to, static_cast<const char *>(a.h) + at * a.ld_h);
                 to += pitch;
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
                     get(x, 0, a.dy[0], a.ld_dy);
 #pragma unroll
                     for (int j = 0; j < N; ++j) G[j] = pair<F>(x, v * N + j);
-#pragma unroll 4
+#pragma unroll (RANKS ? RANKS : 4)
                     for (int r = 1; r < partials; ++r) {
                         get(x, r, a.dy[r], a.ld_dy);
 #pragma unroll
@@ -434,11 +435,11 @@ static GradShape grad_shape(int dtype, size_t rows, size_t cols)
 }
 
 /* The attribute for the ring's shared memory is set once per kernel and device. */
-template <typename F, bool POST, bool PRE, bool AHEAD>
+template <typename F, bool POST, bool PRE, bool AHEAD, int RANKS>
 static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
     static std::atomic<unsigned long long> ready{0};
-    const auto kernel = k_block_norm_grad<F, POST, PRE, AHEAD>;
+    const auto kernel = k_block_norm_grad<F, POST, PRE, AHEAD, RANKS>;
     size_t stages = 1, smem = 0;
     if (F::ACCESS == kShifted ? AHEAD : Ring<F>::possible) {
         const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes, turns = (a.rows + sh.blocks - 1) / sh.blocks;
@@ -460,15 +461,30 @@ static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStrea
     return launch_op(kernel, grid, block, sh.row.parts, smem, stream, a);
 }
 
+template <typename F, bool POST, bool PRE, int RANKS>
+static cudaError_t launch_grad_r(bool ahead, const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
+{
+    /* bf16 in clusters: a row ahead (2000 x 8200: 162 -> 124 us).  Without a cluster the barrier costs less than what the
+       second row takes (8192 x 4096: 107 -> 115 us), fp32 has no registers for it (1003 x 4099: 50 -> 56 us). */
+    if constexpr (F::DT == SIFAR_BF16)
+        if (ahead) return launch_grad_k<F, POST, PRE, true, RANKS>(sh, arrays, stream, a);
+    return launch_grad_k<F, POST, PRE, false, RANKS>(sh, arrays, stream, a);
+}
+
 template <int DT, Access A, bool POST, bool PRE>
 static cudaError_t launch_grad_n(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
     using F = Form<DT, kGradWords<DT>, A>;
-    /* bf16 in clusters: a row ahead (2000 x 8200: 162 -> 124 us).  Without a cluster the barrier costs less than what the
-       second row takes (8192 x 4096: 107 -> 115 us), fp32 has no registers for it (1003 x 4099: 50 -> 56 us). */
-    if constexpr (DT == SIFAR_BF16)
-        if (sh.row.parts > 1) return launch_grad_k<F, POST, PRE, true>(sh, arrays, stream, a);
-    return launch_grad_k<F, POST, PRE, false>(sh, arrays, stream, a);
+    const bool ahead = DT == SIFAR_BF16 && sh.row.parts > 1;
+    /* loops over few partials cost as much as their work: one and two ranks have none (8192 x 4096 bf16, two: 98 -> 86 us),
+       four in clusters (2000 x 8200: 140 -> 129; in CTAs 8192 x 4096 of four is at 102 us with the loop, at 106 without) */
+    if constexpr (PRE && A == kWhole) {
+        if (a.P == 1) return launch_grad_r<F, POST, PRE, 1>(ahead, sh, arrays, stream, a);
+        if (a.P == 2) return launch_grad_r<F, POST, PRE, 2>(ahead, sh, arrays, stream, a);
+        if constexpr (DT == SIFAR_BF16)
+            if (a.P == 4 && ahead) return launch_grad_k<F, POST, PRE, true, 4>(sh, arrays, stream, a);
+    }
+    return launch_grad_r<F, POST, PRE, 0>(ahead, sh, arrays, stream, a);
 }
 
 template <int DT, Access A>
