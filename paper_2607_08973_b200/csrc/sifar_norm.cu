@@ -26,10 +26,21 @@ struct NormArgs {
  * (One CTA per SM that walks its rows with copies ahead: 124 to 130 us.)  Few ranks move less per row and thread: 8192 x
  * 4096 bf16 of one rank 54 us, 0.76.  Up to a row per SM the launch and one pass of latencies: 3.2 us.
  */
-template <typename F, int PT> constexpr int kNormRegisters = F::W > 8 ? 112 : PT > 4 ? 128 : F::DT == SIFAR_BF16 && PT > 2 ? 80 : 72;
+/*
+ * Registers per thread: as many as keep several CTAs on an SM without much spilling.  8192 x 4096 fp32 of one rank: 105 us
+ * with 64 (two CTAs of 512 threads) against 166 with 72 (one); bf16 47 against 54.  Rows that are put together or read by
+ * elements gain down to 56 (4000 x 3001 fp32: 36 against 42 us).  Eight ranks' rows want them all (8192 x 4096 bf16: 118 us
+ * against 142 with 104), but for shifted ones, whose loads would take twice as many: four partials at a time and 72
+ * (4096 x 4097 of eight: 155 us against 333 with 128).
+ */
+template <typename F, int PT> constexpr int kNormRegisters =
+    F::W > 8 ? 112 : PT <= 2 ? (F::ACCESS == kWhole ? 64 : 56) : PT <= 4 ? (F::ACCESS == kWhole ? 64 : 72) : F::ACCESS == kWhole ? 128 : F::ACCESS == kElement ? 104 : 72;
 
-template <typename F, int PT>
-__global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F, PT>)) k_block_norm(const __grid_constant__ NormArgs a)
+/* Partials that are under way at once. */
+template <typename F, int PT> constexpr int kNormBatch = F::W > 8 ? (F::DT == SIFAR_BF16 ? 2 : 4) : F::ACCESS == kShifted && PT > 4 ? 4 : PT;
+
+template <typename F, int PT, int REGS>
+__global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__(REGS) k_block_norm(const __grid_constant__ NormArgs a)
 {
     __shared__ __align__(16) RowSum<1> s;
     grid_let_next_in();
@@ -45,7 +56,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F,
     const bool edge = at == 0 || at + 1 >= a.rows || a.narrow;
     grid_wait();
 
-    constexpr int B = F::W == 8 ? PT : F::DT == SIFAR_BF16 ? 2 : 4;     /* partials under way at once */
+    constexpr int B = kNormBatch<F, PT>;
     Raw<F> res, rg, rw1, rw2;
     Items<F> f;
     const char *gate = nullptr;
@@ -127,8 +138,14 @@ __global__ void __launch_bounds__(kMaxRowThreads) __maxnreg__((kNormRegisters<F,
 template <int DT, int W, int PT>
 static cudaError_t launch_norm_p(bool vec, dim3 grid, dim3 block, unsigned cluster, cudaStream_t stream, const NormArgs &a)
 {
-    return vec ? launch_op(k_block_norm<Form<DT, W, kWhole>, PT>, grid, block, cluster, 0, stream, a)
-               : launch_op(k_block_norm<Form<DT, W, DT == SIFAR_BF16 ? kShifted : kElement>, PT>, grid, block, cluster, 0, stream, a);
+    using V = Form<DT, W, kWhole>;
+    using E = Form<DT, W, DT == SIFAR_BF16 ? kShifted : kElement>;
+    if (!vec) return launch_op(k_block_norm<E, PT, kNormRegisters<E, PT>>, grid, block, cluster, 0, stream, a);
+    /* three and four ranks in fp32: 64 registers where two CTAs need it (4096 x 4096 of three: 80 us against 94 with 72), else
+       72 (1003 x 4099, CTAs of 288 threads: 28 us against 33) */
+    if constexpr (DT == SIFAR_F32 && W == 8 && PT == 4)
+        if (block.x * block.y * 72 * 2 <= 65536) return launch_op(k_block_norm<V, PT, 72>, grid, block, cluster, 0, stream, a);
+    return launch_op(k_block_norm<V, PT, kNormRegisters<V, PT>>, grid, block, cluster, 0, stream, a);
 }
 
 template <int DT>
