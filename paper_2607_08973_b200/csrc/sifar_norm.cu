@@ -24,7 +24,7 @@ struct NormArgs {
  * Bound by memory where there are many rows: 8192 x 4096 bf16 of eight ranks, both norms and a gate, 118 us = 6.26 TB/s,
  * 0.95 of the measured copy; a row per CTA, two to three CTAs per SM, so that one's sums pass under the other's loads.
  * (One CTA per SM that walks its rows with copies ahead: 124 to 130 us.)  Few ranks move less per row and thread: 8192 x
- * 4096 bf16 of one rank 54 us, 0.76.  Up to a row per SM the launch and one pass of latencies: 3.2 us.
+ * 4096 bf16 of one rank 47 us, 0.87.  Up to a row per SM the launch and one pass of latencies: 3.2 to 3.5 us.
  */
 /*
  * Registers per thread: as many as keep several CTAs on an SM without much spilling.  8192 x 4096 fp32 of one rank: 105 us

@@ -22,7 +22,7 @@ constexpr unsigned kMaxNormCluster = 8;
  *   kWhole    every row of every array starts on a 16-byte boundary: a vector is one access.
  *   kShifted  rows start anywhere, as contiguous rows of an odd number of columns do: a vector is put together from the two
  *             aligned ones that it lies in, and stored in the largest pieces that its address allows.
- *             (4096 x 4097 bf16: by elements 77 us forward and 244 us back.)
+ *             (4096 x 4097 bf16 of one rank: 53 us forward and 142 back, by elements 77 and 244.)
  *   kElement  single elements, neighbours by neighbouring threads.
  */
 enum Access { kWhole, kShifted, kElement };
