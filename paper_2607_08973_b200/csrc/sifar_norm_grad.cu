@@ -335,22 +335,24 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
 struct NormSumArgs {
     const float *sum_post, *sum_pre, *sum_gate;
     float *dpost_weight, *dpre_weight, *dgate;
-    uint32_t rows, cols, pitch, blocks, rows_per_gate, gates, gate_jobs, gate_warps, first_job;
+    uint32_t rows, cols, pitch, blocks, rows_per_gate, gates, gate_jobs, gate_warps, first_job, narrow;
 };
 
 /*
  * 32 columns per CTA, its warps over the blocks: part 0 is the post weight, 1 the pre weight, from 2 on the gate
  * rows that lie in more than one block, `gate_warps` warps each.  A gate row has a few blocks, a weight all of them:
  * with all warps on one gate row at a time 17 gate rows of 1003 x 4099 took 11 us.
+ * Short rows have few columns and many blocks: a warp takes 8 columns of 4 blocks then (narrow).
  */
 __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid_constant__ NormSumArgs a)
 {
     __shared__ float s[kSumWarps][32];
     grid_let_next_in();
     grid_wait();
-    const uint32_t col = blockIdx.x * 32 + threadIdx.x, warp = threadIdx.y;
+    const uint32_t warp = threadIdx.y, lane = threadIdx.x, width = a.narrow ? 8u : 32u, subs = a.narrow ? 4u : 1u;
+    const uint32_t col = blockIdx.x * width + (lane & (width - 1u)), sub = a.narrow ? lane >> 3 : 0u;
     const uint32_t part = blockIdx.y + a.first_job;
-    const uint32_t team = part < 2 ? kSumWarps : a.gate_warps, member = warp % team;
+    const uint32_t warps = part < 2 ? kSumWarps : a.gate_warps, team = warps * subs, member = (warp % warps) * subs + sub;
     const float *p = nullptr;                             /* of the member's blocks; the first one may lie elsewhere */
     float *out = nullptr;
     size_t step = a.pitch;
@@ -361,7 +363,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid
         out = part == 0 ? a.dpost_weight : a.dpre_weight;
         n = out ? a.blocks : 0u;
     } else {
-        const uint32_t job = (part - 2) * (kSumWarps / team) + warp / team;
+        const uint32_t job = (part - 2) * (kSumWarps / warps) + warp / warps;
         /* more gate rows than blocks: one of them at most lies across the end of block `job` */
         const uint32_t g = a.gates < a.blocks || job + 1 >= a.blocks ? job : block_start(a.rows, a.blocks, job + 1) / a.rows_per_gate;
         if (job < a.gate_jobs) {
@@ -381,16 +383,17 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid
             }
         }
     }
-    const bool gate = part >= 2;
     if (out && col < a.cols) {
 #pragma unroll 8
-        for (uint32_t i = member + (gate && member == 0 ? team : 0u); i < n; i += team) v += p[i * step + col];
+        for (uint32_t i = member + (part >= 2 && member == 0 ? team : 0u); i < n; i += team) v += p[i * step + col];
     }
-    s[warp][threadIdx.x] = v;
+    s[warp][lane] = v;
     __syncthreads();
     if (member == 0 && out && col < a.cols) {
-        for (uint32_t i = 1; i < team; ++i) v += s[warp + i][threadIdx.x];
-        out[col] = v;
+        float x = 0.0f;
+        for (uint32_t i = 0; i < warps; ++i)
+            for (uint32_t k = 0; k < subs; ++k) x += s[warp + i][lane + k * width];
+        out[col] = x;
     }
 }
 
@@ -625,7 +628,9 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         /* from the first part that is asked for to the last */
         q.first_job = q.dpost_weight ? 0u : q.dpre_weight ? 1u : 2u;
         const unsigned parts = q.gate_jobs ? 2 + (q.gate_jobs + teams - 1) / teams : q.dpre_weight ? 2u : 1u;
-        const dim3 grid((unsigned)((cols + 31) / 32), parts > q.first_job ? parts - q.first_job : 1u), block(32, kSumWarps);
+        q.narrow = cols <= 1024 && q.blocks >= 16 * kSumWarps;
+        const unsigned width = q.narrow ? 8 : 32;
+        const dim3 grid((unsigned)((cols + width - 1) / width), parts > q.first_job ? parts - q.first_job : 1u), block(32, kSumWarps);
         SIFAR_CUDA(launch_op(k_block_norm_sums, grid, block, 1, 0, (cudaStream_t)stream, q));
     }
     return SIFAR_OK;
