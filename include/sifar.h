@@ -390,14 +390,14 @@ int sifar_noalloc_counters(unsigned long long out[3]);
  *   - One argument block per call, read before the call returns (a program may keep one per layer and pass it again).
  *     Unused pointers and sizes are 0.  Everything is launched on the CURRENT device and on `stream`; nothing synchronizes.
  *   - `rows` x `cols` arrays have a row stride ld_* in elements, at least cols and below 2^30; 0 stands for cols.
- *     Addresses need the alignment of their element type.   Everything works at any address and stride; it is fastest where all rows start on
- *     16-byte boundaries.
+ *     Addresses need the alignment of their element type.  Everything works at any address and stride; it is fastest
+ *     where all rows start on 16-byte boundaries.
  *   - An output may overlap nothing else, except as stated.  Arrays that share a buffer column by column (same stride,
  *     disjoint columns) do not overlap.
  *   - SIFAR_ERR_INVALID: nothing was launched.  rows = 0 (tokens = 0) is valid: no row is read or written; gradients
  *     summed over the rows become 0.
- *   - The first call of each kind on a device loads its kernel; make it before a stream capture begins and while no
- *     kernel waits for another.  Captured calls keep the argument block's addresses.
+ *   - A call of types, ranks, sizes and alignments that the device has not seen may load a kernel; make it once before a
+ *     stream capture begins and while no kernel waits for another.  Captured calls keep the argument block's addresses.
  *   - Results do not depend on what else runs: sums over a row or over rows have a fixed order.
  */
 

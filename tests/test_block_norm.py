@@ -1,4 +1,5 @@
 """sifar_block_norm and its backward pass against their formulas in 64 bits, against differences, and what they refuse."""
+import ctypes
 import itertools
 
 import numpy as np
@@ -110,6 +111,23 @@ def test_the_workspace_is_a_pure_function_of_the_sizes():
     # it does not grow with the rows
     many = [sf.sifar_block_norm_backward_workspace(_backward_args(rows=r)) for r in (1 << 12, 1 << 20, (1 << 31) - 1)]
     assert many[0] == many[1] == many[2]
+
+
+def test_the_argument_blocks_lie_as_the_header_has_them(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    blocks = [sf.sifar_block_norm_args, sf.sifar_block_norm_grad_args, sf.sifar_route_args, sf.sifar_route_grad_args]
+    lines = "".join("P(sizeof(%s));" % b.__name__ + "".join("P(offsetof(%s, %s));" % (b.__name__, f) for f, _ in b._fields_) for b in blocks)
+    src = tmp_path / "offsets.c"
+    src.write_text('#include <stdio.h>\n#include "sifar.h"\n#define P(x) printf("%zu\\n", (size_t)(x))\nint main(void) { ' + lines + " return 0; }\n")
+    exe = tmp_path / "offsets"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(root, "include"), "-o", str(exe), str(src)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    want = []
+    for b in blocks:
+        want += [ctypes.sizeof(b)] + [getattr(b, f).offset for f, _ in b._fields_]
+    assert got == want
 
 
 # ---------------------------------------------------------------------------------------------------------------
@@ -465,3 +483,35 @@ def test_backward_only_what_is_asked_for_and_in_place():
     sf.sifar_block_norm_backward(a, 0)
     torch.cuda.synchronize()
     assert torch.equal(res["dh"].t, keep["dres"])
+
+
+@gpu
+def test_backward_offsets_beyond_32_bits():
+    """Rows 2^17 elements apart: the last ones lie more than 2^32 elements behind the first."""
+    rows, cols, ld = 33000, 64, 1 << 17
+    x = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda")
+    v = x.view(rows, ld)[:, :cols]
+    v.copy_(torch.randn(rows, cols, generator=torch.Generator().manual_seed(2)))
+    stats = 0.5 + torch.rand(2, rows, device="cuda")
+    dx = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda")
+    a = sf.make_block_norm_grad([x.data_ptr()], rows=rows, cols=cols, dtype=sf.BF16, dh=x.data_ptr(), h=x.data_ptr(), stats=stats.data_ptr(),
+                                dx=dx.data_ptr(), ld_dy=ld, ld_dh=ld, ld_h=ld, ld_dx=ld, pre_norm=1)
+    sf.sifar_block_norm_backward(a)
+    torch.cuda.synchronize()
+    at = torch.tensor([0, 1, 16384, 32766, 32767, 32768, 32769, 32999]).cuda()
+    t = ref.f64(v[at])
+    want, err = ref.norm_grad([t], t, t, None, ref.f64(stats[0][at]), ref.f64(stats[1][at]), None, None, None, post=0, pre=1, alpha=1.0,
+                              beta=1.0, offset=0.0, span=0)
+    assert ref.outside(dx.view(rows, ld)[at, :cols], want["dx"], err["dx"], torch.bfloat16) == ""
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+def test_a_gate_row_for_more_rows_than_there_are(dtype):
+    rows, cols = 3, 40
+    opt = dict(post=1, pre=1, span=1000, alpha=1.0, beta=0.5, offset=0.0)
+    d, rnd = _make(rows, cols, 2, dtype, 77, gate="group", span=1000)
+    fwd = _run_forward(d, rows, cols, dtype, pad=0, shift=0, eps=1e-6, **opt)
+    _check_forward(d, fwd[0], fwd[1], rows, dtype, eps=1e-6, **opt)
+    res = _run_backward(d, rnd, fwd, rows, cols, 2, dtype, pad=0, shift=0, **opt)
+    _check_backward(d, res, fwd, rows, cols, dtype, **opt)

@@ -215,6 +215,13 @@ def test_many_tokens_and_wide_rows():
     sf.sifar_route(sf.make_route([x.data_ptr()], tokens=T, experts=E, top_k=2, dtype=sf.BF16, indices=idx.data_ptr(), weights=w.data_ptr(), ld_logits=ld))
     torch.cuda.synchronize()
     assert torch.equal(idx.long(), torch.sort(v, dim=1, descending=True, stable=True).indices[:, :2])
+    dw, out = torch.randn(T, 2, generator=g, device="cuda"), torch.empty(T * ld, dtype=torch.bfloat16, device="cuda")
+    sf.sifar_route_backward(sf.make_route_grad([x.data_ptr()], tokens=T, experts=E, top_k=2, dtype=sf.BF16, indices=idx.data_ptr(),
+                                               dweights=dw.data_ptr(), dlogits=out.data_ptr(), ld_logits=ld, ld_dlogits=ld))
+    torch.cuda.synchronize()
+    at = torch.tensor([0, 16384, 32767, 32768, 32769, 32999]).cuda()
+    want, err = ref.route_grad(ref.f64(v[at]), idx[at].cpu(), ref.f64(dw[at]), sigmoid=False, renorm=False)
+    assert ref.outside(out.view(T, ld)[at, :E], want, err, torch.bfloat16) == ""
 
 
 def _grad(parts, idx, dw, dtype, *, sigmoid, renorm, scale=1.0, pad=0, shift=0):
