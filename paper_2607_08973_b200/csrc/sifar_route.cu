@@ -288,7 +288,7 @@ __device__ __noinline__ int order_exactly(const RouteArgs &a, const float *l, in
  * until the rest is far enough, and the candidates, one per lane, are put in order by their values in binary64.
  * Logits that are compared themselves have no error but the cut bits.  The groups are looked at in the same way.
  * (All values in binary64 and lists searched anew for every choice: 57 us for 8192 tokens, 8 of 256 experts in 8 groups
- * with a bias; so 10.4 us.)
+ * with a bias; so 10.4 to 11.8 us, by box.)
  *
  * Bound by instructions, 890 per token of that shape (250 of them the groups', 21 a choice), issued in 63 % of the
  * cycles with 27 warps per SM; the logits are there in a tenth of the time.  One token takes a launch, 2.7 to 3 us.
