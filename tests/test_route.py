@@ -288,3 +288,17 @@ def test_backward_against_differences_of_the_forward_kernel_s_definition(sigmoid
     v, t = torch.randn(5, 24, generator=g, dtype=torch.float64), 1e-7
     diff = (loss(l.double() + t * v) - loss(l.double() - t * v)) / (2 * t)
     assert abs(float(diff - (got.double() * v).sum())) < float(((err + ref.U * got.abs()) * v.abs()).sum()) + 1e-7
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("shift", [0.0, -30.0, 20.0])
+def test_the_only_choice_renormalised_has_a_gradient_of_exactly_zero(sigmoid, shift, dtype):
+    """Its weight is the scale whatever its logit is: w = s / s = 1, w * (d - d * w) = 0, without a rounding."""
+    g = torch.Generator().manual_seed(23)
+    parts = [torch.randn(301, 70, generator=g) + shift for _ in range(2)]
+    l = _sum32([p.to(DT[dtype]) for p in parts])
+    idx = torch.sort(l, dim=1, descending=True, stable=True).indices[:, :1]
+    got, _ = _grad(parts, idx, torch.randn(301, 1, generator=g), dtype, sigmoid=sigmoid, renorm=True, scale=1.5, pad=1)
+    assert bool((got == 0).all())
