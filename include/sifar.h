@@ -395,7 +395,7 @@ int sifar_noalloc_counters(unsigned long long out[3]);
  *   - An output may overlap nothing else, except as stated.  Arrays that share a buffer column by column (same stride,
  *     disjoint columns) do not overlap.
  *   - SIFAR_ERR_INVALID: nothing was launched.  rows = 0 (tokens = 0) is valid: no row is read or written; gradients
- *     summed over the rows become 0.
+ *     summed over the rows become 0, that of a gate row for all rows (rows_per_gate = 0) among them.
  *   - A call of types, ranks, sizes and alignments that the device has not seen may load a kernel; make it once before a
  *     stream capture begins and while no kernel waits for another.  Captured calls keep the argument block's addresses.
  *   - Results do not depend on what else runs: sums over a row or over rows have a fixed order.
@@ -425,7 +425,7 @@ typedef struct {
     float *stats;                     /* 2 x rows, or NULL: r1 of every row, then r2 of every row; 1 where no norm   */
     size_t rows, cols;                /* cols: 1 .. SIFAR_NORM_MAX_COLS                                              */
     size_t ld_x, ld_residual, ld_gate, ld_z, ld_h, ld_y;
-    size_t rows_per_gate;             /* that many consecutive rows share a gate row; 0: all of them                 */
+    size_t rows_per_gate;             /* that many consecutive rows share a gate row; 0: all of them do, 1 gate row  */
     float alpha, beta, eps, weight_offset;
     int P, dtype, post_norm, pre_norm;/* dtype (of all row and weight arrays): SIFAR_BF16 or SIFAR_F32               */
 } sifar_block_norm_args;

@@ -366,7 +366,9 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid
         const uint32_t job = (part - 2) * (kSumWarps / warps) + warp / warps;
         /* more gate rows than blocks: one of them at most lies across the end of block `job` */
         const uint32_t g = a.gates < a.blocks || job + 1 >= a.blocks ? job : block_start(a.rows, a.blocks, job + 1) / a.rows_per_gate;
-        if (job < a.gate_jobs) {
+        if (job < a.gate_jobs && a.blocks == 0) {         /* no rows, one gate row for all of them: its gradient is 0 */
+            out = a.dgate;
+        } else if (job < a.gate_jobs) {
             const uint32_t r0 = g * a.rows_per_gate, r1 = a.rows - r0 > a.rows_per_gate ? r0 + a.rows_per_gate - 1 : a.rows - 1;
             const uint32_t b0 = block_of(a.rows, a.blocks, r0), b1 = block_of(a.rows, a.blocks, r1);
             /* within one block: already there; across several ends: the first end's */
@@ -551,7 +553,9 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     }
     const size_t rows = g->rows, cols = g->cols, es = elem_size(g->dtype);
     const size_t span = g->rows_per_gate && g->rows_per_gate < rows ? g->rows_per_gate : (rows ? rows : 1);
-    const size_t gates = (rows + span - 1) / span, need = sifar_block_norm_backward_workspace(g);
+    /* one gate row for all rows is there without a row as well */
+    const size_t gates = rows ? (rows + span - 1) / span : g->rows_per_gate ? 0 : 1;
+    const size_t need = sifar_block_norm_backward_workspace(g);
     if (need && (!g->workspace || ((uintptr_t)g->workspace & 15u) || g->workspace_bytes < need)) {
         set_error("%s: need a 16-byte aligned workspace of %zu bytes", fn, need);
         return SIFAR_ERR_INVALID;
@@ -624,7 +628,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         q.gate_warps = 1;
         while (q.gates && q.gate_warps < kSumWarps && q.blocks / q.gates >= 8 * q.gate_warps) q.gate_warps *= 2;
         const unsigned teams = kSumWarps / q.gate_warps;
-        q.gate_jobs = q.gates < q.blocks ? q.gates : q.blocks ? q.blocks - 1 : 0u;
+        q.gate_jobs = q.gates < q.blocks || !q.blocks ? q.gates : q.blocks - 1;
         /* from the first part that is asked for to the last */
         q.first_job = q.dpost_weight ? 0u : q.dpre_weight ? 1u : 2u;
         const unsigned parts = q.gate_jobs ? 2 + (q.gate_jobs + teams - 1) / teams : q.dpre_weight ? 2u : 1u;

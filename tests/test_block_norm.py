@@ -515,3 +515,23 @@ def test_a_gate_row_for_more_rows_than_there_are(dtype):
     _check_forward(d, fwd[0], fwd[1], rows, dtype, eps=1e-6, **opt)
     res = _run_backward(d, rnd, fwd, rows, cols, 2, dtype, pad=0, shift=0, **opt)
     _check_backward(d, res, fwd, rows, cols, dtype, **opt)
+
+
+@gpu
+@pytest.mark.parametrize("alone", [False, True])
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+def test_backward_of_no_rows_clears_the_gradient_of_a_gate_of_all_rows(dtype, alone):
+    """rows_per_gate = 0 is one gate row, whose gradient over no rows is 0; with one row per 5 there is no gate row."""
+    cols = 1100
+    x = torch.full((cols,), 2.0, dtype=DT[dtype], device="cuda")
+    for span in (0, 5):
+        out = torch.full((3, cols + 8), CANARY, device="cuda")
+        a = sf.make_block_norm_grad([x.data_ptr()], rows=0, cols=cols, dtype=dtype, dh=x.data_ptr(), h=x.data_ptr(), z=x.data_ptr(),
+                                    stats=x.data_ptr(), gate=x.data_ptr(), post_norm=1, pre_norm=1, rows_per_gate=span,
+                                    dpost_weight=0 if alone else out[0].data_ptr(), dpre_weight=0 if alone else out[1].data_ptr(),
+                                    dgate=out[2].data_ptr())
+        sf.sifar_block_norm_backward(a, 0)
+        torch.cuda.synchronize()
+        assert bool((out[:2, :cols] == (CANARY if alone else 0)).all())
+        assert bool((out[2, :cols] == (0 if span == 0 else CANARY)).all()), span
+        assert bool((out[:, cols:] == CANARY).all())
