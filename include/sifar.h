@@ -395,7 +395,8 @@ int sifar_noalloc_counters(unsigned long long out[3]);
  *   - An output may overlap nothing else, except as stated.  Arrays that share a buffer column by column (same stride,
  *     disjoint columns) do not overlap.
  *   - SIFAR_ERR_INVALID: nothing was launched.  rows = 0 (tokens = 0) is valid: no row is read or written; gradients
- *     summed over the rows become 0, that of a gate row for all rows (rows_per_gate = 0) among them.
+ *     summed over the rows become 0, that of a gate row for all rows (rows_per_gate = 0) among them.  Arrays that have
+ *     no element then may be NULL, as the address of an empty tensor is.
  *   - A call of types, ranks, sizes and alignments that the device has not seen may load a kernel; make it once before a
  *     stream capture begins and while no kernel waits for another.  Captured calls keep the argument block's addresses.
  *   - Results do not depend on what else runs: sums over a row or over rows have a fixed order.

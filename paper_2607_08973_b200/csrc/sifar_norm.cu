@@ -180,9 +180,9 @@ extern "C" int sifar_block_norm(const sifar_block_norm_args *g, void *stream)
         set_error("%s: alpha, beta, weight_offset and eps must be finite, eps not negative", fn);
         return SIFAR_ERR_INVALID;
     }
-    if (!g->z && !g->h && !g->y) { set_error("%s: no output is asked for", fn); return SIFAR_ERR_INVALID; }
     if (g->y && !g->pre_norm) { set_error("%s: y needs pre_norm", fn); return SIFAR_ERR_INVALID; }
-    if (g->rows == 0) return SIFAR_OK;
+    if (g->rows == 0) return SIFAR_OK;                   /* arrays without an element may be NULL */
+    if (!g->z && !g->h && !g->y) { set_error("%s: no output is asked for", fn); return SIFAR_ERR_INVALID; }
 
     const size_t rows = g->rows, cols = g->cols, es = elem_size(g->dtype);
     const size_t span = g->rows_per_gate && g->rows_per_gate < rows ? g->rows_per_gate : rows, gates = (rows + span - 1) / span;

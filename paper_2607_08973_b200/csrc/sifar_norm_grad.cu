@@ -537,7 +537,8 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         set_error("%s: alpha, beta and weight_offset must be finite", fn);
         return SIFAR_ERR_INVALID;
     }
-    if (!g->dx && !g->dresidual && !g->dpost_weight && !g->dpre_weight && !g->dgate) {
+    /* without rows the arrays of rows have no element and may be NULL */
+    if (g->rows && !g->dx && !g->dresidual && !g->dpost_weight && !g->dpre_weight && !g->dgate) {
         set_error("%s: no output is asked for", fn);
         return SIFAR_ERR_INVALID;
     }
@@ -547,7 +548,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
         return SIFAR_ERR_INVALID;
     }
     const bool need_z = post || g->dgate;
-    if ((pre && !g->h) || (need_z && !g->z) || ((post || pre) && !g->stats) || (!pre && !g->dh)) {
+    if (g->rows && ((pre && !g->h) || (need_z && !g->z) || ((post || pre) && !g->stats) || (!pre && !g->dh))) {
         set_error("%s: h is needed with pre_norm, z with post_norm or dgate, stats with a norm, dh without pre_norm", fn);
         return SIFAR_ERR_INVALID;
     }
@@ -563,7 +564,7 @@ extern "C" int sifar_block_norm_backward(const sifar_block_norm_grad_args *g, vo
     RowArray all[kMaxRanks + 16];
     int n = 0;
     for (int r = 0; pre && r < g->P; ++r) {
-        if (!g->dy[r]) { set_error("%s: dy[%d] is NULL", fn, r); return SIFAR_ERR_INVALID; }
+        if (rows && !g->dy[r]) { set_error("%s: dy[%d] is NULL", fn, r); return SIFAR_ERR_INVALID; }
         all[n++] = RowArray{"dy", g->dy[r], rows, cols, or_cols(g->ld_dy, cols), es, false};
     }
     const RowArray dh{"dh", g->dh, rows, cols, or_cols(g->ld_dh, cols), es, false};

@@ -535,3 +535,31 @@ def test_backward_of_no_rows_clears_the_gradient_of_a_gate_of_all_rows(dtype, al
         assert bool((out[:2, :cols] == (CANARY if alone else 0)).all())
         assert bool((out[2, :cols] == (0 if span == 0 else CANARY)).all()), span
         assert bool((out[:, cols:] == CANARY).all())
+
+
+def test_no_rows_need_no_row_arrays():
+    """An empty tensor has the address 0: a rank without tokens passes those."""
+    assert sf.sifar_block_norm(_forward_args(x=[0, 0], rows=0, residual=0, h=0, y=0)) == sf.OK
+    none = dict(rows=0, dh=0, h=0, z=0, stats=0, dx=0, dresidual=0, dpost_weight=0, dpre_weight=0, workspace=0, workspace_bytes=0)
+    assert sf.sifar_block_norm_backward(_backward_args(dy=[0, 0], dgate=0, **none)) == sf.OK
+    assert sf.sifar_block_norm_backward(_backward_args(dy=[0, 0], gate=0, dgate=0, rows_per_gate=3, **none)) == sf.OK
+    # what is wrong whatever the rows stays refused
+    for over in (dict(x=[]), dict(dtype=7), dict(cols=0), dict(pre_norm=0), dict(eps=-1.0)):
+        with pytest.raises(sf.SifarError):
+            sf.sifar_block_norm(_forward_args(rows=0, **over))
+    for over in (dict(dtype=7), dict(cols=0), dict(beta=float("inf")), dict(post_norm=0), dict(pre_norm=0)):
+        with pytest.raises(sf.SifarError):
+            sf.sifar_block_norm_backward(_backward_args(rows=0, **over))
+
+
+@gpu
+def test_backward_of_no_rows_without_row_arrays_clears_the_sums():
+    cols = 260
+    w = torch.ones(cols, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((3, cols), CANARY, device="cuda")
+    a = sf.make_block_norm_grad([0, 0], rows=0, cols=cols, dtype=sf.BF16, post_norm=1, pre_norm=1, post_weight=w.data_ptr(),
+                                pre_weight=w.data_ptr(), gate=w.data_ptr(), dpost_weight=out[0].data_ptr(),
+                                dpre_weight=out[1].data_ptr(), dgate=out[2].data_ptr())
+    sf.sifar_block_norm_backward(a, 0)
+    torch.cuda.synchronize()
+    assert bool((out == 0).all())
