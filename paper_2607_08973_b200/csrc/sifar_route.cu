@@ -467,9 +467,9 @@ __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 :
         w = softmax ? expf(logit - max) : scaled_sigmoid(logit, max);
         if (!mine || max == -INFINITY) w = 0.0f;
         const float total = sifar::warp_sum(w);
-        w = max == -INFINITY ? 0.0f : __fdividef(w, total);
+        w = max == -INFINITY ? 0.0f : w / total;
     } else if (softmax) {
-        w = top == -INFINITY ? 0.0f : __fdividef(expf(logit - top), sum);
+        w = top == -INFINITY ? 0.0f : expf(logit - top) / sum;
     } else {
         w = sigmoid(logit);
     }

@@ -302,3 +302,21 @@ def test_the_only_choice_renormalised_has_a_gradient_of_exactly_zero(sigmoid, sh
     idx = torch.sort(l, dim=1, descending=True, stable=True).indices[:, :1]
     got, _ = _grad(parts, idx, torch.randn(301, 1, generator=g), dtype, sigmoid=sigmoid, renorm=True, scale=1.5, pad=1)
     assert bool((got == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_weights_are_quotients_rounded_once(sigmoid):
+    """Where numerator and sum are exact in binary32 the weight is their quotient rounded once: of k equal logits 1 / k, of
+    a single choice 1, of E equal experts without renormalising 1 / E."""
+    one = torch.ones((), dtype=torch.float32)
+    for k in range(1, 33):
+        _, w, _ = _go([torch.zeros(2, 40)], sf.F32, k=k, sigmoid=sigmoid, renorm=True)
+        assert bool((w == one / k).all()), k
+    g = torch.Generator().manual_seed(31)
+    _, w, _ = _go([4.0 * torch.randn(500, 40, generator=g)], sf.F32, k=1, sigmoid=sigmoid, renorm=True, scale=1.25)
+    assert bool((w == 1.25).all())
+    if not sigmoid:
+        for E in [*range(1, 70), 100, 187, 255, 257, 511, 771, 1023]:
+            _, w, _ = _go([torch.full((2, E), -3.0)], sf.BF16, k=1, sigmoid=False, renorm=False)
+            assert bool((w == one / E).all()), E
