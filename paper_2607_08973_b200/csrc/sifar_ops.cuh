@@ -120,7 +120,8 @@ inline int check_array(const char *fn, const RowArray &a)
         set_error("%s: %s is not aligned to its %zu-byte elements", fn, a.name, a.es);
         return SIFAR_ERR_INVALID;
     }
-    if (a.ld < a.cols || a.ld > kMaxStride) {
+    /* a list (ld = cols) is as long as it is: its kernels index it in 64 bits.  Rows have at most SIFAR_NORM_MAX_COLS columns */
+    if (a.ld < a.cols || (a.ld > kMaxStride && a.ld != a.cols)) {
         set_error("%s: the row stride of %s (%zu) is less than its %zu columns, or too large", fn, a.name, a.ld, a.cols);
         return SIFAR_ERR_INVALID;
     }

@@ -563,3 +563,38 @@ def test_backward_of_no_rows_without_row_arrays_clears_the_sums():
     sf.sifar_block_norm_backward(a, 0)
     torch.cuda.synchronize()
     assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("rows", [1 << 29, (1 << 31) - 1])
+def test_statistics_of_2_to_the_29_rows_and_more_are_not_refused_for_their_length(rows):
+    """The overlap is what stops these calls: nothing is launched, on any machine."""
+    far = [(16 + i) << 40 for i in range(8)]
+    with pytest.raises(sf.SifarError) as e:
+        sf.sifar_block_norm(_forward_args(x=[far[0]], rows=rows, cols=1, residual=0, y=0, h=far[1], stats=far[1] + 64))
+    assert "overlaps" in str(e.value)
+    with pytest.raises(sf.SifarError) as e:
+        sf.sifar_block_norm_backward(_backward_args(dy=[far[0]], rows=rows, cols=1, dh=0, h=far[1], z=far[2], stats=far[3], gate=0, dx=far[3] + 64,
+                                                    dresidual=0, dpost_weight=0, dpre_weight=0, dgate=0))
+    assert "overlaps" in str(e.value)
+
+
+@gpu
+def test_statistics_of_more_than_2_to_the_29_rows():
+    rows = (1 << 29) + 5
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(rows, generator=g, device="cuda", dtype=torch.bfloat16)
+    h, stats = torch.empty_like(x), torch.empty(2, rows, device="cuda")
+    sf.sifar_block_norm(sf.make_block_norm([x.data_ptr()], rows=rows, cols=1, dtype=sf.BF16, h=h.data_ptr(), stats=stats.data_ptr(), post_norm=1,
+                                           pre_norm=1, eps=0.25))
+    at = torch.tensor([0, 1, (1 << 28) - 1, 1 << 28, (1 << 29) - 1, 1 << 29, rows - 1]).cuda()
+    want, err = ref.norm([ref.f64(x[at])[:, None]], None, None, None, None, post=1, pre=1, alpha=1.0, beta=1.0, eps=0.25, offset=0.0, span=0)
+    assert ref.outside(h[at][:, None], want["h"], err["h"], torch.bfloat16) == ""
+    for i, n in enumerate(("r1", "r2")):
+        assert ref.outside(stats[i][at], want[n], err[n], torch.float32) == "", n
+    dx = torch.empty_like(x)
+    sf.sifar_block_norm_backward(sf.make_block_norm_grad([x.data_ptr()], rows=rows, cols=1, dtype=sf.BF16, h=h.data_ptr(), z=x.data_ptr(),
+                                                         stats=stats.data_ptr(), dx=dx.data_ptr(), post_norm=1, pre_norm=1))
+    c = lambda t: ref.f64(t[at])[:, None]  # noqa: E731
+    want, err = ref.norm_grad([c(x)], None, c(h), c(x), ref.f64(stats[0][at]), ref.f64(stats[1][at]), None, None, None, post=1, pre=1, alpha=1.0,
+                              beta=1.0, offset=0.0, span=0)
+    assert ref.outside(dx[at][:, None], want["dx"], err["dx"], torch.bfloat16) == ""

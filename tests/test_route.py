@@ -320,3 +320,37 @@ def test_weights_are_quotients_rounded_once(sigmoid):
         for E in [*range(1, 70), 100, 187, 255, 257, 511, 771, 1023]:
             _, w, _ = _go([torch.full((2, E), -3.0)], sf.BF16, k=1, sigmoid=False, renorm=False)
             assert bool((w == one / E).all()), E
+
+
+@pytest.mark.parametrize("tokens,top_k", [(1 << 26, 16), ((1 << 31) - 1, 16), ((1 << 30) + 7, 1)])
+def test_lists_of_2_to_the_30_results_and_more_are_not_refused_for_their_length(tokens, top_k):
+    """The overlap is what stops these calls: nothing is launched, on any machine."""
+    far = [(16 + i) << 40 for i in range(4)]
+    with pytest.raises(sf.SifarError) as e:
+        sf.sifar_route(_args(logits=[far[0]], tokens=tokens, experts=16, top_k=top_k, groups=1, top_groups=1, bias=0, indices=far[1], weights=far[1] + 64))
+    assert "overlaps" in str(e.value)
+    with pytest.raises(sf.SifarError) as e:
+        sf.sifar_route_backward(_grad_args(logits=[far[0]], tokens=tokens, experts=16, top_k=top_k, indices=far[1], dweights=far[2], dlogits=far[2] + 64))
+    assert "overlaps" in str(e.value)
+    with pytest.raises(sf.SifarError) as e:                  # the stride of rows has its limit
+        sf.sifar_route(_args(logits=[far[0]], ld_logits=1 << 30, indices=far[1], weights=far[2]))
+    assert "row stride of logits" in str(e.value)
+
+
+@gpu
+def test_more_than_2_to_the_30_results():
+    T, E, k = (1 << 25) + 3, 32, 32
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(T, E, generator=g, device="cuda", dtype=torch.bfloat16)
+    idx, w = torch.full((T, k), -7, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda")
+    a = sf.make_route([x.data_ptr()], tokens=T, experts=E, top_k=k, dtype=sf.BF16, indices=idx.data_ptr(), weights=w.data_ptr(), renormalize=1)
+    sf.sifar_route(a)
+    at = torch.tensor([0, 1, (1 << 24) - 1, 1 << 24, (1 << 25) - 1, 1 << 25, T - 1]).cuda()
+    assert torch.equal(idx[at].long(), torch.sort(x[at], dim=1, descending=True, stable=True).indices)
+    assert bool(((w.sum(1) - 1).abs() < 64 * ref.U).all())
+    dw, out = torch.randn(T, k, generator=g, device="cuda"), torch.empty_like(x)
+    b = sf.make_route_grad([x.data_ptr()], tokens=T, experts=E, top_k=k, dtype=sf.BF16, indices=idx.data_ptr(), dweights=dw.data_ptr(),
+                           dlogits=out.data_ptr(), renormalize=1)
+    sf.sifar_route_backward(b)
+    want, err = ref.route_grad(ref.f64(x[at]), idx[at].cpu(), ref.f64(dw[at]), sigmoid=False, renorm=True)
+    assert ref.outside(out[at], want, err, torch.bfloat16) == ""
