@@ -199,7 +199,8 @@ template <typename F> __device__ __forceinline__ void add_items(Items<F> &acc, c
     for (int i = 0; i < acc.N; ++i) add_pair<F>(acc.p[i], x, i);
 }
 
-/* weight + offset, or 1 where there is no weight */
+/* weight + offset, or 1 where there is no weight.  A vector behind the row's end, in whose place load_whole reads the row's
+   first, is 0: an infinite weight times the zeros there would make the row's sums NaN. */
 template <typename F>
 __device__ __forceinline__ Items<F> load_factor(const void *weight, float offset, const Columns<F> &c, const Lane<F> &l)
 {
@@ -208,7 +209,7 @@ __device__ __forceinline__ Items<F> load_factor(const void *weight, float offset
     load_weight(w, weight, c, l);
     Items<F> f = items<F>(w);
 #pragma unroll
-    for (int i = 0; i < f.N; ++i) f.p[i] = __fadd2_rn(f.p[i], both(offset));
+    for (int i = 0; i < f.N; ++i) f.p[i] = F::VEC && !l.in[i / F::vector_pairs] ? both(0.0f) : __fadd2_rn(f.p[i], both(offset));
     return f;
 }
 

@@ -598,3 +598,23 @@ def test_statistics_of_more_than_2_to_the_29_rows():
     want, err = ref.norm_grad([c(x)], None, c(h), c(x), ref.f64(stats[0][at]), ref.f64(stats[1][at]), None, None, None, post=1, pre=1, alpha=1.0,
                               beta=1.0, offset=0.0, span=0)
     assert ref.outside(dx[at][:, None], want["dx"], err["dx"], torch.bfloat16) == ""
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("cols", [264, 300, 4104])
+def test_an_infinite_weight_gives_the_formula_s_infinities(cols, dtype):
+    """pre_weight[0] = inf: mean(a * n2) is infinite, and so is every column's D but the weight's own, where inf - inf is NaN,
+    whether or not threads of the row have no columns."""
+    rows = 4
+    opt = dict(post=0, pre=1, span=0, alpha=1.0, beta=1.0, offset=0.0)
+    d, rnd = _make(rows, cols, 2, dtype, 63)
+    fwd = _run_forward(d, rows, cols, dtype, pad=0, shift=0, eps=1e-5, **opt)
+    d["w2"][0] = float("inf")
+    res = _run_backward(d, rnd, fwd, rows, cols, 2, dtype, pad=0, shift=0, **opt)
+    want, _ = ref.norm_grad([ref.f64(x.t) for x in res["dys"]], ref.f64(res["dh"].t), ref.f64(fwd[0]["h"].t), None, ref.f64(fwd[1][:rows]),
+                            ref.f64(fwd[1][rows:2 * rows]), None, None, ref.f64(d["w2"]), **opt)
+    got, want = ref.f64(res["dres"].t), want["dres"]
+    assert float(torch.isinf(want[:, 1:]).double().mean()) > 0.99 and bool(torch.isnan(want[:, 0]).all())
+    # NaN as well where h is exactly 0
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(nan=1.0), want.nan_to_num(nan=1.0))
