@@ -10,12 +10,10 @@
 
 #include <atomic>
 
+#include "sifar_norm_shape.cuh"
 #include "sifar_ops.cuh"
 
 namespace sifar {
-
-constexpr int kMaxRowThreads = 512;
-constexpr unsigned kMaxNormCluster = 8;
 
 /*
  * How a kernel reaches its rows.
@@ -506,20 +504,6 @@ template <typename F> struct Ring {
         }
     }
 };
-
-/* How many CTAs hold a row and how many threads of each. */
-struct RowShape {
-    unsigned tx, parts;
-};
-inline RowShape row_shape(int items, size_t cols)          /* items: of a thread */
-{
-    const size_t need = (cols + items - 1) / items;
-    RowShape s;
-    for (s.parts = 1;; s.parts *= 2) {
-        s.tx = (unsigned)(((need + s.parts - 1) / s.parts + 31) / 32 * 32);
-        if (s.tx <= (unsigned)kMaxRowThreads) return s;
-    }
-}
 
 }  /* namespace sifar */
 #endif

@@ -89,10 +89,6 @@ __device__ __forceinline__ void end_of_gate(const NormGradArgs &a, const Columns
     acc = all_items<F>(0.0f);
 }
 
-/* 16 bytes of an array per thread in bf16: with 32 the sums over rows spill (8192 x 4096, two ranks: 107 us against 134;
-   two CTAs per SM with 64 registers each: 163). */
-template <int DT> constexpr int kGradWords = DT == SIFAR_BF16 ? 4 : 8;
-
 /* What a row leaves between the pass that takes its sums and the one that uses them. */
 template <typename F, int N> struct Pending {
     Items<F> D;                              /* dh + r2 * a */
@@ -399,64 +395,24 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_block_norm_sums(const __grid
     }
 }
 
-/*
- * Into how many blocks of consecutive rows the rows are cut, and how the blocks lie in CTAs: as many as have room at
- * once, 512 threads per SM (the rows under way and the sums over rows fill its memory and registers).
- */
-constexpr uint32_t kMaxStages = 4;
-constexpr size_t kRingBytes = 216 * 1024;    /* of the 227 KB that an SM has for its CTAs */
-struct GradShape {
-    RowShape row;
-    unsigned ry, per_sm;                     /* blocks of a CTA, CTAs of an SM */
-    uint32_t blocks;
-};
-
-/* Clusters of `parts` CTAs that a B200 holds at once with k CTAs per SM (cudaOccupancyMaxActiveClusters): its GPCs do not
-   all have a multiple of 4 SMs. */
-static unsigned clusters_at_once(unsigned parts, unsigned k)
-{
-    static const unsigned four[4] = {33, 71, 104, 142}, eight[4] = {15, 33, 48, 71};
-    if (parts <= 2) return kSms * k / parts;
-    const unsigned *t = parts == 4 ? four : eight;
-    return k <= 4 ? t[k - 1] : t[3] * (k / 4);
-}
-
-template <int DT> GradShape grad_shape_of(size_t rows, size_t cols)
-{
-    const int items = kGradWords<DT> * 4 / (int)elem_size(DT);
-    GradShape s;
-    s.row = row_shape(items, cols);
-    s.ry = s.row.tx == 32 ? 4 : 1;
-    s.per_sm = kMaxRowThreads / (s.row.tx * s.ry);
-    uint32_t most = clusters_at_once(s.row.parts, s.per_sm) * s.ry;
-    /* few rows: a CTA of its own for each */
-    while (s.ry > 1 && rows <= most / 2) { s.ry /= 2; most /= 2; }
-    s.blocks = (uint32_t)(rows < most ? rows : most);
-    return s;
-}
-static GradShape grad_shape(int dtype, size_t rows, size_t cols)
-{
-    return dtype == SIFAR_BF16 ? grad_shape_of<SIFAR_BF16>(rows, cols) : grad_shape_of<SIFAR_F32>(rows, cols);
-}
-
 /* The attribute for the ring's shared memory is set once per kernel and device. */
 template <typename F, bool POST, bool PRE, bool AHEAD, int RANKS>
 static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStream_t stream, NormGradArgs &a)
 {
     static std::atomic<unsigned long long> ready{0};
     const auto kernel = k_block_norm_grad<F, POST, PRE, AHEAD, RANKS>;
+    constexpr int kSums = POST && PRE ? 3 : 1;
+    static_assert(sizeof(RowSum<kSums>) == row_sum_bytes(kSums), "what ring_room() leaves for the sums");
     size_t stages = 1, smem = 0;
     if (F::ACCESS == kShifted ? AHEAD : Ring<F>::possible) {
-        const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes, turns = (a.rows + sh.blocks - 1) / sh.blocks;
-        stages = kRingBytes / sh.per_sm / row;
-        if (stages > kMaxStages) stages = kMaxStages;
-        if (stages > turns) stages = turns;
+        const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes;
+        stages = grad_stages(sh, a.rows, row, kSums);
         smem = row * stages;
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
         if (dev > 63 || !(ready.load(std::memory_order_acquire) >> dev & 1ull)) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring_room(1, kSums));
             if (e != cudaSuccess) return e;
             if (dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_release);
         }

@@ -94,7 +94,6 @@ struct RowArray {
     bool out;
 };
 
-constexpr unsigned kSms = 148;               /* of a B200 */
 constexpr size_t kMaxRows = (size_t)1 << 31;
 constexpr size_t kMaxStride = ((size_t)1 << 30) - 1;      /* elements; in bytes it fits 32 bits */
 
