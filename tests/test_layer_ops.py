@@ -1,5 +1,6 @@
 """The operators behind an all-reduce as a layer runs them: one after the other, beside the all-reduce itself, in captured
 graphs, on other streams."""
+import importlib.util
 import os
 import subprocess
 import sys
@@ -241,3 +242,34 @@ def test_without_programmatic_launches():
         path = os.path.join(d, "out.npy")
         subprocess.run([sys.executable, "-c", code, path], check=True, cwd=ROOT, env=dict(os.environ, SIFAR_PDL="0"), timeout=300)
         assert np.array_equal(np.load(path), want)
+
+
+@pytest.mark.parametrize("name", ["norm-1", "norm-grad-64", "route-1", "route-grad-64"])
+def test_the_timed_calls_are_ordered_with_the_stream_that_they_are_made_on(name):
+    """The cases of perf/operators.py under a side stream and in a captured graph: the kernels' form belongs to the current
+    stream as the plain form does."""
+    spec = importlib.util.spec_from_file_location("timed_operators", os.path.join(ROOT, "perf", "operators.py"))
+    cases = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(cases)
+    cases.own = True
+    state = cases.prepare(next(c for c in cases.listed() if c["name"] == name), 3)
+    want = {n: t.clone() for n, t in cases.run(state).items()}
+    torch.cuda.synchronize()
+    outs = cases.run(state)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        sf.sifar_spin(2000, side.cuda_stream)                # what comes before on the stream
+        for t in outs.values():
+            t.zero_()
+        cases.run(state)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want[n]) for n, t in outs.items())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cases.run(state)
+    for t in outs.values():
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want[n]) for n, t in outs.items())
