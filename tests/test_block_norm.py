@@ -618,3 +618,44 @@ def test_an_infinite_weight_gives_the_formula_s_infinities(cols, dtype):
     assert float(torch.isinf(want[:, 1:]).double().mean()) > 0.99 and bool(torch.isnan(want[:, 0]).all())
     # NaN as well where h is exactly 0
     assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(nan=1.0), want.nan_to_num(nan=1.0))
+
+
+# Rows that start on 16 bytes and take a cluster of two, four and eight CTAs, more of them than there are clusters at once (74,
+# 33, 15): blocks hold several rows, and gate rows end inside them.
+ALIGNED = [
+    # rows, cols, P, post, pre, gate, span
+    (160, 8192, 1, 1, 1, "group", 7), (160, 8192, 2, 0, 1, "group", 3), (150, 4104, 4, 1, 1, "channel", 0), (150, 4104, 4, 0, 1, "group", 50),
+    (150, 4104, 1, 0, 1, "none", 0), (150, 4104, 2, 1, 1, "group", 1), (231, 4608, 3, 1, 1, "group", 11), (160, 5120, 8, 1, 1, "none", 0),
+    (160, 5120, 3, 0, 1, "group", 2), (149, 4104, 8, 1, 0, "group", 4), (100, 16384, 2, 1, 1, "group", 6), (70, 12288, 1, 1, 1, "channel", 0),
+    (70, 9000, 4, 1, 1, "group", 9), (50, 32768, 4, 1, 1, "group", 8), (40, 20000, 1, 0, 1, "channel", 0), (33, 32000, 2, 1, 1, "none", 0),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("i", range(len(ALIGNED)))
+def test_backward_of_aligned_rows_in_clusters(i, dtype):
+    rows, cols, P, post, pre, gate, span = ALIGNED[i]
+    opt = dict(post=post, pre=pre, span=span, alpha=0.75, beta=1.5, offset=float(i % 2))
+    d, rnd = _make(rows, cols, P, dtype, 300 + i, 0, 0, gate, span)
+    fwd = _run_forward(d, rows, cols, dtype, pad=0, shift=0, eps=1e-5, **opt)
+    res = _run_backward(d, rnd, fwd, rows, cols, P, dtype, pad=0, shift=0, with_dh=i % 3 != 1 or not pre, **opt)
+    _check_backward(d, res, fwd, rows, cols, dtype, **opt)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("rows,cols,P", [(160, 8192, 2), (150, 4097, 3), (230, 4104, 1), (400, 1001, 2), (50, 20001, 1), (900, 100, 2)])
+def test_the_gradient_of_the_residual_over_dh(rows, cols, P, dtype):
+    """In place, where neighbouring rows' bytes are fetched ahead and where they are not: the bits of the call with a buffer of its own."""
+    opt = dict(post=1, pre=1, span=7, alpha=0.75, beta=1.5, offset=0.0)
+    d, rnd = _make(rows, cols, P, dtype, 41, gate="group", span=7)
+    fwd = _run_forward(d, rows, cols, dtype, pad=0, shift=0, eps=1e-5, **opt)
+    res = _run_backward(d, rnd, fwd, rows, cols, P, dtype, pad=0, shift=0, **opt)
+    want, dx, dgate = res["dres"].t.clone(), res["dx"].t.clone(), res["dgate"].clone()
+    a = res["args"]
+    a.dresidual = a.dh
+    sf.sifar_block_norm_backward(a, 0)
+    torch.cuda.synchronize()
+    assert torch.equal(res["dh"].t, want) and res["dh"].clean()
+    assert torch.equal(res["dx"].t, dx) and torch.equal(res["dgate"], dgate)
