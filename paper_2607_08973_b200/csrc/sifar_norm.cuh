@@ -34,6 +34,7 @@ template <int DT_, int W_, Access A_> struct Form {
     static constexpr uint32_t es = sizeof(T);
     static constexpr int items = W_ * 4 / (int)sizeof(T), pairs = items / 2;
     static constexpr int vectors = W_ / 4, vector_pairs = pairs / vectors;       /* of 16 bytes */
+    static_assert(A_ != kShifted || DT_ == SIFAR_BF16, "fp32 elements are words: single ones do");
     static_assert(SIFAR_NORM_MAX_COLS <= items * kMaxRowThreads * (int)kMaxNormCluster, "columns that a cluster holds");
 };
 
@@ -111,7 +112,7 @@ template <typename F> __device__ __forceinline__ void shift_vectors(Raw<F> &x, i
 #pragma unroll
     for (int i = 0; i < 5; ++i) w[i] = m & 4u ? w[i + 1] : w[i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.w[4 * v + i] = F::DT == SIFAR_F32 ? w[i] : __funnelshift_r(w[i], w[i + 1], (m & 2u) * 8u);
+    for (int i = 0; i < 4; ++i) x.w[4 * v + i] = __funnelshift_r(w[i], w[i + 1], (m & 2u) * 8u);
 }
 template <typename F>
 __device__ __forceinline__ void load_shifted(Raw<F> &x, int v, const void *row, const Lane<F> &l)
@@ -133,8 +134,8 @@ template <typename F>
 __device__ __forceinline__ void load_vector(Raw<F> &x, int v, const void *row, const Columns<F> &c, const Lane<F> &l, bool each)
 {
     if (F::ACCESS == kElement || each) load_each(x, v, row, c);
-    else if (F::ACCESS == kWhole) load_whole(x, v, row, l);
-    else load_shifted(x, v, row, l);
+    else if constexpr (F::ACCESS == kShifted) load_shifted(x, v, row, l);
+    else load_whole(x, v, row, l);
 }
 template <typename F>
 __device__ __forceinline__ void load_row(Raw<F> &x, const void *row, const Columns<F> &c, const Lane<F> &l, bool each)
@@ -429,7 +430,7 @@ __device__ __forceinline__ float rrms(float sum, uint32_t cols, float eps) { ret
  * threads' words side by side, 16 bytes each (VEC) or 4.
  */
 template <typename F> struct Ring {
-    static constexpr bool possible = F::ACCESS != kElement || F::DT == SIFAR_F32;    /* a copy moves 4 bytes at least */
+    static_assert(F::ACCESS != kElement || F::DT == SIFAR_F32, "a copy moves 4 bytes at least");
     static constexpr bool shifted = F::ACCESS == kShifted;
     static constexpr uint32_t unit = F::VEC ? 16 : 4;
     static constexpr int copies = shifted ? 2 : 1;                   /* of a vector: the two aligned ones around it */
@@ -489,7 +490,7 @@ template <typename F> struct Ring {
     __device__ __forceinline__ void read_vector(Raw<F> &x, int v, const unsigned char *smem, uint32_t at, const void *row) const
     {
         const unsigned char *p = smem + at + (threadIdx.y * blockDim.x + threadIdx.x) * unit;
-        if (shifted) {
+        if constexpr (shifted) {
             shift_vectors(x, v, *reinterpret_cast<const uint4 *>(p + 2 * v * threads * unit),
                           *reinterpret_cast<const uint4 *>(p + (2 * v + 1) * threads * unit), (uint32_t)(uintptr_t)row & 15u);
         } else if (F::VEC) {

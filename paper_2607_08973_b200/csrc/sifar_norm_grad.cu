@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kMaxRowThreads, 1) k_block_norm_grad(const __g
     constexpr int kSums = POST && PRE ? 3 : 1;
     /* shifted rows: copied ahead in clusters (4096 x 4097, four ranks: 227 -> 185 us), read from memory, their lines asked
        for two rows before, where a CTA holds them (16384 x 515: 73 us against 86 with copies) */
-    constexpr bool kRing = F::ACCESS == kShifted ? AHEAD : Ring<F>::possible;
+    constexpr bool kRing = F::ACCESS != kShifted || AHEAD;
     extern __shared__ __align__(16) unsigned char ring_bytes[];
     __shared__ __align__(16) RowSum<kSums> s;
     grid_let_next_in();
@@ -404,7 +404,7 @@ static cudaError_t launch_grad_k(const GradShape &sh, unsigned arrays, cudaStrea
     constexpr int kSums = POST && PRE ? 3 : 1;
     static_assert(sizeof(RowSum<kSums>) == row_sum_bytes(kSums), "what ring_room() leaves for the sums");
     size_t stages = 1, smem = 0;
-    if (F::ACCESS == kShifted ? AHEAD : Ring<F>::possible) {
+    if (F::ACCESS != kShifted || AHEAD) {
         const size_t row = (size_t)sh.row.tx * sh.ry * arrays * Ring<F>::bytes;
         stages = grad_stages(sh, a.rows, row, kSums);
         smem = row * stages;

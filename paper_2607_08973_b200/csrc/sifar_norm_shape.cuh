@@ -44,14 +44,11 @@ struct GradShape {
     uint32_t blocks;
 };
 
-/* Clusters of `parts` CTAs that a B200 holds at once with k CTAs per SM (cudaOccupancyMaxActiveClusters): its GPCs do not
-   all have a multiple of 4 SMs. */
-inline unsigned clusters_at_once(unsigned parts, unsigned k)
+/* Blocks of rows that a B200 holds at once as clusters of `parts` CTAs with `per_sm` CTAs per SM: a row that takes a cluster has 288
+   threads of each CTA at least, one CTA per SM (cudaOccupancyMaxActiveClusters: the GPCs do not all have a multiple of 4 SMs). */
+inline unsigned clusters_at_once(unsigned parts, unsigned per_sm)
 {
-    constexpr unsigned four[4] = {33, 71, 104, 142}, eight[4] = {15, 33, 48, 71};
-    if (parts <= 2) return kSms * k / parts;
-    const unsigned *t = parts == 4 ? four : eight;
-    return k <= 4 ? t[k - 1] : t[3] * (k / 4);
+    return parts == 1 ? kSms * per_sm : parts == 2 ? kSms / 2 : parts == 4 ? 33 : 15;
 }
 
 template <int DT> GradShape grad_shape_of(size_t rows, size_t cols)
