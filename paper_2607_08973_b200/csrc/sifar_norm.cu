@@ -21,13 +21,15 @@ struct NormArgs {
  * in a thread, as many partials as its registers take); z, h and y never leave the registers between.  PT is P or the
  * next power of two above it.
  *
- * Bound by memory where there are many rows: 8192 x 4096 bf16 of eight ranks, both norms and a gate, 118 us = 6.26 TB/s,
- * 0.95 of the measured copy; a row per CTA, two to three CTAs per SM, so that one's sums pass under the other's loads.
- * (One CTA per SM that walks its rows with copies ahead: 124 to 130 us.)  Few ranks move less per row and thread: 8192 x
- * 4096 bf16 of one rank 47 us, 0.87.  Up to a row per SM the launch and one pass of latencies: 3.2 to 3.5 us.
+ * Bound by memory where there are many rows: 8192 x 4096 bf16 of eight ranks, both norms and a gate, 118 to 127 us by where
+ * the buffers lie = 6.2 to 5.8 TB/s, 0.95 to 0.89 of the measured copy; a row per CTA of 256 threads, two CTAs per SM (117
+ * registers; four in the forms of 56 and 64), so that one's sums pass under the other's loads.  (One CTA per SM that walks its
+ * rows with copies ahead: 124 to 130 us where this one took 118.)  Few ranks move less per row and thread: 8192 x 4096 bf16 of
+ * one rank 47 us, 0.87.  Up to a row per SM the launch and one pass of latencies: 3.2 to 4.1 us.
  */
 /*
- * Registers per thread: as many as keep several CTAs on an SM without much spilling.  8192 x 4096 fp32 of one rank: 105 us
+ * Registers per thread: as many as keep several CTAs on an SM.  What spills (ptxas, bytes of stores a thread): nothing for
+ * eight ranks but 308 for their shifted rows, up to 128 in the forms of one to four.  8192 x 4096 fp32 of one rank: 105 us
  * with 64 (two CTAs of 512 threads) against 166 with 72 (one); bf16 47 against 54.  Rows that are put together or read by
  * elements gain down to 56 (4000 x 3001 fp32: 36 against 42 us).  Eight ranks' rows want them all (8192 x 4096 bf16: 118 us
  * against 142 with 104), but for shifted ones, whose loads would take twice as many: four partials at a time and 72

@@ -60,7 +60,7 @@ template <typename F> struct Lane {
     bool ragged;
     __device__ __forceinline__ explicit Lane(const Columns<F> &c)
     {
-                bool cut = !F::VEC || c.cols == 0;                /* a row that is not there: nothing is read */
+        bool cut = !F::VEC || c.cols == 0;                /* a row that is not there: nothing is read */
 #pragma unroll
         for (int v = 0; v < F::vectors; ++v) {
             const uint32_t i = c.at(v * c.EPV);

@@ -288,10 +288,11 @@ __device__ __noinline__ int order_exactly(const RouteArgs &a, const float *l, in
  * until the rest is far enough, and the candidates, one per lane, are put in order by their values in binary64.
  * Logits that are compared themselves have no error but the cut bits.  The groups are looked at in the same way.
  * (All values in binary64 and lists searched anew for every choice: 57 us for 8192 tokens, 8 of 256 experts in 8 groups
- * with a bias; so 10.4 to 11.8 us, by box.)
+ * with a bias; so 10.8 to 14.4 us with inputs of eight seeds, whose instructions differ by less than 0.1 %.)
  *
- * Bound by instructions, 890 per token of that shape (250 of them the groups', 21 a choice), issued in 63 % of the
- * cycles with 27 warps per SM; the logits are there in a tenth of the time.  One token takes a launch, 2.7 to 3 us.
+ * Bound by instructions, 933 per token of that shape (317 of them the groups', 21 a choice, 39 the exact division of the
+ * weights), issued in 62 % of the cycles with 26 warps per SM.  Without groups and bias, 524: 6.7 us.  One token takes a
+ * launch, 2.6 to 3 us.
  */
 template <int DT, int NI, bool BIAS, bool GROUPS>
 __global__ void __launch_bounds__(32 * kRouteWarps, NI <= 8 ? 8 : NI <= 16 ? 5 : 3) k_route(const __grid_constant__ RouteArgs a)
