@@ -21,8 +21,8 @@ struct NormArgs {
  * in a thread, as many partials as its registers take); z, h and y never leave the registers between.  PT is P or the
  * next power of two above it.
  *
- * Bound by memory where there are many rows: 8192 x 4096 bf16 of eight ranks, both norms and a gate, 118 to 127 us by where
- * the buffers lie = 6.2 to 5.8 TB/s, 0.95 to 0.89 of the measured copy; a row per CTA of 256 threads, two CTAs per SM (117
+ * Bound by memory where there are many rows: 8192 x 4096 bf16 of eight ranks, both norms and a gate, 118 to 127 us by
+ * run = 6.2 to 5.8 TB/s, 0.95 to 0.89 of the measured copy; a row per CTA of 256 threads, two CTAs per SM (117
  * registers; four in the forms of 56 and 64), so that one's sums pass under the other's loads.  (One CTA per SM that walks its
  * rows with copies ahead: 124 to 130 us where this one took 118.)  Few ranks move less per row and thread: 8192 x 4096 bf16 of
  * one rank 47 us, 0.87.  Up to a row per SM the launch and one pass of latencies: 3.2 to 4.1 us.

@@ -6,7 +6,7 @@
  * registers from row to row and stored once per block.  The second adds the blocks' sums in order, so that the
  * result does not depend on which CTA was first.
  *
- * 8192 x 4096 bf16, two norms and a gate: 86 to 91 us by where the buffers lie with two ranks' partials (5.5 to 5.2 TB/s,
+ * 8192 x 4096 bf16, two norms and a gate: 85 to 91 us by run with two ranks' partials (5.5 to 5.2 TB/s,
  * 0.84 to 0.79 of the measured copy; 2.5 us of it the second kernel), 102 us with four (5.95 TB/s, 0.91).  What bounds it
  * below that is instructions, in 16 warps per SM, which is what the sums over rows leave registers for; each tenth of them
  * that went brought 5 to 6 % of the time.

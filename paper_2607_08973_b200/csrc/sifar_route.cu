@@ -288,7 +288,7 @@ __device__ __noinline__ int order_exactly(const RouteArgs &a, const float *l, in
  * until the rest is far enough, and the candidates, one per lane, are put in order by their values in binary64.
  * Logits that are compared themselves have no error but the cut bits.  The groups are looked at in the same way.
  * (All values in binary64 and lists searched anew for every choice: 57 us for 8192 tokens, 8 of 256 experts in 8 groups
- * with a bias; so 10.8 to 14.4 us with inputs of eight seeds, whose instructions differ by less than 0.1 %.)
+ * with a bias; so 10.8 to 14.4 us by the inputs, whose instructions differ by less than 0.1 %: the same ones repeat to 0.1 us.)
  *
  * Bound by instructions, 933 per token of that shape (317 of them the groups', 21 a choice, 39 the exact division of the
  * weights), issued in 62 % of the cycles with 26 warps per SM.  Without groups and bias, 524: 6.7 us.  One token takes a
