@@ -53,7 +53,8 @@
  *                           the GPU has SMs, one whose producers were all enqueued on other streams or all on its
  *                           own (sifar_pack, sifar_arrive), the sweep kernel, a pack of at most one CTA per SM,
  *                           sifar_arrive, sifar_wait_writable, sifar_allreduce_noalloc and the operators behind an
- *                           all-reduce (sifar_block_norm, sifar_route and their backward passes).  In the two barrier-free
+ *                           all-reduce and between two of them (sifar_block_norm, sifar_route and their backward passes,
+ *                           sifar_cache_append, sifar_decode_attention, sifar_experts).  In the two barrier-free
  *                           modes the loads of a reducer whose producers are on other streams then start at once
  *                           (they are ordered by flags or tags, not by the stream); everything else that such a
  *                           kernel reads or writes waits until the kernel before it is complete.
@@ -519,6 +520,115 @@ typedef struct {
 } sifar_route_grad_args;
 
 int sifar_route_backward(const sifar_route_grad_args *args, void *stream);
+
+/*
+ * What a decode step does between two all-reduces: the new tokens' keys and values go into a paged cache, attention
+ * reads it, and the chosen experts multiply.  The paper has no counterpart for these three calls either; they fill the
+ * two stretches in which its layer produces the partial sums of its next all-reduce (Section 2).  A rank passes its own heads
+ * and its own experts.  The common rules above hold, and:
+ *   - Index arrays (page_table, sequence, position, lengths, indices) are device arrays of int, looked at by the kernels:
+ *     an entry that leads nowhere is left out as stated, it is never followed.
+ *   - A workspace is 16-byte aligned and this call's alone until the call has run; what it holds before does not matter.
+ */
+
+/* Largest head of the two calls on a cache. */
+enum { SIFAR_CACHE_MAX_HEAD_DIM = 256 };
+
+/*
+ * The cache: `pages` pages of `page_size` tokens, in each token kv_heads rows of head_dim elements, keys in k_cache and
+ * values in v_cache, laid out alike.  stride_page, stride_token and stride_head are in elements; all three 0 stand for
+ * contiguous pages x page_size x kv_heads x head_dim.  Either order of tokens and heads in a page will do, no two rows
+ * may overlap.  Token n of sequence s is token n % page_size of page page_table[s * ld_page_table + n / page_size]
+ * (sequences x max_pages, ld_page_table 0: max_pages).  A page is there if n / page_size < max_pages and the entry is in
+ * 0 .. pages - 1.  max_pages * page_size is below 2^31.
+ */
+
+/*
+ * Turns the new tokens' queries and keys by their positions and writes keys and values to the cache.  Per token and head,
+ * for i < rotary_dim / 2, with the pair (a, b) at (i, i + rotary_dim / 2) or, `interleaved`, at (2 i, 2 i + 1):
+ *     angle = position * inv_freq[i]                         (the product as it is, taken modulo a full turn in binary64)
+ *     a' = a * cos(angle) - b * sin(angle)
+ *     b' = a * sin(angle) + b * cos(angle)
+ * in binary32, rounded once; elements from rotary_dim on, and values, are copied.  A token with a negative position or
+ * with a sequence outside 0 .. sequences - 1 is padding: nothing of it is read or written.  One whose page is not there
+ * has its query turned and is not kept.  Where two tokens of a call have the same place, it holds elements of both.
+ */
+typedef struct {
+    const void *q, *k, *v;            /* tokens x heads * head_dim; tokens x kv_heads * head_dim; they may share rows   */
+    void *q_out;                      /* tokens x heads * head_dim; may be q itself (same address and stride)           */
+    void *k_cache, *v_cache;
+    const int *page_table;
+    const int *sequence;              /* tokens, or NULL: token i belongs to sequence i                                 */
+    const int *position;              /* tokens                                                                         */
+    const float *inv_freq;            /* rotary_dim / 2                                                                 */
+    size_t tokens, sequences, pages, page_size, max_pages;
+    size_t ld_q, ld_k, ld_v, ld_q_out, ld_page_table;
+    size_t stride_page, stride_token, stride_head;
+    int dtype, heads, kv_heads, head_dim;   /* heads 0: no queries, q and q_out NULL                                    */
+    int rotary_dim, interleaved;            /* even, 0 .. head_dim                                                      */
+} sifar_cache_append_args;
+
+int sifar_cache_append(const sifar_cache_append_args *args, void *stream);
+
+/*
+ * Attention of one new token per sequence over the cache.  Query head h reads key head h / (heads / kv_heads).  With n =
+ * lengths[s] (the new token, already in the cache, included), over the tokens j of [max(0, n - window), n) (window 0: all n)
+ *     x_j = scale * q . k_j;   out = sum_j exp(x_j) v_j / sum_j exp(x_j);   lse = log(sum_j exp(x_j))
+ * in binary32, out rounded once.  Tokens beyond max_pages * page_size and tokens whose page is not there are left out, as
+ * if masked; a negative length is 0.  Masked tokens are not read.  A head without a score above -infinity gives
+ * 0 and lse = -infinity.
+ * The cache is read once for all query heads of a key head up to 16 of them (binary32: 8); more heads read it again.
+ */
+typedef struct {
+    const void *q;                    /* sequences x heads * head_dim                                                   */
+    const void *k_cache, *v_cache;
+    const int *page_table;
+    const int *lengths;               /* sequences                                                                      */
+    void *out;                        /* sequences x heads * head_dim                                                   */
+    float *lse;                       /* sequences x heads, contiguous, or NULL                                         */
+    void *workspace;
+    size_t workspace_bytes;           /* at least sifar_decode_attention_workspace(args)                                */
+    size_t sequences, pages, page_size, max_pages, window;
+    size_t ld_q, ld_out, ld_page_table;
+    size_t stride_page, stride_token, stride_head;
+    float scale;
+    int dtype, heads, kv_heads, head_dim;   /* kv_heads divides heads                                                   */
+} sifar_decode_attention_args;
+
+/* Bytes of workspace for these sizes (pure function, independent of the lengths; 0 if the sizes are refused). */
+size_t sifar_decode_attention_workspace(const sifar_decode_attention_args *args);
+int sifar_decode_attention(const sifar_decode_attention_args *args, void *stream);
+
+/*
+ * The chosen experts' products for a few tokens.  Over the choices j of token t with e = indices[t][j] - first_expert in
+ * 0 .. experts - 1 (other choices are another rank's, and those that sifar_route_backward calls dropped):
+ *     a_j = weights[t][j] * act(gate_e x_t) * (up_e x_t);     out_t = sum_j down_e a_j
+ * with sums in binary32 and in an order of their own; the bf16 products take a_j as the sum of two bf16 values (16 bits),
+ * out is rounded once.  act is x / (1 + exp(-x)) or x * (1 + erf(x / sqrt 2)) / 2.  An expert that a token has chosen
+ * twice counts with both weights.  A token without a choice here gives 0.  `out` is one rank's partial of the all-reduce
+ * behind the layer: it may lie in the buffer that sifar_rank_buffer returned.
+ * Each chosen expert's weights are read once for up to 64 of its tokens.
+ */
+enum { SIFAR_ACT_SILU = 0, SIFAR_ACT_GELU = 1 };
+enum { SIFAR_EXPERTS_MAX_TOKENS = 256, SIFAR_EXPERTS_MAX_COLS = 32768 };
+
+typedef struct {
+    const void *x;                    /* tokens x hidden                                                                */
+    const int *indices;               /* tokens x top_k, contiguous: as sifar_route leaves them                         */
+    const float *weights;             /* tokens x top_k, contiguous                                                     */
+    const void *gate_up;              /* experts x 2 * inter rows of hidden: an expert's gate rows, then its up rows    */
+    const void *down;                 /* experts x hidden rows of inter                                                 */
+    void *out;                        /* tokens x hidden                                                                */
+    void *workspace;
+    size_t workspace_bytes;           /* at least sifar_experts_workspace(args)                                         */
+    size_t tokens, hidden, inter;     /* tokens: 0 .. SIFAR_EXPERTS_MAX_TOKENS; others 1 .. SIFAR_EXPERTS_MAX_COLS      */
+    size_t ld_x, ld_gate_up, ld_down, ld_out;
+    int dtype, experts, first_expert, top_k;   /* experts: 1 .. SIFAR_ROUTE_MAX_EXPERTS; top_k: 1 .. SIFAR_ROUTE_MAX_TOP_K */
+    int activation;
+} sifar_experts_args;
+
+size_t sifar_experts_workspace(const sifar_experts_args *args);
+int sifar_experts(const sifar_experts_args *args, void *stream);
 
 /* Geometry helpers (no device work). */
 size_t sifar_slot_count(int dtype, size_t n);          /* slots needed for n elements  */

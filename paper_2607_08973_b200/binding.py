@@ -68,6 +68,11 @@ def lib() -> ctypes.CDLL:
             "sifar_block_norm_backward_workspace": (sz, [ctypes.POINTER(sifar_block_norm_grad_args)]),
             "sifar_route": (ci, [ctypes.POINTER(sifar_route_args), vp]),
             "sifar_route_backward": (ci, [ctypes.POINTER(sifar_route_grad_args), vp]),
+            "sifar_cache_append": (ci, [ctypes.POINTER(sifar_cache_append_args), vp]),
+            "sifar_decode_attention": (ci, [ctypes.POINTER(sifar_decode_attention_args), vp]),
+            "sifar_decode_attention_workspace": (sz, [ctypes.POINTER(sifar_decode_attention_args)]),
+            "sifar_experts": (ci, [ctypes.POINTER(sifar_experts_args), vp]),
+            "sifar_experts_workspace": (sz, [ctypes.POINTER(sifar_experts_args)]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -289,6 +294,68 @@ def sifar_route(args: sifar_route_args, stream: int = 0) -> int:
 
 def sifar_route_backward(args: sifar_route_grad_args, stream: int = 0) -> int:
     return _check(lib().sifar_route_backward(args, stream))
+
+
+# ---------------------------------------------------------------------------
+# between two all-reduces of a decode step: the paged cache, its attention, the chosen experts (see include/sifar.h)
+# ---------------------------------------------------------------------------
+CACHE_MAX_HEAD_DIM = 256
+ACT_SILU, ACT_GELU = 0, 1
+EXPERTS_MAX_TOKENS, EXPERTS_MAX_COLS = 256, 32768
+
+sifar_cache_append_args = _struct(
+    "sifar_cache_append_args", ptr="q k v q_out k_cache v_cache page_table sequence position inv_freq",
+    size="tokens sequences pages page_size max_pages ld_q ld_k ld_v ld_q_out ld_page_table stride_page stride_token stride_head",
+    int="dtype heads kv_heads head_dim rotary_dim interleaved")
+sifar_decode_attention_args = _struct(
+    "sifar_decode_attention_args", ptr="q k_cache v_cache page_table lengths out lse workspace",
+    size="workspace_bytes sequences pages page_size max_pages window ld_q ld_out ld_page_table stride_page stride_token stride_head",
+    float="scale", int="dtype heads kv_heads head_dim")
+sifar_experts_args = _struct(
+    "sifar_experts_args", ptr="x indices weights gate_up down out workspace",
+    size="workspace_bytes tokens hidden inter ld_x ld_gate_up ld_down ld_out",
+    int="dtype experts first_expert top_k activation")
+
+
+def make_append(*, tokens: int, sequences: int, heads: int, kv_heads: int, head_dim: int, rotary_dim: int, dtype: int,
+                **fields) -> sifar_cache_append_args:
+    """Argument block of sifar_cache_append: `fields` as in the header, absent ones 0."""
+    return sifar_cache_append_args(tokens=tokens, sequences=sequences, heads=heads, kv_heads=kv_heads, head_dim=head_dim,
+                                   rotary_dim=rotary_dim, dtype=dtype, **fields)
+
+
+def make_attention(*, sequences: int, heads: int, kv_heads: int, head_dim: int, dtype: int, scale: float | None = None,
+                   **fields) -> sifar_decode_attention_args:
+    """Argument block of sifar_decode_attention; `scale` is 1 / sqrt(head_dim) unless given."""
+    scale = max(1, head_dim) ** -0.5 if scale is None else scale
+    return sifar_decode_attention_args(sequences=sequences, heads=heads, kv_heads=kv_heads, head_dim=head_dim, dtype=dtype,
+                                       scale=scale, **fields)
+
+
+def make_experts(*, tokens: int, hidden: int, inter: int, experts: int, top_k: int, dtype: int,
+                 **fields) -> sifar_experts_args:
+    """Argument block of sifar_experts."""
+    return sifar_experts_args(tokens=tokens, hidden=hidden, inter=inter, experts=experts, top_k=top_k, dtype=dtype, **fields)
+
+
+def sifar_cache_append(args: sifar_cache_append_args, stream: int = 0) -> int:
+    return _check(lib().sifar_cache_append(args, stream))
+
+
+def sifar_decode_attention(args: sifar_decode_attention_args, stream: int = 0) -> int:
+    return _check(lib().sifar_decode_attention(args, stream))
+
+
+def sifar_decode_attention_workspace(args: sifar_decode_attention_args) -> int:
+    return lib().sifar_decode_attention_workspace(args)
+
+
+def sifar_experts(args: sifar_experts_args, stream: int = 0) -> int:
+    return _check(lib().sifar_experts(args, stream))
+
+
+def sifar_experts_workspace(args: sifar_experts_args) -> int:
+    return lib().sifar_experts_workspace(args)
 
 
 # ---------------------------------------------------------------------------

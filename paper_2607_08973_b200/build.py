@@ -2,7 +2,8 @@
 
 ``libsifar.so``        the all-reduce itself: context, producer-side store path,
                        reducer kernels, the allocation-free entry point, the norms
-                       and the routing behind an all-reduce
+                       and the routing behind an all-reduce, the paged cache, its
+                       attention and the experts between two of them
                        (``include/sifar.h``).
 ``libsifar_bench.so``  the synthetic decode-step chains, generator probes and
                        measurement helpers (``include/sifar_workload.h``); it
@@ -34,7 +35,8 @@ LIB_BENCH = os.path.join(PKG, "libsifar_bench.so")
 LIB_S8X2 = os.path.join(PKG, "libsifar_s8x2.so")
 
 # which translation units go into which library
-CORE_UNITS = ("sifar_core", "sifar_noalloc", "sifar_norm", "sifar_norm_grad", "sifar_route")
+CORE_UNITS = ("sifar_core", "sifar_noalloc", "sifar_norm", "sifar_norm_grad", "sifar_route",
+              "sifar_append", "sifar_attention", "sifar_experts")
 SLOT_UNITS = ("sifar_core", "sifar_noalloc")          # ... and know the slot format: built a second time for it
 BENCH_UNITS = ("sifar_workload", "sifar_symmetric", "sifar_chain_cluster", "sifar_chain_pipe")
 

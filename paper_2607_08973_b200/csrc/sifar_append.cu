@@ -1,0 +1,235 @@
+/*
+ * sifar_append.cu - new tokens' queries and keys turned by their positions, keys and values into the paged cache.
+ *
+ * A CTA per token: cosines and sines of the token's angles once, in shared memory, for all its heads.  Each thread has
+ * the first loads of its elements under way while they are computed.  Bound by memory: every element is read and
+ * written once.
+ */
+#include "sifar_cache.cuh"
+
+namespace sifar {
+
+struct AppendArgs {
+    const char *q, *k, *v;
+    char *q_out, *k_cache, *v_cache;
+    const int *sequence, *position;
+    const float *inv_freq;
+    Pages pages;
+    unsigned long long ld_q, ld_k, ld_v, ld_q_out;     /* bytes */
+    uint32_t sequences;
+    uint32_t heads, kv_heads, dim, half;               /* half = rotary_dim / 2 */
+    uint32_t turned, copied;                           /* items of a head that turns, of one that is copied */
+    uint32_t turned_magic, copied_magic;               /* ceil(2^32 / items), items > 1: exact quotients below 2^24 */
+};
+
+/* V elements from one place on, as binary32 or as they are. */
+template <int DT, int V> struct Piece {
+    using T = typename Elem<DT>::type;
+    uint32_t w[V == 1 ? 1 : 4];
+    __device__ __forceinline__ void load(const char *p)
+    {
+        if (V == 1) w[0] = *reinterpret_cast<const T *>(p);
+        else *reinterpret_cast<uint4 *>(w) = *reinterpret_cast<const uint4 *>(p);
+    }
+    __device__ __forceinline__ void store(char *p) const
+    {
+        if (V == 1) *reinterpret_cast<T *>(p) = (T)w[0];
+        else *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(w);
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if (DT == SIFAR_F32) return __uint_as_float(w[i]);
+        if (V == 1) return __uint_as_float(w[0] << 16);
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+    __device__ __forceinline__ void set(int i, float f)
+    {
+        if (DT == SIFAR_F32) w[i] = __float_as_uint(f);
+        else if (V == 1) w[0] = narrow<DT>(f);
+        else w[i / 2] = i & 1 ? (w[i / 2] & 0xFFFFu) | (uint32_t)narrow<DT>(f) << 16 : (w[i / 2] & 0xFFFF0000u) | narrow<DT>(f);
+    }
+};
+
+/*
+ * An item is what a thread loads, turns and stores at once: V pairs in two pieces (halves apart), V / 2 pairs in one
+ * piece (interleaved; V = 1: one pair in two pieces), or a piece that is copied.
+ */
+template <int DT, int V, bool INTER>
+__global__ void __launch_bounds__(512) k_append(const __grid_constant__ AppendArgs a)
+{
+    constexpr int es = DT == SIFAR_BF16 ? 2 : 4, B = 4;
+    constexpr bool kOne = INTER && V > 1;              /* a pair lies within a piece */
+    __shared__ float s_cos[SIFAR_CACHE_MAX_HEAD_DIM / 2], s_sin[SIFAR_CACHE_MAX_HEAD_DIM / 2];
+    const uint32_t token = blockIdx.x;
+    grid_let_next_in();
+    grid_wait();
+    const int position = a.position[token];
+    const uint32_t sequence = a.sequence ? (uint32_t)a.sequence[token] : token;
+    if (position < 0 || sequence >= a.sequences) return;
+
+    const uint32_t n_turn = (a.heads + a.kv_heads) * a.turned, n = n_turn + a.kv_heads * a.copied;
+    const uint32_t pairs = kOne ? 2 * a.half / V : a.half / V;       /* items of a head that have pairs */
+    const char *const q = a.q + token * a.ld_q, *const k = a.k + token * a.ld_k, *const v = a.v + token * a.ld_v;
+    char *const q_out = a.q_out + token * a.ld_q_out;
+    const long long at = token_offset(a.pages, a.pages.table + sequence * a.pages.ld_table, (uint32_t)position);
+
+    /* item -> where its pieces lie: the element offsets in the head's row, the second one 0 where there is no second */
+    struct Item { const char *src; char *dst; uint32_t first, second, i; bool turn; };
+    auto item = [&](uint32_t idx) {
+        Item t;
+        uint32_t head;
+        if (idx < n_turn) {
+            head = a.turned == 1 ? idx : __umulhi(idx, a.turned_magic);
+            t.i = idx - head * a.turned;
+            t.turn = t.i < pairs;
+            if (t.turn) {
+                t.first = kOne ? t.i * V : INTER ? 2 * t.i : t.i * V;
+                t.second = kOne ? 0 : INTER ? t.first + 1 : t.first + a.half;
+            } else {
+                t.first = 2 * a.half + (t.i - pairs) * V;
+                t.second = 0;
+            }
+            const bool query = head < a.heads;
+            if (!query) head -= a.heads;
+            t.src = (query ? q : k) + head * a.dim * es;
+            t.dst = query ? q_out + head * a.dim * es : at < 0 ? nullptr : a.k_cache + at + head * a.pages.stride_head;
+        } else {
+            idx -= n_turn;
+            head = a.copied == 1 ? idx : __umulhi(idx, a.copied_magic);
+            t.i = idx - head * a.copied;
+            t.turn = false;
+            t.first = t.i * V;
+            t.second = 0;
+            t.src = v + head * a.dim * es;
+            t.dst = at < 0 ? nullptr : a.v_cache + at + head * a.pages.stride_head;
+        }
+        return t;
+    };
+
+    bool ready = false;
+    for (uint32_t i0 = threadIdx.x; i0 < n || !ready; i0 += B * blockDim.x) {
+        Piece<DT, V> p[B], r[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const uint32_t idx = i0 + b * blockDim.x;
+            if (idx >= n) continue;
+            const Item t = item(idx);
+            if (!t.dst) continue;
+            p[b].load(t.src + t.first * es);
+            if (t.second) r[b].load(t.src + t.second * es);
+        }
+        if (!ready) {
+            /* the angle in full turns, its whole ones taken off before it is narrowed: far positions lose nothing */
+            for (uint32_t i = threadIdx.x; i < a.half; i += blockDim.x) {
+                const double turns = (double)position * (double)a.inv_freq[i] * 0.15915494309189533577;
+                sincospif((float)(2.0 * (turns - rint(turns))), &s_sin[i], &s_cos[i]);
+            }
+            __syncthreads();
+            ready = true;
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const uint32_t idx = i0 + b * blockDim.x;
+            if (idx >= n) continue;
+            const Item t = item(idx);
+            if (!t.dst) continue;
+            if (t.turn) {
+                if (kOne) {
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) {
+                        const float c = s_cos[t.i * (V / 2) + e], s = s_sin[t.i * (V / 2) + e], x = p[b].get(2 * e), y = p[b].get(2 * e + 1);
+                        p[b].set(2 * e, x * c - y * s);
+                        p[b].set(2 * e + 1, x * s + y * c);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float c = s_cos[t.i * V + e], s = s_sin[t.i * V + e], x = p[b].get(e), y = r[b].get(e);
+                        p[b].set(e, x * c - y * s);
+                        r[b].set(e, x * s + y * c);
+                    }
+                }
+            }
+            p[b].store(t.dst + t.first * es);
+            if (t.second) r[b].store(t.dst + t.second * es);
+        }
+    }
+}
+
+}  /* namespace sifar */
+
+using namespace sifar;
+
+extern "C" int sifar_cache_append(const sifar_cache_append_args *g, void *stream)
+{
+    static const char *fn = "sifar_cache_append";
+    if (!g) { set_error("%s: no argument block", fn); return SIFAR_ERR_INVALID; }
+    CacheShape c;
+    if (int rc = check_cache(fn, c, g->dtype, g->kv_heads, g->head_dim, g->pages, g->page_size, g->max_pages, g->sequences, g->ld_page_table,
+                             g->stride_page, g->stride_token, g->stride_head)) return rc;
+    if (g->heads < 0 || ((size_t)g->heads + (size_t)g->kv_heads) * (size_t)g->head_dim >= (1u << 20) || g->rotary_dim < 0 || g->rotary_dim > g->head_dim ||
+        g->rotary_dim % 2 || g->tokens >= kMaxRows) {
+        set_error("%s: need heads >= 0, (heads + kv_heads) * head_dim below 2^20, an even rotary_dim of 0 .. head_dim and tokens below 2^31", fn);
+        return SIFAR_ERR_INVALID;
+    }
+    if (g->tokens == 0) return SIFAR_OK;
+    if (!g->k || !g->v || !g->k_cache || !g->v_cache || !g->position || (g->heads && (!g->q || !g->q_out)) || (!g->heads && (g->q || g->q_out)) ||
+        (!g->page_table && c.max_pages && c.sequences) || (!g->inv_freq && g->rotary_dim)) {
+        set_error("%s: k, v, the caches, page_table and position are needed, inv_freq to turn, q and q_out where there are heads", fn);
+        return SIFAR_ERR_INVALID;
+    }
+    const size_t es = c.es, T = g->tokens, nq = (size_t)g->heads * c.dim, nk = (size_t)g->kv_heads * c.dim;
+    const auto ld = [](size_t given, size_t cols) { return given ? given : cols; };
+    const RowArray q{"q", g->q, T, nq, ld(g->ld_q, nq), es, false}, k{"k", g->k, T, nk, ld(g->ld_k, nk), es, false};
+    const RowArray v{"v", g->v, T, nk, ld(g->ld_v, nk), es, false}, q_out{"q_out", g->q_out, T, nq, ld(g->ld_q_out, nq), es, true};
+    const size_t entries = c.sequences ? (c.sequences - 1) * c.ld_table + c.max_pages : 0;
+    const RowArray table{"page_table", g->page_table, 1, entries, entries, sizeof(int), false};
+    const RowArray sequence{"sequence", g->sequence, 1, T, T, sizeof(int), false}, position{"position", g->position, 1, T, T, sizeof(int), false};
+    const size_t half = (size_t)g->rotary_dim / 2;
+    const RowArray freq{"inv_freq", g->inv_freq, 1, half, half, sizeof(float), false};
+    const bool in_place = g->q && g->q == g->q_out && (q.ld == q_out.ld || T == 1);
+    RowArray all[8] = {k, v, q_out, table, sequence, position, freq, q};
+    if (int rc = check_arrays(fn, all, in_place ? 7 : 8)) return rc;
+    if (int rc = check_array(fn, q)) return rc;
+    const size_t extent = cache_extent(c);
+    const RowArray kc{"k_cache", g->k_cache, 1, 1, 1, es, true}, vc{"v_cache", g->v_cache, 1, 1, 1, es, true};
+    if (int rc = check_array(fn, kc)) return rc;
+    if (int rc = check_array(fn, vc)) return rc;
+    for (const RowArray &x : all)
+        if (touches(x, g->k_cache, extent) || touches(x, g->v_cache, extent)) { set_error("%s: the cache overlaps %s", fn, x.name); return SIFAR_ERR_INVALID; }
+    const long long apart = (long long)((intptr_t)g->v_cache - (intptr_t)g->k_cache);
+    if (c.pages && (apart % (long long)es || rows_meet(c, apart / (long long)es, 0))) { set_error("%s: v_cache overlaps k_cache", fn); return SIFAR_ERR_INVALID; }
+
+    AppendArgs a;
+    a.q = (const char *)g->q; a.k = (const char *)g->k; a.v = (const char *)g->v;
+    a.q_out = (char *)g->q_out; a.k_cache = (char *)g->k_cache; a.v_cache = (char *)g->v_cache;
+    a.sequence = g->sequence; a.position = g->position; a.inv_freq = g->inv_freq;
+    a.pages = device_pages(c, g->page_table);
+    a.ld_q = q.ld * es; a.ld_k = k.ld * es; a.ld_v = v.ld * es; a.ld_q_out = q_out.ld * es;
+    a.sequences = (uint32_t)c.sequences;
+    a.heads = (uint32_t)g->heads; a.kv_heads = (uint32_t)g->kv_heads; a.dim = (uint32_t)c.dim; a.half = (uint32_t)half;
+    /* 16-byte pieces where every head's row and both halves of what turns are whole ones */
+    const size_t per = 16 / es;
+    const bool inter = g->interleaved != 0;
+    const bool vec = rows_aligned16(q) && rows_aligned16(k) && rows_aligned16(v) && rows_aligned16(q_out) && cache_aligned16(c, g->k_cache, g->v_cache) &&
+                     c.dim % per == 0 && (inter ? 2 * half : half) % per == 0;
+    const size_t V = vec ? per : 1;
+    a.turned = (uint32_t)((inter && vec ? 2 * half : half) / V + (c.dim - 2 * half) / V);
+    a.copied = (uint32_t)(c.dim / V);
+    const auto magic = [](uint32_t d) { return d == 1 ? 0u : (uint32_t)((((unsigned long long)1 << 32) + d - 1) / d); };
+    a.turned_magic = magic(a.turned); a.copied_magic = magic(a.copied);
+    const size_t items = (nq + nk) / c.dim * a.turned + (size_t)g->kv_heads * a.copied;
+    size_t threads = 64;
+    while (threads < 512 && threads * 2 < items) threads *= 2;
+    const dim3 grid((unsigned)T), block((unsigned)threads);
+    const cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t err;
+    if (g->dtype == SIFAR_BF16)
+        err = !vec ? (inter ? launch_op(k_append<SIFAR_BF16, 1, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_BF16, 1, false>, grid, block, 1, 0, st, a))
+                   : (inter ? launch_op(k_append<SIFAR_BF16, 8, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_BF16, 8, false>, grid, block, 1, 0, st, a));
+    else
+        err = !vec ? (inter ? launch_op(k_append<SIFAR_F32, 1, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_F32, 1, false>, grid, block, 1, 0, st, a))
+                   : (inter ? launch_op(k_append<SIFAR_F32, 4, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_F32, 4, false>, grid, block, 1, 0, st, a));
+    SIFAR_CUDA(err);
+    return SIFAR_OK;
+}

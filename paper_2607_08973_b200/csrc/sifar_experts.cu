@@ -1,0 +1,728 @@
+/*
+ * sifar_experts.cu - the chosen experts' products for a few tokens: one rank's partial of the next all-reduce.
+ *
+ * Every chosen expert's weights go once from memory through registers into matrix instructions, and that is what bounds
+ * the call: a token has 2 operations per weight, the memory takes 2 bytes for one.  So the weights are the 16 rows of
+ * an instruction and the tokens its 8 columns.  A lane loads 16 bytes in a row of a weight row; the products' order
+ * over k is free, so the eight elements become two instructions' fragments as they lie, with the tokens' taken from the same
+ * places.  No weight passes through shared memory.
+ *
+ *   k_up_few, k_down_few     up to 8 tokens.  All tokens are columns for every expert, the warps of a CTA share the rows' length.
+ *   k_products<UP / DOWN>    more tokens: an expert's tokens are gathered to columns, each warp has 16 rows of its own.
+ *   k_gather                 ... and the sum over a token's choices, in their order.
+ *
+ * bf16: what goes into the second product is kept as two bf16 values, the rounded one and what it leaves (16 bits).
+ */
+#include "sifar_norm_shape.cuh"
+#include "sifar_ops.cuh"
+
+namespace sifar {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kBlock = 64;                   /* bytes of a row that the four lanes of a row load at once */
+constexpr int kAhead = 4;                    /* blocks that a lane loads together: 256 bytes of a row */
+constexpr int kFew = 8;                      /* tokens that fit one instruction's columns */
+constexpr int kChunk = 512;                  /* bytes of the tokens' rows in shared memory at a time (more tokens) */
+constexpr int kChunkRow = kChunk + 64;       /* ... rows shifted by half of the banks: eight lanes read two rows' 64 bytes */
+
+struct ExpertsArgs {
+    const char *x, *gate_up, *down;
+    char *out;
+    const int *indices;
+    const float *weights;
+    char *h;                                 /* few: [active][plane][token], many: [token][choice][plane], rows of h_row bytes */
+    float *y;                                /* many: [token][choice][hidden] */
+    unsigned long long ld_x, ld_gate_up, ld_down, ld_out;    /* bytes */
+    uint32_t tokens, hidden, inter, h_row, top_k, experts;
+    int first, activation;
+    uint32_t x_row;                          /* few: bytes between the tokens' rows in shared memory */
+};
+
+/* ------------------------------------------------------------------------ */
+/* loads                                                                     */
+/* ------------------------------------------------------------------------ */
+__device__ __forceinline__ uint4 load_once(const char *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+/* 16 bytes from any element on: two aligned vectors shifted together, bytes from `left` on 0. */
+__device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
+{
+    const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;
+    const uint4 *const q = reinterpret_cast<const uint4 *>(p - sh);
+    const uint4 lo = __ldg(q);
+    uint4 hi = make_uint4(0u, 0u, 0u, 0u);
+    if (sh && left > 16u - sh) hi = __ldg(q + 1);
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    /* words first, then the bits within them */
+    if (sh & 8u) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (sh & 4u) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (sh & 3u) * 8u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+    if (left < 16u) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) w[i] = left >= 4 * i + 4 ? w[i] : left <= 4 * i ? 0u : w[i] & ((1u << (left - 4 * i) * 8u) - 1u);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+/* 16 bytes of a row of `bytes` from `at` on, zeros behind its end or without a row. */
+template <bool VEC> __device__ __forceinline__ uint4 load_row(const char *row, uint32_t at, uint32_t bytes)
+{
+    if (!row || at >= bytes) return make_uint4(0u, 0u, 0u, 0u);
+    return VEC ? load_once(row + at) : load_shifted(row + at, bytes - at);
+}
+
+__device__ __forceinline__ void multiply(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+/* One block of 16 weight rows (a lane's rows g and g + 8) with 8 tokens (the lane's: g). */
+__device__ __forceinline__ void multiply_block(float (&c)[4], const uint4 &a, const uint4 &b, const uint4 &x)
+{
+    multiply(c, a.x, b.x, a.y, b.y, x.x, x.y);
+    multiply(c, a.z, b.z, a.w, b.w, x.z, x.w);
+}
+__device__ __forceinline__ float dot4(const uint4 &a, const float4 &x, float s)
+{
+    s += __uint_as_float(a.x) * x.x; s += __uint_as_float(a.y) * x.y;
+    s += __uint_as_float(a.z) * x.z; s += __uint_as_float(a.w) * x.w;
+    return s;
+}
+
+__device__ __forceinline__ float activate(float g, int kind)
+{
+    if (kind == SIFAR_ACT_SILU) return g / (1.0f + expf(-g));
+    return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+}
+
+/* Element `col` of a row of h (and, bf16, of the row with its rest, `low` bytes on).  The last one is followed by zeros up to
+   the row's end: the second product reads whole vectors. */
+template <int DT> __device__ __forceinline__ void store_h(const ExpertsArgs &a, char *row, size_t low, uint32_t col, float v)
+{
+    using T = typename Elem<DT>::type;
+    const T hi = narrow<DT>(v);
+    reinterpret_cast<T *>(row)[col] = hi;
+    if constexpr (DT == SIFAR_BF16) reinterpret_cast<T *>(row + low)[col] = narrow<DT>(v - widen<DT>(hi));
+    if (col + 1 == a.inter)
+        for (uint32_t i = a.inter; i < a.h_row / sizeof(T); ++i) {
+            reinterpret_cast<T *>(row)[i] = (T)0;
+            if constexpr (DT == SIFAR_BF16) reinterpret_cast<T *>(row + low)[i] = (T)0;
+        }
+}
+
+/* ------------------------------------------------------------------------ */
+/* which experts                                                             */
+/* ------------------------------------------------------------------------ */
+/* The expert (0 .. experts - 1) that choice i is the token's first one of, or -1: another rank's, or its second. */
+__device__ __forceinline__ int expert_of(const ExpertsArgs &a, uint32_t i)
+{
+    const long long e = (long long)a.indices[i] - a.first;
+    if (e < 0 || e >= (long long)a.experts) return -1;
+    for (uint32_t j = i - i % a.top_k; j < i; ++j)
+        if (a.indices[j] == a.indices[i]) return -1;
+    return (int)e;
+}
+/* The weight of the token that choice i belongs to, for the choice's expert. */
+__device__ __forceinline__ float weight_of(const ExpertsArgs &a, uint32_t i)
+{
+    const uint32_t j0 = i - i % a.top_k;
+    float w = 0.0f;
+    for (uint32_t j = j0; j < j0 + a.top_k; ++j)
+        if (a.indices[j] == a.indices[i]) w += a.weights[j];
+    return w;
+}
+
+/* Keeps the numbers i of 0 .. n - 1 with on(i), in their order: put(place, i).  Returns how many.  All of the CTA, the same for
+   all; scratch: kWarps words. */
+template <typename On, typename Put>
+__device__ __forceinline__ int keep_in_order(uint32_t n, int *scratch, On on, Put put)
+{
+    int total = 0;
+    for (uint32_t i0 = 0; i0 < n; i0 += kThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const bool in = i < n && on(i);
+        const uint32_t votes = __ballot_sync(0xFFFFFFFFu, in);
+        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x / 32] = __popc(votes);
+        __syncthreads();
+        int before = total;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < (int)(threadIdx.x / 32)) before += scratch[w];
+            total += scratch[w];
+        }
+        if (in) put(before + __popc(votes & ((1u << (threadIdx.x & 31)) - 1u)), i);
+        __syncthreads();
+    }
+    return total;
+}
+
+/* The experts that have tokens, in their order: list[i] = the i-th one's number; counts[e] = its tokens.  Returns how many. */
+__device__ __forceinline__ int list_experts(const ExpertsArgs &a, int *counts, int *list, int *scratch)
+{
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kThreads) counts[e] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < a.tokens * a.top_k; i += kThreads) {
+        const int e = expert_of(a, i);
+        if (e >= 0) atomicAdd(&counts[e], 1);
+    }
+    __syncthreads();
+    return keep_in_order(a.experts, scratch, [&](uint32_t e) { return counts[e] > 0; }, [&](int at, uint32_t e) { list[at] = (int)e; });
+}
+
+/* ------------------------------------------------------------------------ */
+/* up to 8 tokens                                                            */
+/* ------------------------------------------------------------------------ */
+/* A lane's accumulators for 16 rows x 8 tokens. */
+template <int DT> struct Few;
+template <> struct Few<SIFAR_BF16> {
+    float c[4] = {};
+    __device__ __forceinline__ void store(float *red) const        /* red: 16 rows x 8 tokens */
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+        *reinterpret_cast<float2 *>(red + g * 8 + 2 * j) = make_float2(c[0], c[1]);
+        *reinterpret_cast<float2 *>(red + (g + 8) * 8 + 2 * j) = make_float2(c[2], c[3]);
+    }
+};
+template <> struct Few<SIFAR_F32> {
+    float c[2][8] = {};
+    __device__ __forceinline__ void store(float *red)
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                float v = c[r][t];
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+                if (j == (t & 3)) red[(g + 8 * r) * 8 + t] = v;
+            }
+    }
+};
+
+struct Weights { uint4 a[kAhead], b[kAhead]; };
+
+template <bool VEC> __device__ __forceinline__ void load_weights(Weights &w, const char *ra, const char *rb, uint32_t at, uint32_t bytes)
+{
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        w.a[i] = load_row<VEC>(ra, at + i * kBlock, bytes);
+        w.b[i] = load_row<VEC>(rb, at + i * kBlock, bytes);
+    }
+}
+
+/*
+ * A unit is 8 gate rows and the 8 up rows that go with them of one expert, so a product's gate and up lie 8 rows apart.
+ * Warp w takes every eighth 256 bytes of the rows; the next 256 are under way while these are multiplied, across units too.
+ */
+template <int DT, bool VEC, bool XVEC>
+__global__ void __launch_bounds__(kThreads, 2) k_up_few(const __grid_constant__ ExpertsArgs a)
+{
+    constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
+    extern __shared__ __align__(128) char smem[];                   /* tokens x x_row */
+    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_scratch[kWarps];
+    __shared__ __align__(16) float s_red[2][kWarps][16 * 8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
+    grid_wait();
+    grid_let_next_in();
+    const int active = list_experts(a, s_counts, s_list, s_scratch);
+    const uint32_t tiles = (a.inter + 7) / 8, bytes = a.hidden * es;
+    const unsigned long long units = (unsigned long long)active * tiles;
+    const uint32_t steps = (bytes + kWarps * kAhead * kBlock - 1) / (kWarps * kAhead * kBlock);
+    auto rows_of = [&](unsigned long long u, const char *&ra, const char *&rb) {
+        ra = rb = nullptr;
+        if (u >= units) return;
+        const uint32_t i = (uint32_t)(u % tiles) * 8 + g;
+        if (i >= a.inter) return;
+        const unsigned long long row = (unsigned long long)s_list[u / tiles] * 2 * a.inter + i;
+        ra = a.gate_up + row * a.ld_gate_up;
+        rb = ra + (unsigned long long)a.inter * a.ld_gate_up;
+    };
+    const uint32_t mine = warp * kAhead * kBlock + j * 16;
+    unsigned long long u = blockIdx.x;
+    const char *ra, *rb;
+    rows_of(u, ra, rb);
+    Weights next;
+    load_weights<VEC>(next, ra, rb, mine, bytes);
+
+    /* the tokens' rows, zeros behind their ends */
+    for (uint32_t i = threadIdx.x; i < a.tokens * (a.x_row / 16); i += kThreads) {
+        const uint32_t t = i / (a.x_row / 16), at = i % (a.x_row / 16) * 16;
+        const char *row = a.x + t * a.ld_x;
+        *reinterpret_cast<uint4 *>(smem + t * a.x_row + at) =
+            at >= bytes ? make_uint4(0u, 0u, 0u, 0u) : XVEC ? __ldg(reinterpret_cast<const uint4 *>(row + at)) : load_shifted(row + at, bytes - at);
+    }
+    __syncthreads();
+
+    for (int parity = 0; u < units; u += gridDim.x, parity ^= 1) {
+        Few<DT> acc;
+        for (uint32_t s = 0; s < steps; ++s) {
+            const Weights now = next;
+            const uint32_t at = s * kWarps * kAhead * kBlock + mine;
+            if (s + 1 < steps) {
+                load_weights<VEC>(next, ra, rb, at + kWarps * kAhead * kBlock, bytes);
+            } else {
+                rows_of(u + gridDim.x, ra, rb);
+                load_weights<VEC>(next, ra, rb, mine, bytes);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (at - j * 16 + i * kBlock >= bytes) break;       /* the same for all lanes */
+                if constexpr (DT == SIFAR_BF16) {
+                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                    if ((uint32_t)g < a.tokens) x = *reinterpret_cast<const uint4 *>(smem + g * a.x_row + at + i * kBlock);
+                    multiply_block(acc.c, now.a[i], now.b[i], x);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) {
+                        if ((uint32_t)t >= a.tokens) break;
+                        const float4 x = *reinterpret_cast<const float4 *>(smem + t * a.x_row + at + i * kBlock);
+                        acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
+                        acc.c[1][t] = dot4(now.b[i], x, acc.c[1][t]);
+                    }
+                }
+            }
+        }
+        acc.store(s_red[parity][warp]);
+        __syncthreads();                                            /* the other parity's sums are read by now */
+        const uint32_t i = threadIdx.x / 8, t = threadIdx.x % 8, which = (uint32_t)(u / tiles), col = (uint32_t)(u % tiles) * 8 + i;
+        if (i < 8 && t < a.tokens && col < a.inter) {
+            float gate = 0.0f, up = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) { gate += s_red[parity][w][i * 8 + t]; up += s_red[parity][w][(i + 8) * 8 + t]; }
+            float weight = 0.0f;
+            bool chosen = false;
+            for (uint32_t c = t * a.top_k; c < (t + 1) * a.top_k; ++c)
+                if ((long long)a.indices[c] - a.first == s_list[which]) { weight += a.weights[c]; chosen = true; }
+            const float v = chosen ? weight * (activate(gate, a.activation) * up) : 0.0f;
+            const size_t low = (size_t)a.tokens * a.h_row;
+            store_h<DT>(a, a.h + (which * (DT == SIFAR_BF16 ? 2 : 1) * low) + t * (size_t)a.h_row, low, col, v);
+        }
+    }
+}
+
+/*
+ * A CTA has 16 columns of the output and goes over all experts that have tokens; its warps take the 256-byte pieces of the
+ * experts' rows in turn.  HALF (bf16, up to 4 tokens): both parts of the products' values are columns of one instruction.
+ */
+template <int DT, bool VEC, bool HALF>
+__global__ void __launch_bounds__(kThreads, 2) k_down_few(const __grid_constant__ ExpertsArgs a)
+{
+    constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
+    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_scratch[kWarps];
+    __shared__ __align__(16) float s_red[kWarps][16 * 8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
+    /* the choices were complete before the kernel in front of this one let it in, so they may be read before it ends */
+    const int active = list_experts(a, s_counts, s_list, s_scratch);
+    const uint32_t bytes = a.inter * es, pieces = (bytes + kAhead * kBlock - 1) / (kAhead * kBlock), items = (uint32_t)active * pieces;
+    const uint32_t col = blockIdx.x * 16 + g;
+    auto load = [&](Weights &w, uint32_t item) {
+        const char *ra = nullptr, *rb = nullptr;
+        if (item < items) {
+            const unsigned long long row = (unsigned long long)s_list[item / pieces] * a.hidden + col;
+            if (col < a.hidden) ra = a.down + row * a.ld_down;
+            if (col + 8 < a.hidden) rb = a.down + (row + 8) * a.ld_down;
+        }
+        load_weights<VEC>(w, ra, rb, item % pieces * (kAhead * kBlock) + j * 16, bytes);
+    };
+    Weights next;
+    load(next, warp);
+    grid_wait();
+    grid_let_next_in();
+    Few<DT> acc;
+    for (uint32_t item = warp; item < items; item += kWarps) {
+        const Weights now = next;
+        load(next, item + kWarps);
+        const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + j * 16;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const uint32_t here = at + i * kBlock;
+            if (here - j * 16 >= bytes) break;
+            const bool in = here < a.h_row;                         /* rows of h are filled up with zeros to 16 bytes */
+            if constexpr (DT == SIFAR_BF16) {
+                const char *const h = a.h + (size_t)which * 2 * a.tokens * a.h_row + here;
+                const uint32_t t = HALF ? g & 3 : g;
+                const size_t low = (size_t)a.tokens * a.h_row;
+                uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
+                if (in && t < a.tokens) {
+                    x = __ldcg(reinterpret_cast<const uint4 *>(h + t * a.h_row + (HALF && g >= 4 ? low : 0)));
+                    if (!HALF) y = __ldcg(reinterpret_cast<const uint4 *>(h + t * a.h_row + low));
+                }
+                multiply_block(acc.c, now.a[i], now.b[i], x);
+                if (!HALF) multiply_block(acc.c, now.a[i], now.b[i], y);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    if ((uint32_t)t >= a.tokens || !in) break;
+                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(a.h + ((size_t)which * a.tokens + t) * a.h_row + here));
+                    acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
+                    acc.c[1][t] = dot4(now.b[i], x, acc.c[1][t]);
+                }
+            }
+        }
+    }
+    acc.store(s_red[warp]);
+    __syncthreads();
+    const uint32_t r = threadIdx.x % 16, t = threadIdx.x / 16;
+    if (t < a.tokens && blockIdx.x * 16 + r < a.hidden) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += s_red[w][r * 8 + t];
+        if (HALF) {
+            float low = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) low += s_red[w][r * 8 + t + 4];
+            v += low;
+        }
+        reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out)[blockIdx.x * 16 + r] = narrow<DT>(v);
+    }
+}
+
+/* ------------------------------------------------------------------------ */
+/* more tokens                                                               */
+/* ------------------------------------------------------------------------ */
+/* Columns of a pass over an expert's rows, and instructions' columns of eight that hold them: bf16 values of the second product
+   come as two parts, a column each. */
+template <int DT, bool DOWN> struct Pass {
+    static constexpr int parts = DT == SIFAR_BF16 && DOWN ? 2 : 1;
+    static constexpr int groups = DT == SIFAR_BF16 ? 8 : 4;
+    static constexpr int tokens = groups * 8 / parts;
+    static constexpr int shared = 2 * groups * 8 * kChunkRow;
+};
+
+/*
+ * A unit is 128 rows of one expert with up to Pass::tokens of its tokens: 64 gate and 64 up rows (UP), or 128 columns of the
+ * output (DOWN).  The columns' rows come through shared memory 512 bytes at a time, the next ones under way; weights as
+ * above, 256 bytes ahead.
+ */
+template <int DT, bool DOWN, bool VEC, bool XVEC>
+__global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant__ ExpertsArgs a)
+{
+    using P = Pass<DT, DOWN>;
+    constexpr int es = DT == SIFAR_BF16 ? 2 : 4, G = P::groups / P::parts;
+    extern __shared__ __align__(128) char smem[];                   /* 2 x columns x kChunkRow */
+    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_before[SIFAR_ROUTE_MAX_EXPERTS + 1];
+    __shared__ int s_scratch[kWarps];
+    __shared__ uint16_t s_slots[SIFAR_EXPERTS_MAX_TOKENS];          /* choices of the expert's tokens: below 2^13 */
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
+    if (!DOWN) grid_wait();
+    grid_let_next_in();
+    const int active = list_experts(a, s_counts, s_list, s_scratch);
+    const uint32_t rows = DOWN ? a.hidden : a.inter, per = DOWN ? 128u : 64u, tiles = (rows + per - 1) / per;
+    const uint32_t bytes = (DOWN ? a.inter : a.hidden) * es, steps = (bytes + kChunk - 1) / kChunk;
+    /* passes before each of them */
+    if (threadIdx.x == 0) {
+        int sum = 0;
+        for (int i = 0; i < active; ++i) { s_before[i] = sum; sum += (s_counts[s_list[i]] + P::tokens - 1) / P::tokens; }
+        s_before[active] = sum;
+    }
+    __syncthreads();
+    const unsigned long long units = (unsigned long long)s_before[active] * tiles;
+    const unsigned long long begin = units * blockIdx.x / gridDim.x, end = units * (blockIdx.x + 1) / gridDim.x;
+
+    struct Unit { uint32_t which, tile, pass; };
+    auto unit = [&](unsigned long long u) {
+        int lo = 0, hi = active - 1;                                /* the last expert with s_before * tiles <= u */
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if ((unsigned long long)s_before[mid] * tiles <= u) lo = mid; else hi = mid - 1;
+        }
+        const uint32_t rest = (uint32_t)(u - (unsigned long long)s_before[lo] * tiles), passes = s_before[lo + 1] - s_before[lo];
+        return Unit{(uint32_t)lo, rest / passes, rest % passes};
+    };
+    auto rows_of = [&](unsigned long long u, const char *&ra, const char *&rb) {
+        ra = rb = nullptr;
+        if (u >= end) return;
+        const Unit t = unit(u);
+        const unsigned long long e = (unsigned long long)s_list[t.which];
+        if (DOWN) {
+            const uint32_t r = t.tile * 128 + warp * 16 + g;
+            if (r < a.hidden) ra = a.down + (e * a.hidden + r) * a.ld_down;
+            if (r + 8 < a.hidden) rb = a.down + (e * a.hidden + r + 8) * a.ld_down;
+        } else {
+            const uint32_t r = t.tile * 64 + warp * 8 + g;
+            if (r >= a.inter) return;
+            ra = a.gate_up + (e * 2 * a.inter + r) * a.ld_gate_up;
+            rb = ra + (unsigned long long)a.inter * a.ld_gate_up;
+        }
+    };
+
+    const char *ra, *rb;
+    rows_of(begin, ra, rb);
+    Weights next;
+    load_weights<VEC>(next, ra, rb, j * 16, bytes);
+    if (DOWN) grid_wait();                                          /* what was loaded so far no kernel writes */
+
+    uint32_t listed = 0xFFFFFFFFu, in_expert = 0;
+    for (unsigned long long u = begin; u < end; ++u) {
+        const Unit at = unit(u);
+        if (at.which != listed) {
+            __syncthreads();
+            /* in the order of the choices: all CTAs cut the same passes */
+            in_expert = (uint32_t)keep_in_order(a.tokens * a.top_k, s_scratch, [&](uint32_t i) { return expert_of(a, i) == s_list[at.which]; },
+                                                [&](int to, uint32_t i) { s_slots[to] = (uint16_t)i; });
+            listed = at.which;
+        }
+        const uint32_t n = min(in_expert - at.pass * P::tokens, (uint32_t)P::tokens), groups = (n + 7) / 8;
+        const uint16_t *const slots = s_slots + at.pass * P::tokens;
+        /* column c: token c of the pass; its second part lies G * 8 columns on */
+        auto fetch = [&](uint32_t step, int buffer) {
+            char *const to = smem + buffer * (P::groups * 8 * kChunkRow);
+            for (uint32_t i = threadIdx.x; i < n * P::parts * (kChunk / 16); i += kThreads) {
+                const uint32_t c = i / (kChunk / 16), piece = i % (kChunk / 16) * 16, off = step * kChunk + piece;
+                const uint32_t token = c % n, part = c / n;
+                const char *row = DOWN ? a.h + ((size_t)slots[token] * P::parts + part) * a.h_row : a.x + (slots[token] / a.top_k) * a.ld_x;
+                char *const dst = to + (part * (G * 8) + token) * kChunkRow + piece;
+                const uint32_t end_of = DOWN ? a.h_row : bytes;
+                if (DOWN || XVEC) {
+                    const uint32_t take = off < end_of ? 16u : 0u;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(row + (take ? off : 0u)), "r"(take) : "memory");
+                } else {
+                    *reinterpret_cast<uint4 *>(dst) = off < end_of ? load_shifted(row + off, end_of - off) : make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        float acc[P::groups][DT == SIFAR_BF16 ? 4 : 16];
+#pragma unroll
+        for (int q = 0; q < P::groups; ++q)
+#pragma unroll
+            for (int i = 0; i < (DT == SIFAR_BF16 ? 4 : 16); ++i) acc[q][i] = 0.0f;
+        fetch(0, 0);
+        for (uint32_t s = 0; s < steps; ++s) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();                                        /* chunk s is there, chunk s - 1 has been read */
+            if (s + 1 < steps) fetch(s + 1, (s + 1) & 1);
+            const char *const cols = smem + (s & 1) * (P::groups * 8 * kChunkRow);
+#pragma unroll
+            for (int half = 0; half < kChunk / (kAhead * kBlock); ++half) {
+                const uint32_t off = s * kChunk + half * kAhead * kBlock;
+                const Weights now = next;
+                if (off + kAhead * kBlock < steps * kChunk) {
+                    load_weights<VEC>(next, ra, rb, off + kAhead * kBlock + j * 16, bytes);
+                } else {
+                    rows_of(u + 1, ra, rb);
+                    load_weights<VEC>(next, ra, rb, j * 16, bytes);
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    if (off + i * kBlock >= bytes) break;
+                    const char *const x = cols + half * kAhead * kBlock + i * kBlock + j * 16;
+                    if constexpr (DT == SIFAR_BF16) {
+#pragma unroll
+                        for (int q = 0; q < G; ++q) {
+                            if ((uint32_t)q >= groups) break;
+                            multiply_block(acc[q], now.a[i], now.b[i], *reinterpret_cast<const uint4 *>(x + (q * 8 + g) * kChunkRow));
+                            if (P::parts == 2)
+                                multiply_block(acc[q + P::groups - G], now.a[i], now.b[i], *reinterpret_cast<const uint4 *>(x + ((q + G) * 8 + g) * kChunkRow));
+                        }
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < G; ++q) {
+                            if ((uint32_t)q >= groups) break;
+#pragma unroll
+                            for (int t = 0; t < 8; ++t) {
+                                const float4 v = *reinterpret_cast<const float4 *>(x + (q * 8 + t) * kChunkRow);
+                                acc[q][t] = dot4(now.a[i], v, acc[q][t]);
+                                acc[q][8 + t] = dot4(now.b[i], v, acc[q][8 + t]);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+        __syncthreads();                                            /* the last chunk has been read */
+        /* rows g (first) and g + 8 (second) of the warp's 16, token t of the pass */
+        auto put = [&](uint32_t t, float first, float second) {
+            if (t >= n) return;
+            const uint32_t slot = slots[t];
+            if (DOWN) {
+                const uint32_t r = at.tile * 128 + warp * 16 + g;
+                float *const y = a.y + (size_t)slot * a.hidden + r;
+                if (r < a.hidden) y[0] = first;
+                if (r + 8 < a.hidden) y[8] = second;
+            } else {
+                const uint32_t r = at.tile * 64 + warp * 8 + g;
+                if (r >= a.inter) return;
+                const float v = weight_of(a, slot) * (activate(first, a.activation) * second);
+                store_h<DT>(a, a.h + (size_t)slot * (DT == SIFAR_BF16 ? 2 : 1) * a.h_row, a.h_row, r, v);
+            }
+        };
+#pragma unroll
+        for (int q = 0; q < G; ++q) {
+            if ((uint32_t)q >= groups) break;
+            if constexpr (DT == SIFAR_BF16) {
+                if (P::parts == 2) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[q][i] += acc[q + P::groups - G][i];
+                }
+                put(q * 8 + 2 * j, acc[q][0], acc[q][2]);
+                put(q * 8 + 2 * j + 1, acc[q][1], acc[q][3]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    float v = acc[q][t], w = acc[q][8 + t];
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1); w += __shfl_xor_sync(0xFFFFFFFFu, w, 1);
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 2); w += __shfl_xor_sync(0xFFFFFFFFu, w, 2);
+                    if (j == (t & 3)) put(q * 8 + t, v, w);
+                }
+            }
+        }
+    }
+}
+
+/* out_t = the sum over its choices here, in their order. */
+template <int DT>
+__global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ ExpertsArgs a)
+{
+    __shared__ int s_slot[SIFAR_ROUTE_MAX_TOP_K];
+    const uint32_t t = blockIdx.y, c0 = (blockIdx.x * kThreads + threadIdx.x) * 4;
+    if (threadIdx.x < a.top_k) s_slot[threadIdx.x] = expert_of(a, t * a.top_k + threadIdx.x);
+    __syncthreads();
+    grid_wait();
+    grid_let_next_in();
+    if (c0 >= a.hidden) return;
+    float v[4] = {};
+    const bool vec = a.hidden % 4 == 0;
+#pragma unroll 4
+    for (uint32_t k = 0; k < a.top_k; ++k) {
+        if (s_slot[k] < 0) continue;
+        const float *const y = a.y + (size_t)(t * a.top_k + k) * a.hidden + c0;
+        if (vec) {
+            const float4 w = __ldcg(reinterpret_cast<const float4 *>(y));
+            v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c0 + i < a.hidden) v[i] += __ldcg(y + i);
+        }
+    }
+    auto *const out = reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out) + c0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c0 + i < a.hidden) out[i] = narrow<DT>(v[i]);
+}
+
+/* ------------------------------------------------------------------------ */
+/* host                                                                      */
+/* ------------------------------------------------------------------------ */
+struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, bytes; };
+
+constexpr size_t kFewShared = 100 * 1024;    /* the tokens' rows in shared memory: two CTAs of 8 warps per SM */
+
+static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan &p)
+{
+    if (!g) { set_error("%s: no argument block", fn); return SIFAR_ERR_INVALID; }
+    if ((g->dtype != SIFAR_BF16 && g->dtype != SIFAR_F32) || g->experts < 1 || g->experts > SIFAR_ROUTE_MAX_EXPERTS || g->top_k < 1 ||
+        g->top_k > SIFAR_ROUTE_MAX_TOP_K || (g->activation != SIFAR_ACT_SILU && g->activation != SIFAR_ACT_GELU)) {
+        set_error("%s: need dtype in {0,1}, 1 <= experts <= %d, 1 <= top_k <= %d and a known activation", fn, (int)SIFAR_ROUTE_MAX_EXPERTS, (int)SIFAR_ROUTE_MAX_TOP_K);
+        return SIFAR_ERR_INVALID;
+    }
+    if (g->tokens > SIFAR_EXPERTS_MAX_TOKENS || g->hidden < 1 || g->hidden > SIFAR_EXPERTS_MAX_COLS || g->inter < 1 || g->inter > SIFAR_EXPERTS_MAX_COLS) {
+        set_error("%s: need tokens of at most %d, hidden and inter of 1 .. %d", fn, (int)SIFAR_EXPERTS_MAX_TOKENS, (int)SIFAR_EXPERTS_MAX_COLS);
+        return SIFAR_ERR_INVALID;
+    }
+    const size_t es = elem_size(g->dtype), T = g->tokens, choices = T * (size_t)g->top_k, parts = g->dtype == SIFAR_BF16 ? 2 : 1;
+    /* a multiple of 128 bytes and 64 more: two rows' pieces lie in different banks */
+    p.x_row = (uint32_t)((g->hidden * es + 127) / 128 * 128 + 64);
+    p.few = T <= (size_t)kFew && T * p.x_row <= kFewShared;
+    p.h_row = (uint32_t)((g->inter * es + 15) / 16 * 16);
+    const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
+    p.h_bytes = ((p.few ? most * T : choices) * parts * p.h_row + 15) / 16 * 16;
+    p.bytes = p.h_bytes + (p.few ? 0 : choices * g->hidden * sizeof(float));
+    return SIFAR_OK;
+}
+
+template <typename... P, typename... A>
+static cudaError_t launch_shared(void (*kernel)(P...), dim3 grid, size_t shared, cudaStream_t stream, const A &...args)
+{
+    if (shared > 24 * 1024)                  /* 48 KB less what the kernels declare themselves */
+        if (cudaError_t e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
+    return launch_op(kernel, grid, dim3(kThreads), 1, shared, stream, args...);
+}
+
+template <int DT>
+static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, const ExpertsArgs &a)
+{
+    const dim3 grid(2 * kSms);
+    cudaError_t e;
+    if (p.few) {
+        const size_t shared = a.tokens * p.x_row;
+        e = !gu_vec ? launch_shared(k_up_few<DT, false, false>, grid, shared, stream, a)
+            : x_vec ? launch_shared(k_up_few<DT, true, true>, grid, shared, stream, a) : launch_shared(k_up_few<DT, true, false>, grid, shared, stream, a);
+        if (e) return e;
+        const dim3 columns((a.hidden + 15) / 16);
+        if (DT == SIFAR_BF16 && a.tokens <= 4)
+            return dn_vec ? launch_shared(k_down_few<DT, true, DT == SIFAR_BF16>, columns, 0, stream, a) : launch_shared(k_down_few<DT, false, DT == SIFAR_BF16>, columns, 0, stream, a);
+        return dn_vec ? launch_shared(k_down_few<DT, true, false>, columns, 0, stream, a) : launch_shared(k_down_few<DT, false, false>, columns, 0, stream, a);
+    }
+    e = !gu_vec ? launch_shared(k_products<DT, false, false, false>, grid, Pass<DT, false>::shared, stream, a)
+        : x_vec ? launch_shared(k_products<DT, false, true, true>, grid, Pass<DT, false>::shared, stream, a)
+                : launch_shared(k_products<DT, false, true, false>, grid, Pass<DT, false>::shared, stream, a);
+    if (e) return e;
+    e = dn_vec ? launch_shared(k_products<DT, true, true, true>, grid, Pass<DT, true>::shared, stream, a)
+               : launch_shared(k_products<DT, true, false, true>, grid, Pass<DT, true>::shared, stream, a);
+    if (e) return e;
+    return launch_shared(k_gather<DT>, dim3((a.hidden + 4 * kThreads - 1) / (4 * kThreads), a.tokens), 0, stream, a);
+}
+
+}  /* namespace sifar */
+
+using namespace sifar;
+
+extern "C" size_t sifar_experts_workspace(const sifar_experts_args *g)
+{
+    ExpertsPlan p;
+    return plan_experts("sifar_experts_workspace", g, p) == SIFAR_OK ? p.bytes : 0;
+}
+
+extern "C" int sifar_experts(const sifar_experts_args *g, void *stream)
+{
+    static const char *fn = "sifar_experts";
+    ExpertsPlan p;
+    if (int rc = plan_experts(fn, g, p)) return rc;
+    if (g->tokens == 0) return SIFAR_OK;
+    if (!g->x || !g->indices || !g->weights || !g->gate_up || !g->down || !g->out) {
+        set_error("%s: x, indices, weights, gate_up, down and out are needed", fn);
+        return SIFAR_ERR_INVALID;
+    }
+    if (!g->workspace || (uintptr_t)g->workspace % 16 || g->workspace_bytes < p.bytes) {
+        set_error("%s: needs %zu bytes of workspace on a 16-byte boundary", fn, p.bytes);
+        return SIFAR_ERR_INVALID;
+    }
+    const size_t es = elem_size(g->dtype), T = g->tokens, H = g->hidden, I = g->inter, E = (size_t)g->experts, choices = T * (size_t)g->top_k;
+    const auto ld = [](size_t given, size_t cols) { return given ? given : cols; };
+    const RowArray all[] = {
+        RowArray{"x", g->x, T, H, ld(g->ld_x, H), es, false},
+        RowArray{"indices", g->indices, 1, choices, choices, sizeof(int), false},
+        RowArray{"weights", g->weights, 1, choices, choices, sizeof(float), false},
+        RowArray{"gate_up", g->gate_up, E * 2 * I, H, ld(g->ld_gate_up, H), es, false},
+        RowArray{"down", g->down, E * H, I, ld(g->ld_down, I), es, false},
+        RowArray{"out", g->out, T, H, ld(g->ld_out, H), es, true},
+        RowArray{"workspace", g->workspace, 1, p.bytes, p.bytes, 1, true},
+    };
+    if (int rc = check_arrays(fn, all, 7)) return rc;
+    ExpertsArgs a;
+    a.x = (const char *)g->x; a.gate_up = (const char *)g->gate_up; a.down = (const char *)g->down; a.out = (char *)g->out;
+    a.indices = g->indices; a.weights = g->weights;
+    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes);
+    a.ld_x = all[0].ld * es; a.ld_gate_up = all[3].ld * es; a.ld_down = all[4].ld * es; a.ld_out = all[5].ld * es;
+    a.tokens = (uint32_t)T; a.hidden = (uint32_t)H; a.inter = (uint32_t)I; a.h_row = p.h_row; a.top_k = (uint32_t)g->top_k;
+    a.experts = (uint32_t)E; a.first = g->first_expert; a.activation = g->activation; a.x_row = p.x_row;
+    const bool gu = rows_aligned16(all[3]) && H * es % 16 == 0, dn = rows_aligned16(all[4]) && I * es % 16 == 0, xv = rows_aligned16(all[0]) && H * es % 16 == 0;
+    const cudaError_t err = g->dtype == SIFAR_BF16 ? launch_experts<SIFAR_BF16>(p, gu, dn, xv, (cudaStream_t)stream, a)
+                                                   : launch_experts<SIFAR_F32>(p, gu, dn, xv, (cudaStream_t)stream, a);
+    SIFAR_CUDA(err);
+    return SIFAR_OK;
+}
