@@ -1,12 +1,12 @@
 /*
  * sifar_attention.cu - attention of one new token per sequence over a paged cache, split over the cache's length.
  *
- * An item is a key head of a sequence with up to 16 (binary32: 8) of the query heads that read it.  All items' tiles of
- * 64 tokens in a row are cut into equal shares, one per CTA, whatever the lengths; an item that ends up with several CTAs is
- * put together by a second kernel from their maxima, sums and weighted values.
- *
- * A warp takes 16 tokens at a time (a strip) through a ring of its own in shared memory, filled by asynchronous
- * 16-byte copies two strips ahead; warps of a CTA meet only when an item is done.
+ * An item is a key head of a sequence with up to 16 (binary32: 8) of the query heads that read it.  All items' strips of 16
+ * tokens in a row are cut into equal shares, one per warp, whatever the lengths: a warp goes through the end of one item, some
+ * whole ones and the start of another without meeting any other warp.  Its strips come through a ring of its own in shared
+ * memory, filled by asynchronous 16-byte copies two strips ahead, across items too; an item's queries come the same way, before its strips.  An item that several warps had is put
+ * together by a second kernel from their maxima, sums and weighted values; where a CTA's warps all have the same item they
+ * join their parts first.
  */
 #include "sifar_cache.cuh"
 #include "sifar_norm_shape.cuh"
@@ -14,11 +14,13 @@
 namespace sifar {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kTile = 64;                    /* tokens; what the shares are counted in */
+constexpr int kItemCost = 1;                 /* what an item's start and end count as, in strips */
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-/* Where a split item lies in the workspace: partials of CTAs first .. last, in the order of the tokens. */
-struct Split { int sequence, kv_head, chunk, first, last, slot, pad[2]; };       /* slot of `first`'s partial; first < 0: none */
+/* Where a split item lies in the workspace: partials of warps first .. last, in the order of the tokens. */
+struct Split { int sequence, item, first, last, slot, one0, one1, pad; };
+/* slot: of `first`'s partial, 0 of the others; first < 0: none.  Warps one0 .. one1 - 1 are whole CTAs that left one partial each, in
+   the place of their first warp. */
 
 struct AttentionArgs {
     const char *q, *k, *v;
@@ -26,12 +28,13 @@ struct AttentionArgs {
     float *lse;
     const int *lengths;
     Pages pages;
-    Split *splits;                           /* one per CTA */
-    float *partial;                          /* CTA x 2 partials */
+    Split *splits;                           /* one per warp */
+    float *partial;                          /* warp x 2 partials */
     unsigned long long ld_q, ld_out;         /* bytes */
     uint32_t sequences, window, limit;       /* limit = max_pages * page_size */
     uint32_t heads, kv_heads, group, chunks, rows, dim;   /* rows = query heads of an item, chunks of them per key head */
     float scale;                             /* times log2(e) */
+    bool q_vec, out_vec;                     /* rows of q in 16-byte pieces; rows of out in pieces of four elements */
 };
 
 /* Floats of a partial: rows x dim_pad values, rows maxima, rows sums; the next one starts on 16 bytes again. */
@@ -43,28 +46,63 @@ __device__ __forceinline__ void visible(const AttentionArgs &a, uint32_t s, uint
     hi = (uint32_t)min(max(a.lengths[s], 0), (int)a.limit);
     lo = a.window && hi > a.window ? hi - a.window : 0u;
 }
-__device__ __forceinline__ uint32_t tiles_of(const AttentionArgs &a, uint32_t s)
+template <int TOKENS> __device__ __forceinline__ uint32_t strips_of(uint32_t lo, uint32_t hi)
 {
-    uint32_t lo, hi;
-    visible(a, s, lo, hi);
-    return max(1u, (hi - lo + kTile - 1) / kTile);       /* an empty sequence has an item too: its zeros */
+    return max(1u, (hi - lo + TOKENS - 1) / TOKENS);     /* an empty sequence has an item too: its zeros */
 }
 
-/* Tile number `at` in the row of all items' tiles: which sequence, and how many of its items' tiles lie before. */
-struct Place { unsigned long long total, begin, end; uint32_t sequence; unsigned long long before; };
+/* A quotient that mostly fits 32 bits. */
+__device__ __forceinline__ unsigned long long quotient(unsigned long long n, uint32_t d)
+{
+    return n >> 32 ? n / d : (unsigned long long)((uint32_t)n / d);
+}
+
+/* Where in the row of all items' strips (each followed by kItemCost places without one) a warp is. */
+template <int TOKENS> struct Cursor {
+    unsigned long long at;                   /* place in the row */
+    uint32_t sequence, item, strip;          /* item: key head and chunk of its query heads */
+    uint32_t lo, hi, strips;                 /* of the sequence */
+
+    __device__ __forceinline__ void enter(const AttentionArgs &a)
+    {
+        lo = hi = 0;
+        if (sequence < a.sequences) visible(a, sequence, lo, hi);
+        strips = strips_of<TOKENS>(lo, hi);
+    }
+    /* Whether the next place is another item's. */
+    __device__ __forceinline__ bool advance(const AttentionArgs &a, uint32_t items)
+    {
+        ++at;
+        if (++strip < strips) return false;
+        at += kItemCost;
+        strip = 0;
+        if (++item < items) return true;
+        item = 0;
+        ++sequence;
+        enter(a);
+        return true;
+    }
+};
+
+/* The row, this CTA's part of it and where its warps' shares begin. */
+struct Shares { unsigned long long total, share; };
 
 /*
- * The share of this CTA and the sequence that it begins in.  Every thread adds up the tiles of a run of sequences; the
- * one whose run holds the share's begin walks it.
+ * Every thread adds up the places of a run of sequences; the one whose run holds the begin of a warp's share walks it.
  */
-__device__ __forceinline__ Place find_share(const AttentionArgs &a, unsigned long long *s_sum, Place *s_place)
+template <int TOKENS>
+__device__ __forceinline__ Shares find_shares(const AttentionArgs &a, unsigned long long *s_sum, Cursor<TOKENS> *s_start)
 {
-    const uint32_t run = (a.sequences + kThreads - 1) / kThreads, s0 = threadIdx.x * run, s1 = min(a.sequences, s0 + run);
-    const unsigned long long items = (unsigned long long)a.kv_heads * a.chunks;
+    const uint32_t run = (a.sequences + kThreads - 1) / kThreads, s0 = min(a.sequences, threadIdx.x * run), s1 = min(a.sequences, s0 + run);
+    const uint32_t items = a.kv_heads * a.chunks;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    auto places = [&](uint32_t s) {
+        uint32_t lo, hi;
+        visible(a, s, lo, hi);
+        return (unsigned long long)(strips_of<TOKENS>(lo, hi) + kItemCost) * items;
+    };
     unsigned long long mine = 0;
-    for (uint32_t s = s0; s < s1; ++s) mine += tiles_of(a, s);
-    mine *= items;
+    for (uint32_t s = s0; s < s1; ++s) mine += places(s);
     unsigned long long sum = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -73,25 +111,40 @@ __device__ __forceinline__ Place find_share(const AttentionArgs &a, unsigned lon
     }
     if (lane == 31) s_sum[warp] = sum;
     __syncthreads();
-    unsigned long long before = 0, total = 0;
+    unsigned long long before = 0;
+    Shares r{0, 0};
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) before += s_sum[w];
-        total += s_sum[w];
+        r.total += s_sum[w];
     }
     before += sum - mine;
-    const unsigned long long share = (total + gridDim.x - 1) / gridDim.x, begin = min(total, share * blockIdx.x), end = min(total, begin + share);
-    if (begin < end && begin >= before && begin < before + mine) {
-        Place p{total, begin, end, s0, before};
-        for (; p.sequence < s1; ++p.sequence) {
-            const unsigned long long t = tiles_of(a, p.sequence) * items;
-            if (begin < p.before + t) break;
-            p.before += t;
+    r.share = quotient(r.total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const unsigned long long begin = r.share * (blockIdx.x * kWarps + w);
+        if (begin < before || begin >= before + mine) continue;
+        Cursor<TOKENS> c;
+        unsigned long long here = before;
+        for (c.sequence = s0; c.sequence + 1 < s1; ++c.sequence) {
+            const unsigned long long n = places(c.sequence);
+            if (begin < here + n) break;
+            here += n;
         }
-        *s_place = p;
+        c.enter(a);
+        c.item = (uint32_t)quotient(begin - here, c.strips + kItemCost);
+        c.strip = (uint32_t)(begin - here - (unsigned long long)c.item * (c.strips + kItemCost));
+        c.at = begin;
+        if (c.strip >= c.strips) {           /* between two items: on to the next */
+            c.at += c.strips + kItemCost - c.strip - 1;
+            c.strip = c.strips;
+            c.at -= kItemCost;
+            c.advance(a, items);
+        }
+        s_start[w] = c;
     }
     __syncthreads();
-    return begin < end ? *s_place : Place{total, begin, end, 0, 0};
+    return r;
 }
 
 __device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -113,7 +166,7 @@ __device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t 
 }
 __device__ __forceinline__ void multiply(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 /* Two values as bf16, the first in the low half, and what that leaves of them, as bf16 again. */
@@ -192,6 +245,38 @@ __device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int st
     }
 }
 
+/* Issues the copies of an item's queries, into the place of a strip's keys: row r of them where token r's key would lie. */
+template <int DT, int DP>
+__device__ __forceinline__ void fetch_queries(const AttentionArgs &a, char *ring, int stage, const char *q, uint32_t rows)
+{
+    using R = Ring<DT, DP>;
+    char *const to = ring + stage * 2 * R::strip;
+    const uint32_t lane = threadIdx.x & 31;
+    if (a.q_vec) {
+        const uint32_t pieces = a.dim * R::es / 16;
+#pragma unroll 4
+        for (uint32_t i = lane; i < (R::tokens > 8 ? 16u : 8u) * R::chunks; i += 32) {
+            const uint32_t r = i / R::chunks, piece = i % R::chunks;
+            const bool there = r < rows && piece < pieces;
+            copy16(shared_at(to + r * R::row + R::place(r, piece) * 16), there ? q + (size_t)r * a.dim * R::es + piece * 16 : a.q, there ? 16u : 0u);
+        }
+    } else {
+        using T = typename Elem<DT>::type;
+#pragma unroll 4
+        for (uint32_t i = lane; i < (R::tokens > 8 ? 16u : 8u) * DP; i += 32) {
+            const uint32_t r = i / DP, d = i % DP;
+            *reinterpret_cast<T *>(to + r * R::row + R::place(r, d * R::es / 16) * 16 + d * R::es % 16) =
+                r < rows && d < a.dim ? reinterpret_cast<const T *>(q)[(size_t)r * a.dim + d] : (T)0;
+        }
+    }
+}
+
+/* A maximum of -infinity says that there is nothing; NaN scores alone leave that too, but a sum of NaN. */
+__device__ __forceinline__ float top_of(float top, float sum) { return sum != sum ? NAN : top; }
+
+/* Where four values of a row lie when a state is left in shared memory: rows are shifted against one another by pieces. */
+template <int DP> __device__ __forceinline__ int value_place(int row, int piece) { return row * DP + ((piece ^ (row & 7)) * 4); }
+
 /* ------------------------------------------------------------------------ */
 /* what a warp holds of an item                                              */
 /* ------------------------------------------------------------------------ */
@@ -207,27 +292,31 @@ template <int DP, int ROWS> struct StateBf16 {
     float o[DP / 8][4];
     float m[H], l[H];                               /* l: this lane's columns */
 
-    __device__ __forceinline__ void begin(const AttentionArgs &a, const char *q_row, uint32_t rows, const float *)
+    __device__ __forceinline__ void clear()
     {
-        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-            m[h] = -INFINITY; l[h] = 0.0f;
-            const uint32_t row = g + 8 * h;
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const uint32_t d = i * 16 + x * 8 + 2 * j;
-                    const uint16_t *p = reinterpret_cast<const uint16_t *>(q_row) + row * a.dim + d;
-                    uint32_t w = 0;
-                    if (row < rows && d < a.dim) w = p[0];
-                    if (row < rows && d + 1 < a.dim) w |= (uint32_t)p[1] << 16;
-                    q[i][x * H + h] = w;
-                }
-        }
+        for (int h = 0; h < H; ++h) { m[h] = -INFINITY; l[h] = 0.0f; }
 #pragma unroll
         for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
+    }
+    /* From the queries' place in the ring. */
+    __device__ __forceinline__ void begin(const char *ring, int stage, float *)
+    {
+        const int lane = threadIdx.x & 31, row = H == 1 ? lane & 7 : lane & 15;
+        const uint32_t qs = shared_at(ring + stage * 2 * R::strip);
+        clear();
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            if constexpr (H == 1) {
+                /* two blocks of 16 columns at a time: rows 0 .. 7 of four pieces */
+                if (i % 2) continue;
+                uint32_t b[4];
+                load_matrices(b, qs + row * R::row + R::place(row, 2 * i + (lane >> 3)) * 16);
+                q[i][0] = b[0]; q[i][1] = b[1]; q[i + 1][0] = b[2]; q[i + 1][1] = b[3];
+            } else {
+                load_matrices(q[i], qs + row * R::row + R::place(row, 2 * i + (lane >> 4)) * 16);
+            }
+        }
     }
 
     /* seen: bit t set where token t of the strip counts */
@@ -235,21 +324,19 @@ template <int DP, int ROWS> struct StateBf16 {
     {
         const int lane = threadIdx.x & 31, j = lane & 3;
         const uint32_t ks = shared_at(ring + stage * 2 * R::strip), vs = ks + R::strip;
-        float s[2][4] = {};
+        float s[2][4] = {}, s2[2][4] = {};                          /* two chains of sums each */
         {
             const int row = (lane & 7) + ((lane >> 4) & 1) * 8, half = (lane >> 3) & 1;
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
                 uint32_t b[4];
                 load_matrices(b, ks + row * R::row + R::place(row, 2 * i + half) * 16);
-                if (H == 1) {
-                    multiply(s[0], q[i][0], 0u, q[i][1], 0u, b[0], b[1]);
-                    multiply(s[1], q[i][0], 0u, q[i][1], 0u, b[2], b[3]);
-                } else {
-                    multiply(s[0], q[i][0], q[i][H - 1], q[i][H], q[i][2 * H - 1], b[0], b[1]);
-                    multiply(s[1], q[i][0], q[i][H - 1], q[i][H], q[i][2 * H - 1], b[2], b[3]);
-                }
+                float (&c)[2][4] = i & 1 ? s2 : s;
+                multiply(c[0], q[i][0], H == 1 ? 0u : q[i][H - 1], q[i][H], H == 1 ? 0u : q[i][2 * H - 1], b[0], b[1]);
+                multiply(c[1], q[i][0], H == 1 ? 0u : q[i][H - 1], q[i][H], H == 1 ? 0u : q[i][2 * H - 1], b[2], b[3]);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { s[0][i] += s2[0][i]; s[1][i] += s2[1][i]; }
         }
         float keep[H];
         uint32_t p[H][2], rest[H][2];
@@ -302,25 +389,19 @@ template <int DP, int ROWS> struct StateBf16 {
         }
     }
 
-    /* The warp's part of the item: `values` rows x DP, then ROWS maxima, ROWS sums. */
-    __device__ __forceinline__ void leave(float *values, float *top, float *sum)
+    /* Values (rows x DP, pieces of four in changed places), maxima and sums into shared memory. */
+    __device__ __forceinline__ void leave(float *values, float *tops, float *sums)
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-            float t = l[h];
-            t += __shfl_xor_sync(0xFFFFFFFFu, t, 1);
-            t += __shfl_xor_sync(0xFFFFFFFFu, t, 2);
-            if (j == 0) { top[g + 8 * h] = m[h]; sum[g + 8 * h] = t; }
-        }
+            l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 1);
+            l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 2);
+            if (j == 0) { tops[g + 8 * h] = top_of(m[h], l[h]); sums[g + 8 * h] = l[h]; }
 #pragma unroll
-        for (int i = 0; i < DP / 8; ++i) {
-            float2 *to = reinterpret_cast<float2 *>(values + g * DP + i * 8 + 2 * j);
-            if (H == 1) *to = make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]);
-            else {
-                *to = make_float2(o[i][0], o[i][1]);
-                to[4 * DP] = make_float2(o[i][2], o[i][3]);
-            }
+            for (int i = 0; i < DP / 8; ++i)
+                *reinterpret_cast<float2 *>(values + value_place<DP>(g + 8 * h, 2 * i + (j >> 1)) + (j & 1) * 2) =
+                    H == 1 ? make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]) : make_float2(o[i][2 * h], o[i][2 * h + 1]);
         }
     }
 };
@@ -339,9 +420,8 @@ template <int DP, int ROWS> struct StateF32 {
     float m[ROWS], l[ROWS];
     const float *q;
 
-    __device__ __forceinline__ void begin(const AttentionArgs &, const char *, uint32_t, const float *q_shared)
+    __device__ __forceinline__ void clear()
     {
-        q = q_shared;
 #pragma unroll
         for (int h = 0; h < ROWS; ++h) {
             m[h] = -INFINITY; l[h] = 0.0f;
@@ -349,14 +429,27 @@ template <int DP, int ROWS> struct StateF32 {
             for (int c = 0; c < C; ++c) o[h][c][0] = o[h][c][1] = o[h][c][2] = o[h][c][3] = 0.0f;
         }
     }
+    __device__ __forceinline__ void begin(const char *ring, int stage, float *q_shared)
+    {
+        clear();
+        q = q_shared;
+        const char *const qs = ring + stage * 2 * R::strip;
+#pragma unroll 4
+        for (int i = threadIdx.x & 31; i < ROWS * R::chunks; i += 32) {
+            const int r = i / R::chunks, piece = i % R::chunks;
+            *reinterpret_cast<float4 *>(q_shared + r * DP + piece * 4) = *reinterpret_cast<const float4 *>(qs + r * R::row + R::place(r, piece) * 16);
+        }
+        __syncwarp();
+    }
 
     __device__ __forceinline__ void strip(const AttentionArgs &a, const char *ring, int stage, uint32_t seen, float *p_shared)
     {
         const int lane = threadIdx.x & 31, t = lane / L, part = lane % L;
         const char *const ks = ring + stage * 2 * R::strip, *const vs = ks + R::strip;
         float s[ROWS] = {};
+        const int pieces = (int)(a.dim + 3) / 4;
 #pragma unroll 4
-        for (int i = part; i < R::chunks; i += L) {
+        for (int i = part; i < pieces; i += L) {
             const float4 k = *reinterpret_cast<const float4 *>(ks + t * R::row + R::place(t, i) * 16);
 #pragma unroll
             for (int h = 0; h < ROWS; ++h) {
@@ -416,22 +509,20 @@ template <int DP, int ROWS> struct StateF32 {
         __syncwarp();
     }
 
-    __device__ __forceinline__ void leave(float *values, float *top, float *sum)
+    __device__ __forceinline__ void leave(float *values, float *tops, float *sums)
     {
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int h = 0; h < ROWS; ++h) {
-            const float t = warp_sum(l[h]);
-            if (lane == 0) { top[h] = m[h]; sum[h] = t; }
+            const float sum = warp_sum(l[h]);
+            if (lane == 0) { tops[h] = top_of(m[h], sum); sums[h] = sum; }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                float4 x = make_float4(o[h][c][0], o[h][c][1], o[h][c][2], o[h][c][3]);
-                if (half == 2) {
-                    x.x += __shfl_xor_sync(0xFFFFFFFFu, x.x, 16); x.y += __shfl_xor_sync(0xFFFFFFFFu, x.y, 16);
-                    x.z += __shfl_xor_sync(0xFFFFFFFFu, x.z, 16); x.w += __shfl_xor_sync(0xFFFFFFFFu, x.w, 16);
-                }
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = half == 2 ? o[h][c][e] + __shfl_xor_sync(0xFFFFFFFFu, o[h][c][e], 16) : o[h][c][e];
                 if (half == 1 || lane < 16)
-                    *reinterpret_cast<float4 *>(values + h * DP + (half == 2 ? lane & 15 : lane + 32 * c) * 4) = x;
+                    *reinterpret_cast<float4 *>(values + value_place<DP>(h, half == 2 ? lane & 15 : lane + 32 * c)) = make_float4(x[0], x[1], x[2], x[3]);
             }
         }
     }
@@ -440,210 +531,298 @@ template <int DP, int ROWS> struct StateF32 {
 template <int DT, int DP, int ROWS> struct StateOf { using type = StateBf16<DP, ROWS>; };
 template <int DP, int ROWS> struct StateOf<SIFAR_F32, DP, ROWS> { using type = StateF32<DP, ROWS>; };
 
-/* Shared memory: the rings, later the warps' parts in their place; behind them binary32 queries and probabilities. */
+/* Shared memory: the rings (a warp leaves its values in its own), behind them each warp's binary32 queries and probabilities. */
 template <int DT, int DP, int ROWS> struct Shared {
-    static constexpr int rings = kWarps * Ring<DT, DP>::bytes, parts = kWarps * ROWS * (DP + 2) * 4;
-    static constexpr int queries = rings > parts ? rings : parts;
-    static constexpr int bytes = queries + (DT == SIFAR_F32 ? (ROWS * DP + kWarps * ROWS * Ring<DT, DP>::tokens) * 4 : 0);
+    static constexpr int rings = kWarps * Ring<DT, DP>::bytes;
+    static constexpr int per_warp = DT == SIFAR_F32 ? ROWS * (DP + Ring<DT, DP>::tokens) * 4 : 0;
+    static constexpr int bytes = rings + kWarps * per_warp;
+    static_assert(ROWS * DP * 4 <= 2 * Ring<DT, DP>::strip, "a state fits a stage");
 };
+
+/* Four values of an output row from column d on. */
+template <int DT> __device__ __forceinline__ void store_out(typename Elem<DT>::type *to, const float (&x)[4], uint32_t d, uint32_t dim, bool vec)
+{
+    if (vec) {
+        if (d >= dim) return;
+        if constexpr (DT == SIFAR_BF16) *reinterpret_cast<uint2 *>(to + d) = make_uint2(pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3]));
+        else *reinterpret_cast<float4 *>(to + d) = make_float4(x[0], x[1], x[2], x[3]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (d + e < dim) to[d + e] = narrow<DT>(x[e]);
+}
 
 template <int DT, int DP, int ROWS, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ AttentionArgs a)
 {
     using R = Ring<DT, DP>;
+    using Sh = Shared<DT, DP, ROWS>;
+    using C = Cursor<R::tokens>;
+    using T = typename Elem<DT>::type;
     extern __shared__ __align__(128) char smem[];
     __shared__ unsigned long long s_sum[kWarps];
-    __shared__ Place s_place;
-    __shared__ float s_w[kWarps][ROWS], s_m[ROWS], s_l[ROWS];
-    constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
+    __shared__ C s_start[kWarps];
+    __shared__ float s_top[kWarps][ROWS], s_l[kWarps][ROWS], s_w[kWarps][ROWS];
+    constexpr int es = sizeof(T);
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const uint32_t number = blockIdx.x * kWarps + warp, items = a.kv_heads * a.chunks;
     char *const ring = smem + warp * R::bytes;
-    float *const parts = reinterpret_cast<float *>(smem);                           /* warp x ROWS x DP, maxima, sums */
-    float *const tops = parts + kWarps * ROWS * DP, *const sums = tops + kWarps * ROWS;
-    float *const q_shared = reinterpret_cast<float *>(smem + Shared<DT, DP, ROWS>::queries);
-    float *const p_shared = q_shared + ROWS * DP + warp * ROWS * R::tokens;
+    float *const q_shared = reinterpret_cast<float *>(smem + Sh::rings + warp * Sh::per_warp), *const p_shared = q_shared + ROWS * DP;
+    const size_t part_floats = partial_floats(a.rows, DP);
     grid_let_next_in();
     grid_wait();
 
-    const Place place = find_share(a, s_sum, &s_place);
-    if (threadIdx.x == 0) a.splits[blockIdx.x].first = -1;
-    unsigned long long at = place.begin, before = place.before;
-    uint32_t sequence = place.sequence;
-    const unsigned long long share = (place.total + gridDim.x - 1) / gridDim.x;
-    const size_t part_floats = partial_floats(a.rows, DP);
+    if (lane == 0) a.splits[number].first = -1;
+    const Shares row = find_shares<R::tokens>(a, s_sum, s_start);
+    const unsigned long long begin = min(row.total, row.share * number), end = min(row.total, begin + row.share);
+    const bool any = begin < end;
+    C now = s_start[warp];                                        /* the strip to be used next */
+    if (!any) now.at = end;
+    /* whether all of the CTA's places belong to one item, from a strip of it on */
+    const unsigned long long cta_begin = row.share * blockIdx.x * kWarps, cta_end = min(row.total, cta_begin + row.share * kWarps);
+    const bool together = cta_begin < cta_end && s_start[0].at == cta_begin && cta_begin - s_start[0].strip + s_start[0].strips + kItemCost >= cta_end;
 
-    while (at < place.end) {
-        /* the item that tile `at` belongs to */
-        const uint32_t tiles = tiles_of(a, sequence);
-        const uint32_t item = (uint32_t)((at - before) / tiles), kv_head = item / a.chunks, chunk = item % a.chunks;
-        const unsigned long long item_begin = before + (unsigned long long)item * tiles, item_end = item_begin + tiles;
-        const uint32_t tile0 = (uint32_t)(at - item_begin), tile1 = (uint32_t)(min(item_end, place.end) - item_begin);
-        uint32_t lo, hi;
-        visible(a, sequence, lo, hi);
-        const uint32_t end = min(hi, lo + tile1 * kTile), begin = lo + tile0 * kTile;
-        const uint32_t rows = min(a.rows, a.group - chunk * a.rows), head = kv_head * a.group + chunk * a.rows;
-        const char *const q_row = a.q + sequence * a.ld_q + (size_t)head * a.dim * es;
-        const int *const table = a.pages.table + sequence * a.pages.ld_table;
-        const unsigned long long head_at = kv_head * a.pages.stride_head;
-
-        if (DT == SIFAR_F32) {
-            for (uint32_t i = threadIdx.x; i < ROWS * DP; i += kThreads) {
-                const uint32_t r = i / DP, d = i % DP;
-                q_shared[i] = r < rows && d < a.dim ? reinterpret_cast<const float *>(q_row)[r * a.dim + d] : 0.0f;
-            }
-            __syncthreads();
-        }
-        typename StateOf<DT, DP, ROWS>::type state;
-
-        /* this warp's strips: begin + (warp + i * kWarps) * tokens */
-        const uint32_t strips = end > begin ? (end - begin + R::tokens - 1) / R::tokens : 0u;
-        const uint32_t mine = strips > (uint32_t)warp ? (strips - warp + kWarps - 1) / kWarps : 0u;
-        auto offset_of = [&](uint32_t i) -> long long {
-            const uint32_t t = begin + (warp + i * kWarps) * R::tokens + lane % R::tokens;
-            return i < mine && t < end ? token_offset(a.pages, table, t) : -1ll;
-        };
-        uint32_t seen[R::stages];
-        /* strips 0 .. stages - 2 are under way before the first is used */
-        long long next = offset_of(0);
-#pragma unroll
-        for (int i = 0; i < R::stages - 1; ++i) {
-            const long long now = next;
-            next = offset_of(i + 1);
-            seen[i] = __ballot_sync(0xFFFFFFFFu, now >= 0);
-            if ((uint32_t)i < mine) fetch<DT, DP, VEC>(a, ring, i, now, head_at);
-            copies_commit();
-        }
-        state.begin(a, q_row, rows, q_shared);
-        for (uint32_t i0 = 0; i0 < mine; i0 += R::stages) {
-#pragma unroll
-            for (int u = 0; u < R::stages; ++u) {
-                const uint32_t i = i0 + u;
-                if (i >= mine) break;
-                constexpr int last = R::stages - 1;
-                const int to = (u + last) % R::stages;
-                const long long now = next;
-                next = offset_of(i + R::stages);
-                copies_wait<R::stages - 2>();
-                __syncwarp();
-                seen[to] = __ballot_sync(0xFFFFFFFFu, now >= 0);
-                if (i + last < mine) fetch<DT, DP, VEC>(a, ring, to, now, head_at);
-                copies_commit();
-                state.strip(a, ring, u, seen[u], p_shared);
+    C then = now;                                                 /* the strip to be fetched next */
+    bool queries = true;                                          /* ... or the queries of its item */
+    auto offset_of = [&](const C &c) -> long long {
+        const uint32_t t = c.lo + c.strip * R::tokens + lane % R::tokens;
+        return c.at < end && t < c.hi ? token_offset(a.pages, a.pages.table + c.sequence * a.pages.ld_table, t) : -1ll;
+    };
+    unsigned long long seen = 0;                                  /* 16 bits per stage: its tokens that count */
+    long long next = offset_of(then);
+    auto fetch_next = [&](int stage) {
+        if (then.at < end) {
+            const uint32_t kv_head = then.item / a.chunks, chunk = then.item - kv_head * a.chunks;
+            if (queries) {
+                const uint32_t head = kv_head * a.group + chunk * a.rows;
+                fetch_queries<DT, DP>(a, ring, stage, a.q + then.sequence * a.ld_q + (size_t)head * a.dim * es, min(a.rows, a.group - chunk * a.rows));
+                queries = false;
+            } else {
+                const long long at = next;
+                queries = then.advance(a, items);
+                next = offset_of(then);
+                seen = (seen & ~(0xFFFFull << (16 * stage))) | (unsigned long long)(__ballot_sync(0xFFFFFFFFu, at >= 0) & ((1u << R::tokens) - 1u)) << (16 * stage);
+                fetch<DT, DP, VEC>(a, ring, stage, at, kv_head * a.pages.stride_head);
             }
         }
-        copies_wait<0>();
-        __syncthreads();                                          /* the rings become the warps' parts */
-        state.leave(parts + warp * ROWS * DP, tops + warp * ROWS, sums + warp * ROWS);
-        __syncthreads();
-        if (threadIdx.x < ROWS) {
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, tops[w * ROWS + threadIdx.x]);
-            const float ref = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float f = exp2f(tops[w * ROWS + threadIdx.x] - ref);
-                s_w[w][threadIdx.x] = f;
-                sum += f * sums[w * ROWS + threadIdx.x];
-            }
-            s_m[threadIdx.x] = top; s_l[threadIdx.x] = sum;
+        copies_commit();
+    };
+    /* stages - 1 strips are under way before the first is used */
+    for (int i = 0; i < R::stages - 1; ++i) fetch_next(i);
+
+    typename StateOf<DT, DP, ROWS>::type state;
+    state.clear();
+    bool left = false, fresh = true, whole = false;                             /* whole: from the item's first strip on */
+    int stage = 0;
+    while (now.at < end) {
+        copies_wait<R::stages - 2>();
+        __syncwarp();
+        fetch_next(stage == 0 ? R::stages - 1 : stage - 1);
+        const int here = stage;
+        stage = stage + 1 == R::stages ? 0 : stage + 1;
+        if (fresh) {
+            state.begin(ring, here, q_shared);
+            whole = now.strip == 0;
+            fresh = false;
+            continue;
         }
-        __syncthreads();
-        const bool whole = tile0 == 0 && tile1 == tiles;
+        state.strip(a, ring, here, (uint32_t)(seen >> (16 * here)) & 0xFFFFu, p_shared);
+        const C done = now;
+        now.advance(a, items);
+        if (done.strip + 1 < done.strips && now.at < end) continue;
+
+        /* the item, or this warp's share of it, is done: it goes through the stage that was used last, in whole rows */
+        fresh = true;
+        float *const values = reinterpret_cast<float *>(together ? ring : ring + here * 2 * R::strip);
+        if (together) copies_wait<0>();
+        __syncwarp();
+        state.leave(values, s_top[warp], s_l[warp]);
+        left = true;
+        __syncwarp();
+        const unsigned long long item_begin = done.at - done.strip;
+        const bool all = whole && done.strip + 1 == done.strips;
         /* slot 0: the item that the share begins in; slot 1: one that it leaves unfinished */
-        const int slot = item_begin <= place.begin ? 0 : 1;
-        float *const part = a.partial + ((size_t)blockIdx.x * 2 + slot) * part_floats;
-        for (uint32_t i = threadIdx.x; i < rows * (DP / 4); i += kThreads) {
-            const uint32_t r = i / (DP / 4), d = i % (DP / 4) * 4;
-            float x[4] = {};
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float f = s_w[w][r];
-                const float4 o = *reinterpret_cast<const float4 *>(parts + (w * ROWS + r) * DP + d);
-                x[0] += f * o.x; x[1] += f * o.y; x[2] += f * o.z; x[3] += f * o.w;
-            }
-            if (whole) {
-                const float sum = s_l[r], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                auto *out = reinterpret_cast<typename Elem<DT>::type *>(a.out + sequence * a.ld_out) + (size_t)(head + r) * a.dim + d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (d + e < a.dim) out[e] = narrow<DT>(x[e] * inv);
+        const int slot = item_begin <= begin ? 0 : 1;
+        if (whole && !all && lane == 0) {
+            const uint32_t last = (uint32_t)quotient(item_begin + done.strips - 1, (uint32_t)row.share);
+            /* CTAs from its first full one to its last that end within it, or behind it before anything else begins */
+            const unsigned long long item_end = min(row.total, item_begin + done.strips + kItemCost), cta = row.share * kWarps;
+            const uint32_t one0 = (uint32_t)((item_begin + cta - 1) / cta) * kWarps;
+            uint32_t one1 = item_end == row.total ? (last / kWarps + 1) * kWarps : (uint32_t)(item_end / cta) * kWarps;
+            one1 = max(one0, min(one1, (last / kWarps + 1) * kWarps));
+            a.splits[number] = Split{(int)done.sequence, (int)done.item, (int)number, (int)last, slot, (int)one0, (int)one1, 0};
+        }
+        if (together && !all) break;
+        const uint32_t kv_head = done.item / a.chunks, chunk = done.item - kv_head * a.chunks, rows = min(a.rows, a.group - chunk * a.rows);
+        const uint32_t head = kv_head * a.group + chunk * a.rows;
+        T *const out = reinterpret_cast<T *>(a.out + done.sequence * a.ld_out) + (size_t)head * a.dim;
+        float *const part = a.partial + ((size_t)number * 2 + slot) * part_floats;
+#pragma unroll 2
+        for (uint32_t i = lane; i < rows * (DP / 4); i += 32) {
+            const uint32_t r = i / (DP / 4), piece = i % (DP / 4);
+            const float4 v = *reinterpret_cast<const float4 *>(values + value_place<DP>(r, piece));
+            if (all) {
+                const float sum = s_l[warp][r], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const float x[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
+                store_out<DT>(out + (size_t)r * a.dim, x, piece * 4, a.dim, a.out_vec);
             } else {
-                *reinterpret_cast<float4 *>(part + r * DP + d) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4 *>(part + r * DP + piece * 4) = v;
             }
         }
-        if (threadIdx.x < rows) {
-            const float top = s_m[threadIdx.x], sum = s_l[threadIdx.x];
-            if (whole) {
-                if (a.lse) a.lse[sequence * (size_t)a.heads + head + threadIdx.x] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
-            } else {
-                part[a.rows * DP + threadIdx.x] = top;
-                part[a.rows * DP + a.rows + threadIdx.x] = sum;
-            }
+        if (lane < (int)rows) {
+            const float top = s_top[warp][lane], sum = s_l[warp][lane];
+            if (!all) { part[a.rows * DP + lane] = top; part[a.rows * DP + a.rows + lane] = sum; }
+            else if (a.lse) a.lse[done.sequence * (size_t)a.heads + head + lane] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
         }
-        if (!whole && threadIdx.x == 0 && tile0 == 0) {
-            Split s{(int)sequence, (int)kv_head, (int)chunk, (int)blockIdx.x, (int)((item_end - 1) / share), slot, {0, 0}};
-            a.splits[blockIdx.x] = s;
+        __syncwarp();
+    }
+    copies_wait<0>();
+    if (!together) return;
+
+    /* all of the CTA's warps have strips of one item, or none: one part of them, in the first one's place */
+    if (!left && lane < ROWS) { s_top[warp][lane] = -INFINITY; s_l[warp][lane] = 0.0f; }
+    __syncthreads();
+    const uint32_t chunk = s_start[0].item % a.chunks, rows = min(a.rows, a.group - chunk * a.rows);
+    float *const part = a.partial + (size_t)blockIdx.x * kWarps * 2 * part_floats;
+    if (threadIdx.x < rows) {
+        const int r = threadIdx.x;
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_top[w][r]);
+        const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float f = exp2f(s_top[w][r] - ref);
+            s_w[w][r] = f;
+            sum += f * s_l[w][r];
         }
-        __syncthreads();                                          /* before the rings are filled again */
-        at = item_begin + tile1;
-        if (at == before + (unsigned long long)a.kv_heads * a.chunks * tiles) { before = at; ++sequence; }
+        part[a.rows * DP + r] = top_of(top, sum);
+        part[a.rows * DP + a.rows + r] = sum;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < rows * (DP / 4); i += kThreads) {
+        const uint32_t r = i / (DP / 4), piece = i % (DP / 4);
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float f = s_w[w][r];
+            if (s_top[w][r] == -INFINITY) continue;               /* it left nothing */
+            const float4 o = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + w * R::bytes) + value_place<DP>(r, piece));
+            x.x += f * o.x; x.y += f * o.y; x.z += f * o.z; x.w += f * o.w;
+        }
+        *reinterpret_cast<float4 *>(part + r * DP + piece * 4) = x;
     }
 }
 
 /*
- * An item whose tiles several CTAs had: one CTA per query head.  Warps take partials in turn, each lane four (eight) columns.
+ * The items that begin in a CTA's warps and end in others, a query head per CTA.  Items of up to kAlone parts have a warp each; at
+ * most one of a CTA's has more (it goes on into other CTAs), and all warps share its parts.  Lanes have four columns each.
  */
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps, kAlone = 8;
+
+/* A running join: values brought to the maximum so far. */
+template <int DP> struct Joined {
+    static constexpr int C = DP > 128 ? 2 : 1;
+    float top = -INFINITY, sum = 0.0f, o[C][4] = {};
+    __device__ __forceinline__ void add(float t, float s, const float4 (&v)[C])
+    {
+        if (t == -INFINITY) return;                               /* nothing there; the same for the whole warp */
+        const float now = t > top ? t : t != t || top != top ? NAN : top;
+        const float keep = top == -INFINITY ? 0.0f : exp2f(top - now), f = exp2f(t - now);
+        top = now;
+        sum = sum * keep + s * f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            o[c][0] = o[c][0] * keep + v[c].x * f; o[c][1] = o[c][1] * keep + v[c].y * f;
+            o[c][2] = o[c][2] * keep + v[c].z * f; o[c][3] = o[c][3] * keep + v[c].w * f;
+        }
+    }
+};
+
 template <int DT, int DP>
-__global__ void __launch_bounds__(32 * kJoinWarps) k_attend_join(const __grid_constant__ AttentionArgs a)
+__global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_constant__ AttentionArgs a)
 {
+    using J = Joined<DP>;
+    using T = typename Elem<DT>::type;
     __shared__ float s_top[kJoinWarps], s_sum[kJoinWarps];
     __shared__ __align__(16) float s_o[kJoinWarps][DP];
     grid_let_next_in();
     grid_wait();
-    const Split s = a.splits[blockIdx.x];
     const uint32_t r = blockIdx.y;
-    if (s.first < 0 || r >= min(a.rows, a.group - s.chunk * a.rows)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const size_t part_floats = partial_floats(a.rows, DP);
-    const int n = s.last - s.first + 1;
-    auto part = [&](int i) { return a.partial + ((size_t)(s.first + i) * 2 + (i == 0 ? s.slot : 0)) * part_floats; };
-    /* the largest maximum, then the sum with every part brought to it */
-    float top = -INFINITY;
-    for (int i = threadIdx.x; i < n; i += 32 * kJoinWarps) top = fmaxf(top, part(i)[a.rows * DP + r]);
+    /* this warp's split, and the one that all share */
+    const Split mine = warp < kWarps ? a.splits[blockIdx.x * kWarps + warp] : Split{0, 0, -1, 0, 0, 0, 0, 0};
+    const Split last = a.splits[blockIdx.x * kWarps + kWarps - 1];
+    Split big = last;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    if (lane == 0) s_top[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_top[w]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o[DP / 32] = {};
-#pragma unroll 4
-    for (int i = warp; i < n; i += kJoinWarps) {
-        const float *p = part(i);
-        const float f = exp2f(p[a.rows * DP + r] - ref);
-        sum += f * p[a.rows * DP + a.rows + r];
-#pragma unroll
-        for (int c = 0; c < DP / 32; ++c) o[c] += f * p[r * DP + c * 32 + lane];
+    for (int k = 0; k < kWarps - 1; ++k) {
+        const Split s = a.splits[blockIdx.x * kWarps + k];
+        if (s.first >= 0 && s.last - s.first + 1 > kAlone) big = s;
     }
+    /* parts in their order: warps up to one0, a part per CTA up to one1, warps again */
+    auto parts_of = [](const Split &s) { return min(s.one0, s.last + 1) - s.first + (s.one1 - s.one0) / kWarps + max(0, s.last + 1 - s.one1); };
+    auto part_at = [&](const Split &s, int i) {
+        const int before = min(s.one0, s.last + 1) - s.first, ones = (s.one1 - s.one0) / kWarps;
+        const int w = i < before ? s.first + i : i < before + ones ? s.one0 + (i - before) * kWarps : s.one1 + (i - before - ones);
+        return a.partial + ((size_t)w * 2 + (w == s.first ? s.slot : 0)) * part_floats;
+    };
+    auto there = [&](const Split &s) { return s.first >= 0 && r < min(a.rows, a.group - s.item % a.chunks * a.rows); };
+    auto walk = [&](const Split &s, int i0, int i1, J &j) {
+        for (; i0 < i1; i0 += 4) {
+            float t[4], l[4];
+            float4 v[4][J::C];
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c) s_o[warp][c * 32 + lane] = o[c];
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    sum = 0.0f;
+            for (int k = 0; k < 4; ++k) {
+                const float *const p = part_at(s, min(i0 + k, i1 - 1));
+                t[k] = i0 + k < i1 ? __ldcg(p + a.rows * DP + r) : -INFINITY;
+                l[k] = __ldcg(p + a.rows * DP + a.rows + r);
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) sum += s_sum[w];
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const uint32_t head = s.kv_head * a.group + s.chunk * a.rows + r;
-    for (uint32_t d = threadIdx.x; d < a.dim; d += 32 * kJoinWarps) {
-        float x = 0.0f;
+                for (int c = 0; c < J::C; ++c)
+                    if (DP >= 128 || lane < DP / 4) v[k][c] = __ldcg(reinterpret_cast<const float4 *>(p + r * DP + (lane + 32 * c) * 4));
+            }
 #pragma unroll
-        for (int w = 0; w < kJoinWarps; ++w) x += s_o[w][d];
-        reinterpret_cast<typename Elem<DT>::type *>(a.out + (size_t)s.sequence * a.ld_out)[(size_t)head * a.dim + d] = narrow<DT>(x * inv);
+            for (int k = 0; k < 4; ++k) j.add(t[k], l[k], v[k]);
+        }
+    };
+    auto finish = [&](const Split &s, const J &j) {
+        const uint32_t head = s.item / a.chunks * a.group + s.item % a.chunks * a.rows + r;
+        const float inv = j.sum == 0.0f ? 0.0f : 1.0f / j.sum;
+        T *const out = reinterpret_cast<T *>(a.out + (size_t)s.sequence * a.ld_out) + (size_t)head * a.dim;
+#pragma unroll
+        for (int c = 0; c < J::C; ++c) {
+            const float x[4] = {j.o[c][0] * inv, j.o[c][1] * inv, j.o[c][2] * inv, j.o[c][3] * inv};
+            store_out<DT>(out, x, (lane + 32 * c) * 4, a.dim, a.out_vec);
+        }
+        if (a.lse && lane == 0) a.lse[(size_t)s.sequence * a.heads + head] = j.sum == 0.0f ? -INFINITY : (j.top + log2f(j.sum)) * kLn2;
+    };
+
+    if (there(mine) && parts_of(mine) <= kAlone) {
+        J j;
+        walk(mine, 0, parts_of(mine), j);
+        finish(mine, j);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[(size_t)s.sequence * a.heads + head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (!there(big) || parts_of(big) <= kAlone) return;           /* the same for the whole CTA */
+    const int n = parts_of(big);
+    J j;
+    walk(big, n * warp / kJoinWarps, n * (warp + 1) / kJoinWarps, j);
+#pragma unroll
+    for (int c = 0; c < J::C; ++c)
+        if (DP >= 128 || lane < DP / 4) *reinterpret_cast<float4 *>(&s_o[warp][(lane + 32 * c) * 4]) = make_float4(j.o[c][0], j.o[c][1], j.o[c][2], j.o[c][3]);
+    if (lane == 0) { s_top[warp] = j.top; s_sum[warp] = j.sum; }
+    __syncthreads();
+    if (warp) return;
+    J total;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+        float4 v[J::C];
+#pragma unroll
+        for (int c = 0; c < J::C; ++c)
+            if (DP >= 128 || lane < DP / 4) v[c] = *reinterpret_cast<const float4 *>(&s_o[w][(lane + 32 * c) * 4]);
+        total.add(s_top[w], s_sum[w], v);
+    }
+    finish(big, total);
 }
 
 /* ------------------------------------------------------------------------ */
@@ -662,7 +841,7 @@ static cudaError_t launch_attend(const AttentionPlan &plan, cudaStream_t stream,
     /* per device: an attribute of the kernel there */
     if (cudaError_t e = cudaFuncSetAttribute(k_attend<DT, DP, ROWS, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared)) return e;
     if (cudaError_t e = launch_op(k_attend<DT, DP, ROWS, VEC>, dim3(plan.ctas), dim3(kThreads), 1, shared, stream, a)) return e;
-    return launch_op(k_attend_join<DT, DP>, dim3(plan.ctas, plan.rows), dim3(32 * kJoinWarps), 1, 0, stream, a);
+    return launch_op(k_attend_join<DT, DP>, dim3(plan.ctas, plan.rows), dim3(kJoinThreads), 1, 0, stream, a);
 }
 
 template <int DT, int DP>
@@ -670,6 +849,9 @@ static cudaError_t launch_attend_d(bool vec, const AttentionPlan &plan, cudaStre
 {
     if constexpr (DT == SIFAR_BF16) {
         if (plan.rows > 8) return vec ? launch_attend<DT, DP, 16, true>(plan, stream, a) : launch_attend<DT, DP, 16, false>(plan, stream, a);
+    }
+    if constexpr (DT == SIFAR_F32) {                              /* every head costs instructions */
+        if (plan.rows <= 4) return vec ? launch_attend<DT, DP, 4, true>(plan, stream, a) : launch_attend<DT, DP, 4, false>(plan, stream, a);
     }
     return vec ? launch_attend<DT, DP, 8, true>(plan, stream, a) : launch_attend<DT, DP, 8, false>(plan, stream, a);
 }
@@ -705,8 +887,8 @@ static int plan_attention(const char *fn, const sifar_decode_attention_args *g, 
     p.rows = (group + p.chunks - 1) / p.chunks;
     p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
     p.ctas = kSms * (unsigned)ctas_per_sm(bf16 ? shared_of<SIFAR_BF16>(p.dp, p.rows > 8) : shared_of<SIFAR_F32>(p.dp, false));
-    p.split_bytes = p.ctas * sizeof(Split);
-    p.bytes = p.split_bytes + (size_t)p.ctas * 2 * partial_floats(p.rows, p.dp) * sizeof(float);
+    p.split_bytes = (size_t)p.ctas * kWarps * sizeof(Split);
+    p.bytes = p.split_bytes + (size_t)p.ctas * kWarps * 2 * partial_floats(p.rows, p.dp) * sizeof(float);
     p.bytes = (p.bytes + 15) / 16 * 16;
     return SIFAR_OK;
 }
@@ -768,6 +950,8 @@ extern "C" int sifar_decode_attention(const sifar_decode_attention_args *g, void
     a.heads = (uint32_t)g->heads; a.kv_heads = (uint32_t)g->kv_heads; a.group = a.heads / a.kv_heads;
     a.chunks = p.chunks; a.rows = p.rows; a.dim = (uint32_t)c.dim;
     a.scale = g->scale * kLog2e;
+    a.q_vec = rows_aligned16(all[0]) && c.dim * es % 16 == 0;
+    a.out_vec = (uintptr_t)g->out % (4 * es) == 0 && c.dim % 4 == 0 && (S == 1 || all[3].ld % 4 == 0);
     const bool vec = cache_aligned16(c, g->k_cache, g->v_cache) && c.dim * es % 16 == 0;
     const cudaError_t err = g->dtype == SIFAR_BF16 ? launch_attend_t<SIFAR_BF16>(vec, p, (cudaStream_t)stream, a)
                                                    : launch_attend_t<SIFAR_F32>(vec, p, (cudaStream_t)stream, a);

@@ -212,6 +212,33 @@ def test_scores_that_are_not_finite(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("n", [5, 70, 3000])
+def test_nan_in_every_key_gives_nan(n):
+    c = Cache([n, n], page=16, kv=1, dim=64)
+    for t in range(n):
+        c.k[int(c.table[0, t // 16]), t % 16, 0, 7] = math.nan
+    q = torch.ones(2, 64, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros(2, 1, device="cuda")
+    lengths = torch.tensor([n, n], dtype=torch.int32, device="cuda")
+    a = sf.make_attention(q=q.data_ptr(), out=out.data_ptr(), lse=lse.data_ptr(), lengths=lengths.data_ptr(), heads=1, **c.fields())
+    ws = torch.empty(sf.sifar_decode_attention_workspace(a), dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+    sf.sifar_decode_attention(a)
+    torch.cuda.synchronize()
+    assert bool(out[0].isnan().all()) and bool(lse[0].isnan().all()) and bool(out[1].isfinite().all()) and bool(lse[1].isfinite().all())
+
+
+@gpu
+@pytest.mark.parametrize("heads,kv", [(1, 1), (2, 2), (3, 3)])
+def test_few_strips_for_many_warps(heads, kv):
+    """Shares of one strip and of the places between items: whole items in a warp, in a CTA, over CTAs, at the row's end."""
+    for n in (1, 16, 17, 33, 48, 64, 65, 79, 81, 113, 160, 1000, 16 * 1183, 16 * 1184, 16 * 1185):
+        _run([n], heads=heads, kv=kv, dim=64, seed=n)
+    for lengths in ([16, 17], [1, 1, 1], [15, 64, 1], [33] * 5, [16 * 200, 1, 16 * 300], [1] * 700):
+        _run(lengths, heads=heads, kv=kv, dim=64)
+
+
+@gpu
 def test_a_cache_beyond_32_bits():
     pages, n = (1 << 31) // (64 * 8 * 128) + 2, 100
     k = torch.zeros(pages, 64, 8, 128, dtype=torch.bfloat16, device="cuda")
