@@ -634,10 +634,10 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
 
         /* the item, or this warp's share of it, is done: it goes through the stage that was used last, in whole rows */
         fresh = true;
-        float *const values = reinterpret_cast<float *>(together ? ring : ring + here * 2 * R::strip);
+        const int values = warp * R::bytes + (together ? 0 : here * 2 * R::strip);       /* in smem */
         if (together) copies_wait<0>();
         __syncwarp();
-        state.leave(values, s_top[warp], s_l[warp]);
+        state.leave(reinterpret_cast<float *>(smem + values), s_top[warp], s_l[warp]);
         left = true;
         __syncwarp();
         const unsigned long long item_begin = done.at - done.strip;
@@ -658,22 +658,34 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
         const uint32_t head = kv_head * a.group + chunk * a.rows;
         T *const out = reinterpret_cast<T *>(a.out + done.sequence * a.ld_out) + (size_t)head * a.dim;
         float *const part = a.partial + ((size_t)number * 2 + slot) * part_floats;
-#pragma unroll 2
-        for (uint32_t i = lane; i < rows * (DP / 4); i += 32) {
-            const uint32_t r = i / (DP / 4), piece = i % (DP / 4);
-            const float4 v = *reinterpret_cast<const float4 *>(values + value_place<DP>(r, piece));
-            if (all) {
-                const float sum = s_l[warp][r], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                const float x[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
-                store_out<DT>(out + (size_t)r * a.dim, x, piece * 4, a.dim, a.out_vec);
-            } else {
-                *reinterpret_cast<float4 *>(part + r * DP + piece * 4) = v;
-            }
-        }
         if (lane < (int)rows) {
             const float top = s_top[warp][lane], sum = s_l[warp][lane];
+            s_w[warp][lane] = sum == 0.0f ? 0.0f : 1.0f / sum;
             if (!all) { part[a.rows * DP + lane] = top; part[a.rows * DP + a.rows + lane] = sum; }
             else if (a.lse) a.lse[done.sequence * (size_t)a.heads + head + lane] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+        }
+        __syncwarp();
+        /* several loads before the first store: a warp has nobody to hide them behind */
+        for (uint32_t i0 = lane; i0 < rows * (DP / 4); i0 += 32 * 4) {
+            float4 v[4];
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t r = min(i0 + k * 32, rows * (DP / 4) - 1) / (DP / 4), piece = (i0 + k * 32) % (DP / 4);
+                v[k] = *reinterpret_cast<const float4 *>(smem + values + value_place<DP>(r, piece) * 4);
+                f[k] = s_w[warp][r];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t i = i0 + k * 32, r = i / (DP / 4), piece = i % (DP / 4);
+                if (i >= rows * (DP / 4)) break;
+                if (all) {
+                    const float x[4] = {v[k].x * f[k], v[k].y * f[k], v[k].z * f[k], v[k].w * f[k]};
+                    store_out<DT>(out + (size_t)r * a.dim, x, piece * 4, a.dim, a.out_vec);
+                } else {
+                    *reinterpret_cast<float4 *>(part + r * DP + piece * 4) = v[k];
+                }
+            }
         }
         __syncwarp();
     }
@@ -707,9 +719,8 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float f = s_w[w][r];
-            if (s_top[w][r] == -INFINITY) continue;               /* it left nothing */
-            const float4 o = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + w * R::bytes) + value_place<DP>(r, piece));
-            x.x += f * o.x; x.y += f * o.y; x.z += f * o.z; x.w += f * o.w;
+            const float4 o = *reinterpret_cast<const float4 *>(smem + w * R::bytes + value_place<DP>(r, piece) * 4);
+            if (f != 0.0f) { x.x += f * o.x; x.y += f * o.y; x.z += f * o.z; x.w += f * o.w; }      /* 0: it may have left nothing */
         }
         *reinterpret_cast<float4 *>(part + r * DP + piece * 4) = x;
     }
@@ -721,21 +732,30 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
  */
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps, kAlone = 8;
 
-/* A running join: values brought to the maximum so far. */
+/* A running join: values brought to the maximum so far.  A maximum of -infinity stands for nothing, whatever its values are. */
 template <int DP> struct Joined {
     static constexpr int C = DP > 128 ? 2 : 1;
     float top = -INFINITY, sum = 0.0f, o[C][4] = {};
-    __device__ __forceinline__ void add(float t, float s, const float4 (&v)[C])
+    template <int N> __device__ __forceinline__ void add(const float (&t)[N], const float (&s)[N], const float4 (&v)[N][C])
     {
-        if (t == -INFINITY) return;                               /* nothing there; the same for the whole warp */
-        const float now = t > top ? t : t != t || top != top ? NAN : top;
-        const float keep = top == -INFINITY ? 0.0f : exp2f(top - now), f = exp2f(t - now);
-        top = now;
-        sum = sum * keep + s * f;
+        float now = top;
+        bool nan = false;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            o[c][0] = o[c][0] * keep + v[c].x * f; o[c][1] = o[c][1] * keep + v[c].y * f;
-            o[c][2] = o[c][2] * keep + v[c].z * f; o[c][3] = o[c][3] * keep + v[c].w * f;
+        for (int k = 0; k < N; ++k) { now = fmaxf(now, t[k]); nan = nan || t[k] != t[k]; }
+        const float ref = now == -INFINITY ? 0.0f : now, keep = exp2f(top - ref);
+        top = now;
+        sum = nan ? NAN : sum * keep;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][e] *= keep;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float f = exp2f(t[k] - ref);
+            if (f == 0.0f) continue;
+            sum += s[k] * f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) { o[c][0] += v[k][c].x * f; o[c][1] += v[k][c].y * f; o[c][2] += v[k][c].z * f; o[c][3] += v[k][c].w * f; }
         }
     }
 };
@@ -782,8 +802,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
                 for (int c = 0; c < J::C; ++c)
                     if (DP >= 128 || lane < DP / 4) v[k][c] = __ldcg(reinterpret_cast<const float4 *>(p + r * DP + (lane + 32 * c) * 4));
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) j.add(t[k], l[k], v[k]);
+            j.add(t, l, v);
         }
     };
     auto finish = [&](const Split &s, const J &j) {
@@ -810,18 +829,20 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
 #pragma unroll
     for (int c = 0; c < J::C; ++c)
         if (DP >= 128 || lane < DP / 4) *reinterpret_cast<float4 *>(&s_o[warp][(lane + 32 * c) * 4]) = make_float4(j.o[c][0], j.o[c][1], j.o[c][2], j.o[c][3]);
-    if (lane == 0) { s_top[warp] = j.top; s_sum[warp] = j.sum; }
+    if (lane == 0) { s_top[warp] = top_of(j.top, j.sum); s_sum[warp] = j.sum; }
     __syncthreads();
     if (warp) return;
     J total;
+    float tops[kJoinWarps], l[kJoinWarps];
+    float4 v[kJoinWarps][J::C];
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) {
-        float4 v[J::C];
+        tops[w] = s_top[w]; l[w] = s_sum[w];
 #pragma unroll
         for (int c = 0; c < J::C; ++c)
-            if (DP >= 128 || lane < DP / 4) v[c] = *reinterpret_cast<const float4 *>(&s_o[w][(lane + 32 * c) * 4]);
-        total.add(s_top[w], s_sum[w], v);
+            if (DP >= 128 || lane < DP / 4) v[w][c] = *reinterpret_cast<const float4 *>(&s_o[w][(lane + 32 * c) * 4]);
     }
+    total.add(tops, l, v);
     finish(big, total);
 }
 
