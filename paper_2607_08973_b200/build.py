@@ -36,7 +36,7 @@ LIB_S8X2 = os.path.join(PKG, "libsifar_s8x2.so")
 
 # which translation units go into which library
 CORE_UNITS = ("sifar_core", "sifar_noalloc", "sifar_norm", "sifar_norm_grad", "sifar_route",
-              "sifar_append", "sifar_attention", "sifar_experts")
+              "sifar_append", "sifar_attention", "sifar_experts", "sifar_experts_tiles")
 SLOT_UNITS = ("sifar_core", "sifar_noalloc")          # ... and know the slot format: built a second time for it
 BENCH_UNITS = ("sifar_workload", "sifar_symmetric", "sifar_chain_cluster", "sifar_chain_pipe")
 

@@ -1,0 +1,407 @@
+/*
+ * sifar_experts_tiles.cu - the chosen experts' products for more than a few tokens, bf16: tcgen05 matrix instructions on
+ * tiles of 128 weight rows.
+ *
+ * The weights are the instruction's rows (M = 128) and an expert's tokens its columns (N = 16 .. 64), so that every weight is
+ * read once whatever the number of tokens.  A stage of the ring in shared memory is 64 elements (128 bytes, a swizzle atom)
+ * of the tile's rows and of the tokens' rows.  The warps of a CTA have parts of their own and meet only through the stages'
+ * barriers:
+ *   warp 0      one thread fetches the weights (TMA, 16 rows at a time: no more than the share has)
+ *   warp 1      one thread issues the products
+ *   warps 2, 3  gather the tokens' rows (asynchronous 16-byte copies)
+ *   warps 4 - 7 take a tile's sums out of tensor memory while the next tile's go into its other half
+ * What bounds it is the memory; the ring keeps up to 160 KB of weights per SM on the way, across tiles.
+ *
+ * First product: a tile is 128 gate rows and the 128 up rows that go with them, two accumulators; a thread then has both values of
+ * its row.  Second product: the values come as two bf16 parts, and both go into one accumulator.
+ */
+#include <cuda.h>
+
+#include "sifar_experts.cuh"
+
+namespace sifar {
+
+constexpr int kRows = 128;                   /* of an instruction */
+constexpr int kSpan = 128;                   /* bytes of a row in a stage */
+constexpr int kGroup = 16;                   /* rows that shares are counted in, and that a fetch of weights has */
+constexpr int kRing = 198 * 1024;            /* bytes of all stages: what the lists leave of an SM's 227 KB */
+constexpr int kMaxRing = 8;
+constexpr int kGatherers = 64;               /* threads that gather the tokens' rows */
+constexpr int kLag = 2;                      /* stages that they have under way while they fill another */
+constexpr uint32_t kPolls = 1u << 22;        /* a wait's limit: about 0.1 s, where the products take less than a microsecond */
+
+template <bool DOWN> struct Tile {
+    static constexpr int halves = DOWN ? 1 : 2;                  /* blocks of kRows weight rows */
+    static constexpr int parts = DOWN ? 2 : 1;                   /* of the tokens' values */
+    static constexpr int weights = halves * kRows * kSpan;       /* bytes of a stage */
+};
+
+struct TilesArgs {
+    ExpertsArgs e;
+    uint32_t columns, stages, choices;       /* columns of a pass over an expert's rows */
+};
+
+__device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+/* Operand in shared memory: rows of 128 bytes in 128-byte swizzle, eight rows every 1024 bytes. */
+__device__ __forceinline__ unsigned long long operand(uint32_t at)
+{
+    return (unsigned long long)((at & 0x3FFFFu) >> 4) | 1ull << 16 | (unsigned long long)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ void product(uint32_t to, unsigned long long rows, unsigned long long cols, uint32_t kind, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(to), "l"(rows), "l"(cols), "r"(kind), "r"((uint32_t)add) : "memory");
+}
+/* The barrier is told when all products issued so far are done. */
+__device__ __forceinline__ void tell_when_done(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void sums_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void sums_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void read_sums(uint32_t (&v)[8], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(at));
+}
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_arrive_and_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+/* Waits until the barrier's phase `parity` is over.  `fine` turns false where that takes too long; nothing is waited for after that. */
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, bool &fine)
+{
+    for (uint32_t i = 0; fine; ++i) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return;
+        if (i == kPolls) fine = false;
+    }
+}
+
+/* kGroup rows x 64 elements from (column, row) on. */
+__device__ __forceinline__ void fetch_rows(uint32_t to, const CUtensorMap *map, uint32_t column, uint32_t row, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(to), "l"(map), "r"(column), "r"(row), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const char *from, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
+/* A tile: rows row .. row + count - 1 of a pass over an expert with the choices first .. first + n - 1 of the list. */
+struct TileAt { uint32_t expert, row, count, first, n; };
+
+template <bool DOWN>
+__global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid_constant__ CUtensorMap map, const __grid_constant__ TilesArgs ta)
+{
+    using S = Tile<DOWN>;
+    const ExpertsArgs &a = ta.e;
+    extern __shared__ __align__(1024) char smem[];                  /* the ring, then the choices by expert */
+    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_scratch[kExpertWarps];
+    __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];            /* experts that have tokens */
+    __shared__ uint16_t s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];   /* choices, passes before each */
+    __shared__ __align__(8) unsigned long long s_full[kMaxRing], s_empty[kMaxRing], s_sums[2], s_free[2];
+    __shared__ uint32_t s_tmem;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const uint32_t stage_bytes = S::weights + S::parts * ta.columns * kSpan;
+    uint16_t *const s_choices = reinterpret_cast<uint16_t *>(smem + ta.stages * stage_bytes);
+    int16_t *const s_expert = reinterpret_cast<int16_t *>(smem);    /* of each choice, until the ring is used */
+    if (!DOWN) grid_wait();
+    grid_let_next_in();                                             /* the choices are complete: the next kernel may read them too */
+
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(shared_at(&s_tmem)), "r"(256u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < ta.stages; ++i) {
+            bar_init(shared_at(&s_full[i]), 1 + kGatherers / 32);
+            bar_init(shared_at(&s_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(shared_at(&s_sums[i]), 1);
+            bar_init(shared_at(&s_free[i]), 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    /* the choices' experts, how many choices each has, which have any */
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kExpertThreads) s_counts[e] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < ta.choices; i += kExpertThreads) {
+        const int e = expert_of(a, i);
+        s_expert[i] = (int16_t)e;
+        if (e >= 0) atomicAdd(&s_counts[e], 1);
+    }
+    __syncthreads();
+    const int active = keep_in_order(a.experts, s_scratch, [&](uint32_t e) { return s_counts[e] > 0; }, [&](int at, uint32_t e) { s_list[at] = (uint16_t)e; });
+    if (warp == 0) {
+        int choices = 0, passes = 0;
+        for (int i0 = 0; i0 < active; i0 += 32) {
+            const int n = i0 + lane < active ? s_counts[s_list[i0 + lane]] : 0, p = (n + (int)ta.columns - 1) / (int)ta.columns;
+            int x = n, y = p;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int ox = __shfl_up_sync(0xFFFFFFFFu, x, d), oy = __shfl_up_sync(0xFFFFFFFFu, y, d);
+                if (lane >= d) { x += ox; y += oy; }
+            }
+            if (i0 + lane < active) {
+                s_first[i0 + lane] = (uint16_t)(choices + x - n);
+                s_passes[i0 + lane] = (uint16_t)(passes + y - p);
+                s_counts[s_list[i0 + lane]] = choices + x - n;
+            }
+            choices += __shfl_sync(0xFFFFFFFFu, x, 31);
+            passes += __shfl_sync(0xFFFFFFFFu, y, 31);
+        }
+        if (lane == 0) { s_first[active] = (uint16_t)choices; s_passes[active] = (uint16_t)passes; }
+        __syncwarp();
+        /* the choices by expert, each expert's in their order, so that all CTAs cut the same passes: 32 at a time */
+        for (uint32_t i0 = 0; i0 < ta.choices; i0 += 32) {
+            const int e = i0 + lane < ta.choices ? s_expert[i0 + lane] : -1;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
+            const int before = __popc(same & ((1u << lane) - 1u)), at = e >= 0 ? s_counts[e] : 0;
+            __syncwarp();
+            if (e >= 0) {
+                s_choices[at + before] = (uint16_t)(i0 + lane);
+                if (before == 0) s_counts[e] = at + __popc(same);
+            }
+            __syncwarp();
+        }
+    }
+    sums_before();
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    /* what was written where the ring is now */
+    __syncthreads();
+    sums_after();
+    const uint32_t tmem = s_tmem;
+
+    /* this CTA's rows: groups of all passes in a row, so that shares differ by one group at most */
+    const uint32_t rows = DOWN ? a.hidden : a.inter, groups = (rows + kGroup - 1) / kGroup, total = s_passes[active] * groups;
+    const uint32_t begin = (uint32_t)((unsigned long long)total * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)total * (blockIdx.x + 1) / gridDim.x);
+    const uint32_t bytes = (DOWN ? a.inter : a.hidden) * 2, steps = (bytes + kSpan - 1) / kSpan;
+    auto for_tiles = [&](auto &&body) {
+        for (uint32_t group = begin; group < end;) {
+            const uint32_t pass = group / groups, g0 = group % groups;
+            int lo = 0, hi = active - 1;                            /* the last expert with no more passes before it */
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (s_passes[mid] <= pass) lo = mid; else hi = mid - 1;
+            }
+            TileAt t;
+            t.expert = s_list[lo];
+            t.first = s_first[lo] + (pass - s_passes[lo]) * ta.columns;
+            t.n = min(ta.columns, s_first[lo + 1] - t.first);
+            /* what is left of this pass in the share, in tiles of nearly equal size */
+            const uint32_t left = min(groups - g0, end - group), tiles = (left + kRows / kGroup - 1) / (kRows / kGroup), mine = (left + tiles - 1) / tiles;
+            t.row = g0 * kGroup;
+            t.count = min(mine * kGroup, rows - t.row);
+            body(t);
+            group += mine;
+        }
+    };
+    bool fine = true;
+    uint32_t stage = 0, phase = 0;                                  /* of this warp's next step; phase: how often the ring went round, mod 2 */
+    auto step_on = [&] { if (++stage == ta.stages) { stage = 0; phase ^= 1; } };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            /* weights are nobody's output: they are fetched before the kernel in front of this one has ended */
+            for_tiles([&](const TileAt &t) {
+                const uint32_t boxes = (t.count + kGroup - 1) / kGroup, row = DOWN ? t.expert * a.hidden + t.row : t.expert * 2 * a.inter + t.row;
+                for (uint32_t s = 0; s < steps; ++s) {
+                    const uint32_t bar = shared_at(&s_full[stage]), to = shared_at(smem) + stage * stage_bytes;
+                    bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
+                    bar_arrive_and_expect(bar, boxes * S::halves * kGroup * kSpan);
+                    for (uint32_t b = 0; b < boxes; ++b) {
+#pragma unroll
+                        for (int h = 0; h < S::halves; ++h)
+                            fetch_rows(to + (h * kRows + b * kGroup) * kSpan, &map, s * (kSpan / 2), row + h * a.inter + b * kGroup, bar);
+                    }
+                    step_on();
+                }
+            });
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t half = 0, round = 0;                           /* of tensor memory */
+            for_tiles([&](const TileAt &t) {
+                const uint32_t width = (t.n + 15) / 16 * 16, to = tmem + half * 128;
+                const uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (width >> 3) << 17 | (kRows >> 4) << 24;     /* binary32 sums of bf16, K-major */
+                bar_wait(shared_at(&s_free[half]), round ^ 1, fine);
+                sums_after();
+                for (uint32_t s = 0; s < steps; ++s) {
+                    bar_wait(shared_at(&s_full[stage]), phase, fine);
+                    sums_after();
+                    const uint32_t at = shared_at(smem) + stage * stage_bytes;
+                    const unsigned long long rows0 = operand(at), cols0 = operand(at + S::weights);
+                    const uint32_t quarters = min(4u, (bytes - s * kSpan + 31) / 32);                              /* of 16 elements */
+                    for (uint32_t k = 0; k < quarters; ++k) {
+                        product(to, rows0 + 2 * k, cols0 + 2 * k, kind, s | k);
+                        if (S::halves == 2) product(to + 64, rows0 + (kRows * kSpan >> 4) + 2 * k, cols0 + 2 * k, kind, s | k);
+                        if (S::parts == 2) product(to, rows0 + 2 * k, cols0 + (ta.columns * kSpan >> 4) + 2 * k, kind, true);
+                    }
+                    tell_when_done(shared_at(&s_empty[stage]));
+                    step_on();
+                }
+                tell_when_done(shared_at(&s_sums[half]));
+                half ^= 1;
+                if (half == 0) round ^= 1;
+            });
+        }
+    } else if (warp < 4) {
+        /* eight lanes per row, eight rows at a time */
+        const uint32_t me = threadIdx.x - 64, r0 = me / 8, piece = me % 8;
+        uint32_t pending = 0, told = 0;                             /* stages filled and not told of; the next one to tell of */
+        auto tell = [&] {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(shared_at(&s_full[told]));
+            if (++told == ta.stages) told = 0;
+            --pending;
+        };
+        if (DOWN) grid_wait();
+        for_tiles([&](const TileAt &t) {
+            const char *cols[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t choice = s_choices[t.first + min(r0 + 8 * i, t.n - 1)];
+                cols[i] = (DOWN ? a.h + (size_t)choice * S::parts * a.h_row : a.x + choice / a.top_k * a.ld_x) + piece * 16;
+            }
+            const uint32_t place = S::weights + r0 * kSpan + ((piece ^ (r0 & 7)) * 16);
+            for (uint32_t s = 0; s < steps; ++s) {
+                const uint32_t to = shared_at(smem) + stage * stage_bytes + place, off = s * kSpan, size = off + piece * 16 < bytes ? 16u : 0u;
+                bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (r0 + 8 * i >= t.n) break;
+#pragma unroll
+                    for (int p = 0; p < S::parts; ++p) copy16(to + (p * ta.columns + 8 * i) * kSpan, cols[i] + (size ? off : 0u) + p * a.h_row, size);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                step_on();
+                if (++pending > kLag) {
+                    asm volatile("cp.async.wait_group %0;" :: "n"(kLag) : "memory");
+                    tell();
+                }
+            }
+        });
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        while (pending) tell();
+    } else {
+        const uint32_t row = (warp - 4) * 32 + lane;
+        uint32_t half = 0, round = 0;
+        if (DOWN) grid_wait();                                      /* what is written was read by kernels in front of this one */
+        for_tiles([&](const TileAt &t) {
+            const uint32_t from = tmem + half * 128 + ((uint32_t)(warp - 4) << 21);
+            /* a lane's choices and their weights: columns lane and lane + 32 */
+            uint32_t choice[2];
+            float weight[2] = {};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                choice[i] = s_choices[t.first + min((uint32_t)lane + 32 * i, t.n - 1)];
+                if (!DOWN && lane + 32 * i < (int)t.n) weight[i] = weight_of(a, choice[i]);
+            }
+            bar_wait(shared_at(&s_sums[half]), round, fine);
+            __syncwarp();
+            sums_after();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                for (uint32_t c = 32 * i; c < t.n && c < 32 * i + 32; c += 8) {
+                    uint32_t v[8], u[8];
+                    read_sums(v, from + c);
+                    if (!DOWN) read_sums(u, from + 64 + c);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t to = __shfl_sync(0xFFFFFFFFu, choice[i], c + k);
+                        const float w = __shfl_sync(0xFFFFFFFFu, weight[i], c + k);
+                        if (c + k >= t.n || row >= t.count) continue;
+                        float x = __uint_as_float(v[k]);
+                        if (!DOWN) x = w * (activate(x, a.activation) * __uint_as_float(u[k]));
+                        if (!fine) x = NAN;
+                        if (DOWN) a.y[(size_t)to * a.hidden + t.row + row] = x;
+                        else store_h<SIFAR_BF16>(a, a.h + (size_t)to * 2 * a.h_row, a.h_row, t.row + row, x);
+                    }
+                }
+            }
+            sums_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(shared_at(&s_free[half]));
+            half ^= 1;
+            if (half == 0) round ^= 1;
+        });
+    }
+    __syncwarp();
+    sums_before();
+    __syncthreads();
+    if (warp == 1) {
+        sums_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(256u));
+    }
+}
+
+/* ------------------------------------------------------------------------ */
+/* host                                                                      */
+/* ------------------------------------------------------------------------ */
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+/* The driver's function by its name: the library does not link against the driver. */
+static EncodeTiled encode_tiled()
+{
+    static const EncodeTiled f = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return (EncodeTiled)p;
+    }();
+    return f;
+}
+
+/* `rows` rows of `cols` bf16 elements, kGroup x 64 at a time. */
+static cudaError_t map_rows(CUtensorMap &map, const void *p, size_t rows, size_t cols, size_t ld_bytes)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t size[2] = {cols, rows}, stride[1] = {ld_bytes};
+    const cuuint32_t box[2] = {kSpan / 2, kGroup}, each[2] = {1, 1};
+    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p), size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <bool DOWN> static cudaError_t launch_tiles(cudaStream_t stream, TilesArgs t)
+{
+    const ExpertsArgs &a = t.e;
+    CUtensorMap map;
+    const cudaError_t bad = DOWN ? map_rows(map, a.down, (size_t)a.experts * a.hidden, a.inter, a.ld_down)
+                                 : map_rows(map, a.gate_up, (size_t)a.experts * 2 * a.inter, a.hidden, a.ld_gate_up);
+    if (bad) return bad;
+    const size_t stage = Tile<DOWN>::weights + Tile<DOWN>::parts * (size_t)t.columns * kSpan;
+    t.stages = (uint32_t)(kRing / stage < kMaxRing ? kRing / stage : kMaxRing);
+    const size_t shared = t.stages * stage + (t.choices * sizeof(uint16_t) + 15) / 16 * 16;
+    if (cudaError_t e = cudaFuncSetAttribute(k_expert_tiles<DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
+    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kExpertThreads), 1, shared, stream, map, t);
+}
+
+cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
+{
+    TilesArgs t;
+    t.e = a;
+    t.choices = a.tokens * a.top_k;
+    /* columns of a pass: four times an expert's share of the choices, were they spread evenly; more take another pass */
+    const uint32_t most = 4 * ((t.choices + a.experts - 1) / a.experts), need = most < a.tokens ? most : a.tokens;
+    t.columns = need <= 16 ? 16 : need <= 32 ? 32 : 64;
+    t.stages = 0;
+    if (cudaError_t e = launch_tiles<false>(stream, t)) return e;
+    return launch_tiles<true>(stream, t);
+}
+
+}  /* namespace sifar */
