@@ -6,11 +6,13 @@
  * read once whatever the number of tokens.  A stage of the ring in shared memory is 64 elements (128 bytes, a swizzle atom)
  * of the tile's rows and of the tokens' rows.  The warps of a CTA have parts of their own and meet only through the stages'
  * barriers:
- *   warp 0      one thread fetches the weights (TMA, 16 rows at a time: no more than the share has)
- *   warp 1      one thread issues the products
+ *   warp 0      fetches the weights (TMA, 128, 64, 32 and 16 rows at a time: no more than the share has)
+ *   warp 1      issues the products
  *   warps 2, 3  gather the tokens' rows (asynchronous 16-byte copies)
  *   warps 4 - 7 take a tile's sums out of tensor memory while the next tile's go into its other half
- * What bounds it is the memory; the ring keeps up to 160 KB of weights per SM on the way, across tiles.
+ * What bounds it is the memory; the ring keeps up to 160 KB of weights per SM on the way, across tiles.  Warps 0 and 1 go through
+ * their loops as whole warps and one lane issues: what an instruction of these needs is in uniform registers then (as one thread's
+ * loop, a product took 150 cycles to issue and a fetch 90).
  *
  * First product: a tile is 128 gate rows and the 128 up rows that go with them, two accumulators; a thread then has both values of
  * its row.  Second product: the values come as two bf16 parts, and both go into one accumulator.
@@ -48,15 +50,23 @@ __device__ __forceinline__ unsigned long long operand(uint32_t at)
 {
     return (unsigned long long)((at & 0x3FFFFu) >> 4) | 1ull << 16 | (unsigned long long)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
-__device__ __forceinline__ void product(uint32_t to, unsigned long long rows, unsigned long long cols, uint32_t kind, bool add)
+/* These are gone through by a whole warp and issued by the lane whose `leader` is not 0. */
+__device__ __forceinline__ uint32_t elect_leader()
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(to), "l"(rows), "l"(cols), "r"(kind), "r"((uint32_t)add) : "memory");
+    uint32_t leader;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(leader));
+    return leader;
+}
+__device__ __forceinline__ void product(uint32_t leader, uint32_t to, unsigned long long rows, unsigned long long cols, uint32_t kind, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(to), "l"(rows), "l"(cols), "r"(kind), "r"((uint32_t)add), "r"(leader) : "memory");
 }
 /* The barrier is told when all products issued so far are done. */
-__device__ __forceinline__ void tell_when_done(uint32_t bar)
+__device__ __forceinline__ void tell_when_done(uint32_t leader, uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+                 :: "r"(bar), "r"(leader) : "memory");
 }
 __device__ __forceinline__ void sums_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void sums_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -68,9 +78,9 @@ __device__ __forceinline__ void read_sums(uint32_t (&v)[8], uint32_t at)
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
-__device__ __forceinline__ void bar_arrive_and_expect(uint32_t bar, uint32_t bytes)
+__device__ __forceinline__ void bar_arrive_and_expect(uint32_t leader, uint32_t bar, uint32_t bytes)
 {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" :: "r"(bar), "r"(bytes), "r"(leader) : "memory");
 }
 /* Waits until the barrier's phase `parity` is over.  `fine` turns false where that takes too long; nothing is waited for after that. */
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, bool &fine)
@@ -84,11 +94,12 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, bool &fi
     }
 }
 
-/* kGroup rows x 64 elements from (column, row) on. */
-__device__ __forceinline__ void fetch_rows(uint32_t to, const CUtensorMap *map, uint32_t column, uint32_t row, uint32_t bar)
+/* The map's number of rows x 64 elements from (column, row) on. */
+__device__ __forceinline__ void fetch_rows(uint32_t leader, uint32_t to, const CUtensorMap *map, uint32_t column, uint32_t row, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 :: "r"(to), "l"(map), "r"(column), "r"(row), "r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "@q cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                 :: "r"(to), "l"(map), "r"(column), "r"(row), "r"(bar), "r"(leader) : "memory");
 }
 __device__ __forceinline__ void copy16(uint32_t to, const char *from, uint32_t bytes)
 {
@@ -98,8 +109,11 @@ __device__ __forceinline__ void copy16(uint32_t to, const char *from, uint32_t b
 /* A tile: rows row .. row + count - 1 of a pass over an expert with the choices first .. first + n - 1 of the list. */
 struct TileAt { uint32_t expert, row, count, first, n; };
 
+/* The same rows, 128 >> i at a time. */
+struct RowMaps { CUtensorMap of[4]; };
+
 template <bool DOWN>
-__global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid_constant__ CUtensorMap map, const __grid_constant__ TilesArgs ta)
+__global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid_constant__ RowMaps maps, const __grid_constant__ TilesArgs ta)
 {
     using S = Tile<DOWN>;
     const ExpertsArgs &a = ta.e;
@@ -112,7 +126,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const uint32_t stage_bytes = S::weights + S::parts * ta.columns * kSpan;
     uint16_t *const s_choices = reinterpret_cast<uint16_t *>(smem + ta.stages * stage_bytes);
-    int16_t *const s_expert = reinterpret_cast<int16_t *>(smem);    /* of each choice, until the ring is used */
+    int *const s_index = reinterpret_cast<int *>(smem);             /* the choices as they come, until the ring is used */
     if (!DOWN) grid_wait();
     grid_let_next_in();                                             /* the choices are complete: the next kernel may read them too */
 
@@ -131,13 +145,22 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    /* the choices' experts, how many choices each has, which have any */
+    /* the experts' choices in any order, which experts have any */
     for (uint32_t e = threadIdx.x; e < a.experts; e += kExpertThreads) s_counts[e] = 0;
+    for (uint32_t i = threadIdx.x; i < ta.choices; i += kExpertThreads) s_index[i] = a.indices[i];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < ta.choices; i += kExpertThreads) {
-        const int e = expert_of(a, i);
-        s_expert[i] = (int16_t)e;
-        if (e >= 0) atomicAdd(&s_counts[e], 1);
+    constexpr int kMine = SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K / kExpertThreads;
+    int16_t mine[kMine], place[kMine];
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+        const uint32_t i = m * kExpertThreads + threadIdx.x;
+        if (m * kExpertThreads >= ta.choices) break;
+        const long long e = i < ta.choices ? (long long)s_index[i] - a.first : -1;
+        bool on = e >= 0 && e < (long long)a.experts;
+        if (on)
+            for (uint32_t j = i - i % a.top_k; j < i; ++j) on = on && s_index[j] != s_index[i];     /* its token's first of this expert */
+        mine[m] = on ? (int16_t)e : (int16_t)-1;
+        if (on) place[m] = (int16_t)atomicAdd(&s_counts[(int)e], 1);
     }
     __syncthreads();
     const int active = keep_in_order(a.experts, s_scratch, [&](uint32_t e) { return s_counts[e] > 0; }, [&](int at, uint32_t e) { s_list[at] = (uint16_t)e; });
@@ -160,19 +183,33 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
             passes += __shfl_sync(0xFFFFFFFFu, y, 31);
         }
         if (lane == 0) { s_first[active] = (uint16_t)choices; s_passes[active] = (uint16_t)passes; }
-        __syncwarp();
-        /* the choices by expert, each expert's in their order, so that all CTAs cut the same passes: 32 at a time */
-        for (uint32_t i0 = 0; i0 < ta.choices; i0 += 32) {
-            const int e = i0 + lane < ta.choices ? s_expert[i0 + lane] : -1;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
-            const int before = __popc(same & ((1u << lane) - 1u)), at = e >= 0 ? s_counts[e] : 0;
-            __syncwarp();
-            if (e >= 0) {
-                s_choices[at + before] = (uint16_t)(i0 + lane);
-                if (before == 0) s_counts[e] = at + __popc(same);
-            }
-            __syncwarp();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+        if (m * kExpertThreads >= ta.choices) break;
+        if (mine[m] >= 0) s_choices[s_counts[mine[m]] + place[m]] = (uint16_t)(m * kExpertThreads + threadIdx.x);
+    }
+    __syncthreads();
+    /* of an expert that takes several passes the choices in their order: all CTAs have to cut the same ones */
+    for (int i = warp; i < active; i += kExpertWarps) {
+        const int n = s_first[i + 1] - s_first[i];
+        if (n <= (int)ta.columns) continue;
+        uint16_t *const list = s_choices + s_first[i];
+        constexpr int kPer = SIFAR_EXPERTS_MAX_TOKENS / 32;
+        uint16_t v[kPer];
+        int rank[kPer];
+#pragma unroll
+        for (int m = 0; m < kPer; ++m) { v[m] = m * 32 + lane < n ? list[m * 32 + lane] : (uint16_t)0; rank[m] = 0; }
+        for (int j = 0; j < n; ++j) {
+            const uint16_t o = list[j];
+#pragma unroll
+            for (int m = 0; m < kPer; ++m) rank[m] += o < v[m] ? 1 : 0;
         }
+        __syncwarp();
+#pragma unroll
+        for (int m = 0; m < kPer; ++m)
+            if (m * 32 + lane < n) list[rank[m]] = v[m];
     }
     sums_before();
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    /* what was written where the ring is now */
@@ -196,8 +233,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
             t.expert = s_list[lo];
             t.first = s_first[lo] + (pass - s_passes[lo]) * ta.columns;
             t.n = min(ta.columns, s_first[lo + 1] - t.first);
-            /* what is left of this pass in the share, in tiles of nearly equal size */
-            const uint32_t left = min(groups - g0, end - group), tiles = (left + kRows / kGroup - 1) / (kRows / kGroup), mine = (left + tiles - 1) / tiles;
+            const uint32_t mine = min(min(groups - g0, end - group), (uint32_t)(kRows / kGroup));
             t.row = g0 * kGroup;
             t.count = min(mine * kGroup, rows - t.row);
             body(t);
@@ -209,50 +245,54 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
     auto step_on = [&] { if (++stage == ta.stages) { stage = 0; phase ^= 1; } };
 
     if (warp == 0) {
-        if (lane == 0) {
-            /* weights are nobody's output: they are fetched before the kernel in front of this one has ended */
-            for_tiles([&](const TileAt &t) {
-                const uint32_t boxes = (t.count + kGroup - 1) / kGroup, row = DOWN ? t.expert * a.hidden + t.row : t.expert * 2 * a.inter + t.row;
-                for (uint32_t s = 0; s < steps; ++s) {
-                    const uint32_t bar = shared_at(&s_full[stage]), to = shared_at(smem) + stage * stage_bytes;
-                    bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
-                    bar_arrive_and_expect(bar, boxes * S::halves * kGroup * kSpan);
-                    for (uint32_t b = 0; b < boxes; ++b) {
+        /* weights are nobody's output: they are fetched before the kernel in front of this one has ended */
+        const uint32_t leader = elect_leader();
+        for_tiles([&](const TileAt &t) {
+            const uint32_t row = DOWN ? t.expert * a.hidden + t.row : t.expert * 2 * a.inter + t.row, boxes = (t.count + kGroup - 1) / kGroup;
+            for (uint32_t s = 0; s < steps; ++s) {
+                const uint32_t bar = shared_at(&s_full[stage]), to = shared_at(smem) + stage * stage_bytes;
+                bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
+                bar_arrive_and_expect(leader, bar, boxes * S::halves * kGroup * kSpan);
+                uint32_t from = 0;
 #pragma unroll
-                        for (int h = 0; h < S::halves; ++h)
-                            fetch_rows(to + (h * kRows + b * kGroup) * kSpan, &map, s * (kSpan / 2), row + h * a.inter + b * kGroup, bar);
-                    }
-                    step_on();
+                for (int i = 0; i < 4; ++i) {
+                    if (!(boxes & (8u >> i))) continue;
+#pragma unroll
+                    for (int h = 0; h < S::halves; ++h)
+                        fetch_rows(leader, to + (h * kRows + from) * kSpan, &maps.of[i], s * (kSpan / 2), row + h * a.inter + from, bar);
+                    from += 128u >> i;
                 }
-            });
-        }
+                step_on();
+            }
+        });
     } else if (warp == 1) {
-        if (lane == 0) {
-            uint32_t half = 0, round = 0;                           /* of tensor memory */
-            for_tiles([&](const TileAt &t) {
-                const uint32_t width = (t.n + 15) / 16 * 16, to = tmem + half * 128;
-                const uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (width >> 3) << 17 | (kRows >> 4) << 24;     /* binary32 sums of bf16, K-major */
-                bar_wait(shared_at(&s_free[half]), round ^ 1, fine);
+        const uint32_t leader = elect_leader();
+        uint32_t half = 0, round = 0;                               /* of tensor memory */
+        for_tiles([&](const TileAt &t) {
+            const uint32_t width = (t.n + 15) / 16 * 16, to = tmem + half * 128;
+            const uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (width >> 3) << 17 | (kRows >> 4) << 24;     /* binary32 sums of bf16, K-major */
+            bar_wait(shared_at(&s_free[half]), round ^ 1, fine);
+            sums_after();
+            for (uint32_t s = 0; s < steps; ++s) {
+                bar_wait(shared_at(&s_full[stage]), phase, fine);
                 sums_after();
-                for (uint32_t s = 0; s < steps; ++s) {
-                    bar_wait(shared_at(&s_full[stage]), phase, fine);
-                    sums_after();
-                    const uint32_t at = shared_at(smem) + stage * stage_bytes;
-                    const unsigned long long rows0 = operand(at), cols0 = operand(at + S::weights);
-                    const uint32_t quarters = min(4u, (bytes - s * kSpan + 31) / 32);                              /* of 16 elements */
-                    for (uint32_t k = 0; k < quarters; ++k) {
-                        product(to, rows0 + 2 * k, cols0 + 2 * k, kind, s | k);
-                        if (S::halves == 2) product(to + 64, rows0 + (kRows * kSpan >> 4) + 2 * k, cols0 + 2 * k, kind, s | k);
-                        if (S::parts == 2) product(to, rows0 + 2 * k, cols0 + (ta.columns * kSpan >> 4) + 2 * k, kind, true);
-                    }
-                    tell_when_done(shared_at(&s_empty[stage]));
-                    step_on();
+                const uint32_t at = shared_at(smem) + stage * stage_bytes;
+                const unsigned long long rows0 = operand(at), cols0 = operand(at + S::weights);
+                const uint32_t quarters = (bytes - s * kSpan + 31) / 32;                                       /* of 16 elements */
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    if (k >= quarters) break;
+                    product(leader, to, rows0 + 2 * k, cols0 + 2 * k, kind, s | k);
+                    if (S::halves == 2) product(leader, to + 64, rows0 + (kRows * kSpan >> 4) + 2 * k, cols0 + 2 * k, kind, s | k);
+                    if (S::parts == 2) product(leader, to, rows0 + 2 * k, cols0 + (ta.columns * kSpan >> 4) + 2 * k, kind, true);
                 }
-                tell_when_done(shared_at(&s_sums[half]));
-                half ^= 1;
-                if (half == 0) round ^= 1;
-            });
-        }
+                tell_when_done(leader, shared_at(&s_empty[stage]));
+                step_on();
+            }
+            tell_when_done(leader, shared_at(&s_sums[half]));
+            half ^= 1;
+            if (half == 0) round ^= 1;
+        });
     } else if (warp < 4) {
         /* eight lanes per row, eight rows at a time */
         const uint32_t me = threadIdx.x - 64, r0 = me / 8, piece = me % 8;
@@ -366,29 +406,33 @@ static EncodeTiled encode_tiled()
     return f;
 }
 
-/* `rows` rows of `cols` bf16 elements, kGroup x 64 at a time. */
-static cudaError_t map_rows(CUtensorMap &map, const void *p, size_t rows, size_t cols, size_t ld_bytes)
+/* `rows` rows of `cols` bf16 elements. */
+static cudaError_t map_rows(RowMaps &maps, const void *p, size_t rows, size_t cols, size_t ld_bytes)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return cudaErrorNotSupported;
     const cuuint64_t size[2] = {cols, rows}, stride[1] = {ld_bytes};
-    const cuuint32_t box[2] = {kSpan / 2, kGroup}, each[2] = {1, 1};
-    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p), size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    for (int i = 0; i < 4; ++i) {
+        const cuuint32_t box[2] = {kSpan / 2, 128u >> i}, each[2] = {1, 1};
+        if (encode(&maps.of[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(p), size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    return cudaSuccess;
 }
 
 template <bool DOWN> static cudaError_t launch_tiles(cudaStream_t stream, TilesArgs t)
 {
     const ExpertsArgs &a = t.e;
-    CUtensorMap map;
-    const cudaError_t bad = DOWN ? map_rows(map, a.down, (size_t)a.experts * a.hidden, a.inter, a.ld_down)
-                                 : map_rows(map, a.gate_up, (size_t)a.experts * 2 * a.inter, a.hidden, a.ld_gate_up);
+    RowMaps maps;
+    const cudaError_t bad = DOWN ? map_rows(maps, a.down, (size_t)a.experts * a.hidden, a.inter, a.ld_down)
+                                 : map_rows(maps, a.gate_up, (size_t)a.experts * 2 * a.inter, a.hidden, a.ld_gate_up);
     if (bad) return bad;
     const size_t stage = Tile<DOWN>::weights + Tile<DOWN>::parts * (size_t)t.columns * kSpan;
     t.stages = (uint32_t)(kRing / stage < kMaxRing ? kRing / stage : kMaxRing);
     const size_t shared = t.stages * stage + (t.choices * sizeof(uint16_t) + 15) / 16 * 16;
     if (cudaError_t e = cudaFuncSetAttribute(k_expert_tiles<DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
-    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kExpertThreads), 1, shared, stream, map, t);
+    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kExpertThreads), 1, shared, stream, maps, t);
 }
 
 cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
