@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
             } else {
                 const uint32_t r = at.tile * 64 + warp * 8 + g;
                 if (r >= a.inter) return;
-                const float v = weight_of(a, slot) * (activate(first, a.activation) * second);
+                const float v = weight_of(a, slot / a.top_k, s_list[at.which]) * (activate(first, a.activation) * second);
                 store_h<DT>(a, a.h + (size_t)slot * (DT == SIFAR_BF16 ? 2 : 1) * a.h_row, a.h_row, r, v);
             }
         };
@@ -489,23 +489,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
     }
 }
 
-/* out_t = the sum over its choices here, in their order. */
+/* out_t = the sum over its choices here, in their order; a second choice of the same expert has its share in the first. */
 template <int DT>
 __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ ExpertsArgs a)
 {
-    __shared__ int s_slot[SIFAR_ROUTE_MAX_TOP_K];
+    __shared__ int s_row[SIFAR_ROUTE_MAX_TOP_K];
     const uint32_t t = blockIdx.y, c0 = (blockIdx.x * kThreads + threadIdx.x) * 4;
-    if (threadIdx.x < a.top_k) s_slot[threadIdx.x] = expert_of(a, t * a.top_k + threadIdx.x);
-    __syncthreads();
+    const uint32_t mine = t * a.top_k + threadIdx.x;
+    int row = threadIdx.x < a.top_k && expert_of(a, mine) >= 0 ? (int)mine : -1;        /* the choices were complete long ago */
     grid_wait();
     grid_let_next_in();
+    if (a.place && row >= 0) row = __ldcg(a.place + mine);
+    if (threadIdx.x < a.top_k) s_row[threadIdx.x] = row;
+    __syncthreads();
     if (c0 >= a.hidden) return;
     float v[4] = {};
     const bool vec = a.hidden % 4 == 0;
 #pragma unroll 4
     for (uint32_t k = 0; k < a.top_k; ++k) {
-        if (s_slot[k] < 0) continue;
-        const float *const y = a.y + (size_t)(t * a.top_k + k) * a.hidden + c0;
+        if (s_row[k] < 0) continue;
+        const float *const y = a.y + (size_t)s_row[k] * a.hidden + c0;
         if (vec) {
             const float4 w = __ldcg(reinterpret_cast<const float4 *>(y));
             v[0] += w.x; v[1] += w.y; v[2] += w.z; v[3] += w.w;
@@ -524,7 +527,7 @@ __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ Exp
 /* ------------------------------------------------------------------------ */
 /* host                                                                      */
 /* ------------------------------------------------------------------------ */
-struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, bytes; };
+struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, y_bytes, bytes; };
 
 constexpr size_t kFewShared = 100 * 1024;    /* the tokens' rows in shared memory: two CTAs of 8 warps per SM */
 
@@ -547,7 +550,8 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     p.h_row = (uint32_t)((g->inter * es + 15) / 16 * 16);
     const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
     p.h_bytes = ((p.few ? most * T : choices) * parts * p.h_row + 15) / 16 * 16;
-    p.bytes = p.h_bytes + (p.few ? 0 : choices * g->hidden * sizeof(float));
+    p.y_bytes = p.few ? 0 : (choices * g->hidden * sizeof(float) + 15) / 16 * 16;
+    p.bytes = p.h_bytes + p.y_bytes + (p.few ? 0 : choices * sizeof(int));
     return SIFAR_OK;
 }
 
@@ -560,7 +564,7 @@ static cudaError_t launch_shared(void (*kernel)(P...), dim3 grid, size_t shared,
 }
 
 template <int DT>
-static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, const ExpertsArgs &a)
+static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, ExpertsArgs a)
 {
     const dim3 grid(2 * kSms);
     cudaError_t e;
@@ -575,6 +579,7 @@ static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec
         return dn_vec ? launch_shared(k_down_few<DT, true, false>, columns, 0, stream, a) : launch_shared(k_down_few<DT, false, false>, columns, 0, stream, a);
     }
     if (DT == SIFAR_BF16 && gu_vec && dn_vec && x_vec) {
+        a.place = (int *)((char *)a.y + p.y_bytes);
         e = launch_expert_tiles(stream, a);
         if (e) return e;
         return launch_shared(k_gather<DT>, dim3((a.hidden + 4 * kThreads - 1) / (4 * kThreads), a.tokens), 0, stream, a);
@@ -628,7 +633,7 @@ extern "C" int sifar_experts(const sifar_experts_args *g, void *stream)
     ExpertsArgs a;
     a.x = (const char *)g->x; a.gate_up = (const char *)g->gate_up; a.down = (const char *)g->down; a.out = (char *)g->out;
     a.indices = g->indices; a.weights = g->weights;
-    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes);
+    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes); a.place = nullptr;
     a.ld_x = all[0].ld * es; a.ld_gate_up = all[3].ld * es; a.ld_down = all[4].ld * es; a.ld_out = all[5].ld * es;
     a.tokens = (uint32_t)T; a.hidden = (uint32_t)H; a.inter = (uint32_t)I; a.h_row = p.h_row; a.top_k = (uint32_t)g->top_k;
     a.experts = (uint32_t)E; a.first = g->first_expert; a.activation = g->activation; a.x_row = p.x_row;

@@ -17,8 +17,10 @@ struct ExpertsArgs {
     char *out;
     const int *indices;
     const float *weights;
-    char *h;                                 /* few: [active][plane][token], many: [token][choice][plane], rows of h_row bytes */
-    float *y;                                /* many: [token][choice][hidden] */
+    char *h;                                 /* between the products, rows of h_row bytes.  few: [active][part][token], tiles: [place][part],
+                                                else [token][choice][part] */
+    float *y;                                /* tiles: [place][hidden], else [token][choice][hidden] */
+    int *place;                              /* tiles: of each choice in the list by experts, or -1 */
     unsigned long long ld_x, ld_gate_up, ld_down, ld_out;    /* bytes */
     uint32_t tokens, hidden, inter, h_row, top_k, experts;
     int first, activation;
@@ -49,22 +51,31 @@ template <int DT> __device__ __forceinline__ void store_h(const ExpertsArgs &a, 
 /* ------------------------------------------------------------------------ */
 /* which experts                                                             */
 /* ------------------------------------------------------------------------ */
+/* An index as a number of this rank's experts; not below their number where it is another's. */
+__device__ __forceinline__ uint32_t local_expert(const ExpertsArgs &a, int index)
+{
+    return index < a.first ? 0xFFFFFFFFu : (uint32_t)index - (uint32_t)a.first;
+}
+
 /* The expert (0 .. experts - 1) that choice i is the token's first one of, or -1: another rank's, or its second. */
 __device__ __forceinline__ int expert_of(const ExpertsArgs &a, uint32_t i)
 {
-    const long long e = (long long)a.indices[i] - a.first;
-    if (e < 0 || e >= (long long)a.experts) return -1;
+    const uint32_t e = local_expert(a, a.indices[i]);
+    if (e >= a.experts) return -1;
     for (uint32_t j = i - i % a.top_k; j < i; ++j)
         if (a.indices[j] == a.indices[i]) return -1;
     return (int)e;
 }
-/* The weight of the token that choice i belongs to, for the choice's expert. */
-__device__ __forceinline__ float weight_of(const ExpertsArgs &a, uint32_t i)
+/* The token's weight for an expert: that of all its choices of it. */
+__device__ __forceinline__ float weight_of(const ExpertsArgs &a, uint32_t token, int expert)
 {
-    const uint32_t j0 = i - i % a.top_k;
+    const int *const at = a.indices + token * a.top_k;
+    const float *const weights = a.weights + token * a.top_k;
+    const uint32_t wanted = (uint32_t)expert + (uint32_t)a.first;
     float w = 0.0f;
-    for (uint32_t j = j0; j < j0 + a.top_k; ++j)
-        if (a.indices[j] == a.indices[i]) w += a.weights[j];
+#pragma unroll 4
+    for (uint32_t j = 0; j < a.top_k; ++j)
+        if ((uint32_t)at[j] == wanted) w += weights[j];
     return w;
 }
 
@@ -104,7 +115,7 @@ __device__ __forceinline__ int list_experts(const ExpertsArgs &a, int *counts, i
     return keep_in_order(a.experts, scratch, [&](uint32_t e) { return counts[e] > 0; }, [&](int at, uint32_t e) { list[at] = (int)e; });
 }
 
-/* bf16 rows of whole 16-byte pieces, more tokens than k_up_few takes: the two products, up to k_gather. */
+/* bf16 rows of whole 16-byte pieces, more tokens than k_up_few takes: the two products, up to k_gather, and `place` for it. */
 cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a);
 
 }  /* namespace sifar */

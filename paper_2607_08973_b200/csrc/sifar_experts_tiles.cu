@@ -25,22 +25,22 @@ namespace sifar {
 
 constexpr int kRows = 128;                   /* of an instruction */
 constexpr int kSpan = 128;                   /* bytes of a row in a stage */
-constexpr int kGroup = 16;                   /* rows that shares are counted in, and that a fetch of weights has */
-constexpr int kRing = 198 * 1024;            /* bytes of all stages: what the lists leave of an SM's 227 KB */
+constexpr int kGroup = 16;                   /* rows that tiles are counted in, and that the smallest fetch of weights has */
+constexpr int kGroups = kRows / kGroup;
+constexpr int kRing = 204 * 1024;            /* bytes of all stages: what the lists leave of an SM's 227 KB */
 constexpr int kMaxRing = 8;
 constexpr int kGatherers = 64;               /* threads that gather the tokens' rows */
-constexpr int kLag = 2;                      /* stages that they have under way while they fill another */
+constexpr int kLag = 3;                      /* stages that they have under way while they fill another: less than a ring has */
 constexpr uint32_t kPolls = 1u << 22;        /* a wait's limit: about 0.1 s, where the products take less than a microsecond */
 
 template <bool DOWN> struct Tile {
     static constexpr int halves = DOWN ? 1 : 2;                  /* blocks of kRows weight rows */
     static constexpr int parts = DOWN ? 2 : 1;                   /* of the tokens' values */
-    static constexpr int weights = halves * kRows * kSpan;       /* bytes of a stage */
 };
 
 struct TilesArgs {
     ExpertsArgs e;
-    uint32_t columns, stages, choices;       /* columns of a pass over an expert's rows */
+    uint32_t columns;                        /* of a pass over an expert's rows */
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -106,7 +106,7 @@ __device__ __forceinline__ void copy16(uint32_t to, const char *from, uint32_t b
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
 }
 
-/* A tile: rows row .. row + count - 1 of a pass over an expert with the choices first .. first + n - 1 of the list. */
+/* A tile: rows row .. row + count - 1 of a pass over an expert with the tokens first .. first + n - 1 of the list. */
 struct TileAt { uint32_t expert, row, count, first, n; };
 
 /* The same rows, 128 >> i at a time. */
@@ -117,16 +117,18 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
 {
     using S = Tile<DOWN>;
     const ExpertsArgs &a = ta.e;
-    extern __shared__ __align__(1024) char smem[];                  /* the ring, then the choices by expert */
-    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_scratch[kExpertWarps];
+    extern __shared__ __align__(1024) char smem[];                  /* the ring; at first each expert's tokens as bits */
+    __shared__ uint16_t s_place[SIFAR_ROUTE_MAX_EXPERTS];           /* of an expert's first token in the list */
     __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];            /* experts that have tokens */
-    __shared__ uint16_t s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];   /* choices, passes before each */
+    __shared__ uint16_t s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];   /* tokens of the list, passes before each */
+    __shared__ uint8_t s_token[SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K];      /* the tokens by expert, in their order */
+    __shared__ unsigned long long s_sum[kExpertWarps];
     __shared__ __align__(8) unsigned long long s_full[kMaxRing], s_empty[kMaxRing], s_sums[2], s_free[2];
     __shared__ uint32_t s_tmem;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-    const uint32_t stage_bytes = S::weights + S::parts * ta.columns * kSpan;
-    uint16_t *const s_choices = reinterpret_cast<uint16_t *>(smem + ta.stages * stage_bytes);
-    int *const s_index = reinterpret_cast<int *>(smem);             /* the choices as they come, until the ring is used */
+    uint32_t *const s_bits = reinterpret_cast<uint32_t *>(smem);
+    const uint32_t words = (a.tokens + 31) / 32, choices = a.tokens * a.top_k;
+    if (warp == 0 && lane < 4) asm volatile("prefetch.tensormap [%0];" :: "l"(&maps.of[lane]) : "memory");
     if (!DOWN) grid_wait();
     grid_let_next_in();                                             /* the choices are complete: the next kernel may read them too */
 
@@ -135,7 +137,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < ta.stages; ++i) {
+        for (int i = 0; i < kMaxRing; ++i) {
             bar_init(shared_at(&s_full[i]), 1 + kGatherers / 32);
             bar_init(shared_at(&s_empty[i]), 1);
         }
@@ -145,85 +147,87 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    /* the experts' choices in any order, which experts have any */
-    for (uint32_t e = threadIdx.x; e < a.experts; e += kExpertThreads) s_counts[e] = 0;
-    for (uint32_t i = threadIdx.x; i < ta.choices; i += kExpertThreads) s_index[i] = a.indices[i];
+    /* a bit per expert and token that chose it (twice: once): an expert's tokens are counted and numbered by bits, in the same order
+       in every CTA */
+    for (uint32_t i = threadIdx.x; i < a.experts * words; i += kExpertThreads) s_bits[i] = 0u;
     __syncthreads();
-    constexpr int kMine = SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K / kExpertThreads;
-    int16_t mine[kMine], place[kMine];
-#pragma unroll
-    for (int m = 0; m < kMine; ++m) {
-        const uint32_t i = m * kExpertThreads + threadIdx.x;
-        if (m * kExpertThreads >= ta.choices) break;
-        const long long e = i < ta.choices ? (long long)s_index[i] - a.first : -1;
-        bool on = e >= 0 && e < (long long)a.experts;
-        if (on)
-            for (uint32_t j = i - i % a.top_k; j < i; ++j) on = on && s_index[j] != s_index[i];     /* its token's first of this expert */
-        mine[m] = on ? (int16_t)e : (int16_t)-1;
-        if (on) place[m] = (int16_t)atomicAdd(&s_counts[(int)e], 1);
+    for (uint32_t i = threadIdx.x; i < choices; i += kExpertThreads) {
+        const uint32_t e = local_expert(a, a.indices[i]), token = i / a.top_k;
+        if (e < a.experts) atomicOr(&s_bits[e * words + token / 32], 1u << (token % 32));
     }
     __syncthreads();
-    const int active = keep_in_order(a.experts, s_scratch, [&](uint32_t e) { return s_counts[e] > 0; }, [&](int at, uint32_t e) { s_list[at] = (uint16_t)e; });
-    if (warp == 0) {
-        int choices = 0, passes = 0;
-        for (int i0 = 0; i0 < active; i0 += 32) {
-            const int n = i0 + lane < active ? s_counts[s_list[i0 + lane]] : 0, p = (n + (int)ta.columns - 1) / (int)ta.columns;
-            int x = n, y = p;
+    /* in one sum over the experts: how many have tokens, their tokens, their passes */
+    constexpr uint32_t kEach = SIFAR_ROUTE_MAX_EXPERTS / kExpertThreads;
+    uint32_t n[kEach];
+    unsigned long long mine = 0;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int ox = __shfl_up_sync(0xFFFFFFFFu, x, d), oy = __shfl_up_sync(0xFFFFFFFFu, y, d);
-                if (lane >= d) { x += ox; y += oy; }
-            }
-            if (i0 + lane < active) {
-                s_first[i0 + lane] = (uint16_t)(choices + x - n);
-                s_passes[i0 + lane] = (uint16_t)(passes + y - p);
-                s_counts[s_list[i0 + lane]] = choices + x - n;
-            }
-            choices += __shfl_sync(0xFFFFFFFFu, x, 31);
-            passes += __shfl_sync(0xFFFFFFFFu, y, 31);
-        }
-        if (lane == 0) { s_first[active] = (uint16_t)choices; s_passes[active] = (uint16_t)passes; }
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = threadIdx.x * kEach + i;
+        n[i] = 0;
+        if (e < a.experts)
+            for (uint32_t w = 0; w < words; ++w) n[i] += __popc(s_bits[e * words + w]);
+        mine += (unsigned long long)(n[i] ? 1u : 0u) << 40 | (unsigned long long)n[i] << 20 | (n[i] + ta.columns - 1) / ta.columns;
     }
-    __syncthreads();
+    unsigned long long upto = mine;
 #pragma unroll
-    for (int m = 0; m < kMine; ++m) {
-        if (m * kExpertThreads >= ta.choices) break;
-        if (mine[m] >= 0) s_choices[s_counts[mine[m]] + place[m]] = (uint16_t)(m * kExpertThreads + threadIdx.x);
+    for (int d = 1; d < 32; d <<= 1) {
+        const unsigned long long o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += o;
     }
-    __syncthreads();
-    /* of an expert that takes several passes the choices in their order: all CTAs have to cut the same ones */
-    for (int i = warp; i < active; i += kExpertWarps) {
-        const int n = s_first[i + 1] - s_first[i];
-        if (n <= (int)ta.columns) continue;
-        uint16_t *const list = s_choices + s_first[i];
-        constexpr int kPer = SIFAR_EXPERTS_MAX_TOKENS / 32;
-        uint16_t v[kPer];
-        int rank[kPer];
-#pragma unroll
-        for (int m = 0; m < kPer; ++m) { v[m] = m * 32 + lane < n ? list[m * 32 + lane] : (uint16_t)0; rank[m] = 0; }
-        for (int j = 0; j < n; ++j) {
-            const uint16_t o = list[j];
-#pragma unroll
-            for (int m = 0; m < kPer; ++m) rank[m] += o < v[m] ? 1 : 0;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int m = 0; m < kPer; ++m)
-            if (m * 32 + lane < n) list[rank[m]] = v[m];
-    }
-    sums_before();
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    /* what was written where the ring is now */
+    if (lane == 31) s_sum[warp] = upto;
+    sums_before();                                                  /* the address of tensor memory, too */
     __syncthreads();
     sums_after();
+    unsigned long long before = upto - mine, all = 0;
+#pragma unroll
+    for (int w = 0; w < kExpertWarps; ++w) {
+        if (w < warp) before += s_sum[w];
+        all += s_sum[w];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        if (!n[i]) continue;
+        const uint32_t e = threadIdx.x * kEach + i, at = (uint32_t)(before >> 40), first = (uint32_t)(before >> 20) & 0xFFFFFu;
+        s_list[at] = (uint16_t)e;
+        s_place[e] = s_first[at] = (uint16_t)first;
+        s_passes[at] = (uint16_t)(before & 0xFFFFFu);
+        before += 1ull << 40 | (unsigned long long)n[i] << 20 | (n[i] + ta.columns - 1) / ta.columns;
+    }
+    const int active = (int)(all >> 40);
+    if (threadIdx.x == 0) {
+        s_first[active] = (uint16_t)((all >> 20) & 0xFFFFFu);
+        s_passes[active] = (uint16_t)(all & 0xFFFFFu);
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < choices; i += kExpertThreads) {
+        const uint32_t e = local_expert(a, a.indices[i]), token = i / a.top_k;
+        int at = -1;
+        if (e < a.experts) {
+            at = s_place[e] + __popc(s_bits[e * words + token / 32] & ((1u << (token % 32)) - 1u));
+            for (uint32_t w = 0; w < token / 32; ++w) at += __popc(s_bits[e * words + w]);
+            s_token[at] = (uint8_t)token;
+        }
+        if (!DOWN && blockIdx.x == 0) a.place[i] = at;              /* for the sum over a token's choices */
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    /* what was read and written where the ring is now */
+    __syncthreads();
     const uint32_t tmem = s_tmem;
 
-    /* this CTA's rows: groups of all passes in a row, so that shares differ by one group at most */
-    const uint32_t rows = DOWN ? a.hidden : a.inter, groups = (rows + kGroup - 1) / kGroup, total = s_passes[active] * groups;
+    /* Groups of a tile: as many as the fullest CTA gets through soonest (lane s - 1 looks at s).  A tile of few groups is not
+       faster than its products, 0.15 to 0.27 us a step: as the weights of 1.6 to 2.8 groups, and half as large ones of DOWN. */
+    const uint32_t rows = DOWN ? a.hidden : a.inter, groups = (rows + kGroup - 1) / kGroup, passes = (uint32_t)(all & 0xFFFFFu);
+    const uint32_t s = (uint32_t)lane % kGroups + 1, most = (passes * ((groups + s - 1) / s) + gridDim.x - 1) / gridDim.x;
+    const uint32_t cost = most * max(10 * s, S::parts * (12 + ta.columns / 4));
+    const uint32_t size = kGroups - __reduce_min_sync(0xFFFFFFFFu, cost << 3 | (kGroups - s)) % kGroups;       /* the larger one of equals */
+    const uint32_t per_pass = (groups + size - 1) / size, total = passes * per_pass;
     const uint32_t begin = (uint32_t)((unsigned long long)total * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)total * (blockIdx.x + 1) / gridDim.x);
     const uint32_t bytes = (DOWN ? a.inter : a.hidden) * 2, steps = (bytes + kSpan - 1) / kSpan;
+    /* a stage has room for a tile's rows; the products read 128 rows all the same, those of no tile for nothing */
+    const uint32_t half_bytes = size * kGroup * kSpan, weight_bytes = S::halves * half_bytes, stage_bytes = weight_bytes + S::parts * ta.columns * kSpan;
+    const uint32_t stages = min((uint32_t)kMaxRing, (kRing - kRows * kSpan) / stage_bytes);
     auto for_tiles = [&](auto &&body) {
-        for (uint32_t group = begin; group < end;) {
-            const uint32_t pass = group / groups, g0 = group % groups;
+        for (uint32_t i = begin; i < end; ++i) {
+            const uint32_t pass = i / per_pass, g0 = i % per_pass * size;
             int lo = 0, hi = active - 1;                            /* the last expert with no more passes before it */
             while (lo < hi) {
                 const int mid = (lo + hi + 1) / 2;
@@ -233,16 +237,14 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
             t.expert = s_list[lo];
             t.first = s_first[lo] + (pass - s_passes[lo]) * ta.columns;
             t.n = min(ta.columns, s_first[lo + 1] - t.first);
-            const uint32_t mine = min(min(groups - g0, end - group), (uint32_t)(kRows / kGroup));
             t.row = g0 * kGroup;
-            t.count = min(mine * kGroup, rows - t.row);
+            t.count = min(size * kGroup, rows - t.row);
             body(t);
-            group += mine;
         }
     };
     bool fine = true;
     uint32_t stage = 0, phase = 0;                                  /* of this warp's next step; phase: how often the ring went round, mod 2 */
-    auto step_on = [&] { if (++stage == ta.stages) { stage = 0; phase ^= 1; } };
+    auto step_on = [&] { if (++stage == stages) { stage = 0; phase ^= 1; } };
 
     if (warp == 0) {
         /* weights are nobody's output: they are fetched before the kernel in front of this one has ended */
@@ -259,7 +261,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
                     if (!(boxes & (8u >> i))) continue;
 #pragma unroll
                     for (int h = 0; h < S::halves; ++h)
-                        fetch_rows(leader, to + (h * kRows + from) * kSpan, &maps.of[i], s * (kSpan / 2), row + h * a.inter + from, bar);
+                        fetch_rows(leader, to + h * half_bytes + from * kSpan, &maps.of[i], s * (kSpan / 2), row + h * a.inter + from, bar);
                     from += 128u >> i;
                 }
                 step_on();
@@ -277,13 +279,13 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
                 bar_wait(shared_at(&s_full[stage]), phase, fine);
                 sums_after();
                 const uint32_t at = shared_at(smem) + stage * stage_bytes;
-                const unsigned long long rows0 = operand(at), cols0 = operand(at + S::weights);
+                const unsigned long long rows0 = operand(at), cols0 = operand(at + weight_bytes);
                 const uint32_t quarters = (bytes - s * kSpan + 31) / 32;                                       /* of 16 elements */
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {
                     if (k >= quarters) break;
                     product(leader, to, rows0 + 2 * k, cols0 + 2 * k, kind, s | k);
-                    if (S::halves == 2) product(leader, to + 64, rows0 + (kRows * kSpan >> 4) + 2 * k, cols0 + 2 * k, kind, s | k);
+                    if (S::halves == 2) product(leader, to + 64, rows0 + (half_bytes >> 4) + 2 * k, cols0 + 2 * k, kind, s | k);
                     if (S::parts == 2) product(leader, to, rows0 + 2 * k, cols0 + (ta.columns * kSpan >> 4) + 2 * k, kind, true);
                 }
                 tell_when_done(leader, shared_at(&s_empty[stage]));
@@ -301,7 +303,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) bar_arrive(shared_at(&s_full[told]));
-            if (++told == ta.stages) told = 0;
+            if (++told == stages) told = 0;
             --pending;
         };
         if (DOWN) grid_wait();
@@ -309,10 +311,10 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
             const char *cols[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t choice = s_choices[t.first + min(r0 + 8 * i, t.n - 1)];
-                cols[i] = (DOWN ? a.h + (size_t)choice * S::parts * a.h_row : a.x + choice / a.top_k * a.ld_x) + piece * 16;
+                const uint32_t at = t.first + min(r0 + 8 * i, t.n - 1);
+                cols[i] = (DOWN ? a.h + (size_t)at * S::parts * a.h_row : a.x + s_token[at] * a.ld_x) + piece * 16;
             }
-            const uint32_t place = S::weights + r0 * kSpan + ((piece ^ (r0 & 7)) * 16);
+            const uint32_t place = weight_bytes + r0 * kSpan + ((piece ^ (r0 & 7)) * 16);
             for (uint32_t s = 0; s < steps; ++s) {
                 const uint32_t to = shared_at(smem) + stage * stage_bytes + place, off = s * kSpan, size = off + piece * 16 < bytes ? 16u : 0u;
                 bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
@@ -338,13 +340,12 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         if (DOWN) grid_wait();                                      /* what is written was read by kernels in front of this one */
         for_tiles([&](const TileAt &t) {
             const uint32_t from = tmem + half * 128 + ((uint32_t)(warp - 4) << 21);
-            /* a lane's choices and their weights: columns lane and lane + 32 */
-            uint32_t choice[2];
+            /* a lane's tokens' weights: columns lane and lane + 32 */
             float weight[2] = {};
+            if (!DOWN) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                choice[i] = s_choices[t.first + min((uint32_t)lane + 32 * i, t.n - 1)];
-                if (!DOWN && lane + 32 * i < (int)t.n) weight[i] = weight_of(a, choice[i]);
+                for (int i = 0; i < 2; ++i)
+                    if (lane + 32 * i < (int)t.n) weight[i] = weight_of(a, s_token[t.first + lane + 32 * i], (int)t.expert);
             }
             bar_wait(shared_at(&s_sums[half]), round, fine);
             __syncwarp();
@@ -358,14 +359,14 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const uint32_t to = __shfl_sync(0xFFFFFFFFu, choice[i], c + k);
+                        const size_t to = t.first + c + k;
                         const float w = __shfl_sync(0xFFFFFFFFu, weight[i], c + k);
                         if (c + k >= t.n || row >= t.count) continue;
                         float x = __uint_as_float(v[k]);
                         if (!DOWN) x = w * (activate(x, a.activation) * __uint_as_float(u[k]));
                         if (!fine) x = NAN;
-                        if (DOWN) a.y[(size_t)to * a.hidden + t.row + row] = x;
-                        else store_h<SIFAR_BF16>(a, a.h + (size_t)to * 2 * a.h_row, a.h_row, t.row + row, x);
+                        if (DOWN) a.y[to * a.hidden + t.row + row] = x;
+                        else store_h<SIFAR_BF16>(a, a.h + to * 2 * a.h_row, a.h_row, t.row + row, x);
                     }
                 }
             }
@@ -428,22 +429,17 @@ template <bool DOWN> static cudaError_t launch_tiles(cudaStream_t stream, TilesA
     const cudaError_t bad = DOWN ? map_rows(maps, a.down, (size_t)a.experts * a.hidden, a.inter, a.ld_down)
                                  : map_rows(maps, a.gate_up, (size_t)a.experts * 2 * a.inter, a.hidden, a.ld_gate_up);
     if (bad) return bad;
-    const size_t stage = Tile<DOWN>::weights + Tile<DOWN>::parts * (size_t)t.columns * kSpan;
-    t.stages = (uint32_t)(kRing / stage < kMaxRing ? kRing / stage : kMaxRing);
-    const size_t shared = t.stages * stage + (t.choices * sizeof(uint16_t) + 15) / 16 * 16;
-    if (cudaError_t e = cudaFuncSetAttribute(k_expert_tiles<DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
-    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kExpertThreads), 1, shared, stream, maps, t);
+    if (cudaError_t e = cudaFuncSetAttribute(k_expert_tiles<DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing)) return e;
+    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kExpertThreads), 1, kRing, stream, maps, t);
 }
 
 cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
 {
     TilesArgs t;
     t.e = a;
-    t.choices = a.tokens * a.top_k;
     /* columns of a pass: four times an expert's share of the choices, were they spread evenly; more take another pass */
-    const uint32_t most = 4 * ((t.choices + a.experts - 1) / a.experts), need = most < a.tokens ? most : a.tokens;
+    const uint32_t most = 4 * ((a.tokens * a.top_k + a.experts - 1) / a.experts), need = most < a.tokens ? most : a.tokens;
     t.columns = need <= 16 ? 16 : need <= 32 ? 32 : 64;
-    t.stages = 0;
     if (cudaError_t e = launch_tiles<false>(stream, t)) return e;
     return launch_tiles<true>(stream, t);
 }
