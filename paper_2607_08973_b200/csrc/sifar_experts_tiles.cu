@@ -9,7 +9,7 @@
  *   warp 0      fetches the weights (TMA, 128, 64, 32 and 16 rows at a time: no more than the share has)
  *   warp 1      issues the products
  *   warps 2, 3  gather the tokens' rows (asynchronous 16-byte copies)
- *   warps 4 - 7 take a tile's sums out of tensor memory while the next tile's go into its other half
+ *   warps 4 - 11  take a tile's sums out of tensor memory while the next tile's go into its other half, each half of the columns
  * What bounds it is the memory; the ring keeps up to 160 KB of weights per SM on the way, across tiles.  Warps 0 and 1 go through
  * their loops as whole warps and one lane issues: what an instruction of these needs is in uniform registers then (as one thread's
  * loop, a product took 150 cycles to issue and a fetch 90).
@@ -29,6 +29,7 @@ constexpr int kGroup = 16;                   /* rows that tiles are counted in, 
 constexpr int kGroups = kRows / kGroup;
 constexpr int kRing = 204 * 1024;            /* bytes of all stages: what the lists leave of an SM's 227 KB */
 constexpr int kMaxRing = 8;
+constexpr int kTileWarps = 12, kTileThreads = 32 * kTileWarps, kDrainers = 8;
 constexpr int kGatherers = 64;               /* threads that gather the tokens' rows */
 constexpr int kLag = 3;                      /* stages that they have under way while they fill another: less than a ring has */
 constexpr uint32_t kPolls = 1u << 22;        /* a wait's limit: about 0.1 s, where the products take less than a microsecond */
@@ -106,6 +107,14 @@ __device__ __forceinline__ void copy16(uint32_t to, const char *from, uint32_t b
     asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
 }
 
+/* With the short exponential and quotient: a few steps of binary32 off (e: 2, its argument: |x|, the quotient: 2), where 16 bits
+   are kept.  A quotient by more than 2^126 is 0. */
+__device__ __forceinline__ float activate_fast(float g, int kind)
+{
+    if (kind == SIFAR_ACT_SILU) return __fdividef(g, 1.0f + __expf(-g));
+    return activate(g, kind);
+}
+
 /* A tile: rows row .. row + count - 1 of a pass over an expert with the tokens first .. first + n - 1 of the list. */
 struct TileAt { uint32_t expert, row, count, first, n; };
 
@@ -113,7 +122,7 @@ struct TileAt { uint32_t expert, row, count, first, n; };
 struct RowMaps { CUtensorMap of[4]; };
 
 template <bool DOWN>
-__global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid_constant__ RowMaps maps, const __grid_constant__ TilesArgs ta)
+__global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_constant__ RowMaps maps, const __grid_constant__ TilesArgs ta)
 {
     using S = Tile<DOWN>;
     const ExpertsArgs &a = ta.e;
@@ -122,9 +131,10 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
     __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];            /* experts that have tokens */
     __shared__ uint16_t s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];   /* tokens of the list, passes before each */
     __shared__ uint8_t s_token[SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K];      /* the tokens by expert, in their order */
-    __shared__ unsigned long long s_sum[kExpertWarps];
+    __shared__ unsigned long long s_sum[kTileWarps];
     __shared__ __align__(8) unsigned long long s_full[kMaxRing], s_empty[kMaxRing], s_sums[2], s_free[2];
     __shared__ uint32_t s_tmem;
+    __shared__ __align__(16) float s_weight[kDrainers][32];         /* of a tile's tokens, each warp's half */
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     uint32_t *const s_bits = reinterpret_cast<uint32_t *>(smem);
     const uint32_t words = (a.tokens + 31) / 32, choices = a.tokens * a.top_k;
@@ -143,21 +153,21 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(shared_at(&s_sums[i]), 1);
-            bar_init(shared_at(&s_free[i]), 4);
+            bar_init(shared_at(&s_free[i]), kDrainers);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     /* a bit per expert and token that chose it (twice: once): an expert's tokens are counted and numbered by bits, in the same order
        in every CTA */
-    for (uint32_t i = threadIdx.x; i < a.experts * words; i += kExpertThreads) s_bits[i] = 0u;
+    for (uint32_t i = threadIdx.x; i < a.experts * words; i += kTileThreads) s_bits[i] = 0u;
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < choices; i += kExpertThreads) {
+    for (uint32_t i = threadIdx.x; i < choices; i += kTileThreads) {
         const uint32_t e = local_expert(a, a.indices[i]), token = i / a.top_k;
         if (e < a.experts) atomicOr(&s_bits[e * words + token / 32], 1u << (token % 32));
     }
     __syncthreads();
     /* in one sum over the experts: how many have tokens, their tokens, their passes */
-    constexpr uint32_t kEach = SIFAR_ROUTE_MAX_EXPERTS / kExpertThreads;
+    constexpr uint32_t kEach = (SIFAR_ROUTE_MAX_EXPERTS + kTileThreads - 1) / kTileThreads;
     uint32_t n[kEach];
     unsigned long long mine = 0;
 #pragma unroll
@@ -180,7 +190,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
     sums_after();
     unsigned long long before = upto - mine, all = 0;
 #pragma unroll
-    for (int w = 0; w < kExpertWarps; ++w) {
+    for (int w = 0; w < kTileWarps; ++w) {
         if (w < warp) before += s_sum[w];
         all += s_sum[w];
     }
@@ -199,7 +209,7 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         s_passes[active] = (uint16_t)(all & 0xFFFFFu);
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < choices; i += kExpertThreads) {
+    for (uint32_t i = threadIdx.x; i < choices; i += kTileThreads) {
         const uint32_t e = local_expert(a, a.indices[i]), token = i / a.top_k;
         int at = -1;
         if (e < a.experts) {
@@ -335,38 +345,43 @@ __global__ void __launch_bounds__(kExpertThreads, 1) k_expert_tiles(const __grid
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         while (pending) tell();
     } else {
-        const uint32_t row = (warp - 4) * 32 + lane;
+        /* a thread has a row, its warp the first or the second half of the columns */
+        const uint32_t row = (warp % 4) * 32 + lane, which = warp >= 8;
+        float *const weights = s_weight[warp - 4];
         uint32_t half = 0, round = 0;
         if (DOWN) grid_wait();                                      /* what is written was read by kernels in front of this one */
         for_tiles([&](const TileAt &t) {
-            const uint32_t from = tmem + half * 128 + ((uint32_t)(warp - 4) << 21);
-            /* a lane's tokens' weights: columns lane and lane + 32 */
-            float weight[2] = {};
-            if (!DOWN) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (lane + 32 * i < (int)t.n) weight[i] = weight_of(a, s_token[t.first + lane + 32 * i], (int)t.expert);
-            }
+            const uint32_t width = (t.n + 15) / 16 * 8, c0 = which * width, n = t.n > c0 ? min(t.n - c0, width) : 0u;
+            const uint32_t from = tmem + half * 128 + ((uint32_t)(warp % 4) << 21) + c0;
+            if (!DOWN) weights[lane] = (uint32_t)lane < n ? weight_of(a, s_token[t.first + c0 + lane], (int)t.expert) : 0.0f;
             bar_wait(shared_at(&s_sums[half]), round, fine);
             __syncwarp();
             sums_after();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                for (uint32_t c = 32 * i; c < t.n && c < 32 * i + 32; c += 8) {
+            if ((uint32_t)(warp % 4) * 32 < t.count) {              /* rows of this warp: the same for all its lanes */
+                const bool in = row < t.count && fine;
+                char *h = a.h + (t.first + c0) * (size_t)(2 * a.h_row) + (t.row + row) * 2;
+                float *y = a.y + (t.first + c0) * (size_t)a.hidden + t.row + row;
+                for (uint32_t c = 0; c < n; c += 8) {
                     uint32_t v[8], u[8];
                     read_sums(v, from + c);
                     if (!DOWN) read_sums(u, from + 64 + c);
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const size_t to = t.first + c + k;
-                        const float w = __shfl_sync(0xFFFFFFFFu, weight[i], c + k);
-                        if (c + k >= t.n || row >= t.count) continue;
+                        if (c + k >= n) break;
                         float x = __uint_as_float(v[k]);
-                        if (!DOWN) x = w * (activate(x, a.activation) * __uint_as_float(u[k]));
-                        if (!fine) x = NAN;
-                        if (DOWN) a.y[to * a.hidden + t.row + row] = x;
-                        else store_h<SIFAR_BF16>(a, a.h + to * 2 * a.h_row, a.h_row, t.row + row, x);
+                        if constexpr (DOWN) {
+                            if (in) *y = x;
+                            y += a.hidden;
+                        } else {
+                            x = weights[c + k] * (activate_fast(x, a.activation) * __uint_as_float(u[k]));
+                            const uint16_t hi = narrow<SIFAR_BF16>(x);
+                            if (in) {
+                                *reinterpret_cast<uint16_t *>(h) = hi;
+                                *reinterpret_cast<uint16_t *>(h + a.h_row) = narrow<SIFAR_BF16>(x - widen<SIFAR_BF16>(hi));
+                            }
+                            h += 2 * a.h_row;
+                        }
                     }
                 }
             }
@@ -430,7 +445,7 @@ template <bool DOWN> static cudaError_t launch_tiles(cudaStream_t stream, TilesA
                                  : map_rows(maps, a.gate_up, (size_t)a.experts * 2 * a.inter, a.hidden, a.ld_gate_up);
     if (bad) return bad;
     if (cudaError_t e = cudaFuncSetAttribute(k_expert_tiles<DOWN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing)) return e;
-    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kExpertThreads), 1, kRing, stream, maps, t);
+    return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kTileThreads), 1, kRing, stream, maps, t);
 }
 
 cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
