@@ -7,8 +7,9 @@
  * over k is free, so the eight elements become two instructions' fragments as they lie, with the tokens' taken from the same
  * places.  No weight passes through shared memory.
  *
- *   k_up_few, k_down_few     up to 8 tokens.  All tokens are columns for every expert, the warps of a CTA share the rows' length.
- *   k_products<UP / DOWN>    more tokens: an expert's tokens are gathered to columns, each warp has 16 rows of its own.
+ *   k_up_few, k_down_few     up to 8 tokens; up to 32 where sifar_experts_tiles.cu does not take them.  All tokens are columns for
+ *                            every expert, the warps of a CTA share the rows' length.
+ *   k_products<UP / DOWN>    more of those: an expert's tokens are gathered to columns, each warp has 16 rows of its own.
  *   k_gather                 ... and the sum over a token's choices, in their order.
  *
  * bf16: what goes into the second product is kept as two bf16 values, the rounded one and what it leaves (16 bits).
@@ -20,7 +21,7 @@ namespace sifar {
 constexpr int kWarps = kExpertWarps, kThreads = kExpertThreads;
 constexpr int kBlock = 64;                   /* bytes of a row that the four lanes of a row load at once */
 constexpr int kAhead = 4;                    /* blocks that a lane loads together: 256 bytes of a row */
-constexpr int kFew = 8;                      /* tokens that fit one instruction's columns */
+constexpr int kFew = 8, kFewMost = 32;       /* tokens that fit one instruction's columns, four ones' */
 constexpr int kChunk = 512;                  /* bytes of the tokens' rows in shared memory at a time (more tokens) */
 constexpr int kChunkRow = kChunk + 64;       /* ... rows shifted by half of the banks: eight lanes read two rows' 64 bytes */
 
@@ -88,35 +89,52 @@ __device__ __forceinline__ float dot4(const uint4 &a, const float4 &x, float s)
 }
 
 /* ------------------------------------------------------------------------ */
-/* up to 8 tokens                                                            */
+/* up to 8 G tokens                                                          */
 /* ------------------------------------------------------------------------ */
-/* A lane's accumulators for 16 rows x 8 tokens. */
-template <int DT> struct Few;
-template <> struct Few<SIFAR_BF16> {
-    float c[4] = {};
-    __device__ __forceinline__ void store(float *red) const        /* red: 16 rows x 8 tokens */
+/* A lane's accumulators for 16 rows x 8 G tokens. */
+template <int DT, int G> struct Few;
+template <int G> struct Few<SIFAR_BF16, G> {
+    float c[G][4] = {};
+    __device__ __forceinline__ void store(float *red) const        /* red: 16 rows x 8 G tokens */
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
-        *reinterpret_cast<float2 *>(red + g * 8 + 2 * j) = make_float2(c[0], c[1]);
-        *reinterpret_cast<float2 *>(red + (g + 8) * 8 + 2 * j) = make_float2(c[2], c[3]);
+#pragma unroll
+        for (int q = 0; q < G; ++q) {
+            *reinterpret_cast<float2 *>(red + g * 8 * G + q * 8 + 2 * j) = make_float2(c[q][0], c[q][1]);
+            *reinterpret_cast<float2 *>(red + (g + 8) * 8 * G + q * 8 + 2 * j) = make_float2(c[q][2], c[q][3]);
+        }
     }
 };
-template <> struct Few<SIFAR_F32> {
-    float c[2][8] = {};
+template <int G> struct Few<SIFAR_F32, G> {
+    float c[2][8 * G] = {};
     __device__ __forceinline__ void store(float *red)
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
+            for (int t = 0; t < 8 * G; ++t) {
                 float v = c[r][t];
                 v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
                 v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
-                if (j == (t & 3)) red[(g + 8 * r) * 8 + t] = v;
+                if (j == (t & 3)) red[(g + 8 * r) * 8 * G + t] = v;
             }
     }
 };
+
+/* The experts that have tokens, in their order, and which (bit t: token t).  Returns how many. */
+__device__ __forceinline__ int list_few(const ExpertsArgs &a, uint16_t *list, uint32_t *tokens, uint32_t *bits, int *scratch)
+{
+    for (uint32_t e = threadIdx.x; e < a.experts; e += kThreads) bits[e] = 0u;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < a.tokens * a.top_k; i += kThreads) {
+        const uint32_t e = local_expert(a, a.indices[i]);
+        if (e < a.experts) atomicOr(&bits[e], 1u << (i / a.top_k));
+    }
+    __syncthreads();
+    return keep_in_order(a.experts, scratch, [&](uint32_t e) { return bits[e] != 0u; },
+                         [&](int at, uint32_t e) { list[at] = (uint16_t)e; tokens[at] = bits[e]; });
+}
 
 struct Weights { uint4 a[kAhead], b[kAhead]; };
 
@@ -129,70 +147,77 @@ template <bool VEC> __device__ __forceinline__ void load_weights(Weights &w, con
     }
 }
 
+constexpr int kFewCtas(int G) { return G == 1 ? 2 : 1; }             /* per SM */
+
 /*
- * A unit is 8 gate rows and the 8 up rows that go with them of one expert, so a product's gate and up lie 8 rows apart.
- * Warp w takes every eighth 256 bytes of the rows; the next 256 are under way while these are multiplied, across units too.
+ * All experts' rows lie in a row and every CTA has an equal share of it, 8 gate rows and the 8 up rows that go with them at a
+ * time, so a product's gate and up lie 8 rows apart.  Warp w takes every eighth 256 bytes of the rows; the next 256 are under
+ * way while these are multiplied, across tiles too.
  */
-template <int DT, bool VEC, bool XVEC>
-__global__ void __launch_bounds__(kThreads, 2) k_up_few(const __grid_constant__ ExpertsArgs a)
+template <int DT, int G, bool VEC, bool XVEC>
+__global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_constant__ ExpertsArgs a)
 {
     constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
     extern __shared__ __align__(128) char smem[];                   /* tokens x x_row */
-    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_scratch[kWarps];
-    __shared__ __align__(16) float s_red[2][kWarps][16 * 8];
+    __shared__ uint32_t s_bits[SIFAR_ROUTE_MAX_EXPERTS], s_tokens[SIFAR_ROUTE_MAX_EXPERTS];
+    __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];
+    __shared__ int s_scratch[kWarps];
+    __shared__ __align__(16) float s_red[2][kWarps][16 * 8 * G];
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     grid_wait();
     grid_let_next_in();
-    const int active = list_experts(a, s_counts, s_list, s_scratch);
-    const uint32_t tiles = (a.inter + 7) / 8, bytes = a.hidden * es;
-    const unsigned long long units = (unsigned long long)active * tiles;
+    const uint32_t pairs = (uint32_t)list_few(a, s_list, s_tokens, s_bits, s_scratch) * a.inter, bytes = a.hidden * es;
+    const uint32_t begin = (uint32_t)((unsigned long long)pairs * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)pairs * (blockIdx.x + 1) / gridDim.x);
     const uint32_t steps = (bytes + kWarps * kAhead * kBlock - 1) / (kWarps * kAhead * kBlock);
-    auto rows_of = [&](unsigned long long u, const char *&ra, const char *&rb) {
+    auto rows_of = [&](uint32_t p, const char *&ra, const char *&rb) {
         ra = rb = nullptr;
-        if (u >= units) return;
-        const uint32_t i = (uint32_t)(u % tiles) * 8 + g;
-        if (i >= a.inter) return;
-        const unsigned long long row = (unsigned long long)s_list[u / tiles] * 2 * a.inter + i;
-        ra = a.gate_up + row * a.ld_gate_up;
+        p += g;
+        if (p >= end) return;
+        const uint32_t which = p / a.inter;
+        ra = a.gate_up + ((unsigned long long)s_list[which] * 2 * a.inter + (p - which * a.inter)) * a.ld_gate_up;
         rb = ra + (unsigned long long)a.inter * a.ld_gate_up;
     };
     const uint32_t mine = warp * kAhead * kBlock + j * 16;
-    unsigned long long u = blockIdx.x;
     const char *ra, *rb;
-    rows_of(u, ra, rb);
+    rows_of(begin, ra, rb);
     Weights next;
     load_weights<VEC>(next, ra, rb, mine, bytes);
 
     /* the tokens' rows, zeros behind their ends */
-    for (uint32_t i = threadIdx.x; i < a.tokens * (a.x_row / 16); i += kThreads) {
-        const uint32_t t = i / (a.x_row / 16), at = i % (a.x_row / 16) * 16;
+    for (uint32_t t = 0; t < a.tokens; ++t) {
         const char *row = a.x + t * a.ld_x;
-        *reinterpret_cast<uint4 *>(smem + t * a.x_row + at) =
-            at >= bytes ? make_uint4(0u, 0u, 0u, 0u) : XVEC ? __ldg(reinterpret_cast<const uint4 *>(row + at)) : load_shifted(row + at, bytes - at);
+#pragma unroll 2
+        for (uint32_t at = threadIdx.x * 16; at < a.x_row; at += kThreads * 16)
+            *reinterpret_cast<uint4 *>(smem + t * a.x_row + at) =
+                at >= bytes ? make_uint4(0u, 0u, 0u, 0u) : XVEC ? __ldg(reinterpret_cast<const uint4 *>(row + at)) : load_shifted(row + at, bytes - at);
     }
     __syncthreads();
 
-    for (int parity = 0; u < units; u += gridDim.x, parity ^= 1) {
-        Few<DT> acc;
+    int parity = 0;
+    for (uint32_t p = begin; p < end; p += 8, parity ^= 1) {
+        Few<DT, G> acc;
         for (uint32_t s = 0; s < steps; ++s) {
             const Weights now = next;
             const uint32_t at = s * kWarps * kAhead * kBlock + mine;
             if (s + 1 < steps) {
                 load_weights<VEC>(next, ra, rb, at + kWarps * kAhead * kBlock, bytes);
             } else {
-                rows_of(u + gridDim.x, ra, rb);
+                rows_of(p + 8, ra, rb);
                 load_weights<VEC>(next, ra, rb, mine, bytes);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (at - j * 16 + i * kBlock >= bytes) break;       /* the same for all lanes */
                 if constexpr (DT == SIFAR_BF16) {
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if ((uint32_t)g < a.tokens) x = *reinterpret_cast<const uint4 *>(smem + g * a.x_row + at + i * kBlock);
-                    multiply_block(acc.c, now.a[i], now.b[i], x);
+#pragma unroll
+                    for (int q = 0; q < G; ++q) {
+                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                        if ((uint32_t)(q * 8 + g) < a.tokens) x = *reinterpret_cast<const uint4 *>(smem + (q * 8 + g) * a.x_row + at + i * kBlock);
+                        multiply_block(acc.c[q], now.a[i], now.b[i], x);
+                    }
                 } else {
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) {
+                    for (int t = 0; t < 8 * G; ++t) {
                         if ((uint32_t)t >= a.tokens) break;
                         const float4 x = *reinterpret_cast<const float4 *>(smem + t * a.x_row + at + i * kBlock);
                         acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
@@ -203,96 +228,112 @@ __global__ void __launch_bounds__(kThreads, 2) k_up_few(const __grid_constant__ 
         }
         acc.store(s_red[parity][warp]);
         __syncthreads();                                            /* the other parity's sums are read by now */
-        const uint32_t i = threadIdx.x / 8, t = threadIdx.x % 8, which = (uint32_t)(u / tiles), col = (uint32_t)(u % tiles) * 8 + i;
-        if (i < 8 && t < a.tokens && col < a.inter) {
+        const uint32_t i = threadIdx.x / 32, t = lane, which = (p + i) / a.inter;
+        if (p + i < end && t < a.tokens && (s_tokens[which] >> t & 1u)) {
             float gate = 0.0f, up = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) { gate += s_red[parity][w][i * 8 + t]; up += s_red[parity][w][(i + 8) * 8 + t]; }
-            float weight = 0.0f;
-            bool chosen = false;
-            for (uint32_t c = t * a.top_k; c < (t + 1) * a.top_k; ++c)
-                if ((long long)a.indices[c] - a.first == s_list[which]) { weight += a.weights[c]; chosen = true; }
-            const float v = chosen ? weight * (activate(gate, a.activation) * up) : 0.0f;
+            for (int w = 0; w < kWarps; ++w) { gate += s_red[parity][w][i * 8 * G + t]; up += s_red[parity][w][(i + 8) * 8 * G + t]; }
             const size_t low = (size_t)a.tokens * a.h_row;
-            store_h<DT>(a, a.h + (which * (DT == SIFAR_BF16 ? 2 : 1) * low) + t * (size_t)a.h_row, low, col, v);
+            store_h<DT>(a, a.h + which * (DT == SIFAR_BF16 ? 2 : 1) * low + t * (size_t)a.h_row, low, p + i - which * a.inter,
+                        weight_of(a, t, s_list[which]) * (activate(gate, a.activation) * up));
         }
     }
 }
 
 /*
- * A CTA has 16 columns of the output and goes over all experts that have tokens; its warps take the 256-byte pieces of the
- * experts' rows in turn.  HALF (bf16, up to 4 tokens): both parts of the products' values are columns of one instruction.
+ * A CTA has an equal share of the output's columns, 16 at a time, and goes over all experts that have tokens; its warps take
+ * the 256-byte pieces of the experts' rows in turn.  Tokens that did not choose an expert have zeros there and are not read.
+ * HALF (bf16, up to 4 tokens): both parts of the products' values are columns of one instruction.
  */
-template <int DT, bool VEC, bool HALF>
-__global__ void __launch_bounds__(kThreads, 2) k_down_few(const __grid_constant__ ExpertsArgs a)
+template <int DT, int G, bool VEC, bool HALF>
+__global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid_constant__ ExpertsArgs a)
 {
     constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
-    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_scratch[kWarps];
-    __shared__ __align__(16) float s_red[kWarps][16 * 8];
+    __shared__ uint32_t s_bits[SIFAR_ROUTE_MAX_EXPERTS], s_tokens[SIFAR_ROUTE_MAX_EXPERTS];
+    __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];
+    __shared__ int s_scratch[kWarps];
+    __shared__ __align__(16) float s_red[kWarps][16 * 8 * G];
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     /* the choices were complete before the kernel in front of this one let it in, so they may be read before it ends */
-    const int active = list_experts(a, s_counts, s_list, s_scratch);
+    const int active = list_few(a, s_list, s_tokens, s_bits, s_scratch);
     const uint32_t bytes = a.inter * es, pieces = (bytes + kAhead * kBlock - 1) / (kAhead * kBlock), items = (uint32_t)active * pieces;
-    const uint32_t col = blockIdx.x * 16 + g;
-    auto load = [&](Weights &w, uint32_t item) {
+    const uint32_t begin = (uint32_t)((unsigned long long)a.hidden * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)a.hidden * (blockIdx.x + 1) / gridDim.x);
+    auto load = [&](Weights &w, uint32_t col, uint32_t item) {
         const char *ra = nullptr, *rb = nullptr;
         if (item < items) {
-            const unsigned long long row = (unsigned long long)s_list[item / pieces] * a.hidden + col;
-            if (col < a.hidden) ra = a.down + row * a.ld_down;
-            if (col + 8 < a.hidden) rb = a.down + (row + 8) * a.ld_down;
+            const unsigned long long row = (unsigned long long)s_list[item / pieces] * a.hidden + col + g;
+            if (col + g < end) ra = a.down + row * a.ld_down;
+            if (col + g + 8 < end) rb = a.down + (row + 8) * a.ld_down;
         }
         load_weights<VEC>(w, ra, rb, item % pieces * (kAhead * kBlock) + j * 16, bytes);
     };
     Weights next;
-    load(next, warp);
+    load(next, begin, warp);
     grid_wait();
     grid_let_next_in();
-    Few<DT> acc;
-    for (uint32_t item = warp; item < items; item += kWarps) {
-        const Weights now = next;
-        load(next, item + kWarps);
-        const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + j * 16;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const uint32_t here = at + i * kBlock;
-            if (here - j * 16 >= bytes) break;
-            const bool in = here < a.h_row;                         /* rows of h are filled up with zeros to 16 bytes */
+    const size_t low = (size_t)a.tokens * a.h_row;
+    for (uint32_t col = begin; col < end; col += 16) {
+        Few<DT, G> acc;
+        for (uint32_t item = warp; item < items; item += kWarps) {
+            const Weights now = next;
+            const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + j * 16, tokens = s_tokens[which];
+            const char *const h = a.h + (size_t)which * (DT == SIFAR_BF16 ? 2 : 1) * low;
             if constexpr (DT == SIFAR_BF16) {
-                const char *const h = a.h + (size_t)which * 2 * a.tokens * a.h_row + here;
-                const uint32_t t = HALF ? g & 3 : g;
-                const size_t low = (size_t)a.tokens * a.h_row;
-                uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
-                if (in && t < a.tokens) {
-                    x = __ldcg(reinterpret_cast<const uint4 *>(h + t * a.h_row + (HALF && g >= 4 ? low : 0)));
-                    if (!HALF) y = __ldcg(reinterpret_cast<const uint4 *>(h + t * a.h_row + low));
-                }
-                multiply_block(acc.c, now.a[i], now.b[i], x);
-                if (!HALF) multiply_block(acc.c, now.a[i], now.b[i], y);
-            } else {
+                uint4 x[kAhead][G], y[HALF ? 1 : kAhead][G];
 #pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    if ((uint32_t)t >= a.tokens || !in) break;
-                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(a.h + ((size_t)which * a.tokens + t) * a.h_row + here));
-                    acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
-                    acc.c[1][t] = dot4(now.b[i], x, acc.c[1][t]);
+                for (int q = 0; q < G; ++q) {
+                    const uint32_t t = HALF ? g & 3 : q * 8 + g;
+                    const char *const from = h + t * (size_t)a.h_row + (HALF && g >= 4 ? low : 0) + at;
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const bool in = (tokens >> t & 1u) && at + i * kBlock < a.h_row;        /* rows of h are filled up with zeros to 16 bytes */
+                        x[i][q] = in ? __ldcg(reinterpret_cast<const uint4 *>(from + i * kBlock)) : make_uint4(0u, 0u, 0u, 0u);
+                        if (!HALF) y[i][q] = in ? __ldcg(reinterpret_cast<const uint4 *>(from + low + i * kBlock)) : make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+                load(next, item + kWarps < items ? col : col + 16, item + kWarps < items ? item + kWarps : warp);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    if (at - j * 16 + i * kBlock >= bytes) break;
+#pragma unroll
+                    for (int q = 0; q < G; ++q) {
+                        if (!(HALF ? tokens : tokens >> (8 * q) & 0xFFu)) continue;
+                        multiply_block(acc.c[q], now.a[i], now.b[i], x[i][q]);
+                        if (!HALF) multiply_block(acc.c[q], now.a[i], now.b[i], y[i][q]);
+                    }
+                }
+            } else {
+                load(next, item + kWarps < items ? col : col + 16, item + kWarps < items ? item + kWarps : warp);
+#pragma unroll
+                for (int t = 0; t < 8 * G; ++t) {
+                    if (!(tokens >> t & 1u)) continue;              /* the same for the whole warp */
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        if (at + i * kBlock >= a.h_row) continue;
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(h + t * (size_t)a.h_row + at + i * kBlock));
+                        acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
+                        acc.c[1][t] = dot4(now.b[i], x, acc.c[1][t]);
+                    }
                 }
             }
         }
-    }
-    acc.store(s_red[warp]);
-    __syncthreads();
-    const uint32_t r = threadIdx.x % 16, t = threadIdx.x / 16;
-    if (t < a.tokens && blockIdx.x * 16 + r < a.hidden) {
-        float v = 0.0f;
+        acc.store(s_red[warp]);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 16 * a.tokens; i += kThreads) {
+            const uint32_t r = i % 16, t = i / 16;
+            if (col + r >= end) continue;
+            float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += s_red[w][r * 8 + t];
-        if (HALF) {
-            float low = 0.0f;
+            for (int w = 0; w < kWarps; ++w) v += s_red[w][r * 8 * G + t];
+            if (HALF) {
+                float rest = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) low += s_red[w][r * 8 + t + 4];
-            v += low;
+                for (int w = 0; w < kWarps; ++w) rest += s_red[w][r * 8 * G + t + 4];
+                v += rest;
+            }
+            reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out)[col + r] = narrow<DT>(v);
         }
-        reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out)[blockIdx.x * 16 + r] = narrow<DT>(v);
+        __syncthreads();
     }
 }
 
@@ -529,7 +570,8 @@ __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ Exp
 /* ------------------------------------------------------------------------ */
 struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, y_bytes, bytes; };
 
-constexpr size_t kFewShared = 100 * 1024;    /* the tokens' rows in shared memory: two CTAs of 8 warps per SM */
+constexpr size_t kFewShared = 92 * 1024;     /* the tokens' rows in shared memory: two CTAs of 8 warps per SM */
+constexpr size_t kFewMostShared = 180 * 1024;  /* ... one */
 
 static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan &p)
 {
@@ -546,7 +588,8 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     const size_t es = elem_size(g->dtype), T = g->tokens, choices = T * (size_t)g->top_k, parts = g->dtype == SIFAR_BF16 ? 2 : 1;
     /* a multiple of 128 bytes and 64 more: two rows' pieces lie in different banks */
     p.x_row = (uint32_t)((g->hidden * es + 127) / 128 * 128 + 64);
-    p.few = T <= (size_t)kFew && T * p.x_row <= kFewShared;
+    const bool tiles = g->dtype == SIFAR_BF16 && g->hidden % 8 == 0 && g->inter % 8 == 0;      /* as far as the sizes go */
+    p.few = T <= (size_t)(tiles ? kFew : kFewMost) && T * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);
     p.h_row = (uint32_t)((g->inter * es + 15) / 16 * 16);
     const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
     p.h_bytes = ((p.few ? most * T : choices) * parts * p.h_row + 15) / 16 * 16;
@@ -558,9 +601,24 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
 template <typename... P, typename... A>
 static cudaError_t launch_shared(void (*kernel)(P...), dim3 grid, size_t shared, cudaStream_t stream, const A &...args)
 {
-    if (shared > 24 * 1024)                  /* 48 KB less what the kernels declare themselves */
+    if (shared)                              /* with what the kernels declare themselves it may be more than 48 KB */
         if (cudaError_t e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
     return launch_op(kernel, grid, dim3(kThreads), 1, shared, stream, args...);
+}
+
+template <int DT, int G>
+static cudaError_t launch_few(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, const ExpertsArgs &a)
+{
+    const size_t shared = a.tokens * p.x_row;
+    const unsigned ctas = kSms * kFewCtas(G);
+    const dim3 grid(ctas), columns(a.hidden < 8 * ctas ? (a.hidden + 7) / 8 : ctas);       /* of the output: 8 at least */
+    cudaError_t e = !gu_vec ? launch_shared(k_up_few<DT, G, false, false>, grid, shared, stream, a)
+                    : x_vec ? launch_shared(k_up_few<DT, G, true, true>, grid, shared, stream, a) : launch_shared(k_up_few<DT, G, true, false>, grid, shared, stream, a);
+    if (e) return e;
+    if constexpr (DT == SIFAR_BF16 && G == 1) {
+        if (a.tokens <= 4) return dn_vec ? launch_shared(k_down_few<DT, G, true, true>, columns, 0, stream, a) : launch_shared(k_down_few<DT, G, false, true>, columns, 0, stream, a);
+    }
+    return dn_vec ? launch_shared(k_down_few<DT, G, true, false>, columns, 0, stream, a) : launch_shared(k_down_few<DT, G, false, false>, columns, 0, stream, a);
 }
 
 template <int DT>
@@ -569,14 +627,8 @@ static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec
     const dim3 grid(2 * kSms);
     cudaError_t e;
     if (p.few) {
-        const size_t shared = a.tokens * p.x_row;
-        e = !gu_vec ? launch_shared(k_up_few<DT, false, false>, grid, shared, stream, a)
-            : x_vec ? launch_shared(k_up_few<DT, true, true>, grid, shared, stream, a) : launch_shared(k_up_few<DT, true, false>, grid, shared, stream, a);
-        if (e) return e;
-        const dim3 columns((a.hidden + 15) / 16);
-        if (DT == SIFAR_BF16 && a.tokens <= 4)
-            return dn_vec ? launch_shared(k_down_few<DT, true, DT == SIFAR_BF16>, columns, 0, stream, a) : launch_shared(k_down_few<DT, false, DT == SIFAR_BF16>, columns, 0, stream, a);
-        return dn_vec ? launch_shared(k_down_few<DT, true, false>, columns, 0, stream, a) : launch_shared(k_down_few<DT, false, false>, columns, 0, stream, a);
+        if (a.tokens <= 8) return launch_few<DT, 1>(p, gu_vec, dn_vec, x_vec, stream, a);
+        return a.tokens <= 16 ? launch_few<DT, 2>(p, gu_vec, dn_vec, x_vec, stream, a) : launch_few<DT, 4>(p, gu_vec, dn_vec, x_vec, stream, a);
     }
     if (DT == SIFAR_BF16 && gu_vec && dn_vec && x_vec) {
         a.place = (int *)((char *)a.y + p.y_bytes);

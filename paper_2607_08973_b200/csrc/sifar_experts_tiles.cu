@@ -358,7 +358,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             __syncwarp();
             sums_after();
             if ((uint32_t)(warp % 4) * 32 < t.count) {              /* rows of this warp: the same for all its lanes */
-                const bool in = row < t.count && fine;
+                const bool in = row < t.count;
+                const float right = fine ? 1.0f : NAN;              /* a wait that ran out shows */
                 char *h = a.h + (t.first + c0) * (size_t)(2 * a.h_row) + (t.row + row) * 2;
                 float *y = a.y + (t.first + c0) * (size_t)a.hidden + t.row + row;
                 for (uint32_t c = 0; c < n; c += 8) {
@@ -371,10 +372,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
                         if (c + k >= n) break;
                         float x = __uint_as_float(v[k]);
                         if constexpr (DOWN) {
-                            if (in) *y = x;
+                            if (in) *y = x * right;
                             y += a.hidden;
                         } else {
-                            x = weights[c + k] * (activate_fast(x, a.activation) * __uint_as_float(u[k]));
+                            x = weights[c + k] * right * (activate_fast(x, a.activation) * __uint_as_float(u[k]));
                             const uint16_t hi = narrow<SIFAR_BF16>(x);
                             if (in) {
                                 *reinterpret_cast<uint16_t *>(h) = hi;
