@@ -21,6 +21,7 @@ namespace sifar {
 constexpr int kWarps = kExpertWarps, kThreads = kExpertThreads;
 constexpr int kBlock = 64;                   /* bytes of a row that the four lanes of a row load at once */
 constexpr int kAhead = 4;                    /* blocks that a lane loads together: 256 bytes of a row */
+constexpr uint32_t kFetchAhead = 6;          /* items of a warp that k_down_few asks for before its values are there */
 constexpr int kFew = 8, kFewMost = 32;       /* tokens that fit one instruction's columns, four ones' */
 constexpr int kChunk = 512;                  /* bytes of the tokens' rows in shared memory at a time (more tokens) */
 constexpr int kChunkRow = kChunk + 64;       /* ... rows shifted by half of the banks: eight lanes read two rows' 64 bytes */
@@ -35,14 +36,9 @@ __device__ __forceinline__ uint4 load_once(const char *p)
     return v;
 }
 
-/* 16 bytes from any element on: two aligned vectors shifted together, bytes from `left` on 0. */
-__device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
+/* Bytes sh .. sh + 15 of two vectors in a row, those from `left` on 0. */
+__device__ __forceinline__ uint4 shifted(const uint4 &lo, const uint4 &hi, uint32_t sh, int left)
 {
-    const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;
-    const uint4 *const q = reinterpret_cast<const uint4 *>(p - sh);
-    const uint4 lo = __ldg(q);
-    uint4 hi = make_uint4(0u, 0u, 0u, 0u);
-    if (sh && left > 16u - sh) hi = __ldg(q + 1);
     uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
     /* words first, then the bits within them */
     if (sh & 8u) {
@@ -56,19 +52,84 @@ __device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
     const uint32_t bits = (sh & 3u) * 8u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-    if (left < 16u) {
+    if (left < 16) {
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) w[i] = left >= 4 * i + 4 ? w[i] : left <= 4 * i ? 0u : w[i] & ((1u << (left - 4 * i) * 8u) - 1u);
+        for (int i = 0; i < 4; ++i) w[i] = left >= 4 * i + 4 ? w[i] : left <= 4 * i ? 0u : w[i] & ((1u << (left - 4 * i) * 8) - 1u);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-/* 16 bytes of a row of `bytes` from `at` on, zeros behind its end or without a row. */
-template <bool VEC> __device__ __forceinline__ uint4 load_row(const char *row, uint32_t at, uint32_t bytes)
+/* 16 bytes from any element on, zeros from `left` on. */
+__device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
 {
-    if (!row || at >= bytes) return make_uint4(0u, 0u, 0u, 0u);
-    return VEC ? load_once(row + at) : load_shifted(row + at, bytes - at);
+    const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;
+    const uint4 *const q = reinterpret_cast<const uint4 *>(p - sh);
+    const uint4 lo = __ldg(q);
+    uint4 hi = make_uint4(0u, 0u, 0u, 0u);
+    if (sh && left > 16u - sh) hi = __ldg(q + 1);
+    return shifted(lo, hi, sh, (int)left);
 }
+
+/*
+ * What a lane has on the way of its two rows: 16 bytes of each of kAhead blocks, a block being the 64 bytes of the row's four lanes.
+ * Rows that start anywhere (not VEC) are loaded as the aligned vectors that hold them, and put together when they are used: the
+ * vector behind a lane's own is the next lane's, the last lane's the first one's of the next block, of which the first lane has
+ * one more.
+ */
+template <bool VEC> struct Weights {
+    static constexpr int n = VEC ? kAhead : kAhead + 1;
+    uint4 a[n], b[n];
+    uint32_t sh_a, sh_b;
+
+    static __device__ __forceinline__ uint32_t row(uint4 (&v)[n], const char *p, uint32_t at, uint32_t bytes)
+    {
+        const uint32_t sh = VEC ? 0u : (uint32_t)(uintptr_t)p & 15u;
+        const char *const from = p - sh + at;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (p && at + i * kBlock < bytes + sh && (i < kAhead || (threadIdx.x & 3) == 0)) {
+                if (VEC) v[i] = load_once(from + i * kBlock);
+                else v[i] = __ldg(reinterpret_cast<const uint4 *>(from + i * kBlock));
+            }
+        }
+        return sh;
+    }
+    /* From byte `at` (the lane's own) of two rows of `bytes`; a row may be missing. */
+    __device__ __forceinline__ void load(const char *ra, const char *rb, uint32_t at, uint32_t bytes)
+    {
+        sh_a = row(a, ra, at, bytes);
+        sh_b = row(b, rb, at, bytes);
+    }
+    static __device__ __forceinline__ uint4 use(const uint4 (&v)[n], uint32_t sh, int i, int left)
+    {
+        if (VEC) return v[i];
+        const int lane = threadIdx.x & 31, from = (lane & ~3) | ((lane + 1) & 3);
+        const bool first = (lane & 3) == 0;
+        const uint4 own = v[i], behind = v[i + 1 < n ? i + 1 : i];
+        const uint4 give = make_uint4(first ? behind.x : own.x, first ? behind.y : own.y, first ? behind.z : own.z, first ? behind.w : own.w);
+        uint4 hi;
+        hi.x = __shfl_sync(0xFFFFFFFFu, give.x, from); hi.y = __shfl_sync(0xFFFFFFFFu, give.y, from);
+        hi.z = __shfl_sync(0xFFFFFFFFu, give.z, from); hi.w = __shfl_sync(0xFFFFFFFFu, give.w, from);
+        return shifted(own, hi, sh, left);
+    }
+    /* Block i; `left`: bytes of the rows from the lane's own on.  All lanes together. */
+    __device__ __forceinline__ uint4 of_a(int i, int left) const { return use(a, sh_a, i, left); }
+    __device__ __forceinline__ uint4 of_b(int i, int left) const { return use(b, sh_b, i, left); }
+};
+
+/* An asynchronous copy of 4 bytes into shared memory; of 0 bytes: zeros. */
+__device__ __forceinline__ void copy4(void *to, const char *from, uint32_t bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+}
+/* ... of 16 bytes. */
+__device__ __forceinline__ void copy16(void *to, const char *from, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
 
 __device__ __forceinline__ void multiply(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -136,18 +197,7 @@ __device__ __forceinline__ int list_few(const ExpertsArgs &a, uint16_t *list, ui
                          [&](int at, uint32_t e) { list[at] = (uint16_t)e; tokens[at] = bits[e]; });
 }
 
-struct Weights { uint4 a[kAhead], b[kAhead]; };
-
-template <bool VEC> __device__ __forceinline__ void load_weights(Weights &w, const char *ra, const char *rb, uint32_t at, uint32_t bytes)
-{
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-        w.a[i] = load_row<VEC>(ra, at + i * kBlock, bytes);
-        w.b[i] = load_row<VEC>(rb, at + i * kBlock, bytes);
-    }
-}
-
-constexpr int kFewCtas(int G) { return G == 1 ? 2 : 1; }             /* per SM */
+constexpr int kFewCtas(int G) { return G <= 2 ? 2 : 1; }             /* per SM */
 
 /*
  * All experts' rows lie in a row and every CTA has an equal share of it, 8 gate rows and the 8 up rows that go with them at a
@@ -166,7 +216,22 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     grid_wait();
     grid_let_next_in();
-    const uint32_t pairs = (uint32_t)list_few(a, s_list, s_tokens, s_bits, s_scratch) * a.inter, bytes = a.hidden * es;
+    const uint32_t bytes = a.hidden * es, per_row = a.x_row / 16, all = a.tokens * per_row;
+    /* the tokens' rows, zeros behind their ends: on their way while the experts are listed */
+    constexpr bool kCopy = XVEC || DT == SIFAR_F32;
+    if (XVEC) {
+        for (uint32_t i = threadIdx.x; i < all; i += kThreads) {
+            const uint32_t t = i / per_row, at = (i - t * per_row) * 16;
+            copy16(smem + i * 16, at < bytes ? a.x + t * a.ld_x + at : a.x, at < bytes ? 16u : 0u);
+        }
+    } else if (kCopy) {
+        for (uint32_t t = 0; t < a.tokens; ++t)
+#pragma unroll 4
+            for (uint32_t at = threadIdx.x * 4; at < a.x_row; at += kThreads * 4)
+                copy4(smem + t * a.x_row + at, at < bytes ? a.x + t * a.ld_x + at : a.x, at < bytes ? 4u : 0u);
+    }
+    if (kCopy) copies_commit();
+    const uint32_t pairs = (uint32_t)list_few(a, s_list, s_tokens, s_bits, s_scratch) * a.inter;
     const uint32_t begin = (uint32_t)((unsigned long long)pairs * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)pairs * (blockIdx.x + 1) / gridDim.x);
     const uint32_t steps = (bytes + kWarps * kAhead * kBlock - 1) / (kWarps * kAhead * kBlock);
     auto rows_of = [&](uint32_t p, const char *&ra, const char *&rb) {
@@ -180,16 +245,23 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     const uint32_t mine = warp * kAhead * kBlock + j * 16;
     const char *ra, *rb;
     rows_of(begin, ra, rb);
-    Weights next;
-    load_weights<VEC>(next, ra, rb, mine, bytes);
+    Weights<VEC> next;
+    next.load(ra, rb, mine, bytes);
 
-    /* the tokens' rows, zeros behind their ends */
-    for (uint32_t t = 0; t < a.tokens; ++t) {
-        const char *row = a.x + t * a.ld_x;
-#pragma unroll 2
-        for (uint32_t at = threadIdx.x * 16; at < a.x_row; at += kThreads * 16)
-            *reinterpret_cast<uint4 *>(smem + t * a.x_row + at) =
-                at >= bytes ? make_uint4(0u, 0u, 0u, 0u) : XVEC ? __ldg(reinterpret_cast<const uint4 *>(row + at)) : load_shifted(row + at, bytes - at);
+    if (kCopy) {
+        copies_wait<0>();
+    } else {
+        for (uint32_t i0 = threadIdx.x; i0 < all; i0 += 4 * kThreads) {
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t i = i0 + k * kThreads, t = i / per_row, at = (i - t * per_row) * 16;
+                v[k] = i < all && at < bytes ? load_shifted(a.x + t * a.ld_x + at, bytes - at) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i0 + k * kThreads < all) *reinterpret_cast<uint4 *>(smem + (i0 + k * kThreads) * 16) = v[k];
+        }
     }
     __syncthreads();
 
@@ -197,31 +269,36 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     for (uint32_t p = begin; p < end; p += 8, parity ^= 1) {
         Few<DT, G> acc;
         for (uint32_t s = 0; s < steps; ++s) {
-            const Weights now = next;
+            const Weights<VEC> now = next;
             const uint32_t at = s * kWarps * kAhead * kBlock + mine;
             if (s + 1 < steps) {
-                load_weights<VEC>(next, ra, rb, at + kWarps * kAhead * kBlock, bytes);
+                next.load(ra, rb, at + kWarps * kAhead * kBlock, bytes);
             } else {
                 rows_of(p + 8, ra, rb);
-                load_weights<VEC>(next, ra, rb, mine, bytes);
+                next.load(ra, rb, mine, bytes);
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (at - j * 16 + i * kBlock >= bytes) break;       /* the same for all lanes */
+                const int left = (int)bytes - (int)(at + i * kBlock);
+                const uint4 wa = now.of_a(i, left), wb = now.of_b(i, left);
                 if constexpr (DT == SIFAR_BF16) {
 #pragma unroll
                     for (int q = 0; q < G; ++q) {
                         uint4 x = make_uint4(0u, 0u, 0u, 0u);
                         if ((uint32_t)(q * 8 + g) < a.tokens) x = *reinterpret_cast<const uint4 *>(smem + (q * 8 + g) * a.x_row + at + i * kBlock);
-                        multiply_block(acc.c[q], now.a[i], now.b[i], x);
+                        multiply_block(acc.c[q], wa, wb, x);
                     }
                 } else {
 #pragma unroll
-                    for (int t = 0; t < 8 * G; ++t) {
-                        if ((uint32_t)t >= a.tokens) break;
-                        const float4 x = *reinterpret_cast<const float4 *>(smem + t * a.x_row + at + i * kBlock);
-                        acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
-                        acc.c[1][t] = dot4(now.b[i], x, acc.c[1][t]);
+                    for (int q = 0; q < 2 * G; ++q) {
+                        if ((uint32_t)q * 4 >= a.tokens) break;     /* by fours: rows of no token are whatever they are */
+#pragma unroll
+                        for (int t = 4 * q; t < 4 * q + 4; ++t) {
+                            const float4 x = *reinterpret_cast<const float4 *>(smem + t * a.x_row + at + i * kBlock);
+                            acc.c[0][t] = dot4(wa, x, acc.c[0][t]);
+                            acc.c[1][t] = dot4(wb, x, acc.c[1][t]);
+                        }
                     }
                 }
             }
@@ -240,6 +317,9 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     }
 }
 
+/* What an item's binary32 values take: 256 bytes of each token's row. */
+template <int G> struct Staged { static constexpr int bytes = 8 * G * kAhead * kBlock; };
+
 /*
  * A CTA has an equal share of the output's columns, 16 at a time, and goes over all experts that have tokens; its warps take
  * the 256-byte pieces of the experts' rows in turn.  Tokens that did not choose an expert have zeros there and are not read.
@@ -253,37 +333,63 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
     __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];
     __shared__ int s_scratch[kWarps];
     __shared__ __align__(16) float s_red[kWarps][16 * 8 * G];
+    extern __shared__ __align__(128) char smem[];                   /* binary32: each warp's two items' values */
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     /* the choices were complete before the kernel in front of this one let it in, so they may be read before it ends */
     const int active = list_few(a, s_list, s_tokens, s_bits, s_scratch);
     const uint32_t bytes = a.inter * es, pieces = (bytes + kAhead * kBlock - 1) / (kAhead * kBlock), items = (uint32_t)active * pieces;
     const uint32_t begin = (uint32_t)((unsigned long long)a.hidden * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)a.hidden * (blockIdx.x + 1) / gridDim.x);
-    auto load = [&](Weights &w, uint32_t col, uint32_t item) {
+    auto load = [&](Weights<VEC> &w, uint32_t col, uint32_t item) {
         const char *ra = nullptr, *rb = nullptr;
         if (item < items) {
             const unsigned long long row = (unsigned long long)s_list[item / pieces] * a.hidden + col + g;
             if (col + g < end) ra = a.down + row * a.ld_down;
             if (col + g + 8 < end) rb = a.down + (row + 8) * a.ld_down;
         }
-        load_weights<VEC>(w, ra, rb, item % pieces * (kAhead * kBlock) + j * 16, bytes);
+        w.load(ra, rb, item % pieces * (kAhead * kBlock) + j * 16, bytes);
     };
-    Weights next;
+    Weights<VEC> next;
     load(next, begin, warp);
+    /* the next items' weights, too, as far as the L2: a lane has half a row's piece of each */
+    for (uint32_t k = 1; k <= kFetchAhead; ++k) {
+        const uint32_t item = warp + k * kWarps, c = begin + lane / 2, at = item % pieces * (kAhead * kBlock) + (lane & 1) * 128;
+        if (item >= items) break;
+        if (c < end && at < bytes)
+            asm volatile("prefetch.global.L2 [%0];" :: "l"(a.down + ((unsigned long long)s_list[item / pieces] * a.hidden + c) * a.ld_down + at));
+    }
     grid_wait();
     grid_let_next_in();
     const size_t low = (size_t)a.tokens * a.h_row;
+    /* binary32: the values that go with an item, two tokens' rows at a time, zeros behind their ends */
+    char *const staged = smem + warp * (2 * Staged<G>::bytes);
+    auto fetch = [&](uint32_t item, int half) {
+        if (item < items) {
+            const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + (lane & 15) * 16, size = at < a.h_row ? 16u : 0u;
+            const char *const h = a.h + (size_t)which * low + (size ? at : 0u);
+            uint32_t rest = s_tokens[which];
+            while (rest) {
+                uint32_t t = __ffs(rest) - 1;
+                rest &= rest - 1u;
+                if (lane >= 16 && rest) t = __ffs(rest) - 1;
+                rest &= rest - 1u;
+                copy16(staged + half * Staged<G>::bytes + t * (kAhead * kBlock) + (lane & 15) * 16, h + t * (size_t)a.h_row, size);
+            }
+        }
+        copies_commit();
+    };
     for (uint32_t col = begin; col < end; col += 16) {
         Few<DT, G> acc;
-        for (uint32_t item = warp; item < items; item += kWarps) {
-            const Weights now = next;
+        int half = 0;
+        if (DT == SIFAR_F32) fetch(warp, 0);
+        for (uint32_t item = warp; item < items; item += kWarps, half ^= 1) {
+            const Weights<VEC> now = next;
             const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + j * 16, tokens = s_tokens[which];
-            const char *const h = a.h + (size_t)which * (DT == SIFAR_BF16 ? 2 : 1) * low;
             if constexpr (DT == SIFAR_BF16) {
                 uint4 x[kAhead][G], y[HALF ? 1 : kAhead][G];
 #pragma unroll
                 for (int q = 0; q < G; ++q) {
                     const uint32_t t = HALF ? g & 3 : q * 8 + g;
-                    const char *const from = h + t * (size_t)a.h_row + (HALF && g >= 4 ? low : 0) + at;
+                    const char *const from = a.h + (size_t)which * 2 * low + t * (size_t)a.h_row + (HALF && g >= 4 ? low : 0) + at;
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
                         const bool in = (tokens >> t & 1u) && at + i * kBlock < a.h_row;        /* rows of h are filled up with zeros to 16 bytes */
@@ -295,28 +401,42 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     if (at - j * 16 + i * kBlock >= bytes) break;
+                    const int left = (int)bytes - (int)(at + i * kBlock);
+                    const uint4 wa = now.of_a(i, left), wb = now.of_b(i, left);
 #pragma unroll
                     for (int q = 0; q < G; ++q) {
                         if (!(HALF ? tokens : tokens >> (8 * q) & 0xFFu)) continue;
-                        multiply_block(acc.c[q], now.a[i], now.b[i], x[i][q]);
-                        if (!HALF) multiply_block(acc.c[q], now.a[i], now.b[i], y[i][q]);
+                        multiply_block(acc.c[q], wa, wb, x[i][q]);
+                        if (!HALF) multiply_block(acc.c[q], wa, wb, y[i][q]);
                     }
                 }
             } else {
                 load(next, item + kWarps < items ? col : col + 16, item + kWarps < items ? item + kWarps : warp);
+                fetch(item + kWarps, half ^ 1);
+                uint4 wa[kAhead], wb[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int left = (int)bytes - (int)(at + i * kBlock);
+                    wa[i] = now.of_a(i, left);
+                    wb[i] = now.of_b(i, left);
+                }
+                copies_wait<1>();
+                __syncwarp();
+                const char *const x0 = staged + half * Staged<G>::bytes + j * 16;
 #pragma unroll
                 for (int t = 0; t < 8 * G; ++t) {
                     if (!(tokens >> t & 1u)) continue;              /* the same for the whole warp */
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
-                        if (at + i * kBlock >= a.h_row) continue;
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(h + t * (size_t)a.h_row + at + i * kBlock));
-                        acc.c[0][t] = dot4(now.a[i], x, acc.c[0][t]);
-                        acc.c[1][t] = dot4(now.b[i], x, acc.c[1][t]);
+                        const float4 x = *reinterpret_cast<const float4 *>(x0 + t * (kAhead * kBlock) + i * kBlock);
+                        acc.c[0][t] = dot4(wa[i], x, acc.c[0][t]);
+                        acc.c[1][t] = dot4(wb[i], x, acc.c[1][t]);
                     }
                 }
+                __syncwarp();
             }
         }
+        if (DT == SIFAR_F32) copies_wait<0>();
         acc.store(s_red[warp]);
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 16 * a.tokens; i += kThreads) {
@@ -408,8 +528,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
 
     const char *ra, *rb;
     rows_of(begin, ra, rb);
-    Weights next;
-    load_weights<VEC>(next, ra, rb, j * 16, bytes);
+    Weights<VEC> next;
+    next.load(ra, rb, j * 16, bytes);
     if (DOWN) grid_wait();                                          /* what was loaded so far no kernel writes */
 
     uint32_t listed = 0xFFFFFFFFu, in_expert = 0;
@@ -435,12 +555,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
                 const uint32_t end_of = DOWN ? a.h_row : bytes;
                 if (DOWN || XVEC) {
                     const uint32_t take = off < end_of ? 16u : 0u;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(row + (take ? off : 0u)), "r"(take) : "memory");
+                    copy16(dst, row + (take ? off : 0u), take);
                 } else {
                     *reinterpret_cast<uint4 *>(dst) = off < end_of ? load_shifted(row + off, end_of - off) : make_uint4(0u, 0u, 0u, 0u);
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            copies_commit();
         };
         float acc[P::groups][DT == SIFAR_BF16 ? 4 : 16];
 #pragma unroll
@@ -449,31 +569,33 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
             for (int i = 0; i < (DT == SIFAR_BF16 ? 4 : 16); ++i) acc[q][i] = 0.0f;
         fetch(0, 0);
         for (uint32_t s = 0; s < steps; ++s) {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            copies_wait<0>();
             __syncthreads();                                        /* chunk s is there, chunk s - 1 has been read */
             if (s + 1 < steps) fetch(s + 1, (s + 1) & 1);
             const char *const cols = smem + (s & 1) * (P::groups * 8 * kChunkRow);
 #pragma unroll
             for (int half = 0; half < kChunk / (kAhead * kBlock); ++half) {
                 const uint32_t off = s * kChunk + half * kAhead * kBlock;
-                const Weights now = next;
+                const Weights<VEC> now = next;
                 if (off + kAhead * kBlock < steps * kChunk) {
-                    load_weights<VEC>(next, ra, rb, off + kAhead * kBlock + j * 16, bytes);
+                    next.load(ra, rb, off + kAhead * kBlock + j * 16, bytes);
                 } else {
                     rows_of(u + 1, ra, rb);
-                    load_weights<VEC>(next, ra, rb, j * 16, bytes);
+                    next.load(ra, rb, j * 16, bytes);
                 }
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     if (off + i * kBlock >= bytes) break;
                     const char *const x = cols + half * kAhead * kBlock + i * kBlock + j * 16;
+                    const int left = (int)bytes - (int)(off + i * kBlock + j * 16);
+                    const uint4 wa = now.of_a(i, left), wb = now.of_b(i, left);
                     if constexpr (DT == SIFAR_BF16) {
 #pragma unroll
                         for (int q = 0; q < G; ++q) {
                             if ((uint32_t)q >= groups) break;
-                            multiply_block(acc[q], now.a[i], now.b[i], *reinterpret_cast<const uint4 *>(x + (q * 8 + g) * kChunkRow));
+                            multiply_block(acc[q], wa, wb, *reinterpret_cast<const uint4 *>(x + (q * 8 + g) * kChunkRow));
                             if (P::parts == 2)
-                                multiply_block(acc[q + P::groups - G], now.a[i], now.b[i], *reinterpret_cast<const uint4 *>(x + ((q + G) * 8 + g) * kChunkRow));
+                                multiply_block(acc[q + P::groups - G], wa, wb, *reinterpret_cast<const uint4 *>(x + ((q + G) * 8 + g) * kChunkRow));
                         }
                     } else {
 #pragma unroll
@@ -482,8 +604,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
 #pragma unroll
                             for (int t = 0; t < 8; ++t) {
                                 const float4 v = *reinterpret_cast<const float4 *>(x + (q * 8 + t) * kChunkRow);
-                                acc[q][t] = dot4(now.a[i], v, acc[q][t]);
-                                acc[q][8 + t] = dot4(now.b[i], v, acc[q][8 + t]);
+                                acc[q][t] = dot4(wa, v, acc[q][t]);
+                                acc[q][8 + t] = dot4(wb, v, acc[q][8 + t]);
                             }
                         }
                     }
@@ -589,7 +711,7 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     /* a multiple of 128 bytes and 64 more: two rows' pieces lie in different banks */
     p.x_row = (uint32_t)((g->hidden * es + 127) / 128 * 128 + 64);
     const bool tiles = g->dtype == SIFAR_BF16 && g->hidden % 8 == 0 && g->inter % 8 == 0;      /* as far as the sizes go */
-    p.few = T <= (size_t)(tiles ? kFew : kFewMost) && T * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);
+    p.few = T <= (size_t)(tiles ? kFew : kFewMost) && (T + 3) / 4 * 4 * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);
     p.h_row = (uint32_t)((g->inter * es + 15) / 16 * 16);
     const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
     p.h_bytes = ((p.few ? most * T : choices) * parts * p.h_row + 15) / 16 * 16;
@@ -609,16 +731,16 @@ static cudaError_t launch_shared(void (*kernel)(P...), dim3 grid, size_t shared,
 template <int DT, int G>
 static cudaError_t launch_few(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, const ExpertsArgs &a)
 {
-    const size_t shared = a.tokens * p.x_row;
-    const unsigned ctas = kSms * kFewCtas(G);
+    const size_t shared = (a.tokens + 3) / 4 * 4 * (size_t)p.x_row, staged = DT == SIFAR_F32 ? (size_t)kWarps * 2 * Staged<G>::bytes : 0;
+    const unsigned ctas = kSms * (shared <= kFewShared ? kFewCtas(G) : 1);
     const dim3 grid(ctas), columns(a.hidden < 8 * ctas ? (a.hidden + 7) / 8 : ctas);       /* of the output: 8 at least */
     cudaError_t e = !gu_vec ? launch_shared(k_up_few<DT, G, false, false>, grid, shared, stream, a)
                     : x_vec ? launch_shared(k_up_few<DT, G, true, true>, grid, shared, stream, a) : launch_shared(k_up_few<DT, G, true, false>, grid, shared, stream, a);
     if (e) return e;
     if constexpr (DT == SIFAR_BF16 && G == 1) {
-        if (a.tokens <= 4) return dn_vec ? launch_shared(k_down_few<DT, G, true, true>, columns, 0, stream, a) : launch_shared(k_down_few<DT, G, false, true>, columns, 0, stream, a);
+        if (a.tokens <= 4) return dn_vec ? launch_shared(k_down_few<DT, G, true, true>, columns, staged, stream, a) : launch_shared(k_down_few<DT, G, false, true>, columns, staged, stream, a);
     }
-    return dn_vec ? launch_shared(k_down_few<DT, G, true, false>, columns, 0, stream, a) : launch_shared(k_down_few<DT, G, false, false>, columns, 0, stream, a);
+    return dn_vec ? launch_shared(k_down_few<DT, G, true, false>, columns, staged, stream, a) : launch_shared(k_down_few<DT, G, false, false>, columns, staged, stream, a);
 }
 
 template <int DT>
