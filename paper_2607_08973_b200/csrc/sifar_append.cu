@@ -1,11 +1,12 @@
 /*
  * sifar_append.cu - new tokens' queries and keys turned by their positions, keys and values into the paged cache.
  *
- * A CTA per token: cosines and sines of the token's angles once, in shared memory, for all its heads.  Each thread has
- * the first loads of its elements under way while they are computed.  Bound by memory: every element is read and
- * written once.
+ * A CTA per token: cosines and sines of the token's angles once, in shared memory, for all its heads.  A thread has the same
+ * place in every head that it takes; its first loads, into shared memory, are under way while it is looked up where the token
+ * belongs and the angles are computed.  Bound by memory: every element is read and written once.
  */
 #include "sifar_cache.cuh"
+#include "sifar_norm_shape.cuh"
 
 namespace sifar {
 
@@ -19,7 +20,6 @@ struct AppendArgs {
     uint32_t sequences;
     uint32_t heads, kv_heads, dim, half;               /* half = rotary_dim / 2 */
     uint32_t turned, copied;                           /* items of a head that turns, of one that is copied */
-    uint32_t turned_magic, copied_magic;               /* ceil(2^32 / items), items > 1: exact quotients below 2^24 */
 };
 
 /* V elements from one place on, as binary32 or as they are. */
@@ -31,6 +31,7 @@ template <int DT, int V> struct Piece {
         if (V == 1) w[0] = *reinterpret_cast<const T *>(p);
         else *reinterpret_cast<uint4 *>(w) = *reinterpret_cast<const uint4 *>(p);
     }
+    __device__ __forceinline__ void load_shared(const uint4 *p) { *reinterpret_cast<uint4 *>(w) = *p; }
     __device__ __forceinline__ void store(char *p) const
     {
         if (V == 1) *reinterpret_cast<T *>(p) = (T)w[0];
@@ -50,109 +51,99 @@ template <int DT, int V> struct Piece {
     }
 };
 
+__device__ __forceinline__ void copy16(uint4 *to, const char *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
 /*
  * An item is what a thread loads, turns and stores at once: V pairs in two pieces (halves apart), V / 2 pairs in one
  * piece (interleaved; V = 1: one pair in two pieces), or a piece that is copied.
  */
 template <int DT, int V, bool INTER>
-__global__ void __launch_bounds__(512) k_append(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(512, 3) k_append(const __grid_constant__ AppendArgs a)
 {
-    constexpr int es = DT == SIFAR_BF16 ? 2 : 4, B = 4;
+    constexpr int es = DT == SIFAR_BF16 ? 2 : 4, B = 2;
     constexpr bool kOne = INTER && V > 1;              /* a pair lies within a piece */
-    __shared__ float s_cos[SIFAR_CACHE_MAX_HEAD_DIM / 2], s_sin[SIFAR_CACHE_MAX_HEAD_DIM / 2];
+    constexpr int n = kOne ? V / 2 : V;                /* pairs of an item */
+    extern __shared__ uint4 s_item[];                  /* whole pieces: a thread's first items, [piece][thread] */
+    __shared__ __align__(16) float s_cos[SIFAR_CACHE_MAX_HEAD_DIM / 2], s_sin[SIFAR_CACHE_MAX_HEAD_DIM / 2];
     const uint32_t token = blockIdx.x;
     grid_let_next_in();
     grid_wait();
     const int position = a.position[token];
     const uint32_t sequence = a.sequence ? (uint32_t)a.sequence[token] : token;
-    if (position < 0 || sequence >= a.sequences) return;
-
-    const uint32_t n_turn = (a.heads + a.kv_heads) * a.turned, n = n_turn + a.kv_heads * a.copied;
+    /* the thread's item of a head, and the first and the next of its heads */
     const uint32_t pairs = kOne ? 2 * a.half / V : a.half / V;       /* items of a head that have pairs */
-    const char *const q = a.q + token * a.ld_q, *const k = a.k + token * a.ld_k, *const v = a.v + token * a.ld_v;
+    const uint32_t first = threadIdx.x / a.turned, i = threadIdx.x - first * a.turned, step = blockDim.x / a.turned;
+    const bool turn = i < pairs;
+    const uint32_t x = turn ? (kOne ? i * V : INTER ? 2 * i : i * V) : 2 * a.half + (i - pairs) * V;     /* elements of the head */
+    const uint32_t y = x + (INTER ? 1u : a.half);                    /* the second piece: of pairs in two */
+    const bool two = turn && !kOne;
+    const uint32_t heads = first < step ? a.heads + a.kv_heads : 0u;
+    const char *const q = a.q + token * a.ld_q, *const k = a.k + token * a.ld_k;
     char *const q_out = a.q_out + token * a.ld_q_out;
+    auto source = [&](uint32_t h) { return h < a.heads ? q + (size_t)h * a.dim * es : k + (size_t)(h - a.heads) * a.dim * es; };
+    /* the first loads go out before it is known where the token belongs */
+    const uint32_t vfirst = threadIdx.x / a.copied, vi = threadIdx.x - vfirst * a.copied, vstep = blockDim.x / a.copied, values = vfirst < vstep ? a.kv_heads : 0u;
+    const char *const v = a.v + token * a.ld_v + vi * V * es;
+    auto slot = [&](int i) { return s_item + i * blockDim.x + threadIdx.x; };
+    if constexpr (V > 1) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const uint32_t h = first + b * step;
+            if (h >= heads) break;
+            copy16(slot(2 * b), source(h) + x * es);
+            if (two) copy16(slot(2 * b + 1), source(h) + y * es);
+        }
+        if (vfirst < values) copy16(slot(2 * B), v + (size_t)vfirst * a.dim * es);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (position < 0 || sequence >= a.sequences) return;
     const long long at = token_offset(a.pages, a.pages.table + sequence * a.pages.ld_table, (uint32_t)position);
+    auto target = [&](uint32_t h) { return h < a.heads ? q_out + (size_t)h * a.dim * es : at < 0 ? nullptr : a.k_cache + at + (h - a.heads) * a.pages.stride_head; };
 
-    /* item -> where its pieces lie: the element offsets in the head's row, the second one 0 where there is no second */
-    struct Item { const char *src; char *dst; uint32_t first, second, i; bool turn; };
-    auto item = [&](uint32_t idx) {
-        Item t;
-        uint32_t head;
-        if (idx < n_turn) {
-            head = a.turned == 1 ? idx : __umulhi(idx, a.turned_magic);
-            t.i = idx - head * a.turned;
-            t.turn = t.i < pairs;
-            if (t.turn) {
-                t.first = kOne ? t.i * V : INTER ? 2 * t.i : t.i * V;
-                t.second = kOne ? 0 : INTER ? t.first + 1 : t.first + a.half;
-            } else {
-                t.first = 2 * a.half + (t.i - pairs) * V;
-                t.second = 0;
-            }
-            const bool query = head < a.heads;
-            if (!query) head -= a.heads;
-            t.src = (query ? q : k) + head * a.dim * es;
-            t.dst = query ? q_out + head * a.dim * es : at < 0 ? nullptr : a.k_cache + at + head * a.pages.stride_head;
+    /* the angle in full turns, its whole ones taken off before it is narrowed: far positions lose nothing */
+    for (uint32_t j = threadIdx.x; j < a.half; j += blockDim.x) {
+        const double turns = (double)position * (double)a.inv_freq[j] * 0.15915494309189533577;
+        sincospif((float)(2.0 * (turns - rint(turns))), &s_sin[j], &s_cos[j]);
+    }
+    __syncthreads();
+    if constexpr (V > 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    /* values: copied */
+    if (at >= 0) {
+        char *const to = a.v_cache + at + vi * V * es;
+        for (uint32_t h = vfirst; h < values; h += vstep) {
+            Piece<DT, V> w;
+            if (V > 1 && h == vfirst) w.load_shared(slot(2 * B));
+            else w.load(v + (size_t)h * a.dim * es);
+            w.store(to + h * a.pages.stride_head);
+        }
+    }
+    uint32_t b = 0;
+    for (uint32_t h = first; h < heads; h += step, ++b) {
+        char *const to = target(h);
+        if (!to) continue;
+        Piece<DT, V> p, r;
+        if (V > 1 && b < B) {
+            p.load_shared(slot(2 * b));
+            if (two) r.load_shared(slot(2 * b + 1));
         } else {
-            idx -= n_turn;
-            head = a.copied == 1 ? idx : __umulhi(idx, a.copied_magic);
-            t.i = idx - head * a.copied;
-            t.turn = false;
-            t.first = t.i * V;
-            t.second = 0;
-            t.src = v + head * a.dim * es;
-            t.dst = at < 0 ? nullptr : a.v_cache + at + head * a.pages.stride_head;
+            p.load(source(h) + x * es);
+            if (two) r.load(source(h) + y * es);
         }
-        return t;
-    };
-
-    bool ready = false;
-    for (uint32_t i0 = threadIdx.x; i0 < n || !ready; i0 += B * blockDim.x) {
-        Piece<DT, V> p[B], r[B];
+        if (turn) {
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const uint32_t idx = i0 + b * blockDim.x;
-            if (idx >= n) continue;
-            const Item t = item(idx);
-            if (!t.dst) continue;
-            p[b].load(t.src + t.first * es);
-            if (t.second) r[b].load(t.src + t.second * es);
-        }
-        if (!ready) {
-            /* the angle in full turns, its whole ones taken off before it is narrowed: far positions lose nothing */
-            for (uint32_t i = threadIdx.x; i < a.half; i += blockDim.x) {
-                const double turns = (double)position * (double)a.inv_freq[i] * 0.15915494309189533577;
-                sincospif((float)(2.0 * (turns - rint(turns))), &s_sin[i], &s_cos[i]);
+            for (int e = 0; e < n; ++e) {
+                const float c = s_cos[i * n + e], s = s_sin[i * n + e];
+                const float u = p.get(kOne ? 2 * e : e), w = kOne ? p.get(2 * e + 1) : r.get(e);
+                const float first_of = u * c - w * s, second_of = u * s + w * c;
+                if (kOne) { p.set(2 * e, first_of); p.set(2 * e + 1, second_of); }
+                else { p.set(e, first_of); r.set(e, second_of); }
             }
-            __syncthreads();
-            ready = true;
         }
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const uint32_t idx = i0 + b * blockDim.x;
-            if (idx >= n) continue;
-            const Item t = item(idx);
-            if (!t.dst) continue;
-            if (t.turn) {
-                if (kOne) {
-#pragma unroll
-                    for (int e = 0; e < V / 2; ++e) {
-                        const float c = s_cos[t.i * (V / 2) + e], s = s_sin[t.i * (V / 2) + e], x = p[b].get(2 * e), y = p[b].get(2 * e + 1);
-                        p[b].set(2 * e, x * c - y * s);
-                        p[b].set(2 * e + 1, x * s + y * c);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float c = s_cos[t.i * V + e], s = s_sin[t.i * V + e], x = p[b].get(e), y = r[b].get(e);
-                        p[b].set(e, x * c - y * s);
-                        r[b].set(e, x * s + y * c);
-                    }
-                }
-            }
-            p[b].store(t.dst + t.first * es);
-            if (t.second) r[b].store(t.dst + t.second * es);
-        }
+        p.store(to + x * es);
+        if (two) r.store(to + y * es);
     }
 }
 
@@ -216,20 +207,20 @@ extern "C" int sifar_cache_append(const sifar_cache_append_args *g, void *stream
     const size_t V = vec ? per : 1;
     a.turned = (uint32_t)((inter && vec ? 2 * half : half) / V + (c.dim - 2 * half) / V);
     a.copied = (uint32_t)(c.dim / V);
-    const auto magic = [](uint32_t d) { return d == 1 ? 0u : (uint32_t)((((unsigned long long)1 << 32) + d - 1) / d); };
-    a.turned_magic = magic(a.turned); a.copied_magic = magic(a.copied);
-    const size_t items = (nq + nk) / c.dim * a.turned + (size_t)g->kv_heads * a.copied;
+    /* up to 256 threads, 512 for few tokens: about two items of each */
+    const size_t items = ((size_t)a.heads + a.kv_heads) * a.turned, most = T < 2 * kSms ? 512 : 256;
     size_t threads = 64;
-    while (threads < 512 && threads * 2 < items) threads *= 2;
+    while (threads < a.turned || threads < a.copied || (threads < most && threads * 2 < items)) threads *= 2;
+    const size_t shared = vec ? threads * 5 * 16 : 0;                /* two items of a key or query head, one of a value's */
     const dim3 grid((unsigned)T), block((unsigned)threads);
     const cudaStream_t st = (cudaStream_t)stream;
     cudaError_t err;
     if (g->dtype == SIFAR_BF16)
-        err = !vec ? (inter ? launch_op(k_append<SIFAR_BF16, 1, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_BF16, 1, false>, grid, block, 1, 0, st, a))
-                   : (inter ? launch_op(k_append<SIFAR_BF16, 8, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_BF16, 8, false>, grid, block, 1, 0, st, a));
+        err = !vec ? (inter ? launch_op(k_append<SIFAR_BF16, 1, true>, grid, block, 1, shared, st, a) : launch_op(k_append<SIFAR_BF16, 1, false>, grid, block, 1, shared, st, a))
+                   : (inter ? launch_op(k_append<SIFAR_BF16, 8, true>, grid, block, 1, shared, st, a) : launch_op(k_append<SIFAR_BF16, 8, false>, grid, block, 1, shared, st, a));
     else
-        err = !vec ? (inter ? launch_op(k_append<SIFAR_F32, 1, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_F32, 1, false>, grid, block, 1, 0, st, a))
-                   : (inter ? launch_op(k_append<SIFAR_F32, 4, true>, grid, block, 1, 0, st, a) : launch_op(k_append<SIFAR_F32, 4, false>, grid, block, 1, 0, st, a));
+        err = !vec ? (inter ? launch_op(k_append<SIFAR_F32, 1, true>, grid, block, 1, shared, st, a) : launch_op(k_append<SIFAR_F32, 1, false>, grid, block, 1, shared, st, a))
+                   : (inter ? launch_op(k_append<SIFAR_F32, 4, true>, grid, block, 1, shared, st, a) : launch_op(k_append<SIFAR_F32, 4, false>, grid, block, 1, shared, st, a));
     SIFAR_CUDA(err);
     return SIFAR_OK;
 }
