@@ -246,27 +246,26 @@ __device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int st
 }
 
 /* Issues the copies of an item's queries, into the place of a strip's keys: row r of them where token r's key would lie. */
-template <int DT, int DP>
+template <int DT, int DP, int ROWS>
 __device__ __forceinline__ void fetch_queries(const AttentionArgs &a, char *ring, int stage, const char *q, uint32_t rows)
 {
     using R = Ring<DT, DP>;
     char *const to = ring + stage * 2 * R::strip;
-    const uint32_t lane = threadIdx.x & 31;
+    const uint32_t lane = threadIdx.x & 31, row = a.dim * R::es;
     if (a.q_vec) {
-        const uint32_t pieces = a.dim * R::es / 16;
 #pragma unroll 4
-        for (uint32_t i = lane; i < (R::tokens > 8 ? 16u : 8u) * R::chunks; i += 32) {
+        for (uint32_t i = lane; i < ROWS * R::chunks; i += 32) {
             const uint32_t r = i / R::chunks, piece = i % R::chunks;
-            const bool there = r < rows && piece < pieces;
-            copy16(shared_at(to + r * R::row + R::place(r, piece) * 16), there ? q + (size_t)r * a.dim * R::es + piece * 16 : a.q, there ? 16u : 0u);
+            const bool there = r < rows && piece * 16 < row;
+            copy16(shared_at(to + r * R::row + R::place(r, piece) * 16), a.q + (there ? q - a.q + (r * row + piece * 16) : 0), there ? 16u : 0u);
         }
     } else {
         using T = typename Elem<DT>::type;
 #pragma unroll 4
-        for (uint32_t i = lane; i < (R::tokens > 8 ? 16u : 8u) * DP; i += 32) {
+        for (uint32_t i = lane; i < ROWS * DP; i += 32) {
             const uint32_t r = i / DP, d = i % DP;
             *reinterpret_cast<T *>(to + r * R::row + R::place(r, d * R::es / 16) * 16 + d * R::es % 16) =
-                r < rows && d < a.dim ? reinterpret_cast<const T *>(q)[(size_t)r * a.dim + d] : (T)0;
+                r < rows && d < a.dim ? reinterpret_cast<const T *>(q)[r * a.dim + d] : (T)0;
         }
     }
 }
@@ -585,23 +584,27 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
 
     C then = now;                                                 /* the strip to be fetched next */
     bool queries = true;                                          /* ... or the queries of its item */
-    auto offset_of = [&](const C &c) -> long long {
-        const uint32_t t = c.lo + c.strip * R::tokens + lane % R::tokens;
-        return c.at < end && t < c.hi ? token_offset(a.pages, a.pages.table + c.sequence * a.pages.ld_table, t) : -1ll;
+    /* the lane's token of strip `then`: its page, asked for a strip ahead, and its place there */
+    int page;
+    uint32_t in;
+    auto look_up = [&] {
+        const uint32_t t = then.lo + then.strip * R::tokens + lane % R::tokens, at = page_of(a.pages, t, in);
+        page = -1;
+        if (then.at < end && t < then.hi && at < a.pages.max_pages) page = __ldg(a.pages.table + then.sequence * a.pages.ld_table + at);
     };
     unsigned long long seen = 0;                                  /* 16 bits per stage: its tokens that count */
-    long long next = offset_of(then);
+    look_up();
     auto fetch_next = [&](int stage) {
         if (then.at < end) {
             const uint32_t kv_head = then.item / a.chunks, chunk = then.item - kv_head * a.chunks;
             if (queries) {
                 const uint32_t head = kv_head * a.group + chunk * a.rows;
-                fetch_queries<DT, DP>(a, ring, stage, a.q + then.sequence * a.ld_q + (size_t)head * a.dim * es, min(a.rows, a.group - chunk * a.rows));
+                fetch_queries<DT, DP, ROWS>(a, ring, stage, a.q + then.sequence * a.ld_q + (size_t)head * a.dim * es, min(a.rows, a.group - chunk * a.rows));
                 queries = false;
             } else {
-                const long long at = next;
+                const long long at = place_offset(a.pages, page, in);
                 queries = then.advance(a, items);
-                next = offset_of(then);
+                look_up();
                 seen = (seen & ~(0xFFFFull << (16 * stage))) | (unsigned long long)(__ballot_sync(0xFFFFFFFFu, at >= 0) & ((1u << R::tokens) - 1u)) << (16 * stage);
                 fetch<DT, DP, VEC>(a, ring, stage, at, kv_head * a.pages.stride_head);
             }
@@ -666,24 +669,30 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
         }
         __syncwarp();
         /* several loads before the first store: a warp has nobody to hide them behind */
-        for (uint32_t i0 = lane; i0 < rows * (DP / 4); i0 += 32 * 4) {
-            float4 v[4];
-            float f[4];
+        constexpr uint32_t kPieces = DP / 4, kAtOnce = kPieces < 32 ? 32 / kPieces : 1, kTurns = kPieces > 32 ? kPieces / 32 : 1, kRows = 4 / kTurns;
+        for (uint32_t r0 = lane / kPieces; r0 < rows; r0 += kAtOnce * kRows) {
+            float4 v[kRows][kTurns];
+            float f[kRows];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t r = min(i0 + k * 32, rows * (DP / 4) - 1) / (DP / 4), piece = (i0 + k * 32) % (DP / 4);
-                v[k] = *reinterpret_cast<const float4 *>(smem + values + value_place<DP>(r, piece) * 4);
+            for (uint32_t k = 0; k < kRows; ++k) {
+                const uint32_t r = min(r0 + k * kAtOnce, rows - 1);
                 f[k] = s_w[warp][r];
+#pragma unroll
+                for (uint32_t c = 0; c < kTurns; ++c) v[k][c] = *reinterpret_cast<const float4 *>(smem + values + value_place<DP>(r, lane % kPieces + 32 * c) * 4);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t i = i0 + k * 32, r = i / (DP / 4), piece = i % (DP / 4);
-                if (i >= rows * (DP / 4)) break;
-                if (all) {
-                    const float x[4] = {v[k].x * f[k], v[k].y * f[k], v[k].z * f[k], v[k].w * f[k]};
-                    store_out<DT>(out + (size_t)r * a.dim, x, piece * 4, a.dim, a.out_vec);
-                } else {
-                    *reinterpret_cast<float4 *>(part + r * DP + piece * 4) = v[k];
+            for (uint32_t k = 0; k < kRows; ++k) {
+                const uint32_t r = r0 + k * kAtOnce;
+                if (r >= rows) break;
+#pragma unroll
+                for (uint32_t c = 0; c < kTurns; ++c) {
+                    const uint32_t d = (lane % kPieces + 32 * c) * 4;
+                    if (all) {
+                        const float x[4] = {v[k][c].x * f[k], v[k][c].y * f[k], v[k][c].z * f[k], v[k][c].w * f[k]};
+                        store_out<DT>(out + r * a.dim, x, d, a.dim, a.out_vec);
+                    } else {
+                        *reinterpret_cast<float4 *>(part + r * DP + d) = v[k][c];
+                    }
                 }
             }
         }

@@ -14,16 +14,29 @@ struct Pages {
     unsigned long long ld_table;         /* entries between two sequences */
     unsigned long long stride_page, stride_token, stride_head;
     uint32_t pages, page_size, max_pages;
+    uint32_t magic, shift;               /* n / page_size = n * magic >> 32 >> shift for n < 2^31; page_size 1: magic 0 */
 };
+
+/* Number of the page that holds token n, and n's place in it. */
+__device__ __forceinline__ uint32_t page_of(const Pages &p, uint32_t n, uint32_t &in)
+{
+    const uint32_t at = p.magic ? __umulhi(n, p.magic) >> p.shift : n;
+    in = n - at * p.page_size;
+    return at;
+}
+/* Bytes from the start of the cache to place `in` of a page (its first head), or -1 where there is no such page. */
+__device__ __forceinline__ long long place_offset(const Pages &p, int page, uint32_t in)
+{
+    if ((uint32_t)page >= p.pages) return -1;                 /* negative ones too */
+    return (long long)((unsigned long long)page * p.stride_page + (unsigned long long)in * p.stride_token);
+}
 
 /* Bytes from the start of the cache to token n of a sequence (its first head), or -1 where the page is not there. */
 __device__ __forceinline__ long long token_offset(const Pages &p, const int *row, uint32_t n)
 {
-    const uint32_t at = n / p.page_size;
-    if (at >= p.max_pages) return -1;
-    const int page = __ldg(row + at);
-    if ((uint32_t)page >= p.pages) return -1;                 /* negative ones too */
-    return (long long)((unsigned long long)page * p.stride_page + (unsigned long long)(n - at * p.page_size) * p.stride_token);
+    uint32_t in;
+    const uint32_t at = page_of(p, n, in);
+    return at < p.max_pages ? place_offset(p, __ldg(row + at), in) : -1;
 }
 
 /* ------------------------------------------------------------------------ */
@@ -109,6 +122,12 @@ inline Pages device_pages(const CacheShape &c, const int *table)
     p.table = table; p.ld_table = c.ld_table;
     p.stride_page = c.stride_page * c.es; p.stride_token = c.stride_token * c.es; p.stride_head = c.stride_head * c.es;
     p.pages = (uint32_t)c.pages; p.page_size = (uint32_t)c.page_size; p.max_pages = (uint32_t)c.max_pages;
+    /* magic = 2^(31 + l) / page_size rounded up, 2^l the next power of two: n * magic / 2^(31 + l) is less than 1 / page_size above
+       n / page_size */
+    uint32_t l = 0;
+    while (((uint64_t)1 << l) < c.page_size) ++l;
+    p.magic = l ? (uint32_t)((((uint64_t)1 << (31 + l)) + c.page_size - 1) / c.page_size) : 0u;
+    p.shift = l ? l - 1 : 0u;
     return p;
 }
 
