@@ -2,25 +2,28 @@
  * sifar_attention.cu - attention of one new token per sequence over a paged cache, split over the cache's length.
  *
  * An item is a key head of a sequence with up to 16 (binary32: 8) of the query heads that read it.  All items' strips of 16
- * tokens in a row are cut into equal shares, one per warp, whatever the lengths: a warp goes through the end of one item, some
- * whole ones and the start of another without meeting any other warp.  Its strips come through a ring of its own in shared
- * memory, filled by asynchronous 16-byte copies two strips ahead, across items too; an item's queries come the same way, before its strips.  An item that several warps had is put
- * together by a second kernel from their maxima, sums and weighted values; where a CTA's warps all have the same item they
- * join their parts first.
+ * tokens in a row are cut into equal shares, one per team, whatever the lengths: a team goes through the end of one item, some
+ * whole ones and the start of another without meeting any other team.  Its strips come through a ring of its own in shared
+ * memory, filled by asynchronous 16-byte copies two strips ahead, across items too; an item's queries come the same way, before
+ * its strips.  An item that several teams had is put together by a second kernel from their maxima, sums and weighted values;
+ * where a CTA's teams all have the same item they join their parts first.
+ *
+ * A team is a warp, and where an item has more than eight query heads in bf16 two warps, eight heads each, that fill and read the
+ * same ring.
  */
 #include "sifar_cache.cuh"
 #include "sifar_norm_shape.cuh"
 
 namespace sifar {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kTeams = 4;                    /* of a CTA */
 constexpr int kItemCost = 1;                 /* what an item's start and end count as, in strips */
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-/* Where a split item lies in the workspace: partials of warps first .. last, in the order of the tokens. */
+/* Where a split item lies in the workspace: partials of teams first .. last, in the order of the tokens. */
 struct Split { int sequence, item, first, last, slot, one0, one1, pad; };
-/* slot: of `first`'s partial, 0 of the others; first < 0: none.  Warps one0 .. one1 - 1 are whole CTAs that left one partial each, in
-   the place of their first warp. */
+/* slot: of `first`'s partial, 0 of the others; first < 0: none.  Teams one0 .. one1 - 1 are whole CTAs that left one partial each, in
+   the place of their first team. */
 
 struct AttentionArgs {
     const char *q, *k, *v;
@@ -28,8 +31,8 @@ struct AttentionArgs {
     float *lse;
     const int *lengths;
     Pages pages;
-    Split *splits;                           /* one per warp */
-    float *partial;                          /* warp x 2 partials */
+    Split *splits;                           /* one per team */
+    float *partial;                          /* team x 2 partials */
     unsigned long long ld_q, ld_out;         /* bytes */
     uint32_t sequences, window, limit;       /* limit = max_pages * page_size */
     uint32_t heads, kv_heads, group, chunks, rows, dim;   /* rows = query heads of an item, chunks of them per key head */
@@ -57,7 +60,7 @@ __device__ __forceinline__ unsigned long long quotient(unsigned long long n, uin
     return n >> 32 ? n / d : (unsigned long long)((uint32_t)n / d);
 }
 
-/* Where in the row of all items' strips (each followed by kItemCost places without one) a warp is. */
+/* Where in the row of all items' strips (each followed by kItemCost places without one) a team is. */
 template <int TOKENS> struct Cursor {
     unsigned long long at;                   /* place in the row */
     uint32_t sequence, item, strip;          /* item: key head and chunk of its query heads */
@@ -84,16 +87,17 @@ template <int TOKENS> struct Cursor {
     }
 };
 
-/* The row, this CTA's part of it and where its warps' shares begin. */
+/* The row and what of it is a team's. */
 struct Shares { unsigned long long total, share; };
 
 /*
- * Every thread adds up the places of a run of sequences; the one whose run holds the begin of a warp's share walks it.
+ * Every thread adds up the places of a run of sequences; the one whose run holds the begin of a team's share walks it.
  */
-template <int TOKENS>
+template <int TOKENS, int WARPS>
 __device__ __forceinline__ Shares find_shares(const AttentionArgs &a, unsigned long long *s_sum, Cursor<TOKENS> *s_start)
 {
-    const uint32_t run = (a.sequences + kThreads - 1) / kThreads, s0 = min(a.sequences, threadIdx.x * run), s1 = min(a.sequences, s0 + run);
+    constexpr uint32_t threads = 32 * WARPS;
+    const uint32_t run = (a.sequences + threads - 1) / threads, s0 = min(a.sequences, threadIdx.x * run), s1 = min(a.sequences, s0 + run);
     const uint32_t items = a.kv_heads * a.chunks;
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     auto places = [&](uint32_t s) {
@@ -114,15 +118,15 @@ __device__ __forceinline__ Shares find_shares(const AttentionArgs &a, unsigned l
     unsigned long long before = 0;
     Shares r{0, 0};
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
         if (w < warp) before += s_sum[w];
         r.total += s_sum[w];
     }
     before += sum - mine;
-    r.share = quotient(r.total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
+    r.share = quotient(r.total + gridDim.x * kTeams - 1, gridDim.x * kTeams);
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        const unsigned long long begin = r.share * (blockIdx.x * kWarps + w);
+    for (int w = 0; w < kTeams; ++w) {
+        const unsigned long long begin = r.share * (blockIdx.x * kTeams + w);
         if (begin < before || begin >= before + mine) continue;
         Cursor<TOKENS> c;
         unsigned long long here = before;
@@ -197,9 +201,9 @@ template <int DT, int DP> struct Ring {
     }
 };
 
-/* Issues the copies of the strip from token t0 on.  `offset` is that of token t0 + (lane % tokens), -1 if it is masked. */
-template <int DT, int DP, bool VEC>
-__device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int stage, long long offset, unsigned long long head)
+/* Issues the copies of a strip, a warp of a team its part of the tokens.  `offset` is that of token lane % tokens, -1 if it is masked. */
+template <int DT, int DP, int TW, bool VEC>
+__device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int stage, long long offset, unsigned long long head, int sub)
 {
     using R = Ring<DT, DP>;
     const int lane = threadIdx.x & 31;
@@ -208,8 +212,8 @@ __device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int st
         /* R::chunks lanes per row */
         constexpr int rows = 32 / R::chunks > 0 ? 32 / R::chunks : 1, per = R::chunks > 32 ? R::chunks / 32 : 1;
 #pragma unroll
-        for (int r0 = 0; r0 < R::tokens; r0 += rows) {
-            const int r = r0 + (R::chunks >= 32 ? 0 : lane / R::chunks);
+        for (int i = 0; i < R::tokens / TW; i += rows) {
+            const int r = sub * (R::tokens / TW) + i + (R::chunks >= 32 ? 0 : lane / R::chunks);
             const long long at = __shfl_sync(0xFFFFFFFFu, offset, r);
 #pragma unroll
             for (int c = 0; c < per; ++c) {
@@ -224,7 +228,7 @@ __device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int st
     } else {
         using T = typename Elem<DT>::type;
 #pragma unroll 1
-        for (int r = 0; r < R::tokens; ++r) {
+        for (int r = sub * (R::tokens / TW); r < (sub + 1) * (R::tokens / TW); ++r) {
             const long long at = __shfl_sync(0xFFFFFFFFu, offset, r);
             T k[DP / 32], v[DP / 32];
 #pragma unroll
@@ -245,9 +249,9 @@ __device__ __forceinline__ void fetch(const AttentionArgs &a, char *ring, int st
     }
 }
 
-/* Issues the copies of an item's queries, into the place of a strip's keys: row r of them where token r's key would lie. */
+/* Issues the copies of an item's queries r0 .. r0 + ROWS - 1, into the place of a strip's keys: row r of them where token r's key would lie. */
 template <int DT, int DP, int ROWS>
-__device__ __forceinline__ void fetch_queries(const AttentionArgs &a, char *ring, int stage, const char *q, uint32_t rows)
+__device__ __forceinline__ void fetch_queries(const AttentionArgs &a, char *ring, int stage, const char *q, uint32_t rows, uint32_t r0)
 {
     using R = Ring<DT, DP>;
     char *const to = ring + stage * 2 * R::strip;
@@ -255,7 +259,7 @@ __device__ __forceinline__ void fetch_queries(const AttentionArgs &a, char *ring
     if (a.q_vec) {
 #pragma unroll 4
         for (uint32_t i = lane; i < ROWS * R::chunks; i += 32) {
-            const uint32_t r = i / R::chunks, piece = i % R::chunks;
+            const uint32_t r = r0 + i / R::chunks, piece = i % R::chunks;
             const bool there = r < rows && piece * 16 < row;
             copy16(shared_at(to + r * R::row + R::place(r, piece) * 16), a.q + (there ? q - a.q + (r * row + piece * 16) : 0), there ? 16u : 0u);
         }
@@ -263,7 +267,7 @@ __device__ __forceinline__ void fetch_queries(const AttentionArgs &a, char *ring
         using T = typename Elem<DT>::type;
 #pragma unroll 4
         for (uint32_t i = lane; i < ROWS * DP; i += 32) {
-            const uint32_t r = i / DP, d = i % DP;
+            const uint32_t r = r0 + i / DP, d = i % DP;
             *reinterpret_cast<T *>(to + r * R::row + R::place(r, d * R::es / 16) * 16 + d * R::es % 16) =
                 r < rows && d < a.dim ? reinterpret_cast<const T *>(q)[r * a.dim + d] : (T)0;
         }
@@ -280,41 +284,33 @@ template <int DP> __device__ __forceinline__ int value_place(int row, int piece)
 /* what a warp holds of an item                                              */
 /* ------------------------------------------------------------------------ */
 /*
- * bf16: matrix instructions of 16 rows (query heads) x 16 x 8.  Up to eight heads (ROWS = 8) take the upper half of the
- * rows, and the probabilities go in as two bf16 values, the rounded one above and what it leaves below: they keep 16 bits
- * at no further instruction.  With 16 heads that takes a second product.
+ * bf16: matrix instructions of 16 rows x 16 x 8.  A warp's eight query heads take the upper half of the rows, and the
+ * probabilities go in as two bf16 values, the rounded one above and what it leaves below: they keep 16 bits at no further
+ * instruction.
  */
-template <int DP, int ROWS> struct StateBf16 {
+template <int DP> struct StateBf16 {
     using R = Ring<SIFAR_BF16, DP>;
-    static constexpr int H = ROWS / 8;
-    uint32_t q[DP / 16][2 * H];
+    uint32_t q[DP / 16][2];
     float o[DP / 8][4];
-    float m[H], l[H];                               /* l: this lane's columns */
+    float m, l;                                     /* l: this lane's columns */
 
     __device__ __forceinline__ void clear()
     {
-#pragma unroll
-        for (int h = 0; h < H; ++h) { m[h] = -INFINITY; l[h] = 0.0f; }
+        m = -INFINITY; l = 0.0f;
 #pragma unroll
         for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
     }
-    /* From the queries' place in the ring. */
-    __device__ __forceinline__ void begin(const char *ring, int stage, float *)
+    /* From the queries' place in the ring, rows r0 .. r0 + 7. */
+    __device__ __forceinline__ void begin(const char *ring, int stage, int r0, float *)
     {
-        const int lane = threadIdx.x & 31, row = H == 1 ? lane & 7 : lane & 15;
+        const int lane = threadIdx.x & 31, row = r0 + (lane & 7);
         const uint32_t qs = shared_at(ring + stage * 2 * R::strip);
         clear();
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-            if constexpr (H == 1) {
-                /* two blocks of 16 columns at a time: rows 0 .. 7 of four pieces */
-                if (i % 2) continue;
-                uint32_t b[4];
-                load_matrices(b, qs + row * R::row + R::place(row, 2 * i + (lane >> 3)) * 16);
-                q[i][0] = b[0]; q[i][1] = b[1]; q[i + 1][0] = b[2]; q[i + 1][1] = b[3];
-            } else {
-                load_matrices(q[i], qs + row * R::row + R::place(row, 2 * i + (lane >> 4)) * 16);
-            }
+        for (int i = 0; i < DP / 16; i += 2) {      /* four pieces at a time */
+            uint32_t b[4];
+            load_matrices(b, qs + row * R::row + R::place(row, 2 * i + (lane >> 3)) * 16);
+            q[i][0] = b[0]; q[i][1] = b[1]; q[i + 1][0] = b[2]; q[i + 1][1] = b[3];
         }
     }
 
@@ -331,77 +327,54 @@ template <int DP, int ROWS> struct StateBf16 {
                 uint32_t b[4];
                 load_matrices(b, ks + row * R::row + R::place(row, 2 * i + half) * 16);
                 float (&c)[2][4] = i & 1 ? s2 : s;
-                multiply(c[0], q[i][0], H == 1 ? 0u : q[i][H - 1], q[i][H], H == 1 ? 0u : q[i][2 * H - 1], b[0], b[1]);
-                multiply(c[1], q[i][0], H == 1 ? 0u : q[i][H - 1], q[i][H], H == 1 ? 0u : q[i][2 * H - 1], b[2], b[3]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { s[0][i] += s2[0][i]; s[1][i] += s2[1][i]; }
-        }
-        float keep[H];
-        uint32_t p[H][2], rest[H][2];
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-            float x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool in = seen >> ((i >> 1) * 8 + 2 * j + (i & 1)) & 1u;
-                x[i] = in ? s[i >> 1][2 * h + (i & 1)] * a.scale : -INFINITY;
-            }
-            float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const float now = fmaxf(m[h], top), ref = now == -INFINITY ? 0.0f : now;
-            keep[h] = exp2f(m[h] - ref);
-            m[h] = now;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = exp2f(x[i] - ref);
-            l[h] = l[h] * keep[h] + ((x[0] + x[1]) + (x[2] + x[3]));
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                p[h][i] = pair_bf16(x[2 * i], x[2 * i + 1]);
-                rest[h][i] = rest_bf16(x[2 * i], x[2 * i + 1], p[h][i]);
+                multiply(c[0], q[i][0], 0u, q[i][1], 0u, b[0], b[1]);
+                multiply(c[1], q[i][0], 0u, q[i][1], 0u, b[2], b[3]);
             }
         }
-        bool moved = keep[0] != 1.0f;
-        if (H == 2) moved = moved || keep[H - 1] != 1.0f;
-        if (__any_sync(0xFFFFFFFFu, moved)) {
+        float x[4];
 #pragma unroll
-            for (int i = 0; i < DP / 8; ++i) {
-                o[i][0] *= keep[0]; o[i][1] *= keep[0];
-                o[i][2] *= keep[H - 1]; o[i][3] *= keep[H - 1];
-            }
+        for (int i = 0; i < 4; ++i) {
+            const bool in = seen >> ((i >> 1) * 8 + 2 * j + (i & 1)) & 1u;
+            x[i] = in ? (s[i >> 1][i & 1] + s2[i >> 1][i & 1]) * a.scale : -INFINITY;
+        }
+        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const float now = fmaxf(m, top), ref = now == -INFINITY ? 0.0f : now, keep = exp2f(m - ref);
+        m = now;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = exp2f(x[i] - ref);
+        l = l * keep + ((x[0] + x[1]) + (x[2] + x[3]));
+        uint32_t p[2], rest[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            p[i] = pair_bf16(x[2 * i], x[2 * i + 1]);
+            rest[i] = rest_bf16(x[2 * i], x[2 * i + 1], p[i]);
+        }
+        if (__any_sync(0xFFFFFFFFu, keep != 1.0f)) {
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) { o[i][0] *= keep; o[i][1] *= keep; o[i][2] *= keep; o[i][3] *= keep; }
         }
         const int row = lane & 15, half = lane >> 4;
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             uint32_t b[4];
             load_matrices_turned(b, vs + row * R::row + R::place(row, 2 * i + half) * 16);
-            if (H == 1) {
-                multiply(o[2 * i], p[0][0], rest[0][0], p[0][1], rest[0][1], b[0], b[1]);
-                multiply(o[2 * i + 1], p[0][0], rest[0][0], p[0][1], rest[0][1], b[2], b[3]);
-            } else {
-                multiply(o[2 * i], p[0][0], p[H - 1][0], p[0][1], p[H - 1][1], b[0], b[1]);
-                multiply(o[2 * i + 1], p[0][0], p[H - 1][0], p[0][1], p[H - 1][1], b[2], b[3]);
-                multiply(o[2 * i], rest[0][0], rest[H - 1][0], rest[0][1], rest[H - 1][1], b[0], b[1]);
-                multiply(o[2 * i + 1], rest[0][0], rest[H - 1][0], rest[0][1], rest[H - 1][1], b[2], b[3]);
-            }
+            multiply(o[2 * i], p[0], rest[0], p[1], rest[1], b[0], b[1]);
+            multiply(o[2 * i + 1], p[0], rest[0], p[1], rest[1], b[2], b[3]);
         }
     }
 
-    /* Values (rows x DP, pieces of four in changed places), maxima and sums into shared memory. */
-    __device__ __forceinline__ void leave(float *values, float *tops, float *sums)
+    /* Values (rows x DP, pieces of four in changed places), maxima and sums of rows r0 .. r0 + 7 into shared memory. */
+    __device__ __forceinline__ void leave(float *values, int r0, float *tops, float *sums)
     {
-        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+        const int lane = threadIdx.x & 31, j = lane & 3, row = r0 + (lane >> 2);
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
+        l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+        if (j == 0) { tops[row] = top_of(m, l); sums[row] = l; }
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-            l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 1);
-            l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 2);
-            if (j == 0) { tops[g + 8 * h] = top_of(m[h], l[h]); sums[g + 8 * h] = l[h]; }
-#pragma unroll
-            for (int i = 0; i < DP / 8; ++i)
-                *reinterpret_cast<float2 *>(values + value_place<DP>(g + 8 * h, 2 * i + (j >> 1)) + (j & 1) * 2) =
-                    H == 1 ? make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]) : make_float2(o[i][2 * h], o[i][2 * h + 1]);
-        }
+        for (int i = 0; i < DP / 8; ++i)
+            *reinterpret_cast<float2 *>(values + value_place<DP>(row, 2 * i + (j >> 1)) + (j & 1) * 2) = make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]);
     }
 };
 
@@ -428,7 +401,7 @@ template <int DP, int ROWS> struct StateF32 {
             for (int c = 0; c < C; ++c) o[h][c][0] = o[h][c][1] = o[h][c][2] = o[h][c][3] = 0.0f;
         }
     }
-    __device__ __forceinline__ void begin(const char *ring, int stage, float *q_shared)
+    __device__ __forceinline__ void begin(const char *ring, int stage, int, float *q_shared)
     {
         clear();
         q = q_shared;
@@ -508,7 +481,7 @@ template <int DP, int ROWS> struct StateF32 {
         __syncwarp();
     }
 
-    __device__ __forceinline__ void leave(float *values, float *tops, float *sums)
+    __device__ __forceinline__ void leave(float *values, int, float *tops, float *sums)
     {
         const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -527,14 +500,14 @@ template <int DP, int ROWS> struct StateF32 {
     }
 };
 
-template <int DT, int DP, int ROWS> struct StateOf { using type = StateBf16<DP, ROWS>; };
+template <int DT, int DP, int ROWS> struct StateOf { using type = StateBf16<DP>; };
 template <int DP, int ROWS> struct StateOf<SIFAR_F32, DP, ROWS> { using type = StateF32<DP, ROWS>; };
 
-/* Shared memory: the rings (a warp leaves its values in its own), behind them each warp's binary32 queries and probabilities. */
+/* Shared memory: the rings (a team leaves its values in its own), behind them each team's binary32 queries and probabilities. */
 template <int DT, int DP, int ROWS> struct Shared {
-    static constexpr int rings = kWarps * Ring<DT, DP>::bytes;
-    static constexpr int per_warp = DT == SIFAR_F32 ? ROWS * (DP + Ring<DT, DP>::tokens) * 4 : 0;
-    static constexpr int bytes = rings + kWarps * per_warp;
+    static constexpr int rings = kTeams * Ring<DT, DP>::bytes;
+    static constexpr int per_team = DT == SIFAR_F32 ? ROWS * (DP + Ring<DT, DP>::tokens) * 4 : 0;
+    static constexpr int bytes = rings + kTeams * per_team;
     static_assert(ROWS * DP * 4 <= 2 * Ring<DT, DP>::strip, "a state fits a stage");
 };
 
@@ -552,34 +525,47 @@ template <int DT> __device__ __forceinline__ void store_out(typename Elem<DT>::t
         if (d + e < dim) to[d + e] = narrow<DT>(x[e]);
 }
 
+/* Warps of a team, and CTAs that an SM holds by shared memory (227 KB, 1 KB of it per CTA for the system) and by 255 registers of
+   128 threads, 128 of 256. */
+template <int DT, int ROWS> __host__ __device__ constexpr int team_warps() { return DT == SIFAR_BF16 && ROWS > 8 ? 2 : 1; }
+template <int DT, int DP, int ROWS> __host__ __device__ constexpr int ctas_per_sm()
+{
+    return 227 * 1024 / (Shared<DT, DP, ROWS>::bytes + 2048) < 2 ? 1 : 2;
+}
+
 template <int DT, int DP, int ROWS, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ AttentionArgs a)
+__global__ void __launch_bounds__(32 * kTeams * team_warps<DT, ROWS>(), ctas_per_sm<DT, DP, ROWS>()) k_attend(const __grid_constant__ AttentionArgs a)
 {
     using R = Ring<DT, DP>;
     using Sh = Shared<DT, DP, ROWS>;
     using C = Cursor<R::tokens>;
     using T = typename Elem<DT>::type;
     extern __shared__ __align__(128) char smem[];
-    __shared__ unsigned long long s_sum[kWarps];
-    __shared__ C s_start[kWarps];
-    __shared__ float s_top[kWarps][ROWS], s_l[kWarps][ROWS], s_w[kWarps][ROWS];
-    constexpr int es = sizeof(T);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-    const uint32_t number = blockIdx.x * kWarps + warp, items = a.kv_heads * a.chunks;
-    char *const ring = smem + warp * R::bytes;
-    float *const q_shared = reinterpret_cast<float *>(smem + Sh::rings + warp * Sh::per_warp), *const p_shared = q_shared + ROWS * DP;
+    __shared__ unsigned long long s_sum[kTeams * team_warps<DT, ROWS>()];
+    __shared__ C s_start[kTeams];
+    __shared__ float s_top[kTeams][ROWS], s_l[kTeams][ROWS], s_w[kTeams][ROWS];
+    constexpr int es = sizeof(T), TW = team_warps<DT, ROWS>(), own = ROWS / TW;             /* own: rows of a warp */
+    const int lane = threadIdx.x & 31, team = threadIdx.x / 32 / TW, sub = TW == 1 ? 0 : threadIdx.x / 32 % TW;
+    const uint32_t number = blockIdx.x * kTeams + team, items = a.kv_heads * a.chunks;
+    char *const ring = smem + team * R::bytes;
+    float *const q_shared = reinterpret_cast<float *>(smem + Sh::rings + team * Sh::per_team), *const p_shared = q_shared + ROWS * DP;
     const size_t part_floats = partial_floats(a.rows, DP);
     grid_let_next_in();
     grid_wait();
 
-    if (lane == 0) a.splits[number].first = -1;
-    const Shares row = find_shares<R::tokens>(a, s_sum, s_start);
+    /* the warps of a team meet where one warp alone would only meet its lanes */
+    auto meet = [&] {
+        if constexpr (TW == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" :: "r"(1 + team), "n"(32 * TW) : "memory");
+    };
+    if (lane == 0 && sub == 0) a.splits[number].first = -1;
+    const Shares row = find_shares<R::tokens, kTeams * TW>(a, s_sum, s_start);
     const unsigned long long begin = min(row.total, row.share * number), end = min(row.total, begin + row.share);
     const bool any = begin < end;
-    C now = s_start[warp];                                        /* the strip to be used next */
+    C now = s_start[team];                                        /* the strip to be used next */
     if (!any) now.at = end;
     /* whether all of the CTA's places belong to one item, from a strip of it on */
-    const unsigned long long cta_begin = row.share * blockIdx.x * kWarps, cta_end = min(row.total, cta_begin + row.share * kWarps);
+    const unsigned long long cta_begin = row.share * blockIdx.x * kTeams, cta_end = min(row.total, cta_begin + row.share * kTeams);
     const bool together = cta_begin < cta_end && s_start[0].at == cta_begin && cta_begin - s_start[0].strip + s_start[0].strips + kItemCost >= cta_end;
 
     C then = now;                                                 /* the strip to be fetched next */
@@ -599,14 +585,14 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
             const uint32_t kv_head = then.item / a.chunks, chunk = then.item - kv_head * a.chunks;
             if (queries) {
                 const uint32_t head = kv_head * a.group + chunk * a.rows;
-                fetch_queries<DT, DP, ROWS>(a, ring, stage, a.q + then.sequence * a.ld_q + (size_t)head * a.dim * es, min(a.rows, a.group - chunk * a.rows));
+                fetch_queries<DT, DP, own>(a, ring, stage, a.q + then.sequence * a.ld_q + (size_t)head * a.dim * es, min(a.rows, a.group - chunk * a.rows), sub * own);
                 queries = false;
             } else {
                 const long long at = place_offset(a.pages, page, in);
                 queries = then.advance(a, items);
                 look_up();
                 seen = (seen & ~(0xFFFFull << (16 * stage))) | (unsigned long long)(__ballot_sync(0xFFFFFFFFu, at >= 0) & ((1u << R::tokens) - 1u)) << (16 * stage);
-                fetch<DT, DP, VEC>(a, ring, stage, at, kv_head * a.pages.stride_head);
+                fetch<DT, DP, TW, VEC>(a, ring, stage, at, kv_head * a.pages.stride_head, sub);
             }
         }
         copies_commit();
@@ -620,12 +606,12 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
     int stage = 0;
     while (now.at < end) {
         copies_wait<R::stages - 2>();
-        __syncwarp();
+        meet();
         fetch_next(stage == 0 ? R::stages - 1 : stage - 1);
         const int here = stage;
         stage = stage + 1 == R::stages ? 0 : stage + 1;
         if (fresh) {
-            state.begin(ring, here, q_shared);
+            state.begin(ring, here, sub * own, q_shared);
             whole = now.strip == 0;
             fresh = false;
             continue;
@@ -635,25 +621,25 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
         now.advance(a, items);
         if (done.strip + 1 < done.strips && now.at < end) continue;
 
-        /* the item, or this warp's share of it, is done: it goes through the stage that was used last, in whole rows */
+        /* the item, or this team's share of it, is done: it goes through the stage that was used last, in whole rows */
         fresh = true;
-        const int values = warp * R::bytes + (together ? 0 : here * 2 * R::strip);       /* in smem */
+        const int values = team * R::bytes + (together ? 0 : here * 2 * R::strip);       /* in smem */
         if (together) copies_wait<0>();
-        __syncwarp();
-        state.leave(reinterpret_cast<float *>(smem + values), s_top[warp], s_l[warp]);
+        meet();
+        state.leave(reinterpret_cast<float *>(smem + values), sub * own, s_top[team], s_l[team]);
         left = true;
-        __syncwarp();
+        meet();
         const unsigned long long item_begin = done.at - done.strip;
         const bool all = whole && done.strip + 1 == done.strips;
         /* slot 0: the item that the share begins in; slot 1: one that it leaves unfinished */
         const int slot = item_begin <= begin ? 0 : 1;
-        if (whole && !all && lane == 0) {
+        if (whole && !all && lane == 0 && sub == 0) {
             const uint32_t last = (uint32_t)quotient(item_begin + done.strips - 1, (uint32_t)row.share);
             /* CTAs from its first full one to its last that end within it, or behind it before anything else begins */
-            const unsigned long long item_end = min(row.total, item_begin + done.strips + kItemCost), cta = row.share * kWarps;
-            const uint32_t one0 = (uint32_t)((item_begin + cta - 1) / cta) * kWarps;
-            uint32_t one1 = item_end == row.total ? (last / kWarps + 1) * kWarps : (uint32_t)(item_end / cta) * kWarps;
-            one1 = max(one0, min(one1, (last / kWarps + 1) * kWarps));
+            const unsigned long long item_end = min(row.total, item_begin + done.strips + kItemCost), cta = row.share * kTeams;
+            const uint32_t one0 = (uint32_t)((item_begin + cta - 1) / cta) * kTeams;
+            uint32_t one1 = item_end == row.total ? (last / kTeams + 1) * kTeams : (uint32_t)(item_end / cta) * kTeams;
+            one1 = max(one0, min(one1, (last / kTeams + 1) * kTeams));
             a.splits[number] = Split{(int)done.sequence, (int)done.item, (int)number, (int)last, slot, (int)one0, (int)one1, 0};
         }
         if (together && !all) break;
@@ -661,29 +647,31 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
         const uint32_t head = kv_head * a.group + chunk * a.rows;
         T *const out = reinterpret_cast<T *>(a.out + done.sequence * a.ld_out) + (size_t)head * a.dim;
         float *const part = a.partial + ((size_t)number * 2 + slot) * part_floats;
-        if (lane < (int)rows) {
-            const float top = s_top[warp][lane], sum = s_l[warp][lane];
-            s_w[warp][lane] = sum == 0.0f ? 0.0f : 1.0f / sum;
-            if (!all) { part[a.rows * DP + lane] = top; part[a.rows * DP + a.rows + lane] = sum; }
-            else if (a.lse) a.lse[done.sequence * (size_t)a.heads + head + lane] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+        const uint32_t mine = min(rows, (uint32_t)(sub + 1) * own);   /* behind the warp's last row */
+        if (lane < own && sub * own + lane < (int)rows) {
+            const int r = sub * own + lane;
+            const float top = s_top[team][r], sum = s_l[team][r];
+            s_w[team][r] = sum == 0.0f ? 0.0f : 1.0f / sum;
+            if (!all) { part[a.rows * DP + r] = top; part[a.rows * DP + a.rows + r] = sum; }
+            else if (a.lse) a.lse[done.sequence * (size_t)a.heads + head + r] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
         }
-        __syncwarp();
+        meet();
         /* several loads before the first store: a warp has nobody to hide them behind */
         constexpr uint32_t kPieces = DP / 4, kAtOnce = kPieces < 32 ? 32 / kPieces : 1, kTurns = kPieces > 32 ? kPieces / 32 : 1, kRows = 4 / kTurns;
-        for (uint32_t r0 = lane / kPieces; r0 < rows; r0 += kAtOnce * kRows) {
+        for (uint32_t r0 = sub * own + lane / kPieces; r0 < mine; r0 += kAtOnce * kRows) {
             float4 v[kRows][kTurns];
             float f[kRows];
 #pragma unroll
             for (uint32_t k = 0; k < kRows; ++k) {
-                const uint32_t r = min(r0 + k * kAtOnce, rows - 1);
-                f[k] = s_w[warp][r];
+                const uint32_t r = min(r0 + k * kAtOnce, mine - 1);
+                f[k] = s_w[team][r];
 #pragma unroll
                 for (uint32_t c = 0; c < kTurns; ++c) v[k][c] = *reinterpret_cast<const float4 *>(smem + values + value_place<DP>(r, lane % kPieces + 32 * c) * 4);
             }
 #pragma unroll
             for (uint32_t k = 0; k < kRows; ++k) {
                 const uint32_t r = r0 + k * kAtOnce;
-                if (r >= rows) break;
+                if (r >= mine) break;
 #pragma unroll
                 for (uint32_t c = 0; c < kTurns; ++c) {
                     const uint32_t d = (lane % kPieces + 32 * c) * 4;
@@ -696,24 +684,24 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
                 }
             }
         }
-        __syncwarp();
+        meet();
     }
     copies_wait<0>();
     if (!together) return;
 
     /* all of the CTA's warps have strips of one item, or none: one part of them, in the first one's place */
-    if (!left && lane < ROWS) { s_top[warp][lane] = -INFINITY; s_l[warp][lane] = 0.0f; }
+    if (!left && lane < own) { s_top[team][sub * own + lane] = -INFINITY; s_l[team][sub * own + lane] = 0.0f; }
     __syncthreads();
     const uint32_t chunk = s_start[0].item % a.chunks, rows = min(a.rows, a.group - chunk * a.rows);
-    float *const part = a.partial + (size_t)blockIdx.x * kWarps * 2 * part_floats;
+    float *const part = a.partial + (size_t)blockIdx.x * kTeams * 2 * part_floats;
     if (threadIdx.x < rows) {
         const int r = threadIdx.x;
         float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_top[w][r]);
+        for (int w = 0; w < kTeams; ++w) top = fmaxf(top, s_top[w][r]);
         const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kTeams; ++w) {
             const float f = exp2f(s_top[w][r] - ref);
             s_w[w][r] = f;
             sum += f * s_l[w][r];
@@ -722,11 +710,11 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
         part[a.rows * DP + a.rows + r] = sum;
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < rows * (DP / 4); i += kThreads) {
+    for (uint32_t i = threadIdx.x; i < rows * (DP / 4); i += 32 * kTeams * TW) {
         const uint32_t r = i / (DP / 4), piece = i % (DP / 4);
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kTeams; ++w) {
             const float f = s_w[w][r];
             const float4 o = *reinterpret_cast<const float4 *>(smem + w * R::bytes + value_place<DP>(r, piece) * 4);
             if (f != 0.0f) { x.x += f * o.x; x.y += f * o.y; x.z += f * o.z; x.w += f * o.w; }      /* 0: it may have left nothing */
@@ -736,7 +724,7 @@ __global__ void __launch_bounds__(kThreads) k_attend(const __grid_constant__ Att
 }
 
 /*
- * The items that begin in a CTA's warps and end in others, a query head per CTA.  Items of up to kAlone parts have a warp each; at
+ * The items that begin in a CTA's teams and end in others, a query head per CTA.  Items of up to kAlone parts have a warp each; at
  * most one of a CTA's has more (it goes on into other CTAs), and all warps share its parts.  Lanes have four columns each.
  */
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps, kAlone = 8;
@@ -782,19 +770,19 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     const size_t part_floats = partial_floats(a.rows, DP);
     /* this warp's split, and the one that all share */
-    const Split mine = warp < kWarps ? a.splits[blockIdx.x * kWarps + warp] : Split{0, 0, -1, 0, 0, 0, 0, 0};
-    const Split last = a.splits[blockIdx.x * kWarps + kWarps - 1];
+    const Split mine = warp < kTeams ? a.splits[blockIdx.x * kTeams + warp] : Split{0, 0, -1, 0, 0, 0, 0, 0};
+    const Split last = a.splits[blockIdx.x * kTeams + kTeams - 1];
     Split big = last;
 #pragma unroll
-    for (int k = 0; k < kWarps - 1; ++k) {
-        const Split s = a.splits[blockIdx.x * kWarps + k];
+    for (int k = 0; k < kTeams - 1; ++k) {
+        const Split s = a.splits[blockIdx.x * kTeams + k];
         if (s.first >= 0 && s.last - s.first + 1 > kAlone) big = s;
     }
     /* parts in their order: warps up to one0, a part per CTA up to one1, warps again */
-    auto parts_of = [](const Split &s) { return min(s.one0, s.last + 1) - s.first + (s.one1 - s.one0) / kWarps + max(0, s.last + 1 - s.one1); };
+    auto parts_of = [](const Split &s) { return min(s.one0, s.last + 1) - s.first + (s.one1 - s.one0) / kTeams + max(0, s.last + 1 - s.one1); };
     auto part_at = [&](const Split &s, int i) {
-        const int before = min(s.one0, s.last + 1) - s.first, ones = (s.one1 - s.one0) / kWarps;
-        const int w = i < before ? s.first + i : i < before + ones ? s.one0 + (i - before) * kWarps : s.one1 + (i - before - ones);
+        const int before = min(s.one0, s.last + 1) - s.first, ones = (s.one1 - s.one0) / kTeams;
+        const int w = i < before ? s.first + i : i < before + ones ? s.one0 + (i - before) * kTeams : s.one1 + (i - before - ones);
         return a.partial + ((size_t)w * 2 + (w == s.first ? s.slot : 0)) * part_floats;
     };
     auto there = [&](const Split &s) { return s.first >= 0 && r < min(a.rows, a.group - s.item % a.chunks * a.rows); };
@@ -860,9 +848,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
 /* ------------------------------------------------------------------------ */
 struct AttentionPlan { uint32_t rows, chunks, ctas; int dp; size_t split_bytes, bytes; };
 
-/* CTAs that an SM holds by shared memory (227 KB, 1 KB of it per CTA for the system). */
-constexpr int ctas_per_sm(int shared) { return 227 * 1024 / (shared + 1024) < 8 ? 227 * 1024 / (shared + 1024) : 8; }
-
 template <int DT, int DP, int ROWS, bool VEC>
 static cudaError_t launch_attend(const AttentionPlan &plan, cudaStream_t stream, const AttentionArgs &a)
 {
@@ -870,7 +855,7 @@ static cudaError_t launch_attend(const AttentionPlan &plan, cudaStream_t stream,
     static_assert(shared <= 227 * 1024 - 1024, "rings");
     /* per device: an attribute of the kernel there */
     if (cudaError_t e = cudaFuncSetAttribute(k_attend<DT, DP, ROWS, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared)) return e;
-    if (cudaError_t e = launch_op(k_attend<DT, DP, ROWS, VEC>, dim3(plan.ctas), dim3(kThreads), 1, shared, stream, a)) return e;
+    if (cudaError_t e = launch_op(k_attend<DT, DP, ROWS, VEC>, dim3(plan.ctas), dim3(32 * kTeams * team_warps<DT, ROWS>()), 1, shared, stream, a)) return e;
     return launch_op(k_attend_join<DT, DP>, dim3(plan.ctas, plan.rows), dim3(kJoinThreads), 1, 0, stream, a);
 }
 
@@ -894,12 +879,12 @@ static cudaError_t launch_attend_t(bool vec, const AttentionPlan &plan, cudaStre
     return launch_attend_d<DT, 256>(vec, plan, stream, a);
 }
 
-template <int DT> static int shared_of(int dp, bool many)
+template <int DT> static int ctas_of(int dp, bool many)
 {
     if constexpr (DT == SIFAR_BF16) {
-        if (many) return dp == 64 ? Shared<DT, 64, 16>::bytes : dp == 128 ? Shared<DT, 128, 16>::bytes : Shared<DT, 256, 16>::bytes;
+        if (many) return dp == 64 ? ctas_per_sm<DT, 64, 16>() : dp == 128 ? ctas_per_sm<DT, 128, 16>() : ctas_per_sm<DT, 256, 16>();
     }
-    return dp == 64 ? Shared<DT, 64, 8>::bytes : dp == 128 ? Shared<DT, 128, 8>::bytes : Shared<DT, 256, 8>::bytes;
+    return dp == 64 ? ctas_per_sm<DT, 64, 8>() : dp == 128 ? ctas_per_sm<DT, 128, 8>() : ctas_per_sm<DT, 256, 8>();
 }
 
 static int plan_attention(const char *fn, const sifar_decode_attention_args *g, CacheShape &c, AttentionPlan &p)
@@ -916,9 +901,9 @@ static int plan_attention(const char *fn, const sifar_decode_attention_args *g, 
     p.chunks = (group + most - 1) / most;
     p.rows = (group + p.chunks - 1) / p.chunks;
     p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
-    p.ctas = kSms * (unsigned)ctas_per_sm(bf16 ? shared_of<SIFAR_BF16>(p.dp, p.rows > 8) : shared_of<SIFAR_F32>(p.dp, false));
-    p.split_bytes = (size_t)p.ctas * kWarps * sizeof(Split);
-    p.bytes = p.split_bytes + (size_t)p.ctas * kWarps * 2 * partial_floats(p.rows, p.dp) * sizeof(float);
+    p.ctas = kSms * (unsigned)(bf16 ? ctas_of<SIFAR_BF16>(p.dp, p.rows > 8) : ctas_of<SIFAR_F32>(p.dp, false));
+    p.split_bytes = (size_t)p.ctas * kTeams * sizeof(Split);
+    p.bytes = p.split_bytes + (size_t)p.ctas * kTeams * 2 * partial_floats(p.rows, p.dp) * sizeof(float);
     p.bytes = (p.bytes + 15) / 16 * 16;
     return SIFAR_OK;
 }
