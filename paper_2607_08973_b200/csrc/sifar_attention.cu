@@ -724,8 +724,9 @@ __global__ void __launch_bounds__(32 * kTeams * team_warps<DT, ROWS>(), ctas_per
 }
 
 /*
- * The items that begin in a CTA's teams and end in others, a query head per CTA.  Items of up to kAlone parts have a warp each; at
- * most one of a CTA's has more (it goes on into other CTAs), and all warps share its parts.  Lanes have four columns each.
+ * The items that begin in a CTA's teams and end in others, a query head per CTA, or two with half of the warps each where there
+ * would be more CTAs than the GPU holds.  Items of up to kAlone parts have a warp each; at most one of a CTA's has more (it goes on
+ * into other CTAs), and all warps of the head share its parts.  Lanes have four columns each.
  */
 constexpr int kJoinWarps = 8, kJoinThreads = 32 * kJoinWarps, kAlone = 8;
 
@@ -758,7 +759,7 @@ template <int DP> struct Joined {
 };
 
 template <int DT, int DP>
-__global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_constant__ AttentionArgs a)
+__global__ void __launch_bounds__(kJoinThreads, 4) k_attend_join(const __grid_constant__ AttentionArgs a)
 {
     using J = Joined<DP>;
     using T = typename Elem<DT>::type;
@@ -766,11 +767,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
     __shared__ __align__(16) float s_o[kJoinWarps][DP];
     grid_let_next_in();
     grid_wait();
-    const uint32_t r = blockIdx.y;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, warps = gridDim.y == a.rows ? kJoinWarps : kJoinWarps / 2, first = warp - warp % warps, nth = warp - first;
+    const uint32_t r = blockIdx.y * (kJoinWarps / warps) + first / warps;
     const size_t part_floats = partial_floats(a.rows, DP);
     /* this warp's split, and the one that all share */
-    const Split mine = warp < kTeams ? a.splits[blockIdx.x * kTeams + warp] : Split{0, 0, -1, 0, 0, 0, 0, 0};
+    const Split mine = nth < kTeams ? a.splits[blockIdx.x * kTeams + nth] : Split{0, 0, -1, 0, 0, 0, 0, 0};
     const Split last = a.splits[blockIdx.x * kTeams + kTeams - 1];
     Split big = last;
 #pragma unroll
@@ -787,11 +788,12 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
     };
     auto there = [&](const Split &s) { return s.first >= 0 && r < min(a.rows, a.group - s.item % a.chunks * a.rows); };
     auto walk = [&](const Split &s, int i0, int i1, J &j) {
-        for (; i0 < i1; i0 += 4) {
-            float t[4], l[4];
-            float4 v[4][J::C];
+        constexpr int N = 4 / J::C;                               /* parts under way together */
+        for (; i0 < i1; i0 += N) {
+            float t[N], l[N];
+            float4 v[N][J::C];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < N; ++k) {
                 const float *const p = part_at(s, min(i0 + k, i1 - 1));
                 t[k] = i0 + k < i1 ? __ldcg(p + a.rows * DP + r) : -INFINITY;
                 l[k] = __ldcg(p + a.rows * DP + a.rows + r);
@@ -819,27 +821,30 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
         walk(mine, 0, parts_of(mine), j);
         finish(mine, j);
     }
-    if (!there(big) || parts_of(big) <= kAlone) return;           /* the same for the whole CTA */
-    const int n = parts_of(big);
+    if (big.first < 0 || parts_of(big) <= kAlone) return;         /* the same for the whole CTA */
+    const int n = there(big) ? parts_of(big) : 0;
     J j;
-    walk(big, n * warp / kJoinWarps, n * (warp + 1) / kJoinWarps, j);
+    walk(big, n * nth / warps, n * (nth + 1) / warps, j);
 #pragma unroll
     for (int c = 0; c < J::C; ++c)
         if (DP >= 128 || lane < DP / 4) *reinterpret_cast<float4 *>(&s_o[warp][(lane + 32 * c) * 4]) = make_float4(j.o[c][0], j.o[c][1], j.o[c][2], j.o[c][3]);
     if (lane == 0) { s_top[warp] = top_of(j.top, j.sum); s_sum[warp] = j.sum; }
     __syncthreads();
-    if (warp) return;
+    if (nth || !n) return;
     J total;
-    float tops[kJoinWarps], l[kJoinWarps];
-    float4 v[kJoinWarps][J::C];
+    constexpr int N = 4 / J::C;
+    for (int w0 = first; w0 < first + warps; w0 += N) {
+        float tops[N], l[N];
+        float4 v[N][J::C];
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) {
-        tops[w] = s_top[w]; l[w] = s_sum[w];
+        for (int w = 0; w < N; ++w) {
+            tops[w] = s_top[w0 + w]; l[w] = s_sum[w0 + w];
 #pragma unroll
-        for (int c = 0; c < J::C; ++c)
-            if (DP >= 128 || lane < DP / 4) v[w][c] = *reinterpret_cast<const float4 *>(&s_o[w][(lane + 32 * c) * 4]);
+            for (int c = 0; c < J::C; ++c)
+                if (DP >= 128 || lane < DP / 4) v[w][c] = *reinterpret_cast<const float4 *>(&s_o[w0 + w][(lane + 32 * c) * 4]);
+        }
+        total.add(tops, l, v);
     }
-    total.add(tops, l, v);
     finish(big, total);
 }
 
@@ -856,7 +861,7 @@ static cudaError_t launch_attend(const AttentionPlan &plan, cudaStream_t stream,
     /* per device: an attribute of the kernel there */
     if (cudaError_t e = cudaFuncSetAttribute(k_attend<DT, DP, ROWS, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared)) return e;
     if (cudaError_t e = launch_op(k_attend<DT, DP, ROWS, VEC>, dim3(plan.ctas), dim3(32 * kTeams * team_warps<DT, ROWS>()), 1, shared, stream, a)) return e;
-    return launch_op(k_attend_join<DT, DP>, dim3(plan.ctas, plan.rows), dim3(kJoinThreads), 1, 0, stream, a);
+    return launch_op(k_attend_join<DT, DP>, dim3(plan.ctas, plan.ctas * plan.rows <= 4 * kSms ? plan.rows : (plan.rows + 1) / 2), dim3(kJoinThreads), 1, 0, stream, a);
 }
 
 template <int DT, int DP>
