@@ -36,40 +36,6 @@ __device__ __forceinline__ uint4 load_once(const char *p)
     return v;
 }
 
-/* Bytes sh .. sh + 15 of two vectors in a row, those from `left` on 0. */
-__device__ __forceinline__ uint4 shifted(const uint4 &lo, const uint4 &hi, uint32_t sh, int left)
-{
-    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    /* words first, then the bits within them */
-    if (sh & 8u) {
-#pragma unroll
-        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-    }
-    if (sh & 4u) {
-#pragma unroll
-        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-    }
-    const uint32_t bits = (sh & 3u) * 8u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-    if (left < 16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = left >= 4 * i + 4 ? w[i] : left <= 4 * i ? 0u : w[i] & ((1u << (left - 4 * i) * 8) - 1u);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-/* 16 bytes from any element on, zeros from `left` on. */
-__device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
-{
-    const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;
-    const uint4 *const q = reinterpret_cast<const uint4 *>(p - sh);
-    const uint4 lo = __ldg(q);
-    uint4 hi = make_uint4(0u, 0u, 0u, 0u);
-    if (sh && left > 16u - sh) hi = __ldg(q + 1);
-    return shifted(lo, hi, sh, (int)left);
-}
-
 /*
  * What a lane has on the way of its two rows: 16 bytes of each of kAhead blocks, a block being the 64 bytes of the row's four lanes.
  * Rows that start anywhere (not VEC) are loaded as the aligned vectors that hold them, and put together when they are used: the
@@ -317,12 +283,24 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     }
 }
 
-/* What an item's binary32 values take: 256 bytes of each token's row. */
-template <int G> struct Staged { static constexpr int bytes = 8 * G * kAhead * kBlock; };
+/* What an item's values take: 256 bytes of each row; bf16 rows, eight of which are read at once, shifted by half of the banks.
+   0: too much for two items of each warp, the values are read where they are used. */
+template <int DT, int G> struct Staged {
+    static constexpr int row = kAhead * kBlock + (DT == SIFAR_BF16 ? 64 : 0), bytes = DT == SIFAR_F32 ? 8 * G * row : G == 1 ? 2 * 8 * row : 0;
+};
+constexpr int kMaxSplit = 8;                 /* CTAs that share columns of the output */
+
+/* Into the same place of CTA `rank`'s shared memory. */
+__device__ __forceinline__ void store_cluster(float *local, uint32_t rank, float v)
+{
+    asm volatile("{\n\t.reg .u32 q;\n\tmapa.shared::cluster.u32 q, %0, %1;\n\tst.shared::cluster.f32 [q], %2;\n\t}"
+                 :: "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank), "f"(v) : "memory");
+}
 
 /*
  * A CTA has an equal share of the output's columns, 16 at a time, and goes over all experts that have tokens; its warps take
- * the 256-byte pieces of the experts' rows in turn.  Tokens that did not choose an expert have zeros there and are not read.
+ * the 256-byte pieces of the experts' rows in turn.  Where there are few columns, the CTAs of a cluster share them and take turns, and
+ * the first one adds their sums up.  Tokens that did not choose an expert have zeros there and are not read.
  * HALF (bf16, up to 4 tokens): both parts of the products' values are columns of one instruction.
  */
 template <int DT, int G, bool VEC, bool HALF>
@@ -332,13 +310,15 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
     __shared__ uint32_t s_bits[SIFAR_ROUTE_MAX_EXPERTS], s_tokens[SIFAR_ROUTE_MAX_EXPERTS];
     __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];
     __shared__ int s_scratch[kWarps];
-    __shared__ __align__(16) float s_red[kWarps][16 * 8 * G];
-    extern __shared__ __align__(128) char smem[];                   /* binary32: each warp's two items' values */
+    __shared__ __align__(16) float s_red[kWarps][16 * 8 * G], s_part[kMaxSplit][16 * 8 * G];
+    extern __shared__ __align__(128) char smem[];                   /* not HALF: each warp's two items' values */
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     /* the choices were complete before the kernel in front of this one let it in, so they may be read before it ends */
     const int active = list_few(a, s_list, s_tokens, s_bits, s_scratch);
     const uint32_t bytes = a.inter * es, pieces = (bytes + kAhead * kBlock - 1) / (kAhead * kBlock), items = (uint32_t)active * pieces;
-    const uint32_t begin = (uint32_t)((unsigned long long)a.hidden * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)a.hidden * (blockIdx.x + 1) / gridDim.x);
+    const uint32_t split = a.split, rank = split > 1 ? cluster_rank() : 0u, block = blockIdx.x / split, blocks = gridDim.x / split;
+    const uint32_t begin = (uint32_t)((unsigned long long)a.hidden * block / blocks), end = (uint32_t)((unsigned long long)a.hidden * (block + 1) / blocks);
+    const uint32_t warp0 = rank * kWarps + warp, turn = split * kWarps;                  /* the warp's first item, and how many lie between two */
     auto load = [&](Weights<VEC> &w, uint32_t col, uint32_t item) {
         const char *ra = nullptr, *rb = nullptr;
         if (item < items) {
@@ -349,10 +329,10 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
         w.load(ra, rb, item % pieces * (kAhead * kBlock) + j * 16, bytes);
     };
     Weights<VEC> next;
-    load(next, begin, warp);
+    load(next, begin, warp0);
     /* the next items' weights, too, as far as the L2: a lane has half a row's piece of each */
     for (uint32_t k = 1; k <= kFetchAhead; ++k) {
-        const uint32_t item = warp + k * kWarps, c = begin + lane / 2, at = item % pieces * (kAhead * kBlock) + (lane & 1) * 128;
+        const uint32_t item = warp0 + k * turn, c = begin + lane / 2, at = item % pieces * (kAhead * kBlock) + (lane & 1) * 128;
         if (item >= items) break;
         if (c < end && at < bytes)
             asm volatile("prefetch.global.L2 [%0];" :: "l"(a.down + ((unsigned long long)s_list[item / pieces] * a.hidden + c) * a.ld_down + at));
@@ -360,19 +340,26 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
     grid_wait();
     grid_let_next_in();
     const size_t low = (size_t)a.tokens * a.h_row;
-    /* binary32: the values that go with an item, two tokens' rows at a time, zeros behind their ends */
-    char *const staged = smem + warp * (2 * Staged<G>::bytes);
+    /* the values that go with an item, two rows at a time (bf16: a token's parts, the second ones 8 G rows on), zeros behind their ends */
+    constexpr bool kStaged = !HALF && Staged<DT, G>::bytes > 0;
+    char *const staged = smem + warp * (2 * Staged<DT, G>::bytes);
     auto fetch = [&](uint32_t item, int half) {
         if (item < items) {
             const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + (lane & 15) * 16, size = at < a.h_row ? 16u : 0u;
-            const char *const h = a.h + (size_t)which * low + (size ? at : 0u);
+            const char *const h = a.h + (size_t)which * (DT == SIFAR_BF16 ? 2 : 1) * low + (size ? at : 0u);
+            char *const to = staged + half * Staged<DT, G>::bytes + (lane & 15) * 16;
             uint32_t rest = s_tokens[which];
             while (rest) {
                 uint32_t t = __ffs(rest) - 1;
                 rest &= rest - 1u;
-                if (lane >= 16 && rest) t = __ffs(rest) - 1;
-                rest &= rest - 1u;
-                copy16(staged + half * Staged<G>::bytes + t * (kAhead * kBlock) + (lane & 15) * 16, h + t * (size_t)a.h_row, size);
+                if constexpr (DT == SIFAR_BF16) {
+                    const uint32_t part = lane / 16;
+                    copy16(to + (part * 8 * G + t) * Staged<DT, G>::row, h + part * low + t * (size_t)a.h_row, size);
+                } else {
+                    if (lane >= 16 && rest) t = __ffs(rest) - 1;
+                    rest &= rest - 1u;
+                    copy16(to + t * Staged<DT, G>::row, h + t * (size_t)a.h_row, size);
+                }
             }
         }
         copies_commit();
@@ -380,39 +367,28 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
     for (uint32_t col = begin; col < end; col += 16) {
         Few<DT, G> acc;
         int half = 0;
-        if (DT == SIFAR_F32) fetch(warp, 0);
-        for (uint32_t item = warp; item < items; item += kWarps, half ^= 1) {
+        if (kStaged) fetch(warp0, 0);
+        for (uint32_t item = warp0; item < items; item += turn, half ^= 1) {
             const Weights<VEC> now = next;
             const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + j * 16, tokens = s_tokens[which];
-            if constexpr (DT == SIFAR_BF16) {
-                uint4 x[kAhead][G], y[HALF ? 1 : kAhead][G];
+            const bool more = item + turn < items;
+            if constexpr (HALF) {
+                uint4 x[kAhead];
+                const uint32_t t = g & 3;
+                const char *const from = a.h + (size_t)which * 2 * low + t * (size_t)a.h_row + (g >= 4 ? low : 0) + at;
 #pragma unroll
-                for (int q = 0; q < G; ++q) {
-                    const uint32_t t = HALF ? g & 3 : q * 8 + g;
-                    const char *const from = a.h + (size_t)which * 2 * low + t * (size_t)a.h_row + (HALF && g >= 4 ? low : 0) + at;
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const bool in = (tokens >> t & 1u) && at + i * kBlock < a.h_row;        /* rows of h are filled up with zeros to 16 bytes */
-                        x[i][q] = in ? __ldcg(reinterpret_cast<const uint4 *>(from + i * kBlock)) : make_uint4(0u, 0u, 0u, 0u);
-                        if (!HALF) y[i][q] = in ? __ldcg(reinterpret_cast<const uint4 *>(from + low + i * kBlock)) : make_uint4(0u, 0u, 0u, 0u);
-                    }
-                }
-                load(next, item + kWarps < items ? col : col + 16, item + kWarps < items ? item + kWarps : warp);
+                for (int i = 0; i < kAhead; ++i)                    /* rows of h are filled up with zeros to 16 bytes */
+                    x[i] = (tokens >> t & 1u) && at + i * kBlock < a.h_row ? __ldcg(reinterpret_cast<const uint4 *>(from + i * kBlock)) : make_uint4(0u, 0u, 0u, 0u);
+                load(next, more ? col : col + 16, more ? item + turn : warp0);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     if (at - j * 16 + i * kBlock >= bytes) break;
                     const int left = (int)bytes - (int)(at + i * kBlock);
-                    const uint4 wa = now.of_a(i, left), wb = now.of_b(i, left);
-#pragma unroll
-                    for (int q = 0; q < G; ++q) {
-                        if (!(HALF ? tokens : tokens >> (8 * q) & 0xFFu)) continue;
-                        multiply_block(acc.c[q], wa, wb, x[i][q]);
-                        if (!HALF) multiply_block(acc.c[q], wa, wb, y[i][q]);
-                    }
+                    multiply_block(acc.c[0], now.of_a(i, left), now.of_b(i, left), x[i]);
                 }
             } else {
-                load(next, item + kWarps < items ? col : col + 16, item + kWarps < items ? item + kWarps : warp);
-                fetch(item + kWarps, half ^ 1);
+                load(next, more ? col : col + 16, more ? item + turn : warp0);
+                if (kStaged) fetch(item + turn, half ^ 1);
                 uint4 wa[kAhead], wb[kAhead];
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
@@ -420,28 +396,55 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                     wa[i] = now.of_a(i, left);
                     wb[i] = now.of_b(i, left);
                 }
-                copies_wait<1>();
+                if (kStaged) copies_wait<1>();
                 __syncwarp();
-                const char *const x0 = staged + half * Staged<G>::bytes + j * 16;
+                const char *const x0 = staged + half * Staged<DT, G>::bytes + j * 16;
+                if constexpr (DT == SIFAR_BF16) {
 #pragma unroll
-                for (int t = 0; t < 8 * G; ++t) {
-                    if (!(tokens >> t & 1u)) continue;              /* the same for the whole warp */
+                    for (int q = 0; q < G; ++q) {
+                        if (!(tokens >> (8 * q) & 0xFFu)) continue;
+                        const uint32_t t = q * 8 + g;
+                        const char *const from = a.h + (size_t)which * 2 * low + t * (size_t)a.h_row + at;
+                        uint4 x[kAhead], y[kAhead];
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const float4 x = *reinterpret_cast<const float4 *>(x0 + t * (kAhead * kBlock) + i * kBlock);
-                        acc.c[0][t] = dot4(wa[i], x, acc.c[0][t]);
-                        acc.c[1][t] = dot4(wb[i], x, acc.c[1][t]);
+                        for (int i = 0; i < kAhead; ++i) {
+                            x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
+                            if (!(tokens >> t & 1u)) continue;
+                            if (kStaged) {
+                                x[i] = *reinterpret_cast<const uint4 *>(x0 + t * Staged<DT, G>::row + i * kBlock);
+                                y[i] = *reinterpret_cast<const uint4 *>(x0 + (t + 8 * G) * Staged<DT, G>::row + i * kBlock);
+                            } else if (at + i * kBlock < a.h_row) {
+                                x[i] = __ldcg(reinterpret_cast<const uint4 *>(from + i * kBlock));
+                                y[i] = __ldcg(reinterpret_cast<const uint4 *>(from + low + i * kBlock));
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i) {
+                            multiply_block(acc.c[q], wa[i], wb[i], x[i]);
+                            multiply_block(acc.c[q], wa[i], wb[i], y[i]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 8 * G; ++t) {
+                        if (!(tokens >> t & 1u)) continue;          /* the same for the whole warp */
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i) {
+                            const float4 x = *reinterpret_cast<const float4 *>(x0 + t * Staged<DT, G>::row + i * kBlock);
+                            acc.c[0][t] = dot4(wa[i], x, acc.c[0][t]);
+                            acc.c[1][t] = dot4(wb[i], x, acc.c[1][t]);
+                        }
                     }
                 }
                 __syncwarp();
             }
         }
-        if (DT == SIFAR_F32) copies_wait<0>();
+        if (kStaged) copies_wait<0>();
         acc.store(s_red[warp]);
         __syncthreads();
+        auto out = [&](uint32_t t, uint32_t r, float v) { reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out)[col + r] = narrow<DT>(v); };
         for (uint32_t i = threadIdx.x; i < 16 * a.tokens; i += kThreads) {
             const uint32_t r = i % 16, t = i / 16;
-            if (col + r >= end) continue;
             float v = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) v += s_red[w][r * 8 * G + t];
@@ -451,7 +454,22 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                 for (int w = 0; w < kWarps; ++w) rest += s_red[w][r * 8 * G + t + 4];
                 v += rest;
             }
-            reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out)[col + r] = narrow<DT>(v);
+            if (split > 1) store_cluster(&s_part[rank][i], 0, v);
+            else if (col + r < end) out(t, r, v);
+        }
+        if (split > 1) {
+            cluster_arrive();
+            cluster_wait();
+            if (rank == 0)
+                for (uint32_t i = threadIdx.x; i < 16 * a.tokens; i += kThreads) {
+                    float v = 0.0f;
+                    for (uint32_t k = 0; k < split; ++k) v += s_part[k][i];
+                    if (col + i % 16 < end) out(i / 16, i % 16, v);
+                }
+            if (col + 16 < end) {                                   /* before the next columns' sums come */
+                cluster_arrive();
+                cluster_wait();
+            }
         }
         __syncthreads();
     }
@@ -461,10 +479,10 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
 /* more tokens                                                               */
 /* ------------------------------------------------------------------------ */
 /* Columns of a pass over an expert's rows, and instructions' columns of eight that hold them: bf16 values of the second product
-   come as two parts, a column each. */
+   come as two parts, a column each.  binary32: as many as registers hold. */
 template <int DT, bool DOWN> struct Pass {
     static constexpr int parts = DT == SIFAR_BF16 && DOWN ? 2 : 1;
-    static constexpr int groups = DT == SIFAR_BF16 ? 8 : 4;
+    static constexpr int groups = DT == SIFAR_BF16 ? 8 : 2;
     static constexpr int tokens = groups * 8 / parts;
     static constexpr int shared = 2 * groups * 8 * kChunkRow;
 };
@@ -479,41 +497,35 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
 {
     using P = Pass<DT, DOWN>;
     constexpr int es = DT == SIFAR_BF16 ? 2 : 4, G = P::groups / P::parts;
-    extern __shared__ __align__(128) char smem[];                   /* 2 x columns x kChunkRow */
-    __shared__ int s_counts[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_before[SIFAR_ROUTE_MAX_EXPERTS + 1];
-    __shared__ int s_scratch[kWarps];
-    __shared__ uint16_t s_slots[SIFAR_EXPERTS_MAX_TOKENS];          /* choices of the expert's tokens: below 2^13 */
+    extern __shared__ __align__(128) char smem[];                   /* 2 x columns x kChunkRow; at first each expert's tokens as bits */
+    __shared__ uint16_t s_place[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];
+    __shared__ uint8_t s_token[SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K];
+    __shared__ unsigned long long s_sum[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     if (!DOWN) grid_wait();
     grid_let_next_in();
-    const int active = list_experts(a, s_counts, s_list, s_scratch);
-    const uint32_t rows = DOWN ? a.hidden : a.inter, per = DOWN ? 128u : 64u, tiles = (rows + per - 1) / per;
-    const uint32_t bytes = (DOWN ? a.inter : a.hidden) * es, steps = (bytes + kChunk - 1) / kChunk;
-    /* passes before each of them */
-    if (threadIdx.x == 0) {
-        int sum = 0;
-        for (int i = 0; i < active; ++i) { s_before[i] = sum; sum += (s_counts[s_list[i]] + P::tokens - 1) / P::tokens; }
-        s_before[active] = sum;
-    }
+    const ExpertPlan plan = plan_experts<kThreads>(a, P::tokens, reinterpret_cast<uint32_t *>(smem), s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
     __syncthreads();
-    const unsigned long long units = (unsigned long long)s_before[active] * tiles;
-    const unsigned long long begin = units * blockIdx.x / gridDim.x, end = units * (blockIdx.x + 1) / gridDim.x;
+    const uint32_t rows = DOWN ? a.hidden : a.inter, per = DOWN ? 128u : 64u, tiles = (rows + per - 1) / per, units = plan.passes * tiles;
+    const uint32_t bytes = (DOWN ? a.inter : a.hidden) * es, steps = (bytes + kChunk - 1) / kChunk;
+    const uint32_t begin = (uint32_t)((unsigned long long)units * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)units * (blockIdx.x + 1) / gridDim.x);
 
-    struct Unit { uint32_t which, tile, pass; };
-    auto unit = [&](unsigned long long u) {
-        int lo = 0, hi = active - 1;                                /* the last expert with s_before * tiles <= u */
+    struct Unit { uint32_t expert, tile, first, n; };               /* tokens first .. first + n - 1 of the list */
+    auto unit = [&](uint32_t u) {
+        const uint32_t pass = u / tiles;
+        int lo = 0, hi = plan.active - 1;                           /* the last expert with no more passes before it */
         while (lo < hi) {
             const int mid = (lo + hi + 1) / 2;
-            if ((unsigned long long)s_before[mid] * tiles <= u) lo = mid; else hi = mid - 1;
+            if (s_passes[mid] <= pass) lo = mid; else hi = mid - 1;
         }
-        const uint32_t rest = (uint32_t)(u - (unsigned long long)s_before[lo] * tiles), passes = s_before[lo + 1] - s_before[lo];
-        return Unit{(uint32_t)lo, rest / passes, rest % passes};
+        const uint32_t first = s_first[lo] + (pass - s_passes[lo]) * P::tokens;
+        return Unit{s_list[lo], u % tiles, first, min((uint32_t)P::tokens, s_first[lo + 1] - first)};
     };
-    auto rows_of = [&](unsigned long long u, const char *&ra, const char *&rb) {
+    auto rows_of = [&](uint32_t u, const char *&ra, const char *&rb) {
         ra = rb = nullptr;
         if (u >= end) return;
         const Unit t = unit(u);
-        const unsigned long long e = (unsigned long long)s_list[t.which];
+        const unsigned long long e = t.expert;
         if (DOWN) {
             const uint32_t r = t.tile * 128 + warp * 16 + g;
             if (r < a.hidden) ra = a.down + (e * a.hidden + r) * a.ld_down;
@@ -532,25 +544,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
     next.load(ra, rb, j * 16, bytes);
     if (DOWN) grid_wait();                                          /* what was loaded so far no kernel writes */
 
-    uint32_t listed = 0xFFFFFFFFu, in_expert = 0;
-    for (unsigned long long u = begin; u < end; ++u) {
+    for (uint32_t u = begin; u < end; ++u) {
         const Unit at = unit(u);
-        if (at.which != listed) {
-            __syncthreads();
-            /* in the order of the choices: all CTAs cut the same passes */
-            in_expert = (uint32_t)keep_in_order(a.tokens * a.top_k, s_scratch, [&](uint32_t i) { return expert_of(a, i) == s_list[at.which]; },
-                                                [&](int to, uint32_t i) { s_slots[to] = (uint16_t)i; });
-            listed = at.which;
-        }
-        const uint32_t n = min(in_expert - at.pass * P::tokens, (uint32_t)P::tokens), groups = (n + 7) / 8;
-        const uint16_t *const slots = s_slots + at.pass * P::tokens;
+        const uint32_t n = at.n, groups = (n + 7) / 8;
         /* column c: token c of the pass; its second part lies G * 8 columns on */
         auto fetch = [&](uint32_t step, int buffer) {
             char *const to = smem + buffer * (P::groups * 8 * kChunkRow);
             for (uint32_t i = threadIdx.x; i < n * P::parts * (kChunk / 16); i += kThreads) {
                 const uint32_t c = i / (kChunk / 16), piece = i % (kChunk / 16) * 16, off = step * kChunk + piece;
-                const uint32_t token = c % n, part = c / n;
-                const char *row = DOWN ? a.h + ((size_t)slots[token] * P::parts + part) * a.h_row : a.x + (slots[token] / a.top_k) * a.ld_x;
+                const uint32_t part = P::parts == 2 && c >= n ? 1 : 0, token = c - part * n, in_list = at.first + token;
+                const char *row = DOWN ? a.h + ((size_t)in_list * P::parts + part) * a.h_row : a.x + s_token[in_list] * a.ld_x;
                 char *const dst = to + (part * (G * 8) + token) * kChunkRow + piece;
                 const uint32_t end_of = DOWN ? a.h_row : bytes;
                 if (DOWN || XVEC) {
@@ -573,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
             __syncthreads();                                        /* chunk s is there, chunk s - 1 has been read */
             if (s + 1 < steps) fetch(s + 1, (s + 1) & 1);
             const char *const cols = smem + (s & 1) * (P::groups * 8 * kChunkRow);
-#pragma unroll
+#pragma unroll 1
             for (int half = 0; half < kChunk / (kAhead * kBlock); ++half) {
                 const uint32_t off = s * kChunk + half * kAhead * kBlock;
                 const Weights<VEC> now = next;
@@ -599,13 +602,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
                         }
                     } else {
 #pragma unroll
-                        for (int q = 0; q < G; ++q) {
-                            if ((uint32_t)q >= groups) break;
+                        for (int q = 0; q < 2 * G; ++q) {
+                            if ((uint32_t)q * 4 >= n) break;        /* by fours: columns of no token are whatever they are */
 #pragma unroll
-                            for (int t = 0; t < 8; ++t) {
-                                const float4 v = *reinterpret_cast<const float4 *>(x + (q * 8 + t) * kChunkRow);
-                                acc[q][t] = dot4(wa, v, acc[q][t]);
-                                acc[q][8 + t] = dot4(wb, v, acc[q][8 + t]);
+                            for (int t = 4 * q; t < 4 * q + 4; ++t) {
+                                const float4 v = *reinterpret_cast<const float4 *>(x + t * kChunkRow);
+                                acc[t / 8][t % 8] = dot4(wa, v, acc[t / 8][t % 8]);
+                                acc[t / 8][8 + t % 8] = dot4(wb, v, acc[t / 8][8 + t % 8]);
                             }
                         }
                     }
@@ -616,17 +619,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
         /* rows g (first) and g + 8 (second) of the warp's 16, token t of the pass */
         auto put = [&](uint32_t t, float first, float second) {
             if (t >= n) return;
-            const uint32_t slot = slots[t];
+            const size_t to = at.first + t;
             if (DOWN) {
                 const uint32_t r = at.tile * 128 + warp * 16 + g;
-                float *const y = a.y + (size_t)slot * a.hidden + r;
+                float *const y = a.y + to * a.hidden + r;
                 if (r < a.hidden) y[0] = first;
                 if (r + 8 < a.hidden) y[8] = second;
             } else {
                 const uint32_t r = at.tile * 64 + warp * 8 + g;
                 if (r >= a.inter) return;
-                const float v = weight_of(a, slot / a.top_k, s_list[at.which]) * (activate(first, a.activation) * second);
-                store_h<DT>(a, a.h + (size_t)slot * (DT == SIFAR_BF16 ? 2 : 1) * a.h_row, a.h_row, r, v);
+                const float v = weight_of(a, s_token[to], at.expert) * (activate(first, a.activation) * second);
+                store_h<DT>(a, a.h + to * (DT == SIFAR_BF16 ? 2 : 1) * a.h_row, a.h_row, r, v);
             }
         };
 #pragma unroll
@@ -659,10 +662,10 @@ __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ Exp
     __shared__ int s_row[SIFAR_ROUTE_MAX_TOP_K];
     const uint32_t t = blockIdx.y, c0 = (blockIdx.x * kThreads + threadIdx.x) * 4;
     const uint32_t mine = t * a.top_k + threadIdx.x;
-    int row = threadIdx.x < a.top_k && expert_of(a, mine) >= 0 ? (int)mine : -1;        /* the choices were complete long ago */
+    int row = threadIdx.x < a.top_k && expert_of(a, mine) >= 0 ? 0 : -1;                 /* the choices were complete long ago */
     grid_wait();
     grid_let_next_in();
-    if (a.place && row >= 0) row = __ldcg(a.place + mine);
+    if (row >= 0) row = __ldcg(a.place + mine);
     if (threadIdx.x < a.top_k) s_row[threadIdx.x] = row;
     __syncthreads();
     if (c0 >= a.hidden) return;
@@ -720,27 +723,36 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     return SIFAR_OK;
 }
 
-template <typename... P, typename... A>
-static cudaError_t launch_shared(void (*kernel)(P...), dim3 grid, size_t shared, cudaStream_t stream, const A &...args)
+static cudaError_t launch_shared(void (*kernel)(ExpertsArgs), dim3 grid, size_t shared, cudaStream_t stream, unsigned cluster, const ExpertsArgs &a)
 {
     if (shared)                              /* with what the kernels declare themselves it may be more than 48 KB */
         if (cudaError_t e = cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared)) return e;
-    return launch_op(kernel, grid, dim3(kThreads), 1, shared, stream, args...);
+    return launch_op(kernel, grid, dim3(kThreads), cluster, shared, stream, a);
+}
+static cudaError_t launch_shared(void (*kernel)(ExpertsArgs), dim3 grid, size_t shared, cudaStream_t stream, const ExpertsArgs &a)
+{
+    return launch_shared(kernel, grid, shared, stream, 1, a);
 }
 
 template <int DT, int G>
-static cudaError_t launch_few(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, const ExpertsArgs &a)
+static cudaError_t launch_few(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, ExpertsArgs a)
 {
-    const size_t shared = (a.tokens + 3) / 4 * 4 * (size_t)p.x_row, staged = DT == SIFAR_F32 ? (size_t)kWarps * 2 * Staged<G>::bytes : 0;
+    const size_t shared = (a.tokens + 3) / 4 * 4 * (size_t)p.x_row, staged = (size_t)kWarps * 2 * Staged<DT, G>::bytes;
     const unsigned ctas = kSms * (shared <= kFewShared ? kFewCtas(G) : 1);
-    const dim3 grid(ctas), columns(a.hidden < 8 * ctas ? (a.hidden + 7) / 8 : ctas);       /* of the output: 8 at least */
-    cudaError_t e = !gu_vec ? launch_shared(k_up_few<DT, G, false, false>, grid, shared, stream, a)
-                    : x_vec ? launch_shared(k_up_few<DT, G, true, true>, grid, shared, stream, a) : launch_shared(k_up_few<DT, G, true, false>, grid, shared, stream, a);
+    cudaError_t e = !gu_vec ? launch_shared(k_up_few<DT, G, false, false>, dim3(ctas), shared, stream, a)
+                    : x_vec ? launch_shared(k_up_few<DT, G, true, true>, dim3(ctas), shared, stream, a) : launch_shared(k_up_few<DT, G, true, false>, dim3(ctas), shared, stream, a);
     if (e) return e;
+    /* at least 8 columns per CTA, or per cluster where the items can be shared: two per warp at least */
+    const unsigned most = kSms * kFewCtas(G), columns = a.hidden < 8 * most ? (a.hidden + 7) / 8 : most;
+    const size_t pieces = ((size_t)a.inter * elem_size(DT) + kAhead * kBlock - 1) / (kAhead * kBlock), choices = (size_t)a.tokens * a.top_k;
+    const size_t items = (choices < a.experts ? choices : a.experts) * pieces;
+    a.split = 1;
+    while (a.split < kMaxSplit && 2 * a.split * columns <= most && 2 * 2 * a.split * kWarps <= items) a.split *= 2;
+    const auto down = [&](auto kernel, size_t bytes) { return launch_shared(kernel, dim3(columns * a.split), bytes, stream, a.split, a); };
     if constexpr (DT == SIFAR_BF16 && G == 1) {
-        if (a.tokens <= 4) return dn_vec ? launch_shared(k_down_few<DT, G, true, true>, columns, staged, stream, a) : launch_shared(k_down_few<DT, G, false, true>, columns, staged, stream, a);
+        if (a.tokens <= 4) return dn_vec ? down(k_down_few<DT, G, true, true>, 0) : down(k_down_few<DT, G, false, true>, 0);
     }
-    return dn_vec ? launch_shared(k_down_few<DT, G, true, false>, columns, staged, stream, a) : launch_shared(k_down_few<DT, G, false, false>, columns, staged, stream, a);
+    return dn_vec ? down(k_down_few<DT, G, true, false>, staged) : down(k_down_few<DT, G, false, false>, staged);
 }
 
 template <int DT>
@@ -752,18 +764,19 @@ static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec
         if (a.tokens <= 8) return launch_few<DT, 1>(p, gu_vec, dn_vec, x_vec, stream, a);
         return a.tokens <= 16 ? launch_few<DT, 2>(p, gu_vec, dn_vec, x_vec, stream, a) : launch_few<DT, 4>(p, gu_vec, dn_vec, x_vec, stream, a);
     }
-    if (DT == SIFAR_BF16 && gu_vec && dn_vec && x_vec) {
-        a.place = (int *)((char *)a.y + p.y_bytes);
-        e = launch_expert_tiles(stream, a);
+    if (DT == SIFAR_BF16 && gu_vec && dn_vec) {
+        e = launch_expert_tiles(stream, a, x_vec);
         if (e) return e;
         return launch_shared(k_gather<DT>, dim3((a.hidden + 4 * kThreads - 1) / (4 * kThreads), a.tokens), 0, stream, a);
     }
-    e = !gu_vec ? launch_shared(k_products<DT, false, false, false>, grid, Pass<DT, false>::shared, stream, a)
-        : x_vec ? launch_shared(k_products<DT, false, true, true>, grid, Pass<DT, false>::shared, stream, a)
-                : launch_shared(k_products<DT, false, true, false>, grid, Pass<DT, false>::shared, stream, a);
+    const size_t bits = (size_t)a.experts * ((a.tokens + 31) / 32) * sizeof(uint32_t);
+    const auto shared = [&](size_t columns) { return columns > bits ? columns : bits; };
+    e = !gu_vec ? launch_shared(k_products<DT, false, false, false>, grid, shared(Pass<DT, false>::shared), stream, a)
+        : x_vec ? launch_shared(k_products<DT, false, true, true>, grid, shared(Pass<DT, false>::shared), stream, a)
+                : launch_shared(k_products<DT, false, true, false>, grid, shared(Pass<DT, false>::shared), stream, a);
     if (e) return e;
-    e = dn_vec ? launch_shared(k_products<DT, true, true, true>, grid, Pass<DT, true>::shared, stream, a)
-               : launch_shared(k_products<DT, true, false, true>, grid, Pass<DT, true>::shared, stream, a);
+    e = dn_vec ? launch_shared(k_products<DT, true, true, true>, grid, shared(Pass<DT, true>::shared), stream, a)
+               : launch_shared(k_products<DT, true, false, true>, grid, shared(Pass<DT, true>::shared), stream, a);
     if (e) return e;
     return launch_shared(k_gather<DT>, dim3((a.hidden + 4 * kThreads - 1) / (4 * kThreads), a.tokens), 0, stream, a);
 }
@@ -807,7 +820,7 @@ extern "C" int sifar_experts(const sifar_experts_args *g, void *stream)
     ExpertsArgs a;
     a.x = (const char *)g->x; a.gate_up = (const char *)g->gate_up; a.down = (const char *)g->down; a.out = (char *)g->out;
     a.indices = g->indices; a.weights = g->weights;
-    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes); a.place = nullptr;
+    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes); a.place = (int *)((char *)a.y + p.y_bytes);
     a.ld_x = all[0].ld * es; a.ld_gate_up = all[3].ld * es; a.ld_down = all[4].ld * es; a.ld_out = all[5].ld * es;
     a.tokens = (uint32_t)T; a.hidden = (uint32_t)H; a.inter = (uint32_t)I; a.h_row = p.h_row; a.top_k = (uint32_t)g->top_k;
     a.experts = (uint32_t)E; a.first = g->first_expert; a.activation = g->activation; a.x_row = p.x_row;

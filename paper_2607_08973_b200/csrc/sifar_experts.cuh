@@ -17,15 +17,49 @@ struct ExpertsArgs {
     char *out;
     const int *indices;
     const float *weights;
-    char *h;                                 /* between the products, rows of h_row bytes.  few: [active][part][token], tiles: [place][part],
-                                                else [token][choice][part] */
-    float *y;                                /* tiles: [place][hidden], else [token][choice][hidden] */
-    int *place;                              /* tiles: of each choice in the list by experts, or -1 */
+    char *h;                                 /* between the products, rows of h_row bytes.  few: [active][part][token], else [place][part] */
+    float *y;                                /* [place][hidden] */
+    int *place;                              /* of each choice in the list by experts, or -1 */
     unsigned long long ld_x, ld_gate_up, ld_down, ld_out;    /* bytes */
     uint32_t tokens, hidden, inter, h_row, top_k, experts;
     int first, activation;
     uint32_t x_row;                          /* few: bytes between the tokens' rows in shared memory */
+    uint32_t split;                          /* few: CTAs that share columns of the output */
 };
+
+/* Bytes sh .. sh + 15 of two vectors in a row, those from `left` on 0. */
+__device__ __forceinline__ uint4 shifted(const uint4 &lo, const uint4 &hi, uint32_t sh, int left)
+{
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    /* words first, then the bits within them */
+    if (sh & 8u) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    }
+    if (sh & 4u) {
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    }
+    const uint32_t bits = (sh & 3u) * 8u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+    if (left < 16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = left >= 4 * i + 4 ? w[i] : left <= 4 * i ? 0u : w[i] & ((1u << (left - 4 * i) * 8) - 1u);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+/* 16 bytes from any element on, zeros from `left` on. */
+__device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
+{
+    const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;
+    const uint4 *const q = reinterpret_cast<const uint4 *>(p - sh);
+    const uint4 lo = __ldg(q);
+    uint4 hi = make_uint4(0u, 0u, 0u, 0u);
+    if (sh && left > 16u - sh) hi = __ldg(q + 1);
+    return shifted(lo, hi, sh, (int)left);
+}
 
 __device__ __forceinline__ float activate(float g, int kind)
 {
@@ -102,21 +136,85 @@ __device__ __forceinline__ int keep_in_order(uint32_t n, int *scratch, On on, Pu
     return total;
 }
 
-/* The experts that have tokens, in their order: list[i] = the i-th one's number; counts[e] = its tokens.  Returns how many. */
-__device__ __forceinline__ int list_experts(const ExpertsArgs &a, int *counts, int *list, int *scratch)
+/* What a CTA works out of the choices: experts that have tokens (list), where each one's tokens begin in the list by experts (first, and
+   place by the expert's number), passes of `columns` tokens before each (passes), the tokens by expert in their order (token). */
+struct ExpertPlan { int active; uint32_t passes; };
+
+/*
+ * A bit per expert and token that chose it (twice: once): an expert's tokens are counted and numbered by bits, in the same order in
+ * every CTA.  bits: experts x (tokens / 32) words, sum: a word per warp.  `tell`: this CTA writes the places for the sum over a
+ * token's choices.  All of the CTA; the barrier behind it is the caller's.
+ */
+template <int THREADS>
+__device__ __forceinline__ ExpertPlan plan_experts(const ExpertsArgs &a, uint32_t columns, uint32_t *bits, unsigned long long *sum, uint16_t *place, uint16_t *list,
+                                                   uint16_t *first, uint16_t *passes, uint8_t *token, bool tell)
 {
-    for (uint32_t e = threadIdx.x; e < a.experts; e += kExpertThreads) counts[e] = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    const uint32_t words = (a.tokens + 31) / 32, choices = a.tokens * a.top_k;
+    for (uint32_t i = threadIdx.x; i < a.experts * words; i += THREADS) bits[i] = 0u;
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < a.tokens * a.top_k; i += kExpertThreads) {
-        const int e = expert_of(a, i);
-        if (e >= 0) atomicAdd(&counts[e], 1);
+    for (uint32_t i = threadIdx.x; i < choices; i += THREADS) {
+        const uint32_t e = local_expert(a, a.indices[i]), t = i / a.top_k;
+        if (e < a.experts) atomicOr(&bits[e * words + t / 32], 1u << (t % 32));
     }
     __syncthreads();
-    return keep_in_order(a.experts, scratch, [&](uint32_t e) { return counts[e] > 0; }, [&](int at, uint32_t e) { list[at] = (int)e; });
+    /* in one sum over the experts: how many have tokens, their tokens, their passes */
+    constexpr uint32_t kEach = (SIFAR_ROUTE_MAX_EXPERTS + THREADS - 1) / THREADS;
+    uint32_t n[kEach];
+    unsigned long long mine = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t e = threadIdx.x * kEach + i;
+        n[i] = 0;
+        if (e < a.experts)
+            for (uint32_t w = 0; w < words; ++w) n[i] += __popc(bits[e * words + w]);
+        mine += (unsigned long long)(n[i] ? 1u : 0u) << 40 | (unsigned long long)n[i] << 20 | (n[i] + columns - 1) / columns;
+    }
+    unsigned long long upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const unsigned long long o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 31) sum[warp] = upto;
+    __syncthreads();
+    unsigned long long before = upto - mine, all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) before += sum[w];
+        all += sum[w];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        if (!n[i]) continue;
+        const uint32_t e = threadIdx.x * kEach + i, at = (uint32_t)(before >> 40);
+        list[at] = (uint16_t)e;
+        place[e] = first[at] = (uint16_t)((before >> 20) & 0xFFFFFu);
+        passes[at] = (uint16_t)(before & 0xFFFFFu);
+        before += 1ull << 40 | (unsigned long long)n[i] << 20 | (n[i] + columns - 1) / columns;
+    }
+    const ExpertPlan plan{(int)(all >> 40), (uint32_t)(all & 0xFFFFFu)};
+    if (threadIdx.x == 0) {
+        first[plan.active] = (uint16_t)((all >> 20) & 0xFFFFFu);
+        passes[plan.active] = (uint16_t)plan.passes;
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < choices; i += THREADS) {
+        const uint32_t e = local_expert(a, a.indices[i]), t = i / a.top_k;
+        int at = -1;
+        if (e < a.experts) {
+            at = place[e] + __popc(bits[e * words + t / 32] & ((1u << (t % 32)) - 1u));
+            for (uint32_t w = 0; w < t / 32; ++w) at += __popc(bits[e * words + w]);
+            token[at] = (uint8_t)t;
+        }
+        if (tell) a.place[i] = at;
+    }
+    return plan;
 }
 
-/* bf16 rows of whole 16-byte pieces, more tokens than k_up_few takes: the two products, up to k_gather, and `place` for it. */
-cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a);
+/* bf16 weight rows of whole 16-byte pieces (x_vec: the tokens', too), more tokens than k_up_few takes: the two products, up to
+   k_gather, and `place` for it. */
+cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a, bool x_vec);
 
 }  /* namespace sifar */
 #endif

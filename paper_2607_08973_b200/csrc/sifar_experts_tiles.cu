@@ -42,6 +42,7 @@ template <bool DOWN> struct Tile {
 struct TilesArgs {
     ExpertsArgs e;
     uint32_t columns;                        /* of a pass over an expert's rows */
+    bool x_vec;                              /* the tokens' rows in 16-byte pieces */
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -137,7 +138,6 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
     __shared__ __align__(16) float s_weight[kDrainers][32];         /* of a tile's tokens, each warp's half */
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     uint32_t *const s_bits = reinterpret_cast<uint32_t *>(smem);
-    const uint32_t words = (a.tokens + 31) / 32, choices = a.tokens * a.top_k;
     if (warp == 0 && lane < 4) asm volatile("prefetch.tensormap [%0];" :: "l"(&maps.of[lane]) : "memory");
     if (!DOWN) grid_wait();
     grid_let_next_in();                                             /* the choices are complete: the next kernel may read them too */
@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(shared_at(&s_tmem)), "r"(256u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        sums_before();
     }
     if (threadIdx.x == 0) {
         for (int i = 0; i < kMaxRing; ++i) {
@@ -157,75 +158,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    /* a bit per expert and token that chose it (twice: once): an expert's tokens are counted and numbered by bits, in the same order
-       in every CTA */
-    for (uint32_t i = threadIdx.x; i < a.experts * words; i += kTileThreads) s_bits[i] = 0u;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < choices; i += kTileThreads) {
-        const uint32_t e = local_expert(a, a.indices[i]), token = i / a.top_k;
-        if (e < a.experts) atomicOr(&s_bits[e * words + token / 32], 1u << (token % 32));
-    }
-    __syncthreads();
-    /* in one sum over the experts: how many have tokens, their tokens, their passes */
-    constexpr uint32_t kEach = (SIFAR_ROUTE_MAX_EXPERTS + kTileThreads - 1) / kTileThreads;
-    uint32_t n[kEach];
-    unsigned long long mine = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kEach; ++i) {
-        const uint32_t e = threadIdx.x * kEach + i;
-        n[i] = 0;
-        if (e < a.experts)
-            for (uint32_t w = 0; w < words; ++w) n[i] += __popc(s_bits[e * words + w]);
-        mine += (unsigned long long)(n[i] ? 1u : 0u) << 40 | (unsigned long long)n[i] << 20 | (n[i] + ta.columns - 1) / ta.columns;
-    }
-    unsigned long long upto = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long o = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-        if (lane >= d) upto += o;
-    }
-    if (lane == 31) s_sum[warp] = upto;
-    sums_before();                                                  /* the address of tensor memory, too */
-    __syncthreads();
-    sums_after();
-    unsigned long long before = upto - mine, all = 0;
-#pragma unroll
-    for (int w = 0; w < kTileWarps; ++w) {
-        if (w < warp) before += s_sum[w];
-        all += s_sum[w];
-    }
-#pragma unroll
-    for (uint32_t i = 0; i < kEach; ++i) {
-        if (!n[i]) continue;
-        const uint32_t e = threadIdx.x * kEach + i, at = (uint32_t)(before >> 40), first = (uint32_t)(before >> 20) & 0xFFFFFu;
-        s_list[at] = (uint16_t)e;
-        s_place[e] = s_first[at] = (uint16_t)first;
-        s_passes[at] = (uint16_t)(before & 0xFFFFFu);
-        before += 1ull << 40 | (unsigned long long)n[i] << 20 | (n[i] + ta.columns - 1) / ta.columns;
-    }
-    const int active = (int)(all >> 40);
-    if (threadIdx.x == 0) {
-        s_first[active] = (uint16_t)((all >> 20) & 0xFFFFFu);
-        s_passes[active] = (uint16_t)(all & 0xFFFFFu);
-    }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < choices; i += kTileThreads) {
-        const uint32_t e = local_expert(a, a.indices[i]), token = i / a.top_k;
-        int at = -1;
-        if (e < a.experts) {
-            at = s_place[e] + __popc(s_bits[e * words + token / 32] & ((1u << (token % 32)) - 1u));
-            for (uint32_t w = 0; w < token / 32; ++w) at += __popc(s_bits[e * words + w]);
-            s_token[at] = (uint8_t)token;
-        }
-        if (!DOWN && blockIdx.x == 0) a.place[i] = at;              /* for the sum over a token's choices */
-    }
+    const ExpertPlan plan = plan_experts<kTileThreads>(a, ta.columns, s_bits, s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
+    sums_after();                                                   /* the address of tensor memory */
+    const int active = plan.active;
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    /* what was read and written where the ring is now */
     __syncthreads();
     const uint32_t tmem = s_tmem;
 
     /* Groups of a tile: as many as the fullest CTA gets through soonest (lane s - 1 looks at s).  A tile of few groups is not
        faster than its products, 0.15 to 0.27 us a step: as the weights of 1.6 to 2.8 groups, and half as large ones of DOWN. */
-    const uint32_t rows = DOWN ? a.hidden : a.inter, groups = (rows + kGroup - 1) / kGroup, passes = (uint32_t)(all & 0xFFFFFu);
+    const uint32_t rows = DOWN ? a.hidden : a.inter, groups = (rows + kGroup - 1) / kGroup, passes = plan.passes;
     const uint32_t s = (uint32_t)lane % kGroups + 1, most = (passes * ((groups + s - 1) / s) + gridDim.x - 1) / gridDim.x;
     const uint32_t cost = most * max(10 * s, S::parts * (12 + ta.columns / 4));
     const uint32_t size = kGroups - __reduce_min_sync(0xFFFFFFFFu, cost << 3 | (kGroups - s)) % kGroups;       /* the larger one of equals */
@@ -328,11 +270,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             for (uint32_t s = 0; s < steps; ++s) {
                 const uint32_t to = shared_at(smem) + stage * stage_bytes + place, off = s * kSpan, size = off + piece * 16 < bytes ? 16u : 0u;
                 bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
+                if (DOWN || ta.x_vec) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (r0 + 8 * i >= t.n) break;
+                    for (int i = 0; i < 8; ++i) {
+                        if (r0 + 8 * i >= t.n) break;
 #pragma unroll
-                    for (int p = 0; p < S::parts; ++p) copy16(to + (p * ta.columns + 8 * i) * kSpan, cols[i] + (size ? off : 0u) + p * a.h_row, size);
+                        for (int p = 0; p < S::parts; ++p) copy16(to + (p * ta.columns + 8 * i) * kSpan, cols[i] + (size ? off : 0u) + p * a.h_row, size);
+                    }
+                } else {
+                    uint4 v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = size && r0 + 8 * i < t.n ? load_shifted(cols[i] + off, bytes - off - piece * 16) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (r0 + 8 * i < t.n) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(to + 8 * i * kSpan), "r"(v[i].x), "r"(v[i].y), "r"(v[i].z), "r"(v[i].w) : "memory");
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 step_on();
@@ -449,10 +401,11 @@ template <bool DOWN> static cudaError_t launch_tiles(cudaStream_t stream, TilesA
     return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kTileThreads), 1, kRing, stream, maps, t);
 }
 
-cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
+cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a, bool x_vec)
 {
     TilesArgs t;
     t.e = a;
+    t.x_vec = x_vec;
     /* columns of a pass: four times an expert's share of the choices, were they spread evenly; more take another pass */
     const uint32_t most = 4 * ((a.tokens * a.top_k + a.experts - 1) / a.experts), need = most < a.tokens ? most : a.tokens;
     t.columns = need <= 16 ? 16 : need <= 32 ? 32 : 64;
