@@ -137,14 +137,16 @@ template <int G> struct Few<SIFAR_F32, G> {
     __device__ __forceinline__ void store(float *red)
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+        /* lane j ends with tokens j, j + 4, ...: it sends on what others keep */
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int t = 0; t < 8 * G; ++t) {
-                float v = c[r][t];
-                v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
-                v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
-                if (j == (t & 3)) red[(g + 8 * r) * 8 * G + t] = v;
+            for (int t = 0; t < 8 * G; t += 4) {
+                const float *const v = c[r] + t;
+                const bool high = j & 2, odd = j & 1;
+                const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[2], 2);
+                const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, high ? v[1] : v[3], 2);
+                red[(g + 8 * r) * 8 * G + t + j] = (odd ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 1);
             }
     }
 };
@@ -167,8 +169,8 @@ constexpr int kFewCtas(int G) { return G <= 2 ? 2 : 1; }             /* per SM *
 
 /*
  * All experts' rows lie in a row and every CTA has an equal share of it, 8 gate rows and the 8 up rows that go with them at a
- * time, so a product's gate and up lie 8 rows apart.  Warp w takes every eighth 256 bytes of the rows; the next 256 are under
- * way while these are multiplied, across tiles too.
+ * time, so a product's gate and up lie 8 rows apart.  The warps take the rows' 256-byte pieces in turn, in groups with tiles of their
+ * own where rows have fewer than eight; the next pieces are under way while these are multiplied, across tiles too.
  */
 template <int DT, int G, bool VEC, bool XVEC>
 __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_constant__ ExpertsArgs a)
@@ -199,16 +201,19 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     if (kCopy) copies_commit();
     const uint32_t pairs = (uint32_t)list_few(a, s_list, s_tokens, s_bits, s_scratch) * a.inter;
     const uint32_t begin = (uint32_t)((unsigned long long)pairs * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)pairs * (blockIdx.x + 1) / gridDim.x);
-    const uint32_t steps = (bytes + kWarps * kAhead * kBlock - 1) / (kWarps * kAhead * kBlock);
+    constexpr uint32_t kPiece = kAhead * kBlock;
+    const uint32_t pieces = (bytes + kPiece - 1) / kPiece;
+    const uint32_t group = pieces <= 1 ? 1u : pieces <= 2 ? 2u : pieces <= 4 ? 4u : (uint32_t)kWarps, tiles = kWarps / group;     /* warps of a tile, tiles at a time */
+    const uint32_t steps = (pieces + group - 1) / group, span = group * kPiece;
     auto rows_of = [&](uint32_t p, const char *&ra, const char *&rb) {
         ra = rb = nullptr;
-        p += g;
+        p += warp / group * 8 + g;
         if (p >= end) return;
         const uint32_t which = p / a.inter;
         ra = a.gate_up + ((unsigned long long)s_list[which] * 2 * a.inter + (p - which * a.inter)) * a.ld_gate_up;
         rb = ra + (unsigned long long)a.inter * a.ld_gate_up;
     };
-    const uint32_t mine = warp * kAhead * kBlock + j * 16;
+    const uint32_t mine = warp % group * kPiece + j * 16;
     const char *ra, *rb;
     rows_of(begin, ra, rb);
     Weights<VEC> next;
@@ -232,15 +237,15 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     __syncthreads();
 
     int parity = 0;
-    for (uint32_t p = begin; p < end; p += 8, parity ^= 1) {
+    for (uint32_t p = begin; p < end; p += 8 * tiles, parity ^= 1) {
         Few<DT, G> acc;
         for (uint32_t s = 0; s < steps; ++s) {
             const Weights<VEC> now = next;
-            const uint32_t at = s * kWarps * kAhead * kBlock + mine;
+            const uint32_t at = s * span + mine;
             if (s + 1 < steps) {
-                next.load(ra, rb, at + kWarps * kAhead * kBlock, bytes);
+                next.load(ra, rb, at + span, bytes);
             } else {
-                rows_of(p + 8, ra, rb);
+                rows_of(p + 8 * tiles, ra, rb);
                 next.load(ra, rb, mine, bytes);
             }
 #pragma unroll
@@ -271,13 +276,16 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
         }
         acc.store(s_red[parity][warp]);
         __syncthreads();                                            /* the other parity's sums are read by now */
-        const uint32_t i = threadIdx.x / 32, t = lane, which = (p + i) / a.inter;
-        if (p + i < end && t < a.tokens && (s_tokens[which] >> t & 1u)) {
+        /* a warp has a pair of each tile, its lanes the tokens */
+        const uint32_t t = lane;
+        for (uint32_t tile = 0; tile < tiles; ++tile) {
+            const uint32_t pair = p + tile * 8 + warp, which = pair / a.inter;
+            if (pair >= end) break;
+            if (t >= a.tokens || !(s_tokens[which] >> t & 1u)) continue;
             float gate = 0.0f, up = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) { gate += s_red[parity][w][i * 8 * G + t]; up += s_red[parity][w][(i + 8) * 8 * G + t]; }
+            for (uint32_t w = tile * group; w < (tile + 1) * group; ++w) { gate += s_red[parity][w][warp * 8 * G + t]; up += s_red[parity][w][(warp + 8) * 8 * G + t]; }
             const size_t low = (size_t)a.tokens * a.h_row;
-            store_h<DT>(a, a.h + which * (DT == SIFAR_BF16 ? 2 : 1) * low + t * (size_t)a.h_row, low, p + i - which * a.inter,
+            store_h<DT>(a, a.h + which * (DT == SIFAR_BF16 ? 2 : 1) * low + t * (size_t)a.h_row, low, pair - which * a.inter,
                         weight_of(a, t, s_list[which]) * (activate(gate, a.activation) * up));
         }
     }
@@ -492,7 +500,7 @@ template <int DT, bool DOWN> struct Pass {
  * output (DOWN).  The columns' rows come through shared memory 512 bytes at a time, the next ones under way; weights as
  * above, 256 bytes ahead.
  */
-template <int DT, bool DOWN, bool VEC, bool XVEC>
+template <int DT, bool DOWN, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant__ ExpertsArgs a)
 {
     using P = Pass<DT, DOWN>;
@@ -555,13 +563,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
                 const uint32_t part = P::parts == 2 && c >= n ? 1 : 0, token = c - part * n, in_list = at.first + token;
                 const char *row = DOWN ? a.h + ((size_t)in_list * P::parts + part) * a.h_row : a.x + s_token[in_list] * a.ld_x;
                 char *const dst = to + (part * (G * 8) + token) * kChunkRow + piece;
-                const uint32_t end_of = DOWN ? a.h_row : bytes;
-                if (DOWN || XVEC) {
-                    const uint32_t take = off < end_of ? 16u : 0u;
-                    copy16(dst, row + (take ? off : 0u), take);
-                } else {
-                    *reinterpret_cast<uint4 *>(dst) = off < end_of ? load_shifted(row + off, end_of - off) : make_uint4(0u, 0u, 0u, 0u);
-                }
+                const uint32_t end_of = DOWN ? a.h_row : (bytes + 15u) & ~15u;
+                const uint32_t take = off < end_of ? 16u : 0u;
+                copy16(dst, row + (take ? off : 0u), take);
             }
             copies_commit();
         };
@@ -655,6 +659,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
     }
 }
 
+/* The tokens' rows once more, on 16-byte boundaries, zeros behind their ends. */
+template <int DT>
+__global__ void __launch_bounds__(kThreads) k_align(const __grid_constant__ ExpertsArgs a)
+{
+    constexpr uint32_t es = DT == SIFAR_BF16 ? 2 : 4;
+    const uint32_t bytes = a.hidden * es, ld = (bytes + 15u) & ~15u, at = (blockIdx.x * kThreads + threadIdx.x) * 16;
+    grid_wait();
+    grid_let_next_in();
+    if (at < bytes) *reinterpret_cast<uint4 *>(a.rows + (size_t)blockIdx.y * ld + at) = load_shifted(a.x + blockIdx.y * a.ld_x + at, bytes - at);
+}
+
 /* out_t = the sum over its choices here, in their order; a second choice of the same expert has its share in the first. */
 template <int DT>
 __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ ExpertsArgs a)
@@ -693,7 +708,7 @@ __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ Exp
 /* ------------------------------------------------------------------------ */
 /* host                                                                      */
 /* ------------------------------------------------------------------------ */
-struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, y_bytes, bytes; };
+struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, y_bytes, rows_bytes, bytes; };
 
 constexpr size_t kFewShared = 92 * 1024;     /* the tokens' rows in shared memory: two CTAs of 8 warps per SM */
 constexpr size_t kFewMostShared = 180 * 1024;  /* ... one */
@@ -719,7 +734,8 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
     p.h_bytes = ((p.few ? most * T : choices) * parts * p.h_row + 15) / 16 * 16;
     p.y_bytes = p.few ? 0 : (choices * g->hidden * sizeof(float) + 15) / 16 * 16;
-    p.bytes = p.h_bytes + p.y_bytes + (p.few ? 0 : choices * sizeof(int));
+    p.rows_bytes = p.few ? 0 : T * ((g->hidden * es + 15) / 16 * 16);
+    p.bytes = p.h_bytes + p.y_bytes + p.rows_bytes + (p.few ? 0 : choices * sizeof(int));
     return SIFAR_OK;
 }
 
@@ -742,12 +758,14 @@ static cudaError_t launch_few(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bo
     cudaError_t e = !gu_vec ? launch_shared(k_up_few<DT, G, false, false>, dim3(ctas), shared, stream, a)
                     : x_vec ? launch_shared(k_up_few<DT, G, true, true>, dim3(ctas), shared, stream, a) : launch_shared(k_up_few<DT, G, true, false>, dim3(ctas), shared, stream, a);
     if (e) return e;
-    /* at least 8 columns per CTA, or per cluster where the items can be shared: two per warp at least */
-    const unsigned most = kSms * kFewCtas(G), columns = a.hidden < 8 * most ? (a.hidden + 7) / 8 : most;
+    /* Blocks of up to 16 columns.  Where they would leave half of the CTAs without work, clusters share them, each warp two items at
+       least: of 8 columns per block only half of a warp's loads are under way.  Between that and all CTAs, blocks of 8 to 16. */
+    const unsigned most = kSms * kFewCtas(G), full = (a.hidden + 15) / 16;
     const size_t pieces = ((size_t)a.inter * elem_size(DT) + kAhead * kBlock - 1) / (kAhead * kBlock), choices = (size_t)a.tokens * a.top_k;
     const size_t items = (choices < a.experts ? choices : a.experts) * pieces;
     a.split = 1;
-    while (a.split < kMaxSplit && 2 * a.split * columns <= most && 2 * 2 * a.split * kWarps <= items) a.split *= 2;
+    while (a.split < kMaxSplit && 2 * a.split * full <= most && 2 * 2 * a.split * kWarps <= items) a.split *= 2;
+    const unsigned half = (a.hidden + 7) / 8, columns = a.split > 1 ? full : half < most ? half : most;
     const auto down = [&](auto kernel, size_t bytes) { return launch_shared(kernel, dim3(columns * a.split), bytes, stream, a.split, a); };
     if constexpr (DT == SIFAR_BF16 && G == 1) {
         if (a.tokens <= 4) return dn_vec ? down(k_down_few<DT, G, true, true>, 0) : down(k_down_few<DT, G, false, true>, 0);
@@ -764,19 +782,24 @@ static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec
         if (a.tokens <= 8) return launch_few<DT, 1>(p, gu_vec, dn_vec, x_vec, stream, a);
         return a.tokens <= 16 ? launch_few<DT, 2>(p, gu_vec, dn_vec, x_vec, stream, a) : launch_few<DT, 4>(p, gu_vec, dn_vec, x_vec, stream, a);
     }
+    if (!x_vec) {                            /* the products below take the tokens' rows in whole pieces */
+        ExpertsArgs rows = a;
+        a.x = a.rows; a.ld_x = (a.hidden * elem_size(DT) + 15) / 16 * 16;
+        e = launch_shared(k_align<DT>, dim3((unsigned)((a.ld_x / 16 + kThreads - 1) / kThreads), a.tokens), 0, stream, rows);
+        if (e) return e;
+    }
     if (DT == SIFAR_BF16 && gu_vec && dn_vec) {
-        e = launch_expert_tiles(stream, a, x_vec);
+        e = launch_expert_tiles(stream, a);
         if (e) return e;
         return launch_shared(k_gather<DT>, dim3((a.hidden + 4 * kThreads - 1) / (4 * kThreads), a.tokens), 0, stream, a);
     }
     const size_t bits = (size_t)a.experts * ((a.tokens + 31) / 32) * sizeof(uint32_t);
     const auto shared = [&](size_t columns) { return columns > bits ? columns : bits; };
-    e = !gu_vec ? launch_shared(k_products<DT, false, false, false>, grid, shared(Pass<DT, false>::shared), stream, a)
-        : x_vec ? launch_shared(k_products<DT, false, true, true>, grid, shared(Pass<DT, false>::shared), stream, a)
-                : launch_shared(k_products<DT, false, true, false>, grid, shared(Pass<DT, false>::shared), stream, a);
+    e = gu_vec ? launch_shared(k_products<DT, false, true>, grid, shared(Pass<DT, false>::shared), stream, a)
+               : launch_shared(k_products<DT, false, false>, grid, shared(Pass<DT, false>::shared), stream, a);
     if (e) return e;
-    e = dn_vec ? launch_shared(k_products<DT, true, true, true>, grid, shared(Pass<DT, true>::shared), stream, a)
-               : launch_shared(k_products<DT, true, false, true>, grid, shared(Pass<DT, true>::shared), stream, a);
+    e = dn_vec ? launch_shared(k_products<DT, true, true>, grid, shared(Pass<DT, true>::shared), stream, a)
+               : launch_shared(k_products<DT, true, false>, grid, shared(Pass<DT, true>::shared), stream, a);
     if (e) return e;
     return launch_shared(k_gather<DT>, dim3((a.hidden + 4 * kThreads - 1) / (4 * kThreads), a.tokens), 0, stream, a);
 }
@@ -820,7 +843,7 @@ extern "C" int sifar_experts(const sifar_experts_args *g, void *stream)
     ExpertsArgs a;
     a.x = (const char *)g->x; a.gate_up = (const char *)g->gate_up; a.down = (const char *)g->down; a.out = (char *)g->out;
     a.indices = g->indices; a.weights = g->weights;
-    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes); a.place = (int *)((char *)a.y + p.y_bytes);
+    a.h = (char *)g->workspace; a.y = (float *)((char *)g->workspace + p.h_bytes); a.rows = (char *)a.y + p.y_bytes; a.place = (int *)(a.rows + p.rows_bytes);
     a.ld_x = all[0].ld * es; a.ld_gate_up = all[3].ld * es; a.ld_down = all[4].ld * es; a.ld_out = all[5].ld * es;
     a.tokens = (uint32_t)T; a.hidden = (uint32_t)H; a.inter = (uint32_t)I; a.h_row = p.h_row; a.top_k = (uint32_t)g->top_k;
     a.experts = (uint32_t)E; a.first = g->first_expert; a.activation = g->activation; a.x_row = p.x_row;

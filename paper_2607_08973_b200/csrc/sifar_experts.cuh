@@ -20,6 +20,7 @@ struct ExpertsArgs {
     char *h;                                 /* between the products, rows of h_row bytes.  few: [active][part][token], else [place][part] */
     float *y;                                /* [place][hidden] */
     int *place;                              /* of each choice in the list by experts, or -1 */
+    char *rows;                              /* not few: the tokens' rows on 16-byte boundaries, where x has them elsewhere */
     unsigned long long ld_x, ld_gate_up, ld_down, ld_out;    /* bytes */
     uint32_t tokens, hidden, inter, h_row, top_k, experts;
     int first, activation;
@@ -212,9 +213,8 @@ __device__ __forceinline__ ExpertPlan plan_experts(const ExpertsArgs &a, uint32_
     return plan;
 }
 
-/* bf16 weight rows of whole 16-byte pieces (x_vec: the tokens', too), more tokens than k_up_few takes: the two products, up to
-   k_gather, and `place` for it. */
-cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a, bool x_vec);
+/* bf16 rows of whole 16-byte pieces, more tokens than k_up_few takes: the two products, up to k_gather, and `place` for it. */
+cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a);
 
 }  /* namespace sifar */
 #endif

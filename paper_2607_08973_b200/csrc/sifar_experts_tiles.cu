@@ -42,7 +42,6 @@ template <bool DOWN> struct Tile {
 struct TilesArgs {
     ExpertsArgs e;
     uint32_t columns;                        /* of a pass over an expert's rows */
-    bool x_vec;                              /* the tokens' rows in 16-byte pieces */
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -270,21 +269,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             for (uint32_t s = 0; s < steps; ++s) {
                 const uint32_t to = shared_at(smem) + stage * stage_bytes + place, off = s * kSpan, size = off + piece * 16 < bytes ? 16u : 0u;
                 bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
-                if (DOWN || ta.x_vec) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (r0 + 8 * i >= t.n) break;
+                for (int i = 0; i < 8; ++i) {
+                    if (r0 + 8 * i >= t.n) break;
 #pragma unroll
-                        for (int p = 0; p < S::parts; ++p) copy16(to + (p * ta.columns + 8 * i) * kSpan, cols[i] + (size ? off : 0u) + p * a.h_row, size);
-                    }
-                } else {
-                    uint4 v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        v[i] = size && r0 + 8 * i < t.n ? load_shifted(cols[i] + off, bytes - off - piece * 16) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (r0 + 8 * i < t.n) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(to + 8 * i * kSpan), "r"(v[i].x), "r"(v[i].y), "r"(v[i].z), "r"(v[i].w) : "memory");
+                    for (int p = 0; p < S::parts; ++p) copy16(to + (p * ta.columns + 8 * i) * kSpan, cols[i] + (size ? off : 0u) + p * a.h_row, size);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 step_on();
@@ -401,11 +390,10 @@ template <bool DOWN> static cudaError_t launch_tiles(cudaStream_t stream, TilesA
     return launch_op(k_expert_tiles<DOWN>, dim3(kSms), dim3(kTileThreads), 1, kRing, stream, maps, t);
 }
 
-cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a, bool x_vec)
+cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
 {
     TilesArgs t;
     t.e = a;
-    t.x_vec = x_vec;
     /* columns of a pass: four times an expert's share of the choices, were they spread evenly; more take another pass */
     const uint32_t most = 4 * ((a.tokens * a.top_k + a.experts - 1) / a.experts), need = most < a.tokens ? most : a.tokens;
     t.columns = need <= 16 ? 16 : need <= 32 ? 32 : 64;
