@@ -23,8 +23,7 @@ constexpr int kBlock = 64;                   /* bytes of a row that the four lan
 constexpr int kAhead = 4;                    /* blocks that a lane loads together: 256 bytes of a row */
 constexpr uint32_t kFetchAhead = 6;          /* items of a warp that k_down_few asks for before its values are there */
 constexpr int kFew = 8, kFewMost = 32;       /* tokens that fit one instruction's columns, four ones' */
-constexpr int kChunk = 512;                  /* bytes of the tokens' rows in shared memory at a time (more tokens) */
-constexpr int kChunkRow = kChunk + 64;       /* ... rows shifted by half of the banks: eight lanes read two rows' 64 bytes */
+constexpr int kChunk = 512;                  /* bytes of the weights' rows that go with what is in shared memory at a time (more tokens) */
 
 /* ------------------------------------------------------------------------ */
 /* loads                                                                     */
@@ -99,28 +98,74 @@ template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("c
 
 __device__ __forceinline__ void multiply(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-/* One block of 16 weight rows (a lane's rows g and g + 8) with 8 tokens (the lane's: g). */
-__device__ __forceinline__ void multiply_block(float (&c)[4], const uint4 &a, const uint4 &b, const uint4 &x)
+/*
+ * binary32: a value is the sum of three bf16 ones, each the nearest to what the ones before it leave (24 bits).  Of the nine products
+ * of two values' parts the three least are left out, together 2^-25 of the product.  Values that are not finite, or that round
+ * to no finite bf16 value, give NaN.
+ */
+struct Parts { uint2 high, mid, low; };
+__device__ __forceinline__ uint32_t bf16_pair(float first, float second)
 {
-    multiply(c, a.x, b.x, a.y, b.y, x.x, x.y);
-    multiply(c, a.z, b.z, a.w, b.w, x.z, x.w);
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(second), "f"(first));
+    return r;
 }
-__device__ __forceinline__ float dot4(const uint4 &a, const float4 &x, float s)
+__device__ __forceinline__ void part(uint32_t first, uint32_t second, uint32_t &high, uint32_t &mid, uint32_t &low)
 {
-    s += __uint_as_float(a.x) * x.x; s += __uint_as_float(a.y) * x.y;
-    s += __uint_as_float(a.z) * x.z; s += __uint_as_float(a.w) * x.w;
-    return s;
+    float a = __uint_as_float(first), b = __uint_as_float(second);
+    high = bf16_pair(a, b);
+    a -= __uint_as_float(high << 16); b -= __uint_as_float(high & 0xFFFF0000u);
+    mid = bf16_pair(a, b);
+    a -= __uint_as_float(mid << 16); b -= __uint_as_float(mid & 0xFFFF0000u);
+    low = bf16_pair(a, b);
+}
+__device__ __forceinline__ Parts parts_of(const uint4 &v)
+{
+    Parts p;
+    part(v.x, v.y, p.high.x, p.mid.x, p.low.x);
+    part(v.z, v.w, p.high.y, p.mid.y, p.low.y);
+    return p;
+}
+/* A block's weights as the instructions take them. */
+template <int DT> __device__ __forceinline__ auto operand(const uint4 &v)
+{
+    if constexpr (DT == SIFAR_BF16) return v;
+    else return parts_of(v);
+}
+
+/*
+ * One block of 16 weight rows (a lane's rows g and g + 8) with 8 N tokens (the lane's: g, g + 8, ...).  An instruction waits for the one
+ * before it with the same sums: those of the N groups take turns.
+ */
+template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], const uint4 &a, const uint4 &b, const uint4 (&x)[N])
+{
+#pragma unroll
+    for (int q = 0; q < N; ++q) multiply(c[q], a.x, b.x, a.y, b.y, x[q].x, x[q].y);
+#pragma unroll
+    for (int q = 0; q < N; ++q) multiply(c[q], a.z, b.z, a.w, b.w, x[q].z, x[q].w);
+}
+template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], const Parts &a, const Parts &b, const Parts (&x)[N])
+{
+    const auto all = [&](const uint2 &a0, const uint2 &b0, uint2 Parts::*of) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) multiply(c[q], a0.x, b0.x, a0.y, b0.y, (x[q].*of).x, (x[q].*of).y);
+    };
+    all(a.low, b.low, &Parts::high);
+    all(a.high, b.high, &Parts::low);
+    all(a.mid, b.mid, &Parts::mid);
+    all(a.mid, b.mid, &Parts::high);
+    all(a.high, b.high, &Parts::mid);
+    all(a.high, b.high, &Parts::high);
 }
 
 /* ------------------------------------------------------------------------ */
 /* up to 8 G tokens                                                          */
 /* ------------------------------------------------------------------------ */
 /* A lane's accumulators for 16 rows x 8 G tokens. */
-template <int DT, int G> struct Few;
-template <int G> struct Few<SIFAR_BF16, G> {
+template <int G> struct Few {
     float c[G][4] = {};
     __device__ __forceinline__ void store(float *red) const        /* red: 16 rows x 8 G tokens */
     {
@@ -130,24 +175,6 @@ template <int G> struct Few<SIFAR_BF16, G> {
             *reinterpret_cast<float2 *>(red + g * 8 * G + q * 8 + 2 * j) = make_float2(c[q][0], c[q][1]);
             *reinterpret_cast<float2 *>(red + (g + 8) * 8 * G + q * 8 + 2 * j) = make_float2(c[q][2], c[q][3]);
         }
-    }
-};
-template <int G> struct Few<SIFAR_F32, G> {
-    float c[2][8 * G] = {};
-    __device__ __forceinline__ void store(float *red)
-    {
-        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
-        /* lane j ends with tokens j, j + 4, ...: it sends on what others keep */
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int t = 0; t < 8 * G; t += 4) {
-                const float *const v = c[r] + t;
-                const bool high = j & 2, odd = j & 1;
-                const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[2], 2);
-                const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, high ? v[1] : v[3], 2);
-                red[(g + 8 * r) * 8 * G + t + j] = (odd ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 1);
-            }
     }
 };
 
@@ -238,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
 
     int parity = 0;
     for (uint32_t p = begin; p < end; p += 8 * tiles, parity ^= 1) {
-        Few<DT, G> acc;
+        Few<G> acc;
         for (uint32_t s = 0; s < steps; ++s) {
             const Weights<VEC> now = next;
             const uint32_t at = s * span + mine;
@@ -252,25 +279,20 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
             for (int i = 0; i < kAhead; ++i) {
                 if (at - j * 16 + i * kBlock >= bytes) break;       /* the same for all lanes */
                 const int left = (int)bytes - (int)(at + i * kBlock);
-                const uint4 wa = now.of_a(i, left), wb = now.of_b(i, left);
+                const auto wa = operand<DT>(now.of_a(i, left)), wb = operand<DT>(now.of_b(i, left));
+                uint4 x[G];
+#pragma unroll
+                for (int q = 0; q < G; ++q) {
+                    x[q] = make_uint4(0u, 0u, 0u, 0u);
+                    if ((uint32_t)(q * 8 + g) < a.tokens) x[q] = *reinterpret_cast<const uint4 *>(smem + (q * 8 + g) * a.x_row + at + i * kBlock);
+                }
                 if constexpr (DT == SIFAR_BF16) {
-#pragma unroll
-                    for (int q = 0; q < G; ++q) {
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if ((uint32_t)(q * 8 + g) < a.tokens) x = *reinterpret_cast<const uint4 *>(smem + (q * 8 + g) * a.x_row + at + i * kBlock);
-                        multiply_block(acc.c[q], wa, wb, x);
-                    }
+                    multiply_block<G>(acc.c, wa, wb, x);
                 } else {
+                    Parts parts[G];
 #pragma unroll
-                    for (int q = 0; q < 2 * G; ++q) {
-                        if ((uint32_t)q * 4 >= a.tokens) break;     /* by fours: rows of no token are whatever they are */
-#pragma unroll
-                        for (int t = 4 * q; t < 4 * q + 4; ++t) {
-                            const float4 x = *reinterpret_cast<const float4 *>(smem + t * a.x_row + at + i * kBlock);
-                            acc.c[0][t] = dot4(wa, x, acc.c[0][t]);
-                            acc.c[1][t] = dot4(wb, x, acc.c[1][t]);
-                        }
-                    }
+                    for (int q = 0; q < G; ++q) parts[q] = parts_of(x[q]);
+                    multiply_block<G>(acc.c, wa, wb, parts);
                 }
             }
         }
@@ -285,16 +307,16 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
             float gate = 0.0f, up = 0.0f;
             for (uint32_t w = tile * group; w < (tile + 1) * group; ++w) { gate += s_red[parity][w][warp * 8 * G + t]; up += s_red[parity][w][(warp + 8) * 8 * G + t]; }
             const size_t low = (size_t)a.tokens * a.h_row;
-            store_h<DT>(a, a.h + which * (DT == SIFAR_BF16 ? 2 : 1) * low + t * (size_t)a.h_row, low, pair - which * a.inter,
+            store_h<DT == SIFAR_BF16 ? 2 : 0>(a, a.h + which * (DT == SIFAR_BF16 ? 2 : 1) * low + t * (size_t)a.h_row, low, pair - which * a.inter,
                         weight_of(a, t, s_list[which]) * (activate(gate, a.activation) * up));
         }
     }
 }
 
-/* What an item's values take: 256 bytes of each row; bf16 rows, eight of which are read at once, shifted by half of the banks.
+/* What an item's values take: 256 bytes of each row, eight of which are read at once, shifted by half of the banks.
    0: too much for two items of each warp, the values are read where they are used. */
 template <int DT, int G> struct Staged {
-    static constexpr int row = kAhead * kBlock + (DT == SIFAR_BF16 ? 64 : 0), bytes = DT == SIFAR_F32 ? 8 * G * row : G == 1 ? 2 * 8 * row : 0;
+    static constexpr int row = kAhead * kBlock + 64, bytes = DT == SIFAR_F32 ? 8 * G * row : G == 1 ? 2 * 8 * row : 0;
 };
 constexpr int kMaxSplit = 8;                 /* CTAs that share columns of the output */
 
@@ -373,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
         copies_commit();
     };
     for (uint32_t col = begin; col < end; col += 16) {
-        Few<DT, G> acc;
+        Few<G> acc;
         int half = 0;
         if (kStaged) fetch(warp0, 0);
         for (uint32_t item = warp0; item < items; item += turn, half ^= 1) {
@@ -392,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                 for (int i = 0; i < kAhead; ++i) {
                     if (at - j * 16 + i * kBlock >= bytes) break;
                     const int left = (int)bytes - (int)(at + i * kBlock);
-                    multiply_block(acc.c[0], now.of_a(i, left), now.of_b(i, left), x[i]);
+                    multiply_block<1>(acc.c, now.of_a(i, left), now.of_b(i, left), {x[i]});
                 }
             } else {
                 load(next, more ? col : col + 16, more ? item + turn : warp0);
@@ -407,40 +429,36 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                 if (kStaged) copies_wait<1>();
                 __syncwarp();
                 const char *const x0 = staged + half * Staged<DT, G>::bytes + j * 16;
-                if constexpr (DT == SIFAR_BF16) {
+                constexpr bool two = DT == SIFAR_BF16;
+                constexpr int N = G < 2 ? 1 : 2;                    /* groups at a time */
 #pragma unroll
-                    for (int q = 0; q < G; ++q) {
-                        if (!(tokens >> (8 * q) & 0xFFu)) continue;
-                        const uint32_t t = q * 8 + g;
-                        const char *const from = a.h + (size_t)which * 2 * low + t * (size_t)a.h_row + at;
-                        uint4 x[kAhead], y[kAhead];
+                for (int q = 0; q < G; q += N) {
+                    if (!(tokens >> (8 * q) & (N == 2 ? 0xFFFFu : 0xFFu))) continue;
 #pragma unroll
-                        for (int i = 0; i < kAhead; ++i) {
-                            x[i] = y[i] = make_uint4(0u, 0u, 0u, 0u);
+                    for (int i = 0; i < kAhead; ++i) {
+                        uint4 x[N], y[N];
+#pragma unroll
+                        for (int k = 0; k < N; ++k) {
+                            const uint32_t t = (q + k) * 8 + g;
+                            const char *const from = a.h + (size_t)which * (two ? 2 : 1) * low + t * (size_t)a.h_row + at + i * kBlock;
+                            x[k] = y[k] = make_uint4(0u, 0u, 0u, 0u);
                             if (!(tokens >> t & 1u)) continue;
                             if (kStaged) {
-                                x[i] = *reinterpret_cast<const uint4 *>(x0 + t * Staged<DT, G>::row + i * kBlock);
-                                y[i] = *reinterpret_cast<const uint4 *>(x0 + (t + 8 * G) * Staged<DT, G>::row + i * kBlock);
+                                x[k] = *reinterpret_cast<const uint4 *>(x0 + t * Staged<DT, G>::row + i * kBlock);
+                                if (two) y[k] = *reinterpret_cast<const uint4 *>(x0 + (t + 8 * G) * Staged<DT, G>::row + i * kBlock);
                             } else if (at + i * kBlock < a.h_row) {
-                                x[i] = __ldcg(reinterpret_cast<const uint4 *>(from + i * kBlock));
-                                y[i] = __ldcg(reinterpret_cast<const uint4 *>(from + low + i * kBlock));
+                                x[k] = __ldcg(reinterpret_cast<const uint4 *>(from));
+                                if (two) y[k] = __ldcg(reinterpret_cast<const uint4 *>(from + low));
                             }
                         }
+                        if constexpr (two) {
+                            multiply_block<N>(acc.c + q, wa[i], wb[i], x);
+                            multiply_block<N>(acc.c + q, wa[i], wb[i], y);
+                        } else {
+                            Parts parts[N];
 #pragma unroll
-                        for (int i = 0; i < kAhead; ++i) {
-                            multiply_block(acc.c[q], wa[i], wb[i], x[i]);
-                            multiply_block(acc.c[q], wa[i], wb[i], y[i]);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int t = 0; t < 8 * G; ++t) {
-                        if (!(tokens >> t & 1u)) continue;          /* the same for the whole warp */
-#pragma unroll
-                        for (int i = 0; i < kAhead; ++i) {
-                            const float4 x = *reinterpret_cast<const float4 *>(x0 + t * Staged<DT, G>::row + i * kBlock);
-                            acc.c[0][t] = dot4(wa[i], x, acc.c[0][t]);
-                            acc.c[1][t] = dot4(wb[i], x, acc.c[1][t]);
+                            for (int k = 0; k < N; ++k) parts[k] = parts_of(x[k]);
+                            multiply_block<N>(acc.c + q, parts_of(wa[i]), parts_of(wb[i]), parts);
                         }
                     }
                 }
@@ -486,17 +504,22 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
 /* ------------------------------------------------------------------------ */
 /* more tokens                                                               */
 /* ------------------------------------------------------------------------ */
-/* Columns of a pass over an expert's rows, and instructions' columns of eight that hold them: bf16 values of the second product
-   come as two parts, a column each.  binary32: as many as registers hold. */
+/*
+ * Parts that the tokens' values come in, all bf16; groups of eight columns; columns of a pass.  bf16: the values of the second product
+ * are two parts, in columns of their own.  binary32: three parts, one behind the other in a row.
+ * In shared memory rows are shifted: eight lanes read 64 bytes of two rows, or sixteen 32 of four.
+ */
 template <int DT, bool DOWN> struct Pass {
-    static constexpr int parts = DT == SIFAR_BF16 && DOWN ? 2 : 1;
-    static constexpr int groups = DT == SIFAR_BF16 ? 8 : 2;
-    static constexpr int tokens = groups * 8 / parts;
-    static constexpr int shared = 2 * groups * 8 * kChunkRow;
+    static constexpr int parts = DT == SIFAR_F32 ? 3 : DOWN ? 2 : 1;
+    static constexpr int groups = DT == SIFAR_F32 ? 4 : 8;
+    static constexpr int tokens = DT == SIFAR_F32 ? 32 : 64 / parts;
+    static constexpr int piece = DT == SIFAR_F32 ? kChunk / 2 : kChunk;       /* bytes of a part that go with a chunk of the weights */
+    static constexpr int row = DT == SIFAR_F32 ? 3 * piece + 32 : piece + 64;
+    static constexpr int half = groups * 8 * row, shared = 2 * half;
 };
 
 /*
- * A unit is 128 rows of one expert with up to Pass::tokens of its tokens: 64 gate and 64 up rows (UP), or 128 columns of the
+ * A unit is 128 rows of one expert with 8 up to Pass::tokens of its tokens: 64 gate and 64 up rows (UP), or 128 columns of the
  * output (DOWN).  The columns' rows come through shared memory 512 bytes at a time, the next ones under way; weights as
  * above, 256 bytes ahead.
  */
@@ -504,17 +527,41 @@ template <int DT, bool DOWN, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant__ ExpertsArgs a)
 {
     using P = Pass<DT, DOWN>;
-    constexpr int es = DT == SIFAR_BF16 ? 2 : 4, G = P::groups / P::parts;
-    extern __shared__ __align__(128) char smem[];                   /* 2 x columns x kChunkRow; at first each expert's tokens as bits */
+    constexpr int es = DT == SIFAR_BF16 ? 2 : 4, G = P::tokens / 8;
+    extern __shared__ __align__(128) char smem[];                   /* 2 x columns x Pass::row; at first each expert's tokens as bits */
     __shared__ uint16_t s_place[SIFAR_ROUTE_MAX_EXPERTS], s_list[SIFAR_ROUTE_MAX_EXPERTS], s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];
     __shared__ uint8_t s_token[SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K];
     __shared__ unsigned long long s_sum[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     if (!DOWN) grid_wait();
     grid_let_next_in();
-    const ExpertPlan plan = plan_experts<kThreads>(a, P::tokens, reinterpret_cast<uint32_t *>(smem), s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
+    const uint32_t rows = DOWN ? a.hidden : a.inter, per = DOWN ? 128u : 64u, tiles = (rows + per - 1) / per;
+    /* Columns of a pass: as many as the fullest CTA gets through soonest.  What does not depend on them takes as long as 48 columns. */
+    auto pick = [&](const auto &n) {
+        unsigned long long passes = 0;                              /* with 8, 16, 32, 64 columns, 16 bits each */
+#pragma unroll
+        for (uint32_t m : n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) passes += (unsigned long long)((m + (8u << i) - 1) >> (3 + i)) << (16 * i);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) passes += __shfl_xor_sync(0xFFFFFFFFu, passes, d);
+        if (lane == 0) s_sum[warp] = passes;
+        __syncthreads();
+        passes = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) passes += s_sum[w];
+        __syncthreads();
+        uint32_t best = 0xFFFFFFFFu, columns = P::tokens;
+#pragma unroll
+        for (int i = 3; i >= 0; --i) {
+            const uint32_t cost = ((uint32_t)(passes >> (16 * i) & 0xFFFFu) * tiles + gridDim.x - 1) / gridDim.x * (48 + (8u << i));
+            if ((8 << i) <= P::tokens && cost < best) { best = cost; columns = 8u << i; }
+        }
+        return columns;
+    };
+    const ExpertPlan plan = plan_experts<kThreads>(a, pick, reinterpret_cast<uint32_t *>(smem), s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
     __syncthreads();
-    const uint32_t rows = DOWN ? a.hidden : a.inter, per = DOWN ? 128u : 64u, tiles = (rows + per - 1) / per, units = plan.passes * tiles;
+    const uint32_t units = plan.passes * tiles;
     const uint32_t bytes = (DOWN ? a.inter : a.hidden) * es, steps = (bytes + kChunk - 1) / kChunk;
     const uint32_t begin = (uint32_t)((unsigned long long)units * blockIdx.x / gridDim.x), end = (uint32_t)((unsigned long long)units * (blockIdx.x + 1) / gridDim.x);
 
@@ -526,8 +573,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
             const int mid = (lo + hi + 1) / 2;
             if (s_passes[mid] <= pass) lo = mid; else hi = mid - 1;
         }
-        const uint32_t first = s_first[lo] + (pass - s_passes[lo]) * P::tokens;
-        return Unit{s_list[lo], u % tiles, first, min((uint32_t)P::tokens, s_first[lo + 1] - first)};
+        const uint32_t first = s_first[lo] + (pass - s_passes[lo]) * plan.columns;
+        return Unit{s_list[lo], u % tiles, first, min(plan.columns, s_first[lo + 1] - first)};
     };
     auto rows_of = [&](uint32_t u, const char *&ra, const char *&rb) {
         ra = rb = nullptr;
@@ -551,35 +598,41 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
     Weights<VEC> next;
     next.load(ra, rb, j * 16, bytes);
     if (DOWN) grid_wait();                                          /* what was loaded so far no kernel writes */
+    /* column c: token c of the pass */
+    const uint32_t part_row = DOWN ? a.h_row : ((a.hidden * 2 + 15u) & ~15u);
+    auto fetch = [&](const Unit &at, uint32_t step, int buffer) {
+        char *const to = smem + buffer * P::half;
+        for (uint32_t i = threadIdx.x; i < at.n * P::parts * (P::piece / 16); i += kThreads) {
+            const uint32_t c = i / (P::piece / 16), piece = i % (P::piece / 16) * 16, off = step * P::piece + piece;
+            const uint32_t token = c / P::parts, part = c % P::parts, in_list = at.first + token, take = off < part_row ? 16u : 0u;
+            const char *const row = DOWN ? a.h + ((size_t)in_list * P::parts + part) * a.h_row : a.x + s_token[in_list] * a.ld_x + part * part_row;
+            char *const dst = to + (DT == SIFAR_F32 ? token * P::row + part * P::piece : (part * (G * 8) + token) * P::row) + piece;
+            copy16(dst, row + (take ? off : 0u), take);
+        }
+        copies_commit();
+    };
+    Unit behind = {};
+    int buffer = 0;
+    if (begin < end) {
+        behind = unit(begin);
+        fetch(behind, 0, 0);
+    }
 
     for (uint32_t u = begin; u < end; ++u) {
-        const Unit at = unit(u);
+        const Unit at = behind;
         const uint32_t n = at.n, groups = (n + 7) / 8;
-        /* column c: token c of the pass; its second part lies G * 8 columns on */
-        auto fetch = [&](uint32_t step, int buffer) {
-            char *const to = smem + buffer * (P::groups * 8 * kChunkRow);
-            for (uint32_t i = threadIdx.x; i < n * P::parts * (kChunk / 16); i += kThreads) {
-                const uint32_t c = i / (kChunk / 16), piece = i % (kChunk / 16) * 16, off = step * kChunk + piece;
-                const uint32_t part = P::parts == 2 && c >= n ? 1 : 0, token = c - part * n, in_list = at.first + token;
-                const char *row = DOWN ? a.h + ((size_t)in_list * P::parts + part) * a.h_row : a.x + s_token[in_list] * a.ld_x;
-                char *const dst = to + (part * (G * 8) + token) * kChunkRow + piece;
-                const uint32_t end_of = DOWN ? a.h_row : (bytes + 15u) & ~15u;
-                const uint32_t take = off < end_of ? 16u : 0u;
-                copy16(dst, row + (take ? off : 0u), take);
-            }
-            copies_commit();
-        };
-        float acc[P::groups][DT == SIFAR_BF16 ? 4 : 16];
+        if (u + 1 < end) behind = unit(u + 1);
+        float acc[P::groups][4];
 #pragma unroll
         for (int q = 0; q < P::groups; ++q)
 #pragma unroll
-            for (int i = 0; i < (DT == SIFAR_BF16 ? 4 : 16); ++i) acc[q][i] = 0.0f;
-        fetch(0, 0);
-        for (uint32_t s = 0; s < steps; ++s) {
+            for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
+        for (uint32_t s = 0; s < steps; ++s, buffer ^= 1) {
             copies_wait<0>();
-            __syncthreads();                                        /* chunk s is there, chunk s - 1 has been read */
-            if (s + 1 < steps) fetch(s + 1, (s + 1) & 1);
-            const char *const cols = smem + (s & 1) * (P::groups * 8 * kChunkRow);
+            __syncthreads();                                        /* this chunk is there, the one before has been read */
+            if (s + 1 < steps) fetch(at, s + 1, buffer ^ 1);
+            else if (u + 1 < end) fetch(behind, 0, buffer ^ 1);
+            const char *const cols = smem + buffer * P::half;
 #pragma unroll 1
             for (int half = 0; half < kChunk / (kAhead * kBlock); ++half) {
                 const uint32_t off = s * kChunk + half * kAhead * kBlock;
@@ -593,33 +646,23 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     if (off + i * kBlock >= bytes) break;
-                    const char *const x = cols + half * kAhead * kBlock + i * kBlock + j * 16;
                     const int left = (int)bytes - (int)(off + i * kBlock + j * 16);
-                    const uint4 wa = now.of_a(i, left), wb = now.of_b(i, left);
-                    if constexpr (DT == SIFAR_BF16) {
+                    const auto wa = operand<DT>(now.of_a(i, left)), wb = operand<DT>(now.of_b(i, left));
+                    const char *const x = cols + (half * kAhead + i) * (P::piece / (kChunk / kBlock)) + j * (P::piece / (kChunk / 16));
+                    const auto col = [&](int q) {
+                        const char *const at = x + (q * 8 + g) * P::row;
+                        if constexpr (DT == SIFAR_BF16) return *reinterpret_cast<const uint4 *>(at);
+                        else return Parts{*reinterpret_cast<const uint2 *>(at), *reinterpret_cast<const uint2 *>(at + P::piece), *reinterpret_cast<const uint2 *>(at + 2 * P::piece)};
+                    };
 #pragma unroll
-                        for (int q = 0; q < G; ++q) {
-                            if ((uint32_t)q >= groups) break;
-                            multiply_block(acc[q], wa, wb, *reinterpret_cast<const uint4 *>(x + (q * 8 + g) * kChunkRow));
-                            if (P::parts == 2)
-                                multiply_block(acc[q + P::groups - G], wa, wb, *reinterpret_cast<const uint4 *>(x + ((q + G) * 8 + g) * kChunkRow));
-                        }
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 2 * G; ++q) {
-                            if ((uint32_t)q * 4 >= n) break;        /* by fours: columns of no token are whatever they are */
-#pragma unroll
-                            for (int t = 4 * q; t < 4 * q + 4; ++t) {
-                                const float4 v = *reinterpret_cast<const float4 *>(x + t * kChunkRow);
-                                acc[t / 8][t % 8] = dot4(wa, v, acc[t / 8][t % 8]);
-                                acc[t / 8][8 + t % 8] = dot4(wb, v, acc[t / 8][8 + t % 8]);
-                            }
-                        }
+                    for (int q = 0; q < G; q += 2) {
+                        if ((uint32_t)q >= groups) break;
+                        multiply_block<2>(acc + q, wa, wb, {col(q), col(q + 1)});
+                        if constexpr (P::parts == 2) multiply_block<2>(acc + q + G, wa, wb, {col(q + G), col(q + 1 + G)});
                     }
                 }
             }
         }
-        __syncthreads();                                            /* the last chunk has been read */
         /* rows g (first) and g + 8 (second) of the warp's 16, token t of the pass */
         auto put = [&](uint32_t t, float first, float second) {
             if (t >= n) return;
@@ -633,41 +676,47 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
                 const uint32_t r = at.tile * 64 + warp * 8 + g;
                 if (r >= a.inter) return;
                 const float v = weight_of(a, s_token[to], at.expert) * (activate(first, a.activation) * second);
-                store_h<DT>(a, a.h + to * (DT == SIFAR_BF16 ? 2 : 1) * a.h_row, a.h_row, r, v);
+                store_h<DT == SIFAR_BF16 ? 2 : 3>(a, a.h + to * (DT == SIFAR_BF16 ? 2 : 3) * a.h_row, a.h_row, r, v);
             }
         };
 #pragma unroll
         for (int q = 0; q < G; ++q) {
             if ((uint32_t)q >= groups) break;
-            if constexpr (DT == SIFAR_BF16) {
-                if (P::parts == 2) {
+            if (P::parts == 2) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[q][i] += acc[q + P::groups - G][i];
-                }
-                put(q * 8 + 2 * j, acc[q][0], acc[q][2]);
-                put(q * 8 + 2 * j + 1, acc[q][1], acc[q][3]);
-            } else {
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    float v = acc[q][t], w = acc[q][8 + t];
-                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1); w += __shfl_xor_sync(0xFFFFFFFFu, w, 1);
-                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 2); w += __shfl_xor_sync(0xFFFFFFFFu, w, 2);
-                    if (j == (t & 3)) put(q * 8 + t, v, w);
-                }
+                for (int i = 0; i < 4; ++i) acc[q][i] += acc[(q + G) % P::groups][i];
             }
+            put(q * 8 + 2 * j, acc[q][0], acc[q][2]);
+            put(q * 8 + 2 * j + 1, acc[q][1], acc[q][3]);
         }
     }
 }
 
-/* The tokens' rows once more, on 16-byte boundaries, zeros behind their ends. */
+/* The tokens' rows once more, on 16-byte boundaries, zeros behind their ends; binary32 ones as their three parts. */
 template <int DT>
 __global__ void __launch_bounds__(kThreads) k_align(const __grid_constant__ ExpertsArgs a)
 {
-    constexpr uint32_t es = DT == SIFAR_BF16 ? 2 : 4;
-    const uint32_t bytes = a.hidden * es, ld = (bytes + 15u) & ~15u, at = (blockIdx.x * kThreads + threadIdx.x) * 16;
+    const uint32_t row = (a.hidden * 2 + 15u) & ~15u, at = (blockIdx.x * kThreads + threadIdx.x) * 16;      /* of bf16 values */
     grid_wait();
     grid_let_next_in();
-    if (at < bytes) *reinterpret_cast<uint4 *>(a.rows + (size_t)blockIdx.y * ld + at) = load_shifted(a.x + blockIdx.y * a.ld_x + at, bytes - at);
+    if (at >= row) return;
+    const char *const x = a.x + blockIdx.y * a.ld_x;
+    char *const to = a.rows + (size_t)blockIdx.y * (DT == SIFAR_F32 ? 3 : 1) * row + at;
+    if constexpr (DT == SIFAR_BF16) {
+        *reinterpret_cast<uint4 *>(to) = load_shifted(x + at, a.hidden * 2 - at);
+    } else {
+        uint4 v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t c = at / 2 + 4 * i;
+            const auto get = [&](uint32_t col) { return col < a.hidden ? __ldg(reinterpret_cast<const uint32_t *>(x) + col) : 0u; };
+            v[i] = make_uint4(get(c), get(c + 1), get(c + 2), get(c + 3));
+        }
+        const Parts p = parts_of(v[0]), q = parts_of(v[1]);
+        *reinterpret_cast<uint4 *>(to) = make_uint4(p.high.x, p.high.y, q.high.x, q.high.y);
+        *reinterpret_cast<uint4 *>(to + row) = make_uint4(p.mid.x, p.mid.y, q.mid.x, q.mid.y);
+        *reinterpret_cast<uint4 *>(to + 2 * row) = make_uint4(p.low.x, p.low.y, q.low.x, q.low.y);
+    }
 }
 
 /* out_t = the sum over its choices here, in their order; a second choice of the same expert has its share in the first. */
@@ -730,11 +779,13 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     p.x_row = (uint32_t)((g->hidden * es + 127) / 128 * 128 + 64);
     const bool tiles = g->dtype == SIFAR_BF16 && g->hidden % 8 == 0 && g->inter % 8 == 0;      /* as far as the sizes go */
     p.few = T <= (size_t)(tiles ? kFew : kFewMost) && (T + 3) / 4 * 4 * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);
-    p.h_row = (uint32_t)((g->inter * es + 15) / 16 * 16);
+    /* binary32: a few tokens' products as they are, else three bf16 parts */
+    const size_t h_parts = parts == 2 ? 2 : p.few ? 1 : 3, row2 = (g->hidden * 2 + 15) / 16 * 16;
+    p.h_row = (uint32_t)((g->inter * (h_parts == 1 ? 4 : 2) + 15) / 16 * 16);
     const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
-    p.h_bytes = ((p.few ? most * T : choices) * parts * p.h_row + 15) / 16 * 16;
+    p.h_bytes = ((p.few ? most * T : choices) * h_parts * p.h_row + 15) / 16 * 16;
     p.y_bytes = p.few ? 0 : (choices * g->hidden * sizeof(float) + 15) / 16 * 16;
-    p.rows_bytes = p.few ? 0 : T * ((g->hidden * es + 15) / 16 * 16);
+    p.rows_bytes = p.few ? 0 : T * (parts == 2 ? 1 : 3) * row2;
     p.bytes = p.h_bytes + p.y_bytes + p.rows_bytes + (p.few ? 0 : choices * sizeof(int));
     return SIFAR_OK;
 }
@@ -782,10 +833,11 @@ static cudaError_t launch_experts(const ExpertsPlan &p, bool gu_vec, bool dn_vec
         if (a.tokens <= 8) return launch_few<DT, 1>(p, gu_vec, dn_vec, x_vec, stream, a);
         return a.tokens <= 16 ? launch_few<DT, 2>(p, gu_vec, dn_vec, x_vec, stream, a) : launch_few<DT, 4>(p, gu_vec, dn_vec, x_vec, stream, a);
     }
-    if (!x_vec) {                            /* the products below take the tokens' rows in whole pieces */
-        ExpertsArgs rows = a;
-        a.x = a.rows; a.ld_x = (a.hidden * elem_size(DT) + 15) / 16 * 16;
-        e = launch_shared(k_align<DT>, dim3((unsigned)((a.ld_x / 16 + kThreads - 1) / kThreads), a.tokens), 0, stream, rows);
+    if (DT == SIFAR_F32 || !x_vec) {         /* the products below take the tokens' rows in whole pieces of bf16 values */
+        const ExpertsArgs rows = a;
+        const unsigned row = (a.hidden * 2 + 15) / 16 * 16;
+        a.x = a.rows; a.ld_x = (DT == SIFAR_F32 ? 3 : 1) * row;
+        e = launch_shared(k_align<DT>, dim3((row / 16 + kThreads - 1) / kThreads, a.tokens), 0, stream, rows);
         if (e) return e;
     }
     if (DT == SIFAR_BF16 && gu_vec && dn_vec) {

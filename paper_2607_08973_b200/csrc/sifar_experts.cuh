@@ -68,19 +68,23 @@ __device__ __forceinline__ float activate(float g, int kind)
     return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
 }
 
-/* Element `col` of a row of h (and, bf16, of the row with its rest, `low` bytes on).  The last one is followed by zeros up to
-   the row's end: the second product reads whole vectors. */
-template <int DT> __device__ __forceinline__ void store_h(const ExpertsArgs &a, char *row, size_t low, uint32_t col, float v)
+/* Element `col` of a row of h: as it is (PARTS 0), or as so many bf16 values, each the nearest to what the ones before leave, in rows
+   `low` bytes apart.  The last one is followed by zeros up to the row's end: the second product reads whole vectors. */
+template <int PARTS> __device__ __forceinline__ void store_h(const ExpertsArgs &a, char *row, size_t low, uint32_t col, float v)
 {
-    using T = typename Elem<DT>::type;
-    const T hi = narrow<DT>(v);
-    reinterpret_cast<T *>(row)[col] = hi;
-    if constexpr (DT == SIFAR_BF16) reinterpret_cast<T *>(row + low)[col] = narrow<DT>(v - widen<DT>(hi));
-    if (col + 1 == a.inter)
-        for (uint32_t i = a.inter; i < a.h_row / sizeof(T); ++i) {
-            reinterpret_cast<T *>(row)[i] = (T)0;
-            if constexpr (DT == SIFAR_BF16) reinterpret_cast<T *>(row + low)[i] = (T)0;
+    using T = typename Elem<PARTS ? SIFAR_BF16 : SIFAR_F32>::type;
+    const uint32_t last = col + 1 == a.inter ? a.h_row / (uint32_t)sizeof(T) : 0u;
+#pragma unroll
+    for (int p = 0; p < (PARTS ? PARTS : 1); ++p) {
+        T *const to = reinterpret_cast<T *>(row + p * low);
+        if constexpr (PARTS) {
+            to[col] = narrow<SIFAR_BF16>(v);
+            v -= widen<SIFAR_BF16>(narrow<SIFAR_BF16>(v));
+        } else {
+            to[col] = narrow<SIFAR_F32>(v);
         }
+        for (uint32_t i = a.inter; i < last; ++i) to[i] = (T)0;
+    }
 }
 
 /* ------------------------------------------------------------------------ */
@@ -139,15 +143,16 @@ __device__ __forceinline__ int keep_in_order(uint32_t n, int *scratch, On on, Pu
 
 /* What a CTA works out of the choices: experts that have tokens (list), where each one's tokens begin in the list by experts (first, and
    place by the expert's number), passes of `columns` tokens before each (passes), the tokens by expert in their order (token). */
-struct ExpertPlan { int active; uint32_t passes; };
+struct ExpertPlan { int active; uint32_t passes, columns; };
 
 /*
  * A bit per expert and token that chose it (twice: once): an expert's tokens are counted and numbered by bits, in the same order in
- * every CTA.  bits: experts x (tokens / 32) words, sum: a word per warp.  `tell`: this CTA writes the places for the sum over a
- * token's choices.  All of the CTA; the barrier behind it is the caller's.
+ * every CTA.  bits: experts x (tokens / 32) words, sum: a word per warp.  pick(n): the columns of a pass, the same for all threads;
+ * n: the tokens of the thread's experts.  `tell`: this CTA writes the places for the sum over a token's choices.  All of the
+ * CTA; the barrier behind it is the caller's.
  */
-template <int THREADS>
-__device__ __forceinline__ ExpertPlan plan_experts(const ExpertsArgs &a, uint32_t columns, uint32_t *bits, unsigned long long *sum, uint16_t *place, uint16_t *list,
+template <int THREADS, typename Pick>
+__device__ __forceinline__ ExpertPlan plan_experts(const ExpertsArgs &a, Pick pick, uint32_t *bits, unsigned long long *sum, uint16_t *place, uint16_t *list,
                                                    uint16_t *first, uint16_t *passes, uint8_t *token, bool tell)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
@@ -169,8 +174,11 @@ __device__ __forceinline__ ExpertPlan plan_experts(const ExpertsArgs &a, uint32_
         n[i] = 0;
         if (e < a.experts)
             for (uint32_t w = 0; w < words; ++w) n[i] += __popc(bits[e * words + w]);
-        mine += (unsigned long long)(n[i] ? 1u : 0u) << 40 | (unsigned long long)n[i] << 20 | (n[i] + columns - 1) / columns;
     }
+    const uint32_t columns = pick(n);
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i)
+        mine += (unsigned long long)(n[i] ? 1u : 0u) << 40 | (unsigned long long)n[i] << 20 | (n[i] + columns - 1) / columns;
     unsigned long long upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -194,7 +202,7 @@ __device__ __forceinline__ ExpertPlan plan_experts(const ExpertsArgs &a, uint32_
         passes[at] = (uint16_t)(before & 0xFFFFFu);
         before += 1ull << 40 | (unsigned long long)n[i] << 20 | (n[i] + columns - 1) / columns;
     }
-    const ExpertPlan plan{(int)(all >> 40), (uint32_t)(all & 0xFFFFFu)};
+    const ExpertPlan plan{(int)(all >> 40), (uint32_t)(all & 0xFFFFFu), columns};
     if (threadIdx.x == 0) {
         first[plan.active] = (uint16_t)((all >> 20) & 0xFFFFFu);
         passes[plan.active] = (uint16_t)plan.passes;

@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    const ExpertPlan plan = plan_experts<kTileThreads>(a, ta.columns, s_bits, s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
+    const ExpertPlan plan = plan_experts<kTileThreads>(a, [&](const auto &) { return ta.columns; }, s_bits, s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
     sums_after();                                                   /* the address of tensor memory */
     const int active = plan.active;
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    /* what was read and written where the ring is now */
