@@ -7,7 +7,7 @@
  * over k is free, so the eight elements become two instructions' fragments as they lie, with the tokens' taken from the same
  * places.  No weight passes through shared memory.
  *
- *   k_up_few, k_down_few     up to 8 tokens; up to 32 where sifar_experts_tiles.cu does not take them.  All tokens are columns for
+ *   k_up_few, k_down_few     up to 8 tokens; up to 16 or 32 where sifar_experts_tiles.cu does not take them.  All tokens are columns for
  *                            every expert, the warps of a CTA share the rows' length.
  *   k_products<UP / DOWN>    more of those: an expert's tokens are gathered to columns, each warp has 16 rows of its own.
  *   k_gather                 ... and the sum over a token's choices, in their order.
@@ -778,11 +778,16 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     /* a multiple of 128 bytes and 64 more: two rows' pieces lie in different banks */
     p.x_row = (uint32_t)((g->hidden * es + 127) / 128 * 128 + 64);
     const bool tiles = g->dtype == SIFAR_BF16 && g->hidden % 8 == 0 && g->inter % 8 == 0;      /* as far as the sizes go */
-    p.few = T <= (size_t)(tiles ? kFew : kFewMost) && (T + 3) / 4 * 4 * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);
+    const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
+    /* Up to 16 tokens every expert may as well take them all as columns (binary32, 12 tokens, 32 experts of 1024 x 512: 54 us, 60 with each
+       expert's own); up to 32 where the experts' own would leave SMs without rows (20 tokens, 8 experts of 173 x 701: 36 us, 53), but
+       not where they don't (31 tokens, 64 experts of 512 x 1000: 199 us, 102; bf16, 1022 x 1000: 177 us, 125). */
+    const bool all_sms = most * ((g->hidden + 127) / 128) >= kSms && most * ((g->inter + 63) / 64) >= kSms;
+    const size_t limit = tiles ? kFew : all_sms ? kFewMost / 2 : kFewMost;
+    p.few = T <= limit && (T + 3) / 4 * 4 * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);
     /* binary32: a few tokens' products as they are, else three bf16 parts */
     const size_t h_parts = parts == 2 ? 2 : p.few ? 1 : 3, row2 = (g->hidden * 2 + 15) / 16 * 16;
     p.h_row = (uint32_t)((g->inter * (h_parts == 1 ? 4 : 2) + 15) / 16 * 16);
-    const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
     p.h_bytes = ((p.few ? most * T : choices) * h_parts * p.h_row + 15) / 16 * 16;
     p.y_bytes = p.few ? 0 : (choices * g->hidden * sizeof(float) + 15) / 16 * 16;
     p.rows_bytes = p.few ? 0 : T * (parts == 2 ? 1 : 3) * row2;

@@ -90,7 +90,7 @@ class Moe:
         want, err = dr.experts(ref.f64(self.x), self.idx, ref.f64(self.w), ref.f64(self.gu), ref.f64(self.dn), self.first, self.gelu, self.dtype)
         why = ref.outside(got, want, err, DT[self.dtype])
         assert why == "", why
-        here = ((self.idx >= self.first) & (self.idx < self.first + self.E)).any(1)
+        here = ((self.idx >= self.first) & (self.idx.long() < self.first + self.E)).any(1)
         assert not bool(got.cpu()[~here].any())
         assert bool((self.out[:, self.H:] == 9.0).all()) and bool((self.out_store[: self.off] == 9.0).all()) and bool((self.out_store[self.off + self.out.numel():] == 9.0).all())
         assert bool((self.ws[-64:] == 0xFF).all())
@@ -229,3 +229,55 @@ def test_calls_repeat_bit_for_bit_whatever_the_workspace_held(dtype, T):
         m.ws.fill_(fill)
         m.out.fill_(3.0)
         assert torch.equal(first, m.run())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("T,E,k", [(9, 4, 2), (16, 40, 3), (17, 4, 2), (20, 160, 4), (31, 40, 8), (32, 2, 2), (33, 40, 3), (100, 3, 3), (256, 200, 8)])
+@pytest.mark.parametrize("H,I", [(95, 161), (520, 20), (200, 520), (64, 130)])
+def test_more_tokens_of_sizes_that_are_not_whole_pieces(dtype, T, E, k, H, I):  # noqa: E741
+    Moe(T, H, I, E, k, dtype=dtype, seed=T + H).check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("T", [12, 24, 60, 150])
+@pytest.mark.parametrize("pad,off", [(8, 0), (1, 0), (0, 3), (5, 1)])
+def test_only_the_tokens_rows_start_anywhere(dtype, T, pad, off):
+    m = Moe(T, 264, 72, 12, 3, dtype=dtype, seed=T)
+    store = torch.full((T * (264 + pad) + off,), math.nan, dtype=DT[dtype], device="cuda")
+    x = store[off:].view(T, 264 + pad)
+    x[:, :264] = m.x.cuda()
+    m.args.x, m.args.ld_x = x.data_ptr(), 264 + pad
+    m.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("T", [4, 12, 40, 200])
+def test_all_tokens_of_few_units_choose_the_same(dtype, T):
+    """A hot expert among others: more passes over few rows than columns of one pass."""
+    Moe(T, 96, 40, 30, 3, dtype=dtype, choice=[[7, t % 30, (t * 7 + 1) % 30] for t in range(T)], seed=T).check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("T", [3, 20, 50])
+def test_numbers_of_experts_at_the_ends_of_the_range(dtype, T):
+    """A rank whose first expert is the last number that there is, and choices at the other end."""
+    first, low = 2 ** 31 - 2, -2 ** 31
+    m = Moe(T, 64, 24, 2, 3, dtype=dtype, first=first, choice=[[first + t % 2, low, [first, low, -1, 0][t % 4]] for t in range(T)], seed=T)
+    m.check()
+
+
+@gpu
+@pytest.mark.parametrize("T", [5, 14, 40])
+def test_binary32_values_of_every_size(T):
+    """Values whose parts span the exponents: 2^-40 .. 2^40 in a token, and their products' sums."""
+    m = Moe(T, 77, 33, 6, 2, dtype=sf.F32, seed=T)
+    scale = torch.ldexp(torch.ones(77), torch.arange(77) % 9 * 10 - 40)
+    m.x = (m.x * scale).float()
+    m.xd[:, :77] = m.x.cuda()
+    m.gu = (m.gu / scale).float()
+    m.gud[:, :77] = m.gu.reshape(-1, 77).cuda()
+    m.check()
