@@ -550,7 +550,7 @@ enum { SIFAR_CACHE_MAX_HEAD_DIM = 256 };
  *     a' = a * cos(angle) - b * sin(angle)
  *     b' = a * sin(angle) + b * cos(angle)
  * in binary32, rounded once; elements from rotary_dim on, and values, are copied.  A token with a negative position or
- * with a sequence outside 0 .. sequences - 1 is padding: nothing of it is read or written.  One whose page is not there
+ * with a sequence outside 0 .. sequences - 1 is padding: nothing of it is written.  One whose page is not there
  * has its query turned and is not kept.  Where two tokens of a call have the same place, it holds elements of both.
  */
 typedef struct {
@@ -574,7 +574,8 @@ int sifar_cache_append(const sifar_cache_append_args *args, void *stream);
  * Attention of one new token per sequence over the cache.  Query head h reads key head h / (heads / kv_heads).  With n =
  * lengths[s] (the new token, already in the cache, included), over the tokens j of [max(0, n - window), n) (window 0: all n)
  *     x_j = scale * q . k_j;   out = sum_j exp(x_j) v_j / sum_j exp(x_j);   lse = log(sum_j exp(x_j))
- * in binary32, out rounded once.  Tokens beyond max_pages * page_size and tokens whose page is not there are left out, as
+ * in binary32, out rounded once; bf16 takes each exponential as the sum of two bf16 values (16 bits), so that an infinite value
+ * in v may give NaN.  Tokens beyond max_pages * page_size and tokens whose page is not there are left out, as
  * if masked; a negative length is 0.  Masked tokens are not read.  A head without a score above -infinity gives
  * 0 and lse = -infinity.
  * The cache is read once for all query heads of a key head up to 16 of them (binary32: 8); more heads read it again.
@@ -604,10 +605,11 @@ int sifar_decode_attention(const sifar_decode_attention_args *args, void *stream
  * 0 .. experts - 1 (other choices are another rank's, and those that sifar_route_backward calls dropped):
  *     a_j = weights[t][j] * act(gate_e x_t) * (up_e x_t);     out_t = sum_j down_e a_j
  * with sums in binary32 and in an order of their own; the bf16 products take a_j as the sum of two bf16 values (16 bits),
- * out is rounded once.  act is x / (1 + exp(-x)) or x * (1 + erf(x / sqrt 2)) / 2.  An expert that a token has chosen
+ * the binary32 ones every value as the sum of three (a product is off by at most 2^-25 of it), out is rounded once.  Where
+ * infinite values or weights count, or binary32 ones that round to no finite bf16 value, the elements that they reach may be NaN.  act is x / (1 + exp(-x)) or x * (1 + erf(x / sqrt 2)) / 2.  An expert that a token has chosen
  * twice counts with both weights.  A token without a choice here gives 0.  `out` is one rank's partial of the all-reduce
  * behind the layer: it may lie in the buffer that sifar_rank_buffer returned.
- * Each chosen expert's weights are read once for up to 64 of its tokens.
+ * A chosen expert's weights are read once for as many of its tokens as a pass takes, 8 to 64 by the sizes, and all of them up to 8.
  */
 enum { SIFAR_ACT_SILU = 0, SIFAR_ACT_GELU = 1 };
 enum { SIFAR_EXPERTS_MAX_TOKENS = 256, SIFAR_EXPERTS_MAX_COLS = 32768 };

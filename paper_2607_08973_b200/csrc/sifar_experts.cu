@@ -10,9 +10,16 @@
  *   k_up_few, k_down_few     up to 8 tokens; up to 16 or 32 where sifar_experts_tiles.cu does not take them.  All tokens are columns for
  *                            every expert, the warps of a CTA share the rows' length.
  *   k_products<UP / DOWN>    more of those: an expert's tokens are gathered to columns, each warp has 16 rows of its own.
+ *   k_align                  ... the tokens' rows for those and for the tiles, on whole pieces.
  *   k_gather                 ... and the sum over a token's choices, in their order.
  *
- * bf16: what goes into the second product is kept as two bf16 values, the rounded one and what it leaves (16 bits).
+ * bf16: what goes into the second product is kept as two bf16 values, the rounded one and what it leaves (16 bits).  binary32 values are
+ * three bf16 ones, six instructions for one: as fused multiply-adds the same work was bound by loads from shared memory (83 tokens,
+ * 8 experts of 625 x 1216: 239 us, 119 now; 31 tokens, 64 experts: 199, 102).
+ *
+ * One bf16 token with 8 of 128 experts of 768 x 4096 takes 34 us, 4.5 TB/s (151 MB): two starts of 3 to 4 us each, in which the lists are made and
+ * the first weights come, the rest at 6 TB/s.  13 binary32 tokens, 7 experts of 333 x 1001 whose rows start anywhere: 31 us for
+ * 28 MB, bound by the starts and by the shuffles that put rows together.
  */
 #include "sifar_experts.cuh"
 
