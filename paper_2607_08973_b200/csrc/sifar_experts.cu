@@ -154,29 +154,37 @@ template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], c
 #pragma unroll
     for (int q = 0; q < N; ++q) multiply(c[q], a.z, b.z, a.w, b.w, x[q].z, x[q].w);
 }
-template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], const Parts &a, const Parts &b, const Parts (&x)[N])
+/* The instructions cut their sums off, so the large products have sums of their own, which few instructions add to; the others' sums
+   (less) are small enough for that not to count. */
+template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], float (*less)[4], const Parts &a, const Parts &b, const Parts (&x)[N])
 {
-    const auto all = [&](const uint2 &a0, const uint2 &b0, uint2 Parts::*of) {
+    const auto all = [&](float (*to)[4], const uint2 &a0, const uint2 &b0, uint2 Parts::*of) {
 #pragma unroll
-        for (int q = 0; q < N; ++q) multiply(c[q], a0.x, b0.x, a0.y, b0.y, (x[q].*of).x, (x[q].*of).y);
+        for (int q = 0; q < N; ++q) multiply(to[q], a0.x, b0.x, a0.y, b0.y, (x[q].*of).x, (x[q].*of).y);
     };
-    all(a.low, b.low, &Parts::high);
-    all(a.high, b.high, &Parts::low);
-    all(a.mid, b.mid, &Parts::mid);
-    all(a.mid, b.mid, &Parts::high);
-    all(a.high, b.high, &Parts::mid);
-    all(a.high, b.high, &Parts::high);
+    all(less, a.low, b.low, &Parts::high);
+    all(less, a.high, b.high, &Parts::low);
+    all(less, a.mid, b.mid, &Parts::mid);
+    all(less, a.mid, b.mid, &Parts::high);
+    all(less, a.high, b.high, &Parts::mid);
+    all(c, a.high, b.high, &Parts::high);
 }
 
 /* ------------------------------------------------------------------------ */
 /* up to 8 G tokens                                                          */
 /* ------------------------------------------------------------------------ */
 /* A lane's accumulators for 16 rows x 8 G tokens. */
-template <int G> struct Few {
-    float c[G][4] = {};
-    __device__ __forceinline__ void store(float *red) const        /* red: 16 rows x 8 G tokens */
+template <int DT, int G> struct Few {
+    float c[G][4] = {}, less[DT == SIFAR_F32 ? G : 1][4] = {};
+    __device__ __forceinline__ void store(float *red)              /* red: 16 rows x 8 G tokens */
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
+        if constexpr (DT == SIFAR_F32) {
+#pragma unroll
+            for (int q = 0; q < G; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[q][i] += less[q][i];
+        }
 #pragma unroll
         for (int q = 0; q < G; ++q) {
             *reinterpret_cast<float2 *>(red + g * 8 * G + q * 8 + 2 * j) = make_float2(c[q][0], c[q][1]);
@@ -272,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
 
     int parity = 0;
     for (uint32_t p = begin; p < end; p += 8 * tiles, parity ^= 1) {
-        Few<G> acc;
+        Few<DT, G> acc;
         for (uint32_t s = 0; s < steps; ++s) {
             const Weights<VEC> now = next;
             const uint32_t at = s * span + mine;
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
                     Parts parts[G];
 #pragma unroll
                     for (int q = 0; q < G; ++q) parts[q] = parts_of(x[q]);
-                    multiply_block<G>(acc.c, wa, wb, parts);
+                    multiply_block<G>(acc.c, acc.less, wa, wb, parts);
                 }
             }
         }
@@ -402,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
         copies_commit();
     };
     for (uint32_t col = begin; col < end; col += 16) {
-        Few<G> acc;
+        Few<DT, G> acc;
         int half = 0;
         if (kStaged) fetch(warp0, 0);
         for (uint32_t item = warp0; item < items; item += turn, half ^= 1) {
@@ -465,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                             Parts parts[N];
 #pragma unroll
                             for (int k = 0; k < N; ++k) parts[k] = parts_of(x[k]);
-                            multiply_block<N>(acc.c + q, parts_of(wa[i]), parts_of(wb[i]), parts);
+                            multiply_block<N>(acc.c + q, acc.less + q, parts_of(wa[i]), parts_of(wb[i]), parts);
                         }
                     }
                 }
@@ -629,11 +637,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
         const Unit at = behind;
         const uint32_t n = at.n, groups = (n + 7) / 8;
         if (u + 1 < end) behind = unit(u + 1);
-        float acc[P::groups][4];
-#pragma unroll
-        for (int q = 0; q < P::groups; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
+        float acc[P::groups][4] = {}, less[DT == SIFAR_F32 ? P::groups : 1][4] = {};
         for (uint32_t s = 0; s < steps; ++s, buffer ^= 1) {
             copies_wait<0>();
             __syncthreads();                                        /* this chunk is there, the one before has been read */
@@ -664,7 +668,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
 #pragma unroll
                     for (int q = 0; q < G; q += 2) {
                         if ((uint32_t)q >= groups) break;
-                        multiply_block<2>(acc + q, wa, wb, {col(q), col(q + 1)});
+                        if constexpr (DT == SIFAR_F32) multiply_block<2>(acc + q, less + q, wa, wb, {col(q), col(q + 1)});
+                        else multiply_block<2>(acc + q, wa, wb, {col(q), col(q + 1)});
                         if constexpr (P::parts == 2) multiply_block<2>(acc + q + G, wa, wb, {col(q + G), col(q + 1 + G)});
                     }
                 }
@@ -689,6 +694,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_products(const __grid_constant_
 #pragma unroll
         for (int q = 0; q < G; ++q) {
             if ((uint32_t)q >= groups) break;
+            if constexpr (DT == SIFAR_F32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[q][i] += less[q][i];
+            }
             if (P::parts == 2) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[q][i] += acc[(q + G) % P::groups][i];

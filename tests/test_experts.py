@@ -281,3 +281,10 @@ def test_binary32_values_of_every_size(T):
     m.gu = (m.gu / scale).float()
     m.gud[:, :77] = m.gu.reshape(-1, 77).cuda()
     m.check()
+
+
+@gpu
+@pytest.mark.parametrize("T,H", [(8, 2912), (8, 2944), (16, 2848), (16, 2880), (32, 1408), (32, 1440)])
+def test_the_longest_rows_that_a_few_tokens_keep_in_shared_memory(T, H):  # noqa: E741
+    """binary32, next to both sides of what fits."""
+    Moe(T, H, 24, 2, 2, dtype=sf.F32, seed=T).check()
