@@ -18,7 +18,7 @@
  * 8 experts of 625 x 1216: 239 us, 119 now; 31 tokens, 64 experts: 199, 102).
  *
  * One bf16 token with 8 of 128 experts of 768 x 4096 takes 34 us, 4.5 TB/s (151 MB): two starts of 3 to 4 us each, in which the lists are made and
- * the first weights come, the rest at 6 TB/s.  13 binary32 tokens, 7 experts of 333 x 1001 whose rows start anywhere: 31 us for
+ * the first weights come, the rest at 6 TB/s.  13 binary32 tokens, 7 experts of 333 x 1001 whose rows start anywhere: 33 us for
  * 28 MB, bound by the starts and by the shuffles that put rows together.
  */
 #include "sifar_experts.cuh"
