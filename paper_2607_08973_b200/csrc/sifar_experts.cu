@@ -358,6 +358,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
     __shared__ __align__(16) float s_red[kWarps][16 * 8 * G], s_part[kMaxSplit][16 * 8 * G];
     extern __shared__ __align__(128) char smem[];                   /* not HALF: each warp's two items' values */
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
+    if (a.split > 1) cluster_arrive();                              /* a CTA's shared memory may be written once it has started */
     /* the choices were complete before the kernel in front of this one let it in, so they may be read before it ends */
     const int active = list_few(a, s_list, s_tokens, s_bits, s_scratch);
     const uint32_t bytes = a.inter * es, pieces = (bytes + kAhead * kBlock - 1) / (kAhead * kBlock), items = (uint32_t)active * pieces;
@@ -384,6 +385,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
     }
     grid_wait();
     grid_let_next_in();
+    if (split > 1) cluster_wait();
     const size_t low = (size_t)a.tokens * a.h_row;
     /* the values that go with an item, two rows at a time (bf16: a token's parts, the second ones 8 G rows on), zeros behind their ends */
     constexpr bool kStaged = !HALF && Staged<DT, G>::bytes > 0;
