@@ -100,7 +100,10 @@ __global__ void __launch_bounds__(512, 3) k_append(const __grid_constant__ Appen
         if (vfirst < values) copy16(slot(2 * B), v + (size_t)vfirst * a.dim * es);
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    if (position < 0 || sequence >= a.sequences) return;
+    if (position < 0 || sequence >= a.sequences) {
+        if constexpr (V > 1) asm volatile("cp.async.wait_group 0;" ::: "memory");        /* nothing may arrive in a CTA that is gone */
+        return;
+    }
     const long long at = token_offset(a.pages, a.pages.table + sequence * a.pages.ld_table, (uint32_t)position);
     auto target = [&](uint32_t h) { return h < a.heads ? q_out + (size_t)h * a.dim * es : at < 0 ? nullptr : a.k_cache + at + (h - a.heads) * a.pages.stride_head; };
 
