@@ -61,6 +61,8 @@
  *   SIFAR_BARRIER_EARLY     1 = the loads of a BARRIER_ONESHOT reducer may start early as well (they are ordered by
  *                           its arrival flags); off by default, the baseline keeps the conventional stream order
  *                           (read when the library is loaded)
+ *   SIFAR_EXPERTS_POLLS     how often a warp of sifar_experts' larger bf16 products looks for the next tile before it gives up
+ *                           (4194304, about 0.1 s; read at the first such call)
  *   SIFAR_SWEEP             0 = contexts start with SIFAR_SWEEP_NEVER (see sifar_debug_sweep_policy; read when
  *                           the library is loaded)
  *
@@ -609,6 +611,8 @@ int sifar_decode_attention(const sifar_decode_attention_args *args, void *stream
  * infinite values or weights count, or binary32 ones that round to no finite bf16 value, the elements that they reach may be NaN.  act is x / (1 + exp(-x)) or x * (1 + erf(x / sqrt 2)) / 2.  An expert that a token has chosen
  * twice counts with both weights.  A token without a choice here gives 0.  `out` is one rank's partial of the all-reduce
  * behind the layer: it may lie in the buffer that sifar_rank_buffer returned.
+ * A wait within the kernels that takes longer than SIFAR_EXPERTS_POLLS looks (which nothing but a fault of the GPU is known to cause) gives NaN in
+ * the elements that it was for; no others are touched, and the call and those behind it run to their ends.
  * A chosen expert's weights are read once for as many of its tokens as a pass takes, 8 to 64 by the sizes, and all of them up to 8.
  */
 enum { SIFAR_ACT_SILU = 0, SIFAR_ACT_GELU = 1 };

@@ -18,6 +18,8 @@
  * First product: a tile is 128 gate rows and the 128 up rows that go with them, two accumulators; a thread then has both values of
  * its row.  Second product: the values come as two bf16 parts, and both go into one accumulator.
  */
+#include <cstdlib>
+
 #include <cuda.h>
 
 #include "sifar_experts.cuh"
@@ -33,7 +35,7 @@ constexpr int kMaxRing = 8;
 constexpr int kTileWarps = 12, kTileThreads = 32 * kTileWarps, kDrainers = 8;
 constexpr int kGatherers = 64;               /* threads that gather the tokens' rows */
 constexpr int kLag = 3;                      /* stages that they have under way while they fill another: less than a ring has */
-constexpr uint32_t kPolls = 1u << 22;        /* a wait's limit: about 0.1 s, where the products take less than a microsecond */
+constexpr uint32_t kPolls = 1u << 22;        /* a wait's limit unless the environment has another: about 0.1 s, where the products take less than a microsecond */
 
 template <bool DOWN> struct Tile {
     static constexpr int halves = DOWN ? 1 : 2;                  /* blocks of kRows weight rows */
@@ -43,6 +45,7 @@ template <bool DOWN> struct Tile {
 struct TilesArgs {
     ExpertsArgs e;
     uint32_t columns;                        /* of a pass over an expert's rows */
+    uint32_t polls;                          /* limit of a wait */
 };
 
 __device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -84,16 +87,25 @@ __device__ __forceinline__ void bar_arrive_and_expect(uint32_t leader, uint32_t 
 {
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" :: "r"(bar), "r"(bytes), "r"(leader) : "memory");
 }
-/* Waits until the barrier's phase `parity` is over.  `fine` turns false where that takes too long; nothing is waited for after that. */
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, bool &fine)
+/*
+ * Whether the barrier's phase `parity` is over, the same for the whole warp; false where that takes too long.  A warp whose wait has
+ * run out neither fills stages nor tells a barrier of anything any more, so the waits of those that depend on it run out too, and
+ * what a barrier has told of is right.  The warps that take sums out leave NaN from then on.
+ * UNIFORM: the answer comes by a shuffle from one lane, so that the compiler sees that it is the same for all and keeps what the
+ * instructions behind it need in uniform registers (where it does not: 64 tokens 265 us, quarter 169).
+ */
+template <bool UNIFORM = false>
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t polls)
 {
-    for (uint32_t i = 0; fine; ++i) {
+    uint32_t i = 0;
+    int all;
+    do {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return;
-        if (i == kPolls) fine = false;
-    }
+        all = __all_sync(0xFFFFFFFFu, done);
+    } while (!all && i++ < polls);
+    return UNIFORM ? __shfl_sync(0xFFFFFFFFu, all, 0) : all;
 }
 
 /* The map's number of rows x 64 elements from (column, row) on. */
@@ -133,8 +145,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
     __shared__ uint16_t s_first[SIFAR_ROUTE_MAX_EXPERTS + 1], s_passes[SIFAR_ROUTE_MAX_EXPERTS + 1];   /* tokens of the list, passes before each */
     __shared__ uint8_t s_token[SIFAR_EXPERTS_MAX_TOKENS * SIFAR_ROUTE_MAX_TOP_K];      /* the tokens by expert, in their order */
     __shared__ unsigned long long s_sum[kTileWarps];
-    __shared__ __align__(8) unsigned long long s_full[kMaxRing], s_empty[kMaxRing], s_sums[2], s_free[2];
-    __shared__ uint32_t s_tmem;
+    __shared__ __align__(8) unsigned long long s_full[kMaxRing], s_empty[kMaxRing], s_sums[2], s_free[2], s_done;
+    __shared__ uint32_t s_tmem, s_told[kGatherers / 32];
     __shared__ __align__(16) float s_weight[kDrainers][32];         /* of a tile's tokens, each warp's half */
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
     uint32_t *const s_bits = reinterpret_cast<uint32_t *>(smem);
@@ -156,6 +168,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             bar_init(shared_at(&s_sums[i]), 1);
             bar_init(shared_at(&s_free[i]), kDrainers);
         }
+        bar_init(shared_at(&s_done), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const ExpertPlan plan = plan_experts<kTileThreads>(a, [&](const auto &) { return ta.columns; }, s_bits, s_sum, s_place, s_list, s_first, s_passes, s_token, !DOWN && blockIdx.x == 0);
@@ -177,8 +190,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
     /* a stage has room for a tile's rows; the products read 128 rows all the same, those of no tile for nothing */
     const uint32_t half_bytes = size * kGroup * kSpan, weight_bytes = S::halves * half_bytes, stage_bytes = weight_bytes + S::parts * ta.columns * kSpan;
     const uint32_t stages = min((uint32_t)kMaxRing, (kRing - kRows * kSpan) / stage_bytes);
+    bool fine = true, more = true;                                  /* fine: no wait of this warp has run out; more: it goes on */
+    const uint32_t polls = ta.polls;
     auto for_tiles = [&](auto &&body) {
-        for (uint32_t i = begin; i < end; ++i) {
+        for (uint32_t i = begin; i < end && more; ++i) {
             const uint32_t pass = i / per_pass, g0 = i % per_pass * size;
             int lo = 0, hi = active - 1;                            /* the last expert with no more passes before it */
             while (lo < hi) {
@@ -194,18 +209,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             body(t);
         }
     };
-    bool fine = true;
+    uint32_t issued = 0;                                            /* steps whose weights warp 0 asked for */
     uint32_t stage = 0, phase = 0;                                  /* of this warp's next step; phase: how often the ring went round, mod 2 */
     auto step_on = [&] { if (++stage == stages) { stage = 0; phase ^= 1; } };
 
     if (warp == 0) {
-        /* weights are nobody's output: they are fetched before the kernel in front of this one has ended */
+        /* weights are nobody's output: the ring is filled with them before the kernel in front of this one has ended */
         const uint32_t leader = elect_leader();
         for_tiles([&](const TileAt &t) {
             const uint32_t row = DOWN ? t.expert * a.hidden + t.row : t.expert * 2 * a.inter + t.row, boxes = (t.count + kGroup - 1) / kGroup;
             for (uint32_t s = 0; s < steps; ++s) {
                 const uint32_t bar = shared_at(&s_full[stage]), to = shared_at(smem) + stage * stage_bytes;
-                bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
+                if (DOWN && issued == stages) grid_wait();          /* from here on a wait goes by this kernel's own pace */
+                if (!bar_wait<true>(shared_at(&s_empty[stage]), phase ^ 1, polls)) { fine = more = false; return; }
+                ++issued;
                 bar_arrive_and_expect(leader, bar, boxes * S::halves * kGroup * kSpan);
                 uint32_t from = 0;
 #pragma unroll
@@ -222,13 +239,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
     } else if (warp == 1) {
         const uint32_t leader = elect_leader();
         uint32_t half = 0, round = 0;                               /* of tensor memory */
+        if (DOWN) grid_wait();
         for_tiles([&](const TileAt &t) {
             const uint32_t width = (t.n + 15) / 16 * 16, to = tmem + half * 128;
             const uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (width >> 3) << 17 | (kRows >> 4) << 24;     /* binary32 sums of bf16, K-major */
-            bar_wait(shared_at(&s_free[half]), round ^ 1, fine);
+            if (!bar_wait<true>(shared_at(&s_free[half]), round ^ 1, polls)) { fine = more = false; return; }
             sums_after();
             for (uint32_t s = 0; s < steps; ++s) {
-                bar_wait(shared_at(&s_full[stage]), phase, fine);
+                const bool there = bar_wait<true>(shared_at(&s_full[stage]), phase, polls);
                 sums_after();
                 const uint32_t at = shared_at(smem) + stage * stage_bytes;
                 const unsigned long long rows0 = operand(at), cols0 = operand(at + weight_bytes);
@@ -240,6 +258,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
                     if (S::halves == 2) product(leader, to + 64, rows0 + (half_bytes >> 4) + 2 * k, cols0 + 2 * k, kind, s | k);
                     if (S::parts == 2) product(leader, to, rows0 + 2 * k, cols0 + (ta.columns * kSpan >> 4) + 2 * k, kind, true);
                 }
+                if (!there) { fine = more = false; return; }        /* asked late, beside the products: these were for nothing */
                 tell_when_done(leader, shared_at(&s_empty[stage]));
                 step_on();
             }
@@ -250,12 +269,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
     } else if (warp < 4) {
         /* eight lanes per row, eight rows at a time */
         const uint32_t me = threadIdx.x - 64, r0 = me / 8, piece = me % 8;
-        uint32_t pending = 0, told = 0;                             /* stages filled and not told of; the next one to tell of */
+        uint32_t pending = 0, told = 0, steps_told = 0;             /* stages filled and not told of; the next one to tell of */
         auto tell = [&] {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) bar_arrive(shared_at(&s_full[told]));
             if (++told == stages) told = 0;
+            ++steps_told;
             --pending;
         };
         if (DOWN) grid_wait();
@@ -269,7 +289,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             const uint32_t place = weight_bytes + r0 * kSpan + ((piece ^ (r0 & 7)) * 16);
             for (uint32_t s = 0; s < steps; ++s) {
                 const uint32_t to = shared_at(smem) + stage * stage_bytes + place, off = s * kSpan, size = off + piece * 16 < bytes ? 16u : 0u;
-                bar_wait(shared_at(&s_empty[stage]), phase ^ 1, fine);
+                if (!bar_wait(shared_at(&s_empty[stage]), phase ^ 1, polls)) { fine = more = false; return; }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (r0 + 8 * i >= t.n) break;
@@ -286,6 +306,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
         });
         asm volatile("cp.async.wait_group 0;" ::: "memory");
         while (pending) tell();
+        if (lane == 0) s_told[warp - 2] = steps_told;
     } else {
         /* a thread has a row, its warp the first or the second half of the columns */
         const uint32_t row = (warp % 4) * 32 + lane, which = warp >= 8;
@@ -296,7 +317,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             const uint32_t width = (t.n + 15) / 16 * 8, c0 = which * width, n = t.n > c0 ? min(t.n - c0, width) : 0u;
             const uint32_t from = tmem + half * 128 + ((uint32_t)(warp % 4) << 21) + c0;
             if (!DOWN) weights[lane] = (uint32_t)lane < n ? weight_of(a, s_token[t.first + c0 + lane], (int)t.expert) : 0.0f;
-            bar_wait(shared_at(&s_sums[half]), round, fine);
+            fine = fine && bar_wait(shared_at(&s_sums[half]), round, polls);
             __syncwarp();
             sums_after();
             if ((uint32_t)(warp % 4) * 32 < t.count) {              /* rows of this warp: the same for all its lanes */
@@ -330,14 +351,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
             }
             sums_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(shared_at(&s_free[half]));
+            if (lane == 0 && fine) bar_arrive(shared_at(&s_free[half]));
             half ^= 1;
             if (half == 0) round ^= 1;
         });
     }
     __syncwarp();
     sums_before();
-    __syncthreads();
+    if (__syncthreads_or(!fine)) {
+        /* A wait ran out.  Nothing may be under way when the CTA ends: not the products, nor the weights, whose barriers wait
+           for the gatherers that stopped, too. */
+        if (warp == 0) {
+            for (uint32_t i = issued > stages ? issued - stages : 0u; i < issued; ++i) {
+                const uint32_t bar = shared_at(&s_full[i % stages]);
+                if (lane < kGatherers / 32 && s_told[lane] <= i) bar_arrive(bar);
+                __syncwarp();
+                bar_wait(bar, (i / stages) & 1, kPolls);
+            }
+        } else if (warp == 1) {
+            tell_when_done(elect_leader(), shared_at(&s_done));
+            bar_wait(shared_at(&s_done), 0, kPolls);
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         sums_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(256u));
@@ -349,6 +385,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_expert_tiles(const __grid_c
 /* ------------------------------------------------------------------------ */
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static uint32_t polls_of_a_wait()
+{
+    static const uint32_t n = [] {
+        const char *s = getenv("SIFAR_EXPERTS_POLLS");
+        return s ? (uint32_t)strtoul(s, nullptr, 10) : kPolls;
+    }();
+    return n;
+}
 
 /* The driver's function by its name: the library does not link against the driver. */
 static EncodeTiled encode_tiled()
@@ -398,6 +443,7 @@ cudaError_t launch_expert_tiles(cudaStream_t stream, const ExpertsArgs &a)
     /* columns of a pass: four times an expert's share of the choices, were they spread evenly; more take another pass */
     const uint32_t most = 4 * ((a.tokens * a.top_k + a.experts - 1) / a.experts), need = most < a.tokens ? most : a.tokens;
     t.columns = need <= 16 ? 16 : need <= 32 ? 32 : 64;
+    t.polls = polls_of_a_wait();
     if (cudaError_t e = launch_tiles<false>(stream, t)) return e;
     return launch_tiles<true>(stream, t);
 }
