@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(32 * kTeams * team_warps<DT, ROWS>(), ctas_per
     auto look_up = [&] {
         const uint32_t t = then.lo + then.strip * R::tokens + lane % R::tokens, at = page_of(a.pages, t, in);
         page = -1;
-        if (then.at < end && t < then.hi && at < a.pages.max_pages) page = __ldg(a.pages.table + then.sequence * a.pages.ld_table + at);
+        if (then.at < end && t < then.hi && at < a.pages.max_pages) page = a.pages.table[then.sequence * a.pages.ld_table + at];
     };
     unsigned long long seen = 0;                                  /* 16 bits per stage: its tokens that count */
     look_up();

@@ -31,12 +31,13 @@ __device__ __forceinline__ long long place_offset(const Pages &p, int page, uint
     return (long long)((unsigned long long)page * p.stride_page + (unsigned long long)in * p.stride_token);
 }
 
-/* Bytes from the start of the cache to token n of a sequence (its first head), or -1 where the page is not there. */
+/* Bytes from the start of the cache to token n of a sequence (its first head), or -1 where the page is not there.  (A plain load: the
+   kernel in front may have written the table while this one was started, so the table is not constant for this kernel's life.) */
 __device__ __forceinline__ long long token_offset(const Pages &p, const int *row, uint32_t n)
 {
     uint32_t in;
     const uint32_t at = page_of(p, n, in);
-    return at < p.max_pages ? place_offset(p, __ldg(row + at), in) : -1;
+    return at < p.max_pages ? place_offset(p, row[at], in) : -1;
 }
 
 /* ------------------------------------------------------------------------ */

@@ -35,10 +35,11 @@ constexpr int kChunk = 512;                  /* bytes of the weights' rows that 
 /* ------------------------------------------------------------------------ */
 /* loads                                                                     */
 /* ------------------------------------------------------------------------ */
+/* Plain ones: a kernel may have been started while the one in front still wrote what it reads, so nothing is constant for its life. */
 __device__ __forceinline__ uint4 load_once(const char *p)
 {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.L2::256B.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 
@@ -62,7 +63,7 @@ template <bool VEC> struct Weights {
             v[i] = make_uint4(0u, 0u, 0u, 0u);
             if (p && at + i * kBlock < bytes + sh && (i < kAhead || (threadIdx.x & 3) == 0)) {
                 if (VEC) v[i] = load_once(from + i * kBlock);
-                else v[i] = __ldg(reinterpret_cast<const uint4 *>(from + i * kBlock));
+                else v[i] = *reinterpret_cast<const uint4 *>(from + i * kBlock);
             }
         }
         return sh;
@@ -727,7 +728,7 @@ __global__ void __launch_bounds__(kThreads) k_align(const __grid_constant__ Expe
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t c = at / 2 + 4 * i;
-            const auto get = [&](uint32_t col) { return col < a.hidden ? __ldg(reinterpret_cast<const uint32_t *>(x) + col) : 0u; };
+            const auto get = [&](uint32_t col) { return col < a.hidden ? reinterpret_cast<const uint32_t *>(x)[col] : 0u; };
             v[i] = make_uint4(get(c), get(c + 1), get(c + 2), get(c + 3));
         }
         const Parts p = parts_of(v[0]), q = parts_of(v[1]);

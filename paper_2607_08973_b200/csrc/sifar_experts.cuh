@@ -56,9 +56,9 @@ __device__ __forceinline__ uint4 load_shifted(const char *p, uint32_t left)
 {
     const uint32_t sh = (uint32_t)(uintptr_t)p & 15u;
     const uint4 *const q = reinterpret_cast<const uint4 *>(p - sh);
-    const uint4 lo = __ldg(q);
+    const uint4 lo = *q;
     uint4 hi = make_uint4(0u, 0u, 0u, 0u);
-    if (sh && left > 16u - sh) hi = __ldg(q + 1);
+    if (sh && left > 16u - sh) hi = q[1];
     return shifted(lo, hi, sh, (int)left);
 }
 

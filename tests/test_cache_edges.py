@@ -43,3 +43,40 @@ def test_padding_among_tokens_that_follow_at_once(dtype, interleaved):
     some = call(torch.where(real, at, -1).to(torch.int32))
     for whole, part, fill in zip(every, some, (5.0, 7.0, 7.0)):
         assert torch.equal(part[real], whole[real]) and bool((part[~real] == fill).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype,dim", [(sf.BF16, 64), (sf.BF16, 63), (sf.F32, 64)])
+def test_a_page_table_that_the_kernel_in_front_wrote(dtype, dim):
+    """Another table for every call, written on the stream just before it: append writes, and attention reads, the pages that it names then."""
+    dt, S, page, pages = DT[dtype], 4, 16, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    p = lambda t: t.data_ptr()  # noqa: E731
+    table, at = torch.zeros(S, 2, dtype=torch.int32, device="cuda"), torch.full((S,), 16, dtype=torch.int32, device="cuda")
+    n = at + 1
+    q, out = torch.randn(S, dim, generator=g, device="cuda").to(dt), torch.empty(S, dim, dtype=dt, device="cuda")
+    k, v = (torch.zeros(pages, page, 1, dim, dtype=dt, device="cuda") for _ in range(2))
+    v[:] = torch.arange(pages, device="cuda").to(dt)[:, None, None, None]
+    cache = dict(k_cache=p(k), v_cache=p(v), page_table=p(table), pages=pages, page_size=page, max_pages=2, sequences=S, kv_heads=1, head_dim=dim, dtype=dtype)
+    a = sf.make_attention(q=p(q), out=p(out), lengths=p(n), heads=1, scale=0.0, **cache)
+    ws = torch.empty(sf.sifar_decode_attention_workspace(a), dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = p(ws), ws.numel()
+    new = torch.full((S, dim), 2.0, dtype=dt, device="cuda")
+    add = sf.make_append(k=p(new), v=p(new), position=p(at), tokens=S, heads=0, rotary_dim=0, **cache)
+    tables = [torch.randperm(pages, generator=g, device="cuda").to(torch.int32)[: 2 * S].view(S, 2).contiguous() for _ in range(40)]
+    stream = torch.cuda.current_stream().cuda_stream
+    outs, kept = [], []
+    for t in tables:
+        v[:] = torch.arange(pages, device="cuda").to(dt)[:, None, None, None]
+        torch.add(t, 0, out=table)
+        sf.sifar_cache_append(add, stream)
+        sf.sifar_decode_attention(a, stream)
+        outs.append(out.clone())
+        kept.append(v[t[:, 1].long(), 0, 0].clone())
+    torch.cuda.synchronize()
+    for t, got, last in zip(tables, outs, kept):
+        assert bool((last == 2.0).all())
+        # the mean of 16 tokens of the first page and the new one: whole numbers below 64, the quotient a few roundings of binary32
+        want = (16.0 * t[:, 0].double().cpu() + 2.0) / 17.0
+        bound = {sf.BF16: 2.0 ** -8, sf.F32: 2.0 ** -24}[dtype] * want + 2.0 ** -16 * 64
+        assert bool(((got.double().cpu() - want[:, None]).abs() <= bound[:, None]).all())

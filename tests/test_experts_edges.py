@@ -62,3 +62,32 @@ def test_a_wait_that_runs_out_gives_nan_and_nothing_wrong(polls, tmp_path):
             assert np.array_equal(out[~nan], want[~nan])
             short += int(nan.any())
     assert short == 5 * len(_SHAPES) if polls == 0 else True
+
+
+@gpu
+@pytest.mark.parametrize("dtype,T,H,pad", [(sf.BF16, 4, 256, 0), (sf.BF16, 4, 250, 3), (sf.BF16, 40, 264, 3), (sf.BF16, 40, 250, 0), (sf.F32, 4, 255, 1), (sf.F32, 40, 256, 0), (sf.F32, 40, 255, 1)])
+def test_what_the_kernels_in_front_write_is_seen(dtype, T, H, pad):
+    """Tokens and weights that the kernels just before the call left, while the call's first kernel was started already."""
+    m = Moe(T, H, 64, 6, 2, dtype=dtype, pad=pad)
+    dt = m.x.dtype
+    x0, gu0, dn0 = m.xd.clone(), m.gud.clone(), m.dnd.clone()
+    want = [m.run()]
+    m.xd.copy_(x0 * 2), m.gud.copy_(gu0 * 0.5), m.dnd.copy_(dn0 * -1)        # powers of two: the same products, the other sign
+    torch.cuda.synchronize()
+    want.append(m.run())
+    assert torch.equal(want[0], -want[1])
+    # residual and partials of the norm in front, whose h is the tokens
+    zero, res = torch.zeros(T, H + pad, dtype=dt, device="cuda"), [x0 * s for s in (1, 2)]
+    stream = torch.cuda.current_stream().cuda_stream
+    outs = []
+    for i in range(60):
+        n = i % 2
+        m.gud.copy_(gu0).mul_((1.0, 0.5)[n])
+        m.dnd.copy_(dn0).mul_((1.0, -1.0)[n])
+        a = sf.make_block_norm([zero.data_ptr()], rows=T, cols=H, dtype=dtype, residual=res[n].data_ptr(), h=m.xd.data_ptr(), ld_x=H + pad, ld_residual=H + pad, ld_h=H + pad)
+        sf.sifar_block_norm(a, stream)
+        sf.sifar_experts(m.args, stream)
+        outs.append(m.out[:, :H].clone())
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        assert torch.equal(out, want[i % 2])
