@@ -177,20 +177,33 @@ template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], f
 /* A lane's accumulators for 16 rows x 8 G tokens. */
 template <int DT, int G> struct Few {
     float c[G][4] = {}, less[DT == SIFAR_F32 ? G : 1][4] = {};
-    __device__ __forceinline__ void store(float *red)              /* red: 16 rows x 8 G tokens */
+    __device__ __forceinline__ void join()                         /* c: all of it */
     {
-        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
         if constexpr (DT == SIFAR_F32) {
 #pragma unroll
             for (int q = 0; q < G; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) c[q][i] += less[q][i];
         }
+    }
+    static __device__ __forceinline__ void store(float *red, const float (&v)[G][4])   /* red: 16 rows x 8 G tokens */
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, j = lane & 3;
 #pragma unroll
         for (int q = 0; q < G; ++q) {
-            *reinterpret_cast<float2 *>(red + g * 8 * G + q * 8 + 2 * j) = make_float2(c[q][0], c[q][1]);
-            *reinterpret_cast<float2 *>(red + (g + 8) * 8 * G + q * 8 + 2 * j) = make_float2(c[q][2], c[q][3]);
+            *reinterpret_cast<float2 *>(red + g * 8 * G + q * 8 + 2 * j) = make_float2(v[q][0], v[q][1]);
+            *reinterpret_cast<float2 *>(red + (g + 8) * 8 * G + q * 8 + 2 * j) = make_float2(v[q][2], v[q][3]);
         }
+    }
+    /* Adds the columns whose bit is set. */
+    __device__ __forceinline__ void add_to(float (&sum)[G][4], uint32_t columns)
+    {
+        columns >>= 2 * (threadIdx.x & 3);
+        join();
+#pragma unroll
+        for (int q = 0; q < G; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[q][i] += columns >> (8 * q + (i & 1)) & 1u ? c[q][i] : 0.0f;
     }
 };
 
@@ -312,7 +325,8 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
                 }
             }
         }
-        acc.store(s_red[parity][warp]);
+        acc.join();
+        acc.store(s_red[parity][warp], acc.c);
         __syncthreads();                                            /* the other parity's sums are read by now */
         /* a warp has a pair of each tile, its lanes the tokens */
         const uint32_t t = lane;
@@ -346,7 +360,8 @@ __device__ __forceinline__ void store_cluster(float *local, uint32_t rank, float
 /*
  * A CTA has an equal share of the output's columns, 16 at a time, and goes over all experts that have tokens; its warps take
  * the 256-byte pieces of the experts' rows in turn.  Where there are few columns, the CTAs of a cluster share them and take turns, and
- * the first one adds their sums up.  Tokens that did not choose an expert have zeros there and are not read.
+ * the first one adds their sums up.  Tokens that did not choose an expert have zeros there and are not read; an item's products are added
+ * to the tokens that chose its expert alone, since zero times what its weights may hold need not be zero.
  * HALF (bf16, up to 4 tokens): both parts of the products' values are columns of one instruction.
  */
 template <int DT, int G, bool VEC, bool HALF>
@@ -413,10 +428,11 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
         copies_commit();
     };
     for (uint32_t col = begin; col < end; col += 16) {
-        Few<DT, G> acc;
+        float sum[G][4] = {};
         int half = 0;
         if (kStaged) fetch(warp0, 0);
         for (uint32_t item = warp0; item < items; item += turn, half ^= 1) {
+            Few<DT, G> acc;
             const Weights<VEC> now = next;
             const uint32_t which = item / pieces, at = item % pieces * (kAhead * kBlock) + j * 16, tokens = s_tokens[which];
             const bool more = item + turn < items;
@@ -434,6 +450,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                     const int left = (int)bytes - (int)(at + i * kBlock);
                     multiply_block<1>(acc.c, now.of_a(i, left), now.of_b(i, left), {x[i]});
                 }
+                acc.add_to(sum, tokens | tokens << 4);
             } else {
                 load(next, more ? col : col + 16, more ? item + turn : warp0);
                 if (kStaged) fetch(item + turn, half ^ 1);
@@ -480,11 +497,12 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid
                         }
                     }
                 }
+                acc.add_to(sum, tokens);
                 __syncwarp();
             }
         }
         if (kStaged) copies_wait<0>();
-        acc.store(s_red[warp]);
+        Few<DT, G>::store(s_red[warp], sum);
         __syncthreads();
         auto out = [&](uint32_t t, uint32_t r, float v) { reinterpret_cast<typename Elem<DT>::type *>(a.out + t * a.ld_out)[col + r] = narrow<DT>(v); };
         for (uint32_t i = threadIdx.x; i < 16 * a.tokens; i += kThreads) {

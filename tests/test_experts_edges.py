@@ -8,6 +8,9 @@ import pytest
 import torch
 
 from paper_2607_08973_b200 import binding as sf
+from tests import decode_ref as dr
+from tests import ops_ref as ref
+from tests.decode_ref import DT
 from tests.test_experts import Moe
 
 gpu = pytest.mark.gpu
@@ -91,3 +94,27 @@ def test_what_the_kernels_in_front_write_is_seen(dtype, T, H, pad):
     torch.cuda.synchronize()
     for i, out in enumerate(outs):
         assert torch.equal(out, want[i % 2])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan"), 3.4e38])
+@pytest.mark.parametrize("T,H,I", [(1, 64, 48), (2, 64, 48), (4, 40, 700), (5, 64, 48), (8, 130, 75), (12, 130, 75), (12, 64, 48), (20, 130, 75), (40, 64, 48), (40, 130, 75)])
+def test_weights_that_are_not_finite_reach_the_tokens_that_chose_them_alone(dtype, bad, T, H, I):  # noqa: E741
+    """Expert 2 is token 0's alone; one element of its down weights, then of its gate weights, is not finite (or, 3.4e38, rounds to no finite
+    bf16 value).  All other tokens, and of token 0 what the element does not reach, are the clean weights' sums."""
+    E, col = 5, 3
+    choice = [[2, 0, 7]] + [[0, 1, 9], [3, 4, -1], [-1, 5, 6], [4, 1, 3]] * T
+    m = Moe(T, H, I, E, 3, dtype=dtype, choice=choice[:T], seed=T + H)
+    want, err = dr.experts(ref.f64(m.x), m.idx, ref.f64(m.w), ref.f64(m.gu), ref.f64(m.dn), 0, False, dtype)
+    dt = DT[dtype]
+    keep = m.dnd.clone()
+    m.dnd.view(E, H, I)[2, col, I - 1] = bad
+    got = m.run()
+    assert ref.outside(got[1:], want[1:], err[1:], dt) == ""
+    others = [c for c in range(H) if c != col]
+    assert ref.outside(got[:1, others], want[:1, others], err[:1, others], dt) == ""
+    assert bad == 3.4e38 or not bool(got[0, col].isfinite())
+    m.dnd.copy_(keep)
+    m.gud.view(E, 2 * I, H)[2, I // 2, 1] = bad
+    assert ref.outside(m.run()[1:], want[1:], err[1:], dt) == ""
