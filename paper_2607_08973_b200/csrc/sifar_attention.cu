@@ -51,11 +51,12 @@ struct AttentionArgs {
 /* Floats of a partial: rows x dim_pad values, rows maxima, rows sums; the next one starts on 16 bytes again. */
 __host__ __device__ __forceinline__ size_t partial_floats(uint32_t rows, int dim_pad) { return ((size_t)rows * (dim_pad + 2) + 3) / 4 * 4; }
 
-/* First visible token and the one behind the last. */
+/* First visible token and the one behind the last.  The window ends at the sequence's length, also where the table does not reach it. */
 __device__ __forceinline__ void visible(const AttentionArgs &a, uint32_t s, uint32_t &lo, uint32_t &hi)
 {
-    hi = (uint32_t)min(max(a.lengths[s], 0), (int)a.limit);
-    lo = a.window && hi > a.window ? hi - a.window : 0u;
+    const uint32_t n = (uint32_t)max(a.lengths[s], 0);
+    hi = min(n, a.limit);
+    lo = a.window && n > a.window ? min(n - a.window, hi) : 0u;
 }
 template <int TOKENS> __device__ __forceinline__ uint32_t strips_of(uint32_t lo, uint32_t hi)
 {

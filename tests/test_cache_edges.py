@@ -3,8 +3,10 @@ import pytest
 import torch
 
 from paper_2607_08973_b200 import binding as sf
+from tests import decode_ref as dr
+from tests import ops_ref as ref
 from tests import test_cache_append as append
-from tests.decode_ref import DT
+from tests.decode_ref import DT, Cache
 
 gpu = pytest.mark.gpu
 
@@ -80,3 +82,27 @@ def test_a_page_table_that_the_kernel_in_front_wrote(dtype, dim):
         want = (16.0 * t[:, 0].double().cpu() + 2.0) / 17.0
         bound = {sf.BF16: 2.0 ** -8, sf.F32: 2.0 ** -24}[dtype] * want + 2.0 ** -16 * 64
         assert bool(((got.double().cpu() - want[:, None]).abs() <= bound[:, None]).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("window", [1, 10, 36, 37, 64, 100, 2 ** 31 - 1])
+def test_a_window_of_a_length_that_the_table_does_not_reach(dtype, window):
+    """The window is that of the length: what the table does not hold is masked, and nothing before the window takes its place."""
+    told = [101, 64, 65, 1000, 2 ** 31 - 1, 73, 0, -5]
+    dt, heads, dim = DT[dtype], 4, 64
+    c = Cache([64] * len(told), page=16, kv=2, dim=dim, dtype=dtype)
+    q = torch.randn(len(told), heads * dim, generator=torch.Generator().manual_seed(1), dtype=torch.float64).to(dt).cuda()
+    out, lse = torch.empty_like(q), torch.empty(len(told), heads, device="cuda")
+    n = torch.tensor(told, dtype=torch.int32, device="cuda")
+    a = sf.make_attention(q=q.data_ptr(), out=out.data_ptr(), lse=lse.data_ptr(), lengths=n.data_ptr(), heads=heads, window=window, **c.fields())
+    ws = torch.empty(sf.sifar_decode_attention_workspace(a), dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+    sf.sifar_decode_attention(a)
+    torch.cuda.synchronize()
+    for s, length in enumerate(told):
+        seen = slice(max(0, length - window), max(0, min(length, 64)))
+        want, wl, err, el = dr.attention(ref.f64(q[s]).reshape(heads, dim), ref.f64(c.keys[s][seen]), ref.f64(c.values[s][seen]), a.scale, dtype)
+        assert ref.outside(out[s].reshape(heads, dim), want, err, dt) == "", length
+        got = lse[s].cpu().double()
+        assert bool(((got == wl) | ((got - wl).abs() <= el)).all()), length
