@@ -685,7 +685,8 @@ __global__ void __launch_bounds__(32 * kTeams * team_warps<DT, ROWS>(), ctas_per
                 for (uint32_t c = 0; c < kTurns; ++c) {
                     const uint32_t d = (lane % kPieces + 32 * c) * 4;
                     if (all) {
-                        const float x[4] = {v[k][c].x * f[k], v[k][c].y * f[k], v[k][c].z * f[k], v[k][c].w * f[k]};
+                        float x[4] = {v[k][c].x * f[k], v[k][c].y * f[k], v[k][c].z * f[k], v[k][c].w * f[k]};
+                        if (f[k] == 0.0f) x[0] = x[1] = x[2] = x[3] = 0.0f;     /* nothing, whatever zero times the values left */
                         store_out<DT>(out + r * a.dim, x, d, a.dim, a.out_vec);
                     } else {
                         *reinterpret_cast<float4 *>(part + r * DP + d) = v[k][c];

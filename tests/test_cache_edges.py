@@ -106,3 +106,57 @@ def test_a_window_of_a_length_that_the_table_does_not_reach(dtype, window):
         assert ref.outside(out[s].reshape(heads, dim), want, err, dt) == "", length
         got = lse[s].cpu().double()
         assert bool(((got == wl) | ((got - wl).abs() <= el)).all()), length
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("dim", [64, 256, 72])
+@pytest.mark.parametrize("n", [3, 70, 3000])
+def test_heads_without_a_score_give_zero_whatever_the_values_hold(dtype, dim, n):
+    """Scores of -infinity alone, over one strip, several, several teams; values of NaN and infinity under them.  The second key head has a score."""
+    dt = DT[dtype]
+    c = Cache([n, n], page=16, kv=2, dim=dim, dtype=dtype)
+    t = torch.arange(n)
+    for s, fill in enumerate((float("nan"), float("inf"))):
+        page, slot = c.table[s].long()[t // 16].cuda(), (t % 16).cuda()
+        c.k[page, slot, 0, 0] = float("-inf")
+        c.v[page, slot, 0] = fill
+    q = (torch.rand(2, 4 * dim, device="cuda") + 0.5).to(dt)
+    out, lse = torch.empty_like(q), torch.empty(2, 4, device="cuda")
+    lengths = torch.tensor([n, n], dtype=torch.int32, device="cuda")
+    a = sf.make_attention(q=q.data_ptr(), out=out.data_ptr(), lse=lse.data_ptr(), lengths=lengths.data_ptr(), heads=4, **c.fields())
+    ws = torch.empty(sf.sifar_decode_attention_workspace(a), dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+    sf.sifar_decode_attention(a)
+    torch.cuda.synchronize()
+    out = out.reshape(2, 4, dim)
+    assert bool((out[:, :2] == 0).all()) and bool((lse[:, :2] == float("-inf")).all())
+    for s in range(2):
+        want, _, err, _ = dr.attention(ref.f64(q[s]).reshape(4, dim)[2:], ref.f64(c.keys[s][:, 1:]), ref.f64(c.values[s][:, 1:]), a.scale, dtype)
+        assert ref.outside(out[s, 2:], want, err, dt) == ""
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [sf.BF16, sf.F32])
+@pytest.mark.parametrize("n", [20, 3000])
+def test_a_value_that_is_not_finite_stays_in_its_column(dtype, n):
+    """NaN, and infinity under a weight that is not 0, reach their column of the heads that read them; binary32 keeps the infinity."""
+    dt, dim = DT[dtype], 64
+    c = Cache([n], page=16, kv=2, dim=dim, dtype=dtype)
+    where = lambda t: (int(c.table[0, t // 16]), t % 16)  # noqa: E731
+    c.v[(*where(7), 0, 5)], c.v[(*where(n - 1), 0, 9)] = float("inf"), float("nan")
+    q = torch.randn(1, 4 * dim, generator=torch.Generator().manual_seed(2), dtype=torch.float64).to(dt).cuda()
+    out = torch.empty_like(q)
+    lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+    a = sf.make_attention(q=q.data_ptr(), out=out.data_ptr(), lengths=lengths.data_ptr(), heads=4, **c.fields())
+    ws = torch.empty(sf.sifar_decode_attention_workspace(a), dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+    sf.sifar_decode_attention(a)
+    torch.cuda.synchronize()
+    out = out.reshape(4, dim)
+    want, _, err, _ = dr.attention(ref.f64(q).reshape(4, dim), ref.f64(c.keys[0]), ref.f64(c.values[0]), a.scale, dtype)
+    keep = [d for d in range(dim) if d not in (5, 9)]
+    assert ref.outside(out[:, keep], want[:, keep], err[:, keep], dt) == "" and ref.outside(out[2:], want[2:], err[2:], dt) == ""
+    assert bool(out[:2, 9].isnan().all()) and not bool(out[:2, 5].isfinite().any())
+    if dtype == sf.F32:
+        assert bool((out[:2, 5] == float("inf")).all())
