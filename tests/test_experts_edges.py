@@ -118,3 +118,29 @@ def test_weights_that_are_not_finite_reach_the_tokens_that_chose_them_alone(dtyp
     m.dnd.copy_(keep)
     m.gud.view(E, 2 * I, H)[2, I // 2, 1] = bad
     assert ref.outside(m.run()[1:], want[1:], err[1:], dt) == ""
+
+
+def _sum_error(n: int) -> float:
+    """Error of a sum of n binary32 products, relative to the sum of their sizes.  An instruction adds 16 products and the sum so far, each cut off
+    by at most 2 U of the largest; after at most 8 instructions what they have is added to the row's sum, rounded; a few more adds at the
+    end, and the products' own parts (2^-25)."""
+    return (34 * min(8, -(-n // 16)) + -(-n // 128) + 16) * ref.U
+
+
+@gpu
+@pytest.mark.parametrize("T,H,I", [(40, 32768, 8), (40, 8, 32768), (256, 8, 16384), (33, 32767, 9), (40, 9, 32767), (4, 5700, 8), (4, 8, 32768), (31, 9, 32767), (16, 1000, 2000)])
+def test_binary32_sums_of_long_rows(T, H, I):  # noqa: E741
+    """All products are positive, so that what each add cuts off adds up; the gate is one product, the weight 1."""
+    g = torch.Generator().manual_seed(H)
+    m = Moe(T, H, I, 1, 1, dtype=sf.F32, choice=[[0]] * T, weights=[[1.0]] * T)
+    draw = lambda *s: (torch.rand(*s, generator=g, dtype=torch.float64) + 0.5).float()  # noqa: E731
+    m.x, m.gu, m.dn = draw(T, H), draw(1, 2 * I, H), draw(1, H, I)
+    m.gu[:, :I, 1:] = 0.0
+    m.xd.copy_(m.x), m.gud.copy_(m.gu.reshape(-1, H)), m.dnd.copy_(m.dn.reshape(-1, I))
+    x, gu, dn = ref.f64(m.x), ref.f64(m.gu)[0], ref.f64(m.dn)[0]
+    gate, up = x @ gu[:I].T, x @ gu[I:].T
+    a = gate / (1.0 + torch.exp(-gate)) * up
+    # the gate's one product (1.2 times through the activation, which is a few steps off itself), the sum
+    ea = a * (1.2 * _sum_error(1) + 24 * ref.U + _sum_error(H))
+    want = a @ dn.T
+    assert ref.outside(m.run(), want, ea @ dn.T + _sum_error(I) * want, torch.float32) == ""
