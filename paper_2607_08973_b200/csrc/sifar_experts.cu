@@ -22,6 +22,7 @@
  * 28 MB, bound by the starts and by the shuffles that put rows together.
  */
 #include "sifar_experts.cuh"
+#include "sifar_experts_shape.cuh"
 
 namespace sifar {
 
@@ -222,15 +223,13 @@ __device__ __forceinline__ int list_few(const ExpertsArgs &a, uint16_t *list, ui
                          [&](int at, uint32_t e) { list[at] = (uint16_t)e; tokens[at] = bits[e]; });
 }
 
-constexpr int kFewCtas(int G) { return G <= 2 ? 2 : 1; }             /* per SM */
-
 /*
  * All experts' rows lie in a row and every CTA has an equal share of it, 8 gate rows and the 8 up rows that go with them at a
  * time, so a product's gate and up lie 8 rows apart.  The warps take the rows' 256-byte pieces in turn, in groups with tiles of their
  * own where rows have fewer than eight; the next pieces are under way while these are multiplied, across tiles too.
  */
 template <int DT, int G, bool VEC, bool XVEC>
-__global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_constant__ ExpertsArgs a)
+__global__ void __launch_bounds__(kThreads, kFewCtas<G>) k_up_few(const __grid_constant__ ExpertsArgs a)
 {
     constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
     extern __shared__ __align__(128) char smem[];                   /* tokens x x_row */
@@ -238,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_up_few(const __grid_c
     __shared__ uint16_t s_list[SIFAR_ROUTE_MAX_EXPERTS];
     __shared__ int s_scratch[kWarps];
     __shared__ __align__(16) float s_red[2][kWarps][16 * 8 * G];
+    static_assert(sizeof s_bits + sizeof s_tokens + sizeof s_list + sizeof s_scratch + sizeof s_red <= kFewStatic<G>, "what few_ctas() counts");
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, j = lane & 3;
     grid_wait();
     grid_let_next_in();
@@ -370,7 +370,7 @@ __device__ __forceinline__ void store_cluster(float *local, uint32_t rank, float
  * HALF (bf16, up to 4 tokens): both parts of the products' values are columns of one instruction.
  */
 template <int DT, int G, bool VEC, bool HALF>
-__global__ void __launch_bounds__(kThreads, kFewCtas(G)) k_down_few(const __grid_constant__ ExpertsArgs a)
+__global__ void __launch_bounds__(kThreads, kFewCtas<G>) k_down_few(const __grid_constant__ ExpertsArgs a)
 {
     constexpr int es = DT == SIFAR_BF16 ? 2 : 4;
     __shared__ uint32_t s_bits[SIFAR_ROUTE_MAX_EXPERTS], s_tokens[SIFAR_ROUTE_MAX_EXPERTS];
@@ -810,9 +810,6 @@ __global__ void __launch_bounds__(kThreads) k_gather(const __grid_constant__ Exp
 /* ------------------------------------------------------------------------ */
 struct ExpertsPlan { bool few; uint32_t x_row, h_row; size_t h_bytes, y_bytes, rows_bytes, bytes; };
 
-constexpr size_t kFewShared = 92 * 1024;     /* the tokens' rows in shared memory: two CTAs of 8 warps per SM */
-constexpr size_t kFewMostShared = 180 * 1024;  /* ... one */
-
 static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan &p)
 {
     if (!g) { set_error("%s: no argument block", fn); return SIFAR_ERR_INVALID; }
@@ -861,13 +858,13 @@ template <int DT, int G>
 static cudaError_t launch_few(const ExpertsPlan &p, bool gu_vec, bool dn_vec, bool x_vec, cudaStream_t stream, ExpertsArgs a)
 {
     const size_t shared = (a.tokens + 3) / 4 * 4 * (size_t)p.x_row, staged = (size_t)kWarps * 2 * Staged<DT, G>::bytes;
-    const unsigned ctas = kSms * (shared <= kFewShared ? kFewCtas(G) : 1);
+    const unsigned ctas = kSms * few_ctas<G>(shared);
     cudaError_t e = !gu_vec ? launch_shared(k_up_few<DT, G, false, false>, dim3(ctas), shared, stream, a)
                     : x_vec ? launch_shared(k_up_few<DT, G, true, true>, dim3(ctas), shared, stream, a) : launch_shared(k_up_few<DT, G, true, false>, dim3(ctas), shared, stream, a);
     if (e) return e;
     /* Blocks of up to 16 columns.  Where they would leave half of the CTAs without work, clusters share them, each warp two items at
        least: of 8 columns per block only half of a warp's loads are under way.  Between that and all CTAs, blocks of 8 to 16. */
-    const unsigned most = kSms * kFewCtas(G), full = (a.hidden + 15) / 16;
+    const unsigned most = kSms * kFewCtas<G>, full = (a.hidden + 15) / 16;
     const size_t pieces = ((size_t)a.inter * elem_size(DT) + kAhead * kBlock - 1) / (kAhead * kBlock), choices = (size_t)a.tokens * a.top_k;
     const size_t items = (choices < a.experts ? choices : a.experts) * pieces;
     a.split = 1;
