@@ -3,8 +3,9 @@
  *
  * A CTA per token: cosines and sines of the token's angles once, in shared memory, for all its heads.  A thread has the same
  * place in every head that it takes; its first loads, into shared memory, are under way while it is looked up where the token
- * belongs and the angles are computed.  Bound by memory: every element is read and written once.  8192 tokens of 32 + 8 + 8 bf16
- * heads of 128 take 38 us, 5.3 TB/s (without the loads ahead, a thread's place worked out for each head: 46); one token 3.3 us, the launch.
+ * belongs and the angles are computed.  Bound by memory, every element is read and written once, and by instructions.  8192 tokens of
+ * 32 + 8 + 8 bf16 heads of 128 take 38 us, 5.3 TB/s, 79 % of the issue slots (without the loads ahead, a thread's place worked out for
+ * each head: 46); one token 3.2 us, the launch.
  */
 #include "sifar_cache.cuh"
 #include "sifar_norm_shape.cuh"

@@ -17,7 +17,8 @@
  *
  * Bound by the memory where there is enough of it: two users with 131072 tokens of 8 x 128 171 us, 6.3 TB/s; 64 users of up to
  * 8192 tokens 46 us, 5.0 TB/s, of which about 10 are the start, the uneven ends and the second kernel; one user with 2000 tokens
- * 10.9 us, no more than those.  binary32 is bound by its instructions (37 users of up to 1777 tokens, heads of 80: 19.5 us, 1.4 TB/s).
+ * 11.0 us, no more than those.  binary32 is bound by latencies (37 users of up to 1777 tokens, heads of 80: 19.4 us, 1.4 TB/s): the rings leave an
+ * SM one CTA of four warps, whose schedulers issue in 26 % of the cycles.
  */
 #include "sifar_cache.cuh"
 #include "sifar_norm_shape.cuh"

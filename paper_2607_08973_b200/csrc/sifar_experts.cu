@@ -15,11 +15,11 @@
  *
  * bf16: what goes into the second product is kept as two bf16 values, the rounded one and what it leaves (16 bits).  binary32 values are
  * three bf16 ones, six instructions for one: as fused multiply-adds the same work was bound by loads from shared memory (83 tokens,
- * 8 experts of 625 x 1216: 239 us, 119 now; 31 tokens, 64 experts: 199, 102).
+ * 8 experts of 625 x 1216: 239 us, 132 now; 31 tokens, 64 experts of 1000 x 512: 199, 104).
  *
- * One bf16 token with 8 of 128 experts of 768 x 4096 takes 34 us, 4.5 TB/s (151 MB): two starts of 3 to 4 us each, in which the lists are made and
- * the first weights come, the rest at 6 TB/s.  13 binary32 tokens, 7 experts of 333 x 1001 whose rows start anywhere: 33 us for
- * 28 MB, bound by the starts and by the shuffles that put rows together.
+ * One bf16 token with 8 of 128 experts of 768 x 4096 takes 32.6 us, 4.6 TB/s (151 MB): two starts, in which the lists are made and
+ * the first weights come; the second kernel's CTAs find room when the first one's end.  13 binary32 tokens, 7 experts of 333 x 1001 whose rows
+ * start anywhere: 33.6 us for 28 MB, bound by the starts and by instructions, shuffles that put rows together among them.
  */
 #include "sifar_experts.cuh"
 #include "sifar_experts_shape.cuh"
@@ -157,8 +157,8 @@ template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], c
     for (int q = 0; q < N; ++q) multiply(c[q], a.z, b.z, a.w, b.w, x[q].z, x[q].w);
 }
 /* The instructions cut their sums off, so the large products have sums of their own, and both kinds are taken over by rounded adds after
-   at most eight blocks: one row in one sum is off by 2.0e-5 of the largest value at 16384 columns, so by 5e-7, a plain binary32 product
-   by 1e-6 (83 tokens, 8 experts of 625 x 1216: 3.1e-6 and 4.0e-7, for 132 us in place of 127). */
+   at most eight blocks (40 tokens of 16384 columns: off by 6.6e-7 of the largest value, with a row in one sum 4.0e-5, a plain binary32
+   product 9.9e-7; 83 tokens, 8 experts of 625 x 1216: 4.0e-7, 3.1e-6, for 132 us in place of 127). */
 template <int N> __device__ __forceinline__ void multiply_block(float (*c)[4], float (*less)[4], const Parts &a, const Parts &b, const Parts (&x)[N])
 {
     const auto all = [&](float (*to)[4], const uint2 &a0, const uint2 &b0, uint2 Parts::*of) {
@@ -827,9 +827,9 @@ static int plan_experts(const char *fn, const sifar_experts_args *g, ExpertsPlan
     p.x_row = (uint32_t)((g->hidden * es + 127) / 128 * 128 + 64);
     const bool tiles = g->dtype == SIFAR_BF16 && g->hidden % 8 == 0 && g->inter % 8 == 0;      /* as far as the sizes go */
     const size_t most = choices < (size_t)g->experts ? choices : (size_t)g->experts;       /* experts that can have tokens */
-    /* Up to 16 tokens every expert may as well take them all as columns (binary32, 12 tokens, 32 experts of 1024 x 512: 54 us, 60 with each
-       expert's own); up to 32 where the experts' own would leave SMs without rows (20 tokens, 8 experts of 173 x 701: 36 us, 53), but
-       not where they don't (31 tokens, 64 experts of 512 x 1000: 199 us, 102; bf16, 1022 x 1000: 177 us, 125). */
+    /* Up to 16 tokens every expert may as well take them all as columns (binary32, 12 tokens, 32 experts of 512 x 1024: 56 us, 62 with each
+       expert's own); up to 32 where the experts' own would leave SMs without rows (20 tokens, 8 experts of 173 x 701: 31 us, 61), but
+       not where they don't (31 tokens, 64 experts of 1000 x 512: 227 us, 104; bf16, 1000 x 1022: 169 us, 141). */
     const bool all_sms = most * ((g->hidden + 127) / 128) >= kSms && most * ((g->inter + 63) / 64) >= kSms;
     const size_t limit = tiles ? kFew : all_sms ? kFewMost / 2 : kFewMost;
     p.few = T <= limit && (T + 3) / 4 * 4 * p.x_row <= (T <= (size_t)kFew ? kFewShared : kFewMostShared);

@@ -10,8 +10,8 @@
  *   warp 1      issues the products
  *   warps 2, 3  gather the tokens' rows (asynchronous 16-byte copies)
  *   warps 4 - 11  take a tile's sums out of tensor memory while the next tile's go into its other half, each half of the columns
- * What bounds it is the memory (64 tokens, 128 experts of 768 x 4096: 235 us, 5.6 TB/s), and with many tokens per expert the
- * steps themselves (256 tokens, 32 experts: 129 us, 3.5 TB/s); the ring keeps up to 160 KB of weights per SM on the way, across tiles.  Warps 0 and 1 go through
+ * What bounds it is the memory (64 tokens that chose 70 experts of 768 x 4096: 236 us, 5.6 TB/s), and with many tokens per expert the
+ * steps themselves (256 tokens on 24 experts: 128 us, 3.6 TB/s); the ring keeps up to 160 KB of weights per SM on the way, across tiles.  Warps 0 and 1 go through
  * their loops as whole warps and one lane issues: what an instruction of these needs is in uniform registers then (as one thread's
  * loop, a product took 150 cycles to issue and a fetch 90).
  *
